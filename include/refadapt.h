@@ -467,6 +467,153 @@ typedef struct {
 
 ra_status refadapt_gemm(const ra_gemm_args* args, void* stream);
 
+/* ------------------------------------------------------------------ layers of gated DiT blocks
+ * Further layers that DiT blocks put around the joint attention: rotary
+ * positions with several axes, norms before and after a branch, and the gated
+ * feed-forward. Each has its backward pass, for training such blocks (the
+ * paper's method itself trains nothing). Rows come in segments as above. All
+ * calls are asynchronous on `stream` and allocate nothing; invalid arguments
+ * return RA_EINVAL before anything is launched.
+ */
+
+/* refadapt_rope_axes — rotary positions with several axes (time, height,
+ * width, ...) on up to two tensors (a block's q and k; their head counts may
+ * differ):
+ *   the columns of a head are cut into n_axes runs of axis_dim[a] columns; pair
+ *   i of run a, columns (2i, 2i + 1) of the run, turns by the angle
+ *   pos[s][r][a] * base^(-2i / axis_dim[a])
+ * Columns past the last run are copied. inverse = 1 turns by the negative
+ * angle: the inverse, and the gradient of the forward turn.
+ *
+ *  pos         device fp32 [n][n_axes] per sample, samples pos_stride_s
+ *              elements apart (0: all samples share the positions). Any finite
+ *              values (negative and fractional ones too); the angle is formed
+ *              in two-float arithmetic, exact to fp32 for |angle| < 2^24.
+ *  axis_dim    even, >= 2, sum <= d; 1 to 4 axes; base > 1.
+ *  d           a multiple of 8, at most 256; n * d / 8 < 2^31.
+ *  t[i].x, .out  bf16 segments of n rows; out may equal x (same strides) but
+ *              must not partially overlap it. */
+typedef struct {
+  ra_seg x, out;
+  int32_t heads, reserved;
+} ra_rope_tensor;
+
+typedef struct {
+  int32_t B, n, d, n_axes;
+  int32_t axis_dim[4];
+  double base;
+  const float* pos;
+  int64_t pos_stride_s;
+  int32_t n_tensors, inverse;
+  ra_rope_tensor t[2];
+} ra_rope_args;
+
+ra_status refadapt_rope_axes(const ra_rope_args* args, void* stream);
+
+/* refadapt_rope_axes_table — the same angles as a table for the QKV epilogue
+ * of refadapt_gemm: table[r][i] = (cos, sin) of pair i at the coordinates
+ * pos[r], fp32, [n][d/2][2] (16-byte aligned); a segment's pos_offset is then
+ * its first row of the table. Pairs past the last run get (1, 0). d a multiple
+ * of 4. axis_dim: host array of n_axes entries. */
+ra_status refadapt_rope_axes_table(float* table, const float* pos, int32_t n, int32_t d, int32_t n_axes,
+                                   const int32_t* axis_dim, double base, void* stream);
+
+typedef enum { RA_NORM_NONE = 0, RA_NORM_LAYER = 1, RA_NORM_RMS = 2 } ra_norm;
+
+/* refadapt_residual_norm — what stands between two branches of a block, in
+ * one pass over the rows: the norm after the branch, its gate, the residual sum
+ * and the norm before the next branch with its modulation:
+ *   h_out = alpha * h + gate[s] * (N_post(y) * post_w)
+ *   x     = N_pre(h_out) * pre_w * (1 + scale[s]) + shift[s]
+ * N_LAYER(v) = (v - mean) / sqrt(var + eps), N_RMS(v) = v / sqrt(mean(v^2) +
+ * eps) over the C features of a row, N_NONE(v) = v; fp32 throughout, x from the
+ * unrounded h_out, one rounding to bf16 per output.
+ *
+ *  h, y         bf16 rows; y NULL: h_out = alpha * h.
+ *  h_out, x     bf16 rows; either may be NULL (not both). Each may equal h or
+ *               y (same strides), in place, but must not partially overlap them.
+ *  gate, scale, shift  fp32 [B][C] (rows gate_stride_s; mod_stride_s for both
+ *               scale and shift); NULL: 1, 0 and 0.
+ *  post_w, pre_w  fp32 [C] or NULL (1).
+ * C a multiple of 8, at most 5120; pointers 16-byte aligned, row strides >= C
+ * and multiples of 8 elements (of 4 for the fp32 vectors). A segment with
+ * gated = 1 is skipped for samples whose mode is RA_MODE_REUSE. B * rows of all
+ * segments below 2^30. */
+typedef struct {
+  const void* h;
+  int64_t h_stride_s, h_stride_r;
+  const void* y;
+  int64_t y_stride_s, y_stride_r;
+  void* h_out;
+  int64_t h_out_stride_s, h_out_stride_r;
+  void* x;
+  int64_t x_stride_s, x_stride_r;
+  const float* gate;
+  int64_t gate_stride_s;
+  const float* scale;
+  const float* shift;
+  int64_t mod_stride_s;
+  const float* post_w;
+  const float* pre_w;
+  int32_t rows;       /* rows per sample, >= 0 */
+  int32_t gated;
+} ra_resnorm_seg;
+
+typedef struct {
+  int32_t B, C, n_seg, post, pre, reserved;  /* post, pre: ra_norm */
+  float eps, alpha;
+  ra_resnorm_seg seg[3];
+  const int32_t* mode;  /* device [B]; required when a segment is gated */
+} ra_resnorm_args;
+
+ra_status refadapt_residual_norm(const ra_resnorm_args* args, void* stream);
+
+/* refadapt_residual_norm_backward — gradients of refadapt_residual_norm for
+ * one segment. From h (the forward call's h_out), y, dx and dh_out (gradients
+ * with respect to x and h_out; one of them may be NULL, taken as zero):
+ *   dh, dy                  bf16 rows, gradients of the forward call's h and y
+ *   dgate, dscale, dshift   fp32 [B][C], contiguous
+ *   dpost_w, dpre_w         fp32 [C], summed over the samples
+ * Any output may be NULL. y may be NULL (then dy, dgate and dpost_w too).
+ * dh may equal dh_out or dx, and dy may equal y, in place. Column sums are fp32
+ * in a fixed order (deterministic).
+ *  workspace   device scratch of
+ *              refadapt_residual_norm_backward_workspace_size(B, rows, C) bytes
+ *              (on the device that is current), 16-byte aligned; calls that
+ *              share it must be stream-ordered. */
+typedef struct {
+  int32_t B, C, rows, post, pre, reserved;
+  float eps, alpha;
+  const void* h;
+  int64_t h_stride_s, h_stride_r;
+  const void* y;
+  int64_t y_stride_s, y_stride_r;
+  const void* dx;
+  int64_t dx_stride_s, dx_stride_r;
+  const void* dh_out;
+  int64_t dh_out_stride_s, dh_out_stride_r;
+  void* dh;
+  int64_t dh_stride_s, dh_stride_r;
+  void* dy;
+  int64_t dy_stride_s, dy_stride_r;
+  const float* gate;
+  int64_t gate_stride_s;
+  const float* scale;
+  int64_t mod_stride_s;
+  const float* post_w;
+  const float* pre_w;
+  float* dgate;
+  float* dscale;
+  float* dshift;
+  float* dpost_w;
+  float* dpre_w;
+  void* workspace;
+  size_t workspace_bytes;
+} ra_resnorm_grad_args;
+
+size_t refadapt_residual_norm_backward_workspace_size(int32_t B, int32_t rows, int32_t C);
+ra_status refadapt_residual_norm_backward(const ra_resnorm_grad_args* args, void* stream);
+
 /* ------------------------------------------------------------------ misc */
 const char* refadapt_status_string(ra_status s);
 const char* refadapt_last_error(void);

@@ -24,8 +24,11 @@ EXPORTED = (
     "refadapt_set_wait_budget_ns", "refadapt_check_error", "refadapt_version",
     "refadapt_selftest_wait_timeout", "refadapt_q_delta_noalloc", "refadapt_rope_table",
     "refadapt_ln_modulate", "refadapt_gemm", "refadapt_q_delta_gate", "refadapt_last_launch",
+    "refadapt_rope_axes", "refadapt_rope_axes_table", "refadapt_residual_norm", "refadapt_residual_norm_backward",
+    "refadapt_residual_norm_backward_workspace_size",
 )
 RA_EPI_STORE, RA_EPI_GELU, RA_EPI_RESID, RA_EPI_QKV = 0, 1, 2, 3
+RA_NORM_NONE, RA_NORM_LAYER, RA_NORM_RMS = 0, 1, 2
 
 
 class RaSeg(ctypes.Structure):
@@ -78,6 +81,42 @@ class RaGemmArgs(ctypes.Structure):
                 ("H", c_int32), ("d", c_int32), ("n_seg", c_int32), ("rope_len", c_int32),
                 ("seg", RaGemmSeg * 3), ("mode", c_void_p), ("rope", c_void_p),
                 ("norm_eps", c_float), ("tile_mode", c_int32), ("err_word", c_void_p)]
+
+
+class RaRopeTensor(ctypes.Structure):
+    _fields_ = [("x", RaSeg), ("out", RaSeg), ("heads", c_int32), ("reserved", c_int32)]
+
+
+class RaRopeArgs(ctypes.Structure):
+    _fields_ = [("B", c_int32), ("n", c_int32), ("d", c_int32), ("n_axes", c_int32), ("axis_dim", c_int32 * 4),
+                ("base", c_double), ("pos", c_void_p), ("pos_stride_s", c_int64), ("n_tensors", c_int32),
+                ("inverse", c_int32), ("t", RaRopeTensor * 2)]
+
+
+def _rows(*names):
+    """A pointer and its sample and row strides, per name."""
+    return [f for n in names for f in ((n, c_void_p), (n + "_stride_s", c_int64), (n + "_stride_r", c_int64))]
+
+
+class RaResnormSeg(ctypes.Structure):
+    _fields_ = _rows("h", "y", "h_out", "x") + [
+        ("gate", c_void_p), ("gate_stride_s", c_int64), ("scale", c_void_p), ("shift", c_void_p),
+        ("mod_stride_s", c_int64), ("post_w", c_void_p), ("pre_w", c_void_p), ("rows", c_int32), ("gated", c_int32)]
+
+
+class RaResnormArgs(ctypes.Structure):
+    _fields_ = [("B", c_int32), ("C", c_int32), ("n_seg", c_int32), ("post", c_int32), ("pre", c_int32),
+                ("reserved", c_int32), ("eps", c_float), ("alpha", c_float), ("seg", RaResnormSeg * 3),
+                ("mode", c_void_p)]
+
+
+class RaResnormGradArgs(ctypes.Structure):
+    _fields_ = [("B", c_int32), ("C", c_int32), ("rows", c_int32), ("post", c_int32), ("pre", c_int32),
+                ("reserved", c_int32), ("eps", c_float), ("alpha", c_float)] + \
+        _rows("h", "y", "dx", "dh_out", "dh", "dy") + [
+        ("gate", c_void_p), ("gate_stride_s", c_int64), ("scale", c_void_p), ("mod_stride_s", c_int64),
+        ("post_w", c_void_p), ("pre_w", c_void_p), ("dgate", c_void_p), ("dscale", c_void_p), ("dshift", c_void_p),
+        ("dpost_w", c_void_p), ("dpre_w", c_void_p), ("workspace", c_void_p), ("workspace_bytes", c_size_t)]
 
 
 class RefAdaptError(RuntimeError):
@@ -146,6 +185,17 @@ def load():
     lib.refadapt_ln_modulate.argtypes = [POINTER(RaLnmodArgs), c_void_p]
     lib.refadapt_gemm.restype = c_int32
     lib.refadapt_gemm.argtypes = [POINTER(RaGemmArgs), c_void_p]
+    lib.refadapt_rope_axes.restype = c_int32
+    lib.refadapt_rope_axes.argtypes = [POINTER(RaRopeArgs), c_void_p]
+    lib.refadapt_rope_axes_table.restype = c_int32
+    lib.refadapt_rope_axes_table.argtypes = [c_void_p, c_void_p, c_int32, c_int32, c_int32, POINTER(c_int32), c_double,
+                                             c_void_p]
+    lib.refadapt_residual_norm.restype = c_int32
+    lib.refadapt_residual_norm.argtypes = [POINTER(RaResnormArgs), c_void_p]
+    lib.refadapt_residual_norm_backward_workspace_size.restype = c_size_t
+    lib.refadapt_residual_norm_backward_workspace_size.argtypes = [c_int32, c_int32, c_int32]
+    lib.refadapt_residual_norm_backward.restype = c_int32
+    lib.refadapt_residual_norm_backward.argtypes = [POINTER(RaResnormGradArgs), c_void_p]
     lib.refadapt_selftest_wait_timeout.restype = c_int32
     lib.refadapt_selftest_wait_timeout.argtypes = [c_void_p, c_uint64, c_void_p]
     _lib = lib

@@ -17,7 +17,10 @@ __all__ = ["seg", "refadapt_joint_attn", "refadapt_mass_partial_len", "refadapt_
            "refadapt_q_delta_workspace_size", "refadapt_q_delta_noalloc", "refadapt_state_size", "refadapt_state_init",
            "refadapt_gate", "refadapt_ref_cache_update", "refadapt_set_wait_budget_ns",
            "refadapt_check_error", "refadapt_version", "refadapt_last_launch", "refadapt_selftest_wait_timeout", "q_delta_workspace", "new_state",
-           "alloc_mass_partial", "refadapt_rope_table", "rope_table", "refadapt_ln_modulate", "refadapt_gemm"]
+           "alloc_mass_partial", "refadapt_rope_table", "rope_table", "refadapt_ln_modulate", "refadapt_gemm",
+           "refadapt_rope_axes", "refadapt_rope_axes_table", "rope_axes_table", "refadapt_residual_norm",
+           "refadapt_residual_norm_backward", "refadapt_residual_norm_backward_workspace_size",
+           "residual_norm_backward_workspace"]
 
 
 def _ptr(t):
@@ -193,3 +196,68 @@ def refadapt_gemm(segs, N, K, epilogue, mode=None, rope=None, H=0, d=0, norm_eps
     return check("refadapt_gemm", _lib.native().gemm(
         segs, int(N), int(K), int(epilogue), mode, rope, int(H), int(d), float(norm_eps), err_word, int(tile_mode),
         _handle(stream)))
+
+
+# --------------------------------------------------------------------------- layers of gated DiT blocks
+def refadapt_rope_axes(tensors, pos, axes, base=10000.0, inverse=False, stream=None):
+    """Rotary positions with several axes. tensors: one or two (x, out) pairs of
+    [B, H, n, d] bf16 (out may be x); pos: [n, len(axes)] or [B, n, len(axes)]
+    fp32 coordinates; axes: columns of a head per axis. inverse: the backward
+    pass (turns by the negative angle)."""
+    return check("refadapt_rope_axes", _lib.native().rope_axes(tensors, pos, axes, float(base), bool(inverse),
+                                                               _handle(stream)))
+
+
+def refadapt_rope_axes_table(table, pos, axes, base=10000.0, stream=None):
+    """Fills table ([n, d/2, 2] fp32) for refadapt_gemm's QKV epilogue from pos ([n, len(axes)] fp32)."""
+    n, pairs = _axes_table_shape(table, pos, axes)
+    dims = (ctypes.c_int32 * len(axes))(*[int(a) for a in axes])
+    return check("refadapt_rope_axes_table", _lib.load().refadapt_rope_axes_table(
+        _ptr(table), _ptr(pos), n, 2 * pairs, len(axes), dims, float(base), _stream(stream)))
+
+
+def _axes_table_shape(table, pos, axes):
+    if pos.dim() != 2 or pos.dtype != torch.float32 or not pos.is_cuda or not pos.is_contiguous() or \
+            pos.shape[1] != len(axes):
+        raise ValueError("pos: expected a contiguous [n, %d] fp32 CUDA tensor, got %s %s %s"
+                         % (len(axes), tuple(pos.shape), pos.dtype, pos.device))
+    if table.dim() != 3 or table.dtype != torch.float32 or not table.is_cuda or not table.is_contiguous() or \
+            table.shape[0] != pos.shape[0] or table.shape[2] != 2:
+        raise ValueError("table: expected a contiguous [%d, d/2, 2] fp32 CUDA tensor, got %s %s %s"
+                         % (pos.shape[0], tuple(table.shape), table.dtype, table.device))
+    return table.shape[0], table.shape[1]
+
+
+def rope_axes_table(pos, d, axes, base=10000.0, stream=None):
+    """[n, d/2, 2] fp32 (cos, sin) table built by refadapt_rope_axes_table."""
+    t = torch.empty((pos.shape[0], int(d) // 2, 2), dtype=torch.float32, device=pos.device)
+    refadapt_rope_axes_table(t, pos, axes, base, stream)
+    return t
+
+
+def refadapt_residual_norm(segs, C, post, pre, eps=1e-6, alpha=1.0, mode=None, stream=None):
+    """h_out = alpha h + gate N_post(y) post_w; x = N_pre(h_out) pre_w (1 + scale) + shift.
+    segs: up to three dicts with h ([B, rows, C] bf16) and, each optional, y,
+    h_out, x (the same shape), gate, scale, shift ([B, C] fp32), post_w, pre_w
+    ([C] fp32), gated; post, pre: RA_NORM_NONE, RA_NORM_LAYER or RA_NORM_RMS."""
+    return check("refadapt_residual_norm", _lib.native().residual_norm(
+        segs, int(C), int(post), int(pre), float(eps), float(alpha), mode, _handle(stream)))
+
+
+def refadapt_residual_norm_backward_workspace_size(B, rows, C) -> int:
+    return int(_lib.load().refadapt_residual_norm_backward_workspace_size(int(B), int(rows), int(C)))
+
+
+def residual_norm_backward_workspace(B, rows, C, device="cuda"):
+    """A workspace for refadapt_residual_norm_backward (reusable across calls)."""
+    return torch.empty(refadapt_residual_norm_backward_workspace_size(B, rows, C), dtype=torch.uint8, device=device)
+
+
+def refadapt_residual_norm_backward(seg, C, post, pre, workspace, eps=1e-6, alpha=1.0, stream=None):
+    """Gradients of refadapt_residual_norm for one segment: a dict with h (the
+    forward call's h_out), y, dx and dh_out (gradients of x and h_out, one may
+    be absent), the forward call's gate, scale, post_w, pre_w, and the outputs
+    wanted: dh, dy ([B, rows, C] bf16), dgate, dscale, dshift ([B, C] fp32),
+    dpost_w, dpre_w ([C] fp32)."""
+    return check("refadapt_residual_norm_backward", _lib.native().residual_norm_backward(
+        seg, int(C), int(post), int(pre), workspace, float(eps), float(alpha), _handle(stream)))

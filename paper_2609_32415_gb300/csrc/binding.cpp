@@ -8,6 +8,7 @@
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <cstdio>
 #include <cstring>
 
 #include "refadapt.h"
@@ -176,6 +177,7 @@ bool truth(PyObject* o) {
 // Interned names of the segments' entries.
 struct Names {
   PyObject *h, *x, *shift, *scale, *gated, *a, *w, *bias, *out, *resid, *gate, *q, *k, *v, *q_norm, *k_norm, *pos_offset;
+  PyObject *y, *h_out, *post_w, *pre_w, *dx, *dh_out, *dh, *dy, *dgate, *dscale, *dshift, *dpost_w, *dpre_w;
 } N;
 
 // Stream argument: None is the calling thread's current stream.
@@ -418,10 +420,217 @@ PyObject* gemm(PyObject*, PyObject* const* g, Py_ssize_t n) {
   });
 }
 
+[[noreturn]] void bad_tensor(PyObject* o, const char* what, const char* want) {
+  PyObject* shape = shape_of(o);
+  PyObject* dtype = PyObject_GetAttrString(o, "dtype");
+  PyObject* device = PyObject_GetAttrString(o, "device");
+  if (dtype && device) PyErr_Format(PyExc_ValueError, "%s: expected %s, got %S %S %S", what, want, shape, dtype, device);
+  Py_DECREF(shape);
+  Py_XDECREF(dtype);
+  Py_XDECREF(device);
+  throw Raised{};
+}
+
+// Rows of a layer call: [B, rows, F] bf16 CUDA, contiguous features; all of one
+// call's rows agree in B and rows, which the first fixes.
+struct RowShape {
+  int64_t B = -1, rows = -1;
+  Rows take(PyObject* o, const char* what, int64_t F) {
+    if (o == Py_None) return Rows{nullptr, 0, 0, 0, 0};
+    const at::Tensor& t = tensor(o);
+    if (t.dim() != 3 || t.scalar_type() != at::kBFloat16 || !t.is_cuda() || t.size(2) != F ||
+        (F > 1 && t.stride(2) != 1) || (B >= 0 && (t.size(0) != B || t.size(1) != rows))) {
+      char want[160];
+      if (B >= 0)
+        snprintf(want, sizeof(want), "a [%lld, %lld, %lld] bf16 CUDA tensor with contiguous last axis", (long long)B,
+                 (long long)rows, (long long)F);
+      else
+        snprintf(want, sizeof(want), "a [B, rows, %lld] bf16 CUDA tensor with contiguous last axis", (long long)F);
+      bad_tensor(o, what, want);
+    }
+    B = t.size(0), rows = t.size(1);
+    if (B > INT32_MAX || rows > INT32_MAX) raise(PyExc_ValueError, "too many samples or rows");
+    // the stride of an axis with one entry says nothing
+    return Rows{t.numel() > 0 ? t.data_ptr() : nullptr, B > 1 ? t.stride(0) : 0, rows > 1 ? t.stride(1) : (F + 7) / 8 * 8,
+                rows, B};
+  }
+};
+
+struct Vecs {
+  float* ptr;
+  int64_t stride;
+};
+// [B, C] fp32 CUDA (None: absent), contiguous last axis.
+Vecs vecs_of(PyObject* o, const char* what, int64_t B, int64_t C, bool contiguous = false) {
+  if (o == Py_None) return Vecs{nullptr, 0};
+  const at::Tensor& t = tensor(o);
+  if (t.dim() != 2 || t.scalar_type() != at::kFloat || !t.is_cuda() || t.size(0) != B || t.size(1) != C ||
+      (C > 1 && t.stride(1) != 1) || (contiguous && !t.is_contiguous())) {
+    char want[128];
+    snprintf(want, sizeof(want), "a %s[%lld, %lld] fp32 CUDA tensor", contiguous ? "contiguous " : "", (long long)B,
+             (long long)C);
+    bad_tensor(o, what, want);
+  }
+  return Vecs{static_cast<float*>(t.data_ptr()), B > 1 ? t.stride(0) : 0};
+}
+// [C] fp32 CUDA (None: absent), contiguous.
+float* vec_of(PyObject* o, const char* what, int64_t C) {
+  if (o == Py_None) return nullptr;
+  const at::Tensor& t = tensor(o);
+  if (t.dim() != 1 || t.scalar_type() != at::kFloat || !t.is_cuda() || t.size(0) != C || !t.is_contiguous()) {
+    char want[96];
+    snprintf(want, sizeof(want), "a contiguous [%lld] fp32 CUDA tensor", (long long)C);
+    bad_tensor(o, what, want);
+  }
+  return static_cast<float*>(t.data_ptr());
+}
+struct Scratch {
+  void* ptr;
+  size_t bytes;
+};
+Scratch scratch_of(PyObject* o) {
+  const at::Tensor& t = tensor(o);
+  if (!t.is_cuda() || !t.is_contiguous()) bad_tensor(o, "workspace", "a contiguous CUDA tensor");
+  return Scratch{t.data_ptr(), bytes_of(o)};
+}
+// [B] int32 CUDA modes (None: absent).
+const int32_t* modes_of(PyObject* o, int64_t B) {
+  if (o == Py_None) return nullptr;
+  const at::Tensor& t = tensor(o);
+  if (t.scalar_type() != at::kInt || !t.is_cuda() || t.dim() != 1 || t.size(0) != B || !t.is_contiguous())
+    bad_tensor(o, "mode", "a contiguous [B] int32 CUDA tensor");
+  return static_cast<const int32_t*>(t.data_ptr());
+}
+
+// rope_axes(tensors, pos, axes, base, inverse, stream)
+PyObject* rope_axes(PyObject*, PyObject* const* g, Py_ssize_t n) {
+  return guarded(n, 6, [&] {
+    const Seq ts(g[0], 1), axes(g[2], 1);
+    ra_rope_args a;
+    std::memset(&a, 0, sizeof(a));
+    if (ts.size() > 2) raise(PyExc_ValueError, "refadapt_rope_axes: at most two tensors");
+    if (axes.size() > 4) raise(PyExc_ValueError, "refadapt_rope_axes: at most four axes");
+    a.n_tensors = int32_t(ts.size());
+    a.n_axes = int32_t(axes.size());
+    for (Py_ssize_t i = 0; i < axes.size(); ++i) a.axis_dim[i] = integer32(axes[i]);
+    for (Py_ssize_t i = 0; i < ts.size(); ++i) {
+      const Seq pair(ts[i], 2);
+      a.t[i].x = seg(pair[0]);
+      a.t[i].out = seg(pair[1]);
+      const at::Tensor &x = tensor(pair[0]), &o = tensor(pair[1]);
+      if (x.sizes() != o.sizes() || x.size(0) != tensor(Seq(ts[0], 2)[0]).size(0) || x.size(2) != a.t[0].x.n ||
+          x.size(3) != tensor(Seq(ts[0], 2)[0]).size(3))
+        raise(PyExc_ValueError, "refadapt_rope_axes: a tensor and its output, and the tensors but for their heads, have "
+                                "one shape");
+      a.t[i].heads = int32_t(x.size(1));
+      a.B = int32_t(x.size(0));
+      a.n = int32_t(x.size(2));
+      a.d = int32_t(x.size(3));
+    }
+    const at::Tensor& pos = tensor(g[1]);
+    const bool per_sample = pos.dim() == 3;
+    if (!pos.is_cuda() || pos.scalar_type() != at::kFloat || (pos.dim() != 2 && !per_sample) ||
+        pos.size(-1) != a.n_axes || pos.size(-2) != a.n || (per_sample && pos.size(0) != a.B && pos.size(0) != 1) ||
+        (a.n > 1 && pos.stride(-2) != a.n_axes) || (a.n_axes > 1 && pos.stride(-1) != 1))
+      bad_tensor(g[1], "pos", "an [n, axes] or [B, n, axes] fp32 CUDA tensor with contiguous rows");
+    a.pos = static_cast<const float*>(pos.data_ptr());
+    a.pos_stride_s = per_sample && pos.size(0) > 1 ? pos.stride(0) : 0;
+    a.base = real(g[3]);
+    a.inverse = truth(g[4]);
+    void* st = stream_of(g[5]);
+    return released([&] { return refadapt_rope_axes(&a, st); });
+  });
+}
+
+// residual_norm(segs, C, post, pre, eps, alpha, mode, stream)
+PyObject* residual_norm(PyObject*, PyObject* const* g, Py_ssize_t n) {
+  return guarded(n, 8, [&] {
+    const Seq segs(g[0], 0);
+    ra_resnorm_args a;
+    std::memset(&a, 0, sizeof(a));
+    a.C = integer32(g[1]);
+    for (Py_ssize_t i = 0; i < segs.size(); ++i) {
+      if (i >= 3) too_many_segments();
+      const Map sd(segs[i]);
+      ra_resnorm_seg& s = a.seg[i];
+      RowShape shape;
+      const Rows h = shape.take(sd.need(N.h), "h", a.C), y = shape.take(sd.get(N.y), "y", a.C),
+                 o = shape.take(sd.get(N.h_out), "h_out", a.C), x = shape.take(sd.get(N.x), "x", a.C);
+      if (shape.B < 0) raise(PyExc_ValueError, "h: expected a tensor");
+      if (i > 0 && a.B != shape.B) raise(PyExc_ValueError, "refadapt_residual_norm: segments of one batch size needed");
+      a.B = int32_t(shape.B);
+      s.h = h.ptr, s.h_stride_s = h.stride_s, s.h_stride_r = h.stride_r;
+      s.y = y.ptr, s.y_stride_s = y.stride_s, s.y_stride_r = y.stride_r;
+      s.h_out = o.ptr, s.h_out_stride_s = o.stride_s, s.h_out_stride_r = o.stride_r;
+      s.x = x.ptr, s.x_stride_s = x.stride_s, s.x_stride_r = x.stride_r;
+      const Vecs gate = vecs_of(sd.get(N.gate), "gate", a.B, a.C), scale = vecs_of(sd.get(N.scale), "scale", a.B, a.C),
+                 shift = vecs_of(sd.get(N.shift), "shift", a.B, a.C);
+      if (scale.ptr && shift.ptr && scale.stride != shift.stride)
+        raise(PyExc_ValueError, "shift and scale must share a row stride");
+      s.gate = gate.ptr, s.gate_stride_s = gate.stride;
+      s.scale = scale.ptr, s.shift = shift.ptr, s.mod_stride_s = scale.ptr ? scale.stride : shift.stride;
+      s.post_w = vec_of(sd.get(N.post_w), "post_w", a.C);
+      s.pre_w = vec_of(sd.get(N.pre_w), "pre_w", a.C);
+      s.rows = int32_t(shape.rows);
+      s.gated = truth(sd.get(N.gated));
+    }
+    if (segs.size() == 0) raise(PyExc_TypeError, "refadapt_residual_norm: no segments");
+    a.n_seg = int32_t(segs.size());
+    a.post = integer32(g[2]);
+    a.pre = integer32(g[3]);
+    a.eps = float(real(g[4]));
+    a.alpha = float(real(g[5]));
+    a.mode = modes_of(g[6], a.B);
+    void* st = stream_of(g[7]);
+    return released([&] { return refadapt_residual_norm(&a, st); });
+  });
+}
+
+// residual_norm_backward(seg, C, post, pre, workspace, eps, alpha, stream)
+PyObject* residual_norm_backward(PyObject*, PyObject* const* g, Py_ssize_t n) {
+  return guarded(n, 8, [&] {
+    const Map sd(g[0]);
+    ra_resnorm_grad_args a;
+    std::memset(&a, 0, sizeof(a));
+    a.C = integer32(g[1]);
+    RowShape shape;
+    const Rows h = shape.take(sd.need(N.h), "h", a.C), y = shape.take(sd.get(N.y), "y", a.C),
+               dx = shape.take(sd.get(N.dx), "dx", a.C), dho = shape.take(sd.get(N.dh_out), "dh_out", a.C),
+               dh = shape.take(sd.get(N.dh), "dh", a.C), dy = shape.take(sd.get(N.dy), "dy", a.C);
+    if (shape.B < 0) raise(PyExc_ValueError, "h: expected a tensor");
+    a.B = int32_t(shape.B), a.rows = int32_t(shape.rows);
+    a.h = h.ptr, a.h_stride_s = h.stride_s, a.h_stride_r = h.stride_r;
+    a.y = y.ptr, a.y_stride_s = y.stride_s, a.y_stride_r = y.stride_r;
+    a.dx = dx.ptr, a.dx_stride_s = dx.stride_s, a.dx_stride_r = dx.stride_r;
+    a.dh_out = dho.ptr, a.dh_out_stride_s = dho.stride_s, a.dh_out_stride_r = dho.stride_r;
+    a.dh = dh.ptr, a.dh_stride_s = dh.stride_s, a.dh_stride_r = dh.stride_r;
+    a.dy = dy.ptr, a.dy_stride_s = dy.stride_s, a.dy_stride_r = dy.stride_r;
+    const Vecs gate = vecs_of(sd.get(N.gate), "gate", a.B, a.C), scale = vecs_of(sd.get(N.scale), "scale", a.B, a.C);
+    a.gate = gate.ptr, a.gate_stride_s = gate.stride;
+    a.scale = scale.ptr, a.mod_stride_s = scale.stride;
+    a.post_w = vec_of(sd.get(N.post_w), "post_w", a.C);
+    a.pre_w = vec_of(sd.get(N.pre_w), "pre_w", a.C);
+    a.dgate = vecs_of(sd.get(N.dgate), "dgate", a.B, a.C, true).ptr;
+    a.dscale = vecs_of(sd.get(N.dscale), "dscale", a.B, a.C, true).ptr;
+    a.dshift = vecs_of(sd.get(N.dshift), "dshift", a.B, a.C, true).ptr;
+    a.dpost_w = vec_of(sd.get(N.dpost_w), "dpost_w", a.C);
+    a.dpre_w = vec_of(sd.get(N.dpre_w), "dpre_w", a.C);
+    a.post = integer32(g[2]);
+    a.pre = integer32(g[3]);
+    const Scratch ws = scratch_of(g[4]);
+    a.workspace = ws.ptr, a.workspace_bytes = ws.bytes;
+    a.eps = float(real(g[5]));
+    a.alpha = float(real(g[6]));
+    void* st = stream_of(g[7]);
+    return released([&] { return refadapt_residual_norm_backward(&a, st); });
+  });
+}
+
 #define RA_METHOD(f) \
   {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {RA_METHOD(joint_attn), RA_METHOD(q_delta), RA_METHOD(gate),   RA_METHOD(q_delta_gate),
-                         RA_METHOD(ln_modulate), RA_METHOD(gemm),   {nullptr, nullptr, 0, nullptr}};
+                         RA_METHOD(ln_modulate), RA_METHOD(gemm),   RA_METHOD(rope_axes), RA_METHOD(residual_norm),
+                         RA_METHOD(residual_norm_backward), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
@@ -434,7 +643,10 @@ PyMODINIT_FUNC PyInit__binding() {
                {&N.gated, "gated"}, {&N.a, "a"},         {&N.w, "w"},           {&N.bias, "bias"},
                {&N.out, "out"},   {&N.resid, "resid"}, {&N.gate, "gate"},     {&N.q, "q"},
                {&N.k, "k"},       {&N.v, "v"},         {&N.q_norm, "q_norm"}, {&N.k_norm, "k_norm"},
-               {&N.pos_offset, "pos_offset"}};
+               {&N.pos_offset, "pos_offset"}, {&N.y, "y"}, {&N.h_out, "h_out"}, {&N.post_w, "post_w"},
+               {&N.pre_w, "pre_w"}, {&N.dx, "dx"}, {&N.dh_out, "dh_out"}, {&N.dh, "dh"}, {&N.dy, "dy"},
+               {&N.dgate, "dgate"}, {&N.dscale, "dscale"}, {&N.dshift, "dshift"}, {&N.dpost_w, "dpost_w"},
+               {&N.dpre_w, "dpre_w"}};
   for (const auto& e : names)
     if (!(*e.slot = PyUnicode_InternFromString(e.name))) return nullptr;
   return PyModule_Create(&module);

@@ -22,6 +22,7 @@
 #include <cstring>
 
 #include "api_common.h"
+#include "row_walk.cuh"
 #include "tc_ptx.cuh"
 
 namespace ra {
@@ -61,51 +62,6 @@ struct Params {
   uint64_t budget_ns;
   float eps;
   const int32_t* mode;
-};
-
-__device__ __forceinline__ bool live(const Params& p, int g, int s) {
-  return !p.seg[g].gated || p.mode[s] != RA_MODE_REUSE;
-}
-
-// Live rows in order: segments, samples within, rows within. A piece is the
-// rows of one live (segment, sample), from row `begin` of the order on.
-struct Piece {
-  int g = 0, s = 0, begin = 0;
-  // Moves to the piece that holds row i (i at or past begin, below the total).
-  __device__ __forceinline__ void seek(const Params& p, int i) {
-    while (i - begin >= p.seg[g].rows || !live(p, g, s)) {
-      if (live(p, g, s)) begin += p.seg[g].rows;
-      if (++s == p.B || p.seg[g].rows == 0) {
-        s = 0;
-        ++g;
-      }
-    }
-  }
-  // The same over many samples (the whole warp, from a segment's first): those of
-  // a segment that is not gated are counted off by a division, others 32 at a
-  // time. seek() takes 0.1 us for each (256 samples of one row: 50 us).
-  __device__ __forceinline__ void jump(const Params& p, int i) {
-    for (;; ++g, s = 0) {
-      const int rows = p.seg[g].rows;
-      if (rows == 0) continue;
-      const int k = int(uint32_t(i - begin) / uint32_t(rows));  // live samples to pass
-      if (!p.seg[g].gated) {
-        s = min(k, p.B);
-        begin += s * rows;
-        if (s < p.B) return;
-        continue;
-      }
-      int passed = 0;
-      for (; s < p.B; s += 32) {
-        const int t = s + (threadIdx.x & 31);
-        const int n = __popc(__ballot_sync(0xffffffffu, t < p.B && live(p, g, t)));
-        if (passed + n > k) break;
-        passed += n;
-      }
-      begin += passed * rows;
-      if (s < p.B) return;  // one of the 32 samples from s on: seek() finds it
-    }
-  }
 };
 
 // A warp whose own copy of row i did not end within the budget: it lets the
@@ -239,17 +195,7 @@ __global__ void __launch_bounds__(32 * Layout<G>::WARPS, 1) ln_mod_kernel(const 
   if (lane < S) mbar_init(full + lane, 1);
   fence_mbar_init();
   __syncwarp();
-  // Live rows of the call (the modes are on the device), and this CTA's share.
-  int total = 0;
-  for (int g = 0; g < p.n_seg; ++g) {
-    int n = p.B;
-    if (p.seg[g].gated) {
-      n = 0;
-      for (int s0 = 0; s0 < p.B; s0 += 32)
-        n += __popc(__ballot_sync(0xffffffffu, s0 + lane < p.B && live(p, g, s0 + lane)));
-    }
-    total += n * p.seg[g].rows;
-  }
+  const int total = live_rows(p);  // and this CTA's share of them
   const int share = total / int(gridDim.x), more = total - share * int(gridDim.x), cta = int(blockIdx.x);
   const int lo = share * cta + min(cta, more);
   const int hi = lo + share + (cta < more ? 1 : 0);
