@@ -614,6 +614,91 @@ typedef struct {
 size_t refadapt_residual_norm_backward_workspace_size(int32_t B, int32_t rows, int32_t C);
 ra_status refadapt_residual_norm_backward(const ra_resnorm_grad_args* args, void* stream);
 
+/* refadapt_glu — the gated feed-forward's projections, activation and product
+ * in one kernel, on tcgen05 tensor cores:
+ *   out = act(x Wg^T) o (x Wu^T)
+ * x bf16 rows of C features, Wg and Wu bf16 [F][C] contiguous (nn.Linear
+ * layout; halves of one [2 F][C] matrix will do), one pair per segment, fp32
+ * accumulation, one rounding to bf16 per output. act: RA_ACT_SILU g / (1 + e^-g)
+ * or RA_ACT_GELU (tanh form). The down projection is refadapt_gemm.
+ *  pre_gate, pre_up   bf16 rows of F, the products before the activation, for
+ *                     refadapt_glu_backward; both or neither (NULL).
+ * C and F multiples of 8, at least 64; pointers 16-byte aligned, row strides
+ * multiples of 8 elements and at least the row's length. A segment with gated =
+ * 1 is skipped for samples whose mode is RA_MODE_REUSE. err_word: device int32
+ * or NULL; bit 0 set if a device wait timed out. Deterministic; how a call is
+ * cut into tiles follows from its sizes. */
+typedef enum { RA_ACT_SILU = 0, RA_ACT_GELU = 1 } ra_act;
+
+typedef struct {
+  const void* x;
+  int64_t x_stride_s, x_stride_r;
+  const void* w_gate;  /* bf16 [F][C] */
+  const void* w_up;    /* bf16 [F][C] */
+  void* out;
+  int64_t out_stride_s, out_stride_r;
+  void* pre_gate;
+  int64_t pre_gate_stride_s, pre_gate_stride_r;
+  void* pre_up;
+  int64_t pre_up_stride_s, pre_up_stride_r;
+  int32_t rows;        /* rows per sample, >= 0 */
+  int32_t gated;
+} ra_glu_seg;
+
+typedef struct {
+  int32_t B, F, C, act, n_seg, reserved;
+  ra_glu_seg seg[3];
+  const int32_t* mode;  /* device [B]; required when a segment is gated */
+  int32_t* err_word;
+} ra_glu_args;
+
+ra_status refadapt_glu(const ra_glu_args* args, void* stream);
+
+/* refadapt_glu_backward — gradients of the gated feed-forward of one segment,
+ *   y = hidden Wd^T,  hidden = act(g) o w,  g = x Wg^T,  w = x Wu^T,
+ * from dy and what refadapt_glu kept (pre_gate = g, pre_up = w, hidden = out):
+ *   du = dy Wd,  dg = du o w o act'(g),  dw = du o act(g),
+ *   dx = dg Wg + dw Wu,  dw_gate = dg^T x,  dw_up = dw^T x,  dw_down = dy^T hidden
+ * dg and dw are formed in the epilogue of dy Wd from its fp32 sums (du is never
+ * stored) and rounded to bf16 once, as operands of the products after them.
+ * Three products' launches, and one more where a long sum is split.
+ *  dy                  bf16 rows of O features; w_down bf16 [O][F].
+ *  dx, dw_*            bf16, contiguous [F][C] and [O][F] for the weights; any
+ *                      may be NULL (frozen weights), not all. hidden may be NULL
+ *                      without dw_down, x without dw_gate and dw_up.
+ *  workspace           device scratch of refadapt_glu_backward_workspace_size()
+ *                      bytes (on the device that is current), 16-byte aligned;
+ *                      calls that share it must be stream-ordered.
+ * C, F, O multiples of 8, at least 64; pointers and strides as for refadapt_glu.
+ * Rows of zero: the weights' gradients are zero. Deterministic. */
+typedef struct {
+  int32_t B, rows, C, F, O, act;
+  const void* dy;
+  int64_t dy_stride_s, dy_stride_r;
+  const void* x;
+  int64_t x_stride_s, x_stride_r;
+  const void* pre_gate;
+  int64_t pre_gate_stride_s, pre_gate_stride_r;
+  const void* pre_up;
+  int64_t pre_up_stride_s, pre_up_stride_r;
+  const void* hidden;
+  int64_t hidden_stride_s, hidden_stride_r;
+  const void* w_gate;
+  const void* w_up;
+  const void* w_down;
+  void* dx;
+  int64_t dx_stride_s, dx_stride_r;
+  void* dw_gate;
+  void* dw_up;
+  void* dw_down;
+  void* workspace;
+  size_t workspace_bytes;
+  int32_t* err_word;
+} ra_glu_grad_args;
+
+size_t refadapt_glu_backward_workspace_size(int32_t B, int32_t rows, int32_t C, int32_t F, int32_t O);
+ra_status refadapt_glu_backward(const ra_glu_grad_args* args, void* stream);
+
 /* ------------------------------------------------------------------ misc */
 const char* refadapt_status_string(ra_status s);
 const char* refadapt_last_error(void);

@@ -25,10 +25,12 @@ EXPORTED = (
     "refadapt_selftest_wait_timeout", "refadapt_q_delta_noalloc", "refadapt_rope_table",
     "refadapt_ln_modulate", "refadapt_gemm", "refadapt_q_delta_gate", "refadapt_last_launch",
     "refadapt_rope_axes", "refadapt_rope_axes_table", "refadapt_residual_norm", "refadapt_residual_norm_backward",
-    "refadapt_residual_norm_backward_workspace_size",
+    "refadapt_residual_norm_backward_workspace_size", "refadapt_glu", "refadapt_glu_backward",
+    "refadapt_glu_backward_workspace_size",
 )
 RA_EPI_STORE, RA_EPI_GELU, RA_EPI_RESID, RA_EPI_QKV = 0, 1, 2, 3
 RA_NORM_NONE, RA_NORM_LAYER, RA_NORM_RMS = 0, 1, 2
+RA_ACT_SILU, RA_ACT_GELU = 0, 1
 
 
 class RaSeg(ctypes.Structure):
@@ -119,6 +121,24 @@ class RaResnormGradArgs(ctypes.Structure):
         ("dpost_w", c_void_p), ("dpre_w", c_void_p), ("workspace", c_void_p), ("workspace_bytes", c_size_t)]
 
 
+class RaGluSeg(ctypes.Structure):
+    _fields_ = _rows("x") + [("w_gate", c_void_p), ("w_up", c_void_p)] + _rows("out", "pre_gate", "pre_up") + [
+        ("rows", c_int32), ("gated", c_int32)]
+
+
+class RaGluArgs(ctypes.Structure):
+    _fields_ = [("B", c_int32), ("F", c_int32), ("C", c_int32), ("act", c_int32), ("n_seg", c_int32),
+                ("reserved", c_int32), ("seg", RaGluSeg * 3), ("mode", c_void_p), ("err_word", c_void_p)]
+
+
+class RaGluGradArgs(ctypes.Structure):
+    _fields_ = [("B", c_int32), ("rows", c_int32), ("C", c_int32), ("F", c_int32), ("O", c_int32), ("act", c_int32)] + \
+        _rows("dy", "x", "pre_gate", "pre_up", "hidden") + [
+        ("w_gate", c_void_p), ("w_up", c_void_p), ("w_down", c_void_p)] + _rows("dx") + [
+        ("dw_gate", c_void_p), ("dw_up", c_void_p), ("dw_down", c_void_p), ("workspace", c_void_p),
+        ("workspace_bytes", c_size_t), ("err_word", c_void_p)]
+
+
 class RefAdaptError(RuntimeError):
     def __init__(self, fn, status, msg):
         super().__init__("%s failed: %s (%s)" % (fn, _status_name(status), msg))
@@ -196,6 +216,12 @@ def load():
     lib.refadapt_residual_norm_backward_workspace_size.argtypes = [c_int32, c_int32, c_int32]
     lib.refadapt_residual_norm_backward.restype = c_int32
     lib.refadapt_residual_norm_backward.argtypes = [POINTER(RaResnormGradArgs), c_void_p]
+    lib.refadapt_glu.restype = c_int32
+    lib.refadapt_glu.argtypes = [POINTER(RaGluArgs), c_void_p]
+    lib.refadapt_glu_backward_workspace_size.restype = c_size_t
+    lib.refadapt_glu_backward_workspace_size.argtypes = [c_int32] * 5
+    lib.refadapt_glu_backward.restype = c_int32
+    lib.refadapt_glu_backward.argtypes = [POINTER(RaGluGradArgs), c_void_p]
     lib.refadapt_selftest_wait_timeout.restype = c_int32
     lib.refadapt_selftest_wait_timeout.argtypes = [c_void_p, c_uint64, c_void_p]
     _lib = lib

@@ -20,7 +20,8 @@ __all__ = ["seg", "refadapt_joint_attn", "refadapt_mass_partial_len", "refadapt_
            "alloc_mass_partial", "refadapt_rope_table", "rope_table", "refadapt_ln_modulate", "refadapt_gemm",
            "refadapt_rope_axes", "refadapt_rope_axes_table", "rope_axes_table", "refadapt_residual_norm",
            "refadapt_residual_norm_backward", "refadapt_residual_norm_backward_workspace_size",
-           "residual_norm_backward_workspace"]
+           "residual_norm_backward_workspace", "refadapt_glu", "refadapt_glu_backward",
+           "refadapt_glu_backward_workspace_size", "glu_backward_workspace"]
 
 
 def _ptr(t):
@@ -261,3 +262,30 @@ def refadapt_residual_norm_backward(seg, C, post, pre, workspace, eps=1e-6, alph
     dpost_w, dpre_w ([C] fp32)."""
     return check("refadapt_residual_norm_backward", _lib.native().residual_norm_backward(
         seg, int(C), int(post), int(pre), workspace, float(eps), float(alpha), _handle(stream)))
+
+
+def refadapt_glu(segs, F, C, act, mode=None, err_word=None, stream=None):
+    """out = act(x w_gate^T) * (x w_up^T). segs: up to three dicts with x ([B,
+    rows, C] bf16), w_gate, w_up ([F, C] bf16), out ([B, rows, F] bf16), optional
+    pre_gate and pre_up (like out, kept for the backward pass), gated; act:
+    RA_ACT_SILU or RA_ACT_GELU. The down projection is refadapt_gemm."""
+    return check("refadapt_glu", _lib.native().glu(segs, int(F), int(C), int(act), mode, err_word, _handle(stream)))
+
+
+def refadapt_glu_backward_workspace_size(B, rows, C, F, O) -> int:
+    return int(_lib.load().refadapt_glu_backward_workspace_size(int(B), int(rows), int(C), int(F), int(O)))
+
+
+def glu_backward_workspace(B, rows, C, F, O, device="cuda"):
+    """A workspace for refadapt_glu_backward (reusable across calls)."""
+    return torch.empty(refadapt_glu_backward_workspace_size(B, rows, C, F, O), dtype=torch.uint8, device=device)
+
+
+def refadapt_glu_backward(dy, x, w_gate, w_up, w_down, pre_gate, pre_up, hidden, act, workspace, dx=None, dw_gate=None,
+                          dw_up=None, dw_down=None, err_word=None, stream=None):
+    """Gradients of y = hidden w_down^T, hidden = act(x w_gate^T) * (x w_up^T), from dy ([B, rows, O] bf16) and what
+    refadapt_glu kept (hidden: its out). Fills those of dx ([B, rows, C]), dw_gate, dw_up ([F, C]) and dw_down ([O,
+    F]) that are given. x may be None without dw_gate and dw_up, hidden without dw_down."""
+    return check("refadapt_glu_backward", _lib.native().glu_backward(
+        dy, x, w_gate, w_up, w_down, pre_gate, pre_up, hidden, int(act), workspace, dx, dw_gate, dw_up, dw_down,
+        err_word, _handle(stream)))

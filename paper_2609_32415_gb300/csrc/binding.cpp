@@ -178,6 +178,7 @@ bool truth(PyObject* o) {
 struct Names {
   PyObject *h, *x, *shift, *scale, *gated, *a, *w, *bias, *out, *resid, *gate, *q, *k, *v, *q_norm, *k_norm, *pos_offset;
   PyObject *y, *h_out, *post_w, *pre_w, *dx, *dh_out, *dh, *dy, *dgate, *dscale, *dshift, *dpost_w, *dpre_w;
+  PyObject *w_gate, *w_up, *pre_gate, *pre_up;
 } N;
 
 // Stream argument: None is the calling thread's current stream.
@@ -626,11 +627,100 @@ PyObject* residual_norm_backward(PyObject*, PyObject* const* g, Py_ssize_t n) {
   });
 }
 
+// [rows, cols] bf16 CUDA weight (None: absent), contiguous.
+void* weight_of(PyObject* o, const char* what, int64_t rows, int64_t cols) {
+  if (o == Py_None) return nullptr;
+  const at::Tensor& t = tensor(o);
+  if (t.dim() != 2 || t.scalar_type() != at::kBFloat16 || !t.is_cuda() || t.size(0) != rows || t.size(1) != cols ||
+      !t.is_contiguous()) {
+    char want[128];
+    snprintf(want, sizeof(want), "a contiguous [%lld, %lld] bf16 CUDA tensor", (long long)rows, (long long)cols);
+    bad_tensor(o, what, want);
+  }
+  return t.data_ptr();
+}
+
+// glu(segs, F, C, act, mode, err_word, stream)
+PyObject* glu(PyObject*, PyObject* const* g, Py_ssize_t n) {
+  return guarded(n, 7, [&] {
+    const Seq segs(g[0], 0);
+    ra_glu_args a;
+    std::memset(&a, 0, sizeof(a));
+    a.F = integer32(g[1]);
+    a.C = integer32(g[2]);
+    a.act = integer32(g[3]);
+    for (Py_ssize_t i = 0; i < segs.size(); ++i) {
+      if (i >= 3) too_many_segments();
+      const Map sd(segs[i]);
+      ra_glu_seg& s = a.seg[i];
+      RowShape shape;
+      const Rows x = shape.take(sd.need(N.x), "x", a.C), o = shape.take(sd.need(N.out), "out", a.F),
+                 pg = shape.take(sd.get(N.pre_gate), "pre_gate", a.F), pu = shape.take(sd.get(N.pre_up), "pre_up", a.F);
+      if (shape.B < 0) raise(PyExc_ValueError, "x: expected a tensor");
+      if (i > 0 && a.B != shape.B) raise(PyExc_ValueError, "refadapt_glu: segments of one batch size needed");
+      a.B = int32_t(shape.B);
+      s.x = x.ptr, s.x_stride_s = x.stride_s, s.x_stride_r = x.stride_r;
+      s.out = o.ptr, s.out_stride_s = o.stride_s, s.out_stride_r = o.stride_r;
+      s.pre_gate = pg.ptr, s.pre_gate_stride_s = pg.stride_s, s.pre_gate_stride_r = pg.stride_r;
+      s.pre_up = pu.ptr, s.pre_up_stride_s = pu.stride_s, s.pre_up_stride_r = pu.stride_r;
+      s.w_gate = weight_of(sd.need(N.w_gate), "w_gate", a.F, a.C);
+      s.w_up = weight_of(sd.need(N.w_up), "w_up", a.F, a.C);
+      s.rows = int32_t(shape.rows);
+      s.gated = truth(sd.get(N.gated));
+    }
+    if (segs.size() == 0) raise(PyExc_TypeError, "refadapt_glu: no segments");
+    a.n_seg = int32_t(segs.size());
+    a.mode = modes_of(g[4], a.B);
+    a.err_word = static_cast<int32_t*>(address(g[5]));
+    void* st = stream_of(g[6]);
+    return released([&] { return refadapt_glu(&a, st); });
+  });
+}
+
+// glu_backward(dy, x, w_gate, w_up, w_down, pre_gate, pre_up, hidden, act, workspace, dx, dw_gate, dw_up, dw_down,
+//              err_word, stream)
+PyObject* glu_backward(PyObject*, PyObject* const* g, Py_ssize_t n) {
+  return guarded(n, 16, [&] {
+    ra_glu_grad_args a;
+    std::memset(&a, 0, sizeof(a));
+    const at::Tensor &dy = tensor(g[0]), &wg = tensor(g[2]);
+    if (dy.dim() != 3) bad_tensor(g[0], "dy", "a [B, rows, O] bf16 CUDA tensor");
+    if (wg.dim() != 2) bad_tensor(g[2], "w_gate", "a contiguous [F, C] bf16 CUDA tensor");
+    if (dy.size(2) > INT32_MAX || wg.size(0) > INT32_MAX || wg.size(1) > INT32_MAX)
+      raise(PyExc_ValueError, "refadapt_glu_backward: too many features");
+    a.O = int32_t(dy.size(2)), a.F = int32_t(wg.size(0)), a.C = int32_t(wg.size(1));
+    RowShape shape;
+    const Rows d = shape.take(g[0], "dy", a.O), x = shape.take(g[1], "x", a.C), pg = shape.take(g[5], "pre_gate", a.F),
+               pu = shape.take(g[6], "pre_up", a.F), h = shape.take(g[7], "hidden", a.F), dx = shape.take(g[10], "dx", a.C);
+    a.B = int32_t(shape.B), a.rows = int32_t(shape.rows);
+    a.dy = d.ptr, a.dy_stride_s = d.stride_s, a.dy_stride_r = d.stride_r;
+    a.x = x.ptr, a.x_stride_s = x.stride_s, a.x_stride_r = x.stride_r;
+    a.pre_gate = pg.ptr, a.pre_gate_stride_s = pg.stride_s, a.pre_gate_stride_r = pg.stride_r;
+    a.pre_up = pu.ptr, a.pre_up_stride_s = pu.stride_s, a.pre_up_stride_r = pu.stride_r;
+    a.hidden = h.ptr, a.hidden_stride_s = h.stride_s, a.hidden_stride_r = h.stride_r;
+    a.dx = dx.ptr, a.dx_stride_s = dx.stride_s, a.dx_stride_r = dx.stride_r;
+    a.w_gate = weight_of(g[2], "w_gate", a.F, a.C);
+    a.w_up = weight_of(g[3], "w_up", a.F, a.C);
+    a.w_down = weight_of(g[4], "w_down", a.O, a.F);
+    a.act = integer32(g[8]);
+    const Scratch ws = scratch_of(g[9]);
+    a.workspace = ws.ptr, a.workspace_bytes = ws.bytes;
+    a.dw_gate = weight_of(g[11], "dw_gate", a.F, a.C);
+    a.dw_up = weight_of(g[12], "dw_up", a.F, a.C);
+    a.dw_down = weight_of(g[13], "dw_down", a.O, a.F);
+    a.err_word = static_cast<int32_t*>(address(g[14]));
+    void* st = stream_of(g[15]);
+    // without rows there is nothing in dx, and its address says nothing
+    if (a.rows == 0 && g[10] != Py_None && !a.dw_gate && !a.dw_up && !a.dw_down) return RA_OK;
+    return released([&] { return refadapt_glu_backward(&a, st); });
+  });
+}
+
 #define RA_METHOD(f) \
   {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {RA_METHOD(joint_attn), RA_METHOD(q_delta), RA_METHOD(gate),   RA_METHOD(q_delta_gate),
                          RA_METHOD(ln_modulate), RA_METHOD(gemm),   RA_METHOD(rope_axes), RA_METHOD(residual_norm),
-                         RA_METHOD(residual_norm_backward), {nullptr, nullptr, 0, nullptr}};
+                         RA_METHOD(residual_norm_backward), RA_METHOD(glu), RA_METHOD(glu_backward), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
@@ -646,7 +736,8 @@ PyMODINIT_FUNC PyInit__binding() {
                {&N.pos_offset, "pos_offset"}, {&N.y, "y"}, {&N.h_out, "h_out"}, {&N.post_w, "post_w"},
                {&N.pre_w, "pre_w"}, {&N.dx, "dx"}, {&N.dh_out, "dh_out"}, {&N.dh, "dh"}, {&N.dy, "dy"},
                {&N.dgate, "dgate"}, {&N.dscale, "dscale"}, {&N.dshift, "dshift"}, {&N.dpost_w, "dpost_w"},
-               {&N.dpre_w, "dpre_w"}};
+               {&N.dpre_w, "dpre_w"}, {&N.w_gate, "w_gate"}, {&N.w_up, "w_up"}, {&N.pre_gate, "pre_gate"},
+               {&N.pre_up, "pre_up"}};
   for (const auto& e : names)
     if (!(*e.slot = PyUnicode_InternFromString(e.name))) return nullptr;
   return PyModule_Create(&module);

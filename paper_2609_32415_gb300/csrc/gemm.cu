@@ -52,6 +52,7 @@
 #include <mutex>
 
 #include "api_common.h"
+#include "epi_rows.cuh"
 #include "tc_ptx.cuh"
 
 namespace ra {
@@ -231,49 +232,6 @@ __device__ __forceinline__ void gelu_tanh2(float& x0, float& x1) {
   float d0, d1;
   f2_unpack(f2_add(f2_pack(ex2_approx(z0), ex2_approx(z1)), f2_pack(1.f, 1.f)), d0, d1);
   f2_unpack(f2_mul(x, f2_pack(rcp_approx(d0), rcp_approx(d1))), x0, x1);
-}
-
-// The 64-byte row slots of a warp's staging buffer: 16-byte piece q of row r.
-// The permutation keeps both access patterns free of bank conflicts (every
-// lane its own row; eight rows, four lanes a row).
-__device__ __forceinline__ uint4* stage_slot(uint8_t* stage, int r, int q) {
-  return reinterpret_cast<uint4*>(stage + r * 64 + ((q ^ ((r >> 1) & 3)) << 4));
-}
-// Four 16-byte loads per lane of up to 32 rows of 64 bytes at `src` (row
-// stride in bytes): load i is piece lane % 4 of row 8 i + lane / 4.
-__device__ __forceinline__ void rows_fetch(const char* src, int64_t stride, int nrow, uint4 (&v)[4]) {
-  const int lane = threadIdx.x & 31, r0 = lane >> 2;
-  const char* ptr = src + r0 * stride + (lane & 3) * 16;
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    v[i] = (r0 + 8 * i < nrow) ? *reinterpret_cast<const uint4*>(ptr + 8 * i * stride) : make_uint4(0, 0, 0, 0);
-}
-// rows_fetch's registers -> the lane's own row (64 bytes), through the staging buffer.
-__device__ __forceinline__ void rows_turn(uint8_t* stage, const uint4 (&v)[4], uint4 (&own)[4]) {
-  const int lane = threadIdx.x & 31;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) *stage_slot(stage, 8 * i + (lane >> 2), lane & 3) = v[i];
-  __syncwarp();
-#pragma unroll
-  for (int q = 0; q < 4; ++q) own[q] = *stage_slot(stage, lane, q);
-  __syncwarp();
-}
-// 32 fp32 of every lane's row -> bf16 -> up to 32 rows of 64 bytes at `dst`.
-__device__ __forceinline__ void rows_store(uint8_t* stage, const float (&x)[32], char* dst, int64_t stride, int nrow) {
-  const int lane = threadIdx.x & 31, r0 = lane >> 2;
-#pragma unroll
-  for (int q = 0; q < 4; ++q)
-    *stage_slot(stage, lane, q) =
-        make_uint4(pack_bf16x2(x[8 * q], x[8 * q + 1]), pack_bf16x2(x[8 * q + 2], x[8 * q + 3]),
-                   pack_bf16x2(x[8 * q + 4], x[8 * q + 5]), pack_bf16x2(x[8 * q + 6], x[8 * q + 7]));
-  __syncwarp();
-  char* ptr = dst + r0 * stride + (lane & 3) * 16;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const uint4 v = *stage_slot(stage, r0 + 8 * i, lane & 3);
-    if (r0 + 8 * i < nrow) *reinterpret_cast<uint4*>(ptr + 8 * i * stride) = v;
-  }
-  __syncwarp();
 }
 
 // What an epilogue warp works on: its 32 rows (row0 + lane, nrow of them in

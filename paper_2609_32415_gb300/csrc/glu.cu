@@ -1,0 +1,956 @@
+// refadapt_glu and refadapt_glu_backward: the gated feed-forward,
+//
+//   hidden = act(g) o w,  g = x Wg^T,  w = x Wu^T,   y = hidden Wd^T
+//   du = dy Wd;  dg = du o w o act'(g),  dw = du o act(g)
+//   dx = dg Wg + dw Wu;  dWg = dg^T x,  dWu = dw^T x,  dWd = dy^T hidden
+//
+// bf16 operands, fp32 sums in TMEM. One kernel of CTA pairs (tcgen05 cta_group::2,
+// a 256-row output tile per pair) runs all of these products; a launch has a
+// list of jobs (products), whose tiles the pairs take in turn:
+//   GLU    a tile is w columns of g and the same w of the up projection: rank 0
+//          stages Wg's rows as its half of the MMA's N = 2 w, rank 1 Wu's, so one
+//          MMA forms both and the epilogue has g and w of a column in one thread;
+//   GRAD   du = dy Wd; the epilogue reads g and w and writes dg and dw;
+//   STORE  the four gradients. dx sums over both pairs of operands in one
+//          accumulator (K = 2 F); a job of few tiles and a long K is cut into
+//          parts, whose fp32 sums a second kernel adds up in order.
+// An operand whose K runs along its rows (Wd, Wg, Wu as B, the rows of every
+// operand of a weight's gradient) is read as it lies, MN-major: nothing is
+// transposed in memory.
+//   warp 0      TMA producer: per stage 128 of K, as two chunks of 64, of the
+//               CTA's 128 A rows and its half of the B tile (128-byte swizzle;
+//               what lies past an edge is read as zeros).
+//   warp 1      TMEM allocator (two accumulators of 256 columns) and MMA issuer
+//               (rank 0's).
+//   warps 2..9  epilogue, two warps per TMEM lane quarter, while the next tile's
+//               MMAs fill the other accumulator.
+// Every mbarrier wait is bounded; on a timeout the CTA drains its own copies and
+// MMAs, frees TMEM, flags the error word and returns.
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+
+#include <cstring>
+
+#include "api_common.h"
+#include "epi_rows.cuh"
+#include "tc_ptx.cuh"
+
+namespace ra {
+namespace glu {
+
+constexpr int TM = 256;              // output rows of a pair's tile
+constexpr int MAX_BN = 256;          // accumulator columns
+constexpr int STAGES = 3;
+constexpr int BK = 128;              // K per stage, two chunks of 64
+constexpr int CHUNK = 128 * 64 * 2;  // 128 rows (or columns) x 64 of K of one operand
+constexpr int OPERAND_BYTES = 2 * CHUNK;
+constexpr int STAGE_BYTES = 2 * OPERAND_BYTES;
+constexpr int OFF_BAR = STAGES * STAGE_BYTES;
+constexpr int NUM_BARS = 2 * STAGES + 2 + 2 + 1;  // full, empty, tfull[2], tempty[2], drain
+constexpr int OFF_MISC = OFF_BAR + NUM_BARS * 8;
+constexpr int EPI_WARPS = 8;
+constexpr int EPI_BYTES = 32 * 64;  // staging of a warp
+constexpr int OFF_EPI = (OFF_MISC + 16 + 127) / 128 * 128;
+constexpr int SMEM_ALLOC = OFF_EPI + EPI_WARPS * EPI_BYTES + 1024;
+constexpr int THREADS = 64 + 32 * EPI_WARPS;
+constexpr int TMEM_COLS = 512;
+constexpr int GROUP_M = 16;  // tile rows per band of the tile order
+constexpr int MAX_JOBS = 4;
+static_assert(SMEM_ALLOC <= 232448, "shared memory budget");
+
+enum Kind { GLU, GRAD, STORE };
+
+struct Rows {
+  __nv_bfloat16* ptr;
+  int64_t ss, sr;
+};
+
+struct Job {
+  int32_t samples, rows, gated;  // output rows per sample
+  int32_t m_tiles, cols;         // row and column tiles of a sample
+  int32_t N;                     // output columns
+  int32_t kb, kb_first;          // K steps of 64: all, and those of the first operand pair
+  int32_t kb_sample;             // K steps of a sample where K runs along the rows, else 0
+  int32_t parts;                 // of K
+  int32_t a_mn, b_mn;            // operands whose K runs along their rows
+  Rows out[3];                   // GLU: out, pre_gate, pre_up; GRAD: dg, dw; STORE: the result
+  Rows pre_gate, pre_up;         // GRAD
+  float* partial;                // parts > 1: [part][sample][row][N]
+};
+
+struct Params {
+  int32_t n_jobs, bn, act;
+  const int32_t* mode;
+  int32_t* err_word;
+  uint64_t budget_ns;
+  Job job[MAX_JOBS];
+  // Operand pairs of a job: STORE's two (dx) follow one another in K; GLU's tm_b
+  // are Wg and Wu, one per rank.
+  CUtensorMap tm_a[MAX_JOBS][2], tm_b[MAX_JOBS][2];
+};
+
+struct Unit {
+  int job, s, m0, n0, part, k0, k1;
+};
+
+// Walks the units (a tile's part of K) of the live jobs and samples in order;
+// unit indices only grow. Bands of GROUP_M tile rows, rows fastest inside a
+// band, so that the tiles in flight share few row and column blocks, held in L2.
+template <int KIND>
+struct Walk {
+  int j = 0, s = 0;
+  int64_t begin = 0;
+  __device__ __forceinline__ int64_t units(const Params& p) const {
+    const Job& job = p.job[j];
+    if (job.gated && p.mode[s] == RA_MODE_REUSE) return 0;
+    return int64_t(job.m_tiles) * job.cols * job.parts;
+  }
+  __device__ __forceinline__ bool at(const Params& p, int64_t t, Unit& u) {
+    int64_t n = units(p);
+    while (t - begin >= n) {
+      begin += n;
+      if (++s == p.job[j].samples) {
+        s = 0;
+        if (++j == p.n_jobs) return false;
+      }
+      n = units(p);
+    }
+    const Job& job = p.job[j];
+    const uint32_t idx = uint32_t(t - begin), tile = idx / uint32_t(job.parts);
+    const uint32_t band_tiles = uint32_t(GROUP_M) * uint32_t(job.cols);
+    const uint32_t band = tile / band_tiles, in_band = tile - band * band_tiles;
+    const int m_first = int(band) * GROUP_M;
+    const uint32_t rows = uint32_t(min(GROUP_M, job.m_tiles - m_first));
+    u.job = j;
+    u.s = s;
+    u.m0 = (m_first + int(in_band % rows)) * TM;
+    u.n0 = int(in_band / rows) * (KIND == GLU ? p.bn / 2 : p.bn);
+    u.part = int(idx - tile * uint32_t(job.parts));
+    u.k0 = int(int64_t(job.kb) * u.part / job.parts);
+    u.k1 = int(int64_t(job.kb) * (u.part + 1) / job.parts);
+    return true;
+  }
+};
+
+// act(g) = g s and act'(g) = s + g s (1 - s) z'(g) with s = 1 / (1 + e^-z):
+// z = g for SiLU; for GELU's tanh form 0.5 (1 + tanh(v)) = 1 / (1 + e^-2v), so
+// z = 2 sqrt(2/pi) (g + 0.044715 g^3). An exponential that overflows gives s = 0.
+__device__ __forceinline__ float sigmoid_of(int act, float g, float& dz) {
+  constexpr float log2e = 1.4426950408889634f, c = 2.f * 0.7978845608028654f;
+  float z = g;
+  dz = 1.f;
+  if (act == RA_ACT_GELU) {
+    const float g2 = g * g;
+    z = c * g * fmaf(0.044715f, g2, 1.f);
+    dz = c * fmaf(3.f * 0.044715f, g2, 1.f);
+  }
+  return rcp_approx(1.f + ex2_approx(-log2e * z));
+}
+
+// What an epilogue warp works on: its 32 rows (row0 + lane, nrow of them in the
+// sample), which of the two warps of its lane quarter it is, its staging buffer
+// and the TMEM address of its lanes in the tile's accumulator.
+struct EpiWarp {
+  int row0, nrow, half;
+  uint8_t* stage;
+  uint32_t acc;
+};
+
+__device__ __forceinline__ char* row_ptr(const Rows& r, int s, int row, int col) {
+  return reinterpret_cast<char*>(r.ptr + s * r.ss + row * r.sr + col);
+}
+
+template <class Ready>
+__device__ __forceinline__ bool epilogue_glu(const Params& p, const Unit& u, const EpiWarp& w, Ready ready) {
+  const Job& job = p.job[u.job];
+  const int width = p.bn / 2;
+  if (!ready()) return false;
+  if (w.nrow <= 0) return true;
+  const bool save = job.out[1].ptr != nullptr;
+#pragma unroll 1
+  for (int c = 32 * w.half; c < width; c += 64) {
+    const int col = u.n0 + c, ncol = min(32, job.N - col);
+    if (ncol <= 0) break;
+    uint32_t g[32], v[32];
+    tmem_ld32(w.acc + c, g);
+    tmem_ld32(w.acc + width + c, v);
+    tmem_ld_wait_for(g);
+    tmem_ld_wait_for(v);
+    uint4 own[4];
+    if (save) {
+      uint32_t* o = reinterpret_cast<uint32_t*>(own);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[i] = pack_bf16x2(__uint_as_float(g[2 * i]), __uint_as_float(g[2 * i + 1]));
+      rows_put(w.stage, own, row_ptr(job.out[1], u.s, w.row0, col), 2 * job.out[1].sr, w.nrow, ncol);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[i] = pack_bf16x2(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1]));
+      rows_put(w.stage, own, row_ptr(job.out[2], u.s, w.row0, col), 2 * job.out[2].sr, w.nrow, ncol);
+    }
+    float x[32];
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+      float dz;
+      const float gi = __uint_as_float(g[i]);
+      x[i] = gi * sigmoid_of(p.act, gi, dz) * __uint_as_float(v[i]);
+    }
+    rows_store(w.stage, x, row_ptr(job.out[0], u.s, w.row0, col), 2 * job.out[0].sr, w.nrow, ncol);
+  }
+  return true;
+}
+
+template <class Ready>
+__device__ __forceinline__ bool epilogue_grad(const Params& p, const Unit& u, const EpiWarp& w, Ready ready) {
+  const Job& job = p.job[u.job];
+  auto cols = [&](int c) { return c < p.bn ? min(32, job.N - u.n0 - c) : 0; };
+  uint4 rg[4], rw[4];  // g and w of the next chunk
+  auto fetch = [&](int c) {
+    const int ncol = cols(c);
+    if (ncol <= 0 || w.nrow <= 0) return;
+    rows_fetch(row_ptr(job.pre_gate, u.s, w.row0, u.n0 + c), 2 * job.pre_gate.sr, w.nrow, rg, ncol);
+    rows_fetch(row_ptr(job.pre_up, u.s, w.row0, u.n0 + c), 2 * job.pre_up.sr, w.nrow, rw, ncol);
+  };
+  fetch(32 * w.half);
+  if (!ready()) return false;
+  if (w.nrow <= 0) return true;
+#pragma unroll 1
+  for (int c = 32 * w.half; cols(c) > 0; c += 64) {
+    uint32_t v[32];
+    uint4 own_g[4], own_w[4];
+    tmem_ld32(w.acc + c, v);
+    rows_turn(w.stage, rg, own_g);
+    rows_turn(w.stage, rw, own_w);
+    fetch(c + 64);
+    tmem_ld_wait_for(v);
+    uint32_t* gp = reinterpret_cast<uint32_t*>(own_g);
+    uint32_t* wp = reinterpret_cast<uint32_t*>(own_w);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      float dg[2], dw[2];
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const float g = __uint_as_float(k ? gp[i] & 0xFFFF0000u : gp[i] << 16);
+        const float up = __uint_as_float(k ? wp[i] & 0xFFFF0000u : wp[i] << 16);
+        const float du = __uint_as_float(v[2 * i + k]);
+        float dz;
+        const float s = sigmoid_of(p.act, g, dz), a = g * s;
+        dg[k] = du * up * fmaf(a * (1.f - s), dz, s);
+        dw[k] = du * a;
+      }
+      gp[i] = pack_bf16x2(dg[0], dg[1]);
+      wp[i] = pack_bf16x2(dw[0], dw[1]);
+    }
+    const int ncol = cols(c);
+    rows_put(w.stage, own_g, row_ptr(job.out[0], u.s, w.row0, u.n0 + c), 2 * job.out[0].sr, w.nrow, ncol);
+    rows_put(w.stage, own_w, row_ptr(job.out[1], u.s, w.row0, u.n0 + c), 2 * job.out[1].sr, w.nrow, ncol);
+  }
+  return true;
+}
+
+template <class Ready>
+__device__ __forceinline__ bool epilogue_store(const Params& p, const Unit& u, const EpiWarp& w, Ready ready) {
+  const Job& job = p.job[u.job];
+  if (!ready()) return false;
+  if (w.nrow <= 0) return true;
+  const int lane = threadIdx.x & 31;
+#pragma unroll 1
+  for (int c = 32 * w.half; c < p.bn; c += 64) {
+    const int col = u.n0 + c, ncol = min(32, job.N - col);
+    if (ncol <= 0) break;
+    uint32_t v[32];
+    tmem_ld32(w.acc + c, v);
+    tmem_ld_wait_for(v);
+    if (job.parts > 1) {
+      if (lane < w.nrow) {
+        const int64_t row = (int64_t(u.part) * job.samples + u.s) * job.rows + w.row0 + lane;
+        float4* dst = reinterpret_cast<float4*>(job.partial + row * job.N + col);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (4 * i < ncol)
+            dst[i] = make_float4(__uint_as_float(v[4 * i]), __uint_as_float(v[4 * i + 1]), __uint_as_float(v[4 * i + 2]),
+                                 __uint_as_float(v[4 * i + 3]));
+      }
+      continue;
+    }
+    float x[32];
+#pragma unroll
+    for (int i = 0; i < 32; ++i) x[i] = __uint_as_float(v[i]);
+    rows_store(w.stage, x, row_ptr(job.out[0], u.s, w.row0, col), 2 * job.out[0].sr, w.nrow, ncol);
+  }
+  return true;
+}
+
+// One operand's chunk of 64 of K: `rows` of its rows (K-major; the box has them),
+// or its columns in blocks of 64 (MN-major: 64 rows of K each).
+__device__ __forceinline__ void load_chunk(uint8_t* dst, const CUtensorMap* tm, uint32_t bar, bool mn, int at, int n,
+                                           int k, int s) {
+  if (!mn) {
+    tma_load_4d_pair(dst, tm, bar, k, at, 0, s);
+  } else {
+    for (int c = 0; c < n; c += 64) tma_load_4d_pair(dst + c * 128, tm, bar, at + c, k, 0, s);
+  }
+}
+
+template <int KIND>
+__global__ void __launch_bounds__(THREADS, 1) glu_kernel(const __grid_constant__ Params p) {
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + OFF_BAR);
+  uint64_t* full = bars;
+  uint64_t* empty = bars + STAGES;
+  uint64_t* tfull = bars + 2 * STAGES;
+  uint64_t* tempty = bars + 2 * STAGES + 2;
+  uint64_t* drain = bars + 2 * STAGES + 4;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + OFF_MISC);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + OFF_MISC + 4);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = cluster_rank();
+  const int64_t cid = blockIdx.x >> 1, ncl = gridDim.x >> 1;
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < STAGES; ++s) {
+      mbar_init(full + s, 1);
+      mbar_init(empty + s, 1);
+    }
+    for (int b = 0; b < 2; ++b) {
+      mbar_init(tfull + b, 1);
+      mbar_init(tempty + b, 2 * EPI_WARPS);
+    }
+    mbar_init(drain, 1);
+    *abort_flag = 0;
+    fence_mbar_init();
+  }
+  if (warp == 1) tmem_alloc_pair(tmem_slot, TMEM_COLS);
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync_all();  // both CTAs' barriers and TMEM exist before any cross-CTA use
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  const WaitCtl ctl{abort_flag, p.err_word, p.budget_ns};
+  pdl_launch();
+  if (warp != 0) pdl_wait();
+
+  if (warp == 0) {
+    if (lane == 0) {
+      // -------------------------------------------------------------- producer (both CTAs)
+      for (int j = 0; j < p.n_jobs; ++j)
+        if (p.job[j].rows > 0) {
+          tma_prefetch_desc(&p.tm_a[j][0]);
+          tma_prefetch_desc(&p.tm_b[j][0]);
+        }
+      pdl_wait();
+      const uint32_t full0 = mapa_shared(smem_u32(full), 0);  // rank 0's full barriers
+      const int half = p.bn / 2;                              // columns of B that a CTA stages
+      int64_t it = 0;
+      bool ok = true;
+      Walk<KIND> walk;
+      Unit u;
+      for (int64_t t = cid; ok && walk.at(p, t, u); t += ncl) {
+        const Job& job = p.job[u.job];
+        const uint32_t chunk_bytes = 2u * (CHUNK + uint32_t(job.b_mn ? (half + 63) / 64 * 64 : half) * 128u);
+        for (int kb = u.k0; kb < u.k1; kb += 2, ++it) {
+          const int st = int(it % STAGES);
+          if (it >= STAGES && !(ok = mbar_wait(empty + st, uint32_t((it / STAGES - 1) & 1), ctl))) break;
+          uint8_t* sa = smem + st * STAGE_BYTES;
+          const int chunks = min(2, u.k1 - kb);  // the last stage may be half
+          if (rank == 0) mbar_arrive_expect_tx(full + st, chunks * chunk_bytes);
+          for (int c = 0; c < chunks; ++c) {
+            const int pair = KIND == STORE && kb + c >= job.kb_first;
+            const int local = kb + c - (pair ? job.kb_first : 0);
+            const int ks = job.kb_sample ? local / job.kb_sample : u.s;  // the sample that K lies in
+            const int k = 64 * (job.kb_sample ? local - ks * job.kb_sample : local);
+            load_chunk(sa + c * CHUNK, &p.tm_a[u.job][pair], full0 + 8u * st, job.a_mn, u.m0 + int(rank) * 128, 128, k,
+                       ks);
+            load_chunk(sa + OPERAND_BYTES + c * CHUNK, &p.tm_b[u.job][KIND == GLU ? int(rank) : pair], full0 + 8u * st,
+                       job.b_mn, u.n0 + (KIND == GLU ? 0 : int(rank) * half), half, k, job.kb_sample ? ks : 0);
+          }
+        }
+      }
+      if (*abort_flag) {
+        if (rank == 0) {
+          // rank 0's full barriers count both CTAs' bytes of every phase it armed
+          for (int st = 0; st < STAGES; ++st) {
+            const int64_t n_s = (it > st) ? (it - st + STAGES - 1) / STAGES : 0;
+            if (n_s > 0) mbar_wait_drain(full + st, uint32_t((n_s - 1) & 1), p.budget_ns);
+          }
+        } else {
+          // this CTA cannot observe its own loads' completion: give them time to land
+          const uint64_t t0 = globaltimer_ns();
+          while (globaltimer_ns() - t0 < 200000ull) {
+          }
+        }
+      }
+    }
+  } else if (warp == 1) {
+    if (lane == 0 && rank == 0) {
+      // -------------------------------------------------------------- MMA issuer (rank 0)
+      const uint32_t s0 = smem_u32(smem);
+      int64_t it = 0;
+      int i = 0;
+      bool ok = true, issued = false;
+      Walk<KIND> walk;
+      Unit u;
+      for (int64_t t = cid; ok && walk.at(p, t, u); t += ncl) {
+        const Job& job = p.job[u.job];
+        const int buf = i & 1, use = i >> 1;
+        const uint32_t idesc = idesc_bf16_f32(TM, p.bn, job.a_mn, job.b_mn);
+        // A step of 16 of K: 32 bytes of a K-major row; 16 rows of 128 bytes of an
+        // MN-major block, whose blocks of 64 columns are 64 rows (8 KB) apart.
+        const uint32_t a_step = job.a_mn ? 2048 : 32, a_lbo = job.a_mn ? 8192 : 16;
+        const uint32_t b_step = job.b_mn ? 2048 : 32, b_lbo = job.b_mn ? 8192 : 16;
+        if (use > 0 && !(ok = mbar_wait_cluster(tempty + buf, uint32_t((use - 1) & 1), ctl))) break;
+        tc_fence_after();
+        const uint32_t d_t = tmem + uint32_t(buf * MAX_BN);
+        for (int kb = u.k0; kb < u.k1; kb += 2, ++it) {
+          const int st = int(it % STAGES);
+          if (!(ok = mbar_wait(full + st, uint32_t((it / STAGES) & 1), ctl))) break;
+          tc_fence_after();
+          const uint32_t sa = s0 + st * STAGE_BYTES, sb = sa + OPERAND_BYTES;
+          const int ksteps = min(2, u.k1 - kb) * 4;
+#pragma unroll
+          for (int kk = 0; kk < BK / 16; ++kk) {
+            if (kk >= ksteps) break;
+            const uint32_t o = uint32_t(kk >> 2) * CHUNK;
+            umma_ss_pair(d_t, sdesc_sw128(sa + o + (kk & 3) * a_step, a_lbo, 1024),
+                         sdesc_sw128(sb + o + (kk & 3) * b_step, b_lbo, 1024), idesc, (kb > u.k0 || kk > 0) ? 1u : 0u);
+          }
+          umma_commit_pair(empty + st, 0x3);
+          issued = true;
+        }
+        if (!ok) break;
+        umma_commit_pair(tfull + buf, 0x3);
+        ++i;
+      }
+      if (!ok && issued) {
+        umma_commit_pair(drain, 0x1);
+        mbar_wait_drain(drain, 0, p.budget_ns);
+      }
+    }
+  } else {
+    // ---------------------------------------------------------------- epilogue (both CTAs)
+    const int quarter = warp & 3;
+    EpiWarp w;
+    w.half = (warp - 2) >> 2;
+    w.stage = smem + OFF_EPI + (warp - 2) * EPI_BYTES;
+    const uint32_t tempty0 = mapa_shared(smem_u32(tempty), 0);
+    int i = 0;
+    Walk<KIND> walk;
+    Unit u;
+    for (int64_t t = cid; walk.at(p, t, u); t += ncl) {
+      const int buf = i & 1, use = i >> 1;
+      w.row0 = u.m0 + int(rank) * 128 + quarter * 32;
+      w.nrow = min(32, p.job[u.job].rows - w.row0);
+      w.acc = tmem + (uint32_t(quarter * 32) << 16) + uint32_t(buf * MAX_BN);
+      auto ready = [&] {
+        const bool ok = __all_sync(0xffffffffu, mbar_wait(tfull + buf, uint32_t(use & 1), ctl));
+        tc_fence_after();
+        return ok;
+      };
+      bool ok;
+      if constexpr (KIND == GLU)
+        ok = epilogue_glu(p, u, w, ready);
+      else if constexpr (KIND == GRAD)
+        ok = epilogue_grad(p, u, w, ready);
+      else
+        ok = epilogue_store(p, u, w, ready);
+      if (!ok) break;
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) {
+        if (rank == 0)
+          mbar_arrive(tempty + buf);
+        else
+          mbar_arrive_remote(tempty0 + 8u * buf);
+      }
+      ++i;
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync_all();
+  tc_fence_after();
+  if (warp == 1) tmem_dealloc_pair(tmem, TMEM_COLS);
+}
+
+// Adds up the parts of the jobs that were cut, in order.
+struct JoinJob {
+  const float* partial;
+  int64_t plane, vecs;  // elements of a part; eight-column pieces of the output
+  int32_t parts, rows, N;
+  Rows out;
+};
+struct JoinParams {
+  int32_t n;
+  JoinJob job[MAX_JOBS];
+};
+__global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ JoinParams p) {
+  pdl_launch();
+  pdl_wait();
+  for (int j = 0; j < p.n; ++j) {
+    const JoinJob& job = p.job[j];
+    const int row_vecs = job.N / 8;
+    for (int64_t v = blockIdx.x * int64_t(256) + threadIdx.x; v < job.vecs; v += int64_t(gridDim.x) * 256) {
+      const int64_t row = v / row_vecs;
+      const int col = 8 * int(v - row * row_vecs);
+      float x[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = 0.f;
+      const float* src = job.partial + row * job.N + col;
+      for (int q = 0; q < job.parts; ++q, src += job.plane) {
+        const float4 a = reinterpret_cast<const float4*>(src)[0], b = reinterpret_cast<const float4*>(src)[1];
+        x[0] += a.x, x[1] += a.y, x[2] += a.z, x[3] += a.w, x[4] += b.x, x[5] += b.y, x[6] += b.z, x[7] += b.w;
+      }
+      const int64_t s = row / job.rows;
+      *reinterpret_cast<uint4*>(job.out.ptr + s * job.out.ss + (row - s * job.rows) * job.out.sr + col) =
+          make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]),
+                     pack_bf16x2(x[6], x[7]));
+    }
+  }
+}
+
+// ------------------------------------------------------------------ host
+bool aligned16(const void* ptr) { return (reinterpret_cast<uintptr_t>(ptr) & 15u) == 0; }
+
+// Row tensor of B samples of n rows of `cols` features; an output of B > 1 samples has a place for each.
+struct RowTensor {
+  const void* ptr;
+  int64_t ss, sr;
+  int B, n, cols;
+};
+bool check_rows(const char* who, const char* what, const RowTensor& t, bool output) {
+  if (t.ptr && aligned16(t.ptr) && t.ss % 8 == 0 && t.sr % 8 == 0 && t.sr >= t.cols &&
+      t.ss >= (output && t.B > 1 ? t.cols : 0))
+    return true;
+  set_error("%s: %s must be given, 16-byte aligned, with strides multiples of 8 elements, row stride >= %d", who, what,
+            t.cols);
+  return false;
+}
+// The samples' rows follow one another: B samples of n rows are one of B n.
+bool joins(const RowTensor& t) { return t.B == 1 || t.ss == t.n * t.sr; }
+
+// Tensor map of a row tensor: boxes of 64 features x box_rows.
+bool encode(CUtensorMap* tm, const RowTensor& t, int box_rows) {
+  const ra_seg s{const_cast<void*>(t.ptr), t.B > 1 ? t.ss : 0, 0, t.sr, t.n, 0};
+  return encode_seg(tm, s, t.B, 1, t.cols, 64, box_rows, true);
+}
+
+ra_status launch(const char* who, void (*fn)(Params), const Params& p, int64_t units, cudaStream_t st) {
+  const ra_status as = ensure_dynamic_smem(reinterpret_cast<const void*>(fn), SMEM_ALLOC, who);
+  if (as != RA_OK) return as;
+  const int64_t pairs = num_sms() / 2 > 0 ? num_sms() / 2 : 1;
+  cudaLaunchAttribute attr[2];
+  attr[0] = pdl_attribute();
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = 2;
+  attr[1].val.clusterDim.y = 1;
+  attr[1].val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(unsigned(2 * (units < pairs ? units : pairs)));
+  cfg.blockDim = dim3(THREADS);
+  cfg.dynamicSmemBytes = SMEM_ALLOC;
+  cfg.stream = st;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, fn, p);
+  if (e != cudaSuccess) {
+    set_error("%s: launch failed: %s", who, cudaGetErrorString(e));
+    cudaGetLastError();
+    return RA_ECUDA;
+  }
+  return launch_status(who);
+}
+
+// Microseconds of a round of tiles of bn columns over kb steps of 64 of K, and
+// of a launch around its rounds: fitted to single waves on a GB300.
+double round_us(int bn, double kb) {
+  const double mma = kb / 16.0 * (3.11 + 0.00766 * bn), epilogue = 0.0085 * bn;
+  return mma > epilogue ? mma : epilogue;
+}
+double fixed_us(int bn) { return 4.4 + 0.0088 * bn; }
+
+int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// A product whose result is stored: M x N over kb steps.
+struct Shape {
+  int64_t samples, M, N, kb;
+  int64_t tiles(int bn) const { return samples * div_up(M, TM) * div_up(N, bn); }
+};
+// Accumulator columns and parts of K of a launch of up to three products with
+// the cheapest sum of rounds.
+struct Plan {
+  int bn, parts;
+};
+constexpr int MAX_PARTS = 16;
+Plan plan_store(const Shape* s, int n, int sms) {
+  const int64_t pairs = sms / 2 > 0 ? sms / 2 : 1;
+  Plan best{256, 1};
+  double best_us = 1e30;
+  for (int bn = 256; bn >= 128; bn /= 2)
+    for (int parts = 1; parts <= MAX_PARTS; ++parts) {
+      double work = 0, bytes = 0, longest = 0;
+      int64_t tiles = 0;
+      bool fits = true;
+      for (int i = 0; i < n; ++i) {
+        fits &= parts == 1 || s[i].kb >= 4 * parts;
+        const double r = round_us(bn, double(s[i].kb) / parts);
+        tiles += s[i].tiles(bn) * parts;
+        work += r * double(s[i].tiles(bn) * parts);
+        longest = r > longest ? r : longest;
+        bytes += 8.0 * parts * double(s[i].samples * s[i].M * s[i].N);
+      }
+      if (!fits || tiles == 0) continue;
+      // rounds of equal units; of unequal ones, their mean
+      const double us = fixed_us(bn) + work / double(tiles) * double(div_up(tiles, pairs)) +
+                        (parts > 1 ? 2.5 + bytes / 5e6 : 0.0);
+      if (us < best_us) {
+        best_us = us;
+        best = Plan{bn, parts};
+      }
+    }
+  return best;
+}
+
+// Products of refadapt_glu_backward after dy Wd: dx, and the weights' gradients.
+// Rows that follow one another are one sample (`flat`).
+Shape dx_shape(int B, int rows, int C, int F) { return Shape{B, rows, C, 2 * div_up(F, 64)}; }
+void dw_shapes(Shape (&s)[3], int B, int rows, int C, int F, int O) {
+  const int64_t kb = B * div_up(rows, 64);
+  s[0] = s[1] = Shape{1, F, C, kb};
+  s[2] = Shape{1, O, F, kb};
+}
+size_t partial_bytes(const Shape& s, int parts) {
+  return parts > 1 ? size_t(parts) * size_t(s.samples) * size_t(s.M) * size_t(s.N) * 4 : 0;
+}
+
+}  // namespace glu
+}  // namespace ra
+
+extern "C" ra_status refadapt_glu(const ra_glu_args* a, void* stream) {
+  using namespace ra;
+  using namespace ra::glu;
+  const char* who = "refadapt_glu";
+  clear_error();
+  if (!a) {
+    set_error("%s: args is NULL", who);
+    return RA_EINVAL;
+  }
+  if (a->B < 1 || a->n_seg < 1 || a->n_seg > 3 || a->C < 64 || a->C % 8 != 0 || a->F < 64 || a->F % 8 != 0 ||
+      (a->act != RA_ACT_SILU && a->act != RA_ACT_GELU)) {
+    set_error("%s: need B >= 1, 1 <= n_seg <= 3, C and F multiples of 8 and at least 64, a known activation (B=%d n_seg=%d "
+              "C=%d F=%d act=%d)", who, a->B, a->n_seg, a->C, a->F, a->act);
+    return RA_EINVAL;
+  }
+  Params p;
+  std::memset(&p, 0, sizeof(p));
+  p.act = a->act;
+  p.mode = a->mode;
+  p.err_word = a->err_word;
+  p.budget_ns = wait_budget_ns();
+  RowTensor x[3];
+  for (int g = 0; g < a->n_seg; ++g) {
+    const ra_glu_seg& s = a->seg[g];
+    if (s.rows < 0) {
+      set_error("%s: seg %d rows < 0", who, g);
+      return RA_EINVAL;
+    }
+    if (s.gated && !a->mode) {
+      set_error("%s: seg %d is gated but mode is NULL", who, g);
+      return RA_EINVAL;
+    }
+    if (s.rows == 0) continue;
+    if (!s.w_gate || !s.w_up || !aligned16(s.w_gate) || !aligned16(s.w_up)) {
+      set_error("%s: seg %d: w_gate and w_up must be given and 16-byte aligned", who, g);
+      return RA_EINVAL;
+    }
+    if (!s.pre_gate != !s.pre_up) {
+      set_error("%s: seg %d: pre_gate and pre_up go together", who, g);
+      return RA_EINVAL;
+    }
+    RowTensor r{s.x, s.x_stride_s, s.x_stride_r, a->B, s.rows, a->C};
+    RowTensor o[3] = {{s.out, s.out_stride_s, s.out_stride_r, a->B, s.rows, a->F},
+                      {s.pre_gate, s.pre_gate_stride_s, s.pre_gate_stride_r, a->B, s.rows, a->F},
+                      {s.pre_up, s.pre_up_stride_s, s.pre_up_stride_r, a->B, s.rows, a->F}};
+    const int outs = s.pre_gate ? 3 : 1;
+    if (!check_rows(who, "x", r, false) || !check_rows(who, "out", o[0], true) ||
+        (s.pre_gate && (!check_rows(who, "pre_gate", o[1], true) || !check_rows(who, "pre_up", o[2], true))))
+      return RA_EINVAL;
+    if (int64_t(a->B) * s.rows >= (int64_t(1) << 30)) {
+      set_error("%s: seg %d: too many rows", who, g);
+      return RA_EINVAL;
+    }
+    // samples whose rows follow one another share row tiles
+    bool flat = !s.gated && joins(r);
+    for (int i = 0; i < outs; ++i) flat &= joins(o[i]);
+    if (flat) {
+      r.n *= r.B;
+      r.B = 1;
+    }
+    const int j = p.n_jobs++;
+    x[j] = r;
+    Job& job = p.job[j];
+    job.samples = r.B;
+    job.rows = r.n;
+    job.gated = s.gated ? 1 : 0;
+    job.m_tiles = int32_t(div_up(r.n, TM));
+    job.N = a->F;
+    job.kb = job.kb_first = int32_t(div_up(a->C, 64));
+    job.parts = 1;
+    for (int i = 0; i < outs; ++i)
+      job.out[i] = Rows{static_cast<__nv_bfloat16*>(const_cast<void*>(o[i].ptr)), o[i].ss, o[i].sr};
+  }
+  if (p.n_jobs == 0) return RA_OK;
+  const int64_t pairs = num_sms() / 2 > 0 ? num_sms() / 2 : 1;
+  double best_us = 1e30;
+  int64_t units = 0;
+  for (int bn = 256; bn >= 64; bn -= 64) {
+    int64_t n = 0;
+    for (int j = 0; j < p.n_jobs; ++j) n += int64_t(p.job[j].samples) * p.job[j].m_tiles * div_up(a->F, bn / 2);
+    const double us = fixed_us(bn) + round_us(bn, double(p.job[0].kb)) * double(div_up(n, pairs));
+    if (us < best_us) best_us = us, p.bn = bn, units = n;
+  }
+  for (int g = 0, j = 0; g < a->n_seg; ++g) {
+    const ra_glu_seg& s = a->seg[g];
+    if (s.rows == 0) continue;
+    p.job[j].cols = int32_t(div_up(a->F, p.bn / 2));
+    const RowTensor wg{s.w_gate, 0, a->C, 1, a->F, a->C}, wu{s.w_up, 0, a->C, 1, a->F, a->C};
+    if (!encode(&p.tm_a[j][0], x[j], 128) || !encode(&p.tm_b[j][0], wg, p.bn / 2) ||
+        !encode(&p.tm_b[j][1], wu, p.bn / 2))
+      return RA_EINVAL;
+    ++j;
+  }
+  if (units > 2147483647) {
+    set_error("%s: too many rows", who);
+    return RA_EINVAL;
+  }
+  note_launch("CTA pairs, %d columns", p.bn / 2);
+  return launch(who, glu_kernel<GLU>, p, units, static_cast<cudaStream_t>(stream));
+}
+
+extern "C" size_t refadapt_glu_backward_workspace_size(int32_t B, int32_t rows, int32_t C, int32_t F, int32_t O) {
+  using namespace ra::glu;
+  if (B < 1 || rows < 0 || C < 64 || F < 64 || O < 64) return 0;
+  const int sms = ra::num_sms();
+  size_t most = 0;
+  if (rows > 0) {
+    Shape w[3];
+    dw_shapes(w, B, rows, C, F, O);
+    // dx and the weights' gradients use the same scratch, one after the other; samples may join
+    for (int flat = 0; flat < 2; ++flat) {
+      const Shape x = dx_shape(flat ? 1 : B, flat ? B * rows : rows, C, F);
+      const size_t b = partial_bytes(x, plan_store(&x, 1, sms).parts);
+      most = b > most ? b : most;
+      dw_shapes(w, flat ? 1 : B, flat ? B * rows : rows, C, F, O);
+      const int parts = plan_store(w, 3, sms).parts;
+      const size_t c = partial_bytes(w[0], parts) + partial_bytes(w[1], parts) + partial_bytes(w[2], parts);
+      most = c > most ? c : most;
+    }
+  }
+  return size_t(2) * size_t(B) * size_t(rows) * size_t(F) * 2 + most + 16;
+}
+
+extern "C" ra_status refadapt_glu_backward(const ra_glu_grad_args* a, void* stream) {
+  using namespace ra;
+  using namespace ra::glu;
+  const char* who = "refadapt_glu_backward";
+  clear_error();
+  if (!a) {
+    set_error("%s: args is NULL", who);
+    return RA_EINVAL;
+  }
+  if (a->B < 1 || a->rows < 0 || a->C < 64 || a->C % 8 != 0 || a->F < 64 || a->F % 8 != 0 || a->O < 64 ||
+      a->O % 8 != 0 || (a->act != RA_ACT_SILU && a->act != RA_ACT_GELU)) {
+    set_error("%s: need B >= 1, rows >= 0, C, F and O multiples of 8 and at least 64, a known activation (B=%d rows=%d "
+              "C=%d F=%d O=%d act=%d)", who, a->B, a->rows, a->C, a->F, a->O, a->act);
+    return RA_EINVAL;
+  }
+  if (int64_t(a->B) * a->rows >= (int64_t(1) << 30)) {
+    set_error("%s: too many rows", who);
+    return RA_EINVAL;
+  }
+  if (!a->dx && !a->dw_gate && !a->dw_up && !a->dw_down) {
+    set_error("%s: no gradient wanted", who);
+    return RA_EINVAL;
+  }
+  if (!aligned16(a->dw_gate) || !aligned16(a->dw_up) || !aligned16(a->dw_down)) {
+    set_error("%s: the weights' gradients must be 16-byte aligned", who);
+    return RA_EINVAL;
+  }
+  const cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (a->rows == 0) {  // sums of no rows
+    const size_t fc = size_t(a->F) * a->C * 2, of = size_t(a->O) * a->F * 2;
+    cudaError_t e = cudaSuccess;
+    if (a->dw_gate) e = cudaMemsetAsync(a->dw_gate, 0, fc, st);
+    if (e == cudaSuccess && a->dw_up) e = cudaMemsetAsync(a->dw_up, 0, fc, st);
+    if (e == cudaSuccess && a->dw_down) e = cudaMemsetAsync(a->dw_down, 0, of, st);
+    if (e != cudaSuccess) {
+      set_error("%s: %s", who, cudaGetErrorString(e));
+      cudaGetLastError();
+      return RA_ECUDA;
+    }
+    return RA_OK;
+  }
+  const bool dw = a->dw_gate || a->dw_up || a->dw_down, dgw = a->dx || a->dw_gate || a->dw_up;
+  RowTensor dy{a->dy, a->dy_stride_s, a->dy_stride_r, a->B, a->rows, a->O};
+  RowTensor x{a->x, a->x_stride_s, a->x_stride_r, a->B, a->rows, a->C};
+  RowTensor g{a->pre_gate, a->pre_gate_stride_s, a->pre_gate_stride_r, a->B, a->rows, a->F};
+  RowTensor w{a->pre_up, a->pre_up_stride_s, a->pre_up_stride_r, a->B, a->rows, a->F};
+  RowTensor hid{a->hidden, a->hidden_stride_s, a->hidden_stride_r, a->B, a->rows, a->F};
+  RowTensor dx{a->dx, a->dx_stride_s, a->dx_stride_r, a->B, a->rows, a->C};
+  if (!check_rows(who, "dy", dy, false) ||
+      (dgw && (!check_rows(who, "pre_gate", g, false) || !check_rows(who, "pre_up", w, false))) ||
+      ((a->dw_gate || a->dw_up) && !check_rows(who, "x", x, false)) ||
+      (a->dw_down && !check_rows(who, "hidden", hid, false)) || (a->dx && !check_rows(who, "dx", dx, true)))
+    return RA_EINVAL;
+  if ((dgw && (!a->w_down || !aligned16(a->w_down))) ||
+      (a->dx && (!a->w_gate || !a->w_up || !aligned16(a->w_gate) || !aligned16(a->w_up)))) {
+    set_error("%s: the weights that the wanted gradients need must be given and 16-byte aligned", who);
+    return RA_EINVAL;
+  }
+  const size_t need = refadapt_glu_backward_workspace_size(a->B, a->rows, a->C, a->F, a->O);
+  if (!a->workspace || !aligned16(a->workspace) || a->workspace_bytes < need) {
+    set_error("%s: workspace NULL, not 16-byte aligned or smaller than refadapt_glu_backward_workspace_size() (%zu bytes)",
+              who, need);
+    return RA_EINVAL;
+  }
+  const int sms = num_sms();
+  const int64_t all = int64_t(a->B) * a->rows;
+  __nv_bfloat16* dg_ptr = static_cast<__nv_bfloat16*>(a->workspace);
+  __nv_bfloat16* dw_ptr = dg_ptr + all * a->F;
+  float* partial = reinterpret_cast<float*>(dw_ptr + all * a->F);
+  const int64_t ss = int64_t(a->rows) * a->F;
+  RowTensor dgt{dg_ptr, ss, a->F, a->B, a->rows, a->F}, dwt{dw_ptr, ss, a->F, a->B, a->rows, a->F};
+  const RowTensor w_gate{a->w_gate, 0, a->C, 1, a->F, a->C}, w_up{a->w_up, 0, a->C, 1, a->F, a->C};
+  const RowTensor w_down{a->w_down, 0, a->F, 1, a->O, a->F};
+  auto flatten = [](RowTensor t) {
+    t.n *= t.B;
+    t.B = 1;
+    return t;
+  };
+  Params p;
+  std::memset(&p, 0, sizeof(p));
+  p.act = a->act;
+  p.err_word = a->err_word;
+  p.budget_ns = wait_budget_ns();
+  auto rows_of = [](const RowTensor& t) {
+    return Rows{static_cast<__nv_bfloat16*>(const_cast<void*>(t.ptr)), t.ss, t.sr};
+  };
+  const int64_t pairs = sms / 2 > 0 ? sms / 2 : 1;
+  const int kb_f = int(div_up(a->F, 64));
+  if (dgw) {
+    const bool flat = joins(dy) && joins(g) && joins(w);
+    const RowTensor src = flat ? flatten(dy) : dy;
+    Job& job = p.job[0];
+    p.n_jobs = 1;
+    job.samples = src.B, job.rows = src.n;
+    job.m_tiles = int32_t(div_up(src.n, TM));
+    job.N = a->F;
+    job.kb = job.kb_first = int32_t(div_up(a->O, 64));
+    job.parts = 1;
+    job.b_mn = 1;
+    job.out[0] = rows_of(dgt), job.out[1] = rows_of(dwt);
+    job.pre_gate = rows_of(g), job.pre_up = rows_of(w);
+    double best_us = 1e30;
+    int64_t units = 0;
+    for (int bn = 256; bn >= 128; bn /= 2) {
+      const int64_t n = int64_t(job.samples) * job.m_tiles * div_up(a->F, bn);
+      const double us = fixed_us(bn) + round_us(bn, double(job.kb)) * double(div_up(n, pairs));
+      if (us < best_us) best_us = us, p.bn = bn, units = n;
+    }
+    job.cols = int32_t(div_up(a->F, p.bn));
+    if (!encode(&p.tm_a[0][0], src, 128) || !encode(&p.tm_b[0][0], w_down, 64)) return RA_EINVAL;
+    if (units > 2147483647) {
+      set_error("%s: too many rows", who);
+      return RA_EINVAL;
+    }
+    const ra_status r = launch(who, glu_kernel<GRAD>, p, units, st);
+    if (r != RA_OK) return r;
+  }
+  auto store = [&](const Shape* shapes, int n, const Plan& plan) -> ra_status {
+    p.n_jobs = n;
+    p.bn = plan.bn;
+    int64_t units = 0;
+    float* at = partial;
+    JoinParams join;
+    join.n = 0;
+    int64_t vecs = 0;
+    for (int j = 0; j < n; ++j) {
+      Job& job = p.job[j];
+      const Shape& s = shapes[j];
+      job.samples = int32_t(s.samples), job.rows = int32_t(s.M), job.N = int32_t(s.N), job.kb = int32_t(s.kb);
+      job.m_tiles = int32_t(div_up(s.M, TM));
+      job.cols = int32_t(div_up(s.N, plan.bn));
+      job.parts = plan.parts;
+      units += s.tiles(plan.bn) * plan.parts;
+      if (plan.parts > 1) {
+        job.partial = at;
+        JoinJob& q = join.job[join.n++];
+        q.partial = at;
+        q.plane = s.samples * s.M * s.N;
+        q.vecs = q.plane / 8;
+        q.parts = plan.parts, q.rows = job.rows, q.N = job.N;
+        q.out = job.out[0];
+        at += q.plane * plan.parts;
+        vecs += q.vecs;
+      }
+    }
+    if (units > 2147483647) {
+      set_error("%s: too many rows", who);
+      return RA_EINVAL;
+    }
+    const ra_status r = launch(who, glu_kernel<STORE>, p, units, st);
+    if (r != RA_OK || join.n == 0) return r;
+    cudaLaunchConfig_t cfg = {};
+    const int64_t blocks = div_up(vecs, 256), most = int64_t(8) * sms;
+    cfg.gridDim = dim3(unsigned(blocks < most ? blocks : most));
+    cfg.blockDim = dim3(256);
+    cfg.stream = st;
+    cudaLaunchAttribute attr = pdl_attribute();
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, join_kernel, join);
+    if (e != cudaSuccess) {
+      set_error("%s: launch failed: %s", who, cudaGetErrorString(e));
+      cudaGetLastError();
+      return RA_ECUDA;
+    }
+    return launch_status(who);
+  };
+  if (a->dx) {
+    const bool flat = joins(dx);
+    const Shape s = dx_shape(flat ? 1 : a->B, flat ? int(all) : a->rows, a->C, a->F);
+    const Plan plan = plan_store(&s, 1, sms);
+    std::memset(p.job, 0, sizeof(p.job));
+    p.job[0].kb_first = kb_f;
+    p.job[0].b_mn = 1;
+    p.job[0].out[0] = rows_of(dx);
+    if (!encode(&p.tm_a[0][0], flat ? flatten(dgt) : dgt, 128) || !encode(&p.tm_a[0][1], flat ? flatten(dwt) : dwt, 128) ||
+        !encode(&p.tm_b[0][0], w_gate, 64) || !encode(&p.tm_b[0][1], w_up, 64))
+      return RA_EINVAL;
+    const ra_status r = store(&s, 1, plan);
+    if (r != RA_OK) return r;
+  }
+  if (dw) {
+    const bool flat = (!(a->dw_gate || a->dw_up) || joins(x)) && (!a->dw_down || (joins(dy) && joins(hid)));
+    Shape every[3], s[3];
+    dw_shapes(every, flat ? 1 : a->B, flat ? int(all) : a->rows, a->C, a->F, a->O);
+    const Plan plan = plan_store(every, 3, sms);
+    std::memset(p.job, 0, sizeof(p.job));
+    void* out[3] = {a->dw_gate, a->dw_up, a->dw_down};
+    int n = 0;
+    for (int i = 0; i < 3; ++i) {
+      if (!out[i]) continue;
+      Job& job = p.job[n];
+      s[n] = every[i];
+      job.a_mn = job.b_mn = 1;
+      job.kb_first = int32_t(every[i].kb);
+      job.kb_sample = int32_t(div_up(flat ? all : a->rows, 64));
+      job.out[0] = Rows{static_cast<__nv_bfloat16*>(out[i]), 0, every[i].N};
+      const RowTensor at = i == 0 ? dgt : i == 1 ? dwt : dy, bt = i == 2 ? hid : x;
+      if (!encode(&p.tm_a[n][0], flat ? flatten(at) : at, 64) || !encode(&p.tm_b[n][0], flat ? flatten(bt) : bt, 64))
+        return RA_EINVAL;
+      ++n;
+    }
+    const ra_status r = store(s, n, plan);
+    if (r != RA_OK) return r;
+  }
+  return RA_OK;
+}
