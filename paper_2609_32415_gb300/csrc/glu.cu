@@ -17,9 +17,9 @@
 // An operand whose K runs along its rows (Wd, Wg, Wu as B, the rows of every
 // operand of a weight's gradient) is read as it lies, MN-major: nothing is
 // transposed in memory.
-//   warp 0      TMA producer: per stage 128 of K, as two chunks of 64, of the
-//               CTA's 128 A rows and its half of the B tile (128-byte swizzle;
-//               what lies past an edge is read as zeros).
+//   warp 0      TMA producer: per stage 128 of K of the CTA's 128 A rows and of
+//               its half of the B tile, two boxes each (128-byte swizzle; what
+//               lies past an edge is read as zeros).
 //   warp 1      TMEM allocator (two accumulators of 256 columns) and MMA issuer
 //               (rank 0's).
 //   warps 2..9  epilogue, two warps per TMEM lane quarter, while the next tile's
@@ -42,9 +42,9 @@ namespace glu {
 constexpr int TM = 256;              // output rows of a pair's tile
 constexpr int MAX_BN = 256;          // accumulator columns
 constexpr int STAGES = 3;
-constexpr int BK = 128;              // K per stage, two chunks of 64
-constexpr int CHUNK = 128 * 64 * 2;  // 128 rows (or columns) x 64 of K of one operand
-constexpr int OPERAND_BYTES = 2 * CHUNK;
+constexpr int BK = 128;              // K per stage
+constexpr int BOX = 128 * 64 * 2;    // K-major: 128 rows x 64 of K; MN-major: 128 of K x 64 columns
+constexpr int OPERAND_BYTES = 2 * BOX;
 constexpr int STAGE_BYTES = 2 * OPERAND_BYTES;
 constexpr int OFF_BAR = STAGES * STAGE_BYTES;
 constexpr int NUM_BARS = 2 * STAGES + 2 + 2 + 1;  // full, empty, tfull[2], tempty[2], drain
@@ -70,17 +70,18 @@ struct Job {
   int32_t samples, rows, gated;  // output rows per sample
   int32_t m_tiles, cols;         // row and column tiles of a sample
   int32_t N;                     // output columns
-  int32_t kb, kb_first;          // K steps of 64: all, and those of the first operand pair
-  int32_t kb_sample;             // K steps of a sample where K runs along the rows, else 0
-  int32_t parts;                 // of K
-  int32_t a_mn, b_mn;            // operands whose K runs along their rows
+  // K is `spans` runs of span_k, each of span_stages stages: one run; dx: one per
+  // operand pair; a weight's gradient: one per sample (K runs along the rows).
+  int32_t spans, span_k, span_stages;
+  int32_t parts;                 // of K, whole stages each
+  int32_t rows_k;                // K runs along the rows of both operands
   Rows out[3];                   // GLU: out, pre_gate, pre_up; GRAD: dg, dw; STORE: the result
   Rows pre_gate, pre_up;         // GRAD
   float* partial;                // parts > 1: [part][sample][row][N]
 };
 
 struct Params {
-  int32_t n_jobs, bn, act;
+  int32_t n_jobs, bn;
   const int32_t* mode;
   int32_t* err_word;
   uint64_t budget_ns;
@@ -91,7 +92,7 @@ struct Params {
 };
 
 struct Unit {
-  int job, s, m0, n0, part, k0, k1;
+  int job, s, m0, n0, part, k0, k1;  // k0, k1: stages
 };
 
 // Walks the units (a tile's part of K) of the live jobs and samples in order;
@@ -127,25 +128,49 @@ struct Walk {
     u.m0 = (m_first + int(in_band % rows)) * TM;
     u.n0 = int(in_band / rows) * (KIND == GLU ? p.bn / 2 : p.bn);
     u.part = int(idx - tile * uint32_t(job.parts));
-    u.k0 = int(int64_t(job.kb) * u.part / job.parts);
-    u.k1 = int(int64_t(job.kb) * (u.part + 1) / job.parts);
+    const int64_t stages = int64_t(job.spans) * job.span_stages;
+    u.k0 = int(stages * u.part / job.parts);
+    u.k1 = int(stages * (u.part + 1) / job.parts);
     return true;
   }
 };
 
-// act(g) = g s and act'(g) = s + g s (1 - s) z'(g) with s = 1 / (1 + e^-z):
-// z = g for SiLU; for GELU's tanh form 0.5 (1 + tanh(v)) = 1 / (1 + e^-2v), so
-// z = 2 sqrt(2/pi) (g + 0.044715 g^3). An exponential that overflows gives s = 0.
-__device__ __forceinline__ float sigmoid_of(int act, float g, float& dz) {
-  constexpr float log2e = 1.4426950408889634f, c = 2.f * 0.7978845608028654f;
-  float z = g;
-  dz = 1.f;
-  if (act == RA_ACT_GELU) {
-    const float g2 = g * g;
-    z = c * g * fmaf(0.044715f, g2, 1.f);
-    dz = c * fmaf(3.f * 0.044715f, g2, 1.f);
+// Two values at once of act(g) = g s and act'(g) = s + g s (1 - s) z'(g), with
+// s = 1 / (1 + e^-z): z = g for SiLU; for GELU's tanh form 0.5 (1 + tanh(v)) =
+// 1 / (1 + e^-2v), so z = 2 sqrt(2/pi) (g + 0.044715 g^3). An exponential that
+// overflows gives s = 0. The exponential and the reciprocal are the approximate
+// instructions, good to about 2^-22, which a bf16 result does not see.
+template <int ACT>
+__device__ __forceinline__ uint64_t act2(uint64_t g, uint64_t* grad) {
+  constexpr float log2e = 1.4426950408889634f, c = 2.f * 0.7978845608028654f, c3 = 0.044715f * c;
+  uint64_t z, q;
+  if constexpr (ACT == RA_ACT_GELU) {
+    q = f2_mul(g, g);
+    z = f2_mul(g, f2_fma(q, f2_pack(-log2e * c3, -log2e * c3), f2_pack(-log2e * c, -log2e * c)));
+  } else {
+    z = f2_mul(g, f2_pack(-log2e, -log2e));
   }
-  return rcp_approx(1.f + ex2_approx(-log2e * z));
+  float z0, z1;
+  f2_unpack(z, z0, z1);
+  f2_unpack(f2_add(f2_pack(ex2_approx(z0), ex2_approx(z1)), f2_pack(1.f, 1.f)), z0, z1);
+  const uint64_t s = f2_pack(rcp_approx(z0), rcp_approx(z1)), a = f2_mul(g, s);
+  if (grad) {
+    const uint64_t t = f2_fma(f2_mul(a, f2_pack(-1.f, -1.f)), s, a);
+    if constexpr (ACT == RA_ACT_GELU)
+      *grad = f2_fma(t, f2_fma(q, f2_pack(3.f * c3, 3.f * c3), f2_pack(c, c)), s);
+    else
+      *grad = f2_add(t, s);
+  }
+  return a;
+}
+
+__device__ __forceinline__ uint32_t f2_bf16(uint64_t v) {
+  float a, b;
+  f2_unpack(v, a, b);
+  return pack_bf16x2(a, b);
+}
+__device__ __forceinline__ uint64_t f2_regs(const uint32_t (&v)[32], int i) {
+  return f2_pack(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1]));
 }
 
 // What an epilogue warp works on: its 32 rows (row0 + lane, nrow of them in the
@@ -161,7 +186,7 @@ __device__ __forceinline__ char* row_ptr(const Rows& r, int s, int row, int col)
   return reinterpret_cast<char*>(r.ptr + s * r.ss + row * r.sr + col);
 }
 
-template <class Ready>
+template <int ACT, class Ready>
 __device__ __forceinline__ bool epilogue_glu(const Params& p, const Unit& u, const EpiWarp& w, Ready ready) {
   const Job& job = p.job[u.job];
   const int width = p.bn / 2;
@@ -178,28 +203,23 @@ __device__ __forceinline__ bool epilogue_glu(const Params& p, const Unit& u, con
     tmem_ld_wait_for(g);
     tmem_ld_wait_for(v);
     uint4 own[4];
+    uint32_t* o = reinterpret_cast<uint32_t*>(own);
     if (save) {
-      uint32_t* o = reinterpret_cast<uint32_t*>(own);
 #pragma unroll
-      for (int i = 0; i < 16; ++i) o[i] = pack_bf16x2(__uint_as_float(g[2 * i]), __uint_as_float(g[2 * i + 1]));
+      for (int i = 0; i < 16; ++i) o[i] = f2_bf16(f2_regs(g, i));
       rows_put(w.stage, own, row_ptr(job.out[1], u.s, w.row0, col), 2 * job.out[1].sr, w.nrow, ncol);
 #pragma unroll
-      for (int i = 0; i < 16; ++i) o[i] = pack_bf16x2(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1]));
+      for (int i = 0; i < 16; ++i) o[i] = f2_bf16(f2_regs(v, i));
       rows_put(w.stage, own, row_ptr(job.out[2], u.s, w.row0, col), 2 * job.out[2].sr, w.nrow, ncol);
     }
-    float x[32];
 #pragma unroll
-    for (int i = 0; i < 32; ++i) {
-      float dz;
-      const float gi = __uint_as_float(g[i]);
-      x[i] = gi * sigmoid_of(p.act, gi, dz) * __uint_as_float(v[i]);
-    }
-    rows_store(w.stage, x, row_ptr(job.out[0], u.s, w.row0, col), 2 * job.out[0].sr, w.nrow, ncol);
+    for (int i = 0; i < 16; ++i) o[i] = f2_bf16(f2_mul(act2<ACT>(f2_regs(g, i), nullptr), f2_regs(v, i)));
+    rows_put(w.stage, own, row_ptr(job.out[0], u.s, w.row0, col), 2 * job.out[0].sr, w.nrow, ncol);
   }
   return true;
 }
 
-template <class Ready>
+template <int ACT, class Ready>
 __device__ __forceinline__ bool epilogue_grad(const Params& p, const Unit& u, const EpiWarp& w, Ready ready) {
   const Job& job = p.job[u.job];
   auto cols = [&](int c) { return c < p.bn ? min(32, job.N - u.n0 - c) : 0; };
@@ -226,19 +246,10 @@ __device__ __forceinline__ bool epilogue_grad(const Params& p, const Unit& u, co
     uint32_t* wp = reinterpret_cast<uint32_t*>(own_w);
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      float dg[2], dw[2];
-#pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        const float g = __uint_as_float(k ? gp[i] & 0xFFFF0000u : gp[i] << 16);
-        const float up = __uint_as_float(k ? wp[i] & 0xFFFF0000u : wp[i] << 16);
-        const float du = __uint_as_float(v[2 * i + k]);
-        float dz;
-        const float s = sigmoid_of(p.act, g, dz), a = g * s;
-        dg[k] = du * up * fmaf(a * (1.f - s), dz, s);
-        dw[k] = du * a;
-      }
-      gp[i] = pack_bf16x2(dg[0], dg[1]);
-      wp[i] = pack_bf16x2(dw[0], dw[1]);
+      uint64_t da;
+      const uint64_t a = act2<ACT>(bf2_unpack(gp[i]), &da), du = f2_regs(v, i);
+      gp[i] = f2_bf16(f2_mul(f2_mul(du, bf2_unpack(wp[i])), da));
+      wp[i] = f2_bf16(f2_mul(du, a));
     }
     const int ncol = cols(c);
     rows_put(w.stage, own_g, row_ptr(job.out[0], u.s, w.row0, u.n0 + c), 2 * job.out[0].sr, w.nrow, ncol);
@@ -280,18 +291,110 @@ __device__ __forceinline__ bool epilogue_store(const Params& p, const Unit& u, c
   return true;
 }
 
-// One operand's chunk of 64 of K: `rows` of its rows (K-major; the box has them),
-// or its columns in blocks of 64 (MN-major: 64 rows of K each).
-__device__ __forceinline__ void load_chunk(uint8_t* dst, const CUtensorMap* tm, uint32_t bar, bool mn, int at, int n,
-                                           int k, int s) {
-  if (!mn) {
-    tma_load_4d_pair(dst, tm, bar, k, at, 0, s);
-  } else {
-    for (int c = 0; c < n; c += 64) tma_load_4d_pair(dst + c * 128, tm, bar, at + c, k, 0, s);
-  }
-}
-
+// ------------------------------------------------------------------ pipeline
+// The majorness of a job's operands: A and B of a weight's gradient are MN-major
+// (both rows run along K), so is B where a weight is used untransposed.
 template <int KIND>
+constexpr bool kBRowsK = KIND != GLU;
+
+// Loads of a unit's stages. it: stages issued so far.
+struct Producer {
+  uint8_t* smem;
+  uint64_t *full, *empty;
+  uint32_t full0;  // rank 0's full barriers
+  int rank;
+  int64_t it = 0;
+
+  template <int KIND, bool A_MN>
+  __device__ __forceinline__ bool unit(const Params& p, const Unit& u, const WaitCtl& ctl) {
+    constexpr bool B_MN = kBRowsK<KIND>;
+    const Job& job = p.job[u.job];
+    const int half = p.bn / 2;  // columns of B that a CTA stages
+    const uint32_t b_box = B_MN ? uint32_t(BOX) : uint32_t(half) * 128u;
+    const int b_boxes = B_MN ? half / 64 : 2;
+    const int m = u.m0 + rank * 128, n = u.n0 + (KIND == GLU ? 0 : rank * half);
+    int span = u.k0 / job.span_stages, k = (u.k0 - span * job.span_stages) * BK;
+    for (int q = u.k0; q < u.k1; ++q, ++it) {
+      const int st = int(it % STAGES);
+      if (it >= STAGES && !mbar_wait(empty + st, uint32_t((it / STAGES - 1) & 1), ctl)) return false;
+      uint8_t* sa = smem + st * STAGE_BYTES;
+      uint8_t* sb = sa + OPERAND_BYTES;
+      const uint32_t bar = full0 + 8u * st;
+      const int pair = KIND == STORE && !A_MN ? span : 0;  // dx: the operand pair
+      const int ks = A_MN ? span : u.s;                    // sample of A
+      const bool second = job.span_k - k > 64;             // K-major: the second box lies inside
+      const CUtensorMap* ta = &p.tm_a[u.job][pair];
+      const CUtensorMap* tb = &p.tm_b[u.job][KIND == GLU ? rank : pair];
+      if (rank == 0)
+        mbar_arrive_expect_tx(full + st, 2u * ((A_MN || second ? 2u : 1u) * uint32_t(BOX) +
+                                               (B_MN || second ? uint32_t(b_boxes) : 1u) * b_box));
+      if (A_MN) {
+        tma_load_4d_pair(sa, ta, bar, m, k, 0, ks);
+        tma_load_4d_pair(sa + BOX, ta, bar, m + 64, k, 0, ks);
+      } else {
+        tma_load_4d_pair(sa, ta, bar, k, m, 0, ks);
+        if (second) tma_load_4d_pair(sa + BOX, ta, bar, k + 64, m, 0, ks);
+      }
+      if (B_MN) {
+        tma_load_4d_pair(sb, tb, bar, n, k, 0, A_MN ? ks : 0);
+        if (b_boxes > 1) tma_load_4d_pair(sb + BOX, tb, bar, n + 64, k, 0, A_MN ? ks : 0);
+      } else {
+        tma_load_4d_pair(sb, tb, bar, k, n, 0, 0);
+        if (second) tma_load_4d_pair(sb + BOX, tb, bar, k + 64, n, 0, 0);
+      }
+      k += BK;
+      if (k >= job.span_k) k = 0, ++span;
+    }
+    return true;
+  }
+};
+
+// MMAs of a unit's stages into the accumulator at d_t.
+struct Issuer {
+  uint32_t s0;
+  uint64_t *full, *empty;
+  int64_t it = 0;
+  bool issued = false;
+
+  template <int KIND, bool A_MN>
+  __device__ __forceinline__ bool unit(const Params& p, const Unit& u, uint32_t d_t, const WaitCtl& ctl) {
+    constexpr bool B_MN = kBRowsK<KIND>;
+    const Job& job = p.job[u.job];
+    const uint32_t idesc = idesc_bf16_f32(TM, p.bn, A_MN, B_MN);
+    // A step of 16 of K, in descriptor units of 16 bytes: 32 bytes of a K-major
+    // row (64 of K, then the next box), 16 rows of 128 bytes of an MN-major box
+    // (whose next 64 columns are the next box).
+    const uint64_t da = sdesc_sw128(s0, A_MN ? BOX : 16, 1024);
+    const uint64_t db = sdesc_sw128(s0 + OPERAND_BYTES, B_MN ? BOX : 16, 1024);
+    int k = (u.k0 % job.span_stages) * BK;
+    for (int q = u.k0; q < u.k1; ++q, ++it) {
+      const int st = int(it % STAGES);
+      if (!mbar_wait(full + st, uint32_t((it / STAGES) & 1), ctl)) return false;
+      tc_fence_after();
+      const uint64_t a = da + uint64_t(st * (STAGE_BYTES >> 4)), b = db + uint64_t(st * (STAGE_BYTES >> 4));
+      const int left = job.span_k - k;
+      auto step = [&](int kk) {
+        const uint32_t oa = A_MN ? kk * 128 : (kk >> 2) * (BOX >> 4) + (kk & 3) * 2;
+        const uint32_t ob = B_MN ? kk * 128 : (kk >> 2) * (BOX >> 4) + (kk & 3) * 2;
+        umma_ss_pair(d_t, a + oa, b + ob, idesc, (q > u.k0 || kk > 0) ? 1u : 0u);
+      };
+      if (left >= BK) {
+#pragma unroll
+        for (int kk = 0; kk < BK / 16; ++kk) step(kk);
+      } else {
+#pragma unroll 1
+        for (int kk = 0; 16 * kk < left; ++kk) step(kk);
+      }
+      umma_commit_pair(empty + st, 0x3);
+      issued = true;
+      k += BK;
+      if (k >= job.span_k) k = 0;
+    }
+    return true;
+  }
+};
+
+template <int KIND, int ACT>
 __global__ void __launch_bounds__(THREADS, 1) glu_kernel(const __grid_constant__ Params p) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
@@ -338,33 +441,17 @@ __global__ void __launch_bounds__(THREADS, 1) glu_kernel(const __grid_constant__
           tma_prefetch_desc(&p.tm_b[j][0]);
         }
       pdl_wait();
-      const uint32_t full0 = mapa_shared(smem_u32(full), 0);  // rank 0's full barriers
-      const int half = p.bn / 2;                              // columns of B that a CTA stages
-      int64_t it = 0;
+      Producer pr{smem, full, empty, mapa_shared(smem_u32(full), 0), int(rank)};
       bool ok = true;
       Walk<KIND> walk;
       Unit u;
       for (int64_t t = cid; ok && walk.at(p, t, u); t += ncl) {
-        const Job& job = p.job[u.job];
-        const uint32_t chunk_bytes = 2u * (CHUNK + uint32_t(job.b_mn ? (half + 63) / 64 * 64 : half) * 128u);
-        for (int kb = u.k0; kb < u.k1; kb += 2, ++it) {
-          const int st = int(it % STAGES);
-          if (it >= STAGES && !(ok = mbar_wait(empty + st, uint32_t((it / STAGES - 1) & 1), ctl))) break;
-          uint8_t* sa = smem + st * STAGE_BYTES;
-          const int chunks = min(2, u.k1 - kb);  // the last stage may be half
-          if (rank == 0) mbar_arrive_expect_tx(full + st, chunks * chunk_bytes);
-          for (int c = 0; c < chunks; ++c) {
-            const int pair = KIND == STORE && kb + c >= job.kb_first;
-            const int local = kb + c - (pair ? job.kb_first : 0);
-            const int ks = job.kb_sample ? local / job.kb_sample : u.s;  // the sample that K lies in
-            const int k = 64 * (job.kb_sample ? local - ks * job.kb_sample : local);
-            load_chunk(sa + c * CHUNK, &p.tm_a[u.job][pair], full0 + 8u * st, job.a_mn, u.m0 + int(rank) * 128, 128, k,
-                       ks);
-            load_chunk(sa + OPERAND_BYTES + c * CHUNK, &p.tm_b[u.job][KIND == GLU ? int(rank) : pair], full0 + 8u * st,
-                       job.b_mn, u.n0 + (KIND == GLU ? 0 : int(rank) * half), half, k, job.kb_sample ? ks : 0);
-          }
-        }
+        if (KIND == STORE && p.job[u.job].rows_k)
+          ok = pr.unit<KIND, KIND == STORE>(p, u, ctl);
+        else
+          ok = pr.unit<KIND, false>(p, u, ctl);
       }
+      const int64_t it = pr.it;
       if (*abort_flag) {
         if (rank == 0) {
           // rank 0's full barriers count both CTAs' bytes of every phase it armed
@@ -383,44 +470,25 @@ __global__ void __launch_bounds__(THREADS, 1) glu_kernel(const __grid_constant__
   } else if (warp == 1) {
     if (lane == 0 && rank == 0) {
       // -------------------------------------------------------------- MMA issuer (rank 0)
-      const uint32_t s0 = smem_u32(smem);
-      int64_t it = 0;
+      Issuer mma{smem_u32(smem), full, empty};
       int i = 0;
-      bool ok = true, issued = false;
+      bool ok = true;
       Walk<KIND> walk;
       Unit u;
-      for (int64_t t = cid; ok && walk.at(p, t, u); t += ncl) {
-        const Job& job = p.job[u.job];
+      for (int64_t t = cid; walk.at(p, t, u); t += ncl) {
         const int buf = i & 1, use = i >> 1;
-        const uint32_t idesc = idesc_bf16_f32(TM, p.bn, job.a_mn, job.b_mn);
-        // A step of 16 of K: 32 bytes of a K-major row; 16 rows of 128 bytes of an
-        // MN-major block, whose blocks of 64 columns are 64 rows (8 KB) apart.
-        const uint32_t a_step = job.a_mn ? 2048 : 32, a_lbo = job.a_mn ? 8192 : 16;
-        const uint32_t b_step = job.b_mn ? 2048 : 32, b_lbo = job.b_mn ? 8192 : 16;
         if (use > 0 && !(ok = mbar_wait_cluster(tempty + buf, uint32_t((use - 1) & 1), ctl))) break;
         tc_fence_after();
         const uint32_t d_t = tmem + uint32_t(buf * MAX_BN);
-        for (int kb = u.k0; kb < u.k1; kb += 2, ++it) {
-          const int st = int(it % STAGES);
-          if (!(ok = mbar_wait(full + st, uint32_t((it / STAGES) & 1), ctl))) break;
-          tc_fence_after();
-          const uint32_t sa = s0 + st * STAGE_BYTES, sb = sa + OPERAND_BYTES;
-          const int ksteps = min(2, u.k1 - kb) * 4;
-#pragma unroll
-          for (int kk = 0; kk < BK / 16; ++kk) {
-            if (kk >= ksteps) break;
-            const uint32_t o = uint32_t(kk >> 2) * CHUNK;
-            umma_ss_pair(d_t, sdesc_sw128(sa + o + (kk & 3) * a_step, a_lbo, 1024),
-                         sdesc_sw128(sb + o + (kk & 3) * b_step, b_lbo, 1024), idesc, (kb > u.k0 || kk > 0) ? 1u : 0u);
-          }
-          umma_commit_pair(empty + st, 0x3);
-          issued = true;
-        }
+        if (KIND == STORE && p.job[u.job].rows_k)
+          ok = mma.unit<KIND, KIND == STORE>(p, u, d_t, ctl);
+        else
+          ok = mma.unit<KIND, false>(p, u, d_t, ctl);
         if (!ok) break;
         umma_commit_pair(tfull + buf, 0x3);
         ++i;
       }
-      if (!ok && issued) {
+      if (!ok && mma.issued) {
         umma_commit_pair(drain, 0x1);
         mbar_wait_drain(drain, 0, p.budget_ns);
       }
@@ -447,9 +515,9 @@ __global__ void __launch_bounds__(THREADS, 1) glu_kernel(const __grid_constant__
       };
       bool ok;
       if constexpr (KIND == GLU)
-        ok = epilogue_glu(p, u, w, ready);
+        ok = epilogue_glu<ACT>(p, u, w, ready);
       else if constexpr (KIND == GRAD)
-        ok = epilogue_grad(p, u, w, ready);
+        ok = epilogue_grad<ACT>(p, u, w, ready);
       else
         ok = epilogue_store(p, u, w, ready);
       if (!ok) break;
@@ -527,10 +595,16 @@ bool check_rows(const char* who, const char* what, const RowTensor& t, bool outp
 // The samples' rows follow one another: B samples of n rows are one of B n.
 bool joins(const RowTensor& t) { return t.B == 1 || t.ss == t.n * t.sr; }
 
-// Tensor map of a row tensor: boxes of 64 features x box_rows.
+// Tensor map of a row tensor: boxes of 64 features x box_rows (MN-major: 128 of K).
 bool encode(CUtensorMap* tm, const RowTensor& t, int box_rows) {
   const ra_seg s{const_cast<void*>(t.ptr), t.B > 1 ? t.ss : 0, 0, t.sr, t.n, 0};
   return encode_seg(tm, s, t.B, 1, t.cols, 64, box_rows, true);
+}
+
+void one_span(Job& job, int k) {
+  job.spans = job.parts = 1;
+  job.span_k = k;
+  job.span_stages = (k + BK - 1) / BK;
 }
 
 ra_status launch(const char* who, void (*fn)(Params), const Params& p, int64_t units, cudaStream_t st) {
@@ -559,19 +633,19 @@ ra_status launch(const char* who, void (*fn)(Params), const Params& p, int64_t u
   return launch_status(who);
 }
 
-// Microseconds of a round of tiles of bn columns over kb steps of 64 of K, and
-// of a launch around its rounds: fitted to single waves on a GB300.
-double round_us(int bn, double kb) {
-  const double mma = kb / 16.0 * (3.11 + 0.00766 * bn), epilogue = 0.0085 * bn;
+// Microseconds of a round of tiles of bn columns over `stages` of K, and of a
+// launch around its rounds: fitted to single waves on a GB300.
+double round_us(int bn, double stages) {
+  const double mma = stages / 8.0 * (3.11 + 0.00766 * bn), epilogue = 0.0085 * bn;
   return mma > epilogue ? mma : epilogue;
 }
 double fixed_us(int bn) { return 4.4 + 0.0088 * bn; }
 
 int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// A product whose result is stored: M x N over kb steps.
+// A product whose result is stored: M x N over `stages` of K.
 struct Shape {
-  int64_t samples, M, N, kb;
+  int64_t samples, M, N, stages;
   int64_t tiles(int bn) const { return samples * div_up(M, TM) * div_up(N, bn); }
 };
 // Accumulator columns and parts of K of a launch of up to three products with
@@ -590,8 +664,8 @@ Plan plan_store(const Shape* s, int n, int sms) {
       int64_t tiles = 0;
       bool fits = true;
       for (int i = 0; i < n; ++i) {
-        fits &= parts == 1 || s[i].kb >= 4 * parts;
-        const double r = round_us(bn, double(s[i].kb) / parts);
+        fits &= parts == 1 || s[i].stages >= 2 * parts;
+        const double r = round_us(bn, double(s[i].stages) / parts);
         tiles += s[i].tiles(bn) * parts;
         work += r * double(s[i].tiles(bn) * parts);
         longest = r > longest ? r : longest;
@@ -611,11 +685,11 @@ Plan plan_store(const Shape* s, int n, int sms) {
 
 // Products of refadapt_glu_backward after dy Wd: dx, and the weights' gradients.
 // Rows that follow one another are one sample (`flat`).
-Shape dx_shape(int B, int rows, int C, int F) { return Shape{B, rows, C, 2 * div_up(F, 64)}; }
+Shape dx_shape(int B, int rows, int C, int F) { return Shape{B, rows, C, 2 * div_up(F, BK)}; }
 void dw_shapes(Shape (&s)[3], int B, int rows, int C, int F, int O) {
-  const int64_t kb = B * div_up(rows, 64);
-  s[0] = s[1] = Shape{1, F, C, kb};
-  s[2] = Shape{1, O, F, kb};
+  const int64_t stages = B * div_up(rows, BK);
+  s[0] = s[1] = Shape{1, F, C, stages};
+  s[2] = Shape{1, O, F, stages};
 }
 size_t partial_bytes(const Shape& s, int parts) {
   return parts > 1 ? size_t(parts) * size_t(s.samples) * size_t(s.M) * size_t(s.N) * 4 : 0;
@@ -641,7 +715,6 @@ extern "C" ra_status refadapt_glu(const ra_glu_args* a, void* stream) {
   }
   Params p;
   std::memset(&p, 0, sizeof(p));
-  p.act = a->act;
   p.mode = a->mode;
   p.err_word = a->err_word;
   p.budget_ns = wait_budget_ns();
@@ -692,8 +765,7 @@ extern "C" ra_status refadapt_glu(const ra_glu_args* a, void* stream) {
     job.gated = s.gated ? 1 : 0;
     job.m_tiles = int32_t(div_up(r.n, TM));
     job.N = a->F;
-    job.kb = job.kb_first = int32_t(div_up(a->C, 64));
-    job.parts = 1;
+    one_span(job, a->C);
     for (int i = 0; i < outs; ++i)
       job.out[i] = Rows{static_cast<__nv_bfloat16*>(const_cast<void*>(o[i].ptr)), o[i].ss, o[i].sr};
   }
@@ -704,7 +776,7 @@ extern "C" ra_status refadapt_glu(const ra_glu_args* a, void* stream) {
   for (int bn = 256; bn >= 64; bn -= 64) {
     int64_t n = 0;
     for (int j = 0; j < p.n_jobs; ++j) n += int64_t(p.job[j].samples) * p.job[j].m_tiles * div_up(a->F, bn / 2);
-    const double us = fixed_us(bn) + round_us(bn, double(p.job[0].kb)) * double(div_up(n, pairs));
+    const double us = fixed_us(bn) + round_us(bn, double(p.job[0].span_stages)) * double(div_up(n, pairs));
     if (us < best_us) best_us = us, p.bn = bn, units = n;
   }
   for (int g = 0, j = 0; g < a->n_seg; ++g) {
@@ -722,7 +794,7 @@ extern "C" ra_status refadapt_glu(const ra_glu_args* a, void* stream) {
     return RA_EINVAL;
   }
   note_launch("CTA pairs, %d columns", p.bn / 2);
-  return launch(who, glu_kernel<GLU>, p, units, static_cast<cudaStream_t>(stream));
+  return launch(who, a->act == RA_ACT_GELU ? glu_kernel<GLU, RA_ACT_GELU> : glu_kernel<GLU, RA_ACT_SILU>, p, units, static_cast<cudaStream_t>(stream));
 }
 
 extern "C" size_t refadapt_glu_backward_workspace_size(int32_t B, int32_t rows, int32_t C, int32_t F, int32_t O) {
@@ -827,14 +899,12 @@ extern "C" ra_status refadapt_glu_backward(const ra_glu_grad_args* a, void* stre
   };
   Params p;
   std::memset(&p, 0, sizeof(p));
-  p.act = a->act;
   p.err_word = a->err_word;
   p.budget_ns = wait_budget_ns();
   auto rows_of = [](const RowTensor& t) {
     return Rows{static_cast<__nv_bfloat16*>(const_cast<void*>(t.ptr)), t.ss, t.sr};
   };
   const int64_t pairs = sms / 2 > 0 ? sms / 2 : 1;
-  const int kb_f = int(div_up(a->F, 64));
   if (dgw) {
     const bool flat = joins(dy) && joins(g) && joins(w);
     const RowTensor src = flat ? flatten(dy) : dy;
@@ -843,25 +913,24 @@ extern "C" ra_status refadapt_glu_backward(const ra_glu_grad_args* a, void* stre
     job.samples = src.B, job.rows = src.n;
     job.m_tiles = int32_t(div_up(src.n, TM));
     job.N = a->F;
-    job.kb = job.kb_first = int32_t(div_up(a->O, 64));
-    job.parts = 1;
-    job.b_mn = 1;
+    one_span(job, a->O);
     job.out[0] = rows_of(dgt), job.out[1] = rows_of(dwt);
     job.pre_gate = rows_of(g), job.pre_up = rows_of(w);
     double best_us = 1e30;
     int64_t units = 0;
     for (int bn = 256; bn >= 128; bn /= 2) {
       const int64_t n = int64_t(job.samples) * job.m_tiles * div_up(a->F, bn);
-      const double us = fixed_us(bn) + round_us(bn, double(job.kb)) * double(div_up(n, pairs));
+      const double us = fixed_us(bn) + round_us(bn, double(job.span_stages)) * double(div_up(n, pairs));
       if (us < best_us) best_us = us, p.bn = bn, units = n;
     }
     job.cols = int32_t(div_up(a->F, p.bn));
-    if (!encode(&p.tm_a[0][0], src, 128) || !encode(&p.tm_b[0][0], w_down, 64)) return RA_EINVAL;
+    if (!encode(&p.tm_a[0][0], src, 128) || !encode(&p.tm_b[0][0], w_down, BK)) return RA_EINVAL;
     if (units > 2147483647) {
       set_error("%s: too many rows", who);
       return RA_EINVAL;
     }
-    const ra_status r = launch(who, glu_kernel<GRAD>, p, units, st);
+    const ra_status r = launch(who, a->act == RA_ACT_GELU ? glu_kernel<GRAD, RA_ACT_GELU> : glu_kernel<GRAD, RA_ACT_SILU>, p,
+                               units, st);
     if (r != RA_OK) return r;
   }
   auto store = [&](const Shape* shapes, int n, const Plan& plan) -> ra_status {
@@ -875,7 +944,7 @@ extern "C" ra_status refadapt_glu_backward(const ra_glu_grad_args* a, void* stre
     for (int j = 0; j < n; ++j) {
       Job& job = p.job[j];
       const Shape& s = shapes[j];
-      job.samples = int32_t(s.samples), job.rows = int32_t(s.M), job.N = int32_t(s.N), job.kb = int32_t(s.kb);
+      job.samples = int32_t(s.samples), job.rows = int32_t(s.M), job.N = int32_t(s.N);
       job.m_tiles = int32_t(div_up(s.M, TM));
       job.cols = int32_t(div_up(s.N, plan.bn));
       job.parts = plan.parts;
@@ -896,7 +965,7 @@ extern "C" ra_status refadapt_glu_backward(const ra_glu_grad_args* a, void* stre
       set_error("%s: too many rows", who);
       return RA_EINVAL;
     }
-    const ra_status r = launch(who, glu_kernel<STORE>, p, units, st);
+    const ra_status r = launch(who, glu_kernel<STORE, 0>, p, units, st);
     if (r != RA_OK || join.n == 0) return r;
     cudaLaunchConfig_t cfg = {};
     const int64_t blocks = div_up(vecs, 256), most = int64_t(8) * sms;
@@ -919,11 +988,11 @@ extern "C" ra_status refadapt_glu_backward(const ra_glu_grad_args* a, void* stre
     const Shape s = dx_shape(flat ? 1 : a->B, flat ? int(all) : a->rows, a->C, a->F);
     const Plan plan = plan_store(&s, 1, sms);
     std::memset(p.job, 0, sizeof(p.job));
-    p.job[0].kb_first = kb_f;
-    p.job[0].b_mn = 1;
+    one_span(p.job[0], a->F);
+    p.job[0].spans = 2;
     p.job[0].out[0] = rows_of(dx);
     if (!encode(&p.tm_a[0][0], flat ? flatten(dgt) : dgt, 128) || !encode(&p.tm_a[0][1], flat ? flatten(dwt) : dwt, 128) ||
-        !encode(&p.tm_b[0][0], w_gate, 64) || !encode(&p.tm_b[0][1], w_up, 64))
+        !encode(&p.tm_b[0][0], w_gate, BK) || !encode(&p.tm_b[0][1], w_up, BK))
       return RA_EINVAL;
     const ra_status r = store(&s, 1, plan);
     if (r != RA_OK) return r;
@@ -940,12 +1009,12 @@ extern "C" ra_status refadapt_glu_backward(const ra_glu_grad_args* a, void* stre
       if (!out[i]) continue;
       Job& job = p.job[n];
       s[n] = every[i];
-      job.a_mn = job.b_mn = 1;
-      job.kb_first = int32_t(every[i].kb);
-      job.kb_sample = int32_t(div_up(flat ? all : a->rows, 64));
+      one_span(job, flat ? int(all) : a->rows);
+      job.spans = flat ? 1 : a->B;
+      job.rows_k = 1;
       job.out[0] = Rows{static_cast<__nv_bfloat16*>(out[i]), 0, every[i].N};
       const RowTensor at = i == 0 ? dgt : i == 1 ? dwt : dy, bt = i == 2 ? hid : x;
-      if (!encode(&p.tm_a[n][0], flat ? flatten(at) : at, 64) || !encode(&p.tm_b[n][0], flat ? flatten(bt) : bt, 64))
+      if (!encode(&p.tm_a[n][0], flat ? flatten(at) : at, BK) || !encode(&p.tm_b[n][0], flat ? flatten(bt) : bt, BK))
         return RA_EINVAL;
       ++n;
     }
