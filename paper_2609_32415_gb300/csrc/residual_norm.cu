@@ -57,7 +57,7 @@ struct Seg {
 
 struct Params {
   int32_t n_seg, B, C, post, pre;
-  int32_t warps, groups;  // warps of a group, groups of a CTA
+  int32_t groups;  // of a CTA
   float eps, alpha;
   const int32_t* mode;
   Seg seg[3];
@@ -65,7 +65,7 @@ struct Params {
 
 struct GradParams {
   int32_t B, C, rows, post, pre;
-  int32_t warps, groups;
+  int32_t groups;
   int32_t parts;  // CTAs that share a sample's rows
   float eps, alpha;
   const __nv_bfloat16 *h, *y, *dx, *dh_out;
@@ -87,51 +87,73 @@ __device__ __forceinline__ void cp_async_wait() {
   asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
 
-__device__ __forceinline__ void widen(uint4 u, float (&v)[8]) {
-  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    v[2 * i] = __uint_as_float(w[i] << 16);
-    v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
-  }
+// Eight values as four packed pairs (the FMA pipe's two-wide instructions).
+struct Vec {
+  uint64_t p[4];
+};
+__device__ __forceinline__ uint64_t both(float v) { return f2_pack(v, v); }
+__device__ __forceinline__ Vec widen(uint4 u) { return {{bf2_unpack(u.x), bf2_unpack(u.y), bf2_unpack(u.z), bf2_unpack(u.w)}}; }
+__device__ __forceinline__ uint32_t narrow2(uint64_t v) {
+  float a, b;
+  f2_unpack(v, a, b);
+  return pack_bf16x2(a, b);
 }
-__device__ __forceinline__ uint4 narrow(const float (&v)[8]) {
-  return make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]),
-                    pack_bf16x2(v[6], v[7]));
+__device__ __forceinline__ uint4 narrow(const Vec& v) {
+  return make_uint4(narrow2(v.p[0]), narrow2(v.p[1]), narrow2(v.p[2]), narrow2(v.p[3]));
 }
+__device__ __forceinline__ Vec all(float v) { return {{both(v), both(v), both(v), both(v)}}; }
 // Eight values of an fp32 vector, or `none` where the caller gave no vector.
-__device__ __forceinline__ void vec8(const float* src, int col, float none, float (&v)[8]) {
-  if (!src) {
+__device__ __forceinline__ Vec vec8(const float* src, int col, float none) {
+  if (!src) return all(none);
+  const ulonglong2 a = reinterpret_cast<const ulonglong2*>(src + col)[0], b = reinterpret_cast<const ulonglong2*>(src + col)[1];
+  return {{a.x, a.y, b.x, b.y}};
+}
+__device__ __forceinline__ Vec operator+(const Vec& a, const Vec& b) {
+  Vec r;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = none;
-    return;
-  }
-  const float4 a = reinterpret_cast<const float4*>(src + col)[0], b = reinterpret_cast<const float4*>(src + col)[1];
-  v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+  for (int i = 0; i < 4; ++i) r.p[i] = f2_add(a.p[i], b.p[i]);
+  return r;
+}
+__device__ __forceinline__ Vec operator*(const Vec& a, const Vec& b) {
+  Vec r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) r.p[i] = f2_mul(a.p[i], b.p[i]);
+  return r;
+}
+__device__ __forceinline__ Vec fma(const Vec& a, const Vec& b, const Vec& c) {
+  Vec r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) r.p[i] = f2_fma(a.p[i], b.p[i], c.p[i]);
+  return r;
+}
+__device__ __forceinline__ float sum2(uint64_t v) {
+  float a, b;
+  f2_unpack(v, a, b);
+  return a + b;
 }
 
-// This thread's place: piece j of a row is columns 8 (lane_g + j threads).
+// This thread's place in its group of T warps: piece j < V of a row is columns
+// 8 (lane_g + 32 T j); only the last piece can be missing.
+template <int V, int T>
 struct Place {
-  int group, warp, lane_g, threads;  // group of the CTA, warp of the group, thread of the group, threads of a group
-  int C, pieces;
-  __device__ __forceinline__ Place(int warps, int C_) {
-    threads = 32 * warps;
-    group = threadIdx.x / threads;
-    lane_g = threadIdx.x - group * threads;
+  int group, warp, lane_g;
+  int pieces;
+  bool last;
+  float n_warp, inv_n;  // elements of a row in this warp
+  __device__ __forceinline__ explicit Place(int C) {
+    group = threadIdx.x / (32 * T);
+    lane_g = threadIdx.x - group * (32 * T);
     warp = lane_g >> 5;
-    C = C_;
     pieces = C >> 3;
-  }
-  __device__ __forceinline__ bool has(int j) const { return lane_g + j * threads < pieces; }
-  __device__ __forceinline__ int col(int j) const { return 8 * (lane_g + j * threads); }
-  // Elements of a row in warp w of the group.
-  template <int V>
-  __device__ __forceinline__ float count(int w) const {
+    last = lane_g + 32 * T * (V - 1) < pieces;
     int n = 0;
 #pragma unroll
-    for (int j = 0; j < V; ++j) n += min(max(pieces - (32 * w + j * threads), 0), 32);
-    return float(8 * n);
+    for (int j = 0; j < V; ++j) n += min(max(pieces - 32 * (warp + T * j), 0), 32);
+    n_warp = float(8 * n);
+    inv_n = 1.f / fmaxf(n_warp, 1.f);
   }
+  __device__ __forceinline__ bool has(int j) const { return j < V - 1 || last; }
+  __device__ __forceinline__ int col(int j) const { return 8 * (lane_g + 32 * T * j); }
 };
 
 __device__ __forceinline__ float warp_sum(float v) {
@@ -140,93 +162,117 @@ __device__ __forceinline__ float warp_sum(float v) {
   return v;
 }
 
-// Values that the warps of a group hand one another: two float2 per warp, two
-// sets in turn, so that one barrier an exchange is enough.
-constexpr int MAX_WARPS = 16;
+// What the warps of a group hand one another: two entries of four floats per
+// warp, two sets in turn, so that one barrier an exchange is enough.
+template <int T>
 struct Exchange {
-  float2* mem;  // of the group: [2][warps][2]
-  int warps, bar, set;
-  __device__ __forceinline__ Exchange(float2* base, const Place& at, int warps_)
-      : mem(base + at.group * 4 * warps_), warps(warps_), bar(1 + at.group), set(0) {}
-  // Puts the warp's a and b and returns the group's (entry w: a at [2 w], b at [2 w + 1]).
-  __device__ __forceinline__ const float2* swap(int warp, float2 a, float2 b) {
-    float2* m = mem + set * 2 * warps;
+  float4* mem;  // of the group: [2][T][2]
+  int bar, set;
+  __device__ __forceinline__ Exchange(void* base, int group)
+      : mem(reinterpret_cast<float4*>(base) + group * 4 * T), bar(1 + group), set(0) {}
+  static constexpr int BYTES = 4 * T * int(sizeof(float4));  // of a group
+  // Returns the group's entries: warp w's at [2 w] and [2 w + 1].
+  __device__ __forceinline__ const float4* swap(int warp, float4 a, float4 b) {
+    float4* m = mem + set * 2 * T;
     set ^= 1;
     if ((threadIdx.x & 31) == 0) m[2 * warp] = a, m[2 * warp + 1] = b;
-    if (warps == 1)
+    if (T == 1)
       __syncwarp();
     else
-      named_bar_sync(bar, 32 * warps);
+      named_bar_sync(bar, 32 * T);
     return m;
   }
   // Sums of two values over the group.
   __device__ __forceinline__ float2 sums(int warp, float a, float b) {
     a = warp_sum(a), b = warp_sum(b);
-    if (warps == 1) return make_float2(a, b);
-    const float2* m = swap(warp, make_float2(a, b), make_float2(0.f, 0.f));
+    if (T == 1) return make_float2(a, b);
+    const float4 e = make_float4(a, b, 0.f, 0.f);
+    float4* m = mem + set * 2 * T;
+    set ^= 1;
+    if ((threadIdx.x & 31) == 0) m[warp] = e;
+    named_bar_sync(bar, 32 * T);
     float2 r = make_float2(0.f, 0.f);
-    for (int w = 0; w < warps; ++w) r.x += m[2 * w].x, r.y += m[2 * w].y;
+#pragma unroll
+    for (int w = 0; w < T; ++w) {
+      const float4 t = m[w];
+      r.x += t.x, r.y += t.y;
+    }
     return r;
   }
 };
 
-// A warp's share of a norm's statistics: its mean and the squares around it
-// (LAYER), or zero and the squares (RMS).
-template <int V>
-__device__ __forceinline__ float2 warp_stats(int kind, const Place& at, const float (&v)[V][8], float n_warp) {
-  if (kind == RA_NORM_NONE) return make_float2(0.f, 0.f);
+// A warp's share of a norm's statistics: its mean, the squares around it and
+// their count (LAYER), or zero and the squares (RMS).
+template <int V, int T>
+__device__ __forceinline__ float4 warp_stats(int kind, const Place<V, T>& at, const Vec (&v)[V]) {
   float mean = 0.f;
+  uint64_t acc0 = both(0.f), acc1 = acc0;
   if (kind == RA_NORM_LAYER) {
-    float sum = 0.f;
+#pragma unroll
+    for (int j = 0; j < V; ++j) {  // a missing piece is zeros
+      acc0 = f2_add(acc0, f2_add(v[j].p[0], v[j].p[1]));
+      acc1 = f2_add(acc1, f2_add(v[j].p[2], v[j].p[3]));
+    }
+    mean = warp_sum(sum2(f2_add(acc0, acc1))) * at.inv_n;
+    acc0 = acc1 = both(0.f);
+    const uint64_t neg = both(-mean);
+#pragma unroll
+    for (int j = 0; j < V; ++j)
+      if (at.has(j)) {
+#pragma unroll
+        for (int i = 0; i < 4; i += 2) {
+          const uint64_t d0 = f2_add(v[j].p[i], neg), d1 = f2_add(v[j].p[i + 1], neg);
+          acc0 = f2_fma(d0, d0, acc0);
+          acc1 = f2_fma(d1, d1, acc1);
+        }
+      }
+  } else {
 #pragma unroll
     for (int j = 0; j < V; ++j)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) sum += v[j][i];  // absent pieces are zeros
-    mean = warp_sum(sum) / fmaxf(n_warp, 1.f);
+      for (int i = 0; i < 4; i += 2) {
+        acc0 = f2_fma(v[j].p[i], v[j].p[i], acc0);
+        acc1 = f2_fma(v[j].p[i + 1], v[j].p[i + 1], acc1);
+      }
   }
-  float sq = 0.f;
-#pragma unroll
-  for (int j = 0; j < V; ++j)
-    if (at.has(j)) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) sq = fmaf(v[j][i] - mean, v[j][i] - mean, sq);
-    }
-  return make_float2(mean, warp_sum(sq));
+  return make_float4(mean, warp_sum(sum2(f2_add(acc0, acc1))), at.n_warp, 0.f);
 }
-// Mean and 1 / deviation of the row from its warps' shares (share w at m[2 w + which]).
-template <int V>
-__device__ __forceinline__ float2 join_stats(int kind, const Place& at, int warps, const float2* m, int which,
-                                             float eps) {
-  if (kind == RA_NORM_NONE) return make_float2(0.f, 1.f);
-  const float inv_c = 1.f / float(at.C);
+// -mean and 1 / deviation of the row from its warps' shares (warp w's at m[2 w]).
+template <int T>
+__device__ __forceinline__ float2 join_stats(int kind, const float4* m, float inv_c, float eps) {
   float mean = 0.f, sq = 0.f;
   if (kind == RA_NORM_LAYER) {
-    for (int w = 0; w < warps; ++w) mean = fmaf(at.count<V>(w), m[2 * w + which].x, mean);
-    mean *= inv_c;
-  }
-  for (int w = 0; w < warps; ++w) {
-    const float2 s = m[2 * w + which];
-    sq += s.y;
-    if (kind == RA_NORM_LAYER) {
-      const float d = s.x - mean;
-      sq = fmaf(at.count<V>(w) * d, d, sq);
+#pragma unroll
+    for (int w = 0; w < T; ++w) {
+      const float4 t = m[2 * w];
+      mean = fmaf(t.z, t.x, mean);
     }
+    mean *= inv_c;
+    asm volatile("" ::: "memory");  // read again: 3 T registers would spill
+#pragma unroll
+    for (int w = 0; w < T; ++w) {
+      const float4 t = m[2 * w];
+      const float d = t.x - mean;
+      sq = fmaf(t.z * d, d, sq + t.y);
+    }
+  } else {
+#pragma unroll
+    for (int w = 0; w < T; ++w) sq += m[2 * w].y;
   }
-  return make_float2(mean, rsqrtf(sq * inv_c + eps));
+  return make_float2(-mean, rsqrtf(fmaf(sq, inv_c, eps)));
 }
 
 // ------------------------------------------------------------------ forward
-template <int V>
+template <int V, int T>
 __global__ void __launch_bounds__(FWD_THREADS, 1) residual_norm_kernel(const __grid_constant__ Params p) {
   constexpr int S = FWD_STAGES;
   extern __shared__ __align__(16) uint8_t smem[];
-  // ring[stage][y, h][piece][thread of the CTA], then the exchange
-  uint4* ring = reinterpret_cast<uint4*>(smem) + threadIdx.x;
-  const int stride = blockDim.x;
-  auto slot = [&](int stage, int which, int j) { return ring + ((stage * 2 + which) * V + j) * stride; };
-  const Place at(p.warps, p.C);
-  Exchange ex(reinterpret_cast<float2*>(smem + size_t(S) * 2 * V * 16 * stride), at, p.warps);
-  const float n_warp = at.count<V>(at.warp);
+  // ring[stage][piece of y, of h][thread of the CTA], then the exchange
+  const uint32_t piece_bytes = 16 * blockDim.x, stage_bytes = 2 * V * piece_bytes;
+  uint8_t* const ring = smem + 16 * threadIdx.x;
+  const Place<V, T> at(p.C);
+  Exchange<T> ex(smem + S * stage_bytes, at.group);
+  const float inv_c = 1.f / float(p.C);
   pdl_launch();
   pdl_wait();
   const int total = live_rows(p);
@@ -235,226 +281,238 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) residual_norm_kernel(const __g
   Piece ld;
   if (lo < hi && p.B > 4) ld.jump(p, lo);
   Piece w = ld;
-  int ld_i = lo + at.group;
-  auto load = [&](int stage) {
+  // This thread's first piece of the next row to copy and of the row at work, and
+  // the steps to the group's next rows; found anew where a (segment, sample) ends.
+  const __nv_bfloat16 *h_src = nullptr, *y_src = nullptr;
+  __nv_bfloat16 *h_dst = nullptr, *x_dst = nullptr;
+  int64_t h_step = 0, y_step = 0, h_out_step = 0, x_step = 0;
+  int ld_i = lo + at.group, ld_end = lo, w_end = lo;
+  auto load = [&](uint32_t off) {
     if (ld_i < hi) {
-      ld.seek(p, ld_i);
-      const Seg& sg = p.seg[ld.g];
-      const int64_t r = ld_i - ld.begin;
-      const __nv_bfloat16* h = sg.h + ld.s * sg.h_ss + r * sg.h_sr;
-      const __nv_bfloat16* y = sg.y ? sg.y + ld.s * sg.y_ss + r * sg.y_sr : nullptr;
+      if (ld_i >= ld_end) {
+        ld.seek(p, ld_i);
+        const Seg& sg = p.seg[ld.g];
+        ld_end = ld.begin + sg.rows;
+        const int64_t r = ld_i - ld.begin;
+        h_src = sg.h + ld.s * sg.h_ss + r * sg.h_sr + at.col(0);
+        y_src = sg.y ? sg.y + ld.s * sg.y_ss + r * sg.y_sr + at.col(0) : nullptr;
+        h_step = p.groups * sg.h_sr, y_step = sg.y ? p.groups * sg.y_sr : 0;
+      }
 #pragma unroll
       for (int j = 0; j < V; ++j)
         if (at.has(j)) {
-          if (y) cp_async16(slot(stage, 0, j), y + at.col(j));
-          cp_async16(slot(stage, 1, j), h + at.col(j));
+          if (y_src) cp_async16(ring + off + j * piece_bytes, y_src + 256 * T * j);
+          cp_async16(ring + off + (V + j) * piece_bytes, h_src + 256 * T * j);
         }
+      h_src += h_step, y_src += y_step;
     }
     ld_i += p.groups;
     cp_async_commit();
   };
 #pragma unroll
-  for (int k = 0; k < S - 1; ++k) load(k);
-  float gate[V][8], mul[V][8], add[V][8];
-  int cur_g = -1, cur_s = -1, stage = 0;
+  for (int k = 0; k < S - 1; ++k) load(k * stage_bytes);
+  Vec gate[V], mul[V], add[V];
+  bool has_y = false;
+  uint32_t off = 0, ld_off = (S - 1) * stage_bytes;
   for (int i = lo + at.group; i < hi; i += p.groups) {
-    w.seek(p, i);
-    const Seg& sg = p.seg[w.g];
-    if (w.g != cur_g || w.s != cur_s) {  // another sample's rows: its vectors
-      cur_g = w.g, cur_s = w.s;
+    if (i >= w_end) {  // another sample's rows: its vectors
+      w.seek(p, i);
+      const Seg& sg = p.seg[w.g];
+      w_end = w.begin + sg.rows;
+      const int64_t r = i - w.begin;
+      has_y = sg.y != nullptr;
+      h_dst = sg.h_out ? sg.h_out + w.s * sg.o_ss + r * sg.o_sr + at.col(0) : nullptr;
+      x_dst = sg.x ? sg.x + w.s * sg.x_ss + r * sg.x_sr + at.col(0) : nullptr;
+      h_out_step = sg.h_out ? p.groups * sg.o_sr : 0, x_step = sg.x ? p.groups * sg.x_sr : 0;
 #pragma unroll
       for (int j = 0; j < V; ++j) {
         if (!at.has(j)) continue;
-        float t[8];
-        vec8(sg.gate ? sg.gate + w.s * sg.gate_ss : nullptr, at.col(j), 1.f, gate[j]);
-        vec8(sg.post_w, at.col(j), 1.f, t);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) gate[j][k] *= t[k];
-        vec8(sg.scale ? sg.scale + w.s * sg.mod_ss : nullptr, at.col(j), 0.f, mul[j]);
-        vec8(sg.pre_w, at.col(j), 1.f, t);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) mul[j][k] = (1.f + mul[j][k]) * t[k];
-        vec8(sg.shift ? sg.shift + w.s * sg.mod_ss : nullptr, at.col(j), 0.f, add[j]);
+        const int c = at.col(j);
+        gate[j] = vec8(sg.gate ? sg.gate + w.s * sg.gate_ss : nullptr, c, 1.f) * vec8(sg.post_w, c, 1.f);
+        mul[j] = (vec8(sg.scale ? sg.scale + w.s * sg.mod_ss : nullptr, c, 0.f) + all(1.f)) * vec8(sg.pre_w, c, 1.f);
+        add[j] = vec8(sg.shift ? sg.shift + w.s * sg.mod_ss : nullptr, c, 0.f);
       }
     }
-    load(stage == 0 ? S - 1 : stage - 1);
+    load(ld_off);
+    ld_off = off;
     cp_async_wait<S - 1>();
-    float v[V][8];
+    Vec v[V];
+    auto fetch = [&](int q, int j) {
+      return widen(at.has(j) ? *reinterpret_cast<const uint4*>(ring + off + (q * V + j) * piece_bytes)
+                             : make_uint4(0, 0, 0, 0));
+    };
+    if (has_y) {
 #pragma unroll
-    for (int j = 0; j < V; ++j) {
-      const bool in = at.has(j) && sg.y;
-      widen(in ? *slot(stage, 0, j) : make_uint4(0, 0, 0, 0), v[j]);
-    }
-    float2 st = make_float2(0.f, 1.f);
-    if (p.post != RA_NORM_NONE) {
-      const float2 mine = warp_stats<V>(p.post, at, v, n_warp);
-      st = join_stats<V>(p.post, at, p.warps, ex.swap(at.warp, mine, mine), 0, p.eps);
-    }
-    const int64_t r = i - w.begin;
-    __nv_bfloat16* h_out = sg.h_out ? sg.h_out + w.s * sg.o_ss + r * sg.o_sr : nullptr;
+      for (int j = 0; j < V; ++j) v[j] = fetch(0, j);
+      if (p.post != RA_NORM_NONE) {
+        const float4 mine = warp_stats<V, T>(p.post, at, v);
+        const float2 st = join_stats<T>(p.post, ex.swap(at.warp, mine, mine), inv_c, p.eps);
 #pragma unroll
-    for (int j = 0; j < V; ++j) {
-      if (!at.has(j)) continue;
-      float h[8];
-      widen(*slot(stage, 1, j), h);
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        // without y the branch adds nothing, whatever the gate (0 times an infinite gate would be NaN)
-        const float z = sg.y ? gate[j][k] * ((v[j][k] - st.x) * st.y) : 0.f;
-        v[j][k] = fmaf(p.alpha, h[k], z);
+        for (int j = 0; j < V; ++j) v[j] = (v[j] + all(st.x)) * all(st.y);
       }
-      if (h_out) *reinterpret_cast<uint4*>(h_out + at.col(j)) = narrow(v[j]);
+#pragma unroll
+      for (int j = 0; j < V; ++j)
+        if (at.has(j)) v[j] = fma(v[j], gate[j], all(p.alpha) * fetch(1, j));
+    } else {
+#pragma unroll
+      for (int j = 0; j < V; ++j) v[j] = all(p.alpha) * fetch(1, j);
     }
-    if (sg.x) {
+    if (!at.last) v[V - 1] = all(0.f);
+    if (h_dst) {
+#pragma unroll
+      for (int j = 0; j < V; ++j)
+        if (at.has(j)) *reinterpret_cast<uint4*>(h_dst + 256 * T * j) = narrow(v[j]);
+      h_dst += h_out_step;
+    }
+    if (x_dst) {
+      float2 st = make_float2(0.f, 1.f);
       if (p.pre != RA_NORM_NONE) {
-        const float2 mine = warp_stats<V>(p.pre, at, v, n_warp);
-        st = join_stats<V>(p.pre, at, p.warps, ex.swap(at.warp, mine, mine), 0, p.eps);
-      } else {
-        st = make_float2(0.f, 1.f);
+        const float4 mine = warp_stats<V, T>(p.pre, at, v);
+        st = join_stats<T>(p.pre, ex.swap(at.warp, mine, mine), inv_c, p.eps);
       }
-      __nv_bfloat16* x = sg.x + w.s * sg.x_ss + r * sg.x_sr;
 #pragma unroll
-      for (int j = 0; j < V; ++j) {
-        if (!at.has(j)) continue;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) v[j][k] = fmaf((v[j][k] - st.x) * st.y, mul[j][k], add[j][k]);
-        *reinterpret_cast<uint4*>(x + at.col(j)) = narrow(v[j]);
-      }
+      for (int j = 0; j < V; ++j)
+        if (at.has(j))
+          *reinterpret_cast<uint4*>(x_dst + 256 * T * j) = narrow(fma((v[j] + all(st.x)) * all(st.y), mul[j], add[j]));
+      x_dst += x_step;
     }
-    if (++stage == S) stage = 0;
+    off += stage_bytes;
+    if (off == S * stage_bytes) off = 0;
   }
 }
 
 // ------------------------------------------------------------------ backward
-template <int V>
+template <int V, int T>
 __global__ void __launch_bounds__(BWD_THREADS, 1) residual_norm_grad_kernel(const __grid_constant__ GradParams p) {
   constexpr int S = BWD_STAGES;
   extern __shared__ __align__(16) uint8_t smem[];
-  uint4* ring = reinterpret_cast<uint4*>(smem) + threadIdx.x;
-  const int stride = blockDim.x;
-  auto slot = [&](int stage, int which, int j) { return ring + ((stage * 4 + which) * V + j) * stride; };
-  const Place at(p.warps, p.C);
-  Exchange ex(reinterpret_cast<float2*>(smem + size_t(S) * 4 * V * 16 * stride), at, p.warps);
-  const float n_warp = at.count<V>(at.warp), inv_c = 1.f / float(p.C);
+  const uint32_t piece_bytes = 16 * blockDim.x, stage_bytes = 4 * V * piece_bytes;
+  uint8_t* const ring = smem + 16 * threadIdx.x;
+  const Place<V, T> at(p.C);
+  Exchange<T> ex(smem + S * stage_bytes, at.group);
+  const float inv_c = 1.f / float(p.C);
   pdl_launch();
   pdl_wait();
   const int s = int(blockIdx.x) / p.parts, part = int(blockIdx.x) - s * p.parts;
   const int lo = int(int64_t(p.rows) * part / p.parts), hi = int(int64_t(p.rows) * (part + 1) / p.parts);
-  const __nv_bfloat16* src[4] = {p.h + s * p.h_ss, p.y ? p.y + s * p.y_ss : nullptr,
-                                 p.dx ? p.dx + s * p.dx_ss : nullptr, p.dh_out ? p.dh_out + s * p.dho_ss : nullptr};
-  const int64_t sr[4] = {p.h_sr, p.y_sr, p.dx_sr, p.dho_sr};
-  int ld_i = lo + at.group;
-  auto load = [&](int stage) {
+  const int first = lo + at.group;
+  // this thread's first piece of the group's next row of h, y, dx and dh_out
+  auto start = [&](const __nv_bfloat16* t, int64_t ss, int64_t sr) {
+    return t ? t + s * ss + first * sr + at.col(0) : nullptr;
+  };
+  const __nv_bfloat16 *h = start(p.h, p.h_ss, p.h_sr), *y = start(p.y, p.y_ss, p.y_sr),
+                      *dx = start(p.dx, p.dx_ss, p.dx_sr), *dho = start(p.dh_out, p.dho_ss, p.dho_sr);
+  const bool has_y = y != nullptr, has_dx = dx != nullptr, has_dho = dho != nullptr;
+  int ld_i = first;
+  const int64_t h_step = p.groups * p.h_sr, y_step = p.groups * p.y_sr, dx_step = p.groups * p.dx_sr,
+                dho_step = p.groups * p.dho_sr;
+  auto load = [&](uint32_t off) {
     if (ld_i < hi) {
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        if (!src[q]) continue;
-        const __nv_bfloat16* row = src[q] + ld_i * sr[q];
-#pragma unroll
-        for (int j = 0; j < V; ++j)
-          if (at.has(j)) cp_async16(slot(stage, q, j), row + at.col(j));
-      }
+      for (int j = 0; j < V; ++j)
+        if (at.has(j)) {
+          uint8_t* to = ring + off + j * piece_bytes;
+          cp_async16(to, h + 256 * T * j);
+          if (has_y) cp_async16(to + V * piece_bytes, y + 256 * T * j);
+          if (has_dx) cp_async16(to + 2 * V * piece_bytes, dx + 256 * T * j);
+          if (has_dho) cp_async16(to + 3 * V * piece_bytes, dho + 256 * T * j);
+        }
+      h += h_step, y += y_step, dx += dx_step, dho += dho_step;
     }
     ld_i += p.groups;
     cp_async_commit();
   };
 #pragma unroll
-  for (int k = 0; k < S - 1; ++k) load(k);
-  float mul[V][8], gate[V][8];             // pre_w (1 + scale), gate post_w
-  float s0[V][8], s1[V][8], s2[V][8];      // column sums of the group's rows
+  for (int k = 0; k < S - 1; ++k) load(k * stage_bytes);
+  Vec mul[V], gate[V];          // pre_w (1 + scale), gate post_w
+  Vec s0[V], s1[V], s2[V];      // column sums of the group's rows
 #pragma unroll
   for (int j = 0; j < V; ++j) {
-#pragma unroll
-    for (int k = 0; k < 8; ++k) s0[j][k] = s1[j][k] = s2[j][k] = mul[j][k] = gate[j][k] = 0.f;
+    s0[j] = s1[j] = s2[j] = mul[j] = gate[j] = all(0.f);
     if (!at.has(j)) continue;
-    float t[8];
-    vec8(p.scale ? p.scale + s * p.mod_ss : nullptr, at.col(j), 0.f, mul[j]);
-    vec8(p.pre_w, at.col(j), 1.f, t);
-#pragma unroll
-    for (int k = 0; k < 8; ++k) mul[j][k] = (1.f + mul[j][k]) * t[k];
-    vec8(p.gate ? p.gate + s * p.gate_ss : nullptr, at.col(j), 1.f, gate[j]);
-    vec8(p.post_w, at.col(j), 1.f, t);
-#pragma unroll
-    for (int k = 0; k < 8; ++k) gate[j][k] *= t[k];
+    const int c = at.col(j);
+    mul[j] = (vec8(p.scale ? p.scale + s * p.mod_ss : nullptr, c, 0.f) + all(1.f)) * vec8(p.pre_w, c, 1.f);
+    gate[j] = vec8(p.gate ? p.gate + s * p.gate_ss : nullptr, c, 1.f) * vec8(p.post_w, c, 1.f);
   }
-  int stage = 0;
-  for (int i = lo + at.group; i < hi; i += p.groups) {
-    load(stage == 0 ? S - 1 : stage - 1);
+  auto place = [&](__nv_bfloat16* t, int64_t ss, int64_t sr) {
+    return t ? t + s * ss + first * sr + at.col(0) : nullptr;
+  };
+  __nv_bfloat16 *dh = place(p.dh, p.dh_ss, p.dh_sr), *dy = place(p.dy, p.dy_ss, p.dy_sr);
+  const int64_t dh_step = p.groups * p.dh_sr, dy_step = p.groups * p.dy_sr;
+  uint32_t off = 0, ld_off = (S - 1) * stage_bytes;
+  for (int i = first; i < hi; i += p.groups) {
+    load(ld_off);
+    ld_off = off;
     cp_async_wait<S - 1>();
-    float a[V][8], b[V][8];  // x^ and then dH; y^
-    auto fetch = [&](int q, int j, float (&v)[8]) {
-      widen(src[q] && at.has(j) ? *slot(stage, q, j) : make_uint4(0, 0, 0, 0), v);
+    auto fetch = [&](bool given, int q, int j) {
+      return widen(given && at.has(j) ? *reinterpret_cast<const uint4*>(ring + off + (q * V + j) * piece_bytes)
+                                      : make_uint4(0, 0, 0, 0));
     };
+    Vec a[V], b[V];  // x^, then dH and what follows from it; y^
 #pragma unroll
-    for (int j = 0; j < V; ++j) fetch(0, j, a[j]), fetch(1, j, b[j]);
+    for (int j = 0; j < V; ++j) a[j] = fetch(true, 0, j), b[j] = fetch(has_y, 1, j);
     float2 sa = make_float2(0.f, 1.f), sb = sa;
     if (p.pre != RA_NORM_NONE || p.post != RA_NORM_NONE) {
-      const float2 ma = warp_stats<V>(p.pre, at, a, n_warp), mb = warp_stats<V>(p.post, at, b, n_warp);
-      const float2* m = ex.swap(at.warp, ma, mb);
-      sa = join_stats<V>(p.pre, at, p.warps, m, 0, p.eps);
-      sb = join_stats<V>(p.post, at, p.warps, m, 1, p.eps);
+      const float4 ma = warp_stats<V, T>(p.pre, at, a), mb = warp_stats<V, T>(p.post, at, b);
+      const float4* m = ex.swap(at.warp, ma, mb);
+      if (p.pre != RA_NORM_NONE) sa = join_stats<T>(p.pre, m, inv_c, p.eps);
+      if (p.post != RA_NORM_NONE) sb = join_stats<T>(p.post, m + 1, inv_c, p.eps);
     }
     // the norm before the next branch
-    float e0 = 0.f, e1 = 0.f;
+    uint64_t e0 = both(0.f), e1 = e0;
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-      float dx[8];
-      fetch(2, j, dx);
+      a[j] = (a[j] + all(sa.x)) * all(sa.y);
+      if (!at.has(j)) a[j] = all(0.f);
+      const Vec d = fetch(has_dx, 2, j), e = d * mul[j];
+      s0[j] = s0[j] + d;
+      s1[j] = fma(d, a[j], s1[j]);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        a[j][k] = at.has(j) ? (a[j][k] - sa.x) * sa.y : 0.f;
-        s0[j][k] += dx[k];
-        s1[j][k] = fmaf(dx[k], a[j][k], s1[j][k]);
-        const float e = dx[k] * mul[j][k];
-        e0 += e;
-        e1 = fmaf(e, a[j][k], e1);
+      for (int k = 0; k < 4; ++k) {
+        e0 = f2_add(e0, e.p[k]);
+        e1 = f2_fma(e.p[k], a[j].p[k], e1);
       }
     }
     float2 m = make_float2(0.f, 0.f);
-    if (p.pre != RA_NORM_NONE && p.dx) {
-      m = ex.sums(at.warp, e0, e1);
-      m.x = p.pre == RA_NORM_LAYER ? m.x * inv_c : 0.f;
-      m.y *= inv_c;
+    if (p.pre != RA_NORM_NONE && has_dx) {
+      m = ex.sums(at.warp, sum2(e0), sum2(e1));
+      m.x = p.pre == RA_NORM_LAYER ? -m.x * inv_c : 0.f;
+      m.y *= -inv_c;
     }
-    __nv_bfloat16* dh = p.dh ? p.dh + s * p.dh_ss + i * p.dh_sr : nullptr;
-    float f0 = 0.f, f1 = 0.f;
+    e0 = e1 = both(0.f);
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-      if (!at.has(j)) continue;
-      float dx[8], dho[8], out[8];
-      fetch(2, j, dx);
-      fetch(3, j, dho);
+      // dH = dh' + r (e - m(e) - x^ m(e x^))
+      const Vec e = fma(a[j], all(m.y), fma(fetch(has_dx, 2, j), mul[j], all(m.x)));
+      a[j] = fma(e, all(sa.y), fetch(has_dho, 3, j));
+      if (!at.has(j)) a[j] = all(0.f);
+      b[j] = (b[j] + all(sb.x)) * all(sb.y);
+      if (dh && at.has(j)) *reinterpret_cast<uint4*>(dh + 256 * T * j) = narrow(a[j] * all(p.alpha));
+      s2[j] = fma(a[j], b[j], s2[j]);
+      a[j] = a[j] * gate[j];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        a[j][k] = fmaf(sa.y, dx[k] * mul[j][k] - m.x - a[j][k] * m.y, dho[k]);
-        b[j][k] = (b[j][k] - sb.x) * sb.y;
-        out[k] = p.alpha * a[j][k];
-        s2[j][k] = fmaf(a[j][k], b[j][k], s2[j][k]);
-        a[j][k] *= gate[j][k];
-        f0 += a[j][k];
-        f1 = fmaf(a[j][k], b[j][k], f1);
+      for (int k = 0; k < 4; ++k) {
+        e0 = f2_add(e0, a[j].p[k]);
+        e1 = f2_fma(a[j].p[k], b[j].p[k], e1);
       }
-      if (dh) *reinterpret_cast<uint4*>(dh + at.col(j)) = narrow(out);
     }
+    if (dh) dh += dh_step;
     // the norm after the branch
-    if (p.dy) {
+    if (dy) {
       m = make_float2(0.f, 0.f);
       if (p.post != RA_NORM_NONE) {
-        m = ex.sums(at.warp, f0, f1);
-        m.x = p.post == RA_NORM_LAYER ? m.x * inv_c : 0.f;
-        m.y *= inv_c;
+        m = ex.sums(at.warp, sum2(e0), sum2(e1));
+        m.x = p.post == RA_NORM_LAYER ? -m.x * inv_c : 0.f;
+        m.y *= -inv_c;
       }
-      __nv_bfloat16* dy = p.dy + s * p.dy_ss + i * p.dy_sr;
 #pragma unroll
-      for (int j = 0; j < V; ++j) {
-        if (!at.has(j)) continue;
-        float out[8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) out[k] = sb.y * (a[j][k] - m.x - b[j][k] * m.y);
-        *reinterpret_cast<uint4*>(dy + at.col(j)) = narrow(out);
-      }
+      for (int j = 0; j < V; ++j)
+        if (at.has(j))
+          *reinterpret_cast<uint4*>(dy + 256 * T * j) = narrow(fma(b[j], all(m.y), a[j] + all(m.x)) * all(sb.y));
+      dy += dy_step;
     }
-    if (++stage == S) stage = 0;
+    off += stage_bytes;
+    if (off == S * stage_bytes) off = 0;
   }
   // The CTA's column sums: its groups' in order, through the ring's memory.
   cp_async_wait<0>();
@@ -463,80 +521,76 @@ __global__ void __launch_bounds__(BWD_THREADS, 1) residual_norm_grad_kernel(cons
 #pragma unroll
   for (int j = 0; j < V; ++j) {
     if (!at.has(j)) continue;
-    float* at0 = sums + size_t(at.group) * 3 * p.C + at.col(j);
-#pragma unroll
-    for (int k = 0; k < 8; ++k) at0[k] = s0[j][k], at0[p.C + k] = s1[j][k], at0[2 * p.C + k] = s2[j][k];
+    float* to = sums + at.group * 3 * p.C + at.col(j);
+    auto put = [](float* dst, const Vec& v) {
+      reinterpret_cast<ulonglong2*>(dst)[0] = make_ulonglong2(v.p[0], v.p[1]);
+      reinterpret_cast<ulonglong2*>(dst)[1] = make_ulonglong2(v.p[2], v.p[3]);
+    };
+    put(to, s0[j]);
+    put(to + p.C, s1[j]);
+    put(to + 2 * p.C, s2[j]);
   }
   __syncthreads();
   float* out = p.partial + int64_t(blockIdx.x) * 3 * p.C;
   for (int c = threadIdx.x; c < 3 * p.C; c += blockDim.x) {
     float v = 0.f;
-    for (int g = 0; g < p.groups; ++g) v += sums[size_t(g) * 3 * p.C + c];
+    for (int g = 0; g < p.groups; ++g) v += sums[g * 3 * p.C + c];
     out[c] = v;
   }
 }
 
-// Sums of a sample's parts: 32 columns by 32 slices of the parts a CTA, the
-// slices then added in order. Writes the sample's gradients, and S1 and S2
-// (over its first part) where weights want them summed over the samples.
+// The column sums of the samples and what follows from them: 32 columns a CTA, up
+// to 32 samples at once, whose parts are divided among its 32 warps; the warps'
+// sums are then added in order.
 struct SumParams {
   int32_t B, C, parts;
-  float* partial;
-  const float *post_w, *pre_w;
-  float *dgate, *dscale, *dshift;
-  bool keep;
+  const float* partial;
+  const float *gate, *scale, *post_w, *pre_w;
+  int64_t gate_ss, mod_ss;
+  float *dgate, *dscale, *dshift, *dpost_w, *dpre_w;
 };
-__global__ void __launch_bounds__(1024) column_sum_kernel(const SumParams p) {
+__global__ void __launch_bounds__(1024) column_sum_kernel(const __grid_constant__ SumParams p) {
   __shared__ float red[3][32][33];
   pdl_launch();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
+  const bool in = c < p.C;
   pdl_wait();
-  const int lane = threadIdx.x & 31, slice = threadIdx.x >> 5, s = blockIdx.y;
-  const int c = blockIdx.x * 32 + lane;
-  float v[3] = {0.f, 0.f, 0.f};
-  if (c < p.C)
-    for (int q = slice; q < p.parts; q += 32) {
-      const float* src = p.partial + (int64_t(s) * p.parts + q) * 3 * p.C + c;
-#pragma unroll
-      for (int z = 0; z < 3; ++z) v[z] += src[int64_t(z) * p.C];
-    }
-#pragma unroll
-  for (int z = 0; z < 3; ++z) red[z][slice][lane] = v[z];
-  __syncthreads();
-  if (slice >= 3 || c >= p.C) return;
-  const int z = slice;
-  float t = 0.f;
-#pragma unroll
-  for (int q = 0; q < 32; ++q) t += red[z][q][lane];
-  const int64_t at = int64_t(s) * p.C + c;
-  if (z == 0) {
-    if (p.dshift) p.dshift[at] = t;
-  } else if (z == 1) {
-    if (p.dscale) p.dscale[at] = p.pre_w ? p.pre_w[c] * t : t;
-  } else {
-    if (p.dgate) p.dgate[at] = p.post_w ? p.post_w[c] * t : t;
-  }
-  // every part of these columns of the sample has been read (the barrier above)
-  if (p.keep && p.parts > 0) p.partial[int64_t(s) * p.parts * 3 * p.C + int64_t(z) * p.C + c] = t;
-}
-
-// dpre_w and dpost_w: sums over the samples, in order.
-__global__ void __launch_bounds__(128) weight_sum_kernel(const float* partial, int B, int C, int parts,
-                                                         const float* gate, int64_t gate_ss, const float* scale,
-                                                         int64_t mod_ss, float* dpost_w, float* dpre_w) {
-  pdl_launch();
-  pdl_wait();
-  const int c = blockIdx.x * 128 + threadIdx.x;
-  if (c >= C) return;
-  float pre = 0.f, post = 0.f;
-  if (parts > 0)
+  float weight = 0.f;  // of dpre_w (warp 1), dpost_w (warp 2)
+  for (int s0 = 0; s0 < p.B; s0 += 32) {
+    const int n = min(32, p.B - s0), per = 32 / n, mine = warp / per;  // samples, warps of each, this warp's
+    float v[3] = {0.f, 0.f, 0.f};
+    if (in && mine < n) {
+      const float* src = p.partial + (int64_t(s0 + mine) * p.parts + warp % per) * 3 * p.C + c;
 #pragma unroll 4
-    for (int s = 0; s < B; ++s) {
-      const float* src = partial + int64_t(s) * parts * 3 * C + c;
-      pre = fmaf(scale ? 1.f + scale[s * mod_ss + c] : 1.f, src[C], pre);
-      post = fmaf(gate ? gate[s * gate_ss + c] : 1.f, src[2 * C], post);
+      for (int q = warp % per; q < p.parts; q += per, src += int64_t(per) * 3 * p.C) {
+        v[0] += src[0];
+        v[1] += src[p.C];
+        v[2] += src[2 * p.C];
+      }
     }
-  if (dpre_w) dpre_w[c] = pre;
-  if (dpost_w) dpost_w[c] = post;
+#pragma unroll
+    for (int z = 0; z < 3; ++z) red[z][warp][lane] = v[z];
+    __syncthreads();
+    if (warp < 3 && in) {
+      // warp 0: S0, dshift; 1: S1, dscale and dpre_w; 2: S2, dgate and dpost_w
+      float* out = warp == 0 ? p.dshift : warp == 1 ? p.dscale : p.dgate;
+      const float* vec = warp == 0 ? nullptr : warp == 1 ? p.scale : p.gate;
+      const int64_t vec_ss = warp == 1 ? p.mod_ss : p.gate_ss;
+      const float* w = warp == 0 ? nullptr : warp == 1 ? p.pre_w : p.post_w;
+      const float own = w ? w[c] : 1.f;
+#pragma unroll 4
+      for (int s = 0; s < n; ++s) {
+        const float f = vec ? vec[(s0 + s) * vec_ss + c] : warp == 1 ? 0.f : 1.f;
+        float t = 0.f;
+        for (int k = 0; k < per; ++k) t += red[warp][s * per + k][lane];
+        if (out) out[int64_t(s0 + s) * p.C + c] = own * t;
+        weight = fmaf(warp == 1 ? 1.f + f : f, t, weight);
+      }
+    }
+    __syncthreads();
+  }
+  if (in && warp == 1 && p.dpre_w) p.dpre_w[c] = weight;
+  if (in && warp == 2 && p.dpost_w) p.dpost_w[c] = weight;
 }
 
 // ------------------------------------------------------------------ host
@@ -586,6 +640,8 @@ ra_status launch(const char* who, void (*fn)(P), const P& p, dim3 grid, int thre
 // Pieces per thread, warps of a row's group, groups of a CTA.
 struct Shape {
   int V, warps, groups;
+  int threads() const { return 32 * warps * groups; }
+  int exchange() const { return groups * 4 * warps * int(sizeof(float4)); }
 };
 Shape make_shape(int C, int max_threads) {
   Shape s;
@@ -595,6 +651,14 @@ Shape make_shape(int C, int max_threads) {
   if (s.groups > 15) s.groups = 15;  // named barriers
   return s;
 }
+using Fwd = void (*)(Params);
+using Bwd = void (*)(GradParams);
+#define RA_RESNORM_PICK(kernel, s)                                                                          \
+  (s.V == 1 ? kernel<1, 1>                                                                                  \
+   : s.warps == 1 ? kernel<2, 1> : s.warps == 2 ? kernel<2, 2> : s.warps == 3 ? kernel<2, 3>                \
+   : s.warps == 4 ? kernel<2, 4> : s.warps == 5 ? kernel<2, 5> : s.warps == 6 ? kernel<2, 6>                \
+   : s.warps == 7 ? kernel<2, 7> : s.warps == 8 ? kernel<2, 8> : s.warps == 9 ? kernel<2, 9> : kernel<2, 10>)
+static_assert(MAX_C <= 10 * 512, "a group has at most ten warps");
 
 // CTAs that share a sample's rows: as many as make the fewest rounds of rows.
 int grad_parts(int B, int rows, int sms) {
@@ -692,13 +756,12 @@ extern "C" ra_status refadapt_residual_norm(const ra_resnorm_args* a, void* stre
     return RA_EINVAL;
   }
   const Shape sh = make_shape(a->C, FWD_THREADS);
-  p.warps = sh.warps;
   p.groups = sh.groups;
-  const int threads = 32 * sh.warps * sh.groups;
-  const int smem = FWD_STAGES * 2 * sh.V * 16 * threads + sh.groups * 4 * sh.warps * int(sizeof(float2));
+  const int smem = FWD_STAGES * 2 * sh.V * 16 * sh.threads() + sh.exchange();
   const int64_t sms = num_sms();
-  return launch(who, sh.V == 1 ? residual_norm_kernel<1> : residual_norm_kernel<2>, p,
-                dim3(unsigned(rows < sms ? rows : sms)), threads, smem, static_cast<cudaStream_t>(stream));
+  const Fwd fn = RA_RESNORM_PICK(residual_norm_kernel, sh);
+  return launch(who, fn, p, dim3(unsigned(rows < sms ? rows : sms)), sh.threads(), smem,
+                static_cast<cudaStream_t>(stream));
 }
 
 extern "C" size_t refadapt_residual_norm_backward_workspace_size(int32_t B, int32_t rows, int32_t C) {
@@ -777,40 +840,20 @@ extern "C" ra_status refadapt_residual_norm_backward(const ra_resnorm_grad_args*
   p.partial = static_cast<float*>(a->workspace);
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
   const Shape sh = make_shape(a->C, BWD_THREADS);
-  p.warps = sh.warps;
   p.groups = sh.groups;
   p.parts = a->rows > 0 ? grad_parts(a->B, a->rows, num_sms()) : 0;
   if (a->rows > 0) {
-    const int threads = 32 * sh.warps * sh.groups;
-    const int ring = BWD_STAGES * 4 * sh.V * 16 * threads;
-    const int smem = ring + sh.groups * 4 * sh.warps * int(sizeof(float2));
-    const ra_status r = launch(who, sh.V == 1 ? residual_norm_grad_kernel<1> : residual_norm_grad_kernel<2>, p,
-                               dim3(unsigned(a->B * p.parts)), threads, smem, st);
+    const int smem = BWD_STAGES * 4 * sh.V * 16 * sh.threads() + sh.exchange();
+    const Bwd fn = RA_RESNORM_PICK(residual_norm_grad_kernel, sh);
+    const ra_status r = launch(who, fn, p, dim3(unsigned(a->B * p.parts)), sh.threads(), smem, st);
     if (r != RA_OK) return r;
   }
-  const bool weights = a->dpre_w || a->dpost_w;
-  if (!weights && !a->dgate && !a->dscale && !a->dshift) return RA_OK;
+  if (!a->dpre_w && !a->dpost_w && !a->dgate && !a->dscale && !a->dshift) return RA_OK;
   SumParams q;
   q.B = a->B, q.C = a->C, q.parts = p.parts, q.partial = p.partial;
+  q.gate = a->gate, q.gate_ss = a->gate_stride_s, q.scale = a->scale, q.mod_ss = a->mod_stride_s;
   q.post_w = a->post_w, q.pre_w = a->pre_w;
   q.dgate = a->dgate, q.dscale = a->dscale, q.dshift = a->dshift;
-  q.keep = weights;
-  const ra_status r = launch(who, column_sum_kernel, q, dim3((a->C + 31) / 32, a->B), 1024, 0, st);
-  if (r != RA_OK || !weights) return r;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((a->C + 127) / 128);
-  cfg.blockDim = dim3(128);
-  cfg.stream = st;
-  cudaLaunchAttribute attr = pdl_attribute();
-  cfg.attrs = &attr;
-  cfg.numAttrs = 1;
-  const cudaError_t e = cudaLaunchKernelEx(&cfg, weight_sum_kernel, static_cast<const float*>(p.partial), int(a->B),
-                                           int(a->C), int(p.parts), a->gate, a->gate_stride_s, a->scale,
-                                           a->mod_stride_s, a->dpost_w, a->dpre_w);
-  if (e != cudaSuccess) {
-    set_error("%s: launch failed: %s", who, cudaGetErrorString(e));
-    cudaGetLastError();
-    return RA_ECUDA;
-  }
-  return launch_status(who);
+  q.dpost_w = a->dpost_w, q.dpre_w = a->dpre_w;
+  return launch(who, column_sum_kernel, q, dim3((a->C + 31) / 32), 1024, 0, st);
 }
