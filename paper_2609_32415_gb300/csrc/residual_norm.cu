@@ -12,14 +12,16 @@
 //   dpre_w = sum_s (1 + scale_s) S1_s,  dpost_w = sum_s gate_s S2_s
 //
 // HBM-bound: 8 C bytes a row forward (h, y read, h', x written), 12 C backward.
-// A row belongs to a group of warps, eight columns per thread and piece, so that
-// what a sample's rows share (gate, scale, shift; the column sums) stays in
-// registers while a CTA walks its rows: read per row instead, the fp32 vectors
-// would be 12 C bytes through L1, more than the row. Each thread copies its own
-// pieces of the rows to come into a ring of its own in shared memory (cp.async),
-// which needs no barrier and keeps S - 1 rows a group in flight. A warp reduces
-// the mean and then the squares around it with shuffles; the warps of a group
-// join theirs (count, sum, squares) through shared memory with one barrier.
+// What holds it up is the latency of the reductions between. A row belongs to a
+// group of warps, one or two pieces of eight columns a thread. Forward, a group works
+// on two rows of a sample at once: their reductions share shuffles and barriers, and
+// their instructions fill each other's latencies (backward, the norms' two reductions
+// go together likewise; two rows would spill). A thread copies its own pieces of the
+// rows to come into a ring of its own in shared memory (cp.async: no barrier);
+// what a sample's rows share (gate, scale, shift with the weights; 12 C bytes, more
+// than the row) lies in shared memory, the column sums of the backward pass in
+// registers. A warp reduces the mean and then the squares around it; the warps of a
+// group join theirs (count, mean, squares) through shared memory with one barrier.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -33,8 +35,10 @@ namespace ra {
 namespace resnorm {
 
 constexpr int MAX_C = 5120;
-constexpr int FWD_STAGES = 4, BWD_STAGES = 3;
-constexpr int FWD_THREADS = 512, BWD_THREADS = 384;  // at most, per CTA: 128 and 168 registers a thread
+constexpr int MAX_PIECES = 2;                        // of a row, a thread's at most
+constexpr int FWD_THREADS = 640, BWD_THREADS = 384;  // of a CTA at most: 96 and 168 registers a thread
+constexpr int MAX_STAGES = 4;                        // rows of a group in its ring
+constexpr int SMEM_MAX = 227 * 1024;
 
 struct Seg {
   const __nv_bfloat16* h;
@@ -57,7 +61,7 @@ struct Seg {
 
 struct Params {
   int32_t n_seg, B, C, post, pre;
-  int32_t groups;  // of a CTA
+  int32_t groups, stages;  // of a CTA; of a ring
   float eps, alpha;
   const int32_t* mode;
   Seg seg[3];
@@ -65,7 +69,7 @@ struct Params {
 
 struct GradParams {
   int32_t B, C, rows, post, pre;
-  int32_t groups;
+  int32_t groups, stages;
   int32_t parts;  // CTAs that share a sample's rows
   float eps, alpha;
   const __nv_bfloat16 *h, *y, *dx, *dh_out;
@@ -85,6 +89,16 @@ __device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commi
 template <int N>
 __device__ __forceinline__ void cp_async_wait() {
   asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+// All but the newest n of this thread's copies have landed.
+__device__ __forceinline__ void cp_async_wait_upto(int n) {
+  static_assert(MAX_STAGES == 4, "one case per ring length");
+  if (n == 1)
+    cp_async_wait<1>();
+  else if (n == 2)
+    cp_async_wait<2>();
+  else
+    cp_async_wait<3>();
 }
 
 // Eight values as four packed pairs (the FMA pipe's two-wide instructions).
@@ -133,264 +147,354 @@ __device__ __forceinline__ float sum2(uint64_t v) {
 }
 
 // This thread's place in its group of T warps: piece j < V of a row is columns
-// 8 (lane_g + 32 T j); only the last piece can be missing.
+// 8 (lane_g + 32 T j); the last piece can be missing.
 template <int V, int T>
 struct Place {
   int group, warp, lane_g;
-  int pieces;
   bool last;
-  float n_warp, inv_n;  // elements of a row in this warp
+  float inv_n;  // 1 / elements of a row in this warp
   __device__ __forceinline__ explicit Place(int C) {
     group = threadIdx.x / (32 * T);
     lane_g = threadIdx.x - group * (32 * T);
     warp = lane_g >> 5;
-    pieces = C >> 3;
+    const int pieces = C >> 3;
     last = lane_g + 32 * T * (V - 1) < pieces;
-    int n = 0;
-#pragma unroll
-    for (int j = 0; j < V; ++j) n += min(max(pieces - 32 * (warp + T * j), 0), 32);
-    n_warp = float(8 * n);
-    inv_n = 1.f / fmaxf(n_warp, 1.f);
+    inv_n = 1.f / fmaxf(count(warp, pieces), 1.f);
   }
   __device__ __forceinline__ bool has(int j) const { return j < V - 1 || last; }
   __device__ __forceinline__ int col(int j) const { return 8 * (lane_g + 32 * T * j); }
+  // Elements of a row in warp w of the group.
+  static __device__ __forceinline__ float count(int w, int pieces) {
+    return float(256 * (V - 1) + 8 * min(max(pieces - 32 * (w + T * (V - 1)), 0), 32));
+  }
 };
 
-__device__ __forceinline__ float warp_sum(float v) {
+// Two sums in the shuffles of one: even lanes get a's, odd lanes b's.
+__device__ __forceinline__ float warp_sum2(float a, float b) {
+  const bool odd = threadIdx.x & 1;
+  float v = (odd ? b : a) + __shfl_xor_sync(0xffffffffu, odd ? a : b, 1);
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  for (int o = 16; o > 1; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
   return v;
 }
-
-// What the warps of a group hand one another: two entries of four floats per
-// warp, two sets in turn, so that one barrier an exchange is enough.
+// What the warps of a group hand one another: four floats per warp, two sets in
+// turn, so that one barrier an exchange is enough.
 template <int T>
 struct Exchange {
-  float4* mem;  // of the group: [2][T][2]
+  float4* mem;  // of the group: [2][T]
   int bar, set;
+  static constexpr int BYTES = 2 * T * 16;
   __device__ __forceinline__ Exchange(void* base, int group)
-      : mem(reinterpret_cast<float4*>(base) + group * 4 * T), bar(1 + group), set(0) {}
-  static constexpr int BYTES = 4 * T * int(sizeof(float4));  // of a group
-  // Returns the group's entries: warp w's at [2 w] and [2 w + 1].
-  __device__ __forceinline__ const float4* swap(int warp, float4 a, float4 b) {
-    float4* m = mem + set * 2 * T;
+      : mem(reinterpret_cast<float4*>(base) + group * 2 * T), bar(1 + group), set(0) {}
+  __device__ __forceinline__ float* entries() {
+    float4* m = mem + set * T;
     set ^= 1;
-    if ((threadIdx.x & 31) == 0) m[2 * warp] = a, m[2 * warp + 1] = b;
+    return reinterpret_cast<float*>(m);
+  }
+  __device__ __forceinline__ void meet() {
     if (T == 1)
       __syncwarp();
     else
       named_bar_sync(bar, 32 * T);
-    return m;
   }
   // Sums of two values over the group.
   __device__ __forceinline__ float2 sums(int warp, float a, float b) {
-    a = warp_sum(a), b = warp_sum(b);
-    if (T == 1) return make_float2(a, b);
-    const float4 e = make_float4(a, b, 0.f, 0.f);
-    float4* m = mem + set * 2 * T;
-    set ^= 1;
-    if ((threadIdx.x & 31) == 0) m[warp] = e;
-    named_bar_sync(bar, 32 * T);
-    float2 r = make_float2(0.f, 0.f);
+    const float v = warp_sum2(a, b);
+    float* m = entries();
+    if ((threadIdx.x & 30) == 0) m[2 * warp + (threadIdx.x & 1)] = v;
+    meet();
+    const float2* e = reinterpret_cast<const float2*>(m);
+    float2 r = e[0];
 #pragma unroll
-    for (int w = 0; w < T; ++w) {
-      const float4 t = m[w];
+    for (int w = 1; w < T; ++w) {
+      const float2 t = e[w];
       r.x += t.x, r.y += t.y;
     }
     return r;
   }
 };
 
-// A warp's share of a norm's statistics: its mean, the squares around it and
-// their count (LAYER), or zero and the squares (RMS).
+template <int V>
+__device__ __forceinline__ float sum_of(const Vec (&v)[V]) {  // missing pieces are zeros
+  uint64_t a = f2_add(v[0].p[0], v[0].p[1]), b = f2_add(v[0].p[2], v[0].p[3]);
+#pragma unroll
+  for (int j = 1; j < V; ++j) {
+    a = f2_add(a, f2_add(v[j].p[0], v[j].p[1]));
+    b = f2_add(b, f2_add(v[j].p[2], v[j].p[3]));
+  }
+  return sum2(f2_add(a, b));
+}
 template <int V, int T>
-__device__ __forceinline__ float4 warp_stats(int kind, const Place<V, T>& at, const Vec (&v)[V]) {
-  float mean = 0.f;
-  uint64_t acc0 = both(0.f), acc1 = acc0;
-  if (kind == RA_NORM_LAYER) {
+__device__ __forceinline__ float squares_around(const Place<V, T>& at, const Vec (&v)[V], float mean) {
+  uint64_t a = both(0.f), b = a;
+  const uint64_t neg = both(-mean);
 #pragma unroll
-    for (int j = 0; j < V; ++j) {  // a missing piece is zeros
-      acc0 = f2_add(acc0, f2_add(v[j].p[0], v[j].p[1]));
-      acc1 = f2_add(acc1, f2_add(v[j].p[2], v[j].p[3]));
-    }
-    mean = warp_sum(sum2(f2_add(acc0, acc1))) * at.inv_n;
-    acc0 = acc1 = both(0.f);
-    const uint64_t neg = both(-mean);
-#pragma unroll
-    for (int j = 0; j < V; ++j)
-      if (at.has(j)) {
-#pragma unroll
-        for (int i = 0; i < 4; i += 2) {
-          const uint64_t d0 = f2_add(v[j].p[i], neg), d1 = f2_add(v[j].p[i + 1], neg);
-          acc0 = f2_fma(d0, d0, acc0);
-          acc1 = f2_fma(d1, d1, acc1);
-        }
-      }
-  } else {
-#pragma unroll
-    for (int j = 0; j < V; ++j)
+  for (int j = 0; j < V; ++j)
+    if (at.has(j)) {
 #pragma unroll
       for (int i = 0; i < 4; i += 2) {
-        acc0 = f2_fma(v[j].p[i], v[j].p[i], acc0);
-        acc1 = f2_fma(v[j].p[i + 1], v[j].p[i + 1], acc1);
+        const uint64_t d0 = f2_add(v[j].p[i], neg), d1 = f2_add(v[j].p[i + 1], neg);
+        a = f2_fma(d0, d0, a);
+        b = f2_fma(d1, d1, b);
       }
-  }
-  return make_float4(mean, warp_sum(sum2(f2_add(acc0, acc1))), at.n_warp, 0.f);
-}
-// -mean and 1 / deviation of the row from its warps' shares (warp w's at m[2 w]).
-template <int T>
-__device__ __forceinline__ float2 join_stats(int kind, const float4* m, float inv_c, float eps) {
-  float mean = 0.f, sq = 0.f;
-  if (kind == RA_NORM_LAYER) {
-#pragma unroll
-    for (int w = 0; w < T; ++w) {
-      const float4 t = m[2 * w];
-      mean = fmaf(t.z, t.x, mean);
     }
-    mean *= inv_c;
-    asm volatile("" ::: "memory");  // read again: 3 T registers would spill
+  return sum2(f2_add(a, b));
+}
+template <int V>
+__device__ __forceinline__ float squares_of(const Vec (&v)[V]) {
+  uint64_t a = both(0.f), b = a;
+#pragma unroll
+  for (int j = 0; j < V; ++j)
+#pragma unroll
+    for (int i = 0; i < 4; i += 2) {
+      a = f2_fma(v[j].p[i], v[j].p[i], a);
+      b = f2_fma(v[j].p[i + 1], v[j].p[i + 1], b);
+    }
+  return sum2(f2_add(a, b));
+}
+
+// -mean and 1 / deviation of two rows from their warps' shares, four floats each:
+// mean and squares around it of the one row and of the other. layer: the means
+// count (those of RMS are zeros).
+template <int V, int T>
+__device__ __forceinline__ float4 join_stats(bool layer, const float4* m, int pieces, float inv_c, float eps) {
+  float mean0 = 0.f, mean1 = 0.f, sq0 = 0.f, sq1 = 0.f;
+  if (T == 1) {
+    const float4 t = m[0];
+    mean0 = t.x, sq0 = t.y, mean1 = t.z, sq1 = t.w;
+  } else if (layer) {
 #pragma unroll
     for (int w = 0; w < T; ++w) {
-      const float4 t = m[2 * w];
-      const float d = t.x - mean;
-      sq = fmaf(t.z * d, d, sq + t.y);
+      const float n = Place<V, T>::count(w, pieces);
+      const float4 t = m[w];
+      mean0 = fmaf(n, t.x, mean0), mean1 = fmaf(n, t.z, mean1);
+    }
+    mean0 *= inv_c, mean1 *= inv_c;
+    asm volatile("" ::: "memory");  // read again: the entries of all warps would spill
+#pragma unroll
+    for (int w = 0; w < T; ++w) {
+      const float n = Place<V, T>::count(w, pieces);
+      const float4 t = m[w];
+      const float d0 = t.x - mean0, d1 = t.z - mean1;
+      sq0 = fmaf(n * d0, d0, sq0 + t.y), sq1 = fmaf(n * d1, d1, sq1 + t.w);
     }
   } else {
 #pragma unroll
-    for (int w = 0; w < T; ++w) sq += m[2 * w].y;
+    for (int w = 0; w < T; ++w) {
+      const float4 t = m[w];
+      sq0 += t.y, sq1 += t.w;
+    }
   }
-  return make_float2(-mean, rsqrtf(fmaf(sq, inv_c, eps)));
+  return make_float4(-mean0, rsqrtf(fmaf(sq0, inv_c, eps)), -mean1, rsqrtf(fmaf(sq1, inv_c, eps)));
 }
 
+// The statistics of two rows, of kinds k0 and k1 (one at least is a norm).
+template <int V, int T>
+__device__ __forceinline__ float4 row_stats(int k0, int k1, const Place<V, T>& at, Exchange<T>& ex, const Vec (&v0)[V],
+                                            const Vec (&v1)[V], int pieces, float inv_c, float eps) {
+  float* m = ex.entries();
+  const int lane = threadIdx.x & 31;
+  const bool layer = k0 == RA_NORM_LAYER || k1 == RA_NORM_LAYER;
+  float mean = 0.f, sq;  // of the row that the lane's parity says
+  if (layer) {
+    mean = warp_sum2(sum_of(v0), sum_of(v1)) * at.inv_n;
+    if (k0 != k1 && (lane & 1 ? k1 : k0) != RA_NORM_LAYER) mean = 0.f;
+    const float other = __shfl_xor_sync(0xffffffffu, mean, 1);
+    sq = warp_sum2(squares_around(at, v0, lane & 1 ? other : mean), squares_around(at, v1, lane & 1 ? mean : other));
+  } else {
+    sq = warp_sum2(squares_of(v0), squares_of(v1));
+  }
+  if (lane < 2) *reinterpret_cast<float2*>(m + 4 * at.warp + 2 * lane) = make_float2(mean, sq);
+  ex.meet();
+  return join_stats<V, T>(layer, reinterpret_cast<const float4*>(m), pieces, inv_c, eps);
+}
+
+// A sample's vector in shared memory, piece by piece: a piece's halves apart, so
+// that a warp's 16-byte reads meet no bank conflicts.
+template <int V, int T>
+struct SharedVec {
+  ulonglong2* mem;  // [V][2][32 T]
+  static constexpr int BYTES = V * 2 * 32 * T * 16;
+  __device__ __forceinline__ void put(int j, int lane_g, const Vec& v) const {
+    mem[(2 * j) * 32 * T + lane_g] = make_ulonglong2(v.p[0], v.p[1]);
+    mem[(2 * j + 1) * 32 * T + lane_g] = make_ulonglong2(v.p[2], v.p[3]);
+  }
+  __device__ __forceinline__ Vec get(int j, int lane_g) const {
+    const ulonglong2 a = mem[(2 * j) * 32 * T + lane_g], b = mem[(2 * j + 1) * 32 * T + lane_g];
+    return {{a.x, a.y, b.x, b.y}};
+  }
+};
+
 // ------------------------------------------------------------------ forward
+// The pairs of rows that a group takes: a CTA's share [lo, hi) of the live rows
+// goes sample by sample (piece); of a piece's pairs group g takes g, g + groups, ...
+struct Cursor {
+  Piece w;
+  int lo, hi, at;  // the piece's rows in the share; the pair's first row
+  template <class P>
+  __device__ __forceinline__ void enter(const P& p, int row, int share_hi, int group) {
+    w.seek(p, row);
+    lo = row;
+    hi = min(share_hi, w.begin + p.seg[w.g].rows);
+    at = lo + 2 * group;
+  }
+};
+
 template <int V, int T>
 __global__ void __launch_bounds__(FWD_THREADS, 1) residual_norm_kernel(const __grid_constant__ Params p) {
-  constexpr int S = FWD_STAGES;
   extern __shared__ __align__(16) uint8_t smem[];
-  // ring[stage][piece of y, of h][thread of the CTA], then the exchange
-  const uint32_t piece_bytes = 16 * blockDim.x, stage_bytes = 2 * V * piece_bytes;
-  uint8_t* const ring = smem + 16 * threadIdx.x;
+  // gate, mul, add of the sample; the exchange; ring[stage][row of the pair][piece of y, of h][thread of the CTA]
+  using Shared = SharedVec<V, T>;
+  const Shared gate{reinterpret_cast<ulonglong2*>(smem)}, mul{reinterpret_cast<ulonglong2*>(smem + Shared::BYTES)},
+      add{reinterpret_cast<ulonglong2*>(smem + 2 * Shared::BYTES)};
   const Place<V, T> at(p.C);
-  Exchange<T> ex(smem + S * stage_bytes, at.group);
+  Exchange<T> ex(smem + 3 * Shared::BYTES, at.group);
+  const uint32_t piece_bytes = 16 * blockDim.x, row_bytes = 2 * V * piece_bytes, stage_bytes = 2 * row_bytes;
+  uint8_t* const ring = smem + 3 * Shared::BYTES + p.groups * Exchange<T>::BYTES + 16 * threadIdx.x;
   const float inv_c = 1.f / float(p.C);
+  const int pieces = p.C >> 3, S = p.stages;
   pdl_launch();
   pdl_wait();
   const int total = live_rows(p);
   const int share = total / int(gridDim.x), more = total - share * int(gridDim.x), cta = int(blockIdx.x);
   const int lo = share * cta + min(cta, more), hi = lo + share + (cta < more ? 1 : 0);
-  Piece ld;
-  if (lo < hi && p.B > 4) ld.jump(p, lo);
-  Piece w = ld;
-  // This thread's first piece of the next row to copy and of the row at work, and
-  // the steps to the group's next rows; found anew where a (segment, sample) ends.
+  if (lo == hi) return;
+  Cursor cur, ld;
+  if (p.B > 4) cur.w.jump(p, lo);
+  ld = cur;
+  ld.enter(p, lo, hi, at.group);
+  // this thread's first piece of the next pair's first row, found anew for each piece
   const __nv_bfloat16 *h_src = nullptr, *y_src = nullptr;
-  __nv_bfloat16 *h_dst = nullptr, *x_dst = nullptr;
-  int64_t h_step = 0, y_step = 0, h_out_step = 0, x_step = 0;
-  int ld_i = lo + at.group, ld_end = lo, w_end = lo;
+  bool fresh = true;
   auto load = [&](uint32_t off) {
-    if (ld_i < hi) {
-      if (ld_i >= ld_end) {
-        ld.seek(p, ld_i);
-        const Seg& sg = p.seg[ld.g];
-        ld_end = ld.begin + sg.rows;
-        const int64_t r = ld_i - ld.begin;
-        h_src = sg.h + ld.s * sg.h_ss + r * sg.h_sr + at.col(0);
-        y_src = sg.y ? sg.y + ld.s * sg.y_ss + r * sg.y_sr + at.col(0) : nullptr;
-        h_step = p.groups * sg.h_sr, y_step = sg.y ? p.groups * sg.y_sr : 0;
+    while (ld.at >= ld.hi && ld.hi < hi) {
+      ld.enter(p, ld.hi, hi, at.group);
+      fresh = true;
+    }
+    if (ld.at < ld.hi) {
+      const Seg& sg = p.seg[ld.w.g];
+      if (fresh) {
+        const int64_t r = ld.at - ld.w.begin;
+        h_src = sg.h + ld.w.s * sg.h_ss + r * sg.h_sr + at.col(0);
+        y_src = sg.y ? sg.y + ld.w.s * sg.y_ss + r * sg.y_sr + at.col(0) : nullptr;
+        fresh = false;
       }
 #pragma unroll
-      for (int j = 0; j < V; ++j)
-        if (at.has(j)) {
-          if (y_src) cp_async16(ring + off + j * piece_bytes, y_src + 256 * T * j);
-          cp_async16(ring + off + (V + j) * piece_bytes, h_src + 256 * T * j);
-        }
-      h_src += h_step, y_src += y_step;
+      for (int k = 0; k < 2; ++k) {
+        if (k == 1 && ld.at + 1 >= ld.hi) break;
+        uint8_t* to = ring + off + k * row_bytes;
+        const __nv_bfloat16 *h = h_src + k * sg.h_sr, *y = y_src + k * sg.y_sr;
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+          if (at.has(j)) {
+            if (y_src) cp_async16(to + j * piece_bytes, y + 256 * T * j);
+            cp_async16(to + (V + j) * piece_bytes, h + 256 * T * j);
+          }
+      }
+      h_src += 2 * p.groups * sg.h_sr;
+      if (y_src) y_src += 2 * p.groups * sg.y_sr;
+      ld.at += 2 * p.groups;
     }
-    ld_i += p.groups;
     cp_async_commit();
   };
-#pragma unroll
   for (int k = 0; k < S - 1; ++k) load(k * stage_bytes);
-  Vec gate[V], mul[V], add[V];
-  bool has_y = false;
   uint32_t off = 0, ld_off = (S - 1) * stage_bytes;
-  for (int i = lo + at.group; i < hi; i += p.groups) {
-    if (i >= w_end) {  // another sample's rows: its vectors
-      w.seek(p, i);
-      const Seg& sg = p.seg[w.g];
-      w_end = w.begin + sg.rows;
-      const int64_t r = i - w.begin;
-      has_y = sg.y != nullptr;
-      h_dst = sg.h_out ? sg.h_out + w.s * sg.o_ss + r * sg.o_sr + at.col(0) : nullptr;
-      x_dst = sg.x ? sg.x + w.s * sg.x_ss + r * sg.x_sr + at.col(0) : nullptr;
-      h_out_step = sg.h_out ? p.groups * sg.o_sr : 0, x_step = sg.x ? p.groups * sg.x_sr : 0;
+  for (cur.hi = lo; cur.hi < hi;) {
+    if (cur.hi != lo) __syncthreads();  // every group is done with the last sample's vectors
+    cur.enter(p, cur.hi, hi, at.group);
+    const Seg& sg = p.seg[cur.w.g];
+    const int s = cur.w.s;
+    if (at.group == 0) {
 #pragma unroll
       for (int j = 0; j < V; ++j) {
         if (!at.has(j)) continue;
         const int c = at.col(j);
-        gate[j] = vec8(sg.gate ? sg.gate + w.s * sg.gate_ss : nullptr, c, 1.f) * vec8(sg.post_w, c, 1.f);
-        mul[j] = (vec8(sg.scale ? sg.scale + w.s * sg.mod_ss : nullptr, c, 0.f) + all(1.f)) * vec8(sg.pre_w, c, 1.f);
-        add[j] = vec8(sg.shift ? sg.shift + w.s * sg.mod_ss : nullptr, c, 0.f);
+        gate.put(j, at.lane_g, vec8(sg.gate ? sg.gate + s * sg.gate_ss : nullptr, c, 1.f) * vec8(sg.post_w, c, 1.f));
+        mul.put(j, at.lane_g,
+                (vec8(sg.scale ? sg.scale + s * sg.mod_ss : nullptr, c, 0.f) + all(1.f)) * vec8(sg.pre_w, c, 1.f));
+        add.put(j, at.lane_g, vec8(sg.shift ? sg.shift + s * sg.mod_ss : nullptr, c, 0.f));
       }
     }
-    load(ld_off);
-    ld_off = off;
-    cp_async_wait<S - 1>();
-    Vec v[V];
-    auto fetch = [&](int q, int j) {
-      return widen(at.has(j) ? *reinterpret_cast<const uint4*>(ring + off + (q * V + j) * piece_bytes)
-                             : make_uint4(0, 0, 0, 0));
-    };
-    if (has_y) {
+    __syncthreads();
+    const bool has_y = sg.y != nullptr;
+    const int64_t r = cur.at - cur.w.begin;
+    __nv_bfloat16* h_dst = sg.h_out ? sg.h_out + s * sg.o_ss + r * sg.o_sr + at.col(0) : nullptr;
+    __nv_bfloat16* x_dst = sg.x ? sg.x + s * sg.x_ss + r * sg.x_sr + at.col(0) : nullptr;
+    for (; cur.at < cur.hi; cur.at += 2 * p.groups) {
+      load(ld_off);
+      ld_off = off;
+      cp_async_wait_upto(S - 1);
+      const bool second = cur.at + 1 < cur.hi;  // else the pair's second row is what the ring held
+      Vec v[2][V];
+      auto fetch = [&](int k, int q, int j) {
+        return widen(at.has(j) ? *reinterpret_cast<const uint4*>(ring + off + k * row_bytes + (q * V + j) * piece_bytes)
+                               : make_uint4(0, 0, 0, 0));
+      };
+      if (has_y) {
 #pragma unroll
-      for (int j = 0; j < V; ++j) v[j] = fetch(0, j);
-      if (p.post != RA_NORM_NONE) {
-        const float4 mine = warp_stats<V, T>(p.post, at, v);
-        const float2 st = join_stats<T>(p.post, ex.swap(at.warp, mine, mine), inv_c, p.eps);
+        for (int k = 0; k < 2; ++k)
 #pragma unroll
-        for (int j = 0; j < V; ++j) v[j] = (v[j] + all(st.x)) * all(st.y);
+          for (int j = 0; j < V; ++j) v[k][j] = fetch(k, 0, j);
+        float4 st = make_float4(0.f, 1.f, 0.f, 1.f);
+        if (p.post != RA_NORM_NONE) st = row_stats<V, T>(p.post, p.post, at, ex, v[0], v[1], pieces, inv_c, p.eps);
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+          if (at.has(j)) {
+            const Vec g = gate.get(j, at.lane_g);
+            v[0][j] = fma((v[0][j] + all(st.x)) * all(st.y), g, all(p.alpha) * fetch(0, 1, j));
+            v[1][j] = fma((v[1][j] + all(st.z)) * all(st.w), g, all(p.alpha) * fetch(1, 1, j));
+          } else {
+            v[0][j] = v[1][j] = all(0.f);
+          }
+        }
+      } else {
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+          for (int j = 0; j < V; ++j) v[k][j] = all(p.alpha) * fetch(k, 1, j);
       }
+      if (h_dst) {
 #pragma unroll
-      for (int j = 0; j < V; ++j)
-        if (at.has(j)) v[j] = fma(v[j], gate[j], all(p.alpha) * fetch(1, j));
-    } else {
-#pragma unroll
-      for (int j = 0; j < V; ++j) v[j] = all(p.alpha) * fetch(1, j);
-    }
-    if (!at.last) v[V - 1] = all(0.f);
-    if (h_dst) {
-#pragma unroll
-      for (int j = 0; j < V; ++j)
-        if (at.has(j)) *reinterpret_cast<uint4*>(h_dst + 256 * T * j) = narrow(v[j]);
-      h_dst += h_out_step;
-    }
-    if (x_dst) {
-      float2 st = make_float2(0.f, 1.f);
-      if (p.pre != RA_NORM_NONE) {
-        const float4 mine = warp_stats<V, T>(p.pre, at, v);
-        st = join_stats<T>(p.pre, ex.swap(at.warp, mine, mine), inv_c, p.eps);
+        for (int j = 0; j < V; ++j)
+          if (at.has(j)) {
+            *reinterpret_cast<uint4*>(h_dst + 256 * T * j) = narrow(v[0][j]);
+            if (second) *reinterpret_cast<uint4*>(h_dst + sg.o_sr + 256 * T * j) = narrow(v[1][j]);
+          }
+        h_dst += 2 * p.groups * sg.o_sr;
       }
+      if (x_dst) {
+        float4 st = make_float4(0.f, 1.f, 0.f, 1.f);
+        if (p.pre != RA_NORM_NONE) st = row_stats<V, T>(p.pre, p.pre, at, ex, v[0], v[1], pieces, inv_c, p.eps);
 #pragma unroll
-      for (int j = 0; j < V; ++j)
-        if (at.has(j))
-          *reinterpret_cast<uint4*>(x_dst + 256 * T * j) = narrow(fma((v[j] + all(st.x)) * all(st.y), mul[j], add[j]));
-      x_dst += x_step;
+        for (int j = 0; j < V; ++j)
+          if (at.has(j)) {
+            const Vec m = mul.get(j, at.lane_g), a = add.get(j, at.lane_g);
+            *reinterpret_cast<uint4*>(x_dst + 256 * T * j) = narrow(fma((v[0][j] + all(st.x)) * all(st.y), m, a));
+            if (second)
+              *reinterpret_cast<uint4*>(x_dst + sg.x_sr + 256 * T * j) =
+                  narrow(fma((v[1][j] + all(st.z)) * all(st.w), m, a));
+          }
+        x_dst += 2 * p.groups * sg.x_sr;
+      }
+      off += stage_bytes;
+      if (off == S * stage_bytes) off = 0;
     }
-    off += stage_bytes;
-    if (off == S * stage_bytes) off = 0;
   }
 }
 
 // ------------------------------------------------------------------ backward
 template <int V, int T>
 __global__ void __launch_bounds__(BWD_THREADS, 1) residual_norm_grad_kernel(const __grid_constant__ GradParams p) {
-  constexpr int S = BWD_STAGES;
   extern __shared__ __align__(16) uint8_t smem[];
-  const uint32_t piece_bytes = 16 * blockDim.x, stage_bytes = 4 * V * piece_bytes;
-  uint8_t* const ring = smem + 16 * threadIdx.x;
+  // mul, gate of the sample; the exchange; ring[stage][piece of h, y, dx, dh_out][thread of the CTA]
+  using Shared = SharedVec<V, T>;
+  const Shared mul{reinterpret_cast<ulonglong2*>(smem)}, gate{reinterpret_cast<ulonglong2*>(smem + Shared::BYTES)};
   const Place<V, T> at(p.C);
-  Exchange<T> ex(smem + S * stage_bytes, at.group);
+  Exchange<T> ex(smem + 2 * Shared::BYTES, at.group);
+  const uint32_t piece_bytes = 16 * blockDim.x, stage_bytes = 4 * V * piece_bytes;
+  uint8_t* const ring = smem + 2 * Shared::BYTES + p.groups * Exchange<T>::BYTES + 16 * threadIdx.x;
   const float inv_c = 1.f / float(p.C);
+  const int pieces = p.C >> 3, S = p.stages;
   pdl_launch();
   pdl_wait();
   const int s = int(blockIdx.x) / p.parts, part = int(blockIdx.x) - s * p.parts;
@@ -404,8 +508,6 @@ __global__ void __launch_bounds__(BWD_THREADS, 1) residual_norm_grad_kernel(cons
                       *dx = start(p.dx, p.dx_ss, p.dx_sr), *dho = start(p.dh_out, p.dho_ss, p.dho_sr);
   const bool has_y = y != nullptr, has_dx = dx != nullptr, has_dho = dho != nullptr;
   int ld_i = first;
-  const int64_t h_step = p.groups * p.h_sr, y_step = p.groups * p.y_sr, dx_step = p.groups * p.dx_sr,
-                dho_step = p.groups * p.dho_sr;
   auto load = [&](uint32_t off) {
     if (ld_i < hi) {
 #pragma unroll
@@ -417,33 +519,38 @@ __global__ void __launch_bounds__(BWD_THREADS, 1) residual_norm_grad_kernel(cons
           if (has_dx) cp_async16(to + 2 * V * piece_bytes, dx + 256 * T * j);
           if (has_dho) cp_async16(to + 3 * V * piece_bytes, dho + 256 * T * j);
         }
-      h += h_step, y += y_step, dx += dx_step, dho += dho_step;
+      h += p.groups * p.h_sr;
+      if (has_y) y += p.groups * p.y_sr;
+      if (has_dx) dx += p.groups * p.dx_sr;
+      if (has_dho) dho += p.groups * p.dho_sr;
     }
     ld_i += p.groups;
     cp_async_commit();
   };
-#pragma unroll
   for (int k = 0; k < S - 1; ++k) load(k * stage_bytes);
-  Vec mul[V], gate[V];          // pre_w (1 + scale), gate post_w
-  Vec s0[V], s1[V], s2[V];      // column sums of the group's rows
+  if (at.group == 0) {
 #pragma unroll
-  for (int j = 0; j < V; ++j) {
-    s0[j] = s1[j] = s2[j] = mul[j] = gate[j] = all(0.f);
-    if (!at.has(j)) continue;
-    const int c = at.col(j);
-    mul[j] = (vec8(p.scale ? p.scale + s * p.mod_ss : nullptr, c, 0.f) + all(1.f)) * vec8(p.pre_w, c, 1.f);
-    gate[j] = vec8(p.gate ? p.gate + s * p.gate_ss : nullptr, c, 1.f) * vec8(p.post_w, c, 1.f);
+    for (int j = 0; j < V; ++j) {
+      if (!at.has(j)) continue;
+      const int c = at.col(j);
+      mul.put(j, at.lane_g,
+              (vec8(p.scale ? p.scale + s * p.mod_ss : nullptr, c, 0.f) + all(1.f)) * vec8(p.pre_w, c, 1.f));
+      gate.put(j, at.lane_g, vec8(p.gate ? p.gate + s * p.gate_ss : nullptr, c, 1.f) * vec8(p.post_w, c, 1.f));
+    }
   }
+  __syncthreads();
+  Vec s0[V], s1[V], s2[V];  // column sums of the group's rows
+#pragma unroll
+  for (int j = 0; j < V; ++j) s0[j] = s1[j] = s2[j] = all(0.f);
   auto place = [&](__nv_bfloat16* t, int64_t ss, int64_t sr) {
     return t ? t + s * ss + first * sr + at.col(0) : nullptr;
   };
   __nv_bfloat16 *dh = place(p.dh, p.dh_ss, p.dh_sr), *dy = place(p.dy, p.dy_ss, p.dy_sr);
-  const int64_t dh_step = p.groups * p.dh_sr, dy_step = p.groups * p.dy_sr;
   uint32_t off = 0, ld_off = (S - 1) * stage_bytes;
   for (int i = first; i < hi; i += p.groups) {
     load(ld_off);
     ld_off = off;
-    cp_async_wait<S - 1>();
+    cp_async_wait_upto(S - 1);
     auto fetch = [&](bool given, int q, int j) {
       return widen(given && at.has(j) ? *reinterpret_cast<const uint4*>(ring + off + (q * V + j) * piece_bytes)
                                       : make_uint4(0, 0, 0, 0));
@@ -453,18 +560,17 @@ __global__ void __launch_bounds__(BWD_THREADS, 1) residual_norm_grad_kernel(cons
     for (int j = 0; j < V; ++j) a[j] = fetch(true, 0, j), b[j] = fetch(has_y, 1, j);
     float2 sa = make_float2(0.f, 1.f), sb = sa;
     if (p.pre != RA_NORM_NONE || p.post != RA_NORM_NONE) {
-      const float4 ma = warp_stats<V, T>(p.pre, at, a), mb = warp_stats<V, T>(p.post, at, b);
-      const float4* m = ex.swap(at.warp, ma, mb);
-      if (p.pre != RA_NORM_NONE) sa = join_stats<T>(p.pre, m, inv_c, p.eps);
-      if (p.post != RA_NORM_NONE) sb = join_stats<T>(p.post, m + 1, inv_c, p.eps);
+      const float4 st = row_stats<V, T>(p.pre, p.post, at, ex, a, b, pieces, inv_c, p.eps);
+      if (p.pre != RA_NORM_NONE) sa = make_float2(st.x, st.y);
+      if (p.post != RA_NORM_NONE) sb = make_float2(st.z, st.w);
     }
     // the norm before the next branch
     uint64_t e0 = both(0.f), e1 = e0;
 #pragma unroll
     for (int j = 0; j < V; ++j) {
+      if (!at.has(j)) continue;
       a[j] = (a[j] + all(sa.x)) * all(sa.y);
-      if (!at.has(j)) a[j] = all(0.f);
-      const Vec d = fetch(has_dx, 2, j), e = d * mul[j];
+      const Vec d = fetch(has_dx, 2, j), e = d * mul.get(j, at.lane_g);
       s0[j] = s0[j] + d;
       s1[j] = fma(d, a[j], s1[j]);
 #pragma unroll
@@ -482,21 +588,21 @@ __global__ void __launch_bounds__(BWD_THREADS, 1) residual_norm_grad_kernel(cons
     e0 = e1 = both(0.f);
 #pragma unroll
     for (int j = 0; j < V; ++j) {
+      if (!at.has(j)) continue;
       // dH = dh' + r (e - m(e) - x^ m(e x^))
-      const Vec e = fma(a[j], all(m.y), fma(fetch(has_dx, 2, j), mul[j], all(m.x)));
+      const Vec e = fma(a[j], all(m.y), fma(fetch(has_dx, 2, j), mul.get(j, at.lane_g), all(m.x)));
       a[j] = fma(e, all(sa.y), fetch(has_dho, 3, j));
-      if (!at.has(j)) a[j] = all(0.f);
       b[j] = (b[j] + all(sb.x)) * all(sb.y);
-      if (dh && at.has(j)) *reinterpret_cast<uint4*>(dh + 256 * T * j) = narrow(a[j] * all(p.alpha));
+      if (dh) *reinterpret_cast<uint4*>(dh + 256 * T * j) = narrow(a[j] * all(p.alpha));
       s2[j] = fma(a[j], b[j], s2[j]);
-      a[j] = a[j] * gate[j];
+      a[j] = a[j] * gate.get(j, at.lane_g);
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         e0 = f2_add(e0, a[j].p[k]);
         e1 = f2_fma(a[j].p[k], b[j].p[k], e1);
       }
     }
-    if (dh) dh += dh_step;
+    if (dh) dh += p.groups * p.dh_sr;
     // the norm after the branch
     if (dy) {
       m = make_float2(0.f, 0.f);
@@ -509,12 +615,12 @@ __global__ void __launch_bounds__(BWD_THREADS, 1) residual_norm_grad_kernel(cons
       for (int j = 0; j < V; ++j)
         if (at.has(j))
           *reinterpret_cast<uint4*>(dy + 256 * T * j) = narrow(fma(b[j], all(m.y), a[j] + all(m.x)) * all(sb.y));
-      dy += dy_step;
+      dy += p.groups * p.dy_sr;
     }
     off += stage_bytes;
     if (off == S * stage_bytes) off = 0;
   }
-  // The CTA's column sums: its groups' in order, through the ring's memory.
+  // The CTA's column sums: its groups' in order, through shared memory.
   cp_async_wait<0>();
   __syncthreads();
   float* sums = reinterpret_cast<float*>(smem);  // [group][3][C]
@@ -617,7 +723,7 @@ bool same_or_apart(const void* a, int64_t a_ss, int64_t a_sr, const void* b, int
 template <class P>
 ra_status launch(const char* who, void (*fn)(P), const P& p, dim3 grid, int threads, int smem, cudaStream_t st) {
   if (smem > 48 * 1024) {
-    const ra_status as = ensure_dynamic_smem(reinterpret_cast<const void*>(fn), 200 * 1024, who);
+    const ra_status as = ensure_dynamic_smem(reinterpret_cast<const void*>(fn), SMEM_MAX, who);
     if (as != RA_OK) return as;
   }
   cudaLaunchConfig_t cfg = {};
@@ -637,28 +743,59 @@ ra_status launch(const char* who, void (*fn)(P), const P& p, dim3 grid, int thre
   return launch_status(who);
 }
 
-// Pieces per thread, warps of a row's group, groups of a CTA.
+// Pieces per thread, warps of a row's group, groups of a CTA and stages of a
+// group's ring: as many groups as the threads and two stages each in shared memory
+// allow. stage_rows: rows (of any tensor) in a stage.
 struct Shape {
-  int V, warps, groups;
+  int V, warps, groups, stages, smem;
   int threads() const { return 32 * warps * groups; }
-  int exchange() const { return groups * 4 * warps * int(sizeof(float4)); }
 };
-Shape make_shape(int C, int max_threads) {
+Shape make_shape(int C, int max_threads, int vectors, int stage_rows) {
   Shape s;
-  s.V = C <= 256 ? 1 : 2;
-  s.warps = (C / 8 + 32 * s.V - 1) / (32 * s.V);
+  const int units = (C + 255) / 256;  // warp-wide pieces of a row
+  s.warps = (units + MAX_PIECES - 1) / MAX_PIECES;
+  s.V = (units + s.warps - 1) / s.warps;
+  const int piece = s.V * 32 * s.warps * 16;  // a row's, with the missing ones
+  const int fixed = vectors * 2 * piece, per_group = 2 * s.warps * 16;
   s.groups = max_threads / (32 * s.warps);
   if (s.groups > 15) s.groups = 15;  // named barriers
+  auto bytes = [&](int groups, int stages) { return fixed + groups * (per_group + stages * stage_rows * piece); };
+  while (s.groups > 1 && bytes(s.groups, 2) > SMEM_MAX) --s.groups;
+  s.stages = 2;
+  while (s.stages < MAX_STAGES && bytes(s.groups, s.stages + 1) <= SMEM_MAX) ++s.stages;
+  s.smem = bytes(s.groups, s.stages);
   return s;
 }
+Shape fwd_shape(int C) { return make_shape(C, FWD_THREADS, 3, 4); }
+Shape bwd_shape(int C) {
+  Shape s = make_shape(C, BWD_THREADS, 2, 4);
+  const int sums = s.groups * 3 * C * 4;  // the column sums take the same memory at the end
+  if (s.smem < sums) s.smem = sums;
+  return s;
+}
+static_assert(MAX_C <= 10 * 512 && MAX_PIECES == 2, "a group has at most ten warps");
 using Fwd = void (*)(Params);
 using Bwd = void (*)(GradParams);
-#define RA_RESNORM_PICK(kernel, s)                                                                          \
-  (s.V == 1 ? kernel<1, 1>                                                                                  \
-   : s.warps == 1 ? kernel<2, 1> : s.warps == 2 ? kernel<2, 2> : s.warps == 3 ? kernel<2, 3>                \
-   : s.warps == 4 ? kernel<2, 4> : s.warps == 5 ? kernel<2, 5> : s.warps == 6 ? kernel<2, 6>                \
-   : s.warps == 7 ? kernel<2, 7> : s.warps == 8 ? kernel<2, 8> : s.warps == 9 ? kernel<2, 9> : kernel<2, 10>)
-static_assert(MAX_C <= 10 * 512, "a group has at most ten warps");
+Fwd pick_fwd(const Shape& s) {
+  if (s.V == 1) return residual_norm_kernel<1, 1>;
+  switch (s.warps) {
+#define RA_CASE(T) \
+  case T: return residual_norm_kernel<2, T>;
+    RA_CASE(1) RA_CASE(2) RA_CASE(3) RA_CASE(4) RA_CASE(5) RA_CASE(6) RA_CASE(7) RA_CASE(8) RA_CASE(9) RA_CASE(10)
+#undef RA_CASE
+    default: return nullptr;
+  }
+}
+Bwd pick_bwd(const Shape& s) {
+  if (s.V == 1) return residual_norm_grad_kernel<1, 1>;
+  switch (s.warps) {
+#define RA_CASE(T) \
+  case T: return residual_norm_grad_kernel<2, T>;
+    RA_CASE(1) RA_CASE(2) RA_CASE(3) RA_CASE(4) RA_CASE(5) RA_CASE(6) RA_CASE(7) RA_CASE(8) RA_CASE(9) RA_CASE(10)
+#undef RA_CASE
+    default: return nullptr;
+  }
+}
 
 // CTAs that share a sample's rows: as many as make the fewest rounds of rows.
 int grad_parts(int B, int rows, int sms) {
@@ -755,12 +892,11 @@ extern "C" ra_status refadapt_residual_norm(const ra_resnorm_args* a, void* stre
     set_error("%s: too many rows", who);
     return RA_EINVAL;
   }
-  const Shape sh = make_shape(a->C, FWD_THREADS);
+  const Shape sh = fwd_shape(a->C);
   p.groups = sh.groups;
-  const int smem = FWD_STAGES * 2 * sh.V * 16 * sh.threads() + sh.exchange();
+  p.stages = sh.stages;
   const int64_t sms = num_sms();
-  const Fwd fn = RA_RESNORM_PICK(residual_norm_kernel, sh);
-  return launch(who, fn, p, dim3(unsigned(rows < sms ? rows : sms)), sh.threads(), smem,
+  return launch(who, pick_fwd(sh), p, dim3(unsigned(rows < sms ? rows : sms)), sh.threads(), sh.smem,
                 static_cast<cudaStream_t>(stream));
 }
 
@@ -839,13 +975,12 @@ extern "C" ra_status refadapt_residual_norm_backward(const ra_resnorm_grad_args*
   p.post_w = a->post_w, p.pre_w = a->pre_w;
   p.partial = static_cast<float*>(a->workspace);
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
-  const Shape sh = make_shape(a->C, BWD_THREADS);
+  const Shape sh = bwd_shape(a->C);
   p.groups = sh.groups;
+  p.stages = sh.stages;
   p.parts = a->rows > 0 ? grad_parts(a->B, a->rows, num_sms()) : 0;
   if (a->rows > 0) {
-    const int smem = BWD_STAGES * 4 * sh.V * 16 * sh.threads() + sh.exchange();
-    const Bwd fn = RA_RESNORM_PICK(residual_norm_grad_kernel, sh);
-    const ra_status r = launch(who, fn, p, dim3(unsigned(a->B * p.parts)), sh.threads(), smem, st);
+    const ra_status r = launch(who, pick_bwd(sh), p, dim3(unsigned(a->B * p.parts)), sh.threads(), sh.smem, st);
     if (r != RA_OK) return r;
   }
   if (!a->dpre_w && !a->dpost_w && !a->dgate && !a->dscale && !a->dshift) return RA_OK;
