@@ -24,6 +24,8 @@
 //               (rank 0's).
 //   warps 2..9  epilogue, two warps per TMEM lane quarter, while the next tile's
 //               MMAs fill the other accumulator.
+// A forward call of a few rows reads its weights once and little else, so it has a
+// kernel of its own (glu_rows_kernel).
 // Every mbarrier wait is bounded; on a timeout the CTA drains its own copies and
 // MMAs, frees TMEM, flags the error word and returns.
 #include <cuda.h>
@@ -539,6 +541,122 @@ __global__ void __launch_bounds__(THREADS, 1) glu_kernel(const __grid_constant__
   if (warp == 1) tmem_dealloc_pair(tmem, TMEM_COLS);
 }
 
+// ------------------------------------------------------------------ few rows
+// Up to 16 rows per segment: bound by the weights' bytes (4 F C). On the tiles
+// above each CTA would wait for 128-row boxes of x that are nearly all zeros, and
+// all CTAs for the few lines that are not (1 row, C = 2048, F = 5504: 24 us; here
+// 10.2 us, 4.4 TB/s of weights; 8 rows 10.3, 16 rows 14.5, where the tiles take 16
+// and keep that up to 256 rows). A CTA takes eight features, its warps share K, and
+// a weight goes from memory into the registers of the mma.sync that uses it
+// (m16n8k16: the rows of A are the features' gate rows and their up rows, the
+// columns of B eight rows of x), so g and w of a feature and a row end in one
+// thread. K is permuted alike in A and B, so that a lane's operands are 16
+// contiguous bytes. Deeper rounds of loads, two features' groups a CTA, a prefetch
+// into L2 ahead of the previous kernel's end and four warps measured no better.
+constexpr int ROWS_MAX = 16;
+constexpr int ROWS_WARPS = 8;
+
+struct RowsSeg {
+  Rows x;
+  const __nv_bfloat16 *w_gate, *w_up;
+  Rows out[3];
+  int32_t rows, gated;
+};
+struct RowsParams {
+  int32_t B, F, C;
+  const int32_t* mode;
+  RowsSeg seg[3];
+};
+
+__device__ __forceinline__ void mma_16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                          uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// 16 bytes, or zeros. Volatile: the loads of a round keep their place before its
+// products.
+__device__ __forceinline__ uint4 load16_if(const void* ptr, bool in) {
+  uint4 v;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %5, 0;\n\t"
+      "mov.b32 %0, 0;\n\tmov.b32 %1, 0;\n\tmov.b32 %2, 0;\n\tmov.b32 %3, 0;\n\t"
+      "@p ld.global.v4.b32 {%0, %1, %2, %3}, [%4];\n\t}"
+      : "=&r"(v.x), "=&r"(v.y), "=&r"(v.z), "=&r"(v.w)
+      : "l"(ptr), "r"(int(in))
+      : "memory");
+  return v;
+}
+
+// GROUPS: groups of eight rows; DEPTH: K blocks of 64 (a 128-byte line of a
+// weight's row) loaded at once by a warp.
+template <int ACT, int GROUPS, int DEPTH>
+__global__ void __launch_bounds__(32 * ROWS_WARPS) glu_rows_kernel(const __grid_constant__ RowsParams p) {
+  __shared__ float red[ROWS_WARPS][GROUPS][4][32];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  const RowsSeg& sg = p.seg[blockIdx.y];
+  pdl_launch();
+  const int f = int(blockIdx.x) * 8 + g, total = p.B * sg.rows;
+  const __nv_bfloat16 *wg = sg.w_gate + int64_t(f) * p.C + 8 * t, *wu = sg.w_up + int64_t(f) * p.C + 8 * t;
+  const __nv_bfloat16* x[GROUPS];
+  float acc[GROUPS][4];
+#pragma unroll
+  for (int i = 0; i < GROUPS; ++i) {
+    const int row = min(8 * i + g, total - 1), s = row / sg.rows;  // rows past the last repeat it
+    x[i] = sg.x.ptr + s * sg.x.ss + (row - s * sg.rows) * sg.x.sr + 8 * t;
+#pragma unroll
+    for (int z = 0; z < 4; ++z) acc[i][z] = 0.f;
+  }
+  pdl_wait();
+  for (int k0 = 64 * warp; k0 < p.C; k0 += 64 * ROWS_WARPS * DEPTH) {
+    uint4 a[2 * DEPTH][2], b[2 * DEPTH][GROUPS];
+#pragma unroll
+    for (int q = 0; q < 2 * DEPTH; ++q) {
+      const int k = k0 + 64 * ROWS_WARPS * (q >> 1) + 32 * (q & 1);
+      const bool in = k + 8 * t < p.C;
+      a[q][0] = load16_if(wg + k, in);
+      a[q][1] = load16_if(wu + k, in);
+#pragma unroll
+      for (int i = 0; i < GROUPS; ++i) b[q][i] = load16_if(x[i] + k, in);
+    }
+#pragma unroll
+    for (int q = 0; q < 2 * DEPTH; ++q)
+#pragma unroll
+      for (int i = 0; i < GROUPS; ++i) {
+        const uint4 &ga = a[q][0], &up = a[q][1], &xb = b[q][i];
+        mma_16816(acc[i], ga.x, up.x, ga.y, up.y, xb.x, xb.y);
+        mma_16816(acc[i], ga.z, up.z, ga.w, up.w, xb.z, xb.w);
+      }
+  }
+#pragma unroll
+  for (int i = 0; i < GROUPS; ++i)
+#pragma unroll
+    for (int z = 0; z < 4; ++z) red[warp][i][z][lane] = acc[i][z];
+  __syncthreads();
+  if (warp >= GROUPS) return;
+  float v[4];
+#pragma unroll
+  for (int z = 0; z < 4; ++z) {
+    v[z] = 0.f;
+#pragma unroll
+    for (int w = 0; w < ROWS_WARPS; ++w) v[z] += red[w][warp][z][lane];
+  }
+  float h0, h1;
+  f2_unpack(f2_mul(act2<ACT>(f2_pack(v[0], v[1]), nullptr), f2_pack(v[2], v[3])), h0, h1);
+  const float res[2][3] = {{h0, v[0], v[2]}, {h1, v[1], v[3]}};
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const int row = 8 * warp + 2 * t + k, s = row / sg.rows;
+    if (row >= total || (sg.gated && p.mode[s] == RA_MODE_REUSE)) continue;
+#pragma unroll
+    for (int z = 0; z < 3; ++z)
+      if (sg.out[z].ptr)
+        sg.out[z].ptr[s * sg.out[z].ss + (row - s * sg.rows) * sg.out[z].sr + f] = __float2bfloat16_rn(res[k][z]);
+  }
+}
+
 // Adds up the parts of the jobs that were cut, in order.
 struct JoinJob {
   const float* partial;
@@ -770,6 +888,48 @@ extern "C" ra_status refadapt_glu(const ra_glu_args* a, void* stream) {
       job.out[i] = Rows{static_cast<__nv_bfloat16*>(const_cast<void*>(o[i].ptr)), o[i].ss, o[i].sr};
   }
   if (p.n_jobs == 0) return RA_OK;
+  int most = 0;
+  for (int g = 0; g < a->n_seg; ++g)
+    if (int64_t(a->B) * a->seg[g].rows > most) most = a->B * a->seg[g].rows;
+  if (most <= ROWS_MAX) {
+    RowsParams r;
+    std::memset(&r, 0, sizeof(r));
+    r.B = a->B, r.F = a->F, r.C = a->C, r.mode = a->mode;
+    int n = 0;
+    for (int g = 0; g < a->n_seg; ++g) {
+      const ra_glu_seg& s = a->seg[g];
+      if (s.rows == 0) continue;
+      RowsSeg& d = r.seg[n++];
+      auto rows = [](const void* ptr, int64_t ss, int64_t sr) {
+        return Rows{static_cast<__nv_bfloat16*>(const_cast<void*>(ptr)), ss, sr};
+      };
+      d.x = rows(s.x, s.x_stride_s, s.x_stride_r);
+      d.w_gate = static_cast<const __nv_bfloat16*>(s.w_gate), d.w_up = static_cast<const __nv_bfloat16*>(s.w_up);
+      d.out[0] = rows(s.out, s.out_stride_s, s.out_stride_r);
+      d.out[1] = rows(s.pre_gate, s.pre_gate_stride_s, s.pre_gate_stride_r);
+      d.out[2] = rows(s.pre_up, s.pre_up_stride_s, s.pre_up_stride_r);
+      d.rows = s.rows;
+      d.gated = s.gated ? 1 : 0;
+    }
+    const bool gelu = a->act == RA_ACT_GELU;
+    void (*fn)(RowsParams) = most <= 8 ? (gelu ? glu_rows_kernel<RA_ACT_GELU, 1, 2> : glu_rows_kernel<RA_ACT_SILU, 1, 2>)
+                                       : (gelu ? glu_rows_kernel<RA_ACT_GELU, 2, 1> : glu_rows_kernel<RA_ACT_SILU, 2, 1>);
+    note_launch("few rows");
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(unsigned(a->F / 8), unsigned(n));
+    cfg.blockDim = dim3(32 * ROWS_WARPS);
+    cfg.stream = static_cast<cudaStream_t>(stream);
+    cudaLaunchAttribute attr = pdl_attribute();
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, fn, r);
+    if (e != cudaSuccess) {
+      set_error("%s: launch failed: %s", who, cudaGetErrorString(e));
+      cudaGetLastError();
+      return RA_ECUDA;
+    }
+    return launch_status(who);
+  }
   const int64_t pairs = num_sms() / 2 > 0 ? num_sms() / 2 : 1;
   double best_us = 1e30;
   int64_t units = 0;
