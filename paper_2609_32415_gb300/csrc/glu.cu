@@ -11,9 +11,11 @@
 //          stages Wg's rows as its half of the MMA's N = 2 w, rank 1 Wu's, so one
 //          MMA forms both and the epilogue has g and w of a column in one thread;
 //   GRAD   du = dy Wd; the epilogue reads g and w and writes dg and dw;
-//   STORE  the four gradients. dx sums over both pairs of operands in one
-//          accumulator (K = 2 F); a job of few tiles and a long K is cut into
-//          parts, whose fp32 sums a second kernel adds up in order.
+//   STORE  the four gradients, in one launch: dx sums over both pairs of operands
+//          in one accumulator (K = 2 F), so its tiles are the long ones and go
+//          first; pairs that get one fewer of them take more of the weights'
+//          (Schedule). A job of few tiles and a long K is cut into parts, whose
+//          fp32 sums a second kernel adds up in order.
 // An operand whose K runs along its rows (Wd, Wg, Wu as B, the rows of every
 // operand of a weight's gradient) is read as it lies, MN-major: nothing is
 // transposed in memory.
@@ -82,8 +84,23 @@ struct Job {
   float* partial;                // parts > 1: [part][sample][row][N]
 };
 
+// Which units a pair takes. Unit c, c + pairs, ... of the `longs` units that come
+// first (and take longer); the `rest` pairs that have one more of them than the
+// others then wait `early` rounds of the remaining units, which the others share.
+struct Schedule {
+  int32_t longs, early;
+  __device__ __forceinline__ int64_t unit(int c, int pairs, int i) const {
+    const int rest = longs % pairs, mine = longs / pairs + (c < rest ? 1 : 0);
+    if (i < mine) return c + int64_t(i) * pairs;
+    const int ahead = c < rest ? 0 : early, j = i - mine;
+    if (j < ahead) return longs + (c - rest) + int64_t(j) * (pairs - rest);
+    return longs + int64_t(early) * (pairs - rest) + c + int64_t(j - ahead) * pairs;
+  }
+};
+
 struct Params {
   int32_t n_jobs, bn;
+  Schedule order;
   const int32_t* mode;
   int32_t* err_word;
   uint64_t budget_ns;
@@ -410,7 +427,7 @@ __global__ void __launch_bounds__(THREADS, 1) glu_kernel(const __grid_constant__
   volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + OFF_MISC + 4);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = cluster_rank();
-  const int64_t cid = blockIdx.x >> 1, ncl = gridDim.x >> 1;
+  const int cid = int(blockIdx.x >> 1), ncl = int(gridDim.x >> 1);
   if (threadIdx.x == 0) {
     for (int s = 0; s < STAGES; ++s) {
       mbar_init(full + s, 1);
@@ -447,7 +464,7 @@ __global__ void __launch_bounds__(THREADS, 1) glu_kernel(const __grid_constant__
       bool ok = true;
       Walk<KIND> walk;
       Unit u;
-      for (int64_t t = cid; ok && walk.at(p, t, u); t += ncl) {
+      for (int i = 0; ok && walk.at(p, p.order.unit(cid, ncl, i), u); ++i) {
         if (KIND == STORE && p.job[u.job].rows_k)
           ok = pr.unit<KIND, KIND == STORE>(p, u, ctl);
         else
@@ -477,7 +494,7 @@ __global__ void __launch_bounds__(THREADS, 1) glu_kernel(const __grid_constant__
       bool ok = true;
       Walk<KIND> walk;
       Unit u;
-      for (int64_t t = cid; walk.at(p, t, u); t += ncl) {
+      for (; walk.at(p, p.order.unit(cid, ncl, i), u); ++i) {
         const int buf = i & 1, use = i >> 1;
         if (use > 0 && !(ok = mbar_wait_cluster(tempty + buf, uint32_t((use - 1) & 1), ctl))) break;
         tc_fence_after();
@@ -488,7 +505,6 @@ __global__ void __launch_bounds__(THREADS, 1) glu_kernel(const __grid_constant__
           ok = mma.unit<KIND, false>(p, u, d_t, ctl);
         if (!ok) break;
         umma_commit_pair(tfull + buf, 0x3);
-        ++i;
       }
       if (!ok && mma.issued) {
         umma_commit_pair(drain, 0x1);
@@ -505,7 +521,7 @@ __global__ void __launch_bounds__(THREADS, 1) glu_kernel(const __grid_constant__
     int i = 0;
     Walk<KIND> walk;
     Unit u;
-    for (int64_t t = cid; walk.at(p, t, u); t += ncl) {
+    for (; walk.at(p, p.order.unit(cid, ncl, i), u); ++i) {
       const int buf = i & 1, use = i >> 1;
       w.row0 = u.m0 + int(rank) * 128 + quarter * 32;
       w.nrow = min(32, p.job[u.job].rows - w.row0);
@@ -531,7 +547,6 @@ __global__ void __launch_bounds__(THREADS, 1) glu_kernel(const __grid_constant__
         else
           mbar_arrive_remote(tempty0 + 8u * buf);
       }
-      ++i;
     }
   }
   tc_fence_before();
@@ -766,49 +781,57 @@ struct Shape {
   int64_t samples, M, N, stages;
   int64_t tiles(int bn) const { return samples * div_up(M, TM) * div_up(N, bn); }
 };
-// Accumulator columns and parts of K of a launch of up to three products with
-// the cheapest sum of rounds.
+// The products of refadapt_glu_backward after dy Wd: dx, and the weights'
+// gradients. Rows of samples that follow one another are those of one sample.
+struct Products {
+  Shape x, w[3];
+  Products(int B, int rows, int C, int F, int O, bool flat_x, bool flat_w) {
+    const int64_t all = int64_t(B) * rows, stages = flat_w ? div_up(all, BK) : B * div_up(rows, BK);
+    x = Shape{flat_x ? 1 : B, flat_x ? all : rows, C, 2 * div_up(F, BK)};
+    w[0] = w[1] = Shape{1, F, C, stages};
+    w[2] = Shape{1, O, F, stages};
+  }
+};
+
+// How a launch of them is cut: accumulator columns, parts of K of dx and of the
+// weights' gradients, and the schedule's early rounds.
 struct Plan {
-  int bn, parts;
+  int bn, parts_x, parts_w, early;
 };
 constexpr int MAX_PARTS = 16;
-Plan plan_store(const Shape* s, int n, int sms) {
+// The cheapest by the time of the pair that ends last. More than two rounds of
+// tiles are not cut (a part costs a round trip of its fp32 sums).
+Plan make_plan(const Products& pr, int sms) {
   const int64_t pairs = sms / 2 > 0 ? sms / 2 : 1;
-  Plan best{256, 1};
+  Plan best{256, 1, 1, 0};
   double best_us = 1e30;
   for (int bn = 256; bn >= 128; bn /= 2)
-    for (int parts = 1; parts <= MAX_PARTS; ++parts) {
-      double work = 0, bytes = 0, longest = 0;
-      int64_t tiles = 0;
-      bool fits = true;
-      for (int i = 0; i < n; ++i) {
-        fits &= parts == 1 || s[i].stages >= 2 * parts;
-        const double r = round_us(bn, double(s[i].stages) / parts);
-        tiles += s[i].tiles(bn) * parts;
-        work += r * double(s[i].tiles(bn) * parts);
-        longest = r > longest ? r : longest;
-        bytes += 8.0 * parts * double(s[i].samples * s[i].M * s[i].N);
-      }
-      if (!fits || tiles == 0) continue;
-      // rounds of equal units; of unequal ones, their mean
-      const double us = fixed_us(bn) + work / double(tiles) * double(div_up(tiles, pairs)) +
-                        (parts > 1 ? 2.5 + bytes / 5e6 : 0.0);
-      if (us < best_us) {
-        best_us = us;
-        best = Plan{bn, parts};
+    for (int px = 1; px <= MAX_PARTS; px += px < 4 ? 1 : 4) {
+      if (px > 1 && (pr.x.stages < 2 * px || pr.x.tiles(bn) > 2 * pairs)) break;
+      for (int pw = 1; pw <= MAX_PARTS; pw += pw < 4 ? 1 : 4) {
+        const int64_t tiles_w = pr.w[0].tiles(bn) * 2 + pr.w[2].tiles(bn);
+        if (pw > 1 && (pr.w[0].stages < 2 * pw || tiles_w > 2 * pairs)) break;
+        const int64_t nx = pr.x.tiles(bn) * px, nw = tiles_w * pw, rest = nx % pairs;
+        const double a = round_us(bn, double(pr.x.stages) / px), b = round_us(bn, double(pr.w[0].stages) / pw);
+        double bytes = px > 1 ? 8.0 * px * double(pr.x.samples * pr.x.M * pr.x.N) : 0.0;
+        if (pw > 1)
+          for (const Shape& w : pr.w) bytes += 8.0 * pw * double(w.M * w.N);
+        // early rounds until the pairs without a further dx unit have caught up
+        int64_t early = rest > 0 ? int64_t(a / b + 0.5) : 0;
+        if (early * (pairs - rest) > nw) early = nw / (pairs - rest);
+        const int64_t common = div_up(nw - early * (pairs - rest), pairs);
+        const double with = double(div_up(nx, pairs)) * a, without = double(nx / pairs) * a + double(early) * b;
+        const double us = fixed_us(bn) + (with > without ? with : without) + double(common) * b +
+                          (bytes > 0 ? 2.5 + bytes / 5e6 : 0.0);
+        if (us < best_us) {
+          best_us = us;
+          best = Plan{bn, px, pw, int(early)};
+        }
       }
     }
   return best;
 }
 
-// Products of refadapt_glu_backward after dy Wd: dx, and the weights' gradients.
-// Rows that follow one another are one sample (`flat`).
-Shape dx_shape(int B, int rows, int C, int F) { return Shape{B, rows, C, 2 * div_up(F, BK)}; }
-void dw_shapes(Shape (&s)[3], int B, int rows, int C, int F, int O) {
-  const int64_t stages = B * div_up(rows, BK);
-  s[0] = s[1] = Shape{1, F, C, stages};
-  s[2] = Shape{1, O, F, stages};
-}
 size_t partial_bytes(const Shape& s, int parts) {
   return parts > 1 ? size_t(parts) * size_t(s.samples) * size_t(s.M) * size_t(s.N) * 4 : 0;
 }
@@ -962,20 +985,14 @@ extern "C" size_t refadapt_glu_backward_workspace_size(int32_t B, int32_t rows, 
   if (B < 1 || rows < 0 || C < 64 || F < 64 || O < 64) return 0;
   const int sms = ra::num_sms();
   size_t most = 0;
-  if (rows > 0) {
-    Shape w[3];
-    dw_shapes(w, B, rows, C, F, O);
-    // dx and the weights' gradients use the same scratch, one after the other; samples may join
-    for (int flat = 0; flat < 2; ++flat) {
-      const Shape x = dx_shape(flat ? 1 : B, flat ? B * rows : rows, C, F);
-      const size_t b = partial_bytes(x, plan_store(&x, 1, sms).parts);
+  if (rows > 0)
+    for (int flat = 0; flat < (B > 1 ? 4 : 1); ++flat) {
+      const Products pr(B, rows, C, F, O, flat & 1, flat & 2);
+      const Plan plan = make_plan(pr, sms);
+      size_t b = partial_bytes(pr.x, plan.parts_x);
+      for (const Shape& w : pr.w) b += partial_bytes(w, plan.parts_w);
       most = b > most ? b : most;
-      dw_shapes(w, flat ? 1 : B, flat ? B * rows : rows, C, F, O);
-      const int parts = plan_store(w, 3, sms).parts;
-      const size_t c = partial_bytes(w[0], parts) + partial_bytes(w[1], parts) + partial_bytes(w[2], parts);
-      most = c > most ? c : most;
     }
-  }
   return size_t(2) * size_t(B) * size_t(rows) * size_t(F) * 2 + most + 16;
 }
 
@@ -1020,7 +1037,7 @@ extern "C" ra_status refadapt_glu_backward(const ra_glu_grad_args* a, void* stre
     }
     return RA_OK;
   }
-  const bool dw = a->dw_gate || a->dw_up || a->dw_down, dgw = a->dx || a->dw_gate || a->dw_up;
+  const bool dgw = a->dx || a->dw_gate || a->dw_up;
   RowTensor dy{a->dy, a->dy_stride_s, a->dy_stride_r, a->B, a->rows, a->O};
   RowTensor x{a->x, a->x_stride_s, a->x_stride_r, a->B, a->rows, a->C};
   RowTensor g{a->pre_gate, a->pre_gate_stride_s, a->pre_gate_stride_r, a->B, a->rows, a->F};
@@ -1093,93 +1110,82 @@ extern "C" ra_status refadapt_glu_backward(const ra_glu_grad_args* a, void* stre
                                units, st);
     if (r != RA_OK) return r;
   }
-  auto store = [&](const Shape* shapes, int n, const Plan& plan) -> ra_status {
-    p.n_jobs = n;
-    p.bn = plan.bn;
-    int64_t units = 0;
-    float* at = partial;
-    JoinParams join;
-    join.n = 0;
-    int64_t vecs = 0;
-    for (int j = 0; j < n; ++j) {
-      Job& job = p.job[j];
-      const Shape& s = shapes[j];
-      job.samples = int32_t(s.samples), job.rows = int32_t(s.M), job.N = int32_t(s.N);
-      job.m_tiles = int32_t(div_up(s.M, TM));
-      job.cols = int32_t(div_up(s.N, plan.bn));
-      job.parts = plan.parts;
-      units += s.tiles(plan.bn) * plan.parts;
-      if (plan.parts > 1) {
-        job.partial = at;
-        JoinJob& q = join.job[join.n++];
-        q.partial = at;
-        q.plane = s.samples * s.M * s.N;
-        q.vecs = q.plane / 8;
-        q.parts = plan.parts, q.rows = job.rows, q.N = job.N;
-        q.out = job.out[0];
-        at += q.plane * plan.parts;
-        vecs += q.vecs;
-      }
+  // dx and the weights' gradients, in one launch
+  const bool flat_x = a->B == 1 || !a->dx || joins(dx);
+  const bool flat_w = a->B == 1 || ((!(a->dw_gate || a->dw_up) || joins(x)) && (!a->dw_down || (joins(dy) && joins(hid))));
+  const Products pr(a->B, a->rows, a->C, a->F, a->O, flat_x, flat_w);
+  const Plan plan = make_plan(pr, sms);
+  std::memset(p.job, 0, sizeof(p.job));
+  p.n_jobs = 0;
+  p.bn = plan.bn;
+  int64_t units = 0, vecs = 0;
+  JoinParams join;
+  join.n = 0;
+  auto add = [&](const Shape& s, int parts, const Rows& out) -> Job& {
+    Job& job = p.job[p.n_jobs++];
+    job.samples = int32_t(s.samples), job.rows = int32_t(s.M), job.N = int32_t(s.N);
+    job.m_tiles = int32_t(div_up(s.M, TM));
+    job.cols = int32_t(div_up(s.N, plan.bn));
+    job.out[0] = out;
+    units += s.tiles(plan.bn) * parts;
+    if (parts > 1) {
+      job.partial = partial;
+      JoinJob& q = join.job[join.n++];
+      q.partial = partial;
+      q.plane = s.samples * s.M * s.N;
+      q.vecs = q.plane / 8;
+      q.parts = parts, q.rows = job.rows, q.N = job.N;
+      q.out = out;
+      partial += q.plane * parts;
+      vecs += q.vecs;
     }
-    if (units > 2147483647) {
-      set_error("%s: too many rows", who);
-      return RA_EINVAL;
-    }
-    const ra_status r = launch(who, glu_kernel<STORE, 0>, p, units, st);
-    if (r != RA_OK || join.n == 0) return r;
-    cudaLaunchConfig_t cfg = {};
-    const int64_t blocks = div_up(vecs, 256), most = int64_t(8) * sms;
-    cfg.gridDim = dim3(unsigned(blocks < most ? blocks : most));
-    cfg.blockDim = dim3(256);
-    cfg.stream = st;
-    cudaLaunchAttribute attr = pdl_attribute();
-    cfg.attrs = &attr;
-    cfg.numAttrs = 1;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, join_kernel, join);
-    if (e != cudaSuccess) {
-      set_error("%s: launch failed: %s", who, cudaGetErrorString(e));
-      cudaGetLastError();
-      return RA_ECUDA;
-    }
-    return launch_status(who);
+    return job;
   };
   if (a->dx) {
-    const bool flat = joins(dx);
-    const Shape s = dx_shape(flat ? 1 : a->B, flat ? int(all) : a->rows, a->C, a->F);
-    const Plan plan = plan_store(&s, 1, sms);
-    std::memset(p.job, 0, sizeof(p.job));
-    one_span(p.job[0], a->F);
-    p.job[0].spans = 2;
-    p.job[0].out[0] = rows_of(dx);
-    if (!encode(&p.tm_a[0][0], flat ? flatten(dgt) : dgt, 128) || !encode(&p.tm_a[0][1], flat ? flatten(dwt) : dwt, 128) ||
+    Job& job = add(pr.x, plan.parts_x, rows_of(dx));
+    one_span(job, a->F);
+    job.spans = 2;
+    job.parts = plan.parts_x;
+    if (!encode(&p.tm_a[0][0], flat_x ? flatten(dgt) : dgt, 128) || !encode(&p.tm_a[0][1], flat_x ? flatten(dwt) : dwt, 128) ||
         !encode(&p.tm_b[0][0], w_gate, BK) || !encode(&p.tm_b[0][1], w_up, BK))
       return RA_EINVAL;
-    const ra_status r = store(&s, 1, plan);
-    if (r != RA_OK) return r;
+    p.order.longs = int32_t(units);
+    p.order.early = plan.early;
   }
-  if (dw) {
-    const bool flat = (!(a->dw_gate || a->dw_up) || joins(x)) && (!a->dw_down || (joins(dy) && joins(hid)));
-    Shape every[3], s[3];
-    dw_shapes(every, flat ? 1 : a->B, flat ? int(all) : a->rows, a->C, a->F, a->O);
-    const Plan plan = plan_store(every, 3, sms);
-    std::memset(p.job, 0, sizeof(p.job));
-    void* out[3] = {a->dw_gate, a->dw_up, a->dw_down};
-    int n = 0;
-    for (int i = 0; i < 3; ++i) {
-      if (!out[i]) continue;
-      Job& job = p.job[n];
-      s[n] = every[i];
-      one_span(job, flat ? int(all) : a->rows);
-      job.spans = flat ? 1 : a->B;
-      job.rows_k = 1;
-      job.out[0] = Rows{static_cast<__nv_bfloat16*>(out[i]), 0, every[i].N};
-      const RowTensor at = i == 0 ? dgt : i == 1 ? dwt : dy, bt = i == 2 ? hid : x;
-      if (!encode(&p.tm_a[n][0], flat ? flatten(at) : at, BK) || !encode(&p.tm_b[n][0], flat ? flatten(bt) : bt, BK))
-        return RA_EINVAL;
-      ++n;
-    }
-    const ra_status r = store(s, n, plan);
-    if (r != RA_OK) return r;
+  void* out[3] = {a->dw_gate, a->dw_up, a->dw_down};
+  for (int i = 0; i < 3; ++i) {
+    if (!out[i]) continue;
+    const int n = p.n_jobs;
+    Job& job = add(pr.w[i], plan.parts_w, Rows{static_cast<__nv_bfloat16*>(out[i]), 0, pr.w[i].N});
+    one_span(job, flat_w ? int(all) : a->rows);
+    job.spans = flat_w ? 1 : a->B;
+    job.parts = plan.parts_w;
+    job.rows_k = 1;
+    const RowTensor at = i == 0 ? dgt : i == 1 ? dwt : dy, bt = i == 2 ? hid : x;
+    if (!encode(&p.tm_a[n][0], flat_w ? flatten(at) : at, BK) || !encode(&p.tm_b[n][0], flat_w ? flatten(bt) : bt, BK))
+      return RA_EINVAL;
   }
-  return RA_OK;
+  if (units > 2147483647) {
+    set_error("%s: too many rows", who);
+    return RA_EINVAL;
+  }
+  const int64_t ctas = units < pairs ? units : pairs;
+  if (ctas < pairs) p.order.early = 0;  // one unit a pair
+  const ra_status r = launch(who, glu_kernel<STORE, 0>, p, units, st);
+  if (r != RA_OK || join.n == 0) return r;
+  cudaLaunchConfig_t cfg = {};
+  const int64_t blocks = div_up(vecs, 256), most = int64_t(8) * sms;
+  cfg.gridDim = dim3(unsigned(blocks < most ? blocks : most));
+  cfg.blockDim = dim3(256);
+  cfg.stream = st;
+  cudaLaunchAttribute attr = pdl_attribute();
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, join_kernel, join);
+  if (e != cudaSuccess) {
+    set_error("%s: launch failed: %s", who, cudaGetErrorString(e));
+    cudaGetLastError();
+    return RA_ECUDA;
+  }
+  return launch_status(who);
 }
