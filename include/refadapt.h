@@ -580,7 +580,9 @@ ra_status refadapt_residual_norm(const ra_resnorm_args* args, void* stream);
  *  workspace   device scratch of
  *              refadapt_residual_norm_backward_workspace_size(B, rows, C) bytes
  *              (on the device that is current), 16-byte aligned; calls that
- *              share it must be stream-ordered. */
+ *              share it must be stream-ordered.
+ *  err_word    device int32 or NULL; bit 0 set if a device wait timed out (the
+ *              sums are NaN then). */
 typedef struct {
   int32_t B, C, rows, post, pre, reserved;
   float eps, alpha;
@@ -609,6 +611,7 @@ typedef struct {
   float* dpre_w;
   void* workspace;
   size_t workspace_bytes;
+  int32_t* err_word;
 } ra_resnorm_grad_args;
 
 size_t refadapt_residual_norm_backward_workspace_size(int32_t B, int32_t rows, int32_t C);

@@ -118,7 +118,8 @@ class RaResnormGradArgs(ctypes.Structure):
         _rows("h", "y", "dx", "dh_out", "dh", "dy") + [
         ("gate", c_void_p), ("gate_stride_s", c_int64), ("scale", c_void_p), ("mod_stride_s", c_int64),
         ("post_w", c_void_p), ("pre_w", c_void_p), ("dgate", c_void_p), ("dscale", c_void_p), ("dshift", c_void_p),
-        ("dpost_w", c_void_p), ("dpre_w", c_void_p), ("workspace", c_void_p), ("workspace_bytes", c_size_t)]
+        ("dpost_w", c_void_p), ("dpre_w", c_void_p), ("workspace", c_void_p), ("workspace_bytes", c_size_t),
+        ("err_word", c_void_p)]
 
 
 class RaGluSeg(ctypes.Structure):

@@ -254,14 +254,14 @@ def residual_norm_backward_workspace(B, rows, C, device="cuda"):
     return torch.empty(refadapt_residual_norm_backward_workspace_size(B, rows, C), dtype=torch.uint8, device=device)
 
 
-def refadapt_residual_norm_backward(seg, C, post, pre, workspace, eps=1e-6, alpha=1.0, stream=None):
+def refadapt_residual_norm_backward(seg, C, post, pre, workspace, eps=1e-6, alpha=1.0, err_word=None, stream=None):
     """Gradients of refadapt_residual_norm for one segment: a dict with h (the
     forward call's h_out), y, dx and dh_out (gradients of x and h_out, one may
     be absent), the forward call's gate, scale, post_w, pre_w, and the outputs
     wanted: dh, dy ([B, rows, C] bf16), dgate, dscale, dshift ([B, C] fp32),
     dpost_w, dpre_w ([C] fp32)."""
     return check("refadapt_residual_norm_backward", _lib.native().residual_norm_backward(
-        seg, int(C), int(post), int(pre), workspace, float(eps), float(alpha), _handle(stream)))
+        seg, int(C), int(post), int(pre), workspace, float(eps), float(alpha), err_word, _handle(stream)))
 
 
 def refadapt_glu(segs, F, C, act, mode=None, err_word=None, stream=None):

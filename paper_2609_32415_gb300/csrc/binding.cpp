@@ -587,9 +587,9 @@ PyObject* residual_norm(PyObject*, PyObject* const* g, Py_ssize_t n) {
   });
 }
 
-// residual_norm_backward(seg, C, post, pre, workspace, eps, alpha, stream)
+// residual_norm_backward(seg, C, post, pre, workspace, eps, alpha, err_word, stream)
 PyObject* residual_norm_backward(PyObject*, PyObject* const* g, Py_ssize_t n) {
-  return guarded(n, 8, [&] {
+  return guarded(n, 9, [&] {
     const Map sd(g[0]);
     ra_resnorm_grad_args a;
     std::memset(&a, 0, sizeof(a));
@@ -622,7 +622,8 @@ PyObject* residual_norm_backward(PyObject*, PyObject* const* g, Py_ssize_t n) {
     a.workspace = ws.ptr, a.workspace_bytes = ws.bytes;
     a.eps = float(real(g[5]));
     a.alpha = float(real(g[6]));
-    void* st = stream_of(g[7]);
+    a.err_word = static_cast<int32_t*>(address(g[7]));
+    void* st = stream_of(g[8]);
     return released([&] { return refadapt_residual_norm_backward(&a, st); });
   });
 }

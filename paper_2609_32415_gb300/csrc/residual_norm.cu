@@ -12,16 +12,17 @@
 //   dpre_w = sum_s (1 + scale_s) S1_s,  dpost_w = sum_s gate_s S2_s
 //
 // HBM-bound: 8 C bytes a row forward (h, y read, h', x written), 12 C backward.
-// What holds it up is the latency of the reductions between. A row belongs to a
-// group of warps, one or two pieces of eight columns a thread. Forward, a group works
-// on two rows of a sample at once: their reductions share shuffles and barriers, and
-// their instructions fill each other's latencies (backward, the norms' two reductions
-// go together likewise; two rows would spill). A thread copies its own pieces of the
-// rows to come into a ring of its own in shared memory (cp.async: no barrier);
-// what a sample's rows share (gate, scale, shift with the weights; 12 C bytes, more
-// than the row) lies in shared memory, the column sums of the backward pass in
-// registers. A warp reduces the mean and then the squares around it; the warps of a
-// group join theirs (count, mean, squares) through shared memory with one barrier.
+// What holds it up is the latency of the reductions between.
+// Forward, a row belongs to a group of warps, one or two pieces of eight columns a
+// thread, which works on two rows of a sample at once: their reductions share
+// shuffles and barriers, and their instructions fill each other's latencies. A
+// thread copies its own pieces of the rows to come into a ring of its own in shared
+// memory (cp.async: no barrier); what a sample's rows share (gate, scale, shift with
+// the weights; 12 C bytes, more than the row) lies in shared memory. A warp reduces
+// the mean and then the squares around it; the warps of a group join theirs (count,
+// mean, squares) through shared memory with one barrier.
+// Backward, three reductions follow one another, and columns have sums too; so the
+// two directions are split (see residual_norm_grad_kernel).
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -36,7 +37,7 @@ namespace resnorm {
 
 constexpr int MAX_C = 5120;
 constexpr int MAX_PIECES = 2;                        // of a row, a thread's at most
-constexpr int FWD_THREADS = 640, BWD_THREADS = 384;  // of a CTA at most: 96 and 168 registers a thread
+constexpr int FWD_THREADS = 640;                     // of a CTA at most: 96 registers a thread
 constexpr int MAX_STAGES = 4;                        // rows of a group in its ring
 constexpr int SMEM_MAX = 227 * 1024;
 
@@ -69,8 +70,8 @@ struct Params {
 
 struct GradParams {
   int32_t B, C, rows, post, pre;
-  int32_t groups, stages;
-  int32_t parts;  // CTAs that share a sample's rows
+  int32_t parts;                          // CTAs that share a sample's rows
+  int32_t row_warps, groups, group_warps;  // of a CTA: see GradShape
   float eps, alpha;
   const __nv_bfloat16 *h, *y, *dx, *dh_out;
   int64_t h_ss, h_sr, y_ss, y_sr, dx_ss, dx_sr, dho_ss, dho_sr;
@@ -79,6 +80,8 @@ struct GradParams {
   const float *gate, *scale, *post_w, *pre_w;
   int64_t gate_ss, mod_ss;
   float* partial;  // [B][parts][3][C]
+  int32_t* err_word;
+  uint64_t budget_ns;
 };
 
 // ------------------------------------------------------------------ pieces of a row
@@ -197,21 +200,6 @@ struct Exchange {
     else
       named_bar_sync(bar, 32 * T);
   }
-  // Sums of two values over the group.
-  __device__ __forceinline__ float2 sums(int warp, float a, float b) {
-    const float v = warp_sum2(a, b);
-    float* m = entries();
-    if ((threadIdx.x & 30) == 0) m[2 * warp + (threadIdx.x & 1)] = v;
-    meet();
-    const float2* e = reinterpret_cast<const float2*>(m);
-    float2 r = e[0];
-#pragma unroll
-    for (int w = 1; w < T; ++w) {
-      const float2 t = e[w];
-      r.x += t.x, r.y += t.y;
-    }
-    return r;
-  }
 };
 
 template <int V>
@@ -288,21 +276,20 @@ __device__ __forceinline__ float4 join_stats(bool layer, const float4* m, int pi
   return make_float4(-mean0, rsqrtf(fmaf(sq0, inv_c, eps)), -mean1, rsqrtf(fmaf(sq1, inv_c, eps)));
 }
 
-// The statistics of two rows, of kinds k0 and k1 (one at least is a norm).
+// The statistics of two rows.
 template <int V, int T>
-__device__ __forceinline__ float4 row_stats(int k0, int k1, const Place<V, T>& at, Exchange<T>& ex, const Vec (&v0)[V],
-                                            const Vec (&v1)[V], int pieces, float inv_c, float eps) {
+__device__ __forceinline__ float4 row_stats(int kind, const Place<V, T>& at, Exchange<T>& ex, const Vec (&v)[2][V],
+                                            int pieces, float inv_c, float eps) {
   float* m = ex.entries();
   const int lane = threadIdx.x & 31;
-  const bool layer = k0 == RA_NORM_LAYER || k1 == RA_NORM_LAYER;
+  const bool layer = kind == RA_NORM_LAYER;
   float mean = 0.f, sq;  // of the row that the lane's parity says
   if (layer) {
-    mean = warp_sum2(sum_of(v0), sum_of(v1)) * at.inv_n;
-    if (k0 != k1 && (lane & 1 ? k1 : k0) != RA_NORM_LAYER) mean = 0.f;
+    mean = warp_sum2(sum_of(v[0]), sum_of(v[1])) * at.inv_n;
     const float other = __shfl_xor_sync(0xffffffffu, mean, 1);
-    sq = warp_sum2(squares_around(at, v0, lane & 1 ? other : mean), squares_around(at, v1, lane & 1 ? mean : other));
+    sq = warp_sum2(squares_around(at, v[0], lane & 1 ? other : mean), squares_around(at, v[1], lane & 1 ? mean : other));
   } else {
-    sq = warp_sum2(squares_of(v0), squares_of(v1));
+    sq = warp_sum2(squares_of(v[0]), squares_of(v[1]));
   }
   if (lane < 2) *reinterpret_cast<float2*>(m + 4 * at.warp + 2 * lane) = make_float2(mean, sq);
   ex.meet();
@@ -436,7 +423,7 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) residual_norm_kernel(const __g
 #pragma unroll
           for (int j = 0; j < V; ++j) v[k][j] = fetch(k, 0, j);
         float4 st = make_float4(0.f, 1.f, 0.f, 1.f);
-        if (p.post != RA_NORM_NONE) st = row_stats<V, T>(p.post, p.post, at, ex, v[0], v[1], pieces, inv_c, p.eps);
+        if (p.post != RA_NORM_NONE) st = row_stats<V, T>(p.post, at, ex, v, pieces, inv_c, p.eps);
 #pragma unroll
         for (int j = 0; j < V; ++j) {
           if (at.has(j)) {
@@ -464,7 +451,7 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) residual_norm_kernel(const __g
       }
       if (x_dst) {
         float4 st = make_float4(0.f, 1.f, 0.f, 1.f);
-        if (p.pre != RA_NORM_NONE) st = row_stats<V, T>(p.pre, p.pre, at, ex, v[0], v[1], pieces, inv_c, p.eps);
+        if (p.pre != RA_NORM_NONE) st = row_stats<V, T>(p.pre, at, ex, v, pieces, inv_c, p.eps);
 #pragma unroll
         for (int j = 0; j < V; ++j)
           if (at.has(j)) {
@@ -483,165 +470,263 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) residual_norm_kernel(const __g
 }
 
 // ------------------------------------------------------------------ backward
-template <int V, int T>
-__global__ void __launch_bounds__(BWD_THREADS, 1) residual_norm_grad_kernel(const __grid_constant__ GradParams p) {
+// A CTA takes a run of a sample's rows. A row warp has a row at a time: it copies
+// h, y, dx and dh' into its slot in shared memory (the next row starts for L2
+// meanwhile) and reduces what the whole row gives, in two passes over the slot: the
+// means, then everything else (RowSums). Then a group of column warps (eight columns
+// a thread) takes the row from the slot: with the row's eight numbers known, dh, dy
+// and the columns' sums need no further reduction, and S0, S1, S2 stay in the
+// threads' registers. Against groups that hold a row and reduce it across warps (8192
+// rows of 2560: 77 us, waiting on shuffles and barriers in 10 warps), a row's
+// reductions are one warp's, and rows overlap.
+struct GradShape {
+  int row_warps, groups, group_warps;  // warps that reduce rows; groups of column warps
+  int smem;
+  __host__ __device__ static int slot_bytes(int C) { return 4 * C * 2; }
+  __host__ __device__ static int vec_bytes(int C) { return (C + 255) / 256 * 1024; }
+  // [mul, gate] [numbers of a slot] [ready, free of a slot] [sum of gate, abort flag] [slots]
+  __host__ __device__ static int off_numbers(int C) { return 2 * vec_bytes(C); }
+  __host__ __device__ int off_bars(int C) const { return off_numbers(C) + row_warps * 32; }
+  __host__ __device__ int off_slots(int C) const { return off_bars(C) + row_warps * 16 + 16; }
+};
+constexpr int MAX_ROW_WARPS = 10;
+constexpr int GRAD_THREADS = 640, GRAD_THREADS_WIDE = 768;  // of a CTA at most: 96 and 80 registers a thread
+
+// Eight values of a sample's vector in shared memory, piece by piece, halves apart
+// (a warp's 16-byte reads meet no bank conflicts).
+__device__ __forceinline__ void shared_put(uint8_t* base, int piece, const Vec& v) {
+  ulonglong2* m = reinterpret_cast<ulonglong2*>(base) + (piece >> 5) * 64 + (piece & 31);
+  m[0] = make_ulonglong2(v.p[0], v.p[1]);
+  m[32] = make_ulonglong2(v.p[2], v.p[3]);
+}
+__device__ __forceinline__ Vec shared_get(const uint8_t* base, int piece) {
+  const ulonglong2* m = reinterpret_cast<const ulonglong2*>(base) + (piece >> 5) * 64 + (piece & 31);
+  const ulonglong2 a = m[0], b = m[32];
+  return {{a.x, a.y, b.x, b.y}};
+}
+__device__ __forceinline__ void add_up(uint64_t& acc, const Vec& v) {
+  acc = f2_add(acc, f2_add(f2_add(v.p[0], v.p[1]), f2_add(v.p[2], v.p[3])));
+}
+__device__ __forceinline__ void dot_up(uint64_t& acc, const Vec& a, const Vec& b) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) acc = f2_fma(a.p[i], b.p[i], acc);
+}
+// Two sums over the warp, in every lane.
+__device__ __forceinline__ float2 warp_sums(uint64_t a, uint64_t b) {
+  const float v = warp_sum2(sum2(a), sum2(b)), w = __shfl_xor_sync(0xffffffffu, v, 1);
+  return threadIdx.x & 1 ? make_float2(w, v) : make_float2(v, w);
+}
+
+// What a row's columns need of it: -mean and 1 / deviation of h and y, and the
+// negated means that the norms' gradients take off.
+struct alignas(16) RowNumbers {
+  float h_mean, h_r, e0, e1, y_mean, y_r, f0, f1;
+};
+
+template <int THREADS>
+__global__ void __launch_bounds__(THREADS, 1) residual_norm_grad_kernel(const __grid_constant__ GradParams p) {
   extern __shared__ __align__(16) uint8_t smem[];
-  // mul, gate of the sample; the exchange; ring[stage][piece of h, y, dx, dh_out][thread of the CTA]
-  using Shared = SharedVec<V, T>;
-  const Shared mul{reinterpret_cast<ulonglong2*>(smem)}, gate{reinterpret_cast<ulonglong2*>(smem + Shared::BYTES)};
-  const Place<V, T> at(p.C);
-  Exchange<T> ex(smem + 2 * Shared::BYTES, at.group);
-  const uint32_t piece_bytes = 16 * blockDim.x, stage_bytes = 4 * V * piece_bytes;
-  uint8_t* const ring = smem + 2 * Shared::BYTES + p.groups * Exchange<T>::BYTES + 16 * threadIdx.x;
-  const float inv_c = 1.f / float(p.C);
-  const int pieces = p.C >> 3, S = p.stages;
+  const GradShape shape{p.row_warps, p.groups, p.group_warps, 0};
+  const int C = p.C, pieces = C >> 3, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, WR = p.row_warps;
+  uint8_t *const mul_sh = smem, *const gate_sh = smem + GradShape::vec_bytes(C);
+  RowNumbers* numbers = reinterpret_cast<RowNumbers*>(smem + GradShape::off_numbers(C));
+  uint64_t* ready = reinterpret_cast<uint64_t*>(smem + shape.off_bars(C));
+  uint64_t* free_ = ready + WR;
+  volatile float* gate_sum = reinterpret_cast<volatile float*>(free_ + WR);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(free_ + WR) + 1;
+  uint8_t* const slots = smem + shape.off_slots(C);
+  const int row_bytes = 2 * C, slot_bytes = GradShape::slot_bytes(C);
   pdl_launch();
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < WR; ++i) {
+      mbar_init(ready + i, 1);
+      mbar_init(free_ + i, p.group_warps);
+    }
+    *abort_flag = 0;
+    fence_mbar_init();
+  }
   pdl_wait();
   const int s = int(blockIdx.x) / p.parts, part = int(blockIdx.x) - s * p.parts;
-  const int lo = int(int64_t(p.rows) * part / p.parts), hi = int(int64_t(p.rows) * (part + 1) / p.parts);
-  const int first = lo + at.group;
-  // this thread's first piece of the group's next row of h, y, dx and dh_out
-  auto start = [&](const __nv_bfloat16* t, int64_t ss, int64_t sr) {
-    return t ? t + s * ss + first * sr + at.col(0) : nullptr;
+  const int lo = int(int64_t(p.rows) * part / p.parts), n = int(int64_t(p.rows) * (part + 1) / p.parts) - lo;
+  const bool has_y = p.y != nullptr;
+  // Tensor q of a row; one that was not given is zeros in every slot.
+  auto row_of = [&](int q, int r) -> const __nv_bfloat16* {
+    const __nv_bfloat16* t = q == 0 ? p.h : q == 1 ? p.y : q == 2 ? p.dx : p.dh_out;
+    const int64_t ss = q == 0 ? p.h_ss : q == 1 ? p.y_ss : q == 2 ? p.dx_ss : p.dho_ss;
+    const int64_t sr = q == 0 ? p.h_sr : q == 1 ? p.y_sr : q == 2 ? p.dx_sr : p.dho_sr;
+    return t ? t + s * ss + int64_t(lo + r) * sr : nullptr;
   };
-  const __nv_bfloat16 *h = start(p.h, p.h_ss, p.h_sr), *y = start(p.y, p.y_ss, p.y_sr),
-                      *dx = start(p.dx, p.dx_ss, p.dx_sr), *dho = start(p.dh_out, p.dho_ss, p.dho_sr);
-  const bool has_y = y != nullptr, has_dx = dx != nullptr, has_dho = dho != nullptr;
-  int ld_i = first;
-  auto load = [&](uint32_t off) {
-    if (ld_i < hi) {
+  auto load = [&](int r) {  // a lane copies the pieces that it reads
+    uint8_t* to = slots + warp * slot_bytes + 16 * lane;
 #pragma unroll
-      for (int j = 0; j < V; ++j)
-        if (at.has(j)) {
-          uint8_t* to = ring + off + j * piece_bytes;
-          cp_async16(to, h + 256 * T * j);
-          if (has_y) cp_async16(to + V * piece_bytes, y + 256 * T * j);
-          if (has_dx) cp_async16(to + 2 * V * piece_bytes, dx + 256 * T * j);
-          if (has_dho) cp_async16(to + 3 * V * piece_bytes, dho + 256 * T * j);
-        }
-      h += p.groups * p.h_sr;
-      if (has_y) y += p.groups * p.y_sr;
-      if (has_dx) dx += p.groups * p.dx_sr;
-      if (has_dho) dho += p.groups * p.dho_sr;
+    for (int q = 0; q < 4; ++q, to += row_bytes) {
+      const __nv_bfloat16* src = row_of(q, r);
+      if (!src) continue;
+      for (int i = lane, o = 0; i < pieces; i += 32, o += 512) cp_async16(to + o, src + 8 * lane + (o >> 1));
     }
-    ld_i += p.groups;
     cp_async_commit();
   };
-  for (int k = 0; k < S - 1; ++k) load(k * stage_bytes);
-  if (at.group == 0) {
-#pragma unroll
-    for (int j = 0; j < V; ++j) {
-      if (!at.has(j)) continue;
-      const int c = at.col(j);
-      mul.put(j, at.lane_g,
-              (vec8(p.scale ? p.scale + s * p.mod_ss : nullptr, c, 0.f) + all(1.f)) * vec8(p.pre_w, c, 1.f));
-      gate.put(j, at.lane_g, vec8(p.gate ? p.gate + s * p.gate_ss : nullptr, c, 1.f) * vec8(p.post_w, c, 1.f));
-    }
+  if (warp < WR) {
+    if (warp < n) load(warp);
+    for (int q = 1; q < 4; ++q)
+      if (!row_of(q, 0))
+        for (int i = lane; i < pieces; i += 32)
+          *reinterpret_cast<uint4*>(slots + warp * slot_bytes + q * row_bytes + 16 * i) = make_uint4(0, 0, 0, 0);
+  }
+  for (int i = threadIdx.x; i < pieces; i += blockDim.x) {
+    const int c = 8 * i;
+    shared_put(mul_sh, i, (vec8(p.scale ? p.scale + s * p.mod_ss : nullptr, c, 0.f) + all(1.f)) * vec8(p.pre_w, c, 1.f));
+    shared_put(gate_sh, i, vec8(p.gate ? p.gate + s * p.gate_ss : nullptr, c, 1.f) * vec8(p.post_w, c, 1.f));
   }
   __syncthreads();
-  Vec s0[V], s1[V], s2[V];  // column sums of the group's rows
-#pragma unroll
-  for (int j = 0; j < V; ++j) s0[j] = s1[j] = s2[j] = all(0.f);
-  auto place = [&](__nv_bfloat16* t, int64_t ss, int64_t sr) {
-    return t ? t + s * ss + first * sr + at.col(0) : nullptr;
-  };
-  __nv_bfloat16 *dh = place(p.dh, p.dh_ss, p.dh_sr), *dy = place(p.dy, p.dy_ss, p.dy_sr);
-  uint32_t off = 0, ld_off = (S - 1) * stage_bytes;
-  for (int i = first; i < hi; i += p.groups) {
-    load(ld_off);
-    ld_off = off;
-    cp_async_wait_upto(S - 1);
-    auto fetch = [&](bool given, int q, int j) {
-      return widen(given && at.has(j) ? *reinterpret_cast<const uint4*>(ring + off + (q * V + j) * piece_bytes)
-                                      : make_uint4(0, 0, 0, 0));
-    };
-    Vec a[V], b[V];  // x^, then dH and what follows from it; y^
-#pragma unroll
-    for (int j = 0; j < V; ++j) a[j] = fetch(true, 0, j), b[j] = fetch(has_y, 1, j);
-    float2 sa = make_float2(0.f, 1.f), sb = sa;
-    if (p.pre != RA_NORM_NONE || p.post != RA_NORM_NONE) {
-      const float4 st = row_stats<V, T>(p.pre, p.post, at, ex, a, b, pieces, inv_c, p.eps);
-      if (p.pre != RA_NORM_NONE) sa = make_float2(st.x, st.y);
-      if (p.post != RA_NORM_NONE) sb = make_float2(st.z, st.w);
-    }
-    // the norm before the next branch
-    uint64_t e0 = both(0.f), e1 = e0;
-#pragma unroll
-    for (int j = 0; j < V; ++j) {
-      if (!at.has(j)) continue;
-      a[j] = (a[j] + all(sa.x)) * all(sa.y);
-      const Vec d = fetch(has_dx, 2, j), e = d * mul.get(j, at.lane_g);
-      s0[j] = s0[j] + d;
-      s1[j] = fma(d, a[j], s1[j]);
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        e0 = f2_add(e0, e.p[k]);
-        e1 = f2_fma(e.p[k], a[j].p[k], e1);
+  const uint64_t zero = both(0.f);
+  if (warp == 0) {
+    uint64_t g = zero;
+    for (int i = lane; i < pieces; i += 32) add_up(g, shared_get(gate_sh, i));
+    const float2 sum = warp_sums(g, zero);
+    if (lane == 0) *gate_sum = sum.x;
+  }
+  __syncthreads();
+  const WaitCtl ctl{abort_flag, p.err_word, p.budget_ns};
+  const float inv_c = 1.f / float(C);
+  Vec s0 = all(0.f), s1 = s0, s2 = s0;  // of a column thread
+  const int group = warp < WR ? -1 : (warp - WR) / p.group_warps;
+  const int piece = 32 * ((warp - WR) - group * p.group_warps) + lane;  // of a column thread
+  if (warp < WR) {
+    // ---------------------------------------------------------------- rows
+    const uint8_t* const slot = slots + warp * slot_bytes + 16 * lane;
+    const bool layer = p.pre == RA_NORM_LAYER || p.post == RA_NORM_LAYER, deep = p.post != RA_NORM_NONE && p.dy;
+    const int mine = (pieces - lane + 31) / 32;  // pieces of this lane
+    auto get = [](const uint8_t* at) { return widen(*reinterpret_cast<const uint4*>(at)); };
+    for (int k = 0, r = warp; r < n; ++k, r += WR) {
+      if (r + WR < n && lane < 4) {
+        const __nv_bfloat16* next = row_of(lane, r + WR);
+        if (next) prefetch_bulk_l2(next, uint32_t(row_bytes));
       }
-    }
-    float2 m = make_float2(0.f, 0.f);
-    if (p.pre != RA_NORM_NONE && has_dx) {
-      m = ex.sums(at.warp, sum2(e0), sum2(e1));
-      m.x = p.pre == RA_NORM_LAYER ? -m.x * inv_c : 0.f;
-      m.y *= -inv_c;
-    }
-    e0 = e1 = both(0.f);
-#pragma unroll
-    for (int j = 0; j < V; ++j) {
-      if (!at.has(j)) continue;
-      // dH = dh' + r (e - m(e) - x^ m(e x^))
-      const Vec e = fma(a[j], all(m.y), fma(fetch(has_dx, 2, j), mul.get(j, at.lane_g), all(m.x)));
-      a[j] = fma(e, all(sa.y), fetch(has_dho, 3, j));
-      b[j] = (b[j] + all(sb.x)) * all(sb.y);
-      if (dh) *reinterpret_cast<uint4*>(dh + 256 * T * j) = narrow(a[j] * all(p.alpha));
-      s2[j] = fma(a[j], b[j], s2[j]);
-      a[j] = a[j] * gate.get(j, at.lane_g);
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        e0 = f2_add(e0, a[j].p[k]);
-        e1 = f2_fma(a[j].p[k], b[j].p[k], e1);
+      cp_async_wait<0>();
+      float hm = 0.f, ym = 0.f;
+      if (layer) {
+        uint64_t a = zero, b = zero;
+        const uint8_t* at = slot;
+#pragma unroll 4
+        for (int i = 0; i < mine; ++i, at += 512) {
+          add_up(a, get(at));
+          add_up(b, get(at + row_bytes));
+        }
+        const float2 m = warp_sums(a, b);
+        if (p.pre == RA_NORM_LAYER) hm = m.x * inv_c;
+        if (p.post == RA_NORM_LAYER) ym = m.y * inv_c;
       }
-    }
-    if (dh) dh += p.groups * p.dh_sr;
-    // the norm after the branch
-    if (dy) {
-      m = make_float2(0.f, 0.f);
+      // With h and y less their means, e = dx mul, g = gate: the squares, sum e, e h;
+      // and what sum f and f y come from, f = g dH, dH = dh' + r (e - m(e) - x^ m(e x^)).
+      uint64_t hh = zero, yy = zero, e0 = zero, eh = zero, dg = zero, eg = zero, hg = zero, dgy = zero, egy = zero,
+               hgy = zero, gy = zero;
+      const Vec neg_h = all(-hm), neg_y = all(-ym);
+      const uint8_t *at = slot, *mul_at = mul_sh + 16 * lane, *gate_at = gate_sh + 16 * lane;
+      auto vec = [](const uint8_t* m) -> Vec {
+        const ulonglong2 a = *reinterpret_cast<const ulonglong2*>(m), b = *reinterpret_cast<const ulonglong2*>(m + 512);
+        return {{a.x, a.y, b.x, b.y}};
+      };
+#pragma unroll 2
+      for (int i = 0; i < mine; ++i, at += 512, mul_at += 1024, gate_at += 1024) {
+        const Vec h = get(at) + neg_h, y = get(at + row_bytes) + neg_y, e = get(at + 2 * row_bytes) * vec(mul_at);
+        dot_up(hh, h, h);
+        dot_up(yy, y, y);
+        add_up(e0, e);
+        dot_up(eh, e, h);
+        if (deep) {
+          const Vec g = vec(gate_at), d = get(at + 3 * row_bytes), w = g * y;
+          dot_up(dg, d, g);
+          dot_up(eg, e, g);
+          dot_up(hg, h, g);
+          dot_up(dgy, d, w);
+          dot_up(egy, e, w);
+          dot_up(hgy, h, w);
+          add_up(gy, w);
+        }
+      }
+      const float2 sq = warp_sums(hh, yy), es = warp_sums(e0, eh);
+      RowNumbers v = {0.f, 1.f, 0.f, 0.f, 0.f, 1.f, 0.f, 0.f};
+      if (p.pre != RA_NORM_NONE) {
+        v.h_mean = -hm, v.h_r = rsqrtf(fmaf(sq.x, inv_c, p.eps));
+        if (p.pre == RA_NORM_LAYER) v.e0 = -es.x * inv_c;
+        v.e1 = -es.y * v.h_r * inv_c;
+      }
       if (p.post != RA_NORM_NONE) {
-        m = ex.sums(at.warp, sum2(e0), sum2(e1));
-        m.x = p.post == RA_NORM_LAYER ? -m.x * inv_c : 0.f;
-        m.y *= -inv_c;
+        v.y_mean = -ym, v.y_r = rsqrtf(fmaf(sq.y, inv_c, p.eps));
+        if (deep) {
+          const float2 d = warp_sums(dg, dgy), e = warp_sums(eg, egy), h = warp_sums(hg, hgy), g = warp_sums(gy, zero);
+          const float f0 = fmaf(v.h_r, fmaf(v.h_r * v.e1, h.x, fmaf(v.e0, *gate_sum, e.x)), d.x);
+          const float f1 = fmaf(v.h_r, fmaf(v.h_r * v.e1, h.y, fmaf(v.e0, g.x, e.y)), d.y);
+          if (p.post == RA_NORM_LAYER) v.f0 = -f0 * inv_c;
+          v.f1 = -f1 * v.y_r * inv_c;
+        }
       }
-#pragma unroll
-      for (int j = 0; j < V; ++j)
-        if (at.has(j))
-          *reinterpret_cast<uint4*>(dy + 256 * T * j) = narrow(fma(b[j], all(m.y), a[j] + all(m.x)) * all(sb.y));
-      dy += p.groups * p.dy_sr;
+      if (lane == 0) numbers[warp] = v;
+      __syncwarp();
+      if (lane == 0) mbar_arrive(ready + warp);
+      if (r + WR < n) {
+        if (!__all_sync(0xffffffffu, mbar_wait(free_ + warp, uint32_t(k & 1), ctl))) break;
+        load(r + WR);
+      }
     }
-    off += stage_bytes;
-    if (off == S * stage_bytes) off = 0;
+    cp_async_wait<0>();
+  } else if (group < p.groups) {
+    // ---------------------------------------------------------------- columns
+    const bool in = piece < pieces;
+    const Vec mul = in ? shared_get(mul_sh, piece) : all(0.f), gate = in ? shared_get(gate_sh, piece) : all(0.f);
+    auto place = [&](__nv_bfloat16* t, int64_t ss, int64_t sr) {
+      return t ? t + s * ss + (lo + group) * sr + 8 * piece : nullptr;
+    };
+    __nv_bfloat16 *dh = place(p.dh, p.dh_ss, p.dh_sr), *dy = place(p.dy, p.dy_ss, p.dy_sr);
+    int w = 0, k = 0;  // row r is the k-th of row warp w
+    for (w = group; w >= WR; w -= WR) ++k;
+    for (int r = group; r < n; r += p.groups) {
+      if (!__all_sync(0xffffffffu, mbar_wait(ready + w, uint32_t(k & 1), ctl))) break;
+      if (in) {
+        const RowNumbers v = numbers[w];
+        const uint8_t* at = slots + w * slot_bytes + 16 * piece;
+        auto get = [&](int q) { return widen(*reinterpret_cast<const uint4*>(at + q * row_bytes)); };
+        const Vec x = (get(0) + all(v.h_mean)) * all(v.h_r), d = get(2);
+        s0 = s0 + d;
+        s1 = fma(d, x, s1);
+        // dH = dh' + r (e - m(e) - x^ m(e x^))
+        const Vec e = fma(d, mul, fma(x, all(v.e1), all(v.e0)));
+        const Vec t = fma(e, all(v.h_r), get(3));
+        if (dh) *reinterpret_cast<uint4*>(dh) = narrow(t * all(p.alpha));
+        if (has_y) {
+          const Vec y = (get(1) + all(v.y_mean)) * all(v.y_r);
+          s2 = fma(t, y, s2);
+          if (dy) *reinterpret_cast<uint4*>(dy) = narrow(fma(y, all(v.f1), fma(t, gate, all(v.f0))) * all(v.y_r));
+        }
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(free_ + w);
+      if (dh) dh += p.groups * p.dh_sr;
+      if (dy) dy += p.groups * p.dy_sr;
+      for (w += p.groups; w >= WR; w -= WR) ++k;
+    }
   }
   // The CTA's column sums: its groups' in order, through shared memory.
-  cp_async_wait<0>();
   __syncthreads();
-  float* sums = reinterpret_cast<float*>(smem);  // [group][3][C]
-#pragma unroll
-  for (int j = 0; j < V; ++j) {
-    if (!at.has(j)) continue;
-    float* to = sums + at.group * 3 * p.C + at.col(j);
+  const bool gave_up = *abort_flag;
+  float* sums = reinterpret_cast<float*>(slots);  // [group][3][C]
+  if (group >= 0 && group < p.groups && piece < pieces) {
+    float* to = sums + group * 3 * C + 8 * piece;
     auto put = [](float* dst, const Vec& v) {
       reinterpret_cast<ulonglong2*>(dst)[0] = make_ulonglong2(v.p[0], v.p[1]);
       reinterpret_cast<ulonglong2*>(dst)[1] = make_ulonglong2(v.p[2], v.p[3]);
     };
-    put(to, s0[j]);
-    put(to + p.C, s1[j]);
-    put(to + 2 * p.C, s2[j]);
+    put(to, s0);
+    put(to + C, s1);
+    put(to + 2 * C, s2);
   }
   __syncthreads();
-  float* out = p.partial + int64_t(blockIdx.x) * 3 * p.C;
-  for (int c = threadIdx.x; c < 3 * p.C; c += blockDim.x) {
+  float* out = p.partial + int64_t(blockIdx.x) * 3 * C;
+  for (int c = threadIdx.x; c < 3 * C; c += blockDim.x) {
     float v = 0.f;
-    for (int g = 0; g < p.groups; ++g) v += sums[g * 3 * p.C + c];
-    out[c] = v;
+    for (int g = 0; g < p.groups; ++g) v += sums[g * 3 * C + c];
+    out[c] = gave_up ? __int_as_float(0x7fffffff) : v;
   }
 }
 
@@ -767,15 +852,23 @@ Shape make_shape(int C, int max_threads, int vectors, int stage_rows) {
   return s;
 }
 Shape fwd_shape(int C) { return make_shape(C, FWD_THREADS, 3, 4); }
-Shape bwd_shape(int C) {
-  Shape s = make_shape(C, BWD_THREADS, 2, 4);
-  const int sums = s.groups * 3 * C * 4;  // the column sums take the same memory at the end
+// As many row warps as there is room for slots, at most ten; column groups of about
+// ten warps together.
+GradShape grad_shape(int C) {
+  GradShape s;
+  s.group_warps = (C + 255) / 256;
+  s.groups = s.group_warps >= 10 ? 1 : 10 / s.group_warps;
+  for (s.row_warps = MAX_ROW_WARPS;; --s.row_warps) {
+    s.smem = s.off_slots(C) + s.row_warps * GradShape::slot_bytes(C);
+    if (s.smem <= SMEM_MAX) break;  // four fit at C = 5120
+  }
+  const int sums = s.off_slots(C) + s.groups * 3 * C * 4;
   if (s.smem < sums) s.smem = sums;
   return s;
 }
+static_assert(2 * 20 * 1024 + 4 * MAX_C * 2 * 4 + 1024 <= SMEM_MAX, "four row warps fit");
 static_assert(MAX_C <= 10 * 512 && MAX_PIECES == 2, "a group has at most ten warps");
 using Fwd = void (*)(Params);
-using Bwd = void (*)(GradParams);
 Fwd pick_fwd(const Shape& s) {
   if (s.V == 1) return residual_norm_kernel<1, 1>;
   switch (s.warps) {
@@ -786,17 +879,6 @@ Fwd pick_fwd(const Shape& s) {
     default: return nullptr;
   }
 }
-Bwd pick_bwd(const Shape& s) {
-  if (s.V == 1) return residual_norm_grad_kernel<1, 1>;
-  switch (s.warps) {
-#define RA_CASE(T) \
-  case T: return residual_norm_grad_kernel<2, T>;
-    RA_CASE(1) RA_CASE(2) RA_CASE(3) RA_CASE(4) RA_CASE(5) RA_CASE(6) RA_CASE(7) RA_CASE(8) RA_CASE(9) RA_CASE(10)
-#undef RA_CASE
-    default: return nullptr;
-  }
-}
-
 // CTAs that share a sample's rows: as many as make the fewest rounds of rows.
 int grad_parts(int B, int rows, int sms) {
   int best = 1;
@@ -975,12 +1057,16 @@ extern "C" ra_status refadapt_residual_norm_backward(const ra_resnorm_grad_args*
   p.post_w = a->post_w, p.pre_w = a->pre_w;
   p.partial = static_cast<float*>(a->workspace);
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
-  const Shape sh = bwd_shape(a->C);
-  p.groups = sh.groups;
-  p.stages = sh.stages;
+  const GradShape sh = grad_shape(a->C);
+  p.row_warps = sh.row_warps, p.groups = sh.groups, p.group_warps = sh.group_warps;
+  p.err_word = a->err_word;
+  p.budget_ns = wait_budget_ns();
   p.parts = a->rows > 0 ? grad_parts(a->B, a->rows, num_sms()) : 0;
   if (a->rows > 0) {
-    const ra_status r = launch(who, pick_bwd(sh), p, dim3(unsigned(a->B * p.parts)), sh.threads(), sh.smem, st);
+    const int threads = 32 * (sh.row_warps + sh.groups * sh.group_warps);
+    const ra_status r = launch(who, threads <= GRAD_THREADS ? residual_norm_grad_kernel<GRAD_THREADS>
+                                                            : residual_norm_grad_kernel<GRAD_THREADS_WIDE>,
+                               p, dim3(unsigned(a->B * p.parts)), threads, sh.smem, st);
     if (r != RA_OK) return r;
   }
   if (!a->dpre_w && !a->dpost_w && !a->dgate && !a->dscale && !a->dshift) return RA_OK;
