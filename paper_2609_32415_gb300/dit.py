@@ -47,13 +47,13 @@ CUES = {"product": 0, "change": 1, "exposure": 2}
 class DiTExecutor:
     def __init__(self, n_blocks, B, H, d, n_text, n_ref, n_tgt, theta, delta_max, eps=1e-6, mlp_ratio=4,
                  forced_boundary=-1, mass_rows=0, ln_eps=1e-6, norm_eps=1e-6, rope_base=10000.0, log_steps=8,
-                 cue="product", device="cuda"):
+                 cue="product", device="cuda", mlp_width=None):
         if cue not in CUES:
             raise ValueError("unknown cue %r" % (cue,))
         dev = torch.device(device)
         self.n_blocks, self.B, self.H, self.d = n_blocks, B, H, d
         self.C = C = H * d
-        self.F = F = mlp_ratio * C
+        self.F = F = mlp_ratio * C if mlp_width is None else int(mlp_width)
         self.n = {"text": n_text, "ref": n_ref, "tgt": n_tgt}
         self.theta, self.delta_max, self.eps = float(theta), int(delta_max), float(eps)
         self.forced_boundary, self.mass_rows, self.cue = int(forced_boundary), int(mass_rows), cue
@@ -107,16 +107,14 @@ class DiTExecutor:
         stream -> six [B, C] fp32 vectors; W: dict stream -> weights."""
         li = (t % self.log_steps) if log_index is None else log_index
         mode = self.modes[li, b]
-        n, C, F = self.n, self.C, self.F
+        C = self.C
         cur = self.q_tgt[t % 2, b]
         prev = self.q_tgt[(t + 1) % 2, b]
         ms = {r: mods[STREAM_OF[r]] for r in ROLES}
         Ws = {r: W[STREAM_OF[r]] for r in ROLES}
         hin = {"text": h_in["text"], "ref": self.hbar[b], "tgt": h_in["tgt"]}
         # 1. text and target rows: modulated LN, QKV (post-RoPE Q of the target kept for D)
-        api.refadapt_ln_modulate(
-            [{"h": hin[r], "x": self.x[r], "shift": ms[r]["shift_a"], "scale": ms[r]["scale_a"]}
-             for r in ("text", "tgt")], C, self.ln_eps, stream=stream)
+        self._branch_input(("text", "tgt"), hin, ms, Ws, None, stream)
         q_out = {"text": self.qkv["text"][0], "tgt": cur}
         self._gemm("qkv", t, b, [
             {"a": self.x[r], "w": Ws[r]["w_qkv"], "bias": Ws[r]["b_qkv"], "q": q_out[r], "k": self.qkv[r][1],
@@ -134,9 +132,7 @@ class DiTExecutor:
                               mass_row_count=self.mass_row_count, forced_boundary=self.forced_boundary,
                               gbar_out=self.gbar[li, b], m_out=self.M[li, b], cue=CUES[self.cue], stream=stream)
         # 3. reference rows (gated on the mode): LN of H_b, QKV into the cache slot
-        api.refadapt_ln_modulate(
-            [{"h": hin["ref"], "x": self.x["ref"], "shift": ms["ref"]["shift_a"], "scale": ms["ref"]["scale_a"],
-              "gated": True}], C, self.ln_eps, mode=mode, stream=stream)
+        self._branch_input(("ref",), hin, ms, Ws, mode, stream)
         self._gemm("qkv_ref", t, b, [
             {"a": self.x["ref"], "w": Ws["ref"]["w_qkv"], "bias": Ws["ref"]["b_qkv"], "q": self.q_ref,
              "k": self.cache_k[b], "v": self.cache_v[b], "q_norm": Ws["ref"]["q_norm"],
@@ -158,6 +154,17 @@ class DiTExecutor:
             ref_fresh=(self.q_ref, self.cache_k[b], self.cache_v[b]), a_b=self.a_b[b], step=t, stream=stream)
         if self.attn_hook is not None:
             self.attn_hook("post", t, b)
+        self._finish_block(t, b, hin, ms, Ws, mode, stream)
+
+    def _branch_input(self, roles, hin, ms, Ws, mode, stream):
+        """x of the attention branch for these roles' rows (reference rows gated on the mode)."""
+        api.refadapt_ln_modulate(
+            [{"h": hin[r], "x": self.x[r], "shift": ms[r]["shift_a"], "scale": ms[r]["scale_a"], "gated": r == "ref"}
+             for r in roles], self.C, self.ln_eps, mode=mode, stream=stream)
+
+    def _finish_block(self, t, b, hin, ms, Ws, mode, stream):
+        """The block after its attention: o, the residual streams -> the next block's inputs."""
+        C, F = self.C, self.F
         # 5. output projection with the gated residual (reference: H_b -> h1_ref)
         self._gemm("o_proj", t, b, [
             {"a": self.o[r], "w": Ws[r]["w_o"], "bias": Ws[r]["b_o"], "resid": hin[r], "gate": ms[r]["gate_a"],
