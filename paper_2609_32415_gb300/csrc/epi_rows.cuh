@@ -61,4 +61,22 @@ __device__ __forceinline__ void rows_store(uint8_t* stage, const float (&x)[32],
   rows_put(stage, own, dst, stride, nrow, ncol);
 }
 
+// The same for rows of 64 columns (128 bytes): whole lines of four rows per
+// instruction, a staging buffer of 4 KB; ncol of the 64 columns exist.
+__device__ __forceinline__ void rows_put128(uint8_t* stage, const uint4 (&own)[8], char* dst, int64_t stride, int nrow,
+                                            int ncol) {
+  const int lane = threadIdx.x & 31, r0 = lane >> 3;
+  auto slot = [&](int r, int q) { return reinterpret_cast<uint4*>(stage + r * 128 + ((q ^ (r & 7)) << 4)); };
+#pragma unroll
+  for (int q = 0; q < 8; ++q) *slot(lane, q) = own[q];
+  __syncwarp();
+  char* ptr = dst + r0 * stride + (lane & 7) * 16;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const uint4 v = *slot(r0 + 4 * i, lane & 7);
+    if (r0 + 4 * i < nrow && 8 * (lane & 7) < ncol) *reinterpret_cast<uint4*>(ptr + 4 * i * stride) = v;
+  }
+  __syncwarp();
+}
+
 }  // namespace ra

@@ -54,7 +54,7 @@ constexpr int OFF_BAR = STAGES * STAGE_BYTES;
 constexpr int NUM_BARS = 2 * STAGES + 2 + 2 + 1;  // full, empty, tfull[2], tempty[2], drain
 constexpr int OFF_MISC = OFF_BAR + NUM_BARS * 8;
 constexpr int EPI_WARPS = 8;
-constexpr int EPI_BYTES = 32 * 64;  // staging of a warp
+constexpr int EPI_BYTES = 32 * 128;  // staging of a warp: 32 rows of 64 columns
 constexpr int OFF_EPI = (OFF_MISC + 16 + 127) / 128 * 128;
 constexpr int SMEM_ALLOC = OFF_EPI + EPI_WARPS * EPI_BYTES + 1024;
 constexpr int THREADS = 64 + 32 * EPI_WARPS;
@@ -70,6 +70,14 @@ struct Rows {
   int64_t ss, sr;
 };
 
+// Division by a number that the host knows: n / d = high word of n * ceil(2^32 / d)
+// for n d < 2^32, what a launch's units stay below. The roles' threads divide a few
+// times per tile; with plain divisions a tile of one or two stages took 1.5 us.
+struct Div {
+  uint32_t d, mul;  // mul 0: d is 1
+  __device__ __forceinline__ uint32_t operator()(uint32_t n) const { return mul ? __umulhi(n, mul) : n; }
+};
+
 struct Job {
   int32_t samples, rows, gated;  // output rows per sample
   int32_t m_tiles, cols;         // row and column tiles of a sample
@@ -78,6 +86,7 @@ struct Job {
   // operand pair; a weight's gradient: one per sample (K runs along the rows).
   int32_t spans, span_k, span_stages;
   int32_t parts;                 // of K, whole stages each
+  Div by_band, by_parts;         // tiles of a band of GROUP_M tile rows; parts
   int32_t rows_k;                // K runs along the rows of both operands
   Rows out[3];                   // GLU: out, pre_gate, pre_up; GRAD: dg, dw; STORE: the result
   Rows pre_gate, pre_up;         // GRAD
@@ -89,12 +98,39 @@ struct Job {
 // others then wait `early` rounds of the remaining units, which the others share.
 struct Schedule {
   int32_t longs, early;
-  __device__ __forceinline__ int64_t unit(int c, int pairs, int i) const {
-    const int rest = longs % pairs, mine = longs / pairs + (c < rest ? 1 : 0);
-    if (i < mine) return c + int64_t(i) * pairs;
-    const int ahead = c < rest ? 0 : early, j = i - mine;
-    if (j < ahead) return longs + (c - rest) + int64_t(j) * (pairs - rest);
-    return longs + int64_t(early) * (pairs - rest) + c + int64_t(j - ahead) * pairs;
+};
+struct Turn {  // the units of pair c, one after the other
+  int c, pairs, rest, ahead;
+  int64_t t, base;  // the next unit; the first that all pairs share
+  bool longs;
+  __device__ __forceinline__ Turn(const Schedule& s, int c_, int pairs_) : c(c_), pairs(pairs_) {
+    rest = s.longs % pairs;
+    ahead = c < rest ? 0 : s.early;
+    base = s.longs + int64_t(s.early) * (pairs - rest);
+    t = c;
+    longs = true;
+    settle(s);
+  }
+  __device__ __forceinline__ void next(const Schedule& s) {
+    if (longs) {
+      t += pairs;
+      settle(s);
+    } else if (ahead > 1) {
+      --ahead;
+      t += pairs - rest;
+    } else if (ahead == 1) {
+      ahead = 0;
+      t = base + c;
+    } else {
+      t += pairs;
+    }
+  }
+
+ private:
+  __device__ __forceinline__ void settle(const Schedule& s) {  // past the long units?
+    if (t < s.longs) return;
+    longs = false;
+    t = ahead > 0 ? s.longs + (c - rest) : base + c;
   }
 };
 
@@ -137,19 +173,22 @@ struct Walk {
       n = units(p);
     }
     const Job& job = p.job[j];
-    const uint32_t idx = uint32_t(t - begin), tile = idx / uint32_t(job.parts);
-    const uint32_t band_tiles = uint32_t(GROUP_M) * uint32_t(job.cols);
-    const uint32_t band = tile / band_tiles, in_band = tile - band * band_tiles;
+    const uint32_t idx = uint32_t(t - begin), tile = job.by_parts(idx), band = job.by_band(tile);
+    const uint32_t in_band = tile - band * job.by_band.d;
     const int m_first = int(band) * GROUP_M;
     const uint32_t rows = uint32_t(min(GROUP_M, job.m_tiles - m_first));
+    const uint32_t col = rows == GROUP_M ? in_band / GROUP_M : in_band / rows;
     u.job = j;
     u.s = s;
-    u.m0 = (m_first + int(in_band % rows)) * TM;
-    u.n0 = int(in_band / rows) * (KIND == GLU ? p.bn / 2 : p.bn);
-    u.part = int(idx - tile * uint32_t(job.parts));
-    const int64_t stages = int64_t(job.spans) * job.span_stages;
-    u.k0 = int(stages * u.part / job.parts);
-    u.k1 = int(stages * (u.part + 1) / job.parts);
+    u.m0 = (m_first + int(in_band - col * rows)) * TM;
+    u.n0 = int(col) * (KIND == GLU ? p.bn / 2 : p.bn);
+    u.part = int(idx - tile * job.by_parts.d);
+    const int stages = job.spans * job.span_stages;
+    u.k0 = 0, u.k1 = stages;
+    if (job.parts > 1) {
+      u.k0 = int(int64_t(stages) * u.part / job.parts);
+      u.k1 = int(int64_t(stages) * (u.part + 1) / job.parts);
+    }
     return true;
   }
 };
@@ -205,35 +244,56 @@ __device__ __forceinline__ char* row_ptr(const Rows& r, int s, int row, int col)
   return reinterpret_cast<char*>(r.ptr + s * r.ss + row * r.sr + col);
 }
 
+// 64 accumulator columns (the last `cols` - 32 of which may be missing) -> bf16.
+__device__ __forceinline__ void pack64(uint32_t acc, int cols, uint4 (&own)[8]) {
+  uint32_t* o = reinterpret_cast<uint32_t*>(own);
+  uint32_t v[32];
+  tmem_ld32(acc, v);
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    if (h == 1 && cols <= 32) break;
+    tmem_ld_wait_for(v);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[16 * h + i] = f2_bf16(f2_regs(v, i));
+    if (h == 0 && cols > 32) tmem_ld32(acc + 32, v);
+  }
+}
+
 template <int ACT, class Ready>
 __device__ __forceinline__ bool epilogue_glu(const Params& p, const Unit& u, const EpiWarp& w, Ready ready) {
   const Job& job = p.job[u.job];
   const int width = p.bn / 2;
   if (!ready()) return false;
   if (w.nrow <= 0) return true;
-  const bool save = job.out[1].ptr != nullptr;
 #pragma unroll 1
-  for (int c = 32 * w.half; c < width; c += 64) {
-    const int col = u.n0 + c, ncol = min(32, job.N - col);
+  for (int c = 64 * w.half; c < width; c += 128) {
+    const int col = u.n0 + c, cols = min(64, width - c), ncol = min(cols, job.N - col);
     if (ncol <= 0) break;
+    uint4 own[8];
+    if (job.out[1].ptr) {
+      pack64(w.acc + c, cols, own);
+      rows_put128(w.stage, own, row_ptr(job.out[1], u.s, w.row0, col), 2 * job.out[1].sr, w.nrow, ncol);
+      pack64(w.acc + width + c, cols, own);
+      rows_put128(w.stage, own, row_ptr(job.out[2], u.s, w.row0, col), 2 * job.out[2].sr, w.nrow, ncol);
+    }
+    uint32_t* o = reinterpret_cast<uint32_t*>(own);
     uint32_t g[32], v[32];
     tmem_ld32(w.acc + c, g);
     tmem_ld32(w.acc + width + c, v);
-    tmem_ld_wait_for(g);
-    tmem_ld_wait_for(v);
-    uint4 own[4];
-    uint32_t* o = reinterpret_cast<uint32_t*>(own);
-    if (save) {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) o[i] = f2_bf16(f2_regs(g, i));
-      rows_put(w.stage, own, row_ptr(job.out[1], u.s, w.row0, col), 2 * job.out[1].sr, w.nrow, ncol);
+    for (int h = 0; h < 2; ++h) {
+      if (h == 1 && cols <= 32) break;
+      tmem_ld_wait_for(g);
+      tmem_ld_wait_for(v);
 #pragma unroll
-      for (int i = 0; i < 16; ++i) o[i] = f2_bf16(f2_regs(v, i));
-      rows_put(w.stage, own, row_ptr(job.out[2], u.s, w.row0, col), 2 * job.out[2].sr, w.nrow, ncol);
+      for (int i = 0; i < 16; ++i)
+        o[16 * h + i] = f2_bf16(f2_mul(act2<ACT>(f2_regs(g, i), nullptr), f2_regs(v, i)));
+      if (h == 0 && cols > 32) {
+        tmem_ld32(w.acc + c + 32, g);
+        tmem_ld32(w.acc + width + c + 32, v);
+      }
     }
-#pragma unroll
-    for (int i = 0; i < 16; ++i) o[i] = f2_bf16(f2_mul(act2<ACT>(f2_regs(g, i), nullptr), f2_regs(v, i)));
-    rows_put(w.stage, own, row_ptr(job.out[0], u.s, w.row0, col), 2 * job.out[0].sr, w.nrow, ncol);
+    rows_put128(w.stage, own, row_ptr(job.out[0], u.s, w.row0, col), 2 * job.out[0].sr, w.nrow, ncol);
   }
   return true;
 }
@@ -283,29 +343,31 @@ __device__ __forceinline__ bool epilogue_store(const Params& p, const Unit& u, c
   if (!ready()) return false;
   if (w.nrow <= 0) return true;
   const int lane = threadIdx.x & 31;
+  if (job.parts == 1) {
 #pragma unroll 1
-  for (int c = 32 * w.half; c < p.bn; c += 64) {
-    const int col = u.n0 + c, ncol = min(32, job.N - col);
-    if (ncol <= 0) break;
+    for (int c = 64 * w.half; c < p.bn && u.n0 + c < job.N; c += 128) {
+      uint4 own[8];
+      pack64(w.acc + c, 64, own);
+      rows_put128(w.stage, own, row_ptr(job.out[0], u.s, w.row0, u.n0 + c), 2 * job.out[0].sr, w.nrow,
+                  job.N - u.n0 - c);
+    }
+    return true;
+  }
+#pragma unroll 1
+  for (int c = 32 * w.half; c < p.bn && u.n0 + c < job.N; c += 64) {
+    const int ncol = job.N - u.n0 - c;
     uint32_t v[32];
     tmem_ld32(w.acc + c, v);
     tmem_ld_wait_for(v);
-    if (job.parts > 1) {
-      if (lane < w.nrow) {
-        const int64_t row = (int64_t(u.part) * job.samples + u.s) * job.rows + w.row0 + lane;
-        float4* dst = reinterpret_cast<float4*>(job.partial + row * job.N + col);
+    if (lane < w.nrow) {
+      const int64_t row = (int64_t(u.part) * job.samples + u.s) * job.rows + w.row0 + lane;
+      float4* dst = reinterpret_cast<float4*>(job.partial + row * job.N + u.n0 + c);
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if (4 * i < ncol)
-            dst[i] = make_float4(__uint_as_float(v[4 * i]), __uint_as_float(v[4 * i + 1]), __uint_as_float(v[4 * i + 2]),
-                                 __uint_as_float(v[4 * i + 3]));
-      }
-      continue;
+      for (int i = 0; i < 8; ++i)
+        if (4 * i < ncol)
+          dst[i] = make_float4(__uint_as_float(v[4 * i]), __uint_as_float(v[4 * i + 1]), __uint_as_float(v[4 * i + 2]),
+                               __uint_as_float(v[4 * i + 3]));
     }
-    float x[32];
-#pragma unroll
-    for (int i = 0; i < 32; ++i) x[i] = __uint_as_float(v[i]);
-    rows_store(w.stage, x, row_ptr(job.out[0], u.s, w.row0, col), 2 * job.out[0].sr, w.nrow, ncol);
   }
   return true;
 }
@@ -332,7 +394,7 @@ struct Producer {
     const uint32_t b_box = B_MN ? uint32_t(BOX) : uint32_t(half) * 128u;
     const int b_boxes = B_MN ? half / 64 : 2;
     const int m = u.m0 + rank * 128, n = u.n0 + (KIND == GLU ? 0 : rank * half);
-    int span = u.k0 / job.span_stages, k = (u.k0 - span * job.span_stages) * BK;
+    int span = u.k0 > 0 ? u.k0 / job.span_stages : 0, k = (u.k0 - span * job.span_stages) * BK;
     for (int q = u.k0; q < u.k1; ++q, ++it) {
       const int st = int(it % STAGES);
       if (it >= STAGES && !mbar_wait(empty + st, uint32_t((it / STAGES - 1) & 1), ctl)) return false;
@@ -385,7 +447,7 @@ struct Issuer {
     // (whose next 64 columns are the next box).
     const uint64_t da = sdesc_sw128(s0, A_MN ? BOX : 16, 1024);
     const uint64_t db = sdesc_sw128(s0 + OPERAND_BYTES, B_MN ? BOX : 16, 1024);
-    int k = (u.k0 % job.span_stages) * BK;
+    int k = u.k0 > 0 ? (u.k0 % job.span_stages) * BK : 0;
     for (int q = u.k0; q < u.k1; ++q, ++it) {
       const int st = int(it % STAGES);
       if (!mbar_wait(full + st, uint32_t((it / STAGES) & 1), ctl)) return false;
@@ -464,7 +526,7 @@ __global__ void __launch_bounds__(THREADS, 1) glu_kernel(const __grid_constant__
       bool ok = true;
       Walk<KIND> walk;
       Unit u;
-      for (int i = 0; ok && walk.at(p, p.order.unit(cid, ncl, i), u); ++i) {
+      for (Turn turn(p.order, cid, ncl); ok && walk.at(p, turn.t, u); turn.next(p.order)) {
         if (KIND == STORE && p.job[u.job].rows_k)
           ok = pr.unit<KIND, KIND == STORE>(p, u, ctl);
         else
@@ -494,7 +556,7 @@ __global__ void __launch_bounds__(THREADS, 1) glu_kernel(const __grid_constant__
       bool ok = true;
       Walk<KIND> walk;
       Unit u;
-      for (; walk.at(p, p.order.unit(cid, ncl, i), u); ++i) {
+      for (Turn turn(p.order, cid, ncl); walk.at(p, turn.t, u); turn.next(p.order), ++i) {
         const int buf = i & 1, use = i >> 1;
         if (use > 0 && !(ok = mbar_wait_cluster(tempty + buf, uint32_t((use - 1) & 1), ctl))) break;
         tc_fence_after();
@@ -521,7 +583,7 @@ __global__ void __launch_bounds__(THREADS, 1) glu_kernel(const __grid_constant__
     int i = 0;
     Walk<KIND> walk;
     Unit u;
-    for (; walk.at(p, p.order.unit(cid, ncl, i), u); ++i) {
+    for (Turn turn(p.order, cid, ncl); walk.at(p, turn.t, u); turn.next(p.order), ++i) {
       const int buf = i & 1, use = i >> 1;
       w.row0 = u.m0 + int(rank) * 128 + quarter * 32;
       w.nrow = min(32, p.job[u.job].rows - w.row0);
@@ -740,7 +802,26 @@ void one_span(Job& job, int k) {
   job.span_stages = (k + BK - 1) / BK;
 }
 
-ra_status launch(const char* who, void (*fn)(Params), const Params& p, int64_t units, cudaStream_t st) {
+// The job's tiles are known: the numbers that its walk divides by.
+void set_divs(Job& job) {
+  auto div = [](int64_t d) { return Div{uint32_t(d), d > 1 ? uint32_t(((int64_t(1) << 32) + d - 1) / d) : 0u}; };
+  job.by_band = div(int64_t(GROUP_M) * job.cols);
+  job.by_parts = div(job.parts);
+}
+// n d < 2^32 for what is divided: units of a sample by parts, its tiles by a band's.
+bool fits(const Job& job) {
+  const int64_t tiles = int64_t(job.m_tiles) * job.cols, most = int64_t(1) << 32;
+  return tiles * job.parts < most / job.parts && int64_t(GROUP_M) * job.cols < most / (tiles + 1);
+}
+
+ra_status launch(const char* who, void (*fn)(Params), Params& p, int64_t units, cudaStream_t st) {
+  for (int j = 0; j < p.n_jobs; ++j) {
+    set_divs(p.job[j]);
+    if (!fits(p.job[j])) {
+      set_error("%s: too many rows and features", who);
+      return RA_EINVAL;
+    }
+  }
   const ra_status as = ensure_dynamic_smem(reinterpret_cast<const void*>(fn), SMEM_ALLOC, who);
   if (as != RA_OK) return as;
   const int64_t pairs = num_sms() / 2 > 0 ? num_sms() / 2 : 1;
