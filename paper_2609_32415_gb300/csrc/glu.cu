@@ -392,7 +392,7 @@ struct Producer {
     const Job& job = p.job[u.job];
     const int half = p.bn / 2;  // columns of B that a CTA stages
     const uint32_t b_box = B_MN ? uint32_t(BOX) : uint32_t(half) * 128u;
-    const int b_boxes = B_MN ? half / 64 : 2;
+    const int b_boxes = B_MN ? (half + 63) / 64 : 2;  // the second may reach past the half: not used
     const int m = u.m0 + rank * 128, n = u.n0 + (KIND == GLU ? 0 : rank * half);
     int span = u.k0 > 0 ? u.k0 / job.span_stages : 0, k = (u.k0 - span * job.span_stages) * BK;
     for (int q = u.k0; q < u.k1; ++q, ++it) {
@@ -886,7 +886,7 @@ Plan make_plan(const Products& pr, int sms) {
   const int64_t pairs = sms / 2 > 0 ? sms / 2 : 1;
   Plan best{256, 1, 1, 0};
   double best_us = 1e30;
-  for (int bn = 256; bn >= 128; bn /= 2)
+  for (int bn = 256; bn >= 128; bn -= 64)
     for (int px = 1; px <= MAX_PARTS; px += px < 4 ? 1 : 4) {
       if (px > 1 && (pr.x.stages < 2 * px || pr.x.tiles(bn) > 2 * pairs)) break;
       for (int pw = 1; pw <= MAX_PARTS; pw += pw < 4 ? 1 : 4) {
@@ -1037,7 +1037,7 @@ extern "C" ra_status refadapt_glu(const ra_glu_args* a, void* stream) {
   const int64_t pairs = num_sms() / 2 > 0 ? num_sms() / 2 : 1;
   double best_us = 1e30;
   int64_t units = 0;
-  for (int bn = 256; bn >= 64; bn -= 64) {
+  for (int bn = 256; bn >= 64; bn -= 32) {
     int64_t n = 0;
     for (int j = 0; j < p.n_jobs; ++j) n += int64_t(p.job[j].samples) * p.job[j].m_tiles * div_up(a->F, bn / 2);
     const double us = fixed_us(bn) + round_us(bn, double(p.job[0].span_stages)) * double(div_up(n, pairs));
@@ -1176,7 +1176,7 @@ extern "C" ra_status refadapt_glu_backward(const ra_glu_grad_args* a, void* stre
     job.pre_gate = rows_of(g), job.pre_up = rows_of(w);
     double best_us = 1e30;
     int64_t units = 0;
-    for (int bn = 256; bn >= 128; bn /= 2) {
+    for (int bn = 256; bn >= 64; bn -= 64) {
       const int64_t n = int64_t(job.samples) * job.m_tiles * div_up(a->F, bn);
       const double us = fixed_us(bn) + round_us(bn, double(job.span_stages)) * double(div_up(n, pairs));
       if (us < best_us) best_us = us, p.bn = bn, units = n;
