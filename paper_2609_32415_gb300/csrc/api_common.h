@@ -42,6 +42,9 @@ bool check_seg(const ra_seg& s, const char* what, bool allow_null_if_empty = tru
 // box box_cols x box_rows, 128-byte swizzle or none, zero fill out of bounds.
 bool encode_seg(CUtensorMap* tm, const ra_seg& s, int B, int H, int d, int box_cols, int box_rows,
                 bool swizzle128);
+// The same with any swizzle mode.
+bool encode_seg(CUtensorMap* tm, const ra_seg& s, int B, int H, int d, int box_cols, int box_rows,
+                CUtensorMapSwizzle swizzle);
 
 // Launch attribute: the kernel may start while the previous one of the stream
 // finishes (it calls pdl_wait() before it touches global memory).

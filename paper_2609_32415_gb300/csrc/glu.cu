@@ -10,7 +10,7 @@
 //   GLU    a tile is w columns of g and the same w of the up projection: rank 0
 //          stages Wg's rows as its half of the MMA's N = 2 w, rank 1 Wu's, so one
 //          MMA forms both and the epilogue has g and w of a column in one thread;
-//   GRAD   du = dy Wd; the epilogue reads g and w and writes dg and dw;
+//   GRAD   du = dy Wd; the epilogue takes g and w and gives dg and dw (TMA tiles);
 //   STORE  the four gradients, in one launch: dx sums over both pairs of operands
 //          in one accumulator (K = 2 F), so its tiles are the long ones and go
 //          first; pairs that get one fewer of them take more of the weights'
@@ -45,25 +45,35 @@ namespace glu {
 
 constexpr int TM = 256;              // output rows of a pair's tile
 constexpr int MAX_BN = 256;          // accumulator columns
-constexpr int STAGES = 3;
-constexpr int BK = 128;              // K per stage
-constexpr int BOX = 128 * 64 * 2;    // K-major: 128 rows x 64 of K; MN-major: 128 of K x 64 columns
-constexpr int OPERAND_BYTES = 2 * BOX;
-constexpr int STAGE_BYTES = 2 * OPERAND_BYTES;
-constexpr int OFF_BAR = STAGES * STAGE_BYTES;
-constexpr int NUM_BARS = 2 * STAGES + 2 + 2 + 1;  // full, empty, tfull[2], tempty[2], drain
-constexpr int OFF_MISC = OFF_BAR + NUM_BARS * 8;
 constexpr int EPI_WARPS = 8;
-constexpr int EPI_BYTES = 32 * 128;  // staging of a warp: 32 rows of 64 columns
-constexpr int OFF_EPI = (OFF_MISC + 16 + 127) / 128 * 128;
-constexpr int SMEM_ALLOC = OFF_EPI + EPI_WARPS * EPI_BYTES + 1024;
 constexpr int THREADS = 64 + 32 * EPI_WARPS;
 constexpr int TMEM_COLS = 512;
 constexpr int GROUP_M = 16;  // tile rows per band of the tile order
 constexpr int MAX_JOBS = 4;
-static_assert(SMEM_ALLOC <= 232448, "shared memory budget");
 
 enum Kind { GLU, GRAD, STORE };
+
+// Shared memory of a kind's kernel. GLU and STORE: three stages of 128 of K (half
+// the hand-offs of six of 64) and a staging buffer per epilogue warp. GRAD: five
+// stages of 64, which leaves each epilogue warp two sets of two 32 x 32 tiles.
+constexpr int TILE_BYTES = 32 * 64;  // 32 rows of 32 columns
+template <int KIND>
+struct Cfg {
+  static constexpr int BK = KIND == GRAD ? 64 : 128;  // K per stage
+  static constexpr int STAGES = KIND == GRAD ? 5 : 3;
+  static constexpr int BOX = 128 * 64 * 2;     // of a K-major operand: 128 rows x 64 of K
+  static constexpr int MN_BOX = BK * 64 * 2;   // of an MN-major operand: BK of K x 64 columns
+  static constexpr int OPERAND_BYTES = 128 * BK * 2;
+  static constexpr int STAGE_BYTES = 2 * OPERAND_BYTES;
+  static constexpr int EPI_BYTES = KIND == GRAD ? 4 * TILE_BYTES : 32 * 128;  // of a warp
+  static constexpr int OFF_EPI = STAGES * STAGE_BYTES;
+  static constexpr int OFF_BAR = OFF_EPI + EPI_WARPS * EPI_BYTES;
+  static constexpr int TILE_BARS = KIND == GRAD ? 2 * EPI_WARPS : 0;          // sets of tiles loaded
+  static constexpr int NUM_BARS = 2 * STAGES + 2 + 2 + 1 + TILE_BARS;  // full, empty, tfull[2], tempty[2], drain
+  static constexpr int OFF_MISC = OFF_BAR + NUM_BARS * 8;
+  static constexpr int SMEM_ALLOC = OFF_MISC + 16 + 1024;
+  static_assert(SMEM_ALLOC <= 232448 && OFF_EPI % 1024 == 0 && EPI_BYTES % 1024 == 0, "shared memory budget");
+};
 
 struct Rows {
   __nv_bfloat16* ptr;
@@ -88,8 +98,7 @@ struct Job {
   int32_t parts;                 // of K, whole stages each
   Div by_band, by_parts;         // tiles of a band of GROUP_M tile rows; parts
   int32_t rows_k;                // K runs along the rows of both operands
-  Rows out[3];                   // GLU: out, pre_gate, pre_up; GRAD: dg, dw; STORE: the result
-  Rows pre_gate, pre_up;         // GRAD
+  Rows out[3];                   // GLU: out, pre_gate, pre_up; STORE: the result
   float* partial;                // parts > 1: [part][sample][row][N]
 };
 
@@ -144,6 +153,7 @@ struct Params {
   // Operand pairs of a job: STORE's two (dx) follow one another in K; GLU's tm_b
   // are Wg and Wu, one per rank.
   CUtensorMap tm_a[MAX_JOBS][2], tm_b[MAX_JOBS][2];
+  CUtensorMap tm_tile[4];  // GRAD: 32 x 32 tiles of pre_gate, pre_up, dg, dw
 };
 
 struct Unit {
@@ -298,31 +308,69 @@ __device__ __forceinline__ bool epilogue_glu(const Params& p, const Unit& u, con
   return true;
 }
 
+// GRAD: a warp's tiles (32 rows of 32 columns of g and of w) come by TMA into one of
+// its two sets, the next one's while it works; dg and dw take their places, row for
+// row, and leave by TMA. Sets are counted over all tiles of the warp: n.
+struct TilePipe {
+  uint8_t* sets;   // [2][g, w]
+  uint64_t* bars;  // [2]
+  int n = 0;       // tiles taken
+  int issued = 0;  // tiles whose loads were issued
+
+  __device__ __forceinline__ void load(const Params& p, const Unit& u, int row0, int c) {
+    if ((threadIdx.x & 31) == 0) {
+      bulk_wait_read_all();  // the set's last dg and dw have left it
+      uint8_t* set = sets + (issued & 1) * 2 * TILE_BYTES;
+      uint64_t* bar = bars + (issued & 1);
+      mbar_arrive_expect_tx(bar, 2 * TILE_BYTES);
+      tma_load_4d(set, &p.tm_tile[0], bar, u.n0 + c, row0, 0, u.s);
+      tma_load_4d(set + TILE_BYTES, &p.tm_tile[1], bar, u.n0 + c, row0, 0, u.s);
+    }
+    ++issued;
+    __syncwarp();
+  }
+  __device__ __forceinline__ bool wait(const WaitCtl& ctl) {
+    return __all_sync(0xffffffffu, mbar_wait(bars + (n & 1), uint32_t((n >> 1) & 1), ctl));
+  }
+  // Nothing of this warp's is in flight afterwards.
+  __device__ __forceinline__ void drain(uint64_t budget_ns) {
+    for (int i = n; i < issued; ++i) mbar_wait_drain(bars + (i & 1), uint32_t((i >> 1) & 1), budget_ns);
+    if ((threadIdx.x & 31) == 0) bulk_wait_all();
+    __syncwarp();
+  }
+};
+
+// next: the unit after u, or NULL; next_row0: this warp's first row in it.
 template <int ACT, class Ready>
-__device__ __forceinline__ bool epilogue_grad(const Params& p, const Unit& u, const EpiWarp& w, Ready ready) {
+__device__ __forceinline__ bool epilogue_grad(const Params& p, const Unit& u, const EpiWarp& w, TilePipe& pipe,
+                                              const WaitCtl& ctl, const Unit* next, int next_row0, Ready ready) {
   const Job& job = p.job[u.job];
-  auto cols = [&](int c) { return c < p.bn ? min(32, job.N - u.n0 - c) : 0; };
-  uint4 rg[4], rw[4];  // g and w of the next chunk
-  auto fetch = [&](int c) {
-    const int ncol = cols(c);
-    if (ncol <= 0 || w.nrow <= 0) return;
-    rows_fetch(row_ptr(job.pre_gate, u.s, w.row0, u.n0 + c), 2 * job.pre_gate.sr, w.nrow, rg, ncol);
-    rows_fetch(row_ptr(job.pre_up, u.s, w.row0, u.n0 + c), 2 * job.pre_up.sr, w.nrow, rw, ncol);
-  };
-  fetch(32 * w.half);
+  const int lane = threadIdx.x & 31;
+  auto has = [&](const Unit& v, int row0, int c) { return c < p.bn && v.n0 + c < job.N && row0 < job.rows; };
+  int c = 32 * w.half;
+  const bool any = has(u, w.row0, c);
+  if (any && pipe.issued == pipe.n) pipe.load(p, u, w.row0, c);
   if (!ready()) return false;
-  if (w.nrow <= 0) return true;
 #pragma unroll 1
-  for (int c = 32 * w.half; cols(c) > 0; c += 64) {
+  for (; any && has(u, w.row0, c); c += 64) {
     uint32_t v[32];
-    uint4 own_g[4], own_w[4];
     tmem_ld32(w.acc + c, v);
-    rows_turn(w.stage, rg, own_g);
-    rows_turn(w.stage, rw, own_w);
-    fetch(c + 64);
+    if (!pipe.wait(ctl)) {
+      tmem_ld_wait_for(v);
+      return false;
+    }
+    uint8_t* set = pipe.sets + (pipe.n & 1) * 2 * TILE_BYTES;
+    ++pipe.n;
+    uint4 g[4], up[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) g[q] = *stage_slot(set, lane, q), up[q] = *stage_slot(set + TILE_BYTES, lane, q);
+    if (has(u, w.row0, c + 64))
+      pipe.load(p, u, w.row0, c + 64);
+    else if (next && has(*next, next_row0, 32 * w.half))
+      pipe.load(p, *next, next_row0, 32 * w.half);
     tmem_ld_wait_for(v);
-    uint32_t* gp = reinterpret_cast<uint32_t*>(own_g);
-    uint32_t* wp = reinterpret_cast<uint32_t*>(own_w);
+    uint32_t* gp = reinterpret_cast<uint32_t*>(g);
+    uint32_t* wp = reinterpret_cast<uint32_t*>(up);
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       uint64_t da;
@@ -330,9 +378,15 @@ __device__ __forceinline__ bool epilogue_grad(const Params& p, const Unit& u, co
       gp[i] = f2_bf16(f2_mul(f2_mul(du, bf2_unpack(wp[i])), da));
       wp[i] = f2_bf16(f2_mul(du, a));
     }
-    const int ncol = cols(c);
-    rows_put(w.stage, own_g, row_ptr(job.out[0], u.s, w.row0, u.n0 + c), 2 * job.out[0].sr, w.nrow, ncol);
-    rows_put(w.stage, own_w, row_ptr(job.out[1], u.s, w.row0, u.n0 + c), 2 * job.out[1].sr, w.nrow, ncol);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) *stage_slot(set, lane, q) = g[q], *stage_slot(set + TILE_BYTES, lane, q) = up[q];
+    fence_proxy_async_smem();
+    __syncwarp();
+    if (lane == 0) {
+      tma_store_4d(&p.tm_tile[2], set, u.n0 + c, w.row0, 0, u.s);
+      tma_store_4d(&p.tm_tile[3], set + TILE_BYTES, u.n0 + c, w.row0, 0, u.s);
+      bulk_commit();
+    }
   }
   return true;
 }
@@ -389,39 +443,41 @@ struct Producer {
   template <int KIND, bool A_MN>
   __device__ __forceinline__ bool unit(const Params& p, const Unit& u, const WaitCtl& ctl) {
     constexpr bool B_MN = kBRowsK<KIND>;
+    using C = Cfg<KIND>;
+    constexpr int STAGES = C::STAGES, BK = C::BK;
     const Job& job = p.job[u.job];
     const int half = p.bn / 2;  // columns of B that a CTA stages
-    const uint32_t b_box = B_MN ? uint32_t(BOX) : uint32_t(half) * 128u;
+    const uint32_t b_box = B_MN ? uint32_t(C::MN_BOX) : uint32_t(half) * 128u;
     const int b_boxes = B_MN ? (half + 63) / 64 : 2;  // the second may reach past the half: not used
     const int m = u.m0 + rank * 128, n = u.n0 + (KIND == GLU ? 0 : rank * half);
     int span = u.k0 > 0 ? u.k0 / job.span_stages : 0, k = (u.k0 - span * job.span_stages) * BK;
     for (int q = u.k0; q < u.k1; ++q, ++it) {
       const int st = int(it % STAGES);
       if (it >= STAGES && !mbar_wait(empty + st, uint32_t((it / STAGES - 1) & 1), ctl)) return false;
-      uint8_t* sa = smem + st * STAGE_BYTES;
-      uint8_t* sb = sa + OPERAND_BYTES;
+      uint8_t* sa = smem + st * C::STAGE_BYTES;
+      uint8_t* sb = sa + C::OPERAND_BYTES;
       const uint32_t bar = full0 + 8u * st;
       const int pair = KIND == STORE && !A_MN ? span : 0;  // dx: the operand pair
       const int ks = A_MN ? span : u.s;                    // sample of A
-      const bool second = job.span_k - k > 64;             // K-major: the second box lies inside
+      const bool second = BK > 64 && job.span_k - k > 64;  // K-major: there is a second box, and it lies inside
       const CUtensorMap* ta = &p.tm_a[u.job][pair];
       const CUtensorMap* tb = &p.tm_b[u.job][KIND == GLU ? rank : pair];
       if (rank == 0)
-        mbar_arrive_expect_tx(full + st, 2u * ((A_MN || second ? 2u : 1u) * uint32_t(BOX) +
+        mbar_arrive_expect_tx(full + st, 2u * ((A_MN ? 2u * C::MN_BOX : (second ? 2u : 1u) * C::BOX) +
                                                (B_MN || second ? uint32_t(b_boxes) : 1u) * b_box));
       if (A_MN) {
         tma_load_4d_pair(sa, ta, bar, m, k, 0, ks);
-        tma_load_4d_pair(sa + BOX, ta, bar, m + 64, k, 0, ks);
+        tma_load_4d_pair(sa + C::MN_BOX, ta, bar, m + 64, k, 0, ks);
       } else {
         tma_load_4d_pair(sa, ta, bar, k, m, 0, ks);
-        if (second) tma_load_4d_pair(sa + BOX, ta, bar, k + 64, m, 0, ks);
+        if (second) tma_load_4d_pair(sa + C::BOX, ta, bar, k + 64, m, 0, ks);
       }
       if (B_MN) {
         tma_load_4d_pair(sb, tb, bar, n, k, 0, A_MN ? ks : 0);
-        if (b_boxes > 1) tma_load_4d_pair(sb + BOX, tb, bar, n + 64, k, 0, A_MN ? ks : 0);
+        if (b_boxes > 1) tma_load_4d_pair(sb + C::MN_BOX, tb, bar, n + 64, k, 0, A_MN ? ks : 0);
       } else {
         tma_load_4d_pair(sb, tb, bar, k, n, 0, 0);
-        if (second) tma_load_4d_pair(sb + BOX, tb, bar, k + 64, n, 0, 0);
+        if (second) tma_load_4d_pair(sb + C::BOX, tb, bar, k + 64, n, 0, 0);
       }
       k += BK;
       if (k >= job.span_k) k = 0, ++span;
@@ -440,23 +496,25 @@ struct Issuer {
   template <int KIND, bool A_MN>
   __device__ __forceinline__ bool unit(const Params& p, const Unit& u, uint32_t d_t, const WaitCtl& ctl) {
     constexpr bool B_MN = kBRowsK<KIND>;
+    using C = Cfg<KIND>;
+    constexpr int STAGES = C::STAGES, BK = C::BK;
     const Job& job = p.job[u.job];
     const uint32_t idesc = idesc_bf16_f32(TM, p.bn, A_MN, B_MN);
     // A step of 16 of K, in descriptor units of 16 bytes: 32 bytes of a K-major
     // row (64 of K, then the next box), 16 rows of 128 bytes of an MN-major box
     // (whose next 64 columns are the next box).
-    const uint64_t da = sdesc_sw128(s0, A_MN ? BOX : 16, 1024);
-    const uint64_t db = sdesc_sw128(s0 + OPERAND_BYTES, B_MN ? BOX : 16, 1024);
+    const uint64_t da = sdesc_sw128(s0, A_MN ? C::MN_BOX : 16, 1024);
+    const uint64_t db = sdesc_sw128(s0 + C::OPERAND_BYTES, B_MN ? C::MN_BOX : 16, 1024);
     int k = u.k0 > 0 ? (u.k0 % job.span_stages) * BK : 0;
     for (int q = u.k0; q < u.k1; ++q, ++it) {
       const int st = int(it % STAGES);
       if (!mbar_wait(full + st, uint32_t((it / STAGES) & 1), ctl)) return false;
       tc_fence_after();
-      const uint64_t a = da + uint64_t(st * (STAGE_BYTES >> 4)), b = db + uint64_t(st * (STAGE_BYTES >> 4));
+      const uint64_t a = da + uint64_t(st * (C::STAGE_BYTES >> 4)), b = db + uint64_t(st * (C::STAGE_BYTES >> 4));
       const int left = job.span_k - k;
       auto step = [&](int kk) {
-        const uint32_t oa = A_MN ? kk * 128 : (kk >> 2) * (BOX >> 4) + (kk & 3) * 2;
-        const uint32_t ob = B_MN ? kk * 128 : (kk >> 2) * (BOX >> 4) + (kk & 3) * 2;
+        const uint32_t oa = A_MN ? kk * 128 : (kk >> 2) * (C::BOX >> 4) + (kk & 3) * 2;
+        const uint32_t ob = B_MN ? kk * 128 : (kk >> 2) * (C::BOX >> 4) + (kk & 3) * 2;
         umma_ss_pair(d_t, a + oa, b + ob, idesc, (q > u.k0 || kk > 0) ? 1u : 0u);
       };
       if (left >= BK) {
@@ -477,16 +535,18 @@ struct Issuer {
 
 template <int KIND, int ACT>
 __global__ void __launch_bounds__(THREADS, 1) glu_kernel(const __grid_constant__ Params p) {
+  using C = Cfg<KIND>;
+  constexpr int STAGES = C::STAGES;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
-  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + OFF_BAR);
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + C::OFF_BAR);
   uint64_t* full = bars;
   uint64_t* empty = bars + STAGES;
   uint64_t* tfull = bars + 2 * STAGES;
   uint64_t* tempty = bars + 2 * STAGES + 2;
   uint64_t* drain = bars + 2 * STAGES + 4;
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + OFF_MISC);
-  volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + OFF_MISC + 4);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + C::OFF_MISC);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + C::OFF_MISC + 4);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = cluster_rank();
   const int cid = int(blockIdx.x >> 1), ncl = int(gridDim.x >> 1);
@@ -500,6 +560,7 @@ __global__ void __launch_bounds__(THREADS, 1) glu_kernel(const __grid_constant__
       mbar_init(tempty + b, 2 * EPI_WARPS);
     }
     mbar_init(drain, 1);
+    for (int i = 0; i < C::TILE_BARS; ++i) mbar_init(drain + 1 + i, 1);
     *abort_flag = 0;
     fence_mbar_init();
   }
@@ -578,14 +639,22 @@ __global__ void __launch_bounds__(THREADS, 1) glu_kernel(const __grid_constant__
     const int quarter = warp & 3;
     EpiWarp w;
     w.half = (warp - 2) >> 2;
-    w.stage = smem + OFF_EPI + (warp - 2) * EPI_BYTES;
+    w.stage = smem + C::OFF_EPI + (warp - 2) * C::EPI_BYTES;
     const uint32_t tempty0 = mapa_shared(smem_u32(tempty), 0);
     int i = 0;
+    TilePipe pipe{w.stage, drain + 1 + 2 * (warp - 2)};
     Walk<KIND> walk;
-    Unit u;
-    for (Turn turn(p.order, cid, ncl); walk.at(p, turn.t, u); turn.next(p.order), ++i) {
-      const int buf = i & 1, use = i >> 1;
-      w.row0 = u.m0 + int(rank) * 128 + quarter * 32;
+    Turn turn(p.order, cid, ncl);
+    Unit u, next;
+    bool more = walk.at(p, turn.t, u);
+    auto step = [&] {
+      turn.next(p.order);
+      more = walk.at(p, turn.t, next);
+    };
+    for (; more; ++i, u = next) {
+      if (KIND == GRAD) step();  // its tiles are loaded ahead
+      const int buf = i & 1, use = i >> 1, row = int(rank) * 128 + quarter * 32;
+      w.row0 = u.m0 + row;
       w.nrow = min(32, p.job[u.job].rows - w.row0);
       w.acc = tmem + (uint32_t(quarter * 32) << 16) + uint32_t(buf * MAX_BN);
       auto ready = [&] {
@@ -597,7 +666,7 @@ __global__ void __launch_bounds__(THREADS, 1) glu_kernel(const __grid_constant__
       if constexpr (KIND == GLU)
         ok = epilogue_glu<ACT>(p, u, w, ready);
       else if constexpr (KIND == GRAD)
-        ok = epilogue_grad<ACT>(p, u, w, ready);
+        ok = epilogue_grad<ACT>(p, u, w, pipe, ctl, more ? &next : nullptr, next.m0 + row, ready);
       else
         ok = epilogue_store(p, u, w, ready);
       if (!ok) break;
@@ -609,7 +678,9 @@ __global__ void __launch_bounds__(THREADS, 1) glu_kernel(const __grid_constant__
         else
           mbar_arrive_remote(tempty0 + 8u * buf);
       }
+      if (KIND != GRAD) step();
     }
+    if (KIND == GRAD) pipe.drain(p.budget_ns);
   }
   tc_fence_before();
   __syncthreads();
@@ -795,12 +866,20 @@ bool encode(CUtensorMap* tm, const RowTensor& t, int box_rows) {
   const ra_seg s{const_cast<void*>(t.ptr), t.B > 1 ? t.ss : 0, 0, t.sr, t.n, 0};
   return encode_seg(tm, s, t.B, 1, t.cols, 64, box_rows, true);
 }
+// 32 x 32 tiles, in shared memory as stage_slot() has them.
+bool encode_tiles(CUtensorMap* tm, const RowTensor& t) {
+  const ra_seg s{const_cast<void*>(t.ptr), t.B > 1 ? t.ss : 0, 0, t.sr, t.n, 0};
+  return encode_seg(tm, s, t.B, 1, t.cols, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B);
+}
 
+template <int KIND>
 void one_span(Job& job, int k) {
   job.spans = job.parts = 1;
   job.span_k = k;
-  job.span_stages = (k + BK - 1) / BK;
+  job.span_stages = (k + Cfg<KIND>::BK - 1) / Cfg<KIND>::BK;
 }
+constexpr int BK = Cfg<STORE>::BK;
+static_assert(BK == Cfg<GLU>::BK, "one stage length in the cost model");
 
 // The job's tiles are known: the numbers that its walk divides by.
 void set_divs(Job& job) {
@@ -814,6 +893,7 @@ bool fits(const Job& job) {
   return tiles * job.parts < most / job.parts && int64_t(GROUP_M) * job.cols < most / (tiles + 1);
 }
 
+template <int KIND>
 ra_status launch(const char* who, void (*fn)(Params), Params& p, int64_t units, cudaStream_t st) {
   for (int j = 0; j < p.n_jobs; ++j) {
     set_divs(p.job[j]);
@@ -822,7 +902,7 @@ ra_status launch(const char* who, void (*fn)(Params), Params& p, int64_t units, 
       return RA_EINVAL;
     }
   }
-  const ra_status as = ensure_dynamic_smem(reinterpret_cast<const void*>(fn), SMEM_ALLOC, who);
+  const ra_status as = ensure_dynamic_smem(reinterpret_cast<const void*>(fn), Cfg<KIND>::SMEM_ALLOC, who);
   if (as != RA_OK) return as;
   const int64_t pairs = num_sms() / 2 > 0 ? num_sms() / 2 : 1;
   cudaLaunchAttribute attr[2];
@@ -834,7 +914,7 @@ ra_status launch(const char* who, void (*fn)(Params), Params& p, int64_t units, 
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(unsigned(2 * (units < pairs ? units : pairs)));
   cfg.blockDim = dim3(THREADS);
-  cfg.dynamicSmemBytes = SMEM_ALLOC;
+  cfg.dynamicSmemBytes = Cfg<KIND>::SMEM_ALLOC;
   cfg.stream = st;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
@@ -987,7 +1067,7 @@ extern "C" ra_status refadapt_glu(const ra_glu_args* a, void* stream) {
     job.gated = s.gated ? 1 : 0;
     job.m_tiles = int32_t(div_up(r.n, TM));
     job.N = a->F;
-    one_span(job, a->C);
+    one_span<GLU>(job, a->C);
     for (int i = 0; i < outs; ++i)
       job.out[i] = Rows{static_cast<__nv_bfloat16*>(const_cast<void*>(o[i].ptr)), o[i].ss, o[i].sr};
   }
@@ -1058,7 +1138,7 @@ extern "C" ra_status refadapt_glu(const ra_glu_args* a, void* stream) {
     return RA_EINVAL;
   }
   note_launch("CTA pairs, %d columns", p.bn / 2);
-  return launch(who, a->act == RA_ACT_GELU ? glu_kernel<GLU, RA_ACT_GELU> : glu_kernel<GLU, RA_ACT_SILU>, p, units, static_cast<cudaStream_t>(stream));
+  return launch<GLU>(who, a->act == RA_ACT_GELU ? glu_kernel<GLU, RA_ACT_GELU> : glu_kernel<GLU, RA_ACT_SILU>, p, units, static_cast<cudaStream_t>(stream));
 }
 
 extern "C" size_t refadapt_glu_backward_workspace_size(int32_t B, int32_t rows, int32_t C, int32_t F, int32_t O) {
@@ -1171,23 +1251,24 @@ extern "C" ra_status refadapt_glu_backward(const ra_glu_grad_args* a, void* stre
     job.samples = src.B, job.rows = src.n;
     job.m_tiles = int32_t(div_up(src.n, TM));
     job.N = a->F;
-    one_span(job, a->O);
-    job.out[0] = rows_of(dgt), job.out[1] = rows_of(dwt);
-    job.pre_gate = rows_of(g), job.pre_up = rows_of(w);
+    one_span<GRAD>(job, a->O);
     double best_us = 1e30;
     int64_t units = 0;
     for (int bn = 256; bn >= 64; bn -= 64) {
       const int64_t n = int64_t(job.samples) * job.m_tiles * div_up(a->F, bn);
-      const double us = fixed_us(bn) + round_us(bn, double(job.span_stages)) * double(div_up(n, pairs));
+      const double us = fixed_us(bn) + round_us(bn, double(job.span_stages) / 2) * double(div_up(n, pairs));
       if (us < best_us) best_us = us, p.bn = bn, units = n;
     }
     job.cols = int32_t(div_up(a->F, p.bn));
-    if (!encode(&p.tm_a[0][0], src, 128) || !encode(&p.tm_b[0][0], w_down, BK)) return RA_EINVAL;
+    if (!encode(&p.tm_a[0][0], src, 128) || !encode(&p.tm_b[0][0], w_down, Cfg<GRAD>::BK) ||
+        !encode_tiles(&p.tm_tile[0], flat ? flatten(g) : g) || !encode_tiles(&p.tm_tile[1], flat ? flatten(w) : w) ||
+        !encode_tiles(&p.tm_tile[2], flat ? flatten(dgt) : dgt) || !encode_tiles(&p.tm_tile[3], flat ? flatten(dwt) : dwt))
+      return RA_EINVAL;
     if (units > 2147483647) {
       set_error("%s: too many rows", who);
       return RA_EINVAL;
     }
-    const ra_status r = launch(who, a->act == RA_ACT_GELU ? glu_kernel<GRAD, RA_ACT_GELU> : glu_kernel<GRAD, RA_ACT_SILU>, p,
+    const ra_status r = launch<GRAD>(who, a->act == RA_ACT_GELU ? glu_kernel<GRAD, RA_ACT_GELU> : glu_kernel<GRAD, RA_ACT_SILU>, p,
                                units, st);
     if (r != RA_OK) return r;
   }
@@ -1224,7 +1305,7 @@ extern "C" ra_status refadapt_glu_backward(const ra_glu_grad_args* a, void* stre
   };
   if (a->dx) {
     Job& job = add(pr.x, plan.parts_x, rows_of(dx));
-    one_span(job, a->F);
+    one_span<STORE>(job, a->F);
     job.spans = 2;
     job.parts = plan.parts_x;
     if (!encode(&p.tm_a[0][0], flat_x ? flatten(dgt) : dgt, 128) || !encode(&p.tm_a[0][1], flat_x ? flatten(dwt) : dwt, 128) ||
@@ -1238,7 +1319,7 @@ extern "C" ra_status refadapt_glu_backward(const ra_glu_grad_args* a, void* stre
     if (!out[i]) continue;
     const int n = p.n_jobs;
     Job& job = add(pr.w[i], plan.parts_w, Rows{static_cast<__nv_bfloat16*>(out[i]), 0, pr.w[i].N});
-    one_span(job, flat_w ? int(all) : a->rows);
+    one_span<STORE>(job, flat_w ? int(all) : a->rows);
     job.spans = flat_w ? 1 : a->B;
     job.parts = plan.parts_w;
     job.rows_k = 1;
@@ -1252,7 +1333,7 @@ extern "C" ra_status refadapt_glu_backward(const ra_glu_grad_args* a, void* stre
   }
   const int64_t ctas = units < pairs ? units : pairs;
   if (ctas < pairs) p.order.early = 0;  // one unit a pair
-  const ra_status r = launch(who, glu_kernel<STORE, 0>, p, units, st);
+  const ra_status r = launch<STORE>(who, glu_kernel<STORE, 0>, p, units, st);
   if (r != RA_OK || join.n == 0) return r;
   cudaLaunchConfig_t cfg = {};
   const int64_t blocks = div_up(vecs, 256), most = int64_t(8) * sms;

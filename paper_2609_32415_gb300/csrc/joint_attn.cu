@@ -160,19 +160,6 @@ __host__ __device__ __forceinline__ int round_items(int live, int slots, int res
 
 __device__ __forceinline__ bool refreshes(int m) { return m == RA_MODE_COMPUTE || m == RA_MODE_FULL; }
 
-// Tile (c0 = column, c1 = row, c2 = head, c3 = sample) of a 4-D tensor map,
-// shared -> global, bulk-group completion; rows past the tensor are clipped.
-__device__ __forceinline__ void tma_store_4d(const void* tmap, const void* src, int32_t c0, int32_t c1,
-                                             int32_t c2, int32_t c3) {
-  asm volatile("cp.async.bulk.tensor.4d.global.shared::cta.bulk_group [%0, {%2, %3, %4, %5}], [%1];" ::"l"(
-                   reinterpret_cast<uint64_t>(tmap)),
-               "r"(smem_u32(src)), "r"(c0), "r"(c1), "r"(c2), "r"(c3)
-               : "memory");
-}
-__device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
-__device__ __forceinline__ void bulk_wait_read_all() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
-__device__ __forceinline__ void bulk_wait_all() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
-
 __device__ __forceinline__ void kv_tile(const Params& p, int j, int& r, int& row0) {
   if (j < p.kv_tiles[0]) {
     r = 0;
