@@ -575,8 +575,8 @@ ra_status refadapt_residual_norm(const ra_resnorm_args* args, void* stream);
  *   dgate, dscale, dshift   fp32 [B][C], contiguous
  *   dpost_w, dpre_w         fp32 [C], summed over the samples
  * Any output may be NULL. y may be NULL (then dy, dgate and dpost_w too).
- * dh may equal dh_out or dx, and dy may equal y, in place. Column sums are fp32
- * in a fixed order (deterministic).
+ * dh and dy may each equal an input (same strides), in place, but must not
+ * overlap one another. Column sums are fp32 in a fixed order (deterministic).
  *  workspace   device scratch of
  *              refadapt_residual_norm_backward_workspace_size(B, rows, C) bytes
  *              (on the device that is current), 16-byte aligned; calls that
@@ -629,8 +629,9 @@ ra_status refadapt_residual_norm_backward(const ra_resnorm_grad_args* args, void
  * C and F multiples of 8, at least 64; pointers 16-byte aligned, row strides
  * multiples of 8 elements and at least the row's length. A segment with gated =
  * 1 is skipped for samples whose mode is RA_MODE_REUSE. err_word: device int32
- * or NULL; bit 0 set if a device wait timed out. Deterministic; how a call is
- * cut into tiles follows from its sizes. */
+ * or NULL; bit 0 set if a device wait timed out. Outputs must not overlap inputs
+ * or one another; B * rows below 2^30. Deterministic; how a call is cut into
+ * tiles follows from its sizes. */
 typedef enum { RA_ACT_SILU = 0, RA_ACT_GELU = 1 } ra_act;
 
 typedef struct {
@@ -672,8 +673,8 @@ ra_status refadapt_glu(const ra_glu_args* args, void* stream);
  *  workspace           device scratch of refadapt_glu_backward_workspace_size()
  *                      bytes (on the device that is current), 16-byte aligned;
  *                      calls that share it must be stream-ordered.
- * C, F, O multiples of 8, at least 64; pointers and strides as for refadapt_glu.
- * Rows of zero: the weights' gradients are zero. Deterministic. */
+ * C, F, O multiples of 8, at least 64; pointers and strides as for refadapt_glu;
+ * outputs must not overlap inputs. Rows of zero: the weights' gradients are zero. Deterministic. */
 typedef struct {
   int32_t B, rows, C, F, O, act;
   const void* dy;

@@ -80,12 +80,16 @@ struct Rows {
   int64_t ss, sr;
 };
 
-// Division by a number that the host knows: n / d = high word of n * ceil(2^32 / d)
-// for n d < 2^32, what a launch's units stay below. The roles' threads divide a few
-// times per tile; with plain divisions a tile of one or two stages took 1.5 us.
+// Division by a number that the host knows, for n and d below 2^31: the high word
+// of n * ceil(2^32 / d) is n / d or one more. The roles' threads divide a few times
+// per tile.
 struct Div {
   uint32_t d, mul;  // mul 0: d is 1
-  __device__ __forceinline__ uint32_t operator()(uint32_t n) const { return mul ? __umulhi(n, mul) : n; }
+  __device__ __forceinline__ uint32_t operator()(uint32_t n) const {
+    if (mul == 0) return n;
+    const uint32_t q = __umulhi(n, mul);
+    return q * d > n ? q - 1 : q;
+  }
 };
 
 struct Job {
@@ -887,21 +891,9 @@ void set_divs(Job& job) {
   job.by_band = div(int64_t(GROUP_M) * job.cols);
   job.by_parts = div(job.parts);
 }
-// n d < 2^32 for what is divided: units of a sample by parts, its tiles by a band's.
-bool fits(const Job& job) {
-  const int64_t tiles = int64_t(job.m_tiles) * job.cols, most = int64_t(1) << 32;
-  return tiles * job.parts < most / job.parts && int64_t(GROUP_M) * job.cols < most / (tiles + 1);
-}
-
 template <int KIND>
 ra_status launch(const char* who, void (*fn)(Params), Params& p, int64_t units, cudaStream_t st) {
-  for (int j = 0; j < p.n_jobs; ++j) {
-    set_divs(p.job[j]);
-    if (!fits(p.job[j])) {
-      set_error("%s: too many rows and features", who);
-      return RA_EINVAL;
-    }
-  }
+  for (int j = 0; j < p.n_jobs; ++j) set_divs(p.job[j]);
   const ra_status as = ensure_dynamic_smem(reinterpret_cast<const void*>(fn), Cfg<KIND>::SMEM_ALLOC, who);
   if (as != RA_OK) return as;
   const int64_t pairs = num_sms() / 2 > 0 ? num_sms() / 2 : 1;
@@ -1052,6 +1044,11 @@ extern "C" ra_status refadapt_glu(const ra_glu_args* a, void* stream) {
       set_error("%s: seg %d: too many rows", who, g);
       return RA_EINVAL;
     }
+    for (int i = 0; i < outs; ++i)
+      if (o[i].ptr == s.x || (i > 0 && (o[i].ptr == s.out || s.pre_gate == s.pre_up))) {
+        set_error("%s: seg %d: x, out, pre_gate and pre_up must not overlap", who, g);
+        return RA_EINVAL;
+      }
     // samples whose rows follow one another share row tiles
     bool flat = !s.gated && joins(r);
     for (int i = 0; i < outs; ++i) flat &= joins(o[i]);
@@ -1210,6 +1207,10 @@ extern "C" ra_status refadapt_glu_backward(const ra_glu_grad_args* a, void* stre
       ((a->dw_gate || a->dw_up) && !check_rows(who, "x", x, false)) ||
       (a->dw_down && !check_rows(who, "hidden", hid, false)) || (a->dx && !check_rows(who, "dx", dx, true)))
     return RA_EINVAL;
+  if (a->dx && (a->dx == a->dy || a->dx == a->x || a->dx == a->hidden || a->dx == a->pre_gate || a->dx == a->pre_up)) {
+    set_error("%s: dx must not overlap an input", who);
+    return RA_EINVAL;
+  }
   if ((dgw && (!a->w_down || !aligned16(a->w_down))) ||
       (a->dx && (!a->w_gate || !a->w_up || !aligned16(a->w_gate) || !aligned16(a->w_up)))) {
     set_error("%s: the weights that the wanted gradients need must be given and 16-byte aligned", who);

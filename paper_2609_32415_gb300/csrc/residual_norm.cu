@@ -802,7 +802,7 @@ bool check_vec(const char* who, const char* what, const void* ptr, int64_t ss) {
 }
 // Where an output shares memory with an input only in place: `a` may be `b` or lie apart from it.
 bool same_or_apart(const void* a, int64_t a_ss, int64_t a_sr, const void* b, int64_t b_ss, int64_t b_sr) {
-  return a != b || (a_ss == b_ss && a_sr == b_sr);
+  return !a || a != b || (a_ss == b_ss && a_sr == b_sr);
 }
 
 template <class P>
@@ -1024,10 +1024,14 @@ extern "C" ra_status refadapt_residual_norm_backward(const ra_resnorm_grad_args*
       set_error("%s: without y there is no dy, dgate or dpost_w", who);
       return RA_EINVAL;
     }
-    if ((a->dy && a->dy == a->dh) ||
-        !same_or_apart(a->dh, a->dh_stride_s, a->dh_stride_r, a->dh_out, a->dh_out_stride_s, a->dh_out_stride_r) ||
-        !same_or_apart(a->dh, a->dh_stride_s, a->dh_stride_r, a->dx, a->dx_stride_s, a->dx_stride_r) ||
-        !same_or_apart(a->dy, a->dy_stride_s, a->dy_stride_r, a->y, a->y_stride_s, a->y_stride_r)) {
+    auto in_place_ok = [&](const void* out, int64_t ss, int64_t sr) {
+      return same_or_apart(out, ss, sr, a->h, a->h_stride_s, a->h_stride_r) &&
+             same_or_apart(out, ss, sr, a->y, a->y_stride_s, a->y_stride_r) &&
+             same_or_apart(out, ss, sr, a->dx, a->dx_stride_s, a->dx_stride_r) &&
+             same_or_apart(out, ss, sr, a->dh_out, a->dh_out_stride_s, a->dh_out_stride_r);
+    };
+    if ((a->dy && a->dy == a->dh) || !in_place_ok(a->dh, a->dh_stride_s, a->dh_stride_r) ||
+        !in_place_ok(a->dy, a->dy_stride_s, a->dy_stride_r)) {
       set_error("%s: dh and dy are the same tensor, or an output in place has other strides than its input", who);
       return RA_EINVAL;
     }

@@ -423,3 +423,29 @@ def test_residual_norm_refusals(cuda_ok):
         api.refadapt_residual_norm_backward({k: v for k, v in b.items() if k not in ("dx", "dh_out")}, 64, 2, 1, ws)
     with pytest.raises(RefAdaptError, match="same tensor"):
         api.refadapt_residual_norm_backward(dict(b, dy=b["dh"]), 64, 2, 1, ws)
+
+
+def test_residual_norm_backward_every_place_in_place(cuda_ok):
+    """dh and dy in the place of any input, and refused where the strides differ."""
+    from paper_2609_32415_gb300 import api
+    from paper_2609_32415_gb300._lib import RefAdaptError
+    g = torch.Generator().manual_seed(12)
+    B, n, C = 1, 70, 512
+    ws = api.residual_norm_backward_workspace(B, n, C)
+    for a, b in (("h", "dx"), ("dx", "dh_out"), ("y", "h"), ("dh_out", "y")):
+        s = norm_case(B, n, C, g, True)
+        s["dx"], s["dh_out"] = bf((B, n, C), g), bf((B, n, C), g)
+        keep = {k: v.clone() for k, v in s.items()}
+        s = backward_case(s, n, C, B)
+        s["dh"], s["dy"] = s[a], s[b]
+        err = torch.zeros(1, dtype=torch.int32, device="cuda")
+        api.refadapt_residual_norm_backward(s, C, 2, 1, ws, err_word=err)
+        api.refadapt_check_error(err)
+        check_backward(s, 2, 1, 1e-6, 1.0, keep)
+    s = norm_case(B, n, C, g, True)
+    wide = bf((B, n, C + 64), g)
+    s["h"], s["dx"], s["dh_out"] = wide[..., :C], bf((B, n, C), g), bf((B, n, C), g)
+    s = backward_case(s, n, C, B)
+    s["dh"] = wide.reshape(-1)[:n * C].view(B, n, C)
+    with pytest.raises(RefAdaptError, match="other strides"):
+        api.refadapt_residual_norm_backward(s, C, 2, 1, ws)

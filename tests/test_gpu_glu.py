@@ -279,3 +279,33 @@ def test_glu_refusals(cuda_ok):
         call({k: v for k, v in b.items() if k != "hidden"}, 0, ws, err)
     with pytest.raises(ValueError, match="dw_down: expected"):
         call(dict(b, dw_down=b["dw_down"].float()), 0, ws, err)
+
+
+def test_glu_overlapping_outputs_are_refused(cuda_ok):
+    from paper_2609_32415_gb300 import api
+    from paper_2609_32415_gb300._lib import RefAdaptError
+    g = torch.Generator().manual_seed(2)
+    s = seg(1, 40, 128, 128, g, True)
+    for bad in ({"out": s["x"]}, {"pre_up": s["pre_gate"]}, {"pre_gate": s["out"]}):
+        with pytest.raises(RefAdaptError, match="overlap"):
+            api.refadapt_glu([dict(s, **bad)], 128, 128, 0)
+    b = grads(1, 40, 128, 128, 128, g, 0)
+    ws = api.glu_backward_workspace(1, 40, 128, 128, 128)
+    err = torch.zeros(1, dtype=torch.int32, device="cuda")
+    for k in ("dy", "x", "hidden"):
+        with pytest.raises(RefAdaptError, match="overlap"):
+            call(dict(b, dx=b[k]), 0, ws, err)
+
+
+def test_glu_many_tiles(cuda_ok):
+    """More tile rows than a band, several bands, and a last band that is not full."""
+    from paper_2609_32415_gb300 import api
+    g = torch.Generator().manual_seed(31)
+    s = seg(1, 256 * 35 + 9, 64, 264, g, False)
+    err = torch.zeros(1, dtype=torch.int32, device="cuda")
+    api.refadapt_glu([s], 264, 64, 0, err_word=err)
+    api.refadapt_check_error(err)
+    check_forward(s, 0)
+    s = grads(2, 256 * 17 + 100, 64, 520, 64, g, 1)
+    call(s, 1, api.glu_backward_workspace(2, 256 * 17 + 100, 64, 520, 64), err)
+    check_grads(s, 1)
