@@ -34,6 +34,7 @@
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
+#include <cmath>
 #include <cstring>
 
 #include "api_common.h"
@@ -920,10 +921,12 @@ ra_status launch(const char* who, void (*fn)(Params), Params& p, int64_t units, 
 }
 
 // Microseconds of a round of tiles of bn columns over `stages` of K, and of a
-// launch around its rounds: fitted to single waves on a GB300.
+// launch around its rounds, fitted on a GB300: single waves of long K, and tiles of
+// one to four stages, where the epilogue (0.01 us a column) is the longer part but
+// not all of the time.
 double round_us(int bn, double stages) {
-  const double mma = stages / 8.0 * (3.11 + 0.00766 * bn), epilogue = 0.0085 * bn;
-  return mma > epilogue ? mma : epilogue;
+  const double mma = stages / 8.0 * (3.11 + 0.00766 * bn), epilogue = 0.0105 * bn;
+  return std::sqrt(mma * mma + epilogue * epilogue);
 }
 double fixed_us(int bn) { return 4.4 + 0.0088 * bn; }
 

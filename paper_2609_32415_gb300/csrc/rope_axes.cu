@@ -174,11 +174,11 @@ bool make_freqs(Freqs& fr, const char* who, int n_axes, const int32_t* axis_dim,
     set_error("%s: the axes have %lld columns, a head %d", who, static_cast<long long>(sum), d);
     return false;
   }
-  const double two_pi = 6.283185307179586476925;
+  const double two_pi = 6.283185307179586476925, log2_base = std::log2(base);
   int pair = 0;
   for (int a = 0; a < n_axes; ++a)
     for (int i = 0; i < axis_dim[a] / 2; ++i, ++pair) {
-      const double f = std::pow(base, -2.0 * i / axis_dim[a]) / two_pi;
+      const double f = std::exp2(log2_base * (-2.0 * i / axis_dim[a])) / two_pi;
       fr.f[pair].x = float(f);
       fr.f[pair].y = float(f - double(fr.f[pair].x));
       fr.axis[pair] = uint8_t(a);
