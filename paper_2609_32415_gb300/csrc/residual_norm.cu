@@ -471,9 +471,8 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) residual_norm_kernel(const __g
 
 // ------------------------------------------------------------------ backward
 // A CTA takes a run of a sample's rows. A row warp has a row at a time: it copies
-// h, y, dx and dh' into its slot in shared memory (the next row starts for L2
-// meanwhile) and reduces what the whole row gives, in two passes over the slot: the
-// means, then everything else (RowSums). Then a group of column warps (eight columns
+// h, y, dx and dh' into its slot in shared memory and reduces what the whole row
+// gives, in two passes over the slot: the means, then everything else. Then a group of column warps (eight columns
 // a thread) takes the row from the slot: with the row's eight numbers known, dh, dy
 // and the columns' sums need no further reduction, and S0, S1, S2 stay in the
 // threads' registers. Against groups that hold a row and reduce it across warps (8192
@@ -599,10 +598,6 @@ __global__ void __launch_bounds__(THREADS, 1) residual_norm_grad_kernel(const __
     const int mine = (pieces - lane + 31) / 32;  // pieces of this lane
     auto get = [](const uint8_t* at) { return widen(*reinterpret_cast<const uint4*>(at)); };
     for (int k = 0, r = warp; r < n; ++k, r += WR) {
-      if (r + WR < n && lane < 4) {
-        const __nv_bfloat16* next = row_of(lane, r + WR);
-        if (next) prefetch_bulk_l2(next, uint32_t(row_bytes));
-      }
       cp_async_wait<0>();
       float hm = 0.f, ym = 0.f;
       if (layer) {
