@@ -522,7 +522,7 @@ struct alignas(16) RowNumbers {
   float h_mean, h_r, e0, e1, y_mean, y_r, f0, f1;
 };
 
-template <int THREADS>
+template <int THREADS, bool PRE, bool POST>
 __global__ void __launch_bounds__(THREADS, 1) residual_norm_grad_kernel(const __grid_constant__ GradParams p) {
   extern __shared__ __align__(16) uint8_t smem[];
   const GradShape shape{p.row_warps, p.groups, p.group_warps, 0};
@@ -594,29 +594,28 @@ __global__ void __launch_bounds__(THREADS, 1) residual_norm_grad_kernel(const __
   if (warp < WR) {
     // ---------------------------------------------------------------- rows
     const uint8_t* const slot = slots + warp * slot_bytes + 16 * lane;
-    const bool layer = p.pre == RA_NORM_LAYER || p.post == RA_NORM_LAYER, deep = p.post != RA_NORM_NONE && p.dy;
+    const bool deep = p.post != RA_NORM_NONE && p.dy;
     const int mine = (pieces - lane + 31) / 32;  // pieces of this lane
+    const float inv_first = 1.f / float(min(C, 256));
     auto get = [](const uint8_t* at) { return widen(*reinterpret_cast<const uint4*>(at)); };
     for (int k = 0, r = warp; r < n; ++k, r += WR) {
       cp_async_wait<0>();
-      float hm = 0.f, ym = 0.f;
-      if (layer) {
+      float hk = 0.f, yk = 0.f;
+      if constexpr (PRE || POST) {
         uint64_t a = zero, b = zero;
-        const uint8_t* at = slot;
-#pragma unroll 4
-        for (int i = 0; i < mine; ++i, at += 512) {
-          add_up(a, get(at));
-          add_up(b, get(at + row_bytes));
+        if (mine > 0) {
+          if constexpr (PRE) add_up(a, get(slot));
+          if constexpr (POST) add_up(b, get(slot + row_bytes));
         }
         const float2 m = warp_sums(a, b);
-        if (p.pre == RA_NORM_LAYER) hm = m.x * inv_c;
-        if (p.post == RA_NORM_LAYER) ym = m.y * inv_c;
+        hk = m.x * inv_first, yk = m.y * inv_first;
       }
-      // With h and y less their means, e = dx mul, g = gate: the squares, sum e, e h;
-      // and what sum f and f y come from, f = g dH, dH = dh' + r (e - m(e) - x^ m(e x^)).
-      uint64_t hh = zero, yy = zero, e0 = zero, eh = zero, dg = zero, eg = zero, hg = zero, dgy = zero, egy = zero,
-               hgy = zero, gy = zero;
-      const Vec neg_h = all(-hm), neg_y = all(-ym);
+      // With h and y less hk and yk, e = dx mul, g = gate: the sums of h, y, their
+      // squares, e and e h; and what sum f and f y come from, f = g dH,
+      // dH = dh' + r (e - m(e) - x^ m(e x^)).
+      uint64_t h0 = zero, y0 = zero, hh = zero, yy = zero, e0 = zero, eh = zero, dg = zero, eg = zero, hg = zero,
+               dgy = zero, egy = zero, hgy = zero, gy = zero;
+      const Vec neg_h = all(-hk), neg_y = all(-yk);
       const uint8_t *at = slot, *mul_at = mul_sh + 16 * lane, *gate_at = gate_sh + 16 * lane;
       auto vec = [](const uint8_t* m) -> Vec {
         const ulonglong2 a = *reinterpret_cast<const ulonglong2*>(m), b = *reinterpret_cast<const ulonglong2*>(m + 512);
@@ -624,37 +623,60 @@ __global__ void __launch_bounds__(THREADS, 1) residual_norm_grad_kernel(const __
       };
 #pragma unroll 2
       for (int i = 0; i < mine; ++i, at += 512, mul_at += 1024, gate_at += 1024) {
-        const Vec h = get(at) + neg_h, y = get(at + row_bytes) + neg_y, e = get(at + 2 * row_bytes) * vec(mul_at);
+        Vec h = get(at), y = get(at + row_bytes);
+        const Vec e = get(at + 2 * row_bytes) * vec(mul_at);
+        if constexpr (PRE) {
+          h = h + neg_h;
+          add_up(h0, h);
+          add_up(e0, e);
+        }
+        if constexpr (POST) {
+          y = y + neg_y;
+          add_up(y0, y);
+        }
         dot_up(hh, h, h);
         dot_up(yy, y, y);
-        add_up(e0, e);
         dot_up(eh, e, h);
         if (deep) {
           const Vec g = vec(gate_at), d = get(at + 3 * row_bytes), w = g * y;
-          dot_up(dg, d, g);
-          dot_up(eg, e, g);
-          dot_up(hg, h, g);
           dot_up(dgy, d, w);
           dot_up(egy, e, w);
           dot_up(hgy, h, w);
-          add_up(gy, w);
+          if constexpr (PRE || POST) add_up(gy, w);
+          if constexpr (POST) {
+            dot_up(dg, d, g);
+            dot_up(eg, e, g);
+            dot_up(hg, h, g);
+          }
         }
       }
-      const float2 sq = warp_sums(hh, yy), es = warp_sums(e0, eh);
+      float2 sq = warp_sums(hh, yy), es = warp_sums(e0, eh), m = make_float2(0.f, 0.f);
+      if constexpr (PRE || POST) {  // what is left to the means, and the sums around them
+        m = warp_sums(h0, y0);
+        m.x *= inv_c, m.y *= inv_c;
+        es.y = fmaf(-m.x, es.x, es.y);
+      }
+      const float var_h = fmaxf(fmaf(sq.x, inv_c, -m.x * m.x), 0.f), var_y = fmaxf(fmaf(sq.y, inv_c, -m.y * m.y), 0.f);
       RowNumbers v = {0.f, 1.f, 0.f, 0.f, 0.f, 1.f, 0.f, 0.f};
       if (p.pre != RA_NORM_NONE) {
-        v.h_mean = -hm, v.h_r = rsqrtf(fmaf(sq.x, inv_c, p.eps));
-        if (p.pre == RA_NORM_LAYER) v.e0 = -es.x * inv_c;
+        v.h_mean = -(hk + m.x), v.h_r = rsqrtf(var_h + p.eps);
+        if constexpr (PRE) v.e0 = -es.x * inv_c;
         v.e1 = -es.y * v.h_r * inv_c;
       }
       if (p.post != RA_NORM_NONE) {
-        v.y_mean = -ym, v.y_r = rsqrtf(fmaf(sq.y, inv_c, p.eps));
+        v.y_mean = -(yk + m.y), v.y_r = rsqrtf(var_y + p.eps);
         if (deep) {
-          const float2 d = warp_sums(dg, dgy), e = warp_sums(eg, egy), h = warp_sums(hg, hgy), g = warp_sums(gy, zero);
-          const float f0 = fmaf(v.h_r, fmaf(v.h_r * v.e1, h.x, fmaf(v.e0, *gate_sum, e.x)), d.x);
-          const float f1 = fmaf(v.h_r, fmaf(v.h_r * v.e1, h.y, fmaf(v.e0, g.x, e.y)), d.y);
-          if (p.post == RA_NORM_LAYER) v.f0 = -f0 * inv_c;
-          v.f1 = -f1 * v.y_r * inv_c;
+          float2 w = warp_sums(dgy, egy), x = warp_sums(hgy, gy);  // sums of d, e; h, 1 times g y
+          if constexpr (POST) {
+            const float2 d = warp_sums(dg, eg);
+            const float all_g = *gate_sum, all_hg = warp_sums(hg, zero).x;  // h still less hk only
+            const float f0 = fmaf(v.h_r, fmaf(v.h_r * v.e1, fmaf(-m.x, all_g, all_hg), fmaf(v.e0, all_g, d.y)), d.x);
+            v.f0 = -f0 * inv_c;
+            w.x = fmaf(-m.y, d.x, w.x), w.y = fmaf(-m.y, d.y, w.y);
+            x.x = fmaf(-m.y, all_hg, x.x), x.y = fmaf(-m.y, all_g, x.y);
+          }
+          if constexpr (PRE) x.x = fmaf(-m.x, x.y, x.x);
+          v.f1 = -fmaf(v.h_r, fmaf(v.h_r * v.e1, x.x, fmaf(v.e0, x.y, w.y)), w.x) * v.y_r * inv_c;
         }
       }
       if (lane == 0) numbers[warp] = v;
@@ -874,6 +896,12 @@ Fwd pick_fwd(const Shape& s) {
     default: return nullptr;
   }
 }
+using Grad = void (*)(GradParams);
+template <int THREADS>
+Grad pick_grad(bool pre, bool post) {
+  return pre ? (post ? residual_norm_grad_kernel<THREADS, true, true> : residual_norm_grad_kernel<THREADS, true, false>)
+             : (post ? residual_norm_grad_kernel<THREADS, false, true> : residual_norm_grad_kernel<THREADS, false, false>);
+}
 // CTAs that share a sample's rows: as many as make the fewest rounds of rows.
 int grad_parts(int B, int rows, int sms) {
   int best = 1;
@@ -1063,8 +1091,9 @@ extern "C" ra_status refadapt_residual_norm_backward(const ra_resnorm_grad_args*
   p.parts = a->rows > 0 ? grad_parts(a->B, a->rows, num_sms()) : 0;
   if (a->rows > 0) {
     const int threads = 32 * (sh.row_warps + sh.groups * sh.group_warps);
-    const ra_status r = launch(who, threads <= GRAD_THREADS ? residual_norm_grad_kernel<GRAD_THREADS>
-                                                            : residual_norm_grad_kernel<GRAD_THREADS_WIDE>,
+    const bool pre = a->pre == RA_NORM_LAYER, post = a->post == RA_NORM_LAYER;
+    const ra_status r = launch(who, threads <= GRAD_THREADS ? pick_grad<GRAD_THREADS>(pre, post)
+                                                            : pick_grad<GRAD_THREADS_WIDE>(pre, post),
                                p, dim3(unsigned(a->B * p.parts)), threads, sh.smem, st);
     if (r != RA_OK) return r;
   }
