@@ -27,6 +27,7 @@
 #include <cuda_runtime.h>
 
 #include <cstring>
+#include <type_traits>
 
 #include "api_common.h"
 #include "row_walk.cuh"
@@ -470,23 +471,31 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) residual_norm_kernel(const __g
 }
 
 // ------------------------------------------------------------------ backward
-// A CTA takes a run of a sample's rows. A row warp has a row at a time: it copies
-// h, y, dx and dh' into its slot in shared memory and reduces what the whole row
-// gives, in two passes over the slot: the means, then everything else. Then a group of column warps (eight columns
-// a thread) takes the row from the slot: with the row's eight numbers known, dh, dy
-// and the columns' sums need no further reduction, and S0, S1, S2 stay in the
-// threads' registers. Against groups that hold a row and reduce it across warps (8192
-// rows of 2560: 77 us, waiting on shuffles and barriers in 10 warps), a row's
-// reductions are one warp's, and rows overlap.
+// A CTA takes a run of a sample's rows. A row warp has a row at a time: it copies h, y,
+// dx and dh' into its slot in shared memory (bulk copies) and reduces what the whole
+// row gives, in one pass over the slot. Then a group of column warps (eight columns a
+// thread) takes the row from the slot: with the row's eight numbers known, dh, dy and
+// the columns' sums need no further reduction, and S0, S1, S2 stay in the threads'
+// registers.
+// Sums are taken around K, the mean of the row's first eight values, and moved to the
+// mean at the end: (mean - K)^2 is at most C / 8 times the variance, whatever the
+// values, so the difference keeps the variance to (C / 8 + 1) of the sum's own
+// roundings; a pass over the slot for the mean is saved.
+// 8192 rows of 2560, two kinds of norms with weights, sums included: 50 us, 5.1 TB/s;
+// 32,768 rows 158 us, 6.4 TB/s, where a copy of the same bytes takes 151: the pipeline
+// of ten rows fills and drains once in a run of 54. (Slots filled by the row warps'
+// own 16-byte copies, means in a pass of their own: 57. Teams of two or three warps a
+// row and a warp of its own for the copies: 50.5, and 25 instead of 16 for rows of 256,
+// where that warp cannot start copies fast enough.)
 struct GradShape {
   int row_warps, groups, group_warps;  // warps that reduce rows; groups of column warps
   int smem;
   __host__ __device__ static int slot_bytes(int C) { return 4 * C * 2; }
   __host__ __device__ static int vec_bytes(int C) { return (C + 255) / 256 * 1024; }
-  // [mul, gate] [numbers of a slot] [ready, free of a slot] [sum of gate, abort flag] [slots]
+  // [mul, gate] [numbers of a slot] [full, ready, free of a slot] [sum of gate, abort flag] [slots]
   __host__ __device__ static int off_numbers(int C) { return 2 * vec_bytes(C); }
   __host__ __device__ int off_bars(int C) const { return off_numbers(C) + row_warps * 32; }
-  __host__ __device__ int off_slots(int C) const { return off_bars(C) + row_warps * 16 + 16; }
+  __host__ __device__ int off_slots(int C) const { return off_bars(C) + (row_warps * 24 + 8 + 15) / 16 * 16; }
 };
 constexpr int MAX_ROW_WARPS = 10;
 constexpr int GRAD_THREADS = 640, GRAD_THREADS_WIDE = 768;  // of a CTA at most: 96 and 80 registers a thread
@@ -516,11 +525,28 @@ __device__ __forceinline__ float2 warp_sums(uint64_t a, uint64_t b) {
   return threadIdx.x & 1 ? make_float2(w, v) : make_float2(v, w);
 }
 
-// What a row's columns need of it: -mean and 1 / deviation of h and y, and the
-// negated means that the norms' gradients take off.
+// What a row's columns need of it: 1 / deviation r and - mean r of h and y, and the
+// negated means that the norms' gradients take off. (h r - mean r is off by 2^-24
+// |mean| r, far below the rounding of h itself to bf16.)
 struct alignas(16) RowNumbers {
-  float h_mean, h_r, e0, e1, y_mean, y_r, f0, f1;
+  float h_r, h_b, e0, e1, y_r, y_b, f0, f1;
 };
+
+// N sums over the warp at once: lane l gets that of v[l % N].
+template <int N>
+__device__ __forceinline__ float warp_sums(float (&v)[N]) {
+  int o = 1;
+#pragma unroll
+  for (int n = N / 2; n > 0; n /= 2, o *= 2) {
+    const bool up = threadIdx.x & o;
+#pragma unroll
+    for (int i = 0; i < n; ++i)
+      v[i] = (up ? v[2 * i + 1] : v[2 * i]) + __shfl_xor_sync(0xffffffffu, up ? v[2 * i] : v[2 * i + 1], o);
+  }
+#pragma unroll
+  for (; o < 32; o *= 2) v[0] += __shfl_xor_sync(0xffffffffu, v[0], o);
+  return v[0];
+}
 
 template <int THREADS, bool PRE, bool POST>
 __global__ void __launch_bounds__(THREADS, 1) residual_norm_grad_kernel(const __grid_constant__ GradParams p) {
@@ -529,49 +555,45 @@ __global__ void __launch_bounds__(THREADS, 1) residual_norm_grad_kernel(const __
   const int C = p.C, pieces = C >> 3, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, WR = p.row_warps;
   uint8_t *const mul_sh = smem, *const gate_sh = smem + GradShape::vec_bytes(C);
   RowNumbers* numbers = reinterpret_cast<RowNumbers*>(smem + GradShape::off_numbers(C));
-  uint64_t* ready = reinterpret_cast<uint64_t*>(smem + shape.off_bars(C));
-  uint64_t* free_ = ready + WR;
-  volatile float* gate_sum = reinterpret_cast<volatile float*>(free_ + WR);
-  volatile int* abort_flag = reinterpret_cast<volatile int*>(free_ + WR) + 1;
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem + shape.off_bars(C));
+  uint64_t *ready = full + WR, *free_ = full + 2 * WR;
+  volatile float* gate_sum = reinterpret_cast<volatile float*>(full + 3 * WR);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(full + 3 * WR) + 1;
   uint8_t* const slots = smem + shape.off_slots(C);
   const int row_bytes = 2 * C, slot_bytes = GradShape::slot_bytes(C);
-  pdl_launch();
-  if (threadIdx.x == 0) {
-    for (int i = 0; i < WR; ++i) {
-      mbar_init(ready + i, 1);
-      mbar_init(free_ + i, p.group_warps);
-    }
-    *abort_flag = 0;
-    fence_mbar_init();
-  }
-  pdl_wait();
   const int s = int(blockIdx.x) / p.parts, part = int(blockIdx.x) - s * p.parts;
   const int lo = int(int64_t(p.rows) * part / p.parts), n = int(int64_t(p.rows) * (part + 1) / p.parts) - lo;
   const bool has_y = p.y != nullptr;
-  // Tensor q of a row; one that was not given is zeros in every slot.
-  auto row_of = [&](int q, int r) -> const __nv_bfloat16* {
-    const __nv_bfloat16* t = q == 0 ? p.h : q == 1 ? p.y : q == 2 ? p.dx : p.dh_out;
-    const int64_t ss = q == 0 ? p.h_ss : q == 1 ? p.y_ss : q == 2 ? p.dx_ss : p.dho_ss;
-    const int64_t sr = q == 0 ? p.h_sr : q == 1 ? p.y_sr : q == 2 ? p.dx_sr : p.dho_sr;
-    return t ? t + s * ss + int64_t(lo + r) * sr : nullptr;
+  pdl_launch();
+  const int given = 1 + (has_y ? 1 : 0) + (p.dx ? 1 : 0) + (p.dh_out ? 1 : 0);
+  auto load = [&](int r) {  // by one lane of a row warp
+    mbar_arrive_expect_tx(full + warp, uint32_t(row_bytes * given));
+    auto copy = [&](int q, const __nv_bfloat16* t, int64_t ss, int64_t sr) {
+      if (t) bulk_load(slots + warp * slot_bytes + q * row_bytes, t + s * ss + int64_t(lo + r) * sr, row_bytes, full + warp);
+    };
+    copy(0, p.h, p.h_ss, p.h_sr);
+    copy(1, p.y, p.y_ss, p.y_sr);
+    copy(2, p.dx, p.dx_ss, p.dx_sr);
+    copy(3, p.dh_out, p.dho_ss, p.dho_sr);
   };
-  auto load = [&](int r) {  // a lane copies the pieces that it reads
-    uint8_t* to = slots + warp * slot_bytes + 16 * lane;
-#pragma unroll
-    for (int q = 0; q < 4; ++q, to += row_bytes) {
-      const __nv_bfloat16* src = row_of(q, r);
-      if (!src) continue;
-      for (int i = lane, o = 0; i < pieces; i += 32, o += 512) cp_async16(to + o, src + 8 * lane + (o >> 1));
-    }
-    cp_async_commit();
-  };
-  if (warp < WR) {
+  if (threadIdx.x == 0) *abort_flag = 0;
+  if (warp < WR && lane == 0) {
+    mbar_init(full + warp, 1);
+    mbar_init(ready + warp, 1);
+    mbar_init(free_ + warp, p.group_warps);
+    fence_mbar_init();
+    fence_proxy_async_smem();
+    pdl_wait();
     if (warp < n) load(warp);
-    for (int q = 1; q < 4; ++q)
-      if (!row_of(q, 0))
-        for (int i = lane; i < pieces; i += 32)
-          *reinterpret_cast<uint4*>(slots + warp * slot_bytes + q * row_bytes + 16 * i) = make_uint4(0, 0, 0, 0);
   }
+  pdl_wait();
+  if (given < 4)  // what was not given is zeros in every slot
+    for (int i = threadIdx.x; i < WR * pieces; i += blockDim.x) {
+      uint4* to = reinterpret_cast<uint4*>(slots + i / pieces * slot_bytes) + i % pieces;
+      if (!has_y) to[pieces] = make_uint4(0, 0, 0, 0);
+      if (!p.dx) to[2 * pieces] = make_uint4(0, 0, 0, 0);
+      if (!p.dh_out) to[3 * pieces] = make_uint4(0, 0, 0, 0);
+    }
   for (int i = threadIdx.x; i < pieces; i += blockDim.x) {
     const int c = 8 * i;
     shared_put(mul_sh, i, (vec8(p.scale ? p.scale + s * p.mod_ss : nullptr, c, 0.f) + all(1.f)) * vec8(p.pre_w, c, 1.f));
@@ -579,44 +601,44 @@ __global__ void __launch_bounds__(THREADS, 1) residual_norm_grad_kernel(const __
   }
   __syncthreads();
   const uint64_t zero = both(0.f);
-  if (warp == 0) {
-    uint64_t g = zero;
-    for (int i = lane; i < pieces; i += 32) add_up(g, shared_get(gate_sh, i));
-    const float2 sum = warp_sums(g, zero);
-    if (lane == 0) *gate_sum = sum.x;
+  if constexpr (POST) {
+    if (warp == 0) {
+      uint64_t g = zero;
+      for (int i = lane; i < pieces; i += 32) add_up(g, shared_get(gate_sh, i));
+      const float2 sum = warp_sums(g, zero);
+      if (lane == 0) *gate_sum = sum.x;
+    }
+    __syncthreads();
   }
-  __syncthreads();
   const WaitCtl ctl{abort_flag, p.err_word, p.budget_ns};
   const float inv_c = 1.f / float(C);
   Vec s0 = all(0.f), s1 = s0, s2 = s0;  // of a column thread
-  const int group = warp < WR ? -1 : (warp - WR) / p.group_warps;
-  const int piece = 32 * ((warp - WR) - group * p.group_warps) + lane;  // of a column thread
+  const int col_warp = warp - WR, group = col_warp < 0 ? -1 : col_warp / p.group_warps;
+  const int piece = 32 * (col_warp - group * p.group_warps) + lane;  // of a column thread
   if (warp < WR) {
     // ---------------------------------------------------------------- rows
-    const uint8_t* const slot = slots + warp * slot_bytes + 16 * lane;
+    const uint8_t* const row = slots + warp * slot_bytes;
     const bool deep = p.post != RA_NORM_NONE && p.dy;
     const int mine = (pieces - lane + 31) / 32;  // pieces of this lane
-    const float inv_first = 1.f / float(min(C, 256));
     auto get = [](const uint8_t* at) { return widen(*reinterpret_cast<const uint4*>(at)); };
+    auto first8 = [&](const uint8_t* at) {  // the mean of a row's first eight values
+      uint64_t v = zero;
+      add_up(v, get(at));
+      return sum2(v) * 0.125f;
+    };
     for (int k = 0, r = warp; r < n; ++k, r += WR) {
-      cp_async_wait<0>();
-      float hk = 0.f, yk = 0.f;
-      if constexpr (PRE || POST) {
-        uint64_t a = zero, b = zero;
-        if (mine > 0) {
-          if constexpr (PRE) add_up(a, get(slot));
-          if constexpr (POST) add_up(b, get(slot + row_bytes));
-        }
-        const float2 m = warp_sums(a, b);
-        hk = m.x * inv_first, yk = m.y * inv_first;
+      if (!__all_sync(0xffffffffu, mbar_wait(full + warp, uint32_t(k & 1), ctl))) {
+        mbar_wait_drain(full + warp, uint32_t(k & 1), p.budget_ns);  // the copies land before the CTA goes on
+        break;
       }
-      // With h and y less hk and yk, e = dx mul, g = gate: the sums of h, y, their
+      const float hk = PRE ? first8(row) : 0.f, yk = POST ? first8(row + row_bytes) : 0.f;
+      // With h and y less K, e = dx mul, g = gate: the sums of h, y, their
       // squares, e and e h; and what sum f and f y come from, f = g dH,
       // dH = dh' + r (e - m(e) - x^ m(e x^)).
       uint64_t h0 = zero, y0 = zero, hh = zero, yy = zero, e0 = zero, eh = zero, dg = zero, eg = zero, hg = zero,
                dgy = zero, egy = zero, hgy = zero, gy = zero;
       const Vec neg_h = all(-hk), neg_y = all(-yk);
-      const uint8_t *at = slot, *mul_at = mul_sh + 16 * lane, *gate_at = gate_sh + 16 * lane;
+      const uint8_t *at = row + 16 * lane, *mul_at = mul_sh + 16 * lane, *gate_at = gate_sh + 16 * lane;
       auto vec = [](const uint8_t* m) -> Vec {
         const ulonglong2 a = *reinterpret_cast<const ulonglong2*>(m), b = *reinterpret_cast<const ulonglong2*>(m + 512);
         return {{a.x, a.y, b.x, b.y}};
@@ -650,44 +672,49 @@ __global__ void __launch_bounds__(THREADS, 1) residual_norm_grad_kernel(const __
           }
         }
       }
-      float2 sq = warp_sums(hh, yy), es = warp_sums(e0, eh), m = make_float2(0.f, 0.f);
-      if constexpr (PRE || POST) {  // what is left to the means, and the sums around them
-        m = warp_sums(h0, y0);
-        m.x *= inv_c, m.y *= inv_c;
-        es.y = fmaf(-m.x, es.x, es.y);
-      }
-      const float var_h = fmaxf(fmaf(sq.x, inv_c, -m.x * m.x), 0.f), var_y = fmaxf(fmaf(sq.y, inv_c, -m.y * m.y), 0.f);
-      RowNumbers v = {0.f, 1.f, 0.f, 0.f, 0.f, 1.f, 0.f, 0.f};
+      constexpr int N = PRE || POST ? 16 : 8;
+      float sums[N] = {sum2(hh), sum2(yy), sum2(eh), sum2(dgy), sum2(egy), sum2(hgy)};
+      if constexpr (PRE) sums[6] = sum2(h0), sums[7] = sum2(e0);
+      if constexpr (PRE || POST) sums[8] = sum2(gy);
+      if constexpr (POST) sums[9] = sum2(y0), sums[10] = sum2(dg), sums[11] = sum2(eg), sums[12] = sum2(hg);
+      const float one = warp_sums(sums);
+      float all_of[N];
+#pragma unroll
+      for (int i = 0; i < N; ++i) all_of[i] = __shfl_sync(0xffffffffu, one, i);
+      float mh = 0.f, my = 0.f, sum_eh = all_of[2];  // what is left to the means; sums around them
+      if constexpr (PRE) mh = all_of[6] * inv_c, sum_eh = fmaf(-mh, all_of[7], sum_eh);
+      if constexpr (POST) my = all_of[9] * inv_c;
+      RowNumbers v = {1.f, 0.f, 0.f, 0.f, 1.f, 0.f, 0.f, 0.f};
       if (p.pre != RA_NORM_NONE) {
-        v.h_mean = -(hk + m.x), v.h_r = rsqrtf(var_h + p.eps);
-        if constexpr (PRE) v.e0 = -es.x * inv_c;
-        v.e1 = -es.y * v.h_r * inv_c;
+        v.h_r = rsqrtf(fmaxf(fmaf(all_of[0], inv_c, -mh * mh), 0.f) + p.eps), v.h_b = -(hk + mh) * v.h_r;
+        if constexpr (PRE) v.e0 = -all_of[7] * inv_c;
+        v.e1 = -sum_eh * v.h_r * inv_c;
       }
       if (p.post != RA_NORM_NONE) {
-        v.y_mean = -(yk + m.y), v.y_r = rsqrtf(var_y + p.eps);
+        v.y_r = rsqrtf(fmaxf(fmaf(all_of[1], inv_c, -my * my), 0.f) + p.eps), v.y_b = -(yk + my) * v.y_r;
         if (deep) {
-          float2 w = warp_sums(dgy, egy), x = warp_sums(hgy, gy);  // sums of d, e; h, 1 times g y
+          float d_gy = all_of[3], e_gy = all_of[4], h_gy = all_of[5], s_gy = 0.f;
+          if constexpr (PRE || POST) s_gy = all_of[8];
           if constexpr (POST) {
-            const float2 d = warp_sums(dg, eg);
-            const float all_g = *gate_sum, all_hg = warp_sums(hg, zero).x;  // h still less hk only
-            const float f0 = fmaf(v.h_r, fmaf(v.h_r * v.e1, fmaf(-m.x, all_g, all_hg), fmaf(v.e0, all_g, d.y)), d.x);
+            const float g = *gate_sum, d_g = all_of[10], e_g = all_of[11], h_g = all_of[12];  // h still less hk only
+            const float f0 = fmaf(v.h_r, fmaf(v.h_r * v.e1, fmaf(-mh, g, h_g), fmaf(v.e0, g, e_g)), d_g);
             v.f0 = -f0 * inv_c;
-            w.x = fmaf(-m.y, d.x, w.x), w.y = fmaf(-m.y, d.y, w.y);
-            x.x = fmaf(-m.y, all_hg, x.x), x.y = fmaf(-m.y, all_g, x.y);
+            d_gy = fmaf(-my, d_g, d_gy), e_gy = fmaf(-my, e_g, e_gy);
+            h_gy = fmaf(-my, h_g, h_gy), s_gy = fmaf(-my, g, s_gy);
           }
-          if constexpr (PRE) x.x = fmaf(-m.x, x.y, x.x);
-          v.f1 = -fmaf(v.h_r, fmaf(v.h_r * v.e1, x.x, fmaf(v.e0, x.y, w.y)), w.x) * v.y_r * inv_c;
+          h_gy = fmaf(-mh, s_gy, h_gy);
+          v.f1 = -fmaf(v.h_r, fmaf(v.h_r * v.e1, h_gy, fmaf(v.e0, s_gy, e_gy)), d_gy) * v.y_r * inv_c;
         }
       }
-      if (lane == 0) numbers[warp] = v;
-      __syncwarp();
-      if (lane == 0) mbar_arrive(ready + warp);
+      if (lane == 0) {
+        numbers[warp] = v;
+        mbar_arrive(ready + warp);
+      }
       if (r + WR < n) {
         if (!__all_sync(0xffffffffu, mbar_wait(free_ + warp, uint32_t(k & 1), ctl))) break;
-        load(r + WR);
+        if (lane == 0) load(r + WR);
       }
     }
-    cp_async_wait<0>();
   } else if (group < p.groups) {
     // ---------------------------------------------------------------- columns
     const bool in = piece < pieces;
@@ -696,54 +723,62 @@ __global__ void __launch_bounds__(THREADS, 1) residual_norm_grad_kernel(const __
       return t ? t + s * ss + (lo + group) * sr + 8 * piece : nullptr;
     };
     __nv_bfloat16 *dh = place(p.dh, p.dh_ss, p.dh_sr), *dy = place(p.dy, p.dy_ss, p.dy_sr);
-    int w = 0, k = 0;  // row r is the k-th of row warp w
-    for (w = group; w >= WR; w -= WR) ++k;
+    int w = group, k = 0;  // row r is the k-th of slot w
     for (int r = group; r < n; r += p.groups) {
+      for (; w >= WR; w -= WR) ++k;
       if (!__all_sync(0xffffffffu, mbar_wait(ready + w, uint32_t(k & 1), ctl))) break;
       if (in) {
         const RowNumbers v = numbers[w];
         const uint8_t* at = slots + w * slot_bytes + 16 * piece;
         auto get = [&](int q) { return widen(*reinterpret_cast<const uint4*>(at + q * row_bytes)); };
-        const Vec x = (get(0) + all(v.h_mean)) * all(v.h_r), d = get(2);
+        auto norm = [](auto centred, const Vec& h, float r, float b) {
+          if constexpr (decltype(centred)::value)
+            return fma(h, all(r), all(b));
+          else
+            return h * all(r);
+        };
+        const Vec x = norm(std::bool_constant<PRE>(), get(0), v.h_r, v.h_b), d = get(2);
         s0 = s0 + d;
         s1 = fma(d, x, s1);
         // dH = dh' + r (e - m(e) - x^ m(e x^))
-        const Vec e = fma(d, mul, fma(x, all(v.e1), all(v.e0)));
+        const Vec e = fma(d, mul, norm(std::bool_constant<PRE>(), x, v.e1, v.e0));
         const Vec t = fma(e, all(v.h_r), get(3));
-        if (dh) *reinterpret_cast<uint4*>(dh) = narrow(t * all(p.alpha));
+        if (dh) *reinterpret_cast<uint4*>(dh) = narrow(p.alpha == 1.f ? t : t * all(p.alpha));
         if (has_y) {
-          const Vec y = (get(1) + all(v.y_mean)) * all(v.y_r);
+          const Vec y = norm(std::bool_constant<POST>(), get(1), v.y_r, v.y_b);
           s2 = fma(t, y, s2);
-          if (dy) *reinterpret_cast<uint4*>(dy) = narrow(fma(y, all(v.f1), fma(t, gate, all(v.f0))) * all(v.y_r));
+          if (dy) *reinterpret_cast<uint4*>(dy) = narrow(fma(t, gate, norm(std::bool_constant<POST>(), y, v.f1, v.f0)) * all(v.y_r));
         }
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(free_ + w);
       if (dh) dh += p.groups * p.dh_sr;
       if (dy) dy += p.groups * p.dy_sr;
-      for (w += p.groups; w >= WR; w -= WR) ++k;
+      w += p.groups;
     }
   }
   // The CTA's column sums: its groups' in order, through shared memory.
   __syncthreads();
   const bool gave_up = *abort_flag;
-  float* sums = reinterpret_cast<float*>(slots);  // [group][3][C]
+  float* out = p.partial + int64_t(blockIdx.x) * 3 * C;
+  float* sums = p.groups > 1 ? reinterpret_cast<float*>(slots) : out;  // [group][3][C]
   if (group >= 0 && group < p.groups && piece < pieces) {
     float* to = sums + group * 3 * C + 8 * piece;
-    auto put = [](float* dst, const Vec& v) {
-      reinterpret_cast<ulonglong2*>(dst)[0] = make_ulonglong2(v.p[0], v.p[1]);
-      reinterpret_cast<ulonglong2*>(dst)[1] = make_ulonglong2(v.p[2], v.p[3]);
+    auto put = [&](float* dst, const Vec& v) {
+      const Vec x = gave_up ? all(__int_as_float(0x7fffffff)) : v;
+      reinterpret_cast<ulonglong2*>(dst)[0] = make_ulonglong2(x.p[0], x.p[1]);
+      reinterpret_cast<ulonglong2*>(dst)[1] = make_ulonglong2(x.p[2], x.p[3]);
     };
     put(to, s0);
     put(to + C, s1);
     put(to + 2 * C, s2);
   }
+  if (p.groups == 1) return;
   __syncthreads();
-  float* out = p.partial + int64_t(blockIdx.x) * 3 * C;
   for (int c = threadIdx.x; c < 3 * C; c += blockDim.x) {
     float v = 0.f;
     for (int g = 0; g < p.groups; ++g) v += sums[g * 3 * C + c];
-    out[c] = gave_up ? __int_as_float(0x7fffffff) : v;
+    out[c] = v;
   }
 }
 
@@ -869,13 +904,14 @@ Shape make_shape(int C, int max_threads, int vectors, int stage_rows) {
   return s;
 }
 Shape fwd_shape(int C) { return make_shape(C, FWD_THREADS, 3, 4); }
-// As many row warps as there is room for slots, at most ten; column groups of about
-// ten warps together.
+// About ten column warps, and as many row warps beside them as there is room for, a
+// multiple of the groups: with a slot's rows all its own, a group cannot run a phase
+// of its barrier ahead.
 GradShape grad_shape(int C) {
   GradShape s;
   s.group_warps = (C + 255) / 256;
   s.groups = s.group_warps >= 10 ? 1 : 10 / s.group_warps;
-  for (s.row_warps = MAX_ROW_WARPS;; --s.row_warps) {
+  for (s.row_warps = MAX_ROW_WARPS / s.groups * s.groups;; s.row_warps -= s.groups) {
     s.smem = s.off_slots(C) + s.row_warps * GradShape::slot_bytes(C);
     if (s.smem <= SMEM_MAX) break;  // four fit at C = 5120
   }
@@ -883,7 +919,7 @@ GradShape grad_shape(int C) {
   if (s.smem < sums) s.smem = sums;
   return s;
 }
-static_assert(2 * 20 * 1024 + 4 * MAX_C * 2 * 4 + 1024 <= SMEM_MAX, "four row warps fit");
+static_assert(2 * 20 * 1024 + 4 * MAX_C * 2 * 4 + 2048 <= SMEM_MAX, "four slots fit");
 static_assert(MAX_C <= 10 * 512 && MAX_PIECES == 2, "a group has at most ten warps");
 using Fwd = void (*)(Params);
 Fwd pick_fwd(const Shape& s) {
