@@ -328,6 +328,45 @@ struct Cursor {
   }
 };
 
+// Shares of few pieces that none of them crosses: [lo, hi) of CTA cta, or false where
+// that takes longer rounds (of `round` rows) than even shares do, by more than a
+// twelfth. A CTA that goes on into another sample has its vectors to fetch, and the
+// rest of the grid waits for it: 2 x (77 + 500) rows of 1280 8.3 us on even shares, 7.0
+// here; 2 x (256 + 4096) of 2560 36.9 and 35.3. (The whole warp.)
+constexpr int FEW_PIECES = 12;
+__device__ __forceinline__ bool piece_share(const Params& p, int total, int round, int& lo, int& hi) {
+  const int grid = int(gridDim.x), cta = int(blockIdx.x), lane = threadIdx.x & 31;
+  uint32_t on[3] = {};
+#pragma unroll
+  for (int g = 0; g < 3; ++g)
+    if (g < p.n_seg && p.seg[g].rows > 0) on[g] = __ballot_sync(0xffffffffu, lane < p.B && live(p, g, lane));
+  const int even = (total + grid - 1) / grid, rounds = (even + round - 1) / round;
+#pragma unroll 1
+  for (int k = 0; k < 3; ++k) {
+    if (k == 2 && rounds < 12) break;
+    const int most = k == 0 ? even : (rounds + k - 1) * round;
+    int used = 0, begin = 0;  // CTAs and rows before the segment
+    lo = hi = 0;
+    int part = 0, ctas = 0, n = 0;  // this CTA's part of its piece
+#pragma unroll
+    for (int g = 0; g < 3; ++g) {
+      if (on[g] == 0) continue;
+      const int rows = p.seg[g].rows, c = (rows + most - 1) / most, pieces = __popc(on[g]);
+      const int mine = int(uint32_t(cta - used) / uint32_t(c));  // cta < used: past all
+      if (cta >= used && mine < pieces) part = cta - used - mine * c, ctas = c, n = rows, lo = begin + mine * rows;
+      used += pieces * c, begin += pieces * rows;
+    }
+    if (used > grid) continue;
+    if (ctas > 0) {
+      const int share = n / ctas, more = n - share * ctas;
+      lo += share * part + min(part, more);
+      hi = lo + share + (part < more ? 1 : 0);
+    }
+    return true;
+  }
+  return false;
+}
+
 template <int V, int T>
 __global__ void __launch_bounds__(FWD_THREADS, 1) residual_norm_kernel(const __grid_constant__ Params p) {
   extern __shared__ __align__(16) uint8_t smem[];
@@ -344,8 +383,12 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) residual_norm_kernel(const __g
   pdl_launch();
   pdl_wait();
   const int total = live_rows(p);
-  const int share = total / int(gridDim.x), more = total - share * int(gridDim.x), cta = int(blockIdx.x);
-  const int lo = share * cta + min(cta, more), hi = lo + share + (cta < more ? 1 : 0);
+  int lo, hi;
+  if (total <= 2 * int(gridDim.x) || p.B * p.n_seg == 1 || p.B * p.n_seg > FEW_PIECES ||
+      !piece_share(p, total, 2 * p.groups, lo, hi)) {
+    const int share = total / int(gridDim.x), more = total - share * int(gridDim.x), cta = int(blockIdx.x);
+    lo = share * cta + min(cta, more), hi = lo + share + (cta < more ? 1 : 0);
+  }
   if (lo == hi) return;
   Cursor cur, ld;
   if (p.B > 4) cur.w.jump(p, lo);
