@@ -19,15 +19,20 @@
 // An operand whose K runs along its rows (Wd, Wg, Wu as B, the rows of every
 // operand of a weight's gradient) is read as it lies, MN-major: nothing is
 // transposed in memory.
-//   warp 0      TMA producer: per stage 128 of K of the CTA's 128 A rows and of
-//               its half of the B tile, two boxes each (128-byte swizzle; what
-//               lies past an edge is read as zeros).
+//   warp 0      TMA producer: per stage 128 of K (GRAD: 64) of the CTA's 128 A rows
+//               and of its half of the B tile, in boxes of 64 columns (128-byte
+//               swizzle; what lies past an edge is read as zeros).
 //   warp 1      TMEM allocator (two accumulators of 256 columns) and MMA issuer
 //               (rank 0's).
 //   warps 2..9  epilogue, two warps per TMEM lane quarter, while the next tile's
 //               MMAs fill the other accumulator.
-// A forward call of a few rows reads its weights once and little else, so it has a
-// kernel of its own (glu_rows_kernel).
+// Measured: 4352 rows, 2048 -> 8192: forward 175 us, 1.67 PFLOP/s, 84-87 % of the tensor
+// cores' measured rate (14.3 rounds of tiles take 15, and the clock sinks under the power
+// cap). Backward, 4333 rows, 557-574 us, 1.52-1.56 PFLOP/s: GRAD 115 us, where the MMAs
+// alone are 82 (its epilogue moves four F-wide tensors through the shared memory that
+// feeds the MMAs), STORE 445.
+// A forward call of up to 128 rows reads its weights once and little else and has
+// kernels of its own (glu_rows_kernel, glu_some_kernel).
 // Every mbarrier wait is bounded; on a timeout the CTA drains its own copies and
 // MMAs, frees TMEM, flags the error word and returns.
 #include <cuda.h>
@@ -695,18 +700,21 @@ __global__ void __launch_bounds__(THREADS, 1) glu_kernel(const __grid_constant__
 }
 
 // ------------------------------------------------------------------ few rows
-// Up to 16 rows per segment: bound by the weights' bytes (4 F C). On the tiles
-// above each CTA would wait for 128-row boxes of x that are nearly all zeros, and
-// all CTAs for the few lines that are not (1 row, C = 2048, F = 5504: 24 us; here
-// 10.2 us, 4.4 TB/s of weights; 8 rows 10.3, 16 rows 14.5, where the tiles take 16
-// and keep that up to 256 rows). A CTA takes eight features, its warps share K, and
-// a weight goes from memory into the registers of the mma.sync that uses it
-// (m16n8k16: the rows of A are the features' gate rows and their up rows, the
-// columns of B eight rows of x), so g and w of a feature and a row end in one
-// thread. K is permuted alike in A and B, so that a lane's operands are 16
-// contiguous bytes. Deeper rounds of loads, two features' groups a CTA, a prefetch
-// into L2 ahead of the previous kernel's end and four warps measured no better.
-constexpr int ROWS_MAX = 16;
+// Up to 16 rows per segment of small weights: bound by the weights' bytes (4 F C) and
+// the latency of reading them once (1024 -> 2736, 11 MB: 4.7 us up to 8 rows, 6.1 at 16;
+// the kernel for some rows below 7.6, the tiles above 10). A CTA takes eight features,
+// its warps share K, and a weight goes from memory into the registers of the mma.sync
+// that uses it (m16n8k16: the rows of A are the features' gate rows and their up rows,
+// the columns of B eight rows of x), so g and w of a feature and a row end in one
+// thread. K is permuted alike in A and B, so that a lane's operands are 16 contiguous
+// bytes. Deeper rounds of loads, two features' groups a CTA, a prefetch into L2 ahead of
+// the previous kernel's end and four warps measured no better.
+// Larger weights go to the kernel for some rows. 8 rows: 45 MB 12.6 us here, 12.3 there,
+// 67 MB 14.4 and 14.5, 180 MB 34.8 and 31.1; 16 rows: 45 MB 14.6 and 12.3, 180 MB 38.5
+// and 31.3.
+bool few_rows(int rows, int64_t weight_bytes) {
+  return rows <= 8 ? weight_bytes <= (int64_t(64) << 20) : rows <= 16 && weight_bytes <= (int64_t(24) << 20);
+}
 constexpr int ROWS_WARPS = 8;
 
 struct RowsSeg {
@@ -807,6 +815,149 @@ __global__ void __launch_bounds__(32 * ROWS_WARPS) glu_rows_kernel(const __grid_
     for (int z = 0; z < 3; ++z)
       if (sg.out[z].ptr)
         sg.out[z].ptr[s * sg.out[z].ss + (row - s * sg.rows) * sg.out[z].sr + f] = __float2bfloat16_rn(res[k][z]);
+  }
+}
+
+// ------------------------------------------------------------------ some rows
+// Up to 128 rows, bound by the weights' bytes too. The weights are the MMA's M (up to 64
+// features' gate rows, then their up rows) and x its N, so a CTA stages no more of x
+// than there are rows, and the features are divided evenly over the SMs. Cold weights,
+// 2048 -> 5504: 17 rows 12.4 us (3.6 TB/s), 128 rows 15.3 (tiles of 256 rows: 19.5 and
+// 16.2); 4096 -> 11,008: 31.9 (5.6 TB/s) and 38.3 (43.4 and 44.6).
+//   warp 0      TMA producer: stages of 64 of K.
+//   warp 1      TMEM allocator, MMA issuer.
+//   warps 2..5  drain the accumulator (a lane is a feature) into shared memory,
+//               where all warps meet g and w of a feature and a row.
+constexpr int SOME_MAX = 128;  // columns; x then has as many bytes a stage as the weights
+constexpr int SOME_THREADS = 192, SOME_RING = 16;
+constexpr int SOME_SLACK = 16384 + 1024;  // the MMA reads 128 rows of A, of which 2 f are its own; alignment
+struct alignas(64) SomeSeg {
+  CUtensorMap x, w[2];
+  Rows out[3];
+  int32_t B, rows, nb, N, gated;  // nb: columns of the accumulator that a sample has
+};
+struct SomeParams {
+  SomeSeg seg[3];
+  int32_t F, f, stages, ring, stage_bytes, tmem_cols;
+  const int32_t* mode;
+  int32_t* err_word;
+  uint64_t budget_ns;
+};
+
+template <int ACT>
+__global__ void __launch_bounds__(SOME_THREADS) glu_some_kernel(const __grid_constant__ SomeParams p) {
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ uint64_t full[SOME_RING], empty[SOME_RING], done, drain;
+  __shared__ uint32_t tmem_slot;
+  __shared__ int abort_word;
+  volatile int* abort_flag = &abort_word;
+  uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const SomeSeg& sg = p.seg[blockIdx.y];
+  const int f0 = int(blockIdx.x) * p.f, a_box = 2 * p.f * 128;
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < p.ring; ++i) {
+      mbar_init(full + i, 1);
+      mbar_init(empty + i, 1);
+    }
+    mbar_init(&done, 1);
+    mbar_init(&drain, 1);
+    *abort_flag = 0;
+    fence_mbar_init();
+  }
+  if (warp == 1) tmem_alloc(&tmem_slot, p.tmem_cols);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = tmem_slot;
+  const WaitCtl ctl{abort_flag, p.err_word, p.budget_ns};
+  pdl_launch();
+  if (warp != 0) pdl_wait();
+  if (warp == 0) {
+    if (lane == 0) {
+      tma_prefetch_desc(&sg.w[0]);
+      tma_prefetch_desc(&sg.w[1]);
+      tma_prefetch_desc(&sg.x);
+      pdl_wait();
+      const uint32_t bytes = uint32_t(a_box + sg.B * sg.nb * 128);
+      int it = 0, st = 0, phase = 1;
+      for (; it < p.stages; ++it) {
+        if (it >= p.ring && !mbar_wait(empty + st, uint32_t(phase), ctl)) break;
+        uint8_t* to = smem + st * p.stage_bytes;
+        mbar_arrive_expect_tx(full + st, bytes);
+        tma_load_4d(to, &sg.w[0], full + st, 64 * it, f0, 0, 0);
+        tma_load_4d(to + p.f * 128, &sg.w[1], full + st, 64 * it, f0, 0, 0);
+        to += a_box;
+        for (int s = 0; s < sg.B; ++s, to += sg.nb * 128) tma_load_4d(to, &sg.x, full + st, 64 * it, 0, 0, s);
+        if (++st == p.ring) st = 0, phase ^= 1;
+      }
+      if (*abort_flag)
+        for (st = 0; st < p.ring && st < it; ++st)
+          mbar_wait_drain(full + st, uint32_t((it - 1 - st) / p.ring & 1), p.budget_ns);
+    }
+  } else if (warp == 1) {
+    if (lane == 0) {
+      const uint32_t idesc = idesc_bf16_f32(128, sg.N, 0, 0), s0 = smem_u32(smem);
+      bool ok = true;
+      int it = 0, st = 0, phase = 0;
+      for (; it < p.stages; ++it) {
+        if (!(ok = mbar_wait(full + st, uint32_t(phase), ctl))) break;
+        tc_fence_after();
+        const uint32_t a = s0 + uint32_t(st * p.stage_bytes), x = a + a_box;
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk)
+          umma_ss(tmem, sdesc_sw128(a + kk * 32, 16, 1024), sdesc_sw128(x + kk * 32, 16, 1024), idesc, it > 0 || kk > 0);
+        umma_commit(empty + st);
+        if (++st == p.ring) st = 0, phase ^= 1;
+      }
+      if (ok) {
+        umma_commit(&done);
+      } else if (it > 0) {
+        umma_commit(&drain);
+        mbar_wait_drain(&drain, 0, p.budget_ns);
+      }
+    }
+  } else if (__all_sync(0xffffffffu, mbar_wait(&done, 0, ctl))) {
+    tc_fence_after();
+    // every load has landed and been used: the accumulator goes where the stages were, [column][feature row]
+    const int quarter = warp & 3, row = 32 * quarter + lane;
+    float* to = reinterpret_cast<float*>(smem) + row;
+    if (32 * quarter < 2 * p.f)
+      for (int c = 0; c < sg.N; c += 32) {
+        uint32_t v[32];
+        tmem_ld32(tmem + (uint32_t(32 * quarter) << 16) + uint32_t(c), v);
+        tmem_ld_wait_for(v);
+        if (row < 2 * p.f)
+#pragma unroll
+          for (int i = 0; i < 32; ++i)
+            if (c + i < sg.N) to[(c + i) * 2 * p.f] = __uint_as_float(v[i]);
+      }
+    tc_fence_before();
+  }
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc(tmem, p.tmem_cols);
+  }
+  if (*abort_flag) return;
+  const int vecs = p.f / 8;
+  for (int i = threadIdx.x; i < sg.B * sg.nb * vecs; i += SOME_THREADS) {
+    const int n = i / vecs, j = 8 * (i - n * vecs), s = n / sg.nb, r = n - s * sg.nb;
+    if (r >= sg.rows || f0 + j >= p.F || (sg.gated && p.mode[s] == RA_MODE_REUSE)) continue;
+    const float* src = reinterpret_cast<const float*>(smem) + n * 2 * p.f + j;
+    uint32_t o[3][4];
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      const ulonglong2 g = *reinterpret_cast<const ulonglong2*>(src + 4 * q);
+      const ulonglong2 w = *reinterpret_cast<const ulonglong2*>(src + p.f + 4 * q);
+      o[0][2 * q] = f2_bf16(f2_mul(act2<ACT>(g.x, nullptr), w.x)), o[0][2 * q + 1] = f2_bf16(f2_mul(act2<ACT>(g.y, nullptr), w.y));
+      o[1][2 * q] = f2_bf16(g.x), o[1][2 * q + 1] = f2_bf16(g.y);
+      o[2][2 * q] = f2_bf16(w.x), o[2][2 * q + 1] = f2_bf16(w.y);
+    }
+#pragma unroll
+    for (int z = 0; z < 3; ++z)
+      if (sg.out[z].ptr)
+        *reinterpret_cast<uint4*>(row_ptr(sg.out[z], s, r, f0 + j)) = make_uint4(o[z][0], o[z][1], o[z][2], o[z][3]);
   }
 }
 
@@ -988,6 +1139,39 @@ Plan make_plan(const Products& pr, int sms) {
   return best;
 }
 
+// Does glu_some_kernel take the call? Its shape: features a CTA so that they fill the
+// SMs once or a whole number of times, stages as the shared memory has room for, or
+// half of it where there is more than one round: then a CTA has its first loads in
+// flight while the one before it ends.
+constexpr int SOME_SMEM = 225 * 1024, SOME_SMEM_HALF = 112 * 1024;
+bool some_rows(const ra_glu_args& a, const Params& p, const RowTensor (&x)[3], SomeParams& sp) {
+  std::memset(&sp, 0, sizeof(sp));
+  int most = 0;
+  for (int j = 0; j < p.n_jobs; ++j) {
+    const Job& job = p.job[j];
+    SomeSeg& d = sp.seg[j];
+    const int64_t nb = (int64_t(job.rows) + 7) / 8 * 8, n = (nb * x[j].B + 15) / 16 * 16;
+    if (n > SOME_MAX) return false;
+    d.B = job.samples, d.rows = job.rows, d.nb = int(nb), d.N = int(n), d.gated = job.gated;
+    for (int z = 0; z < 3; ++z) d.out[z] = job.out[z];
+    most = d.N > most ? d.N : most;
+  }
+  const int sms = num_sms();
+  const int64_t slots = sms / p.n_jobs > 0 ? sms / p.n_jobs : 1, rounds = div_up(a.F, 64 * slots);
+  sp.f = int(div_up(div_up(a.F, rounds * slots), 8) * 8);
+  sp.F = a.F;
+  sp.stages = int(div_up(a.C, 64));
+  sp.stage_bytes = 128 * (2 * sp.f + most);
+  sp.ring = ((rounds > 1 ? SOME_SMEM_HALF : SOME_SMEM) - SOME_SLACK) / sp.stage_bytes;
+  if (sp.ring > SOME_RING) sp.ring = SOME_RING;
+  if (sp.ring > sp.stages) sp.ring = sp.stages;
+  // the fp32 tile takes the place of the stages
+  while (sp.ring * sp.stage_bytes < most * 2 * sp.f * 4) ++sp.ring;
+  sp.tmem_cols = 32;
+  while (sp.tmem_cols < most) sp.tmem_cols *= 2;
+  return true;
+}
+
 size_t partial_bytes(const Shape& s, int parts) {
   return parts > 1 ? size_t(parts) * size_t(s.samples) * size_t(s.M) * size_t(s.N) * 4 : 0;
 }
@@ -1075,7 +1259,7 @@ extern "C" ra_status refadapt_glu(const ra_glu_args* a, void* stream) {
   int most = 0;
   for (int g = 0; g < a->n_seg; ++g)
     if (int64_t(a->B) * a->seg[g].rows > most) most = a->B * a->seg[g].rows;
-  if (most <= ROWS_MAX) {
+  if (few_rows(most, int64_t(4) * a->F * a->C)) {
     RowsParams r;
     std::memset(&r, 0, sizeof(r));
     r.B = a->B, r.F = a->F, r.C = a->C, r.mode = a->mode;
@@ -1107,6 +1291,38 @@ extern "C" ra_status refadapt_glu(const ra_glu_args* a, void* stream) {
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
     const cudaError_t e = cudaLaunchKernelEx(&cfg, fn, r);
+    if (e != cudaSuccess) {
+      set_error("%s: launch failed: %s", who, cudaGetErrorString(e));
+      cudaGetLastError();
+      return RA_ECUDA;
+    }
+    return launch_status(who);
+  }
+  SomeParams sp;
+  if (some_rows(*a, p, x, sp)) {
+    sp.mode = a->mode, sp.err_word = a->err_word, sp.budget_ns = p.budget_ns;
+    for (int g = 0, j = 0; g < a->n_seg; ++g) {
+      const ra_glu_seg& s = a->seg[g];
+      if (s.rows == 0) continue;
+      SomeSeg& d = sp.seg[j];
+      const RowTensor wg{s.w_gate, 0, a->C, 1, a->F, a->C}, wu{s.w_up, 0, a->C, 1, a->F, a->C};
+      if (!encode(&d.x, x[j], d.nb) || !encode(&d.w[0], wg, sp.f) || !encode(&d.w[1], wu, sp.f)) return RA_EINVAL;
+      ++j;
+    }
+    const bool gelu = a->act == RA_ACT_GELU;
+    void (*fn)(SomeParams) = gelu ? glu_some_kernel<RA_ACT_GELU> : glu_some_kernel<RA_ACT_SILU>;
+    const ra_status as = ensure_dynamic_smem(reinterpret_cast<const void*>(fn), SOME_SMEM, who);
+    if (as != RA_OK) return as;
+    note_launch("some rows, %d features", sp.f);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(unsigned(div_up(a->F, sp.f)), unsigned(p.n_jobs));
+    cfg.blockDim = dim3(SOME_THREADS);
+    cfg.dynamicSmemBytes = size_t(sp.ring) * sp.stage_bytes + SOME_SLACK;
+    cfg.stream = static_cast<cudaStream_t>(stream);
+    cudaLaunchAttribute attr = pdl_attribute();
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, fn, sp);
     if (e != cudaSuccess) {
       set_error("%s: launch failed: %s", who, cudaGetErrorString(e));
       cudaGetLastError();
