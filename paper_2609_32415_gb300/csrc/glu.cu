@@ -31,14 +31,16 @@
 // cap). Backward, 4333 rows, 557-574 us, 1.52-1.56 PFLOP/s: GRAD 115 us, where the MMAs
 // alone are 82 (its epilogue moves four F-wide tensors through the shared memory that
 // feeds the MMAs), STORE 445.
-// A forward call of up to 128 rows reads its weights once and little else and has
-// kernels of its own (glu_rows_kernel, glu_some_kernel).
+// Calls of few rows read (backward: and write) the weights once and little else, and
+// have kernels of their own: forward up to 128 rows glu_rows_kernel and
+// glu_some_kernel, du and dx of few rows glu_cols_kernel.
 // Every mbarrier wait is bounded; on a timeout the CTA drains its own copies and
 // MMAs, frees TMEM, flags the error word and returns.
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
+#include <atomic>
 #include <cmath>
 #include <cstring>
 
@@ -961,6 +963,167 @@ __global__ void __launch_bounds__(SOME_THREADS) glu_some_kernel(const __grid_con
   }
 }
 
+// ------------------------------------------------------------------ backward, some rows
+// du (with dg and dw) and dx of few rows: too few tiles of 256 rows for the SMs, and a
+// long K. Here 128 columns of a weight are the MMA's M (MN-major, as they
+// lie), up to 128 rows its N, and a cluster of up to eight CTAs shares K: each sums its
+// part in TMEM and leaves it in its shared memory, then takes its share of the rows from
+// all of them, in order. So nothing goes through memory, and no second kernel joins.
+// Warps as in glu_some_kernel.
+constexpr int COLS_M = 128, COLS_BK = 64, COLS_N = 128;
+constexpr int COLS_W_BYTES = COLS_M * COLS_BK * 2, COLS_RING = 6;
+constexpr int COLS_SMEM = 112 * 1024;  // two CTAs an SM
+struct alignas(64) ColsParams {
+  CUtensorMap a[2], w[2];  // STORE: two operand pairs, one after the other in K
+  Rows out[2], pre[2];     // GRAD: dg, dw; g, w. STORE: the result
+  int32_t rows, cols, blocks, col_tiles, N, spans, span_stages, ring, tmem_cols;  // blocks of N rows of a sample
+  int32_t* err_word;
+  uint64_t budget_ns;
+};
+
+__device__ __forceinline__ float4 ld_cluster_f4(uint32_t addr) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr));
+  return v;
+}
+
+template <int KIND, int ACT>
+__global__ void __launch_bounds__(SOME_THREADS) glu_cols_kernel(const __grid_constant__ ColsParams p) {
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ uint64_t full[COLS_RING], empty[COLS_RING], done, drain;
+  __shared__ uint32_t tmem_slot;
+  __shared__ int abort_word;
+  volatile int* abort_flag = &abort_word;
+  uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int cs = int(cluster_size()), rank = int(cluster_rank()), unit = int(blockIdx.x) / cs;
+  const int tile = unit / p.blocks, r0 = (unit - tile * p.blocks) * p.N, s = tile / p.col_tiles;
+  const int c0 = (tile - s * p.col_tiles) * COLS_M;
+  const int stages = p.spans * p.span_stages, k0 = stages * rank / cs, k1 = stages * (rank + 1) / cs;
+  const int stage_bytes = COLS_W_BYTES + p.N * 128;
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < p.ring; ++i) {
+      mbar_init(full + i, 1);
+      mbar_init(empty + i, 1);
+    }
+    mbar_init(&done, 1);
+    mbar_init(&drain, 1);
+    *abort_flag = 0;
+    fence_mbar_init();
+  }
+  if (warp == 1) tmem_alloc(&tmem_slot, p.tmem_cols);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = tmem_slot;
+  const WaitCtl ctl{abort_flag, p.err_word, p.budget_ns};
+  pdl_launch();
+  if (warp != 0) pdl_wait();
+  if (warp == 0) {
+    if (lane == 0) {
+      tma_prefetch_desc(&p.w[0]);
+      tma_prefetch_desc(&p.a[0]);
+      pdl_wait();
+      int it = 0, st = 0, phase = 1, span = k0 / p.span_stages, k = (k0 - span * p.span_stages) * COLS_BK;
+      for (; it < k1 - k0; ++it) {
+        if (it >= p.ring && !mbar_wait(empty + st, uint32_t(phase), ctl)) break;
+        uint8_t* to = smem + st * stage_bytes;
+        mbar_arrive_expect_tx(full + st, uint32_t(stage_bytes));  // past an edge: zeros
+        tma_load_4d(to, &p.w[span], full + st, c0, k, 0, 0);
+        tma_load_4d(to + COLS_W_BYTES / 2, &p.w[span], full + st, c0 + 64, k, 0, 0);
+        tma_load_4d(to + COLS_W_BYTES, &p.a[span], full + st, k, r0, 0, s);
+        k += COLS_BK;
+        if (k >= p.span_stages * COLS_BK) k = 0, ++span;
+        if (++st == p.ring) st = 0, phase ^= 1;
+      }
+      if (*abort_flag)
+        for (st = 0; st < p.ring && st < it; ++st)
+          mbar_wait_drain(full + st, uint32_t((it - 1 - st) / p.ring & 1), p.budget_ns);
+    }
+  } else if (warp == 1) {
+    if (lane == 0) {
+      const uint32_t idesc = idesc_bf16_f32(COLS_M, p.N, 1, 0), s0 = smem_u32(smem);
+      bool ok = true;
+      int it = 0, st = 0, phase = 0;
+      for (; it < k1 - k0; ++it) {
+        if (!(ok = mbar_wait(full + st, uint32_t(phase), ctl))) break;
+        tc_fence_after();
+        const uint32_t w = s0 + uint32_t(st * stage_bytes), a = w + COLS_W_BYTES;
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk)  // 16 rows of 128 bytes; 32 bytes of a row
+          umma_ss(tmem, sdesc_sw128(w + kk * 2048, COLS_W_BYTES / 2, 1024), sdesc_sw128(a + kk * 32, 16, 1024), idesc,
+                  it > 0 || kk > 0);
+        umma_commit(empty + st);
+        if (++st == p.ring) st = 0, phase ^= 1;
+      }
+      if (ok) {
+        umma_commit(&done);
+      } else if (it > 0) {
+        umma_commit(&drain);
+        mbar_wait_drain(&drain, 0, p.budget_ns);
+      }
+    }
+  } else if (__all_sync(0xffffffffu, mbar_wait(&done, 0, ctl))) {
+    tc_fence_after();
+    // every load has landed and been used: the sums go where the stages were, [row][column]
+    const int quarter = warp & 3;
+    float* to = reinterpret_cast<float*>(smem) + 32 * quarter + lane;
+    for (int c = 0; c < p.N; c += 32) {
+      uint32_t v[32];
+      tmem_ld32(tmem + (uint32_t(32 * quarter) << 16) + uint32_t(c), v);
+      tmem_ld_wait_for(v);
+#pragma unroll
+      for (int i = 0; i < 32; ++i)
+        if (c + i < p.N) to[(c + i) * COLS_M] = __uint_as_float(v[i]);
+    }
+    tc_fence_before();
+  }
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc(tmem, p.tmem_cols);
+  }
+  __syncwarp();
+  cluster_sync_all();
+  const int n0 = p.N * rank / cs, n1 = p.N * (rank + 1) / cs;
+  const uint32_t mine = smem_u32(smem);
+  for (int i = n0 * (COLS_M / 8) + int(threadIdx.x); i < n1 * (COLS_M / 8); i += SOME_THREADS) {
+    const int n = i / (COLS_M / 8), j = 8 * (i % (COLS_M / 8)), r = r0 + n, c = c0 + j;
+    if (r >= p.rows || c >= p.cols) continue;
+    uint4 g, w;
+    if constexpr (KIND == GRAD) {
+      g = *reinterpret_cast<const uint4*>(row_ptr(p.pre[0], s, r, c));
+      w = *reinterpret_cast<const uint4*>(row_ptr(p.pre[1], s, r, c));
+    }
+    float4 lo = make_float4(0.f, 0.f, 0.f, 0.f), hi = lo;
+    for (int q = 0; q < cs; ++q) {
+      const uint32_t at = mapa_shared(mine + uint32_t(n * COLS_M + j) * 4u, uint32_t(q));
+      const float4 x = ld_cluster_f4(at), y = ld_cluster_f4(at + 16);
+      lo.x += x.x, lo.y += x.y, lo.z += x.z, lo.w += x.w;
+      hi.x += y.x, hi.y += y.y, hi.z += y.z, hi.w += y.w;
+    }
+    const uint64_t v[4] = {f2_pack(lo.x, lo.y), f2_pack(lo.z, lo.w), f2_pack(hi.x, hi.y), f2_pack(hi.z, hi.w)};
+    if constexpr (KIND == GRAD) {
+      uint32_t* gp = reinterpret_cast<uint32_t*>(&g);
+      uint32_t* wp = reinterpret_cast<uint32_t*>(&w);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        uint64_t da;
+        const uint64_t a = act2<ACT>(bf2_unpack(gp[q]), &da);
+        gp[q] = f2_bf16(f2_mul(f2_mul(v[q], bf2_unpack(wp[q])), da));
+        wp[q] = f2_bf16(f2_mul(v[q], a));
+      }
+      *reinterpret_cast<uint4*>(row_ptr(p.out[0], s, r, c)) = g;
+      *reinterpret_cast<uint4*>(row_ptr(p.out[1], s, r, c)) = w;
+    } else {
+      *reinterpret_cast<uint4*>(row_ptr(p.out[0], s, r, c)) =
+          make_uint4(f2_bf16(v[0]), f2_bf16(v[1]), f2_bf16(v[2]), f2_bf16(v[3]));
+    }
+  }
+  __syncwarp();
+  cluster_sync_all();  // the others have read this CTA's sums
+}
+
 // Adds up the parts of the jobs that were cut, in order.
 struct JoinJob {
   const float* partial;
@@ -1108,17 +1271,17 @@ struct Plan {
 constexpr int MAX_PARTS = 16;
 // The cheapest by the time of the pair that ends last. More than two rounds of
 // tiles are not cut (a part costs a round trip of its fp32 sums).
-Plan make_plan(const Products& pr, int sms) {
+Plan make_plan(const Products& pr, bool dx, int sms) {
   const int64_t pairs = sms / 2 > 0 ? sms / 2 : 1;
   Plan best{256, 1, 1, 0};
   double best_us = 1e30;
   for (int bn = 256; bn >= 128; bn -= 64)
     for (int px = 1; px <= MAX_PARTS; px += px < 4 ? 1 : 4) {
-      if (px > 1 && (pr.x.stages < 2 * px || pr.x.tiles(bn) > 2 * pairs)) break;
+      if (px > 1 && (!dx || pr.x.stages < 2 * px || pr.x.tiles(bn) > 2 * pairs)) break;
       for (int pw = 1; pw <= MAX_PARTS; pw += pw < 4 ? 1 : 4) {
         const int64_t tiles_w = pr.w[0].tiles(bn) * 2 + pr.w[2].tiles(bn);
         if (pw > 1 && (pr.w[0].stages < 2 * pw || tiles_w > 2 * pairs)) break;
-        const int64_t nx = pr.x.tiles(bn) * px, nw = tiles_w * pw, rest = nx % pairs;
+        const int64_t nx = dx ? pr.x.tiles(bn) * px : 0, nw = tiles_w * pw, rest = nx % pairs;
         const double a = round_us(bn, double(pr.x.stages) / px), b = round_us(bn, double(pr.w[0].stages) / pw);
         double bytes = px > 1 ? 8.0 * px * double(pr.x.samples * pr.x.M * pr.x.N) : 0.0;
         if (pw > 1)
@@ -1170,6 +1333,86 @@ bool some_rows(const ra_glu_args& a, const Params& p, const RowTensor (&x)[3], S
   sp.tmem_cols = 32;
   while (sp.tmem_cols < most) sp.tmem_cols *= 2;
   return true;
+}
+
+// Rows up to which glu_cols_kernel takes du, and dx too: beside the weights' gradients,
+// which are many short tiles, dx by tiles costs little more than they do. All
+// gradients: 4 rows of 1024 -> 2736 34.8 us by tiles alone, 27.7; 30 of 2000 -> 3504
+// 44.9, 38.9 (with dx here 44.9); 64 of 1024 -> 4096 35.2, 34.5; 128 rows even. dx
+// alone: 30 rows 33.6 and 20.0, 128 of 2048 -> 5504 51.6 and 39.9, 200 of 1536 -> 4096
+// 36.9 and 33.9, 400 of 512 -> 8192 36.0 and 42.2.
+constexpr int COLS_ROWS_DU = 64, COLS_ROWS_DX = 16, COLS_ROWS_ALONE = 256;
+int cols_box(int rows) {  // rows of a block, as launch_cols has them
+  const int64_t blocks = div_up(rows, COLS_N);
+  return int(div_up(div_up(rows, blocks), 16) * 16);
+}
+// Clusters of c CTAs of glu_cols_kernel that the GPU holds at once, asked once a size:
+// they lie within GPCs, which are not multiples of every size (of eight: 36, though
+// 304 CTAs fit). One cluster more than fits doubles the kernel's time.
+int resident_clusters(int c) {
+  static std::atomic<int> held[9];
+  int n = held[c].load(std::memory_order_relaxed);
+  if (n == 0) {
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = unsigned(c);
+    attr.val.clusterDim.y = 1;
+    attr.val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(unsigned(c));
+    cfg.blockDim = dim3(SOME_THREADS);
+    cfg.dynamicSmemBytes = COLS_SMEM;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    if (cudaOccupancyMaxActiveClusters(&n, glu_cols_kernel<STORE, 0>, &cfg) != cudaSuccess || n < 1) {
+      cudaGetLastError();
+      n = 1;
+    }
+    held[c].store(n, std::memory_order_relaxed);
+  }
+  return n;
+}
+template <int KIND>
+ra_status launch_cols(const char* who, void (*fn)(ColsParams), ColsParams& p, int samples, cudaStream_t st) {
+  const int sms = num_sms();
+  p.blocks = int(div_up(p.rows, COLS_N));
+  p.N = cols_box(p.rows);
+  p.col_tiles = int(div_up(p.cols, COLS_M));
+  const int stages = p.spans * p.span_stages;
+  const int64_t units = int64_t(samples) * p.blocks * p.col_tiles;
+  const int stage_bytes = COLS_W_BYTES + p.N * 128;
+  p.ring = (COLS_SMEM - 1024) / stage_bytes < COLS_RING ? (COLS_SMEM - 1024) / stage_bytes : COLS_RING;
+  p.tmem_cols = 32;
+  while (p.tmem_cols < p.N) p.tmem_cols *= 2;
+  const ra_status as = ensure_dynamic_smem(reinterpret_cast<const void*>(fn), COLS_SMEM, who);
+  if (as != RA_OK) return as;
+  int cs = 1;
+  double best = 1e30;
+  for (int c = 1; c <= 8 && c <= stages; ++c) {
+    const double us = 2.0 * double(div_up(units, resident_clusters(c))) +
+                      0.2 * double(div_up(units * c, sms) * div_up(stages, c)) + 0.15 * c;
+    if (us < best) best = us, cs = c;
+  }
+  cudaLaunchAttribute attr[2];
+  attr[0] = pdl_attribute();
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = unsigned(cs);
+  attr[1].val.clusterDim.y = 1;
+  attr[1].val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(unsigned(units * cs));
+  cfg.blockDim = dim3(SOME_THREADS);
+  cfg.dynamicSmemBytes = size_t(p.ring) * stage_bytes + 1024;
+  cfg.stream = st;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, fn, p);
+  if (e != cudaSuccess) {
+    set_error("%s: launch failed: %s", who, cudaGetErrorString(e));
+    cudaGetLastError();
+    return RA_ECUDA;
+  }
+  return launch_status(who);
 }
 
 size_t partial_bytes(const Shape& s, int parts) {
@@ -1365,10 +1608,12 @@ extern "C" size_t refadapt_glu_backward_workspace_size(int32_t B, int32_t rows, 
   if (rows > 0)
     for (int flat = 0; flat < (B > 1 ? 4 : 1); ++flat) {
       const Products pr(B, rows, C, F, O, flat & 1, flat & 2);
-      const Plan plan = make_plan(pr, sms);
-      size_t b = partial_bytes(pr.x, plan.parts_x);
-      for (const Shape& w : pr.w) b += partial_bytes(w, plan.parts_w);
-      most = b > most ? b : most;
+      for (int dx = 0; dx < 2; ++dx) {
+        const Plan plan = make_plan(pr, dx, sms);
+        size_t b = partial_bytes(pr.x, plan.parts_x);
+        for (const Shape& w : pr.w) b += partial_bytes(w, plan.parts_w);
+        most = b > most ? b : most;
+      }
     }
   return size_t(2) * size_t(B) * size_t(rows) * size_t(F) * 2 + most + 16;
 }
@@ -1463,7 +1708,28 @@ extern "C" ra_status refadapt_glu_backward(const ra_glu_grad_args* a, void* stre
     return Rows{static_cast<__nv_bfloat16*>(const_cast<void*>(t.ptr)), t.ss, t.sr};
   };
   const int64_t pairs = sms / 2 > 0 ? sms / 2 : 1;
-  if (dgw) {
+  auto cols_params = [&](const RowTensor& t, int cols, int spans, int k) {
+    ColsParams c;
+    std::memset(&c, 0, sizeof(c));
+    c.rows = t.n, c.cols = cols, c.spans = spans;
+    c.span_stages = int(div_up(k, COLS_BK));
+    c.err_word = a->err_word, c.budget_ns = p.budget_ns;
+    return c;
+  };
+  const bool alone = !(a->dw_gate || a->dw_up || a->dw_down);
+  const bool du_cols = all <= (alone ? COLS_ROWS_ALONE : COLS_ROWS_DU), dx_cols = a->dx && du_cols && (alone || all <= COLS_ROWS_DX);
+  if (dgw && du_cols) {
+    const bool flat = joins(dy) && joins(g) && joins(w);
+    auto one = [&](const RowTensor& t) { return flat ? flatten(t) : t; };
+    const RowTensor src = one(dy);
+    ColsParams c = cols_params(src, a->F, 1, a->O);
+    c.out[0] = rows_of(one(dgt)), c.out[1] = rows_of(one(dwt));
+    c.pre[0] = rows_of(one(g)), c.pre[1] = rows_of(one(w));
+    if (!encode(&c.a[0], src, cols_box(src.n)) || !encode(&c.w[0], w_down, COLS_BK)) return RA_EINVAL;
+    const ra_status r = launch_cols<GRAD>(who, a->act == RA_ACT_GELU ? glu_cols_kernel<GRAD, RA_ACT_GELU> : glu_cols_kernel<GRAD, RA_ACT_SILU>,
+                                          c, src.B, st);
+    if (r != RA_OK) return r;
+  } else if (dgw) {
     const bool flat = joins(dy) && joins(g) && joins(w);
     const RowTensor src = flat ? flatten(dy) : dy;
     Job& job = p.job[0];
@@ -1493,10 +1759,24 @@ extern "C" ra_status refadapt_glu_backward(const ra_glu_grad_args* a, void* stre
     if (r != RA_OK) return r;
   }
   // dx and the weights' gradients, in one launch
+  if (dx_cols) {
+    const bool flat = joins(dx);
+    auto one = [&](const RowTensor& t) { return flat ? flatten(t) : t; };
+    const RowTensor src = one(dgt);
+    ColsParams c = cols_params(src, a->C, 2, a->F);
+    c.out[0] = rows_of(one(dx));
+    if (!encode(&c.a[0], src, cols_box(src.n)) || !encode(&c.a[1], one(dwt), cols_box(src.n)) ||
+        !encode(&c.w[0], w_gate, COLS_BK) || !encode(&c.w[1], w_up, COLS_BK))
+      return RA_EINVAL;
+    const ra_status r = launch_cols<STORE>(who, glu_cols_kernel<STORE, 0>, c, src.B, st);
+    if (r != RA_OK) return r;
+  }
+  const bool dx_tiles = a->dx && !dx_cols;
+  if (!dx_tiles && !a->dw_gate && !a->dw_up && !a->dw_down) return RA_OK;
   const bool flat_x = a->B == 1 || !a->dx || joins(dx);
   const bool flat_w = a->B == 1 || ((!(a->dw_gate || a->dw_up) || joins(x)) && (!a->dw_down || (joins(dy) && joins(hid))));
   const Products pr(a->B, a->rows, a->C, a->F, a->O, flat_x, flat_w);
-  const Plan plan = make_plan(pr, sms);
+  const Plan plan = make_plan(pr, dx_tiles, sms);
   std::memset(p.job, 0, sizeof(p.job));
   p.n_jobs = 0;
   p.bn = plan.bn;
@@ -1523,7 +1803,7 @@ extern "C" ra_status refadapt_glu_backward(const ra_glu_grad_args* a, void* stre
     }
     return job;
   };
-  if (a->dx) {
+  if (dx_tiles) {
     Job& job = add(pr.x, plan.parts_x, rows_of(dx));
     one_span<STORE>(job, a->F);
     job.spans = 2;

@@ -1,12 +1,12 @@
 """The gated feed-forward's forward pass at the row counts and widths around its three forms:
 rows that stream the weights (up to 16 and small weights), rows as the product's columns (up to
-128), tiles (more). Tolerances as in test_gpu_glu.py."""
+128), tiles (more); and the backward pass around its two forms. Tolerances as in test_gpu_glu.py."""
 import numpy as np
 import pytest
 import torch
 
 from _helpers import f64
-from test_gpu_glu import check_forward, seg
+from test_gpu_glu import call, check_forward, check_grads, grads, seg
 
 pytestmark = pytest.mark.gpu
 
@@ -77,5 +77,41 @@ def test_the_same_bits_on_every_call(cuda_ok):
     first = {k: s[k].clone() for k in ("out", "pre_gate", "pre_up")}
     for _ in range(20):
         run([s], F, C, 0)
+        for k, v in first.items():
+            assert torch.equal(s[k], v), k
+
+
+EVERY = ("dx", "dw_gate", "dw_up", "dw_down")
+
+
+@pytest.mark.parametrize("B,n,C,F,O,strided", [
+    (1, 3, 2048, 72, 64, False), (1, 16, 520, 2736, 264, True), (2, 8, 72, 1000, 2056, False), (1, 17, 520, 1000, 1032, False),
+    (4, 16, 264, 648, 136, True), (1, 64, 1024, 1368, 200, False), (1, 65, 1024, 1368, 200, False)])
+@pytest.mark.parametrize("want", [EVERY, ("dx",), ("dx", "dw_up")])
+def test_backward(cuda_ok, B, n, C, F, O, strided, want):
+    run_backward(B, n, C, F, O, strided, want, n % 2)
+
+
+@pytest.mark.parametrize("B,n,C,F,O,strided", [
+    (1, 129, 1000, 2000, 1096, False), (1, 256, 264, 4104, 520, True), (3, 85, 136, 712, 264, True),
+    (1, 257, 264, 712, 128, False), (200, 1, 128, 200, 72, True)])
+def test_input_gradient_alone(cuda_ok, B, n, C, F, O, strided):
+    run_backward(B, n, C, F, O, strided, ("dx",), n % 2)
+
+
+def run_backward(B, n, C, F, O, strided, want, act):
+    from paper_2609_32415_gb300 import api
+    g = torch.Generator().manual_seed(n + C + F + O)
+    s = grads(B, n, C, F, O, g, act, strided)
+    ws = torch.full((api.refadapt_glu_backward_workspace_size(B, n, C, F, O) // 2,), float("nan"), dtype=torch.bfloat16,
+                    device="cuda")
+    err = torch.zeros(1, dtype=torch.int32, device="cuda")
+    drop = [k for k in EVERY if k not in want]
+    call(s, act, ws, err, drop)
+    api.refadapt_check_error(err)
+    check_grads(s, act, drop)
+    first = {k: s[k].clone() for k in want}
+    for _ in range(3):
+        call(s, act, ws, err, drop)
         for k, v in first.items():
             assert torch.equal(s[k], v), k
