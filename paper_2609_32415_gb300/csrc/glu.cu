@@ -1346,10 +1346,10 @@ int cols_box(int rows) {  // rows of a block, as launch_cols has them
   const int64_t blocks = div_up(rows, COLS_N);
   return int(div_up(div_up(rows, blocks), 16) * 16);
 }
-// Clusters of c CTAs of glu_cols_kernel that the GPU holds at once, asked once a size:
-// they lie within GPCs, which are not multiples of every size (of eight: 36, though
+// Clusters of c CTAs of glu_cols_kernel that the GPU holds at once, asked once a size
+// (of any of its forms: they differ in neither shared memory nor threads): they lie within GPCs, which are not multiples of every size (of eight: 36, though
 // 304 CTAs fit). One cluster more than fits doubles the kernel's time.
-int resident_clusters(int c) {
+int resident_clusters(void (*fn)(ColsParams), int c) {
   static std::atomic<int> held[9];
   int n = held[c].load(std::memory_order_relaxed);
   if (n == 0) {
@@ -1364,7 +1364,7 @@ int resident_clusters(int c) {
     cfg.dynamicSmemBytes = COLS_SMEM;
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
-    if (cudaOccupancyMaxActiveClusters(&n, glu_cols_kernel<STORE, 0>, &cfg) != cudaSuccess || n < 1) {
+    if (cudaOccupancyMaxActiveClusters(&n, fn, &cfg) != cudaSuccess || n < 1) {
       cudaGetLastError();
       n = 1;
     }
@@ -1389,7 +1389,7 @@ ra_status launch_cols(const char* who, void (*fn)(ColsParams), ColsParams& p, in
   int cs = 1;
   double best = 1e30;
   for (int c = 1; c <= 8 && c <= stages; ++c) {
-    const double us = 2.0 * double(div_up(units, resident_clusters(c))) +
+    const double us = 2.0 * double(div_up(units, resident_clusters(fn, c))) +
                       0.2 * double(div_up(units * c, sms) * div_up(stages, c)) + 0.15 * c;
     if (us < best) best = us, cs = c;
   }
