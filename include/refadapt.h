@@ -665,7 +665,7 @@ ra_status refadapt_glu(const ra_glu_args* args, void* stream);
  *   dx = dg Wg + dw Wu,  dw_gate = dg^T x,  dw_up = dw^T x,  dw_down = dy^T hidden
  * dg and dw are formed in the epilogue of dy Wd from its fp32 sums (du is never
  * stored) and rounded to bf16 once, as operands of the products after them.
- * Three products' launches, and one more where a long sum is split.
+ * Two or three launches, and one more where a long sum is split.
  *  dy                  bf16 rows of O features; w_down bf16 [O][F].
  *  dx, dw_*            bf16, contiguous [F][C] and [O][F] for the weights; any
  *                      may be NULL (frozen weights), not all. hidden may be NULL

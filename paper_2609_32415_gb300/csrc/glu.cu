@@ -825,7 +825,10 @@ __global__ void __launch_bounds__(32 * ROWS_WARPS) glu_rows_kernel(const __grid_
 // features' gate rows, then their up rows) and x its N, so a CTA stages no more of x
 // than there are rows, and the features are divided evenly over the SMs. Cold weights,
 // 2048 -> 5504: 17 rows 12.4 us (3.6 TB/s), 128 rows 15.3 (tiles of 256 rows: 19.5 and
-// 16.2); 4096 -> 11,008: 31.9 (5.6 TB/s) and 38.3 (43.4 and 44.6).
+// 16.2); 4096 -> 11,008: 31.9 (5.6 TB/s) and 38.3 (43.4 and 44.6). Where few features
+// would leave SMs idle or a CTA few of its own, a cluster shares K and adds up as in
+// glu_cols_kernel: 17 rows of 2496 -> 1344 13.6 us without, 8.4; of 3264 -> 4160 17.2
+// and 14.0.
 //   warp 0      TMA producer: stages of 64 of K.
 //   warp 1      TMEM allocator, MMA issuer.
 //   warps 2..5  drain the accumulator (a lane is a feature) into shared memory,
@@ -840,11 +843,17 @@ struct alignas(64) SomeSeg {
 };
 struct SomeParams {
   SomeSeg seg[3];
-  int32_t F, f, stages, ring, stage_bytes, tmem_cols;
+  int32_t F, f, stages, cs, ring, stage_bytes, tmem_cols;
   const int32_t* mode;
   int32_t* err_word;
   uint64_t budget_ns;
 };
+
+__device__ __forceinline__ float4 ld_cluster_f4(uint32_t addr) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr));
+  return v;
+}
 
 template <int ACT>
 __global__ void __launch_bounds__(SOME_THREADS) glu_some_kernel(const __grid_constant__ SomeParams p) {
@@ -856,7 +865,8 @@ __global__ void __launch_bounds__(SOME_THREADS) glu_some_kernel(const __grid_con
   uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const SomeSeg& sg = p.seg[blockIdx.y];
-  const int f0 = int(blockIdx.x) * p.f, a_box = 2 * p.f * 128;
+  const int cs = p.cs, rank = cs > 1 ? int(cluster_rank()) : 0, f0 = int(blockIdx.x) / cs * p.f, a_box = 2 * p.f * 128;
+  const int k0 = p.stages * rank / cs, stages = p.stages * (rank + 1) / cs - k0;  // this CTA's part of K
   if (threadIdx.x == 0) {
     for (int i = 0; i < p.ring; ++i) {
       mbar_init(full + i, 1);
@@ -883,14 +893,14 @@ __global__ void __launch_bounds__(SOME_THREADS) glu_some_kernel(const __grid_con
       pdl_wait();
       const uint32_t bytes = uint32_t(a_box + sg.B * sg.nb * 128);
       int it = 0, st = 0, phase = 1;
-      for (; it < p.stages; ++it) {
+      for (; it < stages; ++it) {
         if (it >= p.ring && !mbar_wait(empty + st, uint32_t(phase), ctl)) break;
         uint8_t* to = smem + st * p.stage_bytes;
         mbar_arrive_expect_tx(full + st, bytes);
-        tma_load_4d(to, &sg.w[0], full + st, 64 * it, f0, 0, 0);
-        tma_load_4d(to + p.f * 128, &sg.w[1], full + st, 64 * it, f0, 0, 0);
+        tma_load_4d(to, &sg.w[0], full + st, 64 * (k0 + it), f0, 0, 0);
+        tma_load_4d(to + p.f * 128, &sg.w[1], full + st, 64 * (k0 + it), f0, 0, 0);
         to += a_box;
-        for (int s = 0; s < sg.B; ++s, to += sg.nb * 128) tma_load_4d(to, &sg.x, full + st, 64 * it, 0, 0, s);
+        for (int s = 0; s < sg.B; ++s, to += sg.nb * 128) tma_load_4d(to, &sg.x, full + st, 64 * (k0 + it), 0, 0, s);
         if (++st == p.ring) st = 0, phase ^= 1;
       }
       if (*abort_flag)
@@ -902,7 +912,7 @@ __global__ void __launch_bounds__(SOME_THREADS) glu_some_kernel(const __grid_con
       const uint32_t idesc = idesc_bf16_f32(128, sg.N, 0, 0), s0 = smem_u32(smem);
       bool ok = true;
       int it = 0, st = 0, phase = 0;
-      for (; it < p.stages; ++it) {
+      for (; it < stages; ++it) {
         if (!(ok = mbar_wait(full + st, uint32_t(phase), ctl))) break;
         tc_fence_after();
         const uint32_t a = s0 + uint32_t(st * p.stage_bytes), x = a + a_box;
@@ -941,25 +951,51 @@ __global__ void __launch_bounds__(SOME_THREADS) glu_some_kernel(const __grid_con
     tc_fence_after();
     tmem_dealloc(tmem, p.tmem_cols);
   }
-  if (*abort_flag) return;
-  const int vecs = p.f / 8;
-  for (int i = threadIdx.x; i < sg.B * sg.nb * vecs; i += SOME_THREADS) {
+  if (cs > 1) {
+    __syncwarp();
+    cluster_sync_all();
+  }
+  // This CTA's share of the columns, each sample's rows among them.
+  const int n0 = sg.N * rank / cs, n1 = *abort_flag ? n0 : min(sg.N * (rank + 1) / cs, sg.B * sg.nb), vecs = p.f / 8;
+  const uint32_t sums = smem_u32(smem);
+  for (int i = n0 * vecs + int(threadIdx.x); i < n1 * vecs; i += SOME_THREADS) {
     const int n = i / vecs, j = 8 * (i - n * vecs), s = n / sg.nb, r = n - s * sg.nb;
     if (r >= sg.rows || f0 + j >= p.F || (sg.gated && p.mode[s] == RA_MODE_REUSE)) continue;
-    const float* src = reinterpret_cast<const float*>(smem) + n * 2 * p.f + j;
+    uint64_t g[4], w[4];
+    const uint32_t at = sums + uint32_t(n * 2 * p.f + j) * 4u;
+    if (cs == 1) {
+      const float* src = reinterpret_cast<const float*>(smem) + n * 2 * p.f + j;
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        const ulonglong2 x = *reinterpret_cast<const ulonglong2*>(src + 4 * q);
+        const ulonglong2 y = *reinterpret_cast<const ulonglong2*>(src + p.f + 4 * q);
+        g[2 * q] = x.x, g[2 * q + 1] = x.y, w[2 * q] = y.x, w[2 * q + 1] = y.y;
+      }
+    } else {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) g[q] = w[q] = 0;
+      for (int c = 0; c < cs; ++c) {  // in order
+        const uint32_t from = mapa_shared(at, uint32_t(c));
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+          const float4 x = ld_cluster_f4(from + 16 * q), y = ld_cluster_f4(from + 4 * p.f + 16 * q);
+          g[2 * q] = f2_add(g[2 * q], f2_pack(x.x, x.y)), g[2 * q + 1] = f2_add(g[2 * q + 1], f2_pack(x.z, x.w));
+          w[2 * q] = f2_add(w[2 * q], f2_pack(y.x, y.y)), w[2 * q + 1] = f2_add(w[2 * q + 1], f2_pack(y.z, y.w));
+        }
+      }
+    }
     uint32_t o[3][4];
 #pragma unroll
-    for (int q = 0; q < 2; ++q) {
-      const ulonglong2 g = *reinterpret_cast<const ulonglong2*>(src + 4 * q);
-      const ulonglong2 w = *reinterpret_cast<const ulonglong2*>(src + p.f + 4 * q);
-      o[0][2 * q] = f2_bf16(f2_mul(act2<ACT>(g.x, nullptr), w.x)), o[0][2 * q + 1] = f2_bf16(f2_mul(act2<ACT>(g.y, nullptr), w.y));
-      o[1][2 * q] = f2_bf16(g.x), o[1][2 * q + 1] = f2_bf16(g.y);
-      o[2][2 * q] = f2_bf16(w.x), o[2][2 * q + 1] = f2_bf16(w.y);
-    }
+    for (int q = 0; q < 4; ++q)
+      o[0][q] = f2_bf16(f2_mul(act2<ACT>(g[q], nullptr), w[q])), o[1][q] = f2_bf16(g[q]), o[2][q] = f2_bf16(w[q]);
 #pragma unroll
     for (int z = 0; z < 3; ++z)
       if (sg.out[z].ptr)
         *reinterpret_cast<uint4*>(row_ptr(sg.out[z], s, r, f0 + j)) = make_uint4(o[z][0], o[z][1], o[z][2], o[z][3]);
+  }
+  if (cs > 1) {
+    __syncwarp();
+    cluster_sync_all();  // the others have read this CTA's sums
   }
 }
 
@@ -980,12 +1016,6 @@ struct alignas(64) ColsParams {
   int32_t* err_word;
   uint64_t budget_ns;
 };
-
-__device__ __forceinline__ float4 ld_cluster_f4(uint32_t addr) {
-  float4 v;
-  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr));
-  return v;
-}
 
 template <int KIND, int ACT>
 __global__ void __launch_bounds__(SOME_THREADS) glu_cols_kernel(const __grid_constant__ ColsParams p) {
@@ -1302,12 +1332,42 @@ Plan make_plan(const Products& pr, bool dx, int sms) {
   return best;
 }
 
-// Does glu_some_kernel take the call? Its shape: features a CTA so that they fill the
-// SMs once or a whole number of times, stages as the shared memory has room for, or
-// half of it where there is more than one round: then a CTA has its first loads in
-// flight while the one before it ends.
-constexpr int SOME_SMEM = 225 * 1024, SOME_SMEM_HALF = 112 * 1024;
-bool some_rows(const ra_glu_args& a, const Params& p, const RowTensor (&x)[3], SomeParams& sp) {
+// Clusters of c CTAs with this shared memory (one of two sizes) that the GPU holds at
+// once, asked once: they lie within GPCs, which are not multiples of every size (of
+// eight CTAs, two an SM: 36, though 304 CTAs fit). One cluster more than fits doubles a
+// kernel's time.
+int resident_clusters(const void* fn, int smem, int c) {
+  static std::atomic<int> held[2][9];
+  std::atomic<int>& known = held[smem > 113 * 1024][c];
+  int n = known.load(std::memory_order_relaxed);
+  if (n == 0) {
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = unsigned(c);
+    attr.val.clusterDim.y = 1;
+    attr.val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(unsigned(c));
+    cfg.blockDim = dim3(SOME_THREADS);
+    cfg.dynamicSmemBytes = size_t(smem);
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    if (cudaOccupancyMaxActiveClusters(&n, fn, &cfg) != cudaSuccess || n < 1) {
+      cudaGetLastError();
+      n = 1;
+    }
+    known.store(n, std::memory_order_relaxed);
+  }
+  return n;
+}
+
+// Does glu_some_kernel take the call? Its shape: features a CTA and CTAs that share K,
+// so that the busiest SM stages the fewest bytes (it stages about 64 a ns; a byte of the
+// sums that a cluster exchanges takes as long as five); stages as the shared memory has room
+// for, or half of it where there is more than one round: then a CTA has its first loads
+// in flight while the one before it ends.
+constexpr int SOME_SMEM = 225 * 1024, SOME_SMEM_HALF = 112 * 1024, SOME_MAX_CS = 4;
+bool some_rows(const ra_glu_args& a, const Params& p, const RowTensor (&x)[3], const void* fn, SomeParams& sp) {
   std::memset(&sp, 0, sizeof(sp));
   int most = 0;
   for (int j = 0; j < p.n_jobs; ++j) {
@@ -1320,14 +1380,21 @@ bool some_rows(const ra_glu_args& a, const Params& p, const RowTensor (&x)[3], S
     most = d.N > most ? d.N : most;
   }
   const int sms = num_sms();
-  const int64_t slots = sms / p.n_jobs > 0 ? sms / p.n_jobs : 1, rounds = div_up(a.F, 64 * slots);
-  sp.f = int(div_up(div_up(a.F, rounds * slots), 8) * 8);
   sp.F = a.F;
   sp.stages = int(div_up(a.C, 64));
+  int64_t best = INT64_MAX, rounds = 1;
+  for (int cs = 1; cs <= SOME_MAX_CS && cs <= sp.stages; ++cs)
+    for (int f = 8; f <= 64; f += 8) {
+      const int64_t units = div_up(a.F, f) * p.n_jobs;
+      if (cs > 1 && units > resident_clusters(fn, SOME_SMEM, cs)) continue;
+      const int64_t turns = cs > 1 ? 1 : div_up(units, sms);
+      const int64_t bytes = turns * (2 * f + most) * 128 * div_up(sp.stages, cs) + (cs > 1 ? 5 * most * 2 * f * 4 : 0);
+      if (bytes < best) best = bytes, rounds = turns, sp.f = f, sp.cs = cs;
+    }
   sp.stage_bytes = 128 * (2 * sp.f + most);
   sp.ring = ((rounds > 1 ? SOME_SMEM_HALF : SOME_SMEM) - SOME_SLACK) / sp.stage_bytes;
   if (sp.ring > SOME_RING) sp.ring = SOME_RING;
-  if (sp.ring > sp.stages) sp.ring = sp.stages;
+  if (sp.ring > div_up(sp.stages, sp.cs)) sp.ring = int(div_up(sp.stages, sp.cs));
   // the fp32 tile takes the place of the stages
   while (sp.ring * sp.stage_bytes < most * 2 * sp.f * 4) ++sp.ring;
   sp.tmem_cols = 32;
@@ -1346,32 +1413,6 @@ int cols_box(int rows) {  // rows of a block, as launch_cols has them
   const int64_t blocks = div_up(rows, COLS_N);
   return int(div_up(div_up(rows, blocks), 16) * 16);
 }
-// Clusters of c CTAs of glu_cols_kernel that the GPU holds at once, asked once a size
-// (of any of its forms: they differ in neither shared memory nor threads): they lie within GPCs, which are not multiples of every size (of eight: 36, though
-// 304 CTAs fit). One cluster more than fits doubles the kernel's time.
-int resident_clusters(void (*fn)(ColsParams), int c) {
-  static std::atomic<int> held[9];
-  int n = held[c].load(std::memory_order_relaxed);
-  if (n == 0) {
-    cudaLaunchAttribute attr;
-    attr.id = cudaLaunchAttributeClusterDimension;
-    attr.val.clusterDim.x = unsigned(c);
-    attr.val.clusterDim.y = 1;
-    attr.val.clusterDim.z = 1;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(unsigned(c));
-    cfg.blockDim = dim3(SOME_THREADS);
-    cfg.dynamicSmemBytes = COLS_SMEM;
-    cfg.attrs = &attr;
-    cfg.numAttrs = 1;
-    if (cudaOccupancyMaxActiveClusters(&n, fn, &cfg) != cudaSuccess || n < 1) {
-      cudaGetLastError();
-      n = 1;
-    }
-    held[c].store(n, std::memory_order_relaxed);
-  }
-  return n;
-}
 template <int KIND>
 ra_status launch_cols(const char* who, void (*fn)(ColsParams), ColsParams& p, int samples, cudaStream_t st) {
   const int sms = num_sms();
@@ -1389,7 +1430,7 @@ ra_status launch_cols(const char* who, void (*fn)(ColsParams), ColsParams& p, in
   int cs = 1;
   double best = 1e30;
   for (int c = 1; c <= 8 && c <= stages; ++c) {
-    const double us = 2.0 * double(div_up(units, resident_clusters(fn, c))) +
+    const double us = 2.0 * double(div_up(units, resident_clusters(reinterpret_cast<const void*>(fn), COLS_SMEM, c))) +
                       0.2 * double(div_up(units * c, sms) * div_up(stages, c)) + 0.15 * c;
     if (us < best) best = us, cs = c;
   }
@@ -1541,8 +1582,13 @@ extern "C" ra_status refadapt_glu(const ra_glu_args* a, void* stream) {
     }
     return launch_status(who);
   }
+  void (*some)(SomeParams) = a->act == RA_ACT_GELU ? glu_some_kernel<RA_ACT_GELU> : glu_some_kernel<RA_ACT_SILU>;
   SomeParams sp;
-  if (some_rows(*a, p, x, sp)) {
+  if (most <= SOME_MAX) {
+    const ra_status as = ensure_dynamic_smem(reinterpret_cast<const void*>(some), SOME_SMEM, who);
+    if (as != RA_OK) return as;
+  }
+  if (most <= SOME_MAX && some_rows(*a, p, x, reinterpret_cast<const void*>(some), sp)) {
     sp.mode = a->mode, sp.err_word = a->err_word, sp.budget_ns = p.budget_ns;
     for (int g = 0, j = 0; g < a->n_seg; ++g) {
       const ra_glu_seg& s = a->seg[g];
@@ -1552,20 +1598,21 @@ extern "C" ra_status refadapt_glu(const ra_glu_args* a, void* stream) {
       if (!encode(&d.x, x[j], d.nb) || !encode(&d.w[0], wg, sp.f) || !encode(&d.w[1], wu, sp.f)) return RA_EINVAL;
       ++j;
     }
-    const bool gelu = a->act == RA_ACT_GELU;
-    void (*fn)(SomeParams) = gelu ? glu_some_kernel<RA_ACT_GELU> : glu_some_kernel<RA_ACT_SILU>;
-    const ra_status as = ensure_dynamic_smem(reinterpret_cast<const void*>(fn), SOME_SMEM, who);
-    if (as != RA_OK) return as;
-    note_launch("some rows, %d features", sp.f);
+    note_launch("some rows, %d features, clusters of %d", sp.f, sp.cs);
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(unsigned(div_up(a->F, sp.f)), unsigned(p.n_jobs));
+    cfg.gridDim = dim3(unsigned(div_up(a->F, sp.f) * sp.cs), unsigned(p.n_jobs));
     cfg.blockDim = dim3(SOME_THREADS);
     cfg.dynamicSmemBytes = size_t(sp.ring) * sp.stage_bytes + SOME_SLACK;
     cfg.stream = static_cast<cudaStream_t>(stream);
-    cudaLaunchAttribute attr = pdl_attribute();
-    cfg.attrs = &attr;
-    cfg.numAttrs = 1;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, fn, sp);
+    cudaLaunchAttribute attr[2];
+    attr[0] = pdl_attribute();
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = unsigned(sp.cs);
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = sp.cs > 1 ? 2 : 1;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, some, sp);
     if (e != cudaSuccess) {
       set_error("%s: launch failed: %s", who, cudaGetErrorString(e));
       cudaGetLastError();
