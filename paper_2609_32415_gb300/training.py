@@ -13,6 +13,20 @@ from ._lib import RA_EPI_STORE
 __all__ = ["gated_feed_forward", "residual_norm", "rope_axes"]
 
 
+# Gradients come in whatever layout the graph gave them (transposed, strides of zero,
+# part of a flat tensor at any offset); the calls want whole 16-byte pieces.
+def _rows(grad):
+    grad = grad.contiguous()
+    return grad if grad.data_ptr() % 16 == 0 else grad.clone()
+
+
+def _heads(grad):
+    """[B, H, n, d]: any order of the axes but the last."""
+    if grad.stride(3) == 1 and all(s % 8 == 0 for s in grad.stride()[:3]) and grad.data_ptr() % 16 == 0:
+        return grad
+    return grad.clone(memory_format=torch.contiguous_format)
+
+
 class _GatedFeedForward(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, w_gate, w_up, w_down, act, err_word):
@@ -35,7 +49,7 @@ class _GatedFeedForward(torch.autograd.Function):
         if any(g is not None for g in grads):
             ws = api.glu_backward_workspace(x.shape[0], x.shape[1], x.shape[2], w_gate.shape[0], w_down.shape[0],
                                             x.device)
-            api.refadapt_glu_backward(dy.contiguous(), x, w_gate, w_up, w_down, pre_gate, pre_up, hidden, ctx.act, ws,
+            api.refadapt_glu_backward(_rows(dy), x, w_gate, w_up, w_down, pre_gate, pre_up, hidden, ctx.act, ws,
                                       dx=grads[0], dw_gate=grads[1], dw_up=grads[2], dw_down=grads[3],
                                       err_word=ctx.err_word)
         return (*grads, None, None)
@@ -63,7 +77,7 @@ class _ResidualNorm(torch.autograd.Function):
         h_out, y, gate, post_w, pre_w, scale, shift = ctx.saved_tensors
         post, pre, eps, alpha, err_word = ctx.args
         B, n, C = h_out.shape
-        seg = {"h": h_out, "y": y, "dx": dx.contiguous(), "dh_out": dh_out.contiguous(), "gate": gate,
+        seg = {"h": h_out, "y": y, "dx": _rows(dx), "dh_out": _rows(dh_out), "gate": gate,
                "post_w": post_w, "pre_w": pre_w, "scale": scale}
         grads = []
         for name, t, need in zip(("dh", "dy", "dgate", "dpost_w", "dpre_w", "dscale", "dshift"),
@@ -97,6 +111,7 @@ class _RopeAxes(torch.autograd.Function):
     def backward(ctx, dout):
         (pos,) = ctx.saved_tensors
         axes, base = ctx.args
+        dout = _heads(dout)
         dx = torch.empty_like(dout)
         api.refadapt_rope_axes([(dout, dx)], pos, axes, base, inverse=True)
         return dx, None, None, None

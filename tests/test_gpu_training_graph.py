@@ -1,0 +1,75 @@
+"""The autograd functions of the gated block's layers inside torch's graph: gradients
+that arrive in every layout torch hands on.
+
+Tolerances are those of test_gpu_block_layers (one rounding to bf16) where an
+operator's backward call is compared on the gradient that it was given; a graph's own
+gradients carry bf16 tensors between layers: a few 2^-9 normwise, 1e-2 has room."""
+import numpy as np
+import pytest
+import torch
+
+from _helpers import f64
+from oracle import layers
+from test_gpu_block_layers import bf, close, d64, f32
+
+pytestmark = pytest.mark.gpu
+
+
+def relative(a, b):
+    return float((a.double() - b).norm() / (b.norm() + 1e-300))
+
+
+# ------------------------------------------------------------------ layouts of gradients
+def rope_loss(layout, y, g):
+    """A loss whose gradient with respect to y ([B, H, n, d]) arrives in the layout."""
+    B, H, n, d = y.shape
+    if layout == "product":      # that of k in q @ k^T: the last axis is not contiguous
+        return (bf((B, H, n, d), g) @ y.transpose(-1, -2)).float().square().sum()
+    if layout == "sum":          # one number for all elements: strides of zero
+        return y.sum()
+    if layout == "sum of rows":  # strides of zero but for the last axis
+        return (y.sum((0, 1, 2)).float() * f32((d,), g)).sum()
+    if layout == "odd offset":   # part of a flat tensor, three elements in: not 16-byte aligned
+        z = torch.cat((y.new_zeros(3), y.reshape(-1)))
+        return (z * bf(z.shape, g)).float().sum()
+    assert layout == "token"     # token-major, taken as it is
+    z = y.transpose(1, 2)
+    return (z * bf(z.shape, g)).float().sum()
+
+
+@pytest.mark.parametrize("layout", ["product", "sum", "sum of rows", "odd offset", "token"])
+def test_rope_gradient_in_every_layout(cuda_ok, layout):
+    from paper_2609_32415_gb300 import training
+    g = torch.Generator().manual_seed(len(layout))
+    B, H, n, d, axes = 2, 4, 75, 64, (24, 32)
+    x = bf((B, H, n, d), g).requires_grad_(True)
+    pos = f32((n, 2), g, 20.0)
+    y = training.rope_axes(x, pos, axes)
+    given = []
+    y.register_hook(lambda v: given.append(v.clone()))
+    rope_loss(layout, y, g).backward()
+    ref = layers.rope_axes(f64(given[0]), d64(pos), axes, inverse=True)
+    ok, worst = close(f64(x.grad), ref, np.abs(f64(given[0])).max())
+    assert ok, worst
+
+
+def test_row_gradients_that_are_not_aligned(cuda_ok):
+    """The other two functions, with gradients that start three elements into a flat tensor."""
+    from paper_2609_32415_gb300 import training
+    g = torch.Generator().manual_seed(7)
+    B, n, C, F = 2, 33, 256, 128
+    leaves = [bf((B, n, C), g).requires_grad_(True), bf((B, n, C), g).requires_grad_(True)]
+    w = [bf((F, C), g, C ** -0.5), bf((F, C), g, C ** -0.5), bf((C, F), g, F ** -0.5)]
+    up = [bf((3 + B * n * C,), g) for _ in range(3)]
+
+    def grads(shift):
+        h, x = training.residual_norm(leaves[0], leaves[1], 2, 1)
+        y = training.gated_feed_forward(leaves[0], *w, 0)
+        loss = 0.0
+        for t, u in zip((h, x, y), up):
+            t = torch.cat((t.new_zeros(3), t.reshape(-1))) if shift else t.reshape(-1)
+            loss = loss + (t * (u if shift else u[3:].clone())).float().sum()
+        return torch.autograd.grad(loss, leaves)
+
+    for a, b in zip(grads(True), grads(False)):
+        assert torch.equal(a, b)
