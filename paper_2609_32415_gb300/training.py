@@ -4,7 +4,10 @@ Forward and backward run in librefadapt.so (refadapt_glu, refadapt_residual_norm
 refadapt_rope_axes and their backward passes); torch keeps the graph, allocates
 the results and supplies the stream. bf16 rows and weights, fp32 vectors, on one
 GPU; shapes as in ``api``. Gradients of bf16 tensors are bf16, of fp32 vectors
-fp32."""
+fp32. ``rope_axes`` can be differentiated any number of times (its gradient is the
+inverse turn); the other two once: a second time raises."""
+import functools
+
 import torch
 
 from . import api
@@ -27,6 +30,37 @@ def _heads(grad):
     return grad.clone(memory_format=torch.contiguous_format)
 
 
+class _Gradients(torch.autograd.Function):
+    """The first n tensors, gradients that a kernel computed from the others."""
+
+    @staticmethod
+    def forward(ctx, n, *tensors):
+        return tensors[:n]
+
+    @staticmethod
+    def backward(ctx, *_):
+        raise RuntimeError("gated_feed_forward and residual_norm cannot be differentiated twice")
+
+
+def _once(backward):
+    """A backward pass without a derivative of its own. Under create_graph its results stay
+    connected to what they came from, so that a second derivative through them raises
+    (torch's once_differentiable ties them to nothing: torch.autograd.grad then drops their
+    part without a word)."""
+    @functools.wraps(backward)
+    def wrapper(ctx, *grads):
+        with torch.no_grad():
+            out = list(backward(ctx, *grads))
+        if torch.is_grad_enabled():
+            given = [i for i, v in enumerate(out) if v is not None]
+            made = _Gradients.apply(len(given), *(out[i] for i in given),
+                                    *(t for t in (*grads, *ctx.saved_tensors) if t is not None)) if given else ()
+            for i, v in zip(given, made):
+                out[i] = v
+        return tuple(out)
+    return wrapper
+
+
 class _GatedFeedForward(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, w_gate, w_up, w_down, act, err_word):
@@ -42,6 +76,7 @@ class _GatedFeedForward(torch.autograd.Function):
         return y
 
     @staticmethod
+    @_once
     def backward(ctx, dy):
         x, w_gate, w_up, w_down, pre_gate, pre_up, hidden = ctx.saved_tensors
         grads = [torch.empty_like(t, memory_format=torch.contiguous_format) if need else None
@@ -73,6 +108,7 @@ class _ResidualNorm(torch.autograd.Function):
         return h_out, x
 
     @staticmethod
+    @_once
     def backward(ctx, dh_out, dx):
         h_out, y, gate, post_w, pre_w, scale, shift = ctx.saved_tensors
         post, pre, eps, alpha, err_word = ctx.args
@@ -100,23 +136,20 @@ def residual_norm(h, y, post, pre, gate=None, post_w=None, pre_w=None, scale=Non
 
 class _RopeAxes(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, pos, axes, base):
+    def forward(ctx, x, pos, axes, base, inverse):
         out = torch.empty_like(x)
-        api.refadapt_rope_axes([(x, out)], pos, axes, base)
+        api.refadapt_rope_axes([(x, out)], pos, axes, base, inverse=inverse)
         ctx.save_for_backward(pos)
-        ctx.args = (axes, base)
+        ctx.args = (axes, base, inverse)
         return out
 
     @staticmethod
     def backward(ctx, dout):
         (pos,) = ctx.saved_tensors
-        axes, base = ctx.args
-        dout = _heads(dout)
-        dx = torch.empty_like(dout)
-        api.refadapt_rope_axes([(dout, dx)], pos, axes, base, inverse=True)
-        return dx, None, None, None
+        axes, base, inverse = ctx.args
+        return _RopeAxes.apply(_heads(dout), pos, axes, base, not inverse), None, None, None, None
 
 
 def rope_axes(x, pos, axes, base=10000.0):
     """x [B, H, n, d] bf16 turned by the rows' coordinates pos ([n, len(axes)] or [B, n, len(axes)] fp32)."""
-    return _RopeAxes.apply(x, pos, tuple(axes), base)
+    return _RopeAxes.apply(x, pos, tuple(axes), base, False)

@@ -1,5 +1,5 @@
 """The autograd functions of the gated block's layers inside torch's graph: gradients
-that arrive in every layout torch hands on.
+that arrive in every layout torch hands on, second derivatives.
 
 Tolerances are those of test_gpu_block_layers (one rounding to bf16) where an
 operator's backward call is compared on the gradient that it was given; a graph's own
@@ -73,3 +73,42 @@ def test_row_gradients_that_are_not_aligned(cuda_ok):
 
     for a, b in zip(grads(True), grads(False)):
         assert torch.equal(a, b)
+
+
+# ------------------------------------------------------------------ second derivatives
+def test_rope_is_differentiable_twice(cuda_ok):
+    """d/dx of |d(sum rope(x)^2 u)/dx|^2: the gradient passes through the backward call."""
+    from paper_2609_32415_gb300 import training
+    g = torch.Generator().manual_seed(11)
+    B, H, n, d, axes = 1, 2, 40, 64, (32, 32)
+    x, u, pos = bf((B, H, n, d), g).requires_grad_(True), f32((B, H, n, d), g), f32((n, 2), g, 5.0)
+    y = training.rope_axes(x, pos, axes)
+    (first,) = torch.autograd.grad((y.float() ** 2 * u).sum(), x, create_graph=True)
+    (got,) = torch.autograd.grad((first.float() ** 2).sum(), x)
+
+    ang = torch.as_tensor(layers.rope_axes_angles(d64(pos), axes)).cuda()
+    c, s = torch.cos(ang), torch.sin(ang)
+
+    def turn(v):
+        e, o = v[..., 0::2], v[..., 1::2]
+        return torch.stack((e * c - o * s, e * s + o * c), -1).flatten(-2)
+
+    x2 = x.detach().double().requires_grad_(True)
+    (first2,) = torch.autograd.grad((turn(x2) ** 2 * u.double()).sum(), x2, create_graph=True)
+    (want,) = torch.autograd.grad((first2 ** 2).sum(), x2)
+    assert float(want.norm()) > 0 and relative(got, want) < 1e-2, relative(got, want)
+
+
+@pytest.mark.parametrize("layer", ["feed-forward", "norm"])
+def test_second_derivatives_are_refused_where_there_are_none(cuda_ok, layer):
+    from paper_2609_32415_gb300 import training
+    g = torch.Generator().manual_seed(12)
+    x = bf((1, 20, 256), g).requires_grad_(True)
+    if layer == "norm":
+        _, y = training.residual_norm(x, None, 0, 2)
+    else:
+        y = training.gated_feed_forward(x, bf((64, 256), g, 0.06), bf((64, 256), g, 0.06), bf((256, 64), g, 0.1), 0)
+    # 0.5 |y|^2 keeps a path to x besides the layer's backward call, so that the graph does not end at once
+    (first,) = torch.autograd.grad(0.5 * (y.float() ** 2).sum() + (x.float() ** 2).sum(), x, create_graph=True)
+    with pytest.raises(RuntimeError, match="twice"):
+        torch.autograd.grad((first.float() ** 2).sum(), x)
