@@ -63,10 +63,11 @@ def _once(backward):
 
 class _GatedFeedForward(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, w_gate, w_up, w_down, act, err_word):
+    def forward(ctx, x, w_gate, w_up, w_down, act, err_word, learn):
         B, n, C = x.shape
         F, O = w_gate.shape[0], w_down.shape[0]
-        hidden, pre_gate, pre_up = (torch.empty((B, n, F), dtype=x.dtype, device=x.device) for _ in range(3))
+        hidden, pre_gate, pre_up = (torch.empty((B, n, F), dtype=x.dtype, device=x.device) if need else None
+                                    for need in (True, learn, learn))
         y = torch.empty((B, n, O), dtype=x.dtype, device=x.device)
         api.refadapt_glu([{"x": x, "w_gate": w_gate, "w_up": w_up, "out": hidden, "pre_gate": pre_gate,
                            "pre_up": pre_up}], F, C, act, err_word=err_word)
@@ -87,13 +88,16 @@ class _GatedFeedForward(torch.autograd.Function):
             api.refadapt_glu_backward(_rows(dy), x, w_gate, w_up, w_down, pre_gate, pre_up, hidden, ctx.act, ws,
                                       dx=grads[0], dw_gate=grads[1], dw_up=grads[2], dw_down=grads[3],
                                       err_word=ctx.err_word)
-        return (*grads, None, None)
+        return (*grads, None, None, None)
 
 
 def gated_feed_forward(x, w_gate, w_up, w_down, act, err_word=None):
     """(act(x w_gate^T) o (x w_up^T)) w_down^T: x [B, rows, C], w_gate and w_up
-    [F, C], w_down [O, F], bf16 (F a multiple of 64, O of 256)."""
-    return _GatedFeedForward.apply(x, w_gate, w_up, w_down, act, err_word)
+    [F, C], w_down [O, F], bf16 (F a multiple of 64, O of 256, which
+    refadapt_gemm needs)."""
+    # The pre-activations (twice the hidden rows) are kept for x, w_gate and w_up only.
+    learn = torch.is_grad_enabled() and any(t.requires_grad for t in (x, w_gate, w_up))
+    return _GatedFeedForward.apply(x, w_gate, w_up, w_down, act, err_word, learn)
 
 
 class _ResidualNorm(torch.autograd.Function):

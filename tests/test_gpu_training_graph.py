@@ -1,5 +1,6 @@
 """The autograd functions of the gated block's layers inside torch's graph: gradients
-that arrive in every layout torch hands on, second derivatives.
+that arrive in every layout torch hands on, second derivatives, and calls that keep
+nothing for a backward pass.
 
 Tolerances are those of test_gpu_block_layers (one rounding to bf16) where an
 operator's backward call is compared on the gradient that it was given; a graph's own
@@ -112,3 +113,45 @@ def test_second_derivatives_are_refused_where_there_are_none(cuda_ok, layer):
     (first,) = torch.autograd.grad(0.5 * (y.float() ** 2).sum() + (x.float() ** 2).sum(), x, create_graph=True)
     with pytest.raises(RuntimeError, match="twice"):
         torch.autograd.grad((first.float() ** 2).sum(), x)
+
+
+# ------------------------------------------------------------------ what a call does not need
+def test_feed_forward_keeps_nothing_where_nothing_is_learned(cuda_ok):
+    """Without gradients a call has its result and the hidden rows only; with the down
+    projection alone to learn it keeps no pre-activations either. The results are those of the
+    call that keeps everything."""
+    from paper_2609_32415_gb300 import training
+    g = torch.Generator().manual_seed(13)
+    n, C, F = 2048, 256, 4096
+    x = bf((1, n, C), g)
+    w = [bf((F, C), g, C ** -0.5), bf((F, C), g, C ** -0.5), bf((C, F), g, F ** -0.5)]
+
+    def peak(f):
+        torch.cuda.synchronize()
+        before = torch.cuda.memory_allocated()
+        torch.cuda.reset_peak_memory_stats()
+        y = f()
+        torch.cuda.synchronize()
+        return y, torch.cuda.max_memory_allocated() - before
+
+    hidden, small = 2 * n * F, 2 * n * C + (1 << 20)
+
+    def call():
+        return training.gated_feed_forward(x, *w, 0)
+
+    frozen, bytes_frozen = peak(call)
+    w[2].requires_grad_(True)
+    down, bytes_down = peak(call)
+    for t in (x, *w):
+        t.requires_grad_(True)
+    everything, bytes_all = peak(call)
+    with torch.no_grad():
+        without, bytes_without = peak(call)
+    assert bytes_all >= 3 * hidden
+    assert max(bytes_frozen, bytes_down, bytes_without) <= hidden + small, (bytes_frozen, bytes_down, bytes_without)
+    for y in (frozen, down, without):
+        assert torch.equal(y, everything)
+    dy = bf(y.shape, g)
+    (got,) = torch.autograd.grad(down, w[2], dy)
+    (want,) = torch.autograd.grad(everything, w[2], dy)
+    assert torch.equal(got, want)
