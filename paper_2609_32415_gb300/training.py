@@ -134,7 +134,10 @@ def residual_norm(h, y, post, pre, gate=None, post_w=None, pre_w=None, scale=Non
                   err_word=None):
     """(h_out, x): h_out = alpha h + gate N_post(y) post_w, x = N_pre(h_out)
     pre_w (1 + scale) + shift. h, y [B, rows, C] bf16 (y may be None); gate,
-    scale, shift [B, C], post_w, pre_w [C] fp32 or None."""
+    scale, shift [B, C], post_w, pre_w [C] fp32 or None. Without y, gate and
+    post_w have no part in the result."""
+    if y is None:
+        gate = post_w = None
     return _ResidualNorm.apply(h, y, gate, post_w, pre_w, scale, shift, post, pre, eps, alpha, err_word)
 
 

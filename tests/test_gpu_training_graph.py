@@ -1,6 +1,6 @@
 """The autograd functions of the gated block's layers inside torch's graph: gradients
-that arrive in every layout torch hands on, second derivatives, and calls that keep
-nothing for a backward pass.
+that arrive in every layout torch hands on, second derivatives, calls that keep
+nothing for a backward pass, and inputs that a call does not use.
 
 Tolerances are those of test_gpu_block_layers (one rounding to bf16) where an
 operator's backward call is compared on the gradient that it was given; a graph's own
@@ -155,3 +155,19 @@ def test_feed_forward_keeps_nothing_where_nothing_is_learned(cuda_ok):
     (got,) = torch.autograd.grad(down, w[2], dy)
     (want,) = torch.autograd.grad(everything, w[2], dy)
     assert torch.equal(got, want)
+
+
+def test_norm_without_a_branch_ignores_its_gate_and_weight(cuda_ok):
+    """h_out = alpha h where y is absent: gate and post_w have no part in it, and no gradient."""
+    from paper_2609_32415_gb300 import training
+    g = torch.Generator().manual_seed(14)
+    h = bf((2, 9, 64), g).requires_grad_(True)
+    gate, post_w = f32((2, 64), g).requires_grad_(True), f32((64,), g).requires_grad_(True)
+    pre_w = f32((64,), g, 0.1, 1.0).requires_grad_(True)
+    up = f32((2, 9, 64), g)
+    h_out, x = training.residual_norm(h, None, 2, 2, gate=gate, post_w=post_w, pre_w=pre_w)
+    got = torch.autograd.grad((x.float() * up).sum() + h_out.float().sum(), (h, pre_w, gate, post_w), allow_unused=True)
+    h_out, x = training.residual_norm(h, None, 2, 2, pre_w=pre_w)
+    want = torch.autograd.grad((x.float() * up).sum() + h_out.float().sum(), (h, pre_w))
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    assert all(v is None or not v.any() for v in got[2:])
