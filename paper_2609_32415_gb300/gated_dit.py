@@ -12,9 +12,10 @@ layers around the joint attention are
 Per block and stream: x = N_pre(h) w_pre (1 + scale) + shift; attention or
 feed-forward of x gives y; h <- h + gate N_post(y) w_post. The norm after a
 branch, the gate, the residual sum and the norm before the next branch are one
-call, across the border of two blocks too: a block's last call also gives the
-next block's x for the text and target rows (not for the reference rows, which
-wait for that block's decision).
+call within a block. With resident weights (see ``step``) they are across the
+border of two blocks too: a block's last call then also gives the next block's x
+for the text and target rows (not for the reference rows, which wait for that
+block's decision).
 """
 import torch
 
@@ -86,7 +87,13 @@ class GatedDiTExecutor(DiTExecutor):
             segs.append(s)
         self._norm(segs, mode, stream)
 
-    def step(self, t, h_in, mods, weights, log_index=None, stream=None, after_block=None):
+    def step(self, t, h_in, mods, weights, log_index=None, stream=None, after_block=None, resident=False):
+        """As DiTExecutor.step. resident: what mods and weights give stays valid, unchanged,
+        until the step's work has run, and they may be asked for a block before the one in
+        front of it is enqueued; the border of two blocks is then one call (x of the next
+        block from the unrounded rows), unless an after_block hook stands on it."""
+        if not resident or after_block is not None:
+            return super().step(t, h_in, mods, weights, log_index, stream, after_block)
         self.hbar[0] = h_in["ref"]
         here = (mods(t, 0), weights(0))
         try:
@@ -96,7 +103,5 @@ class GatedDiTExecutor(DiTExecutor):
                 self._x_ready = b > 0
                 self.block(t, b, src, here[0], here[1], log_index, stream)
                 here = self._next
-                if after_block is not None:
-                    after_block(t, b)
         finally:
             self._next, self._x_ready = None, False
