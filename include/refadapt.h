@@ -492,7 +492,9 @@ ra_status refadapt_gemm(const ra_gemm_args* args, void* stream);
  *  axis_dim    even, >= 2, sum <= d; 1 to 4 axes; base > 1.
  *  d           a multiple of 8, at most 256; n * d / 8 < 2^31.
  *  t[i].x, .out  bf16 segments of n rows; out may equal x (same strides) but
- *              must not partially overlap it. */
+ *              must not partially overlap it, nor the other tensor. The strides
+ *              of an output are at least d; those of axes with one entry say
+ *              nothing. */
 typedef struct {
   ra_seg x, out;
   int32_t heads, reserved;

@@ -190,6 +190,33 @@ bool make_freqs(Freqs& fr, const char* who, int n_axes, const int32_t* axis_dim,
   return true;
 }
 
+// An output has a place for each row, and that of an input in place is the input's own.
+// Strides of axes with one entry say nothing.
+bool check_out(const ra_rope_args& a, const ra_rope_tensor& t, int i) {
+  const int64_t longer[3] = {a.B, t.heads, a.n};
+  const int64_t in[3] = {t.x.stride_b, t.x.stride_h, t.x.stride_n}, out[3] = {t.out.stride_b, t.out.stride_h, t.out.stride_n};
+  bool same = true, apart = true;
+  for (int k = 0; k < 3; ++k) {
+    if (longer[k] < 2) continue;
+    same &= in[k] == out[k];
+    apart &= out[k] >= a.d;
+  }
+  if (!apart) {
+    set_error("refadapt_rope_axes: tensor %d: the output's rows lie on one another", i);
+    return false;
+  }
+  if (t.x.ptr == t.out.ptr && !same) {
+    set_error("refadapt_rope_axes: tensor %d: an output in place needs its input's strides", i);
+    return false;
+  }
+  const ra_rope_tensor& other = a.t[1 - i];
+  if (a.n_tensors == 2 && other.heads > 0 && (t.out.ptr == other.out.ptr || t.out.ptr == other.x.ptr)) {
+    set_error("refadapt_rope_axes: tensor %d: the output is the other's input or output", i);
+    return false;
+  }
+  return true;
+}
+
 }  // namespace rope
 }  // namespace ra
 
@@ -224,6 +251,7 @@ extern "C" ra_status refadapt_rope_axes(const ra_rope_args* a, void* stream) {
     }
     if (t.heads == 0) continue;
     if (!check_seg(t.x, "refadapt_rope_axes: x") || !check_seg(t.out, "refadapt_rope_axes: out")) return RA_EINVAL;
+    if (a->n > 0 && !check_out(*a, t, i)) return RA_EINVAL;
     heads += t.heads;
     p.t[i] = Tensor{static_cast<const __nv_bfloat16*>(t.x.ptr), static_cast<__nv_bfloat16*>(t.out.ptr),
                     t.x.stride_b, t.x.stride_h, t.x.stride_n, t.out.stride_b, t.out.stride_h, t.out.stride_n, t.heads, 0};
