@@ -30,6 +30,7 @@
 #include <type_traits>
 
 #include "api_common.h"
+#include "launch_plan.h"
 #include "row_walk.cuh"
 #include "tc_ptx.cuh"
 
@@ -64,6 +65,7 @@ struct Seg {
 struct Params {
   int32_t n_seg, B, C, post, pre;
   int32_t groups, stages;  // of a CTA; of a ring
+  int32_t few;             // few_pieces()
   float eps, alpha;
   const int32_t* mode;
   Seg seg[3];
@@ -333,7 +335,6 @@ struct Cursor {
 // twelfth. A CTA that goes on into another sample has its vectors to fetch, and the
 // rest of the grid waits for it: 2 x (77 + 500) rows of 1280 8.3 us on even shares, 7.0
 // here; 2 x (256 + 4096) of 2560 36.9 and 35.3. (The whole warp.)
-constexpr int FEW_PIECES = 12;
 __device__ __forceinline__ bool piece_share(const Params& p, int total, int round, int& lo, int& hi) {
   const int grid = int(gridDim.x), cta = int(blockIdx.x), lane = threadIdx.x & 31;
   uint32_t on[3] = {};
@@ -384,8 +385,7 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) residual_norm_kernel(const __g
   pdl_wait();
   const int total = live_rows(p);
   int lo, hi;
-  if (total <= 2 * int(gridDim.x) || p.B * p.n_seg == 1 || p.B * p.n_seg > FEW_PIECES ||
-      !piece_share(p, total, 2 * p.groups, lo, hi)) {
+  if (total <= 2 * int(gridDim.x) || !p.few || !piece_share(p, total, 2 * p.groups, lo, hi)) {
     const int share = total / int(gridDim.x), more = total - share * int(gridDim.x), cta = int(blockIdx.x);
     lo = share * cta + min(cta, more), hi = lo + share + (cta < more ? 1 : 0);
   }
@@ -1079,6 +1079,7 @@ extern "C" ra_status refadapt_residual_norm(const ra_resnorm_args* a, void* stre
   const Shape sh = fwd_shape(a->C);
   p.groups = sh.groups;
   p.stages = sh.stages;
+  p.few = few_pieces(a->B, a->n_seg);
   const int64_t sms = num_sms();
   return launch(who, pick_fwd(sh), p, dim3(unsigned(rows < sms ? rows : sms)), sh.threads(), sh.smem,
                 static_cast<cudaStream_t>(stream));
