@@ -40,12 +40,12 @@
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
-#include <atomic>
 #include <cmath>
 #include <cstring>
 
 #include "api_common.h"
 #include "epi_rows.cuh"
+#include "launch_plan.h"
 #include "tc_ptx.cuh"
 
 namespace ra {
@@ -1332,15 +1332,14 @@ Plan make_plan(const Products& pr, bool dx, int sms) {
   return best;
 }
 
-// Clusters of c CTAs with this shared memory (one of two sizes) that the GPU holds at
-// once, asked once: they lie within GPCs, which are not multiples of every size (of
-// eight CTAs, two an SM: 36, though 304 CTAs fit). One cluster more than fits doubles a
-// kernel's time.
-int resident_clusters(const void* fn, int smem, int c) {
-  static std::atomic<int> held[2][9];
-  std::atomic<int>& known = held[smem > 113 * 1024][c];
-  int n = known.load(std::memory_order_relaxed);
-  if (n == 0) {
+// Clusters of c CTAs of a kernel that the GPU holds at once (of eight CTAs of
+// glu_cols_kernel, two an SM: 36, though 304 CTAs fit). One cluster more than fits
+// doubles a kernel's time.
+ClusterTable::Counts resident_clusters(const void* fn, int smem) {
+  static ClusterTable table;
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) cudaGetLastError();
+  return table.get(dev, fn, smem, [&](int c) {
     cudaLaunchAttribute attr;
     attr.id = cudaLaunchAttributeClusterDimension;
     attr.val.clusterDim.x = unsigned(c);
@@ -1352,13 +1351,11 @@ int resident_clusters(const void* fn, int smem, int c) {
     cfg.dynamicSmemBytes = size_t(smem);
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
-    if (cudaOccupancyMaxActiveClusters(&n, fn, &cfg) != cudaSuccess || n < 1) {
-      cudaGetLastError();
-      n = 1;
-    }
-    known.store(n, std::memory_order_relaxed);
-  }
-  return n;
+    int n = 0;
+    if (cudaOccupancyMaxActiveClusters(&n, fn, &cfg) == cudaSuccess) return n;
+    cudaGetLastError();
+    return -1;
+  });
 }
 
 // Does glu_some_kernel take the call? Its shape: features a CTA and CTAs that share K,
@@ -1383,10 +1380,11 @@ bool some_rows(const ra_glu_args& a, const Params& p, const RowTensor (&x)[3], c
   sp.F = a.F;
   sp.stages = int(div_up(a.C, 64));
   int64_t best = INT64_MAX, rounds = 1;
+  const ClusterTable::Counts held = resident_clusters(fn, SOME_SMEM);
   for (int cs = 1; cs <= SOME_MAX_CS && cs <= sp.stages; ++cs)
     for (int f = 8; f <= 64; f += 8) {
       const int64_t units = div_up(a.F, f) * p.n_jobs;
-      if (cs > 1 && units > resident_clusters(fn, SOME_SMEM, cs)) continue;
+      if (cs > 1 && units > held.of[cs]) continue;
       const int64_t turns = cs > 1 ? 1 : div_up(units, sms);
       const int64_t bytes = turns * (2 * f + most) * 128 * div_up(sp.stages, cs) + (cs > 1 ? 5 * most * 2 * f * 4 : 0);
       if (bytes < best) best = bytes, rounds = turns, sp.f = f, sp.cs = cs;
@@ -1429,8 +1427,10 @@ ra_status launch_cols(const char* who, void (*fn)(ColsParams), ColsParams& p, in
   if (as != RA_OK) return as;
   int cs = 1;
   double best = 1e30;
-  for (int c = 1; c <= 8 && c <= stages; ++c) {
-    const double us = 2.0 * double(div_up(units, resident_clusters(reinterpret_cast<const void*>(fn), COLS_SMEM, c))) +
+  const ClusterTable::Counts held = resident_clusters(reinterpret_cast<const void*>(fn), COLS_SMEM);
+  for (int c = 1; c <= ClusterTable::MAX_CLUSTER && c <= stages; ++c) {
+    if (held.of[c] < 1) continue;
+    const double us = 2.0 * double(div_up(units, held.of[c])) +
                       0.2 * double(div_up(units * c, sms) * div_up(stages, c)) + 0.15 * c;
     if (us < best) best = us, cs = c;
   }

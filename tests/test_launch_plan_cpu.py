@@ -18,3 +18,27 @@ def test_few_pieces_of_any_number_of_samples(tmp_path):
     cases = [(b, s) for s in (1, 2, 3) for b in (1, 2, 4, 5, 6, 7, 12, 13, 32, 715827882, 715827883, (1 << 30) - 1, 1 << 30)]
     got = run(tmp_path, "\n".join('printf("%%d\\n", int(ra::few_pieces(%d, %d)));' % c for c in cases))
     assert [int(v) for v in got] == [int(1 < b * s <= 12) for b, s in cases]
+
+
+def test_resident_clusters_are_those_of_the_device_and_kernel(tmp_path):
+    """Each (device, kernel, shared memory) has its own counts, asked once; a failed query is not kept."""
+    got = run(tmp_path, r"""
+      static ra::ClusterTable table;
+      static int asked;
+      const int kernels[2] = {0, 0};
+      auto count = [&](int device, int kernel, int smem, int c, bool fails = false) {
+        return table.get(device, kernels + kernel, smem, [&](int size) {
+          ++asked;
+          return fails ? -(size == 5) : 10000 * device + 1000 * kernel + 100 * (smem > 1000) + size;
+        }).of[c];
+      };
+      printf("%d %d ", count(1, 0, 500, 4, true), count(1, 0, 500, 5, true));  // failed: not kept
+      for (int again = 0; again < 2; ++again) {
+        printf("%d %d %d %d ", count(1, 0, 500, 4), count(1, 1, 500, 4), count(2, 0, 500, 8), count(1, 0, 2000, 1));
+        printf("%d ", asked);
+      }
+      for (int device = 3; device < 300; ++device)  // past the end of the table
+        if (count(device, 1, 500, 2) != 10000 * device + 1002) return 1;
+      printf("%d\n", count(1, 0, 500, 4));
+    """)
+    assert [int(v) for v in got] == [0, 1, 10004, 11004, 20008, 10101, 48, 10004, 11004, 20008, 10101, 48, 10004]
