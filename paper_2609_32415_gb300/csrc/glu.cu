@@ -586,6 +586,8 @@ __global__ void __launch_bounds__(THREADS, 1) glu_kernel(const __grid_constant__
   pdl_launch();
   if (warp != 0) pdl_wait();
 
+  int64_t loads = 0;    // the producer's: stages that it loaded
+  bool issued = false;  // the issuer's: it has issued MMAs
   if (warp == 0) {
     if (lane == 0) {
       // -------------------------------------------------------------- producer (both CTAs)
@@ -605,21 +607,7 @@ __global__ void __launch_bounds__(THREADS, 1) glu_kernel(const __grid_constant__
         else
           ok = pr.unit<KIND, false>(p, u, ctl);
       }
-      const int64_t it = pr.it;
-      if (*abort_flag) {
-        if (rank == 0) {
-          // rank 0's full barriers count both CTAs' bytes of every phase it armed
-          for (int st = 0; st < STAGES; ++st) {
-            const int64_t n_s = (it > st) ? (it - st + STAGES - 1) / STAGES : 0;
-            if (n_s > 0) mbar_wait_drain(full + st, uint32_t((n_s - 1) & 1), p.budget_ns);
-          }
-        } else {
-          // this CTA cannot observe its own loads' completion: give them time to land
-          const uint64_t t0 = globaltimer_ns();
-          while (globaltimer_ns() - t0 < 200000ull) {
-          }
-        }
-      }
+      loads = pr.it;
     }
   } else if (warp == 1) {
     if (lane == 0 && rank == 0) {
@@ -641,10 +629,7 @@ __global__ void __launch_bounds__(THREADS, 1) glu_kernel(const __grid_constant__
         if (!ok) break;
         umma_commit_pair(tfull + buf, 0x3);
       }
-      if (!ok && mma.issued) {
-        umma_commit_pair(drain, 0x1);
-        mbar_wait_drain(drain, 0, p.budget_ns);
-      }
+      issued = mma.issued;
     }
   } else {
     // ---------------------------------------------------------------- epilogue (both CTAs)
@@ -696,6 +681,25 @@ __global__ void __launch_bounds__(THREADS, 1) glu_kernel(const __grid_constant__
   }
   tc_fence_before();
   __syncthreads();
+  // No role waits any more, so the flag is final: it may have been raised after the
+  // producer and the issuer were through. What a CTA that gave up has on its way lands
+  // before the pair's shared memory and TMEM go. (A rank 0 that did not give up has seen
+  // every MMA end, and with them the loads of both CTAs.)
+  if (*abort_flag && lane == 0) {
+    if (warp == 0 && rank == 0) {
+      // rank 0's full barriers count both CTAs' bytes of every phase it armed
+      for (int st = 0; st < STAGES; ++st) {
+        const int64_t n_s = (loads > st) ? (loads - st + STAGES - 1) / STAGES : 0;
+        if (n_s > 0) mbar_wait_drain(full + st, uint32_t((n_s - 1) & 1), p.budget_ns);
+      }
+    }
+    if (warp == 1 && issued) {
+      umma_commit_pair(drain, 0x1);
+      mbar_wait_drain(drain, 0, p.budget_ns);
+    }
+    pause_ns(kLandNs);  // rank 1's loads, and the commits' arrivals at rank 1
+  }
+  __syncwarp();
   cluster_sync_all();
   tc_fence_after();
   if (warp == 1) tmem_dealloc_pair(tmem, TMEM_COLS);
@@ -903,7 +907,9 @@ __global__ void __launch_bounds__(SOME_THREADS) glu_some_kernel(const __grid_con
         for (int s = 0; s < sg.B; ++s, to += sg.nb * 128) tma_load_4d(to, &sg.x, full + st, 64 * (k0 + it), 0, 0, s);
         if (++st == p.ring) st = 0, phase ^= 1;
       }
-      if (*abort_flag)
+      // The CTA does not go before its loads have landed: the products that read them
+      // have ended, or, where a role gave up, each load is waited for.
+      if (it > 0 && !mbar_wait(&done, 0, ctl))
         for (st = 0; st < p.ring && st < it; ++st)
           mbar_wait_drain(full + st, uint32_t((it - 1 - st) / p.ring & 1), p.budget_ns);
     }
@@ -922,9 +928,8 @@ __global__ void __launch_bounds__(SOME_THREADS) glu_some_kernel(const __grid_con
         umma_commit(empty + st);
         if (++st == p.ring) st = 0, phase ^= 1;
       }
-      if (ok) {
-        umma_commit(&done);
-      } else if (it > 0) {
+      if (ok) umma_commit(&done);
+      if (it > 0 && !(ok && mbar_wait(&done, 0, ctl))) {  // nor before its MMAs have ended
         umma_commit(&drain);
         mbar_wait_drain(&drain, 0, p.budget_ns);
       }
@@ -1066,7 +1071,9 @@ __global__ void __launch_bounds__(SOME_THREADS) glu_cols_kernel(const __grid_con
         if (k >= p.span_stages * COLS_BK) k = 0, ++span;
         if (++st == p.ring) st = 0, phase ^= 1;
       }
-      if (*abort_flag)
+      // The CTA does not go before its loads have landed: the products that read them
+      // have ended, or, where a role gave up, each load is waited for.
+      if (it > 0 && !mbar_wait(&done, 0, ctl))
         for (st = 0; st < p.ring && st < it; ++st)
           mbar_wait_drain(full + st, uint32_t((it - 1 - st) / p.ring & 1), p.budget_ns);
     }
@@ -1086,9 +1093,8 @@ __global__ void __launch_bounds__(SOME_THREADS) glu_cols_kernel(const __grid_con
         umma_commit(empty + st);
         if (++st == p.ring) st = 0, phase ^= 1;
       }
-      if (ok) {
-        umma_commit(&done);
-      } else if (it > 0) {
+      if (ok) umma_commit(&done);
+      if (it > 0 && !(ok && mbar_wait(&done, 0, ctl))) {  // nor before its MMAs have ended
         umma_commit(&drain);
         mbar_wait_drain(&drain, 0, p.budget_ns);
       }
