@@ -557,6 +557,8 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_kernel(const __grid_constant_
   pdl_launch();
   if (warp != 0) pdl_wait();
 
+  int64_t loads = 0;    // the producer's: K steps whose loads may be on their way
+  bool issued = false;  // the issuer's: MMAs may be on their way
   if (warp == 0) {
     if (lane == 0) {
       // -------------------------------------------------------------- producer
@@ -585,6 +587,8 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_kernel(const __grid_constant_
           const int64_t n_s = (it > st) ? (it - st + STAGES - 1) / STAGES : 0;
           if (n_s > 0) mbar_wait_drain(full + st, uint32_t((n_s - 1) & 1), p.budget_ns);
         }
+      } else {
+        loads = it;
       }
     }
   } else if (warp == 1) {
@@ -594,7 +598,7 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_kernel(const __grid_constant_
       const uint32_t s0 = smem_u32(smem), tmem = SPLIT ? *tmem_slot : tmem0;
       int64_t it = 0;
       int i = 0;
-      bool ok = true, issued = false;
+      bool ok = true;
       Walk<BM, EPI> walk;
       Tile tl;
       for (int64_t t = t0; ok && tile_at<EPI, SPLIT>(p, walk, t, tl); t += step) {
@@ -621,6 +625,7 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_kernel(const __grid_constant_
       if (!ok && issued) {
         umma_commit(drain);
         mbar_wait_drain(drain, 0, p.budget_ns);
+        issued = false;
       }
     }
   } else {
@@ -669,6 +674,20 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_kernel(const __grid_constant_
   }
   tc_fence_before();
   __syncthreads();
+  // No role waits any more, so the flag is final: it may have been raised after the
+  // producer and the issuer were through. What this CTA has on its way lands first.
+  if (*abort_flag && lane == 0) {
+    if (warp == 0)
+      for (int st = 0; st < STAGES; ++st) {
+        const int64_t n_s = (loads > st) ? (loads - st + STAGES - 1) / STAGES : 0;
+        if (n_s > 0) mbar_wait_drain(full + st, uint32_t((n_s - 1) & 1), p.budget_ns);
+      }
+    if (warp == 1 && issued) {
+      umma_commit(drain);
+      mbar_wait_drain(drain, 0, p.budget_ns);
+    }
+  }
+  __syncwarp();
   if (warp == 1) {
     tc_fence_after();
     tmem_dealloc(SPLIT ? *tmem_slot : tmem0, TMEM_COLS);
@@ -723,6 +742,8 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_pair_kernel(const __grid_cons
   pdl_launch();
   if (warp != 0) pdl_wait();
 
+  int64_t loads = 0;    // the producer's: stages that it loaded
+  bool issued = false;  // the issuer's: it has issued MMAs
   if (warp == 0) {
     if (lane == 0) {
       // -------------------------------------------------------------- producer (both CTAs)
@@ -753,20 +774,7 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_pair_kernel(const __grid_cons
           }
         }
       }
-      if (*abort_flag) {
-        if (rank == 0) {
-          // rank 0's full barriers count both CTAs' bytes of every phase it armed
-          for (int st = 0; st < P_STAGES; ++st) {
-            const int64_t n_s = (it > st) ? (it - st + P_STAGES - 1) / P_STAGES : 0;
-            if (n_s > 0) mbar_wait_drain(full + st, uint32_t((n_s - 1) & 1), p.budget_ns);
-          }
-        } else {
-          // this CTA cannot observe its own loads' completion: give them time to land
-          const uint64_t t0 = globaltimer_ns();
-          while (globaltimer_ns() - t0 < 200000ull) {
-          }
-        }
-      }
+      loads = it;
     }
   } else if (warp == 1) {
     if (lane == 0 && rank == 0) {
@@ -775,7 +783,7 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_pair_kernel(const __grid_cons
       const uint32_t s0 = smem_u32(smem);
       int64_t it = 0;
       int i = 0;
-      bool ok = true, issued = false;
+      bool ok = true;
       Walk<P_TM, EPI> walk;
       Tile tl;
       const int64_t end = round_tiles<P_TM, EPI>(p);
@@ -803,10 +811,6 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_pair_kernel(const __grid_cons
         if (!ok) break;
         umma_commit_pair(tfull + buf, 0x3);
         ++i;
-      }
-      if (!ok && issued) {
-        umma_commit_pair(drain, 0x1);
-        mbar_wait_drain(drain, 0, p.budget_ns);
       }
     }
   } else {
@@ -847,6 +851,24 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_pair_kernel(const __grid_cons
   }
   tc_fence_before();
   __syncthreads();
+  // No role waits any more, so the flag is final. What a CTA that gave up has on its way
+  // lands before the pair's shared memory and TMEM go. (A rank 0 that did not give up has
+  // seen every MMA end, and with them the loads of both CTAs.)
+  if (*abort_flag && lane == 0) {
+    if (warp == 0 && rank == 0) {
+      // rank 0's full barriers count both CTAs' bytes of every phase it armed
+      for (int st = 0; st < P_STAGES; ++st) {
+        const int64_t n_s = (loads > st) ? (loads - st + P_STAGES - 1) / P_STAGES : 0;
+        if (n_s > 0) mbar_wait_drain(full + st, uint32_t((n_s - 1) & 1), p.budget_ns);
+      }
+    }
+    if (warp == 1 && issued) {
+      umma_commit_pair(drain, 0x1);
+      mbar_wait_drain(drain, 0, p.budget_ns);
+    }
+    pause_ns(kLandNs);  // rank 1's loads, and the commits' arrivals at rank 1
+  }
+  __syncwarp();
   cluster_sync_all();
   tc_fence_after();
   if (warp == 1) tmem_dealloc_pair(tmem, TMEM_COLS);
