@@ -631,8 +631,9 @@ ra_status refadapt_residual_norm_backward(const ra_resnorm_grad_args* args, void
  * C and F multiples of 8, at least 64; pointers 16-byte aligned, row strides
  * multiples of 8 elements and at least the row's length. A segment with gated =
  * 1 is skipped for samples whose mode is RA_MODE_REUSE. err_word: device int32
- * or NULL; bit 0 set if a device wait timed out. Outputs must not overlap inputs
- * or one another; B * rows below 2^30. Deterministic; how a call is cut into
+ * or NULL; bit 0 set if a device wait timed out. No output of any segment may
+ * overlap an input or another output (refused where tensors start at one address
+ * or fill ranges that meet); B * rows below 2^30. Deterministic; how a call is cut into
  * tiles follows from its sizes. */
 typedef enum { RA_ACT_SILU = 0, RA_ACT_GELU = 1 } ra_act;
 
@@ -676,7 +677,8 @@ ra_status refadapt_glu(const ra_glu_args* args, void* stream);
  *                      bytes (on the device that is current), 16-byte aligned;
  *                      calls that share it must be stream-ordered.
  * C, F, O multiples of 8, at least 64; pointers and strides as for refadapt_glu;
- * outputs must not overlap inputs. Rows of zero: the weights' gradients are zero. Deterministic. */
+ * neither outputs nor the workspace may overlap inputs or one another. Rows of
+ * zero: the weights' gradients are zero. Deterministic. */
 typedef struct {
   int32_t B, rows, C, F, O, act;
   const void* dy;

@@ -1213,6 +1213,8 @@ bool check_rows(const char* who, const char* what, const RowTensor& t, bool outp
             t.cols);
   return false;
 }
+RowSpan span_of(const RowTensor& t) { return RowSpan{t.ptr, 2 * t.ss, 2 * t.sr, t.B, t.n, int64_t(2) * t.cols}; }
+RowSpan span_of(const void* ptr, int64_t bytes) { return RowSpan{ptr, 0, 0, 1, 1, bytes}; }
 // The samples' rows follow one another: B samples of n rows are one of B n.
 bool joins(const RowTensor& t) { return t.B == 1 || t.ss == t.n * t.sr; }
 
@@ -1490,6 +1492,8 @@ extern "C" ra_status refadapt_glu(const ra_glu_args* a, void* stream) {
   p.err_word = a->err_word;
   p.budget_ns = wait_budget_ns();
   RowTensor x[3];
+  RowSpan ins[9], all_out[9];  // of all segments
+  int n_in = 0, n_out = 0;
   for (int g = 0; g < a->n_seg; ++g) {
     const ra_glu_seg& s = a->seg[g];
     if (s.rows < 0) {
@@ -1521,11 +1525,10 @@ extern "C" ra_status refadapt_glu(const ra_glu_args* a, void* stream) {
       set_error("%s: seg %d: too many rows", who, g);
       return RA_EINVAL;
     }
-    for (int i = 0; i < outs; ++i)
-      if (o[i].ptr == s.x || (i > 0 && (o[i].ptr == s.out || s.pre_gate == s.pre_up))) {
-        set_error("%s: seg %d: x, out, pre_gate and pre_up must not overlap", who, g);
-        return RA_EINVAL;
-      }
+    ins[n_in++] = span_of(r);
+    ins[n_in++] = span_of(s.w_gate, int64_t(2) * a->F * a->C);
+    ins[n_in++] = span_of(s.w_up, int64_t(2) * a->F * a->C);
+    for (int i = 0; i < outs; ++i) all_out[n_out++] = span_of(o[i]);
     // samples whose rows follow one another share row tiles
     bool flat = !s.gated && joins(r);
     for (int i = 0; i < outs; ++i) flat &= joins(o[i]);
@@ -1546,6 +1549,10 @@ extern "C" ra_status refadapt_glu(const ra_glu_args* a, void* stream) {
       job.out[i] = Rows{static_cast<__nv_bfloat16*>(const_cast<void*>(o[i].ptr)), o[i].ss, o[i].sr};
   }
   if (p.n_jobs == 0) return RA_OK;
+  if (overlapping(all_out, n_out, ins, n_in) >= 0) {
+    set_error("%s: an output must not overlap an input or another output of any segment", who);
+    return RA_EINVAL;
+  }
   int most = 0;
   for (int g = 0; g < a->n_seg; ++g)
     if (int64_t(a->B) * a->seg[g].rows > most) most = a->B * a->seg[g].rows;
@@ -1724,10 +1731,6 @@ extern "C" ra_status refadapt_glu_backward(const ra_glu_grad_args* a, void* stre
       ((a->dw_gate || a->dw_up) && !check_rows(who, "x", x, false)) ||
       (a->dw_down && !check_rows(who, "hidden", hid, false)) || (a->dx && !check_rows(who, "dx", dx, true)))
     return RA_EINVAL;
-  if (a->dx && (a->dx == a->dy || a->dx == a->x || a->dx == a->hidden || a->dx == a->pre_gate || a->dx == a->pre_up)) {
-    set_error("%s: dx must not overlap an input", who);
-    return RA_EINVAL;
-  }
   if ((dgw && (!a->w_down || !aligned16(a->w_down))) ||
       (a->dx && (!a->w_gate || !a->w_up || !aligned16(a->w_gate) || !aligned16(a->w_up)))) {
     set_error("%s: the weights that the wanted gradients need must be given and 16-byte aligned", who);
@@ -1737,6 +1740,15 @@ extern "C" ra_status refadapt_glu_backward(const ra_glu_grad_args* a, void* stre
   if (!a->workspace || !aligned16(a->workspace) || a->workspace_bytes < need) {
     set_error("%s: workspace NULL, not 16-byte aligned or smaller than refadapt_glu_backward_workspace_size() (%zu bytes)",
               who, need);
+    return RA_EINVAL;
+  }
+  const int64_t fc = int64_t(2) * a->F * a->C, of = int64_t(2) * a->O * a->F;
+  const RowSpan ins[] = {span_of(dy), span_of(x), span_of(g), span_of(w), span_of(hid), span_of(a->w_gate, fc),
+                         span_of(a->w_up, fc), span_of(a->w_down, of)};
+  const RowSpan outs[] = {span_of(dx), span_of(a->dw_gate, fc), span_of(a->dw_up, fc), span_of(a->dw_down, of),
+                          span_of(a->workspace, int64_t(need))};
+  if (overlapping(outs, 5, ins, 8) >= 0) {
+    set_error("%s: dx, the weights' gradients and the workspace must not overlap an input or one another", who);
     return RA_EINVAL;
   }
   const int sms = num_sms();

@@ -51,4 +51,34 @@ class ClusterTable {
   int used_ = 0;
 };
 
+// Rows of a tensor in memory: B samples of n rows of `bytes` bytes, strides in bytes.
+struct RowSpan {
+  const void* ptr;  // NULL: absent
+  int64_t ss, sr, B, n, bytes;
+};
+// Do two tensors share memory for certain: they start at one address, or both fill their
+// range and the ranges meet? (Rows side by side in one buffer do not.)
+inline bool surely_overlap(const RowSpan& a, const RowSpan& b) {
+  if (!a.ptr || !b.ptr || a.B * a.n * a.bytes < 1 || b.B * b.n * b.bytes < 1) return false;
+  if (a.ptr == b.ptr) return true;
+  auto fills = [](const RowSpan& t) {  // sample after sample, or row after row of all samples
+    return ((t.n == 1 || t.sr == t.bytes) && (t.B == 1 || t.ss == t.n * t.bytes)) ||
+           (t.ss == t.bytes && t.sr == t.B * t.bytes);
+  };
+  if (!fills(a) || !fills(b)) return false;
+  const uintptr_t pa = reinterpret_cast<uintptr_t>(a.ptr), pb = reinterpret_cast<uintptr_t>(b.ptr);
+  return pa < pb ? pb - pa < uintptr_t(a.B * a.n * a.bytes) : pa - pb < uintptr_t(b.B * b.n * b.bytes);
+}
+// The first of n_out tensors that shares memory with another of them or with one of n_in
+// inputs; -1: none.
+inline int overlapping(const RowSpan* out, int n_out, const RowSpan* in, int n_in) {
+  for (int i = 0; i < n_out; ++i) {
+    for (int j = 0; j < n_in; ++j)
+      if (surely_overlap(out[i], in[j])) return i;
+    for (int j = 0; j < i; ++j)
+      if (surely_overlap(out[i], out[j])) return i;
+  }
+  return -1;
+}
+
 }  // namespace ra

@@ -42,3 +42,30 @@ def test_resident_clusters_are_those_of_the_device_and_kernel(tmp_path):
       printf("%d\n", count(1, 0, 500, 4));
     """)
     assert [int(v) for v in got] == [0, 1, 10004, 11004, 20008, 10101, 48, 10004, 11004, 20008, 10101, 48, 10004]
+
+
+def test_overlap_of_rows_is_seen_where_it_is_certain(tmp_path):
+    """Against the sets of bytes: never said of tensors apart, always of one address and of dense ranges."""
+    import itertools
+    spans = [(0, 0, 64, 1, 4, 64), (64, 0, 64, 1, 4, 64), (192, 0, 64, 1, 1, 64), (256, 256, 64, 2, 4, 64),
+             (0, 0, 128, 1, 4, 64), (64, 0, 128, 1, 4, 64), (0, 512, 128, 2, 4, 64), (0, 64, 128, 2, 4, 64),
+             (240, 0, 0, 1, 1, 16), (256, 0, 0, 1, 1, 0), (0, 64, 0, 4, 1, 64), (64, 0, 64, 1, 0, 64)]
+    body = "const char* base = reinterpret_cast<const char*>(1 << 20);\nconst ra::RowSpan t[] = {%s};\n" % ", ".join(
+        "{base + %d, %d, %d, %d, %d, %d}" % s for s in spans)
+    body += 'for (auto& a : t) for (auto& b : t) printf("%d\\n", int(ra::surely_overlap(a, b)));\n'
+    body += 'ra::RowSpan gone = t[0]; gone.ptr = nullptr; printf("%d\\n", int(ra::surely_overlap(gone, gone)));'
+    got = [bool(int(v)) for v in run(tmp_path, body)]
+
+    def bytes_of(at, ss, sr, B, n, size):
+        return {at + s * ss + r * sr + i for s in range(B) for r in range(n) for i in range(size)}
+
+    def dense(at, ss, sr, B, n, size):
+        return len(bytes_of(at, ss, sr, B, n, size)) == max(bytes_of(at, ss, sr, B, n, size), default=0) - at + 1 == B * n * size
+
+    for (a, b), said in zip(itertools.product(spans, spans), got):
+        shared = bool(bytes_of(*a) & bytes_of(*b))
+        if said:
+            assert shared, (a, b)
+        elif shared:
+            assert a[0] != b[0] and not (dense(*a) and dense(*b)), (a, b)
+    assert got[-1] is False
