@@ -611,16 +611,15 @@ __global__ void __launch_bounds__(NUM_THREADS, 1) joint_attn_kernel(const __grid
         if ((store_kv || store_q) && !*abort_flag && v_issued == nkv) store_tiles(nkv - 1);
         // Shared memory must outlive the reads of every store issued.
         if (store_kv || store_q) bulk_wait_read_all();
-        if (*abort_flag) {
-          // Let every load this thread issued land before the CTA exits: stage s
-          // received loads for j = s, s + S, ...; wait for the last one's phase.
-          mbar_wait_drain(q_full, 0, p.budget_ns);
-          for (int s = 0; s < S; ++s) {
-            const int nk = (k_issued > s) ? (k_issued - s + S - 1) / S : 0;
-            const int nv = (v_issued > s) ? (v_issued - s + S - 1) / S : 0;
-            if (nk > 0) mbar_wait_drain(k_full + s, (nk - 1) & 1, p.budget_ns);
-            if (nv > 0) mbar_wait_drain(v_full + s, (nv - 1) & 1, p.budget_ns);
-          }
+        // Every load this thread issued lands before the CTA exits, whatever another
+        // role gives up on after this one is through: stage s received loads for
+        // j = s, s + S, ...; wait for the last one's phase.
+        mbar_wait_drain(q_full, 0, p.budget_ns);
+        for (int s = 0; s < S; ++s) {
+          const int nk = (k_issued > s) ? (k_issued - s + S - 1) / S : 0;
+          const int nv = (v_issued > s) ? (v_issued - s + S - 1) / S : 0;
+          if (nk > 0) mbar_wait_drain(k_full + s, (nk - 1) & 1, p.budget_ns);
+          if (nv > 0) mbar_wait_drain(v_full + s, (nv - 1) & 1, p.budget_ns);
         }
       }
       if (DUAL && store_q) {  // the store of Q has read its buffer (merge_dual)
@@ -706,7 +705,7 @@ __global__ void __launch_bounds__(NUM_THREADS, 1) joint_attn_kernel(const __grid
             if (next) umma_commit(k_empty + (j + 1) % S);
           }
         }
-        if (!ok && issued_any) {
+        if (issued_any) {  // and its MMAs end
           umma_commit(drain);
           mbar_wait_drain(drain, 0, p.budget_ns);
         }
