@@ -200,11 +200,10 @@ __global__ void __launch_bounds__(THREADS, 1) q_delta_kernel(const __grid_consta
         }
         ++issued;
       }
-      if (*abort_flag) {
-        for (int s = 0; s < STAGES; ++s) {
-          const int n_s = (issued > s) ? (issued - s + STAGES - 1) / STAGES : 0;
-          if (n_s > 0) mbar_wait_drain(full + s, (n_s - 1) & 1, p.budget_ns);
-        }
+      // Every load lands before the CTA exits, whatever a consumer gives up on.
+      for (int s = 0; s < STAGES; ++s) {
+        const int n_s = (issued > s) ? (issued - s + STAGES - 1) / STAGES : 0;
+        if (n_s > 0) mbar_wait_drain(full + s, (n_s - 1) & 1, p.budget_ns);
       }
     }
   } else {
@@ -418,11 +417,10 @@ __global__ void __launch_bounds__(ClLayout<S, UB>::THREADS)
         }
         ++issued;
       }
-      if (*abort_flag) {
-        for (int s = 0; s < CL_STAGES; ++s) {
-          const int n_s = (issued > s) ? (issued - s + CL_STAGES - 1) / CL_STAGES : 0;
-          if (n_s > 0) mbar_wait_drain(full + s, (n_s - 1) & 1, p.budget_ns);
-        }
+      // Every load lands before the CTA exits, whatever a consumer gives up on.
+      for (int s = 0; s < CL_STAGES; ++s) {
+        const int n_s = (issued > s) ? (issued - s + CL_STAGES - 1) / CL_STAGES : 0;
+        if (n_s > 0) mbar_wait_drain(full + s, (n_s - 1) & 1, p.budget_ns);
       }
     }
   } else {
