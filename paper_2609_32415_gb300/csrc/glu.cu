@@ -26,11 +26,15 @@
 //               (rank 0's).
 //   warps 2..9  epilogue, two warps per TMEM lane quarter, while the next tile's
 //               MMAs fill the other accumulator.
-// Measured: 4352 rows, 2048 -> 8192: forward 175 us, 1.67 PFLOP/s, 84-87 % of the tensor
-// cores' measured rate (14.3 rounds of tiles take 15, and the clock sinks under the power
-// cap). Backward, 4333 rows, 557-574 us, 1.52-1.56 PFLOP/s: GRAD 115 us, where the MMAs
-// alone are 82 (its epilogue moves four F-wide tensors through the shared memory that
+// Measured: 4352 rows, 2048 -> 8192: forward 177-182 us, 1.61-1.65 PFLOP/s, 84-86 % of the
+// tensor cores' measured rate (14.3 rounds of tiles take 15, and the clock sinks under the
+// power cap). Backward, 4333 rows, 564-576 us, 1.51-1.55 PFLOP/s: GRAD 115 us, where the
+// MMAs alone are 82 (its epilogue moves four F-wide tensors through the shared memory that
 // feeds the MMAs), STORE 445.
+// dg and dw are rounded to bf16 on their way to the products of dx and the weights'
+// gradients. It is the one rounding beside the results' own, and puts their error at 2.3e-3
+// where 32-bit dg and dw give 1.7e-3. The MMAs of bf16 weights and rows take operands of one
+// type: 32 bits would mean tf32 at half the rate, with the weights and rows widened too.
 // Calls of few rows read (backward: and write) the weights once and little else, and
 // have kernels of their own: forward up to 128 rows glu_rows_kernel and
 // glu_some_kernel, du and dx of few rows glu_cols_kernel.
@@ -1897,7 +1901,9 @@ extern "C" ra_status refadapt_glu_backward(const ra_glu_grad_args* a, void* stre
     return RA_EINVAL;
   }
   const int64_t ctas = units < pairs ? units : pairs;
-  if (ctas < pairs) p.order.early = 0;  // one unit a pair
+  // Fewer units than pairs: the plan's early rounds do not fit. A pair with one of dx's
+  // units takes another `longs` units further on, and as many pairs take none.
+  if (ctas < pairs) p.order.early = 0;
   const ra_status r = launch<STORE>(who, glu_kernel<STORE, 0>, p, units, st);
   if (r != RA_OK || join.n == 0) return r;
   cudaLaunchConfig_t cfg = {};

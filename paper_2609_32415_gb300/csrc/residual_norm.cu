@@ -524,7 +524,7 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) residual_norm_kernel(const __g
 // mean at the end: (mean - K)^2 is at most C / 8 times the variance, whatever the
 // values, so the difference keeps the variance to (C / 8 + 1) of the sum's own
 // roundings; a pass over the slot for the mean is saved.
-// 8192 rows of 2560, two kinds of norms with weights, sums included: 50 us, 5.1 TB/s;
+// 8192 rows of 2560, two kinds of norms with weights, sums included: 51 us, 4.9 TB/s;
 // 32,768 rows 158 us, 6.4 TB/s, where a copy of the same bytes takes 151: the pipeline
 // of ten rows fills and drains once in a run of 54. (Slots filled by the row warps'
 // own 16-byte copies, means in a pass of their own: 57. Teams of two or three warps a
