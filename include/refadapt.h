@@ -707,6 +707,219 @@ typedef struct {
 size_t refadapt_glu_backward_workspace_size(int32_t B, int32_t rows, int32_t C, int32_t F, int32_t O);
 ra_status refadapt_glu_backward(const ra_glu_grad_args* args, void* stream);
 
+/* ------------------------------------------------------------------ linear layers in 4 bits
+ * Products of microscaled 4-bit matrices, on the tensor cores' 4-bit rate: rows
+ * and weights in 4 bits with a scale for every few columns, the sums in fp32, the
+ * epilogues of refadapt_gemm. All calls are asynchronous on `stream` and allocate
+ * nothing; invalid arguments return RA_EINVAL before anything is launched.
+ *
+ * A 4-bit matrix of R rows and K columns:
+ *  codes   two e2m1 values a byte, the even column in the low half: [R][K / 2].
+ *          e2m1: sign in bit 3, then 0, 0.5, 1, 1.5, 2, 3, 4, 6.
+ *  scales  one byte for each block of columns of a row, in tiles of 128 rows by
+ *          four blocks, 512 bytes, [ceil(R / 128)][ceil(K / (4 block))][512]: row r
+ *          and block j of a tile at 16 (r % 32) + 4 (r / 32) + j. What lies behind
+ *          the last row or block is zero.
+ *            RA_Q4_E4M3  blocks of 16; e4m3 value times 2^exponent (one exponent
+ *                        for the matrix, of the caller's choice)
+ *            RA_Q4_E8M0  blocks of 32; 2^(byte - 127); exponent 0
+ * A value is its e2m1 value times its scale. refadapt_quant4_scales_size: bytes of
+ * one matrix's scales; 0 if rows or K are negative or the format is unknown.
+ */
+typedef enum { RA_Q4_E4M3 = 0, RA_Q4_E8M0 = 1 } ra_q4_format;
+
+size_t refadapt_quant4_scales_size(int32_t rows, int32_t K, int32_t format);
+
+/* refadapt_quant4 — bf16 rows to 4 bits, along their features (codes, scales: each
+ * sample's rows a matrix of C columns), along the rows (codes_t, scales_t: the
+ * transposed matrix of all samples' rows, C rows of ceil(B rows / 64) * 64 columns,
+ * zeros behind the last), or both. Per block, amax its largest magnitude:
+ *   RA_Q4_E4M3  scale = e4m3(amax / 2^exponent / 6), at most 448 (exact to the
+ *               nearest, ties to even; larger blocks saturate)
+ *   RA_Q4_E8M0  scale = the smallest power of two (2^-126 or more) with
+ *               amax <= 6 scale
+ *   value       x / (scale 2^exponent) to the nearest e2m1 value, ties to even,
+ *               saturating; 0 where the scale is 0
+ * A block with a value that is not finite gets a scale that is NaN (0x7f, 0xff).
+ *
+ *  x           bf16 rows of C features; pointer 16-byte aligned, strides multiples
+ *              of 8 elements, row stride >= C.
+ *  codes       [B][rows][C / 2], 16-byte aligned, strides in bytes, multiples of 16;
+ *              C a multiple of 64.
+ *  scales      [B][ceil(rows / 128)][..][512] contiguous, 16-byte aligned.
+ *  codes_t     C rows of codes_t_stride bytes (a multiple of 16), 16-byte aligned; C
+ *              a multiple of 8.
+ *  scales_t    as of one matrix of C rows, contiguous, 16-byte aligned.
+ *  exponent    -64 to 64; 0 for RA_Q4_E8M0.
+ * codes and scales go together, codes_t and scales_t too; no output may overlap x or
+ * another output. A segment with gated = 1 is skipped for samples whose mode is
+ * RA_MODE_REUSE (not with codes_t). B * rows of a segment below 2^30. */
+typedef struct {
+  const void* x;
+  int64_t x_stride_s, x_stride_r;
+  void* codes;
+  int64_t codes_stride_s, codes_stride_r;  /* bytes */
+  void* scales;
+  void* codes_t;
+  int64_t codes_t_stride;                  /* bytes */
+  void* scales_t;
+  int32_t rows;       /* rows per sample, >= 0 */
+  int32_t gated;
+  int32_t exponent, reserved;
+} ra_quant4_seg;
+
+typedef struct {
+  int32_t B, C, n_seg, format;
+  ra_quant4_seg seg[3];
+  const int32_t* mode;  /* device [B]; required when a segment is gated */
+} ra_quant4_args;
+
+ra_status refadapt_quant4(const ra_quant4_args* args, void* stream);
+
+/* refadapt_gemm4 — refadapt_gemm with 4-bit operands of one format:
+ *   out = epilogue(2^(a_exponent + w_exponent) A W^T + bias)
+ * with exact products and fp32 sums. lin.a: codes, its strides in bytes (multiples of
+ * 16, a_stride_r >= K / 2); lin.w: codes [N][K / 2]; a_scales, w_scales as above; all
+ * 16-byte aligned. N a multiple of 64 (QKV: as for refadapt_gemm), K of 64. The other
+ * fields, the epilogues, gates, tile_mode and err_word are refadapt_gemm's. No output
+ * may overlap an input (but out may be resid) or another output. Deterministic; the
+ * order of the fp32 sums follows from the sizes of the call. */
+typedef struct {
+  ra_gemm_seg lin;
+  const void* a_scales;
+  const void* w_scales;
+  int32_t a_exponent, w_exponent;
+} ra_gemm4_seg;
+
+typedef struct {
+  int32_t B, N, K, epilogue;
+  int32_t H, d, n_seg, rope_len;       /* H, d, rope_len: QKV only */
+  ra_gemm4_seg seg[3];
+  const int32_t* mode;                 /* device [B]; required when a segment is gated */
+  const float* rope;                   /* QKV: [rope_len][d/2][2] */
+  float norm_eps;
+  int32_t tile_mode;                   /* as ra_gemm_args */
+  int32_t* err_word;
+  int32_t format;                      /* ra_q4_format */
+  int32_t reserved;
+} ra_gemm4_args;
+
+ra_status refadapt_gemm4(const ra_gemm4_args* args, void* stream);
+
+/* refadapt_linear4_backward — gradients of y = x W^T through 4-bit products, all
+ * operands in RA_Q4_E8M0 along the axis that is summed over (Q):
+ *   dx = Q(dy) Q(W^T)^T,   dw = Q(dy^T) Q(x^T)^T
+ *  dy, x        bf16 rows of N and K features; w bf16 [N][K] contiguous.
+ *  dx           bf16 rows of K features, each sample's right behind those of the one
+ *               before (dx_stride_s = rows * dx_stride_r), or NULL (then w may be NULL).
+ *  dw           bf16 [N][K] contiguous, or NULL (then x may be NULL). Not both NULL.
+ *  workspace    device scratch of refadapt_linear4_backward_workspace_size() bytes,
+ *               16-byte aligned; calls that share it must be stream-ordered.
+ * N and K multiples of 64; pointers 16-byte aligned, strides multiples of 8 elements;
+ * neither outputs nor the workspace may overlap inputs or one another. Rows of zero:
+ * dw is zero. B * rows below 2^30. Deterministic. */
+typedef struct {
+  int32_t B, rows, K, N;
+  const void* dy;
+  int64_t dy_stride_s, dy_stride_r;
+  const void* x;
+  int64_t x_stride_s, x_stride_r;
+  const void* w;
+  void* dx;
+  int64_t dx_stride_s, dx_stride_r;
+  void* dw;
+  void* workspace;
+  size_t workspace_bytes;
+  int32_t* err_word;
+} ra_linear4_grad_args;
+
+size_t refadapt_linear4_backward_workspace_size(int32_t B, int32_t rows, int32_t K, int32_t N);
+ra_status refadapt_linear4_backward(const ra_linear4_grad_args* args, void* stream);
+
+/* ------------------------------------------------------------------ the optimiser's step
+ * What turns gradients into weights, over any number of tensors in one call.
+ */
+
+typedef enum { RA_F32 = 0, RA_BF16 = 1 } ra_type;
+
+/* refadapt_grad_norm — out[0] = sqrt(sum of g^2) over the elements of all tensors,
+ * out[1] = min(1, max_norm / out[0]), the factor that clips them to max_norm (out[1]
+ * is NaN where the norm is not finite). Squares are formed in fp32 (a gradient beyond
+ * 1.8e19 makes the norm infinite), summed in fp32 over a few hundred elements and in
+ * fp64 above that, in a fixed order (deterministic).
+ *  tensors    host array; g device, fp32 or bf16, aligned to its type, n >= 0 elements.
+ *  max_norm   > 0 (INFINITY: no clipping).
+ *  out        device fp32 [2].
+ *  workspace  device scratch of refadapt_grad_norm_workspace_size() bytes, 16-byte
+ *             aligned, zero-filled once before its first use; every call leaves it ready
+ *             for the next. Calls that share it must be stream-ordered. */
+typedef struct {
+  const void* g;
+  int64_t n;
+  int32_t type;       /* ra_type */
+  int32_t reserved;
+} ra_grad;
+
+size_t refadapt_grad_norm_workspace_size(void);
+ra_status refadapt_grad_norm(const ra_grad* tensors, int32_t n_tensors, float max_norm, float* out, void* workspace,
+                             size_t workspace_bytes, void* stream);
+
+/* refadapt_adamw — one step of Adam with decoupled weight decay, over all tensors:
+ *   g' = c g                   c = *grad_scale (device), or 1
+ *   m  = beta1 m + (1 - beta1) g'
+ *   v  = beta2 v + (1 - beta2) g'^2
+ *   p  = p - lr decay p - lr (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps)
+ * in fp32, p in place, its rounding to bf16 in w. Where c is not finite the call
+ * changes nothing.
+ *  bits = 32  m and v are fp32.
+ *  bits = 8   m and v are e4m3 in blocks of 32 elements, with a power of two (e8m0
+ *             byte, 2^(byte - 127)) for each in m_scale and v_scale: the smallest one
+ *             (2^-126 or more) with amax <= 448 scale. New moments are rounded to one
+ *             of the two e4m3 values beside them so that the mean is kept: with r of 16
+ *             random bits, the upper one where the part above the lower one is at least
+ *             1 - (16 r + 8) / 2^20 of the step. (Rounding to the nearest would hold v
+ *             where it is: a step changes it by 0.1 %.) A second moment above zero is
+ *             at least the smallest step. The update uses the moments before this
+ *             rounding. A block with a moment that is not finite gets the scale NaN
+ *             (0xff). r is the low (m) and the high (v) half of
+ *               mix(i * 0x9e3779b1 ^ key),  i the element, counted over the call's
+ *             tensors, each from the next multiple of 32 on; key = mix(mix(mix(low
+ *             half of seed) ^ high half) ^ t), and where i passes 32 bits mix(key ^ its
+ *             upper half); mix(x): x ^= x >> 16, x *= 0x243f6a89, x ^= x >> 15,
+ *             x *= 0xb7e15163, x ^= x >> 16, all in 32 bits.
+ *  tensors    host array. p fp32, g fp32 or bf16, w bf16 or NULL; n >= 0 elements,
+ *             contiguous, each pointer aligned to its type (16 bytes is fastest). No
+ *             output may overlap an input or another output.
+ *  lr, step   the rate and the number t >= 1 of the step; lr_dev, step_dev: device fp32
+ *             and int32, or NULL, which count instead (a captured call then goes on with
+ *             what they hold when it is replayed; a step below 1 there counts as 1).
+ *  beta1, beta2 in [0, 1), eps > 0, decay >= 0, lr >= 0. */
+typedef struct {
+  void* p;
+  const void* g;
+  void* m;
+  void* v;
+  void* m_scale;      /* bits = 8: [ceil(n / 32)] */
+  void* v_scale;
+  void* w;
+  int64_t n;
+  int32_t g_type;     /* ra_type */
+  int32_t reserved;
+} ra_adamw_tensor;
+
+typedef struct {
+  const ra_adamw_tensor* tensors;
+  int32_t n_tensors, bits;
+  double lr, beta1, beta2, eps, decay;
+  int64_t step;
+  const float* lr_dev;
+  const int32_t* step_dev;
+  const float* grad_scale;
+  uint64_t seed;
+} ra_adamw_args;
+
+ra_status refadapt_adamw(const ra_adamw_args* args, void* stream);
+
 /* ------------------------------------------------------------------ misc */
 const char* refadapt_status_string(ra_status s);
 const char* refadapt_last_error(void);

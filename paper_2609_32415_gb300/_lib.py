@@ -26,11 +26,15 @@ EXPORTED = (
     "refadapt_ln_modulate", "refadapt_gemm", "refadapt_q_delta_gate", "refadapt_last_launch",
     "refadapt_rope_axes", "refadapt_rope_axes_table", "refadapt_residual_norm", "refadapt_residual_norm_backward",
     "refadapt_residual_norm_backward_workspace_size", "refadapt_glu", "refadapt_glu_backward",
-    "refadapt_glu_backward_workspace_size",
+    "refadapt_glu_backward_workspace_size", "refadapt_quant4_scales_size", "refadapt_quant4", "refadapt_gemm4",
+    "refadapt_linear4_backward_workspace_size", "refadapt_linear4_backward", "refadapt_grad_norm_workspace_size",
+    "refadapt_grad_norm", "refadapt_adamw",
 )
 RA_EPI_STORE, RA_EPI_GELU, RA_EPI_RESID, RA_EPI_QKV = 0, 1, 2, 3
 RA_NORM_NONE, RA_NORM_LAYER, RA_NORM_RMS = 0, 1, 2
 RA_ACT_SILU, RA_ACT_GELU = 0, 1
+RA_Q4_E4M3, RA_Q4_E8M0 = 0, 1
+RA_F32, RA_BF16 = 0, 1
 
 
 class RaSeg(ctypes.Structure):
@@ -140,6 +144,51 @@ class RaGluGradArgs(ctypes.Structure):
         ("workspace_bytes", c_size_t), ("err_word", c_void_p)]
 
 
+class RaQuant4Seg(ctypes.Structure):
+    _fields_ = _rows("x", "codes") + [("scales", c_void_p), ("codes_t", c_void_p), ("codes_t_stride", c_int64),
+                                      ("scales_t", c_void_p), ("rows", c_int32), ("gated", c_int32),
+                                      ("exponent", c_int32), ("reserved", c_int32)]
+
+
+class RaQuant4Args(ctypes.Structure):
+    _fields_ = [("B", c_int32), ("C", c_int32), ("n_seg", c_int32), ("format", c_int32), ("seg", RaQuant4Seg * 3),
+                ("mode", c_void_p)]
+
+
+class RaGemm4Seg(ctypes.Structure):
+    _fields_ = [("lin", RaGemmSeg), ("a_scales", c_void_p), ("w_scales", c_void_p), ("a_exponent", c_int32),
+                ("w_exponent", c_int32)]
+
+
+class RaGemm4Args(ctypes.Structure):
+    _fields_ = [("B", c_int32), ("N", c_int32), ("K", c_int32), ("epilogue", c_int32),
+                ("H", c_int32), ("d", c_int32), ("n_seg", c_int32), ("rope_len", c_int32),
+                ("seg", RaGemm4Seg * 3), ("mode", c_void_p), ("rope", c_void_p),
+                ("norm_eps", c_float), ("tile_mode", c_int32), ("err_word", c_void_p), ("format", c_int32),
+                ("reserved", c_int32)]
+
+
+class RaLinear4GradArgs(ctypes.Structure):
+    _fields_ = [("B", c_int32), ("rows", c_int32), ("K", c_int32), ("N", c_int32)] + _rows("dy", "x") + [
+        ("w", c_void_p)] + _rows("dx") + [("dw", c_void_p), ("workspace", c_void_p), ("workspace_bytes", c_size_t),
+                                          ("err_word", c_void_p)]
+
+
+class RaGrad(ctypes.Structure):
+    _fields_ = [("g", c_void_p), ("n", c_int64), ("type", c_int32), ("reserved", c_int32)]
+
+
+class RaAdamwTensor(ctypes.Structure):
+    _fields_ = [("p", c_void_p), ("g", c_void_p), ("m", c_void_p), ("v", c_void_p), ("m_scale", c_void_p),
+                ("v_scale", c_void_p), ("w", c_void_p), ("n", c_int64), ("g_type", c_int32), ("reserved", c_int32)]
+
+
+class RaAdamwArgs(ctypes.Structure):
+    _fields_ = [("tensors", POINTER(RaAdamwTensor)), ("n_tensors", c_int32), ("bits", c_int32), ("lr", c_double),
+                ("beta1", c_double), ("beta2", c_double), ("eps", c_double), ("decay", c_double), ("step", c_int64),
+                ("lr_dev", c_void_p), ("step_dev", c_void_p), ("grad_scale", c_void_p), ("seed", c_uint64)]
+
+
 class RefAdaptError(RuntimeError):
     def __init__(self, fn, status, msg):
         super().__init__("%s failed: %s (%s)" % (fn, _status_name(status), msg))
@@ -223,6 +272,22 @@ def load():
     lib.refadapt_glu_backward_workspace_size.argtypes = [c_int32] * 5
     lib.refadapt_glu_backward.restype = c_int32
     lib.refadapt_glu_backward.argtypes = [POINTER(RaGluGradArgs), c_void_p]
+    lib.refadapt_quant4_scales_size.restype = c_size_t
+    lib.refadapt_quant4_scales_size.argtypes = [c_int32] * 3
+    lib.refadapt_quant4.restype = c_int32
+    lib.refadapt_quant4.argtypes = [POINTER(RaQuant4Args), c_void_p]
+    lib.refadapt_gemm4.restype = c_int32
+    lib.refadapt_gemm4.argtypes = [POINTER(RaGemm4Args), c_void_p]
+    lib.refadapt_linear4_backward_workspace_size.restype = c_size_t
+    lib.refadapt_linear4_backward_workspace_size.argtypes = [c_int32] * 4
+    lib.refadapt_linear4_backward.restype = c_int32
+    lib.refadapt_linear4_backward.argtypes = [POINTER(RaLinear4GradArgs), c_void_p]
+    lib.refadapt_grad_norm_workspace_size.restype = c_size_t
+    lib.refadapt_grad_norm_workspace_size.argtypes = []
+    lib.refadapt_grad_norm.restype = c_int32
+    lib.refadapt_grad_norm.argtypes = [POINTER(RaGrad), c_int32, c_float, c_void_p, c_void_p, c_size_t, c_void_p]
+    lib.refadapt_adamw.restype = c_int32
+    lib.refadapt_adamw.argtypes = [POINTER(RaAdamwArgs), c_void_p]
     lib.refadapt_selftest_wait_timeout.restype = c_int32
     lib.refadapt_selftest_wait_timeout.argtypes = [c_void_p, c_uint64, c_void_p]
     _lib = lib

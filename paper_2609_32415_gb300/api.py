@@ -6,12 +6,14 @@ of the computation runs in librefadapt.so's kernels.
 Tensors are [B, H, n, d] bf16 CUDA views with a contiguous last axis (any
 other strides, 16-byte aligned).
 """
+import collections
 import ctypes
+import math
 
 import torch
 
 from . import _lib
-from ._lib import RaSeg, check
+from ._lib import RA_Q4_E4M3, RA_Q4_E8M0, RaSeg, check
 
 __all__ = ["seg", "refadapt_joint_attn", "refadapt_mass_partial_len", "refadapt_q_delta",
            "refadapt_q_delta_workspace_size", "refadapt_q_delta_noalloc", "refadapt_state_size", "refadapt_state_init",
@@ -21,7 +23,10 @@ __all__ = ["seg", "refadapt_joint_attn", "refadapt_mass_partial_len", "refadapt_
            "refadapt_rope_axes", "refadapt_rope_axes_table", "rope_axes_table", "refadapt_residual_norm",
            "refadapt_residual_norm_backward", "refadapt_residual_norm_backward_workspace_size",
            "residual_norm_backward_workspace", "refadapt_glu", "refadapt_glu_backward",
-           "refadapt_glu_backward_workspace_size", "glu_backward_workspace"]
+           "refadapt_glu_backward_workspace_size", "glu_backward_workspace", "Weight4", "weight4", "quant4_buffers",
+           "refadapt_quant4", "refadapt_quant4_scales_size", "refadapt_gemm4", "refadapt_linear4_backward",
+           "refadapt_linear4_backward_workspace_size", "linear4_backward_workspace", "refadapt_grad_norm",
+           "refadapt_grad_norm_workspace_size", "grad_norm_workspace", "refadapt_adamw", "adamw_moments"]
 
 
 def _ptr(t):
@@ -289,3 +294,115 @@ def refadapt_glu_backward(dy, x, w_gate, w_up, w_down, pre_gate, pre_up, hidden,
     return check("refadapt_glu_backward", _lib.native().glu_backward(
         dy, x, w_gate, w_up, w_down, pre_gate, pre_up, hidden, int(act), workspace, dx, dw_gate, dw_up, dw_down,
         err_word, _handle(stream)))
+
+
+# --------------------------------------------------------------------------- linear layers in 4 bits
+# A weight [N, K] in 4 bits: codes [N, K / 2] and scales (include/refadapt.h has the layout), uint8;
+# the scales' exponent and the format (RA_Q4_E4M3 or RA_Q4_E8M0).
+Weight4 = collections.namedtuple("Weight4", "codes scales exponent format")
+
+
+def refadapt_quant4_scales_size(rows, K, format) -> int:
+    return int(_lib.load().refadapt_quant4_scales_size(int(rows), int(K), int(format)))
+
+
+def quant4_buffers(B, rows, C, format, device="cuda"):
+    """(codes [B, rows, C / 2], scales [B, row tiles, column tiles, 512]) for refadapt_quant4, uint8."""
+    block = 32 if format == RA_Q4_E8M0 else 16
+    u8 = dict(dtype=torch.uint8, device=device)
+    return (torch.empty((B, rows, C // 2), **u8),
+            torch.empty((B, -(-rows // 128), -(-C // (4 * block)), 512), **u8))
+
+
+def refadapt_quant4(segs, C, format, mode=None, stream=None):
+    """bf16 rows to 4 bits. segs: up to three dicts with x ([B, rows, C] bf16) and
+    codes ([B, rows, C / 2]) with scales, along the features, or codes_t ([C,
+    tokens / 2], tokens = B * rows rounded up to 64) with scales_t, along the rows,
+    or both; optional exponent (RA_Q4_E4M3) and gated. Codes and scales are uint8."""
+    return check("refadapt_quant4", _lib.native().quant4(segs, int(C), int(format), mode, _handle(stream)))
+
+
+def weight4(w, format=RA_Q4_E4M3, exponent=None, stream=None):
+    """A weight [N, K] bf16 as a Weight4. exponent None: from the weight's largest
+    magnitude (which waits for the GPU), so that no scale is cut off and the others have the
+    range of e4m3 below it."""
+    if w.dim() != 2:
+        raise ValueError("w: expected [N, K], got %s" % (tuple(w.shape),))
+    if exponent is None:
+        exponent = 0
+        top = float(w.detach().abs().amax()) if format == RA_Q4_E4M3 and w.numel() else 0.0
+        if 0.0 < top < math.inf:
+            exponent = min(64, max(-64, math.ceil(math.log2(top / (6.0 * 448.0)))))
+    codes, scales = quant4_buffers(1, w.shape[0], w.shape[1], format, w.device)
+    refadapt_quant4([{"x": w.detach().unsqueeze(0), "codes": codes, "scales": scales, "exponent": exponent}],
+                    w.shape[1], format, stream=stream)
+    return Weight4(codes[0], scales[0], exponent, format)
+
+
+def refadapt_gemm4(segs, N, K, epilogue, format, mode=None, rope=None, H=0, d=0, norm_eps=1e-6, err_word=None,
+                   tile_mode=0, stream=None):
+    """refadapt_gemm with 4-bit operands. segs: up to three dicts with a ([B, rows,
+    K / 2] codes), a_scales, w ([N, K / 2] codes), w_scales, uint8, optional
+    a_exponent and w_exponent (RA_Q4_E4M3); the other entries are refadapt_gemm's."""
+    return check("refadapt_gemm4", _lib.native().gemm4(
+        segs, int(N), int(K), int(epilogue), int(format), mode, rope, int(H), int(d), float(norm_eps), err_word,
+        int(tile_mode), _handle(stream)))
+
+
+def refadapt_linear4_backward_workspace_size(B, rows, K, N) -> int:
+    return int(_lib.load().refadapt_linear4_backward_workspace_size(int(B), int(rows), int(K), int(N)))
+
+
+def linear4_backward_workspace(B, rows, K, N, device="cuda"):
+    """A workspace for refadapt_linear4_backward (reusable across calls)."""
+    return torch.empty(refadapt_linear4_backward_workspace_size(B, rows, K, N), dtype=torch.uint8, device=device)
+
+
+def refadapt_linear4_backward(dy, x, w, workspace, dx=None, dw=None, err_word=None, stream=None):
+    """Gradients of y = x w^T through 4-bit products (RA_Q4_E8M0), from dy ([B, rows,
+    N]), x ([B, rows, K]) and w ([N, K]), bf16. Fills dx ([B, rows, K]) and dw ([N, K])
+    where given; x may be None without dw, w without dx."""
+    return check("refadapt_linear4_backward", _lib.native().linear4_backward(dy, x, w, workspace, dx, dw, err_word,
+                                                                             _handle(stream)))
+
+
+# --------------------------------------------------------------------------- the optimiser's step
+def refadapt_grad_norm_workspace_size() -> int:
+    return int(_lib.load().refadapt_grad_norm_workspace_size())
+
+
+def grad_norm_workspace(device="cuda"):
+    """A zero-filled workspace for refadapt_grad_norm (reusable across calls)."""
+    return torch.zeros(refadapt_grad_norm_workspace_size(), dtype=torch.uint8, device=device)
+
+
+def refadapt_grad_norm(grads, max_norm, out, workspace, stream=None):
+    """out ([2] fp32) = the norm of all gradients (contiguous fp32 or bf16 tensors)
+    together and the factor that clips it to max_norm, for refadapt_adamw's grad_scale."""
+    return check("refadapt_grad_norm", _lib.native().grad_norm(grads, float(max_norm), out, workspace,
+                                                               _handle(stream)))
+
+
+def adamw_moments(p, bits=32):
+    """Zero moments of a parameter for refadapt_adamw: a dict with m and v, and with
+    m_scale and v_scale where bits is 8."""
+    if bits == 32:
+        return {z: torch.zeros(p.shape, dtype=torch.float32, device=p.device) for z in ("m", "v")}
+    if bits != 8:
+        raise ValueError("bits: 32 or 8, got %r" % (bits,))
+    return {**{z: torch.zeros(p.shape, dtype=torch.uint8, device=p.device).view(torch.float8_e4m3fn) for z in ("m", "v")},
+            **{z: torch.ones(-(-p.numel() // 32), dtype=torch.uint8, device=p.device).view(torch.float8_e8m0fnu)
+               for z in ("m_scale", "v_scale")}}
+
+
+def refadapt_adamw(tensors, lr, step, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01, grad_scale=None, seed=0,
+                   stream=None):
+    """One AdamW step over all tensors. tensors: a sequence of dicts with p (fp32),
+    g (its gradient, fp32 or bf16), m and v (``adamw_moments``: fp32, or e4m3 with
+    m_scale and v_scale), optional w (bf16, gets p's rounding). lr and step (from 1
+    on): numbers, or fp32 and int32 device tensors of one, which a captured call reads
+    when it is replayed. grad_scale: a device tensor of one that the gradients count
+    times (not finite: nothing changes). seed: of the 8-bit moments' rounding."""
+    return check("refadapt_adamw", _lib.native().adamw(
+        tensors, lr, step if isinstance(step, torch.Tensor) else int(step), float(beta1), float(beta2), float(eps),
+        float(weight_decay), grad_scale, int(seed), _handle(stream)))

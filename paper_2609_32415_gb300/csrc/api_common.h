@@ -46,6 +46,11 @@ bool encode_seg(CUtensorMap* tm, const ra_seg& s, int B, int H, int d, int box_c
 bool encode_seg(CUtensorMap* tm, const ra_seg& s, int B, int H, int d, int box_cols, int box_rows,
                 CUtensorMapSwizzle swizzle);
 
+// 4-D TMA tensor map of 32-bit words: n1 x n2 x n3 runs of `words` words, s1, s2, s3 bytes
+// apart (multiples of 16); boxes of a whole run by box1 by box2, zero fill out of bounds.
+bool encode_words(CUtensorMap* tm, const void* ptr, int words, int64_t n1, int64_t n2, int64_t n3, int64_t s1,
+                  int64_t s2, int64_t s3, int box1, int box2);
+
 // Launch attribute: the kernel may start while the previous one of the stream
 // finishes (it calls pdl_wait() before it touches global memory).
 inline cudaLaunchAttribute pdl_attribute() {

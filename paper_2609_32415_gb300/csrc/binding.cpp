@@ -10,6 +10,7 @@
 
 #include <cstdio>
 #include <cstring>
+#include <vector>
 
 #include "refadapt.h"
 
@@ -179,6 +180,8 @@ struct Names {
   PyObject *h, *x, *shift, *scale, *gated, *a, *w, *bias, *out, *resid, *gate, *q, *k, *v, *q_norm, *k_norm, *pos_offset;
   PyObject *y, *h_out, *post_w, *pre_w, *dx, *dh_out, *dh, *dy, *dgate, *dscale, *dshift, *dpost_w, *dpre_w;
   PyObject *w_gate, *w_up, *pre_gate, *pre_up;
+  PyObject *codes, *scales, *codes_t, *scales_t, *exponent, *a_scales, *w_scales, *a_exponent, *w_exponent;
+  PyObject *p, *g, *m, *m_scale, *v_scale;
 } N;
 
 // Stream argument: None is the calling thread's current stream.
@@ -717,11 +720,301 @@ PyObject* glu_backward(PyObject*, PyObject* const* g, Py_ssize_t n) {
   });
 }
 
+// Bytes of a 4-bit matrix's codes or scales (None: absent): uint8 CUDA.
+struct Bytes {
+  void* ptr;
+  int64_t stride_s, stride_r;
+};
+// Codes [B, rows, width], contiguous last axis.
+Bytes codes_of(PyObject* o, const char* what, int64_t B, int64_t rows, int64_t width) {
+  if (o == Py_None) return Bytes{nullptr, 0, 0};
+  const at::Tensor& t = tensor(o);
+  if (t.dim() != 3 || t.scalar_type() != at::kByte || !t.is_cuda() || t.size(0) != B || t.size(1) != rows ||
+      t.size(2) != width || (width > 1 && t.stride(2) != 1)) {
+    char want[160];
+    snprintf(want, sizeof(want), "a [%lld, %lld, %lld] uint8 CUDA tensor with contiguous last axis", (long long)B,
+             (long long)rows, (long long)width);
+    bad_tensor(o, what, want);
+  }
+  return Bytes{t.numel() > 0 ? t.data_ptr() : nullptr, B > 1 ? t.stride(0) : 0,
+               rows > 1 ? t.stride(1) : (width + 15) / 16 * 16};
+}
+// Scales of `matrices` matrices of rows x cols: any contiguous shape of that many bytes.
+void* scales_of(PyObject* o, const char* what, int64_t matrices, int64_t rows, int64_t cols, int32_t format) {
+  if (o == Py_None) return nullptr;
+  const at::Tensor& t = tensor(o);
+  const int64_t bytes = matrices * int64_t(refadapt_quant4_scales_size(int32_t(rows), int32_t(cols), format));
+  if (t.scalar_type() != at::kByte || !t.is_cuda() || !t.is_contiguous() || t.numel() != bytes) {
+    char want[96];
+    snprintf(want, sizeof(want), "a contiguous uint8 CUDA tensor of %lld bytes", (long long)bytes);
+    bad_tensor(o, what, want);
+  }
+  return bytes > 0 ? t.data_ptr() : nullptr;
+}
+int32_t optional_int(PyObject* o) { return o == Py_None ? 0 : as_int32(o); }
+
+// quant4(segs, C, format, mode, stream)
+PyObject* quant4(PyObject*, PyObject* const* g, Py_ssize_t n) {
+  return guarded(n, 5, [&] {
+    const Seq segs(g[0], 0);
+    ra_quant4_args a;
+    std::memset(&a, 0, sizeof(a));
+    a.C = integer32(g[1]);
+    a.format = integer32(g[2]);
+    for (Py_ssize_t i = 0; i < segs.size(); ++i) {
+      if (i >= 3) too_many_segments();
+      const Map sd(segs[i]);
+      ra_quant4_seg& s = a.seg[i];
+      RowShape shape;
+      const Rows x = shape.take(sd.need(N.x), "x", a.C);
+      if (shape.B < 0) raise(PyExc_ValueError, "x: expected a tensor");
+      if (i > 0 && a.B != shape.B) raise(PyExc_ValueError, "refadapt_quant4: segments of one batch size needed");
+      a.B = int32_t(shape.B);
+      if (shape.B * shape.rows >= (int64_t(1) << 30)) raise(PyExc_ValueError, "too many samples or rows");
+      s.x = x.ptr, s.x_stride_s = x.stride_s, s.x_stride_r = x.stride_r;
+      const Bytes c = codes_of(sd.get(N.codes), "codes", shape.B, shape.rows, a.C / 2);
+      s.codes = c.ptr, s.codes_stride_s = c.stride_s, s.codes_stride_r = c.stride_r;
+      s.scales = scales_of(sd.get(N.scales), "scales", shape.B, shape.rows, a.C, a.format);
+      const int64_t padded = (shape.B * shape.rows + 63) / 64 * 64;
+      if (PyObject* o = sd.get(N.codes_t); o != Py_None) {
+        const at::Tensor& t = tensor(o);
+        if (t.dim() != 2 || t.scalar_type() != at::kByte || !t.is_cuda() || t.size(0) != a.C ||
+            t.size(1) != padded / 2 || (padded > 2 && t.stride(1) != 1)) {
+          char want[128];
+          snprintf(want, sizeof(want), "a [%d, %lld] uint8 CUDA tensor with contiguous last axis", int(a.C),
+                   (long long)(padded / 2));
+          bad_tensor(o, "codes_t", want);
+        }
+        s.codes_t = t.numel() > 0 ? t.data_ptr() : nullptr, s.codes_t_stride = t.stride(0);
+      }
+      s.scales_t = scales_of(sd.get(N.scales_t), "scales_t", 1, a.C, padded, a.format);
+      s.rows = int32_t(shape.rows);
+      s.gated = truth(sd.get(N.gated));
+      s.exponent = optional_int(sd.get(N.exponent));
+    }
+    if (segs.size() == 0) raise(PyExc_TypeError, "refadapt_quant4: no segments");
+    a.n_seg = int32_t(segs.size());
+    a.mode = modes_of(g[3], a.B);
+    void* st = stream_of(g[4]);
+    return released([&] { return refadapt_quant4(&a, st); });
+  });
+}
+
+// ra_seg of a [B, H, rows, d] output.
+ra_seg heads_of(PyObject* o, const char* what, int64_t B, int64_t H, int64_t rows, int64_t d) {
+  const ra_seg s = seg(o);
+  const at::Tensor& t = tensor(o);
+  if (t.size(0) != B || t.size(1) != H || t.size(2) != rows || t.size(3) != d) {
+    char want[128];
+    snprintf(want, sizeof(want), "a [%lld, %lld, %lld, %lld] bf16 CUDA tensor", (long long)B, (long long)H,
+             (long long)rows, (long long)d);
+    bad_tensor(o, what, want);
+  }
+  return s;
+}
+
+// gemm4(segs, N, K, epilogue, format, mode, rope, H, d, norm_eps, err_word, tile_mode, stream)
+PyObject* gemm4(PyObject*, PyObject* const* g, Py_ssize_t n) {
+  return guarded(n, 13, [&] {
+    const Seq segs(g[0], 0);
+    ra_gemm4_args a;
+    std::memset(&a, 0, sizeof(a));
+    a.N = integer32(g[1]);
+    a.K = integer32(g[2]);
+    a.epilogue = integer32(g[3]);
+    a.format = integer32(g[4]);
+    a.H = integer32(g[7]);
+    a.d = integer32(g[8]);
+    for (Py_ssize_t i = 0; i < segs.size(); ++i) {
+      if (i >= 3) too_many_segments();
+      const Map sd(segs[i]);
+      ra_gemm4_seg& q = a.seg[i];
+      ra_gemm_seg& s = q.lin;
+      PyObject* ao = sd.need(N.a);
+      const at::Tensor& at = tensor(ao);
+      if (at.dim() != 3) bad_tensor(ao, "a", "a [B, rows, K / 2] uint8 CUDA tensor with contiguous last axis");
+      const int64_t B = at.size(0), rows = at.size(1);
+      if (i > 0 && a.B != B) raise(PyExc_ValueError, "refadapt_gemm4: segments of one batch size needed");
+      if (B > INT32_MAX || rows > INT32_MAX) raise(PyExc_ValueError, "too many samples or rows");
+      a.B = int32_t(B);
+      const Bytes c = codes_of(ao, "a", B, rows, a.K / 2);
+      s.a = c.ptr, s.a_stride_s = c.stride_s, s.a_stride_r = c.stride_r, s.rows = int32_t(rows);
+      s.gated = truth(sd.get(N.gated));
+      PyObject* wo = sd.need(N.w);
+      const at::Tensor& w = tensor(wo);
+      if (w.dim() != 2 || w.size(0) != a.N || w.size(1) != a.K / 2 || !w.is_contiguous() || !w.is_cuda() ||
+          w.scalar_type() != at::kByte)
+        bad_tensor(wo, "w", "a contiguous [N, K / 2] uint8 CUDA tensor");
+      s.w = w.data_ptr();
+      q.a_scales = scales_of(sd.need(N.a_scales), "a_scales", B, rows, a.K, a.format);
+      q.w_scales = scales_of(sd.need(N.w_scales), "w_scales", 1, a.N, a.K, a.format);
+      q.a_exponent = optional_int(sd.get(N.a_exponent));
+      q.w_exponent = optional_int(sd.get(N.w_exponent));
+      s.bias = vec_of(sd.get(N.bias), "bias", a.N);
+      RowShape shape;
+      shape.B = B, shape.rows = rows;
+      if (a.epilogue == RA_EPI_QKV) {
+        s.q_out = heads_of(sd.need(N.q), "q", B, a.H, rows, a.d);
+        s.k_out = heads_of(sd.need(N.k), "k", B, a.H, rows, a.d);
+        s.v_out = heads_of(sd.need(N.v), "v", B, a.H, rows, a.d);
+        s.q_norm = vec_of(sd.need(N.q_norm), "q_norm", a.d);
+        s.k_norm = vec_of(sd.need(N.k_norm), "k_norm", a.d);
+        s.pos_offset = optional_int(sd.get(N.pos_offset));
+      } else {
+        const Rows o = shape.take(sd.need(N.out), "out", a.N), r = shape.take(sd.get(N.resid), "resid", a.N);
+        s.out = o.ptr, s.out_stride_s = o.stride_s, s.out_stride_r = o.stride_r;
+        s.resid = r.ptr, s.resid_stride_s = r.stride_s, s.resid_stride_r = r.stride_r;
+        const Vecs gate = vecs_of(sd.get(N.gate), "gate", B, a.N);
+        s.gate = gate.ptr, s.gate_stride_s = gate.stride;
+      }
+    }
+    if (segs.size() == 0) raise(PyExc_TypeError, "refadapt_gemm4: no segments");
+    a.n_seg = int32_t(segs.size());
+    a.mode = modes_of(g[5], a.B);
+    if (g[6] != Py_None) {
+      const at::Tensor& r = tensor(g[6]);
+      if (r.dim() != 3 || r.scalar_type() != at::kFloat || !r.is_cuda() || !r.is_contiguous() || 2 * r.size(1) != a.d ||
+          r.size(2) != 2 || r.size(0) > INT32_MAX)
+        bad_tensor(g[6], "rope", "a contiguous [positions, d / 2, 2] fp32 CUDA tensor");
+      a.rope = static_cast<const float*>(r.data_ptr());
+      a.rope_len = int32_t(r.size(0));
+    }
+    a.norm_eps = float(real(g[9]));
+    a.err_word = static_cast<int32_t*>(address(g[10]));
+    a.tile_mode = integer32(g[11]);
+    void* st = stream_of(g[12]);
+    return released([&] { return refadapt_gemm4(&a, st); });
+  });
+}
+
+// linear4_backward(dy, x, w, workspace, dx, dw, err_word, stream)
+PyObject* linear4_backward(PyObject*, PyObject* const* g, Py_ssize_t n) {
+  return guarded(n, 8, [&] {
+    ra_linear4_grad_args a;
+    std::memset(&a, 0, sizeof(a));
+    const at::Tensor &dy = tensor(g[0]), &wide = tensor(g[2] != Py_None ? g[2] : g[1]);
+    if (dy.dim() != 3) bad_tensor(g[0], "dy", "a [B, rows, N] bf16 CUDA tensor");
+    if (wide.dim() < 1 || dy.size(2) > INT32_MAX || wide.size(-1) > INT32_MAX)
+      raise(PyExc_ValueError, "refadapt_linear4_backward: w or x: expected [N, K] or [B, rows, K]");
+    a.N = int32_t(dy.size(2)), a.K = int32_t(wide.size(-1));
+    RowShape shape;
+    const Rows d = shape.take(g[0], "dy", a.N), x = shape.take(g[1], "x", a.K), dx = shape.take(g[4], "dx", a.K);
+    a.B = int32_t(shape.B), a.rows = int32_t(shape.rows);
+    a.dy = d.ptr, a.dy_stride_s = d.stride_s, a.dy_stride_r = d.stride_r;
+    a.x = x.ptr, a.x_stride_s = x.stride_s, a.x_stride_r = x.stride_r;
+    a.dx = dx.ptr, a.dx_stride_s = dx.stride_s, a.dx_stride_r = dx.stride_r;
+    a.w = weight_of(g[2], "w", a.N, a.K);
+    a.dw = weight_of(g[5], "dw", a.N, a.K);
+    const Scratch ws = scratch_of(g[3]);
+    a.workspace = ws.ptr, a.workspace_bytes = ws.bytes;
+    a.err_word = static_cast<int32_t*>(address(g[6]));
+    void* st = stream_of(g[7]);
+    // without rows there is nothing in dx, and its address says nothing
+    if (a.rows == 0 && g[4] != Py_None && !a.dw) return RA_OK;
+    return released([&] { return refadapt_linear4_backward(&a, st); });
+  });
+}
+
+// A contiguous CUDA tensor of n elements (n < 0: any number) of one of two types.
+const at::Tensor& flat_of(PyObject* o, const char* what, int64_t n, at::ScalarType a, at::ScalarType b, const char* want) {
+  const at::Tensor& t = tensor(o);
+  if (!t.is_cuda() || !t.is_contiguous() || (t.scalar_type() != a && t.scalar_type() != b) || (n >= 0 && t.numel() != n))
+    bad_tensor(o, what, want);
+  return t;
+}
+
+// grad_norm(grads, max_norm, out, workspace, stream)
+PyObject* grad_norm(PyObject*, PyObject* const* g, Py_ssize_t n) {
+  return guarded(n, 5, [&] {
+    const Seq grads(g[0], 0);
+    std::vector<ra_grad> list(size_t(grads.size()));
+    for (Py_ssize_t i = 0; i < grads.size(); ++i) {
+      const at::Tensor& t =
+          flat_of(grads[i], "grads", -1, at::kFloat, at::kBFloat16, "contiguous fp32 or bf16 CUDA tensors");
+      list[size_t(i)] = ra_grad{t.data_ptr(), t.numel(), t.scalar_type() == at::kBFloat16 ? RA_BF16 : RA_F32, 0};
+    }
+    float* out = static_cast<float*>(
+        flat_of(g[2], "out", 2, at::kFloat, at::kFloat, "a contiguous [2] fp32 CUDA tensor").data_ptr());
+    const Scratch ws = scratch_of(g[3]);
+    const float most = float(real(g[1]));
+    void* st = stream_of(g[4]);
+    if (list.size() > size_t(INT32_MAX)) raise(PyExc_ValueError, "too many tensors");
+    return released(
+        [&] { return refadapt_grad_norm(list.data(), int32_t(list.size()), most, out, ws.ptr, ws.bytes, st); });
+  });
+}
+
+// adamw(tensors, lr, step, beta1, beta2, eps, decay, grad_scale, seed, stream); lr and step numbers or device tensors
+PyObject* adamw(PyObject*, PyObject* const* g, Py_ssize_t n) {
+  return guarded(n, 10, [&] {
+    const Seq ts(g[0], 0);
+    std::vector<ra_adamw_tensor> list(size_t(ts.size()));
+    ra_adamw_args a;
+    std::memset(&a, 0, sizeof(a));
+    a.bits = 32;
+    for (Py_ssize_t i = 0; i < ts.size(); ++i) {
+      const Map sd(ts[i]);
+      ra_adamw_tensor& d = list[size_t(i)];
+      std::memset(&d, 0, sizeof(d));
+      const at::Tensor& p = flat_of(sd.need(N.p), "p", -1, at::kFloat, at::kFloat, "a contiguous fp32 CUDA tensor");
+      d.n = p.numel();
+      d.p = p.data_ptr();
+      const at::Tensor& gr =
+          flat_of(sd.need(N.g), "g", d.n, at::kFloat, at::kBFloat16, "a contiguous fp32 or bf16 CUDA tensor like p");
+      d.g = gr.data_ptr();
+      d.g_type = gr.scalar_type() == at::kBFloat16 ? RA_BF16 : RA_F32;
+      PyObject *ms = sd.get(N.m_scale), *vs = sd.get(N.v_scale);
+      const bool small = ms != Py_None || vs != Py_None;
+      if (i == 0) a.bits = small ? 8 : 32;
+      if (small != (a.bits == 8)) raise(PyExc_ValueError, "refadapt_adamw: all tensors' moments are in 32 or all in 8 bits");
+      const at::ScalarType state = small ? at::kFloat8_e4m3fn : at::kFloat, other = small ? at::kByte : at::kFloat;
+      const char* want = small ? "a contiguous float8_e4m3fn or uint8 CUDA tensor like p" : "a contiguous fp32 CUDA tensor like p";
+      d.m = flat_of(sd.need(N.m), "m", d.n, state, other, want).data_ptr();
+      d.v = flat_of(sd.need(N.v), "v", d.n, state, other, want).data_ptr();
+      if (small) {
+        const char* s_want = "a contiguous float8_e8m0fnu or uint8 CUDA tensor, one for 32 elements";
+        const int64_t blocks = (d.n + 31) / 32;
+        if (ms == Py_None || vs == Py_None) raise(PyExc_ValueError, "refadapt_adamw: m_scale and v_scale go together");
+        d.m_scale = flat_of(ms, "m_scale", blocks, at::kFloat8_e8m0fnu, at::kByte, s_want).data_ptr();
+        d.v_scale = flat_of(vs, "v_scale", blocks, at::kFloat8_e8m0fnu, at::kByte, s_want).data_ptr();
+      }
+      if (PyObject* w = sd.get(N.w); w != Py_None)
+        d.w = flat_of(w, "w", d.n, at::kBFloat16, at::kBFloat16, "a contiguous bf16 CUDA tensor like p").data_ptr();
+    }
+    if (list.size() > size_t(INT32_MAX)) raise(PyExc_ValueError, "too many tensors");
+    a.tensors = list.data();
+    a.n_tensors = int32_t(list.size());
+    if (THPVariable_Check(g[1]))
+      a.lr_dev = static_cast<const float*>(
+          flat_of(g[1], "lr", 1, at::kFloat, at::kFloat, "a number or an fp32 CUDA tensor of one").data_ptr());
+    else
+      a.lr = real(g[1]);
+    if (THPVariable_Check(g[2]))
+      a.step_dev = static_cast<const int32_t*>(
+          flat_of(g[2], "step", 1, at::kInt, at::kInt, "a number or an int32 CUDA tensor of one").data_ptr());
+    else
+      a.step = integer(g[2]);
+    a.beta1 = real(g[3]);
+    a.beta2 = real(g[4]);
+    a.eps = real(g[5]);
+    a.decay = real(g[6]);
+    if (g[7] != Py_None)
+      a.grad_scale = static_cast<const float*>(
+          flat_of(g[7], "grad_scale", 1, at::kFloat, at::kFloat, "an fp32 CUDA tensor of one").data_ptr());
+    a.seed = PyLong_AsUnsignedLongLong(g[8]);
+    if (PyErr_Occurred()) throw Raised{};
+    void* st = stream_of(g[9]);
+    return released([&] { return refadapt_adamw(&a, st); });
+  });
+}
+
 #define RA_METHOD(f) \
   {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {RA_METHOD(joint_attn), RA_METHOD(q_delta), RA_METHOD(gate),   RA_METHOD(q_delta_gate),
                          RA_METHOD(ln_modulate), RA_METHOD(gemm),   RA_METHOD(rope_axes), RA_METHOD(residual_norm),
-                         RA_METHOD(residual_norm_backward), RA_METHOD(glu), RA_METHOD(glu_backward), {nullptr, nullptr, 0, nullptr}};
+                         RA_METHOD(residual_norm_backward), RA_METHOD(glu), RA_METHOD(glu_backward),
+                         RA_METHOD(quant4), RA_METHOD(gemm4), RA_METHOD(linear4_backward), RA_METHOD(grad_norm),
+                         RA_METHOD(adamw), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
@@ -738,7 +1031,10 @@ PyMODINIT_FUNC PyInit__binding() {
                {&N.pre_w, "pre_w"}, {&N.dx, "dx"}, {&N.dh_out, "dh_out"}, {&N.dh, "dh"}, {&N.dy, "dy"},
                {&N.dgate, "dgate"}, {&N.dscale, "dscale"}, {&N.dshift, "dshift"}, {&N.dpost_w, "dpost_w"},
                {&N.dpre_w, "dpre_w"}, {&N.w_gate, "w_gate"}, {&N.w_up, "w_up"}, {&N.pre_gate, "pre_gate"},
-               {&N.pre_up, "pre_up"}};
+               {&N.pre_up, "pre_up"}, {&N.codes, "codes"}, {&N.scales, "scales"}, {&N.codes_t, "codes_t"},
+               {&N.scales_t, "scales_t"}, {&N.exponent, "exponent"}, {&N.a_scales, "a_scales"},
+               {&N.w_scales, "w_scales"}, {&N.a_exponent, "a_exponent"}, {&N.w_exponent, "w_exponent"}, {&N.p, "p"},
+               {&N.g, "g"}, {&N.m, "m"}, {&N.m_scale, "m_scale"}, {&N.v_scale, "v_scale"}};
   for (const auto& e : names)
     if (!(*e.slot = PyUnicode_InternFromString(e.name))) return nullptr;
   return PyModule_Create(&module);

@@ -182,6 +182,27 @@ bool encode_seg(CUtensorMap* tm, const ra_seg& s, int B, int H, int d, int box_c
   return true;
 }
 
+bool encode_words(CUtensorMap* tm, const void* ptr, int words, int64_t n1, int64_t n2, int64_t n3, int64_t s1,
+                  int64_t s2, int64_t s3, int box1, int box2) {
+  auto fn = encode_fn();
+  if (!fn) {
+    set_error("cuTensorMapEncodeTiled unavailable from the driver");
+    return false;
+  }
+  cuuint64_t dims[4] = {cuuint64_t(words), cuuint64_t(n1), cuuint64_t(n2), cuuint64_t(n3)};
+  cuuint64_t strides[3] = {cuuint64_t(s1), cuuint64_t(s2), cuuint64_t(s3)};
+  cuuint32_t box[4] = {cuuint32_t(words), cuuint32_t(box1), cuuint32_t(box2), 1u};
+  cuuint32_t es[4] = {1u, 1u, 1u, 1u};
+  CUresult r = fn(tm, CU_TENSOR_MAP_DATA_TYPE_UINT32, 4, const_cast<void*>(ptr), dims, strides, box, es,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) {
+    set_error("cuTensorMapEncodeTiled failed (%d)", int(r));
+    return false;
+  }
+  return true;
+}
+
 }  // namespace ra
 
 extern "C" const char* refadapt_status_string(ra_status s) {
