@@ -70,66 +70,105 @@ struct Params4 : Params {
 __device__ __forceinline__ uint32_t idesc_mx4(int M, int N, int e8m0) {
   return (1u << 7) | (1u << 10) | (uint32_t(N >> 3) << 17) | (uint32_t(e8m0) << 23) | (uint32_t(M >> 4) << 24);
 }
-// Which half of a TMEM word of scales an MMA reads (e8m0: two blocks of the word's four).
-__device__ __forceinline__ uint32_t idesc_half(uint32_t half) { return (half << 5) | (half << 30); }
-
 // Matrix descriptor of 32 rows of 16 bytes, 8 rows (128 bytes) after 8 rows, no swizzle.
 __device__ __forceinline__ uint64_t sdesc_scales(uint32_t saddr) {
   return uint64_t((saddr >> 4) & 0x3FFFu) | (uint64_t(8) << 16) | (uint64_t(8) << 32) | (uint64_t(1) << 46);
 }
 
-template <bool PAIR>
-__device__ __forceinline__ void copy_scales(uint32_t taddr, uint64_t desc) {
-  if constexpr (PAIR)
-    asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
-  else
-    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
-}
-
-#define RA_MMA4(GROUP, VEC)                                                                                      \
-  asm volatile(                                                                                                  \
-      "{\n\t.reg .pred p;\n\t"                                                                                   \
-      "setp.ne.b32 p, %6, 0;\n\t"                                                                                \
-      "tcgen05.mma.cta_group::" GROUP ".kind::mxf4nvf4.block_scale.scale_vec::" VEC                              \
-      " [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d),                                                         \
-      "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(acc)                                                     \
+// A stage's scales to TMEM columns sf.., then its MMAs (ksteps of 64, 1 to 4), by one thread of a
+// converged warp. One asm block, whose operands are the same in every lane and whose
+// addresses are the first ones plus immediates (tiles start on 1024 bytes, so that the sums never
+// carry out of a descriptor's address field): issued one by one from a single lane, with
+// descriptors made for each, 12 copies and 4 MMAs took 1.3 us, six times what the tensor core
+// needs for them. half_cols: columns by which the tile's first weight row lies inside a scale tile.
+#define RA_CP(GROUP, COL, DESC, UNITS)                                                                       \
+  "add.u32 c, %1, " COL ";\n\tadd.s64 s, " DESC ", " UNITS ";\n\t"                                           \
+  "@e tcgen05.cp.cta_group::" GROUP ".32x128b.warpx4 [c], s;\n\t"
+#define RA_MMA(GROUP, VEC, K, UNITS, IDESC, SA_COL, SW_COL, ACC)                                             \
+  "setp.gt.and.s32 q, %8, " K ", e;\n\t"                                                                     \
+  "add.s64 s, %4, " UNITS ";\n\tadd.s64 t, %5, " UNITS ";\n\tadd.u32 c, %1, " SA_COL ";\n\tadd.u32 w, %9, "  \
+  SW_COL ";\n\t"                                                                                             \
+  "@q tcgen05.mma.cta_group::" GROUP ".kind::mxf4nvf4.block_scale.scale_vec::" VEC " [%0], s, t, " IDESC     \
+  ", [c], [w], " ACC ";\n\t"
+#define RA_STAGE(GROUP, VEC, COPIES, MMAS)                                                                   \
+  asm volatile(                                                                                              \
+      "{\n\t.reg .pred e, p, q, o;\n\t.reg .b64 s, t;\n\t.reg .b32 c, w, i;\n\t"                            \
+      "elect.sync _|e, 0xffffffff;\n\t"                                                                      \
+      "setp.ne.b32 p, %7, 0;\n\tsetp.eq.b32 o, %7, %7;\n\tor.b32 i, %6, 0x40000020;\n\t" COPIES MMAS "}" ::"r"(d), \
+      "r"(sf), "l"(s_a), "l"(s_w), "l"(a), "l"(b), "r"(idesc), "r"(acc), "r"(ksteps), "r"(sf + half_cols)      \
       : "memory")
-template <bool PAIR, bool E8M0>
-__device__ __forceinline__ void umma4(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sa, uint32_t sb,
-                                      uint32_t acc) {
-  if constexpr (PAIR && E8M0) RA_MMA4("2", "2X");
-  if constexpr (PAIR && !E8M0) RA_MMA4("2", "4X");
-  if constexpr (!PAIR && E8M0) RA_MMA4("1", "2X");
-  if constexpr (!PAIR && !E8M0) RA_MMA4("1", "4X");
-}
-#undef RA_MMA4
-
-// A stage's scales to TMEM columns sf.., then its MMAs (ksteps of 64). stage: its shared
-// address; half_cols: columns by which the tile's first weight row lies inside a scale tile.
+// e4m3: a tile of scales for every 64 of K; e8m0: for 128, whose halves the descriptor selects
+// (bits 4-5 and 30-31).
+#define RA_CP_E4M3(GROUP)                                                                                    \
+  RA_CP(GROUP, "0", "%2", "0") RA_CP(GROUP, "16", "%3", "0") RA_CP(GROUP, "4", "%2", "32")                     \
+  RA_CP(GROUP, "24", "%3", "32") RA_CP(GROUP, "8", "%2", "64") RA_CP(GROUP, "32", "%3", "64")                  \
+  RA_CP(GROUP, "12", "%2", "96") RA_CP(GROUP, "40", "%3", "96")
+#define RA_CP_E4M3_2(GROUP)                                                                                  \
+  RA_CP(GROUP, "20", "%3", "128") RA_CP(GROUP, "28", "%3", "160") RA_CP(GROUP, "36", "%3", "192")              \
+  RA_CP(GROUP, "44", "%3", "224")
+#define RA_CP_E8M0(GROUP)                                                                                    \
+  RA_CP(GROUP, "0", "%2", "0") RA_CP(GROUP, "16", "%3", "0") RA_CP(GROUP, "4", "%2", "32")                     \
+  RA_CP(GROUP, "24", "%3", "32")
+#define RA_CP_E8M0_2(GROUP) RA_CP(GROUP, "20", "%3", "64") RA_CP(GROUP, "28", "%3", "96")
+#define RA_MMA_E4M3(GROUP)                                                                                   \
+  RA_MMA(GROUP, "4X", "0", "0", "%6", "0", "16", "p") RA_MMA(GROUP, "4X", "1", "2", "%6", "4", "24", "o")        \
+  RA_MMA(GROUP, "4X", "2", "4", "%6", "8", "32", "o") RA_MMA(GROUP, "4X", "3", "6", "%6", "12", "40", "o")
+#define RA_MMA_E8M0(GROUP)                                                                                   \
+  RA_MMA(GROUP, "2X", "0", "0", "%6", "0", "16", "p") RA_MMA(GROUP, "2X", "1", "2", "i", "0", "16", "o")         \
+  RA_MMA(GROUP, "2X", "2", "4", "%6", "4", "24", "o") RA_MMA(GROUP, "2X", "3", "6", "i", "4", "24", "o")
 template <bool PAIR>
 __device__ __forceinline__ void issue_stage(const Params4& p, uint32_t stage, uint32_t sf, uint32_t d, uint32_t idesc,
                                             uint32_t half_cols, int ksteps, bool first) {
   using L = Layout<PAIR>;
-  const uint32_t sa = stage, sb = stage + L::OFF_B, s_a = stage + L::OFF_SF, s_w = s_a + SA_BYTES;
-  for (int g = 0; g < p.groups; ++g) {
-    copy_scales<PAIR>(sf + 4 * g, sdesc_scales(s_a + 512 * g));
-    for (int t = 0; t < p.w_tiles; ++t)
-      copy_scales<PAIR>(sf + 16 + 8 * g + 4 * t, sdesc_scales(s_w + 512 * (t * p.groups + g)));
+  const uint64_t a = sdesc_sw128(stage, 16, 1024), b = sdesc_sw128(stage + L::OFF_B, 16, 1024);
+  const uint64_t s_a = sdesc_scales(stage + L::OFF_SF), s_w = sdesc_scales(stage + L::OFF_SF + SA_BYTES);
+  const uint32_t acc = first ? 0u : 1u;
+  if constexpr (PAIR) {
+    if (p.e8m0) {
+      if (p.w_tiles == 2) RA_STAGE("2", "2X", RA_CP_E8M0("2") RA_CP_E8M0_2("2"), RA_MMA_E8M0("2"));
+      else RA_STAGE("2", "2X", RA_CP_E8M0("2"), RA_MMA_E8M0("2"));
+    } else {
+      if (p.w_tiles == 2) RA_STAGE("2", "4X", RA_CP_E4M3("2") RA_CP_E4M3_2("2"), RA_MMA_E4M3("2"));
+      else RA_STAGE("2", "4X", RA_CP_E4M3("2"), RA_MMA_E4M3("2"));
+    }
+  } else {
+    if (p.e8m0) {
+      if (p.w_tiles == 2) RA_STAGE("1", "2X", RA_CP_E8M0("1") RA_CP_E8M0_2("1"), RA_MMA_E8M0("1"));
+      else RA_STAGE("1", "2X", RA_CP_E8M0("1"), RA_MMA_E8M0("1"));
+    } else {
+      if (p.w_tiles == 2) RA_STAGE("1", "4X", RA_CP_E4M3("1") RA_CP_E4M3_2("1"), RA_MMA_E4M3("1"));
+      else RA_STAGE("1", "4X", RA_CP_E4M3("1"), RA_MMA_E4M3("1"));
+    }
   }
-#pragma unroll
-  for (int kk = 0; kk < CHUNK / 64; ++kk) {
-    if (kk >= ksteps) break;
-    const uint64_t a = sdesc_sw128(sa + kk * 32, 16, 1024), b = sdesc_sw128(sb + kk * 32, 16, 1024);
-    const uint32_t acc = !first || kk > 0;
-    if (p.e8m0)
-      umma4<PAIR, true>(d, a, b, idesc | idesc_half(kk & 1), sf + 4 * (kk >> 1), sf + 16 + 8 * (kk >> 1) + half_cols,
-                        acc);
-    else
-      umma4<PAIR, false>(d, a, b, idesc, sf + 4 * kk, sf + 16 + 8 * kk + half_cols, acc);
-  }
+}
+#undef RA_CP
+#undef RA_MMA
+#undef RA_STAGE
+
+// umma_commit and umma_commit_pair by one thread of a converged warp (the one that elect.sync
+// names is the same every time, so the commits cover what it issued).
+template <bool PAIR>
+__device__ __forceinline__ void commit_stage(uint64_t* bar) {
+  if constexpr (PAIR)
+    asm volatile(
+        "{\n\t.reg .pred e;\n\telect.sync _|e, 0xffffffff;\n\t"
+        "@e tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;\n\t}" ::"r"(
+            smem_u32(bar)),
+        "h"(uint16_t(3))
+        : "memory");
+  else
+    asm volatile(
+        "{\n\t.reg .pred e;\n\telect.sync _|e, 0xffffffff;\n\t"
+        "@e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(smem_u32(bar))
+        : "memory");
 }
 
 __device__ __forceinline__ int ksteps_of(const Params4& p, int kb) { return min(CHUNK, p.K - kb * CHUNK) / 64; }
+
+// A whole warp's wait; false for every lane if it was given up in one.
+__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, const WaitCtl& ctl) {
+  return __all_sync(0xffffffffu, mbar_wait(bar, parity, ctl));
+}
 
 // One CTA a tile of 128 rows. SPLIT: a cluster takes a tile, each rank a contiguous part
 // of its K (merge_parts adds them up), then its share of the columns in the epilogue.
@@ -220,8 +259,8 @@ __global__ void __launch_bounds__(THREADS, 1) gemm4_kernel(const __grid_constant
       loads = it;
     }
   } else if (warp == 1) {
-    if (lane == 0) {
-      // -------------------------------------------------------------- MMA issuer
+    {
+      // -------------------------------------------------------------- MMA issuer (a converged warp)
       const uint32_t idesc = idesc_mx4(BM, bn, p.e8m0);
       const uint32_t s0 = smem_u32(smem);
       int64_t it = 0;
@@ -231,23 +270,23 @@ __global__ void __launch_bounds__(THREADS, 1) gemm4_kernel(const __grid_constant
       Tile tl;
       for (int64_t t = t0; ok && walk.at(p, t, tl); t += step) {
         const int buf = i & 1, use = i >> 1;
-        if (use > 0 && !(ok = mbar_wait(tempty + buf, uint32_t((use - 1) & 1), ctl))) break;
+        if (use > 0 && !(ok = warp_wait(tempty + buf, uint32_t((use - 1) & 1), ctl))) break;
         tc_fence_after();
         for (int kb = kb0; kb < kb1; ++kb, ++it) {
           const int st = int(it % STAGES);
-          if (!(ok = mbar_wait(full + st, uint32_t((it / STAGES) & 1), ctl))) break;
+          if (!(ok = warp_wait(full + st, uint32_t((it / STAGES) & 1), ctl))) break;
           // the MMAs that read this buffer of scales have ended
-          if (it >= 2 && !(ok = mbar_wait(empty + int((it - 2) % STAGES), uint32_t(((it - 2) / STAGES) & 1), ctl)))
+          if (it >= 2 && !(ok = warp_wait(empty + int((it - 2) % STAGES), uint32_t(((it - 2) / STAGES) & 1), ctl)))
             break;
           tc_fence_after();
           issue_stage<false>(p, s0 + st * L::STAGE_BYTES, tmem + SF_COL + uint32_t(it & 1) * SF_COLS,
                              tmem + uint32_t(buf * MAX_BN), idesc, uint32_t(tl.n0 & 64) >> 5, ksteps_of(p, kb),
                              kb == kb0);
-          umma_commit(empty + st);
+          commit_stage<false>(empty + st);
           issued = true;
         }
         if (!ok) break;
-        umma_commit(tfull + buf);
+        commit_stage<false>(tfull + buf);
         ++i;
       }
     }
@@ -297,14 +336,14 @@ __global__ void __launch_bounds__(THREADS, 1) gemm4_kernel(const __grid_constant
   tc_fence_before();
   __syncthreads();
   // No role waits any more, so the flag is final. What this CTA has on its way lands first.
-  if (*abort_flag && lane == 0) {
-    if (warp == 0)
+  if (*abort_flag) {
+    if (warp == 0 && lane == 0)
       for (int st = 0; st < STAGES; ++st) {
         const int64_t n_s = (loads > st) ? (loads - st + STAGES - 1) / STAGES : 0;
         if (n_s > 0) mbar_wait_drain(full + st, uint32_t((n_s - 1) & 1), p.budget_ns);
       }
     if (warp == 1 && issued) {
-      umma_commit(drain);
+      commit_stage<false>(drain);
       mbar_wait_drain(drain, 0, p.budget_ns);
     }
   }
@@ -393,8 +432,8 @@ __global__ void __launch_bounds__(THREADS, 1) gemm4_pair_kernel(const __grid_con
       loads = it;
     }
   } else if (warp == 1) {
-    if (lane == 0 && rank == 0) {
-      // -------------------------------------------------------------- MMA issuer (rank 0)
+    if (rank == 0) {
+      // -------------------------------------------------------------- MMA issuer (rank 0, a converged warp)
       const uint32_t idesc = idesc_mx4(P_TM, p.bn, p.e8m0);
       const uint32_t s0 = smem_u32(smem);
       int64_t it = 0;
@@ -404,22 +443,23 @@ __global__ void __launch_bounds__(THREADS, 1) gemm4_pair_kernel(const __grid_con
       Tile tl;
       for (int64_t t = cid; ok && walk.at(p, t, tl); t += ncl) {
         const int buf = i & 1, use = i >> 1;
-        if (use > 0 && !(ok = mbar_wait_cluster(tempty + buf, uint32_t((use - 1) & 1), ctl))) break;
+        if (use > 0 && !(ok = __all_sync(0xffffffffu, mbar_wait_cluster(tempty + buf, uint32_t((use - 1) & 1), ctl))))
+          break;
         tc_fence_after();
         for (int kb = 0; kb < p.kblocks; ++kb, ++it) {
           const int st = int(it % STAGES);
-          if (!(ok = mbar_wait(full + st, uint32_t((it / STAGES) & 1), ctl))) break;
+          if (!(ok = warp_wait(full + st, uint32_t((it / STAGES) & 1), ctl))) break;
           // the MMAs that read this buffer of scales have ended
-          if (it >= 2 && !(ok = mbar_wait(empty + int((it - 2) % STAGES), uint32_t(((it - 2) / STAGES) & 1), ctl)))
+          if (it >= 2 && !(ok = warp_wait(empty + int((it - 2) % STAGES), uint32_t(((it - 2) / STAGES) & 1), ctl)))
             break;
           tc_fence_after();
           issue_stage<true>(p, s0 + st * L::STAGE_BYTES, tmem + SF_COL + uint32_t(it & 1) * SF_COLS,
                             tmem + uint32_t(buf * MAX_BN), idesc, uint32_t(tl.n0 & 64) >> 5, ksteps_of(p, kb), kb == 0);
-          umma_commit_pair(empty + st, 0x3);
+          commit_stage<true>(empty + st);
           issued = true;
         }
         if (!ok) break;
-        umma_commit_pair(tfull + buf, 0x3);
+        commit_stage<true>(tfull + buf);
         ++i;
       }
     }
@@ -463,8 +503,8 @@ __global__ void __launch_bounds__(THREADS, 1) gemm4_pair_kernel(const __grid_con
   // No role waits any more, so the flag is final. What a CTA that gave up has on its way
   // lands before the pair's shared memory and TMEM go. (A rank 0 that did not give up has
   // seen every MMA end, and with them the loads of both CTAs.)
-  if (*abort_flag && lane == 0) {
-    if (warp == 0 && rank == 0) {
+  if (*abort_flag) {
+    if (warp == 0 && lane == 0 && rank == 0) {
       // rank 0's full barriers count both CTAs' bytes of every phase it armed
       for (int st = 0; st < STAGES; ++st) {
         const int64_t n_s = (loads > st) ? (loads - st + STAGES - 1) / STAGES : 0;
@@ -472,7 +512,8 @@ __global__ void __launch_bounds__(THREADS, 1) gemm4_pair_kernel(const __grid_con
       }
     }
     if (warp == 1 && issued) {
-      umma_commit_pair(drain, 0x1);
+      // the peer's barrier of this name is not waited for and has its own CTA's life
+      commit_stage<true>(drain);
       mbar_wait_drain(drain, 0, p.budget_ns);
     }
     pause_ns(kLandNs);  // rank 1's loads, and the commits' arrivals at rank 1
