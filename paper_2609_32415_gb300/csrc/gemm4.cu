@@ -53,14 +53,15 @@ struct Layout {
 static_assert(2 * (MAX_SPLIT - 1) * (BM * 128 * 4 / MAX_SPLIT) <= Layout<false>::OFF_BAR &&
                   2 * (BM * MAX_BN * 4 / 2) <= Layout<false>::OFF_BAR, "parts fit the stages");
 
-constexpr int SF_COL = 2 * MAX_BN;  // TMEM: the scales, behind the accumulators
-constexpr int SF_COLS = 48;         // of a stage: 4 x 4 columns of A, 4 x 8 of W
-static_assert(SF_COL + 2 * SF_COLS <= TMEM_COLS, "TMEM columns");
+// TMEM columns of a stage's scales: four for each tile of A's and of the weight's.
+constexpr int scale_cols(int groups, int w_tiles) { return 4 * groups * (1 + w_tiles); }
+static_assert(2 * MAX_BN + 2 * scale_cols(4, 2) <= TMEM_COLS, "TMEM columns");
 
 struct Params4 : Params {
   int32_t e8m0;                      // format
   int32_t groups;                    // scale tiles of a stage: 4 (e4m3) or 2 (e8m0)
   int32_t w_tiles;                   // scale tiles of a tile's weight rows: 1 or 2
+  int32_t sf_cols, sf_bufs;          // TMEM columns of a stage's scales, buffers of them
   uint32_t stage_tx;                 // bytes of a stage that one CTA loads
   CUtensorMap tm_sa[3], tm_sw[3];
 };
@@ -90,32 +91,42 @@ __device__ __forceinline__ uint64_t sdesc_scales(uint32_t saddr) {
   SW_COL ";\n\t"                                                                                             \
   "@q tcgen05.mma.cta_group::" GROUP ".kind::mxf4nvf4.block_scale.scale_vec::" VEC " [%0], s, t, " IDESC     \
   ", [c], [w], " ACC ";\n\t"
-#define RA_STAGE(GROUP, VEC, COPIES, MMAS)                                                                   \
+#define RA_STAGE(COPIES, MMAS)                                                                   \
   asm volatile(                                                                                              \
       "{\n\t.reg .pred e, p, q, o;\n\t.reg .b64 s, t;\n\t.reg .b32 c, w, i;\n\t"                            \
       "elect.sync _|e, 0xffffffff;\n\t"                                                                      \
       "setp.ne.b32 p, %7, 0;\n\tsetp.eq.b32 o, %7, %7;\n\tor.b32 i, %6, 0x40000020;\n\t" COPIES MMAS "}" ::"r"(d), \
       "r"(sf), "l"(s_a), "l"(s_w), "l"(a), "l"(b), "r"(idesc), "r"(acc), "r"(ksteps), "r"(sf + half_cols)      \
       : "memory")
-// e4m3: a tile of scales for every 64 of K; e8m0: for 128, whose halves the descriptor selects
-// (bits 4-5 and 30-31).
-#define RA_CP_E4M3(GROUP)                                                                                    \
+// Scale tiles of a stage: e4m3 four for 64 of K each, e8m0 two for 128 each, whose halves the
+// descriptor selects (bits 4-5 and 30-31). Columns: A's tiles, four each, then for every one of
+// them the weight's, four or eight.
+#define RA_COPIES_E4M3(GROUP)                                                                                \
   RA_CP(GROUP, "0", "%2", "0") RA_CP(GROUP, "16", "%3", "0") RA_CP(GROUP, "4", "%2", "32")                     \
-  RA_CP(GROUP, "24", "%3", "32") RA_CP(GROUP, "8", "%2", "64") RA_CP(GROUP, "32", "%3", "64")                  \
-  RA_CP(GROUP, "12", "%2", "96") RA_CP(GROUP, "40", "%3", "96")
-#define RA_CP_E4M3_2(GROUP)                                                                                  \
-  RA_CP(GROUP, "20", "%3", "128") RA_CP(GROUP, "28", "%3", "160") RA_CP(GROUP, "36", "%3", "192")              \
-  RA_CP(GROUP, "44", "%3", "224")
-#define RA_CP_E8M0(GROUP)                                                                                    \
-  RA_CP(GROUP, "0", "%2", "0") RA_CP(GROUP, "16", "%3", "0") RA_CP(GROUP, "4", "%2", "32")                     \
-  RA_CP(GROUP, "24", "%3", "32")
-#define RA_CP_E8M0_2(GROUP) RA_CP(GROUP, "20", "%3", "64") RA_CP(GROUP, "28", "%3", "96")
-#define RA_MMA_E4M3(GROUP)                                                                                   \
+  RA_CP(GROUP, "20", "%3", "32") RA_CP(GROUP, "8", "%2", "64") RA_CP(GROUP, "24", "%3", "64")                  \
+  RA_CP(GROUP, "12", "%2", "96") RA_CP(GROUP, "28", "%3", "96")
+#define RA_COPIES_E4M3_2(GROUP)                                                                              \
+  RA_CP(GROUP, "0", "%2", "0") RA_CP(GROUP, "16", "%3", "0") RA_CP(GROUP, "20", "%3", "128")                   \
+  RA_CP(GROUP, "4", "%2", "32") RA_CP(GROUP, "24", "%3", "32") RA_CP(GROUP, "28", "%3", "160")                 \
+  RA_CP(GROUP, "8", "%2", "64") RA_CP(GROUP, "32", "%3", "64") RA_CP(GROUP, "36", "%3", "192")                 \
+  RA_CP(GROUP, "12", "%2", "96") RA_CP(GROUP, "40", "%3", "96") RA_CP(GROUP, "44", "%3", "224")
+#define RA_COPIES_E8M0(GROUP)                                                                                \
+  RA_CP(GROUP, "0", "%2", "0") RA_CP(GROUP, "8", "%3", "0") RA_CP(GROUP, "4", "%2", "32") RA_CP(GROUP, "12", "%3", "32")
+#define RA_COPIES_E8M0_2(GROUP)                                                                              \
+  RA_CP(GROUP, "0", "%2", "0") RA_CP(GROUP, "8", "%3", "0") RA_CP(GROUP, "12", "%3", "64")                     \
+  RA_CP(GROUP, "4", "%2", "32") RA_CP(GROUP, "16", "%3", "32") RA_CP(GROUP, "20", "%3", "96")
+#define RA_MMAS_E4M3(GROUP)                                                                                  \
+  RA_MMA(GROUP, "4X", "0", "0", "%6", "0", "16", "p") RA_MMA(GROUP, "4X", "1", "2", "%6", "4", "20", "o")        \
+  RA_MMA(GROUP, "4X", "2", "4", "%6", "8", "24", "o") RA_MMA(GROUP, "4X", "3", "6", "%6", "12", "28", "o")
+#define RA_MMAS_E4M3_2(GROUP)                                                                                \
   RA_MMA(GROUP, "4X", "0", "0", "%6", "0", "16", "p") RA_MMA(GROUP, "4X", "1", "2", "%6", "4", "24", "o")        \
   RA_MMA(GROUP, "4X", "2", "4", "%6", "8", "32", "o") RA_MMA(GROUP, "4X", "3", "6", "%6", "12", "40", "o")
-#define RA_MMA_E8M0(GROUP)                                                                                   \
-  RA_MMA(GROUP, "2X", "0", "0", "%6", "0", "16", "p") RA_MMA(GROUP, "2X", "1", "2", "i", "0", "16", "o")         \
-  RA_MMA(GROUP, "2X", "2", "4", "%6", "4", "24", "o") RA_MMA(GROUP, "2X", "3", "6", "i", "4", "24", "o")
+#define RA_MMAS_E8M0(GROUP)                                                                                  \
+  RA_MMA(GROUP, "2X", "0", "0", "%6", "0", "8", "p") RA_MMA(GROUP, "2X", "1", "2", "i", "0", "8", "o")           \
+  RA_MMA(GROUP, "2X", "2", "4", "%6", "4", "12", "o") RA_MMA(GROUP, "2X", "3", "6", "i", "4", "12", "o")
+#define RA_MMAS_E8M0_2(GROUP)                                                                                \
+  RA_MMA(GROUP, "2X", "0", "0", "%6", "0", "8", "p") RA_MMA(GROUP, "2X", "1", "2", "i", "0", "8", "o")           \
+  RA_MMA(GROUP, "2X", "2", "4", "%6", "4", "16", "o") RA_MMA(GROUP, "2X", "3", "6", "i", "4", "16", "o")
 template <bool PAIR>
 __device__ __forceinline__ void issue_stage(const Params4& p, uint32_t stage, uint32_t sf, uint32_t d, uint32_t idesc,
                                             uint32_t half_cols, int ksteps, bool first) {
@@ -125,19 +136,19 @@ __device__ __forceinline__ void issue_stage(const Params4& p, uint32_t stage, ui
   const uint32_t acc = first ? 0u : 1u;
   if constexpr (PAIR) {
     if (p.e8m0) {
-      if (p.w_tiles == 2) RA_STAGE("2", "2X", RA_CP_E8M0("2") RA_CP_E8M0_2("2"), RA_MMA_E8M0("2"));
-      else RA_STAGE("2", "2X", RA_CP_E8M0("2"), RA_MMA_E8M0("2"));
+      if (p.w_tiles == 2) RA_STAGE(RA_COPIES_E8M0_2("2"), RA_MMAS_E8M0_2("2"));
+      else RA_STAGE(RA_COPIES_E8M0("2"), RA_MMAS_E8M0("2"));
     } else {
-      if (p.w_tiles == 2) RA_STAGE("2", "4X", RA_CP_E4M3("2") RA_CP_E4M3_2("2"), RA_MMA_E4M3("2"));
-      else RA_STAGE("2", "4X", RA_CP_E4M3("2"), RA_MMA_E4M3("2"));
+      if (p.w_tiles == 2) RA_STAGE(RA_COPIES_E4M3_2("2"), RA_MMAS_E4M3_2("2"));
+      else RA_STAGE(RA_COPIES_E4M3("2"), RA_MMAS_E4M3("2"));
     }
   } else {
     if (p.e8m0) {
-      if (p.w_tiles == 2) RA_STAGE("1", "2X", RA_CP_E8M0("1") RA_CP_E8M0_2("1"), RA_MMA_E8M0("1"));
-      else RA_STAGE("1", "2X", RA_CP_E8M0("1"), RA_MMA_E8M0("1"));
+      if (p.w_tiles == 2) RA_STAGE(RA_COPIES_E8M0_2("1"), RA_MMAS_E8M0_2("1"));
+      else RA_STAGE(RA_COPIES_E8M0("1"), RA_MMAS_E8M0("1"));
     } else {
-      if (p.w_tiles == 2) RA_STAGE("1", "4X", RA_CP_E4M3("1") RA_CP_E4M3_2("1"), RA_MMA_E4M3("1"));
-      else RA_STAGE("1", "4X", RA_CP_E4M3("1"), RA_MMA_E4M3("1"));
+      if (p.w_tiles == 2) RA_STAGE(RA_COPIES_E4M3_2("1"), RA_MMAS_E4M3_2("1"));
+      else RA_STAGE(RA_COPIES_E4M3("1"), RA_MMAS_E4M3("1"));
     }
   }
 }
@@ -165,10 +176,94 @@ __device__ __forceinline__ void commit_stage(uint64_t* bar) {
 
 __device__ __forceinline__ int ksteps_of(const Params4& p, int kb) { return min(CHUNK, p.K - kb * CHUNK) / 64; }
 
-// A whole warp's wait; false for every lane if it was given up in one.
-__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, const WaitCtl& ctl) {
-  return __all_sync(0xffffffffu, mbar_wait(bar, parity, ctl));
+__device__ __forceinline__ bool elect_one() {
+  uint32_t one;
+  asm volatile("{\n\t.reg .pred e;\n\telect.sync _|e, 0xffffffff;\n\tselp.u32 %0, 1, 0, e;\n\t}" : "=r"(one));
+  return one != 0;
 }
+// A converged warp's wait. False if it was given up.
+template <bool CLUSTER = false>
+__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, const WaitCtl& ctl) {
+  return __all_sync(0xffffffffu, CLUSTER ? mbar_wait_cluster(bar, parity, ctl) : mbar_wait(bar, parity, ctl));
+}
+// Has the phase completed? Asked before the work in front of it is issued, so that the answer's
+// latency (50 ns) passes meanwhile.
+__device__ __forceinline__ uint32_t peek(uint64_t* bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(smem_u32(bar)), "r"(parity)
+      : "memory");
+  return ok;
+}
+__device__ __forceinline__ bool warp_wait(uint32_t peeked, uint64_t* bar, uint32_t parity, const WaitCtl& ctl) {
+  return __all_sync(0xffffffffu, peeked != 0) || warp_wait(bar, parity, ctl);
+}
+// A value that is the same in every lane, known to be so.
+__device__ __forceinline__ int same(int v) { return __shfl_sync(0xffffffffu, v, 0); }
+// The walk's tile t, for a converged warp.
+template <int TM, int EPI>
+__device__ __forceinline__ bool tile_at(const Params& p, Walk<TM, EPI>& walk, int64_t t, Tile& tl) {
+  Tile r{0, 0, 0, 0};
+  const int more = same(walk.at(p, t, r));
+  tl = Tile{same(r.seg), same(r.s), same(r.m0), same(r.n0)};
+  return more != 0;
+}
+// tma_load_4d and tma_load_4d_pair by one thread of a converged warp.
+__device__ __forceinline__ void tma_load_one(uint32_t dst, const void* tmap, uint32_t bar, int32_t c0, int32_t c1,
+                                             int32_t c2, int32_t c3) {
+  asm volatile(
+      "{\n\t.reg .pred e;\n\telect.sync _|e, 0xffffffff;\n\t"
+      "@e cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+      " [%0], [%1, {%2, %3, %4, %5}], [%6];\n\t}" ::"r"(dst),
+      "l"(reinterpret_cast<uint64_t>(tmap)), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(bar)
+      : "memory");
+}
+__device__ __forceinline__ void tma_load_one_pair(uint32_t dst, const void* tmap, uint32_t bar, int32_t c0, int32_t c1,
+                                                  int32_t c2, int32_t c3) {
+  asm volatile(
+      "{\n\t.reg .pred e;\n\telect.sync _|e, 0xffffffff;\n\t"
+      "@e cp.async.bulk.tensor.4d.shared::cta.global.tile.mbarrier::complete_tx::bytes.cta_group::2"
+      " [%0], [%1, {%2, %3, %4, %5}], [%6];\n\t}" ::"r"(dst),
+      "l"(reinterpret_cast<uint64_t>(tmap)), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(bar)
+      : "memory");
+}
+
+// A stage of the ring and the parity of its barriers' next phase.
+template <int STAGES>
+struct Ring {
+  int st = 0;
+  uint32_t ph = 0;
+  __device__ __forceinline__ void next() {
+    if (++st == STAGES) {
+      st = 0;
+      ph ^= 1;
+    }
+  }
+};
+
+// The buffers of scales in TMEM, one for a stage's MMAs after another. A buffer is written
+// again once the MMAs that read it, sf_bufs stages ago, have ended. As many buffers as
+// stages: the stage itself was filled again after that.
+template <int STAGES>
+struct Scales {
+  Ring<STAGES> old;  // the stage whose MMAs read the buffer last
+  int col = 0, end, wait;
+  __device__ __forceinline__ explicit Scales(const Params4& p)
+      : end(p.sf_cols * p.sf_bufs), wait(p.sf_bufs < STAGES ? p.sf_bufs : -1) {}
+  __device__ __forceinline__ bool free(uint64_t* empty, const WaitCtl& ctl) const {
+    return wait != 0 || warp_wait(empty + old.st, old.ph, ctl);
+  }
+  __device__ __forceinline__ void next(const Params4& p) {
+    col += p.sf_cols;
+    if (col == end) col = 0;
+    if (wait > 0) --wait;
+    else if (wait == 0) old.next();
+  }
+};
 
 // One CTA a tile of 128 rows. SPLIT: a cluster takes a tile, each rank a contiguous part
 // of its K (merge_parts adds them up), then its share of the columns in the epilogue.
@@ -188,7 +283,7 @@ __global__ void __launch_bounds__(THREADS, 1) gemm4_kernel(const __grid_constant
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + L::OFF_MISC);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + L::OFF_MISC + 4);
   volatile int* live = reinterpret_cast<volatile int*>(smem + L::OFF_MISC + 8);
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = same(int(threadIdx.x >> 5)), lane = threadIdx.x & 31;
   const int rank = SPLIT ? int(cluster_rank()) : 0, cs = SPLIT ? int(cluster_size()) : 1;
   const int64_t t0 = SPLIT ? blockIdx.x / cs : blockIdx.x, step = SPLIT ? gridDim.x / cs : gridDim.x;
   const int kb0 = SPLIT ? p.kblocks * rank / cs : 0;  // this CTA's stages of K
@@ -218,7 +313,7 @@ __global__ void __launch_bounds__(THREADS, 1) gemm4_kernel(const __grid_constant
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = *tmem_slot;
+  const uint32_t tmem = uint32_t(same(int(*tmem_slot)));
   if (SPLIT && !*live) {  // uniform over the cluster: the modes leave it no tile
     if (warp == 1) tmem_dealloc(tmem, TMEM_COLS);
     return;
@@ -230,8 +325,8 @@ __global__ void __launch_bounds__(THREADS, 1) gemm4_kernel(const __grid_constant
   int64_t loads = 0;    // the producer's: stages whose loads may be on their way
   bool issued = false;  // the issuer's: MMAs may be on their way
   if (warp == 0) {
-    if (lane == 0) {
-      // -------------------------------------------------------------- producer
+    {
+      // -------------------------------------------------------------- producer (a converged warp)
       for (int g = 0; g < p.n_seg; ++g)
         if (p.rows[g] > 0) {
           tma_prefetch_desc(&p.tm_a[g]);
@@ -240,50 +335,54 @@ __global__ void __launch_bounds__(THREADS, 1) gemm4_kernel(const __grid_constant
           tma_prefetch_desc(&p.tm_sw[g]);
         }
       pdl_wait();
-      int64_t it = 0;
+      Ring<STAGES> in;
       bool ok = true;
       Walk<BM, EPI> walk;
       Tile tl;
-      for (int64_t t = t0; ok && walk.at(p, t, tl); t += step) {
-        for (int kb = kb0; kb < kb1; ++kb, ++it) {
-          const int st = int(it % STAGES);
-          if (it >= STAGES && !(ok = mbar_wait(empty + st, uint32_t((it / STAGES - 1) & 1), ctl))) break;
-          uint8_t* stage = smem + st * L::STAGE_BYTES;
-          mbar_arrive_expect_tx(full + st, p.stage_tx);
-          tma_load_4d(stage, &p.tm_a[tl.seg], full + st, kb * (CHUNK / 4), tl.m0, 0, tl.s);
-          tma_load_4d(stage + L::OFF_B, &p.tm_w[tl.seg], full + st, kb * (CHUNK / 4), tl.n0, 0, 0);
-          tma_load_4d(stage + L::OFF_SF, &p.tm_sa[tl.seg], full + st, 0, kb * p.groups, tl.m0 / 128, tl.s);
-          tma_load_4d(stage + L::OFF_SF + SA_BYTES, &p.tm_sw[tl.seg], full + st, 0, kb * p.groups, tl.n0 / 128, 0);
+      for (int64_t t = t0; ok && tile_at(p, walk, t, tl); t += step) {
+        for (int kb = kb0; kb < kb1; ++kb) {
+          if (loads >= STAGES && !(ok = warp_wait(empty + in.st, in.ph ^ 1, ctl))) break;
+          const uint32_t stage = smem_u32(smem) + in.st * L::STAGE_BYTES, bar = smem_u32(full + in.st);
+          const bool one = elect_one();
+          if (one) mbar_arrive_expect_tx(full + in.st, p.stage_tx);
+          __syncwarp();
+          tma_load_one(stage, &p.tm_a[tl.seg], bar, kb * (CHUNK / 4), tl.m0, 0, tl.s);
+          tma_load_one(stage + L::OFF_B, &p.tm_w[tl.seg], bar, kb * (CHUNK / 4), tl.n0, 0, 0);
+          tma_load_one(stage + L::OFF_SF, &p.tm_sa[tl.seg], bar, 0, kb * p.groups, tl.m0 / 128, tl.s);
+          tma_load_one(stage + L::OFF_SF + SA_BYTES, &p.tm_sw[tl.seg], bar, 0, kb * p.groups, tl.n0 / 128, 0);
+          ++loads;
+          in.next();
         }
       }
-      loads = it;
     }
   } else if (warp == 1) {
     {
       // -------------------------------------------------------------- MMA issuer (a converged warp)
       const uint32_t idesc = idesc_mx4(BM, bn, p.e8m0);
-      const uint32_t s0 = smem_u32(smem);
-      int64_t it = 0;
+      const uint32_t s0 = smem_u32(smem), sf0 = tmem + uint32_t(2 * bn);
       int i = 0;
+      Ring<STAGES> in;  // stages as they are filled
+      uint32_t filled = 0;
+      Scales<STAGES> sf(p);
       bool ok = true;
       Walk<BM, EPI> walk;
       Tile tl;
-      for (int64_t t = t0; ok && walk.at(p, t, tl); t += step) {
+      for (int64_t t = t0; ok && tile_at(p, walk, t, tl); t += step) {
         const int buf = i & 1, use = i >> 1;
         if (use > 0 && !(ok = warp_wait(tempty + buf, uint32_t((use - 1) & 1), ctl))) break;
         tc_fence_after();
-        for (int kb = kb0; kb < kb1; ++kb, ++it) {
-          const int st = int(it % STAGES);
-          if (!(ok = warp_wait(full + st, uint32_t((it / STAGES) & 1), ctl))) break;
-          // the MMAs that read this buffer of scales have ended
-          if (it >= 2 && !(ok = warp_wait(empty + int((it - 2) % STAGES), uint32_t(((it - 2) / STAGES) & 1), ctl)))
-            break;
+        for (int kb = kb0; kb < kb1; ++kb) {
+          if (!(ok = warp_wait(filled, full + in.st, in.ph, ctl) && sf.free(empty, ctl))) break;
           tc_fence_after();
-          issue_stage<false>(p, s0 + st * L::STAGE_BYTES, tmem + SF_COL + uint32_t(it & 1) * SF_COLS,
-                             tmem + uint32_t(buf * MAX_BN), idesc, uint32_t(tl.n0 & 64) >> 5, ksteps_of(p, kb),
-                             kb == kb0);
-          commit_stage<false>(empty + st);
+          Ring<STAGES> next = in;
+          next.next();
+          filled = peek(full + next.st, next.ph);
+          issue_stage<false>(p, s0 + in.st * L::STAGE_BYTES, sf0 + sf.col, tmem + uint32_t(buf * bn), idesc,
+                             uint32_t(tl.n0 & 64) >> 5, ksteps_of(p, kb), kb == kb0);
+          commit_stage<false>(empty + in.st);
           issued = true;
+          in = next;
+          sf.next(p);
         }
         if (!ok) break;
         commit_stage<false>(tfull + buf);
@@ -305,7 +404,7 @@ __global__ void __launch_bounds__(THREADS, 1) gemm4_kernel(const __grid_constant
       const int buf = i & 1, use = i >> 1;
       w.row0 = tl.m0 + quarter * 32;
       w.nrow = min(32, p.rows[tl.seg] - w.row0);
-      w.acc = tmem + (uint32_t(quarter * 32) << 16) + uint32_t(buf * MAX_BN);
+      w.acc = tmem + (uint32_t(quarter * 32) << 16) + uint32_t(buf * bn);
       w.cols = bn;
       const uint32_t acc = w.acc;
       if (SPLIT) {
@@ -371,8 +470,8 @@ __global__ void __launch_bounds__(THREADS, 1) gemm4_pair_kernel(const __grid_con
   uint64_t* drain = bars + 2 * STAGES + 4;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + L::OFF_MISC);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + L::OFF_MISC + 4);
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const uint32_t rank = cluster_rank();
+  const int warp = same(int(threadIdx.x >> 5)), lane = threadIdx.x & 31;
+  const uint32_t rank = uint32_t(same(int(cluster_rank())));
   const int64_t cid = blockIdx.x >> 1, ncl = gridDim.x >> 1;
   if (threadIdx.x == 0) {
     for (int s = 0; s < STAGES; ++s) {
@@ -392,7 +491,7 @@ __global__ void __launch_bounds__(THREADS, 1) gemm4_pair_kernel(const __grid_con
   __syncthreads();
   cluster_sync_all();  // both CTAs' barriers and TMEM exist before any cross-CTA use
   tc_fence_after();
-  const uint32_t tmem = *tmem_slot;
+  const uint32_t tmem = uint32_t(same(int(*tmem_slot)));
   const WaitCtl ctl{abort_flag, p.err_word, p.budget_ns};
   pdl_launch();
   if (warp != 0) pdl_wait();
@@ -400,8 +499,8 @@ __global__ void __launch_bounds__(THREADS, 1) gemm4_pair_kernel(const __grid_con
   int64_t loads = 0;    // the producer's: stages that it loaded
   bool issued = false;  // the issuer's: it has issued MMAs
   if (warp == 0) {
-    if (lane == 0) {
-      // -------------------------------------------------------------- producer (both CTAs)
+    {
+      // -------------------------------------------------------------- producer (both CTAs, a converged warp)
       for (int g = 0; g < p.n_seg; ++g)
         if (p.rows[g] > 0) {
           tma_prefetch_desc(&p.tm_a[g]);
@@ -411,52 +510,55 @@ __global__ void __launch_bounds__(THREADS, 1) gemm4_pair_kernel(const __grid_con
         }
       pdl_wait();
       const uint32_t full0 = mapa_shared(smem_u32(full), 0);  // rank 0's full barriers
-      int64_t it = 0;
+      Ring<STAGES> in;
       bool ok = true;
       Walk<P_TM, EPI> walk;
       Tile tl;
-      for (int64_t t = cid; ok && walk.at(p, t, tl); t += ncl) {
-        for (int kb = 0; kb < p.kblocks; ++kb, ++it) {
-          const int st = int(it % STAGES);
-          if (it >= STAGES && !(ok = mbar_wait(empty + st, uint32_t((it / STAGES - 1) & 1), ctl))) break;
-          uint8_t* stage = smem + st * L::STAGE_BYTES;
-          const uint32_t bar = full0 + 8u * st;
-          if (rank == 0) mbar_arrive_expect_tx(full + st, 2 * p.stage_tx);
-          tma_load_4d_pair(stage, &p.tm_a[tl.seg], bar, kb * (CHUNK / 4), tl.m0 + int(rank) * 128, 0, tl.s);
-          tma_load_4d_pair(stage + L::OFF_B, &p.tm_w[tl.seg], bar, kb * (CHUNK / 4), tl.n0 + int(rank) * (p.bn / 2), 0,
+      for (int64_t t = cid; ok && tile_at(p, walk, t, tl); t += ncl) {
+        for (int kb = 0; kb < p.kblocks; ++kb) {
+          if (loads >= STAGES && !(ok = warp_wait(empty + in.st, in.ph ^ 1, ctl))) break;
+          const uint32_t stage = smem_u32(smem) + in.st * L::STAGE_BYTES, bar = full0 + 8u * in.st;
+          const bool one = elect_one();
+          if (one && rank == 0) mbar_arrive_expect_tx(full + in.st, 2 * p.stage_tx);
+          __syncwarp();
+          tma_load_one_pair(stage, &p.tm_a[tl.seg], bar, kb * (CHUNK / 4), tl.m0 + int(rank) * 128, 0, tl.s);
+          tma_load_one_pair(stage + L::OFF_B, &p.tm_w[tl.seg], bar, kb * (CHUNK / 4), tl.n0 + int(rank) * (p.bn / 2), 0,
                            0);
-          tma_load_4d_pair(stage + L::OFF_SF, &p.tm_sa[tl.seg], bar, 0, kb * p.groups, tl.m0 / 128 + int(rank), tl.s);
-          tma_load_4d_pair(stage + L::OFF_SF + SA_BYTES, &p.tm_sw[tl.seg], bar, 0, kb * p.groups, tl.n0 / 128, 0);
+          tma_load_one_pair(stage + L::OFF_SF, &p.tm_sa[tl.seg], bar, 0, kb * p.groups, tl.m0 / 128 + int(rank), tl.s);
+          tma_load_one_pair(stage + L::OFF_SF + SA_BYTES, &p.tm_sw[tl.seg], bar, 0, kb * p.groups, tl.n0 / 128, 0);
+          ++loads;
+          in.next();
         }
       }
-      loads = it;
     }
   } else if (warp == 1) {
     if (rank == 0) {
       // -------------------------------------------------------------- MMA issuer (rank 0, a converged warp)
       const uint32_t idesc = idesc_mx4(P_TM, p.bn, p.e8m0);
-      const uint32_t s0 = smem_u32(smem);
-      int64_t it = 0;
+      const uint32_t s0 = smem_u32(smem), sf0 = tmem + uint32_t(2 * p.bn);
       int i = 0;
+      Ring<STAGES> in;  // stages as they are filled
+      uint32_t filled = 0;
+      Scales<STAGES> sf(p);
       bool ok = true;
       Walk<P_TM, EPI> walk;
       Tile tl;
-      for (int64_t t = cid; ok && walk.at(p, t, tl); t += ncl) {
+      for (int64_t t = cid; ok && tile_at(p, walk, t, tl); t += ncl) {
         const int buf = i & 1, use = i >> 1;
-        if (use > 0 && !(ok = __all_sync(0xffffffffu, mbar_wait_cluster(tempty + buf, uint32_t((use - 1) & 1), ctl))))
-          break;
+        if (use > 0 && !(ok = warp_wait<true>(tempty + buf, uint32_t((use - 1) & 1), ctl))) break;
         tc_fence_after();
-        for (int kb = 0; kb < p.kblocks; ++kb, ++it) {
-          const int st = int(it % STAGES);
-          if (!(ok = warp_wait(full + st, uint32_t((it / STAGES) & 1), ctl))) break;
-          // the MMAs that read this buffer of scales have ended
-          if (it >= 2 && !(ok = warp_wait(empty + int((it - 2) % STAGES), uint32_t(((it - 2) / STAGES) & 1), ctl)))
-            break;
+        for (int kb = 0; kb < p.kblocks; ++kb) {
+          if (!(ok = warp_wait(filled, full + in.st, in.ph, ctl) && sf.free(empty, ctl))) break;
           tc_fence_after();
-          issue_stage<true>(p, s0 + st * L::STAGE_BYTES, tmem + SF_COL + uint32_t(it & 1) * SF_COLS,
-                            tmem + uint32_t(buf * MAX_BN), idesc, uint32_t(tl.n0 & 64) >> 5, ksteps_of(p, kb), kb == 0);
-          commit_stage<true>(empty + st);
+          Ring<STAGES> next = in;
+          next.next();
+          filled = peek(full + next.st, next.ph);
+          issue_stage<true>(p, s0 + in.st * L::STAGE_BYTES, sf0 + sf.col, tmem + uint32_t(buf * p.bn), idesc,
+                            uint32_t(tl.n0 & 64) >> 5, ksteps_of(p, kb), kb == 0);
+          commit_stage<true>(empty + in.st);
           issued = true;
+          in = next;
+          sf.next(p);
         }
         if (!ok) break;
         commit_stage<true>(tfull + buf);
@@ -480,7 +582,7 @@ __global__ void __launch_bounds__(THREADS, 1) gemm4_pair_kernel(const __grid_con
       w.row0 = tl.m0 + int(rank) * 128 + quarter * 32;
       w.cols = p.bn;
       w.nrow = min(32, p.rows[tl.seg] - w.row0);
-      w.acc = tmem + (uint32_t(quarter * 32) << 16) + uint32_t(buf * MAX_BN);
+      w.acc = tmem + (uint32_t(quarter * 32) << 16) + uint32_t(buf * p.bn);
       if (!epilogue_tile<EPI, D, true>(p, tl, w, [&] {
             const bool ok = __all_sync(0xffffffffu, mbar_wait(tfull + buf, uint32_t(use & 1), ctl));
             tc_fence_after();
@@ -679,6 +781,10 @@ ra_status run(const char* who, const ra_gemm4_args& a, cudaStream_t st) {
   const int tm = pair ? P_TM : BM;
   p.bn = plan.bn;
   p.w_tiles = plan.bn > 128 ? 2 : 1;
+  p.sf_cols = scale_cols(p.groups, p.w_tiles);
+  p.sf_bufs = (TMEM_COLS - 2 * plan.bn) / p.sf_cols;
+  const int stages = pair ? Layout<true>::STAGES : Layout<false>::STAGES;
+  if (p.sf_bufs > stages) p.sf_bufs = stages;
   p.stage_tx = A_BYTES + (pair ? plan.bn / 2 : plan.bn) * (CHUNK / 2) + p.groups * 512 * (1 + p.w_tiles);
   const int64_t cols = (a.N + plan.bn - 1) / plan.bn;
   p.cols = int32_t(cols);
