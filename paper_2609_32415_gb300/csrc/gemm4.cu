@@ -204,11 +204,52 @@ __device__ __forceinline__ bool warp_wait(uint32_t peeked, uint64_t* bar, uint32
 }
 // A value that is the same in every lane, known to be so.
 __device__ __forceinline__ int same(int v) { return __shfl_sync(0xffffffffu, v, 0); }
-// The walk's tile t, for a converged warp.
+// Walk's order of the tiles (gemm_body.cuh) by counting on from the tile before, without
+// divisions but in the last band: the issuer, whose stages take about as long to issue as their
+// MMAs run, spent 0.6 us a tile on those.
 template <int TM, int EPI>
-__device__ __forceinline__ bool tile_at(const Params& p, Walk<TM, EPI>& walk, int64_t t, Tile& tl) {
+struct Tiles {
+  int g = 0, s = 0, cols = -1;  // the piece: a segment's sample, and its column tiles
+  int band = 0;                 // first row tile of the band of GROUP_M
+  uint32_t idx = 0;             // the tile's number within the band
+  __device__ __forceinline__ int piece_cols(const Params& p) const {
+    if (p.m_tiles[g] == 0) return 0;
+    Walk<TM, EPI> w;
+    w.g = g;
+    w.s = s;
+    return w.piece_cols(p);
+  }
+  // `by` tiles on (the first call: from the first one); false past the last one.
+  __device__ __forceinline__ bool on(const Params& p, uint32_t by, Tile& r) {
+    if (cols < 0) cols = piece_cols(p);
+    idx += by;
+    uint32_t rows = uint32_t(min(GROUP_M, p.m_tiles[g] - band));
+    while (idx >= rows * uint32_t(cols)) {
+      idx -= rows * uint32_t(cols);
+      band += GROUP_M;
+      if (cols == 0 || band >= p.m_tiles[g]) {
+        band = 0;
+        if (++s == p.B) {
+          s = 0;
+          if (++g == p.n_seg) return false;
+        }
+        cols = piece_cols(p);
+      }
+      rows = uint32_t(min(GROUP_M, p.m_tiles[g] - band));
+    }
+    const uint32_t n = rows == GROUP_M ? idx / GROUP_M : idx / rows;
+    r.seg = g;
+    r.s = s;
+    r.m0 = (band + int(idx - n * rows)) * TM;
+    r.n0 = int(n) * p.bn;
+    return true;
+  }
+};
+// The same for a converged warp, whose values are then known to be the same in every lane.
+template <int TM, int EPI>
+__device__ __forceinline__ bool warp_tile(const Params& p, Tiles<TM, EPI>& tiles, uint32_t by, Tile& tl) {
   Tile r{0, 0, 0, 0};
-  const int more = same(walk.at(p, t, r));
+  const int more = same(tiles.on(p, by, r));
   tl = Tile{same(r.seg), same(r.s), same(r.m0), same(r.n0)};
   return more != 0;
 }
@@ -285,7 +326,7 @@ __global__ void __launch_bounds__(THREADS, 1) gemm4_kernel(const __grid_constant
   volatile int* live = reinterpret_cast<volatile int*>(smem + L::OFF_MISC + 8);
   const int warp = same(int(threadIdx.x >> 5)), lane = threadIdx.x & 31;
   const int rank = SPLIT ? int(cluster_rank()) : 0, cs = SPLIT ? int(cluster_size()) : 1;
-  const int64_t t0 = SPLIT ? blockIdx.x / cs : blockIdx.x, step = SPLIT ? gridDim.x / cs : gridDim.x;
+  const uint32_t t0 = SPLIT ? blockIdx.x / cs : blockIdx.x, step = SPLIT ? gridDim.x / cs : gridDim.x;
   const int kb0 = SPLIT ? p.kblocks * rank / cs : 0;  // this CTA's stages of K
   const int kb1 = SPLIT ? p.kblocks * (rank + 1) / cs : p.kblocks;
   const int bn = p.bn;
@@ -306,9 +347,9 @@ __global__ void __launch_bounds__(THREADS, 1) gemm4_kernel(const __grid_constant
   if (warp == 1) tmem_alloc(tmem_slot, TMEM_COLS);
   if (SPLIT && warp == 2) {
     pdl_wait();
-    Walk<BM, EPI> walk;
+    Tiles<BM, EPI> tiles;
     Tile tl;
-    *live = walk.at(p, t0, tl);
+    *live = tiles.on(p, t0, tl);
   }
   tc_fence_before();
   __syncthreads();
@@ -337,9 +378,9 @@ __global__ void __launch_bounds__(THREADS, 1) gemm4_kernel(const __grid_constant
       pdl_wait();
       Ring<STAGES> in;
       bool ok = true;
-      Walk<BM, EPI> walk;
+      Tiles<BM, EPI> tiles;
       Tile tl;
-      for (int64_t t = t0; ok && tile_at(p, walk, t, tl); t += step) {
+      for (uint32_t by = t0; ok && warp_tile(p, tiles, by, tl); by = step) {
         for (int kb = kb0; kb < kb1; ++kb) {
           if (loads >= STAGES && !(ok = warp_wait(empty + in.st, in.ph ^ 1, ctl))) break;
           const uint32_t stage = smem_u32(smem) + in.st * L::STAGE_BYTES, bar = smem_u32(full + in.st);
@@ -365,9 +406,9 @@ __global__ void __launch_bounds__(THREADS, 1) gemm4_kernel(const __grid_constant
       uint32_t filled = 0;
       Scales<STAGES> sf(p);
       bool ok = true;
-      Walk<BM, EPI> walk;
+      Tiles<BM, EPI> tiles;
       Tile tl;
-      for (int64_t t = t0; ok && tile_at(p, walk, t, tl); t += step) {
+      for (uint32_t by = t0; ok && warp_tile(p, tiles, by, tl); by = step) {
         const int buf = i & 1, use = i >> 1;
         if (use > 0 && !(ok = warp_wait(tempty + buf, uint32_t((use - 1) & 1), ctl))) break;
         tc_fence_after();
@@ -398,9 +439,9 @@ __global__ void __launch_bounds__(THREADS, 1) gemm4_kernel(const __grid_constant
     w.vec0 = reinterpret_cast<float*>(w.stage + EPI_STAGE_BYTES);
     w.vec1 = w.vec0 + 128;
     int i = 0;
-    Walk<BM, EPI> walk;
+    Tiles<BM, EPI> tiles;
     Tile tl;
-    for (int64_t t = t0; walk.at(p, t, tl); t += step) {
+    for (uint32_t by = t0; tiles.on(p, by, tl); by = step) {
       const int buf = i & 1, use = i >> 1;
       w.row0 = tl.m0 + quarter * 32;
       w.nrow = min(32, p.rows[tl.seg] - w.row0);
@@ -472,7 +513,7 @@ __global__ void __launch_bounds__(THREADS, 1) gemm4_pair_kernel(const __grid_con
   volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + L::OFF_MISC + 4);
   const int warp = same(int(threadIdx.x >> 5)), lane = threadIdx.x & 31;
   const uint32_t rank = uint32_t(same(int(cluster_rank())));
-  const int64_t cid = blockIdx.x >> 1, ncl = gridDim.x >> 1;
+  const uint32_t cid = blockIdx.x >> 1, ncl = gridDim.x >> 1;
   if (threadIdx.x == 0) {
     for (int s = 0; s < STAGES; ++s) {
       mbar_init(full + s, 1);
@@ -512,9 +553,9 @@ __global__ void __launch_bounds__(THREADS, 1) gemm4_pair_kernel(const __grid_con
       const uint32_t full0 = mapa_shared(smem_u32(full), 0);  // rank 0's full barriers
       Ring<STAGES> in;
       bool ok = true;
-      Walk<P_TM, EPI> walk;
+      Tiles<P_TM, EPI> tiles;
       Tile tl;
-      for (int64_t t = cid; ok && tile_at(p, walk, t, tl); t += ncl) {
+      for (uint32_t by = cid; ok && warp_tile(p, tiles, by, tl); by = ncl) {
         for (int kb = 0; kb < p.kblocks; ++kb) {
           if (loads >= STAGES && !(ok = warp_wait(empty + in.st, in.ph ^ 1, ctl))) break;
           const uint32_t stage = smem_u32(smem) + in.st * L::STAGE_BYTES, bar = full0 + 8u * in.st;
@@ -541,9 +582,9 @@ __global__ void __launch_bounds__(THREADS, 1) gemm4_pair_kernel(const __grid_con
       uint32_t filled = 0;
       Scales<STAGES> sf(p);
       bool ok = true;
-      Walk<P_TM, EPI> walk;
+      Tiles<P_TM, EPI> tiles;
       Tile tl;
-      for (int64_t t = cid; ok && tile_at(p, walk, t, tl); t += ncl) {
+      for (uint32_t by = cid; ok && warp_tile(p, tiles, by, tl); by = ncl) {
         const int buf = i & 1, use = i >> 1;
         if (use > 0 && !(ok = warp_wait<true>(tempty + buf, uint32_t((use - 1) & 1), ctl))) break;
         tc_fence_after();
@@ -575,9 +616,9 @@ __global__ void __launch_bounds__(THREADS, 1) gemm4_pair_kernel(const __grid_con
     w.vec1 = w.vec0 + 128;
     const uint32_t tempty0 = mapa_shared(smem_u32(tempty), 0);
     int i = 0;
-    Walk<P_TM, EPI> walk;
+    Tiles<P_TM, EPI> tiles;
     Tile tl;
-    for (int64_t t = cid; walk.at(p, t, tl); t += ncl) {
+    for (uint32_t by = cid; tiles.on(p, by, tl); by = ncl) {
       const int buf = i & 1, use = i >> 1;
       w.row0 = tl.m0 + int(rank) * 128 + quarter * 32;
       w.cols = p.bn;
