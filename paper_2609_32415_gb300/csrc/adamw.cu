@@ -4,7 +4,7 @@
 //
 // The tensors' descriptions travel as kernel arguments (up to 256 a launch; calls of more
 // launch again), so a call copies nothing to the device and can be captured. Each tensor is
-// cut into chunks of 4096 elements; a CTA finds its chunk's tensor by bisection of the
+// cut into chunks of a few thousand elements; a CTA finds its chunk's tensor by bisection of the
 // first chunks' numbers.
 //
 // Bandwidth-bound: bytes a weight of the step are 8 (p) + 2 or 4 (g) + 2 (w) + 16 with
@@ -26,7 +26,12 @@ namespace ra {
 namespace opt {
 
 constexpr int THREADS = 256;
-constexpr int CHUNK = 4096;     // elements of a CTA's share of a tensor
+// Elements of a CTA's share of a tensor: long ones have more loads on their way in a thread (the
+// norm) or in front of its computations (8-bit moments); the plain streams of the step with
+// fp32 moments took 1262 us at 4096, 1296 at 8192 (317 M weights).
+constexpr int CHUNK = 8192;
+template <int BITS>
+constexpr int STEP_CHUNK = BITS == 8 ? CHUNK : CHUNK / 2;
 constexpr int MAX_TENSORS = 256;  // of a launch
 
 // ------------------------------------------------------------------ norm
@@ -75,7 +80,7 @@ __device__ __forceinline__ double block_sum(double v, double* warps) {
   return s;
 }
 
-// Sums in an order that the sizes alone decide: a thread's squares of a chunk in fp32 (16 of
+// Sums in an order that the sizes alone decide: a thread's squares of a chunk in fp32 (32 of
 // them), its chunks, the CTA's threads and the CTAs in fp64; the CTA that takes the last
 // ticket of the call adds the CTAs' sums up.
 __global__ void __launch_bounds__(THREADS) norm_kernel(const __grid_constant__ NormParams p) {
@@ -92,11 +97,12 @@ __global__ void __launch_bounds__(THREADS) norm_kernel(const __grid_constant__ N
     if (t.bf16) {
       const __nv_bfloat16* g = static_cast<const __nv_bfloat16*>(t.g) + i0;
       if (n == CHUNK && (reinterpret_cast<uintptr_t>(g) & 15) == 0) {
-        uint4 v[2];
+        constexpr int PIECES = CHUNK / (8 * THREADS);
+        uint4 v[PIECES];
 #pragma unroll
-        for (int k = 0; k < 2; ++k) v[k] = reinterpret_cast<const uint4*>(g)[threadIdx.x + k * THREADS];
+        for (int k = 0; k < PIECES; ++k) v[k] = reinterpret_cast<const uint4*>(g)[threadIdx.x + k * THREADS];
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
+        for (int k = 0; k < PIECES; ++k) {
           const uint32_t w[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
@@ -114,11 +120,12 @@ __global__ void __launch_bounds__(THREADS) norm_kernel(const __grid_constant__ N
     } else {
       const float* g = static_cast<const float*>(t.g) + i0;
       if (n == CHUNK && (reinterpret_cast<uintptr_t>(g) & 15) == 0) {
-        float4 v[4];
+        constexpr int PIECES = CHUNK / (4 * THREADS);
+        float4 v[PIECES];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) v[k] = reinterpret_cast<const float4*>(g)[threadIdx.x + k * THREADS];
+        for (int k = 0; k < PIECES; ++k) v[k] = reinterpret_cast<const float4*>(g)[threadIdx.x + k * THREADS];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
+        for (int k = 0; k < PIECES; ++k) {
           s = fmaf(v[k].x, v[k].x, s);
           s = fmaf(v[k].y, v[k].y, s);
           s = fmaf(v[k].z, v[k].z, s);
@@ -184,41 +191,36 @@ __device__ __forceinline__ uint32_t mix(uint32_t x) {
 }
 
 struct Rates {
-  float lr, decay, c, inv1, inv2;  // inv: 1 / (1 - beta^t)
+  float lr1, root2, decay, c;  // lr / (1 - beta1^t), 2^-12 / sqrt(1 - beta2^t), lr times the decay
 };
 
-// Eight elements' update. m and v by the same fp32 operations, each rounded, that the formula
-// names: their 8-bit forms depend on the last bit.
-__device__ __forceinline__ void update(const StepParams& h, const Rates& r, const float (&g)[8], float (&p)[8],
-                                       float (&m)[8], float (&v)[8]) {
+// Eight elements' update; b1, b2: the betas, times the scales of what m and v hold (powers of two:
+// the product with the scale is exact wherever it stands). m and v by the fp32 operations
+// that the formula names, each rounded: their 8-bit forms depend on the last bit. The root and the
+// quotient are the hardware's (2 ulp), of which the weight takes lr times.
+__device__ __forceinline__ void update(const StepParams& h, const Rates& r, float b1, float b2, const float (&g)[8],
+                                       float (&p)[8], float (&m)[8], float (&v)[8]) {
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const float gc = __fmul_rn(g[i], r.c);
-    m[i] = __fadd_rn(__fmul_rn(h.beta1, m[i]), __fmul_rn(h.rest1, gc));
-    v[i] = __fadd_rn(__fmul_rn(h.beta2, v[i]), __fmul_rn(h.rest2, __fmul_rn(gc, gc)));
-    const float down = __fadd_rn(__fsqrt_rn(v[i] * r.inv2), h.eps);
-    p[i] = p[i] - r.decay * p[i] - __fdividef(r.lr * (m[i] * r.inv1), down);
+    m[i] = __fadd_rn(__fmul_rn(b1, m[i]), __fmul_rn(h.rest1, gc));
+    v[i] = __fadd_rn(__fmul_rn(b2, v[i]), __fmul_rn(h.rest2, __fmul_rn(gc, gc)));
+    // lr m / (1 - beta1^t) / (sqrt(v) / sqrt(1 - beta2^t) + eps); the root of 2^24 v, which is no
+    // denormal number, so that the short form of the root will do
+    float root, move;
+    asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(root) : "f"(v[i] * 16777216.f));
+    asm("div.approx.ftz.f32 %0, %1, %2;" : "=f"(move) : "f"(r.lr1 * m[i]), "f"(fmaf(root, r.root2, h.eps)));
+    p[i] = fmaf(-r.decay, p[i], p[i]) - move;
   }
 }
 
 // The smallest power of two with amax <= 448 s (448 = 1.75 2^8), as its biased exponent.
 __device__ __forceinline__ uint32_t block_scale8(float amax) {
-  const uint32_t bits = __float_as_uint(amax);
+  const uint32_t bits = __float_as_uint(amax) & 0x7fffffffu;
   if (bits >= 0x7f800000u) return 0xffu;
   const int b = int((bits + 0x1fffffu) >> 23) - 8;
   return uint32_t(min(max(b, 1), 254));
 }
-// |y| <= 448 to one of the e4m3 values beside it, by 16 random bits. Above 2^-6 the steps are
-// 2^20 units of the fp32 pattern; below they are 2^-9, as just above 2^-6.
-__device__ __forceinline__ uint32_t round8(float y, uint32_t r16) {
-  const float a = fabsf(y);
-  const bool small = a < 0.015625f;
-  const uint32_t z = (__float_as_uint(small ? a + 0.015625f : a) + (r16 << 4) + 8u) >> 20;
-  // exponent and mantissa of z are (z >> 3) - 127 and z & 7; e4m3's bias is 7
-  const uint32_t code = z - ((127 - 7) << 3) - (small ? 8u : 0u);
-  return code | (__float_as_uint(y) >> 31 << 7);
-}
-
 template <bool WIDE>
 __device__ __forceinline__ void load8(const float* src, int n, float (&x)[8]) {
   if (WIDE) {
@@ -275,40 +277,96 @@ __device__ __forceinline__ void store_bytes(uint8_t* dst, int n, uint2 v) {
       if (i < n) dst[i] = uint8_t((i < 4 ? v.x : v.y) >> (8 * (i & 3)));
   }
 }
-__device__ __forceinline__ void values8(uint2 codes, uint32_t scale, float (&x)[8]) {
-  const float s = scale == 0xffu ? __int_as_float(0x7fffffff)
-                                 : scale == 0 ? __uint_as_float(0x00400000u) : __uint_as_float(scale << 23);
+__device__ __forceinline__ void values8(uint2 codes, float (&x)[8]) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const uint32_t w = i < 2 ? codes.x : codes.y;
     const __half2 h(__nv_cvt_fp8x2_to_halfraw2(__nv_fp8x2_storage_t(w >> (16 * (i & 1))), __NV_E4M3));
     const float2 f = __half22float2(h);
-    x[2 * i] = f.x * s;
-    x[2 * i + 1] = f.y * s;
+    x[2 * i] = f.x;
+    x[2 * i + 1] = f.y;
   }
+}
+__device__ __forceinline__ float scale_value(uint32_t scale) {
+  return scale == 0xffu ? __int_as_float(0x7fffffff)
+                        : scale == 0 ? __uint_as_float(0x00400000u) : __uint_as_float(scale << 23);
+}
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float m;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(a), "f"(b));
+  return m;
+}
+__device__ __forceinline__ float max_nan(float a, float b, float c) {
+  float m;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(m) : "f"(a), "f"(b), "f"(c));
+  return m;
 }
 // Four threads (8 elements each) have a block of 32.
 __device__ __forceinline__ uint32_t scale_of_block(const float (&x)[8]) {
-  // as integers, so that NaN counts as the largest
-  uint32_t top = 0;
+  float top = max_nan(fabsf(x[0]), fabsf(x[1]));
 #pragma unroll
-  for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
-  top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-  top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-  return block_scale8(__uint_as_float(top));
+  for (int i = 2; i < 8; i += 2) top = max_nan(top, fabsf(x[i]), fabsf(x[i + 1]));
+  top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, 1));
+  top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, 2));
+  return block_scale8(top);
 }
+// The e4m3 bytes of eight moments under their scale, each rounded by 16 random bits. SECOND: the
+// second moment, whose random bits are the upper halves and which stays above zero.
+// y 2^-120, |y| <= 448, has e4m3's exponent in the fp32 pattern's exponent field, and where e4m3
+// is denormal so is fp32: bits 20 and up of the pattern are the code, those below what lies
+// between two codes. Sixteen patterns plus 256 random numbers plus 128 leave the code in the
+// upper byte.
 template <bool SECOND>
 __device__ __forceinline__ uint2 codes8(const float (&x)[8], uint32_t scale, const uint32_t (&r)[8]) {
-  uint2 c = make_uint2(0, 0);
-  if (scale == 0xffu) return c;
+  if (scale == 0xffu) return make_uint2(0, 0);
   const float f = __uint_as_float((254u - scale) << 23);
+  uint32_t c[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    uint32_t q = round8(x[i] * f, SECOND ? r[i] >> 16 : r[i] & 0xffffu);
-    if (SECOND) q = x[i] > 0.f ? max(q, 1u) : q;
-    (i < 4 ? c.x : c.y) |= q << (8 * (i & 3));
+    const uint32_t y = __float_as_uint(__fmul_rn(__fmul_rn(x[i], f), 7.52316384526264e-37f));  // 2^-120
+    const uint32_t random = __byte_perm(r[i], 0x80u, SECOND ? 0x5324 : 0x5104);  // r16 << 8 | 0x80
+    c[i] = y * 16u + random;
+    if (SECOND)  // 2^24 x has an exponent where x is not zero
+      c[i] = max(c[i], min(__float_as_uint(x[i] * 16777216.f), 1u << 24));
+    else
+      c[i] = (c[i] & 0x7fffffffu) | (y & 0x80000000u);
   }
-  return c;
+  return make_uint2(__byte_perm(__byte_perm(c[0], c[1], 0x0073), __byte_perm(c[2], c[3], 0x0073), 0x5410),
+                    __byte_perm(__byte_perm(c[4], c[5], 0x0073), __byte_perm(c[6], c[7], 0x0073), 0x5410));
+}
+
+// The new weights and their rounding to bf16.
+template <bool WIDE>
+__device__ __forceinline__ void store_weights(const StepTensor& t, int64_t at, int n, const float (&p)[8]) {
+  store8<WIDE>(t.p + at, n, p);
+  if (!t.w) return;
+  if (WIDE) {
+    *reinterpret_cast<uint4*>(t.w + at) =
+        make_uint4(pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3]), pack_bf16x2(p[4], p[5]), pack_bf16x2(p[6], p[7]));
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < n) t.w[at + i] = __float2bfloat16_rn(p[i]);
+  }
+}
+// Rounds eight elements' moments to 8 bits and stores them and the weights.
+template <bool WIDE>
+__device__ __forceinline__ void finish8(const StepTensor& t, uint32_t key, int64_t at, int n, const float (&p)[8],
+                                        const float (&m)[8], const float (&v)[8]) {
+  const uint32_t ms = scale_of_block(m), vs = scale_of_block(v);
+  uint32_t bits[8];
+  const uint64_t c = t.counter + uint64_t(at);
+  const uint32_t k = (c >> 32) ? mix(key ^ uint32_t(c >> 32)) : key;  // a run of 8 from a multiple of 8 on
+#pragma unroll
+  for (int i = 0; i < 8; ++i) bits[i] = mix(((uint32_t(c) + i) * 0x9e3779b1u) ^ k);
+  if (n <= 0) return;
+  store_bytes<WIDE>(static_cast<uint8_t*>(t.m) + at, n, codes8<false>(m, ms, bits));
+  store_bytes<WIDE>(static_cast<uint8_t*>(t.v) + at, n, codes8<true>(v, vs, bits));
+  if ((at & 31) == 0) {
+    t.m_scale[at >> 5] = uint8_t(ms);
+    t.v_scale[at >> 5] = uint8_t(vs);
+  }
+  store_weights<WIDE>(t, at, n, p);
 }
 
 // Eight elements of a tensor from `at` on, n of them in the tensor (at most 0: none, but
@@ -316,7 +374,7 @@ __device__ __forceinline__ uint2 codes8(const float (&x)[8], uint32_t scale, con
 template <int BITS, bool WIDE>
 __device__ __forceinline__ void step8(const StepParams& h, const StepTensor& t, const Rates& r, uint32_t key,
                                       int64_t at, int n) {
-  float p[8], g[8], m[8], v[8];
+  float p[8], g[8], m[8], v[8], b1 = h.beta1, b2 = h.beta2;
   if (n > 0) {
     load8<WIDE>(t.p + at, n, p);
     if (t.bf16)
@@ -327,56 +385,81 @@ __device__ __forceinline__ void step8(const StepParams& h, const StepTensor& t, 
       load8<WIDE>(static_cast<const float*>(t.m) + at, n, m);
       load8<WIDE>(static_cast<const float*>(t.v) + at, n, v);
     } else {
-      values8(load_bytes<WIDE>(static_cast<const uint8_t*>(t.m) + at, n), t.m_scale[at >> 5], m);
-      values8(load_bytes<WIDE>(static_cast<const uint8_t*>(t.v) + at, n), t.v_scale[at >> 5], v);
+      const uint2 mc = load_bytes<WIDE>(static_cast<const uint8_t*>(t.m) + at, n);
+      const uint2 vc = load_bytes<WIDE>(static_cast<const uint8_t*>(t.v) + at, n);
+      b1 *= scale_value(t.m_scale[at >> 5]);
+      b2 *= scale_value(t.v_scale[at >> 5]);
+      values8(mc, m);
+      values8(vc, v);
     }
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i) p[i] = g[i] = m[i] = v[i] = 0.f;
   }
-  update(h, r, g, p, m, v);
+  update(h, r, b1, b2, g, p, m, v);
   if (BITS == 8) {
     if (n < 8) {  // what is not in the tensor has no part in the block
 #pragma unroll
       for (int i = 0; i < 8; ++i)
         if (i >= n) m[i] = v[i] = 0.f;
     }
-    const uint32_t ms = scale_of_block(m), vs = scale_of_block(v);
-    uint32_t bits[8];
-    const uint64_t c = t.counter + uint64_t(at);
-    const uint32_t k = (c >> 32) ? mix(key ^ uint32_t(c >> 32)) : key;  // a run of 8 from a multiple of 8 on
-#pragma unroll
-    for (int i = 0; i < 8; ++i) bits[i] = mix(((uint32_t(c) + i) * 0x9e3779b1u) ^ k);
-    if (n > 0) {
-      store_bytes<WIDE>(static_cast<uint8_t*>(t.m) + at, n, codes8<false>(m, ms, bits));
-      store_bytes<WIDE>(static_cast<uint8_t*>(t.v) + at, n, codes8<true>(v, vs, bits));
-      if ((at & 31) == 0) {
-        t.m_scale[at >> 5] = uint8_t(ms);
-        t.v_scale[at >> 5] = uint8_t(vs);
-      }
-    }
+    finish8<WIDE>(t, key, at, n, p, m, v);
+  } else if (n > 0) {
+    store8<WIDE>(static_cast<float*>(t.m) + at, n, m);
+    store8<WIDE>(static_cast<float*>(t.v) + at, n, v);
+    store_weights<WIDE>(t, at, n, p);
   }
-  if (n > 0) {
-    store8<WIDE>(t.p + at, n, p);
-    if (BITS == 32) {
-      store8<WIDE>(static_cast<float*>(t.m) + at, n, m);
-      store8<WIDE>(static_cast<float*>(t.v) + at, n, v);
-    }
-    if (t.w) {
-      if (WIDE) {
-        *reinterpret_cast<uint4*>(t.w + at) =
-            make_uint4(pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3]), pack_bf16x2(p[4], p[5]), pack_bf16x2(p[6], p[7]));
-      } else {
+}
+
+// What eight elements with 8-bit moments need, as it lies in memory.
+template <bool BF16>
+struct Raw8 {
+  float4 p[2];
+  uint4 g[BF16 ? 1 : 2];
+  uint2 m, v;
+  uint32_t m_scale, v_scale;
+  __device__ __forceinline__ void load(const StepTensor& t, int64_t at) {
+    p[0] = reinterpret_cast<const float4*>(t.p + at)[0];
+    p[1] = reinterpret_cast<const float4*>(t.p + at)[1];
+    const uint4* src = reinterpret_cast<const uint4*>(static_cast<const char*>(t.g) + at * (BF16 ? 2 : 4));
+    g[0] = src[0];
+    if (!BF16) g[BF16 ? 0 : 1] = src[1];
+    m = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(t.m) + at);
+    v = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(t.v) + at);
+    m_scale = t.m_scale[at >> 5];
+    v_scale = t.v_scale[at >> 5];
+  }
+};
+
+// A whole chunk with 8-bit moments: the loads of the next eight elements are on their way while
+// these are computed (70 instructions an element); without, the warps waited for memory half
+// their time: 1144 -> 833 us for 317 M weights, 6.1 TB/s.
+template <bool BF16>
+__device__ __forceinline__ void whole_chunk(const StepParams& h, const StepTensor& t, const Rates& r, uint32_t key,
+                                            int64_t i0) {
+  constexpr int PASSES = CHUNK / (8 * THREADS);
+  int64_t at = i0 + int(threadIdx.x) * 8;
+  Raw8<BF16> next;
+  next.load(t, at);
+#pragma unroll 1
+  for (int k = 0; k < PASSES; ++k, at += 8 * THREADS) {
+    const Raw8<BF16> in = next;
+    if (k + 1 < PASSES) next.load(t, at + 8 * THREADS);
+    float p[8] = {in.p[0].x, in.p[0].y, in.p[0].z, in.p[0].w, in.p[1].x, in.p[1].y, in.p[1].z, in.p[1].w};
+    float g[8], m[8], v[8];
+    const uint32_t* w = reinterpret_cast<const uint32_t*>(in.g);
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if (i < n) t.w[at + i] = __float2bfloat16_rn(p[i]);
-      }
-    }
+    for (int i = 0; i < 8; ++i)
+      g[i] = BF16 ? __uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16) : __uint_as_float(w[i]);
+    values8(in.m, m);
+    values8(in.v, v);
+    update(h, r, h.beta1 * scale_value(in.m_scale), h.beta2 * scale_value(in.v_scale), g, p, m, v);
+    finish8<true>(t, key, at, 8, p, m, v);
   }
 }
 
 template <int BITS>
-__global__ void __launch_bounds__(THREADS) step_kernel(const __grid_constant__ StepParams h) {
+__global__ void __launch_bounds__(THREADS, BITS == 8 ? 3 : 4) step_kernel(const __grid_constant__ StepParams h) {
   pdl_wait();
   pdl_launch();
   const uint32_t chunk = blockIdx.x;
@@ -384,16 +467,24 @@ __global__ void __launch_bounds__(THREADS) step_kernel(const __grid_constant__ S
   Rates r;
   r.c = h.grad_scale ? *h.grad_scale : 1.f;
   if (!isfinite(r.c)) return;
-  r.lr = h.lr_dev ? *h.lr_dev : h.lr;
-  r.decay = r.lr * h.decay;
+  const float lr = h.lr_dev ? *h.lr_dev : h.lr;
+  r.decay = lr * h.decay;
   const uint32_t step = h.step_dev ? uint32_t(max(*h.step_dev, 1)) : h.step;
   // 1 - beta^t = -expm1(t ln beta): no cancellation at small t
-  r.inv1 = h.beta1 > 0.f ? -1.f / expm1f(float(step) * h.log1) : 1.f;
-  r.inv2 = h.beta2 > 0.f ? -1.f / expm1f(float(step) * h.log2) : 1.f;
+  r.lr1 = h.beta1 > 0.f ? -lr / expm1f(float(step) * h.log1) : lr;
+  r.root2 = h.beta2 > 0.f ? rsqrtf(-expm1f(float(step) * h.log2)) : 1.f;
+  r.root2 *= 0.000244140625f;  // of the root of 2^24 v
   const uint32_t key = mix(mix(mix(h.seed_lo) ^ h.seed_hi) ^ step);
-  const int64_t i0 = int64_t(chunk - t.first) * CHUNK;
+  const int64_t i0 = int64_t(chunk - t.first) * STEP_CHUNK<BITS>;
+  if (BITS == 8 && t.wide && t.n - i0 >= STEP_CHUNK<BITS>) {
+    if (t.bf16)
+      whole_chunk<true>(h, t, r, key, i0);
+    else
+      whole_chunk<false>(h, t, r, key, i0);
+    return;
+  }
 #pragma unroll
-  for (int k = 0; k < CHUNK / (8 * THREADS); ++k) {
+  for (int k = 0; k < STEP_CHUNK<BITS> / (8 * THREADS); ++k) {
     const int64_t at = i0 + (k * THREADS + int(threadIdx.x)) * 8;
     const int n = int(min(int64_t(8), t.n - at));
     if (t.wide && n == 8)
@@ -603,6 +694,7 @@ extern "C" ra_status refadapt_adamw(const ra_adamw_args* a, void* stream) {
   p.grad_scale = a->grad_scale;
   uint64_t counter = 0;
   int64_t chunks = 0;
+  const int chunk = small ? STEP_CHUNK<8> : STEP_CHUNK<32>;
   auto flush = [&]() {
     if (p.n_tensors == 0) return RA_OK;
     const ra_status r = opt::launch("refadapt_adamw", p, small ? step_kernel<8> : step_kernel<32>, chunks, st);
@@ -613,7 +705,7 @@ extern "C" ra_status refadapt_adamw(const ra_adamw_args* a, void* stream) {
   for (int32_t i = 0; i < a->n_tensors; ++i) {
     const ra_adamw_tensor& t = a->tensors[i];
     if (t.n == 0) continue;
-    const int64_t mine = (t.n + CHUNK - 1) / CHUNK;
+    const int64_t mine = (t.n + chunk - 1) / chunk;
     if (p.n_tensors == MAX_TENSORS || chunks + mine > 2147483647) {
       const ra_status r = flush();
       if (r != RA_OK) return r;

@@ -261,7 +261,7 @@ def test_norm(cuda_ok, sizes, most):
     for _ in range(2):  # the workspace is ready again
         a.refadapt_grad_norm(grads, most, out, ws)
         want = np.sqrt(sum(float((d64(t) ** 2).sum()) for t in grads))
-        # 16 fp32 sums in a row, the rest in fp64: 17 half steps of the squares, half of that in the root
+        # 32 fp32 sums in a row, the rest in fp64: 33 half steps of the squares, half of that in the root: 2^-19.9
         assert abs(float(out[0]) - want) <= 2.0 ** -19 * want
         clip = most / want if want > most else 1.0
         assert abs(float(out[1]) - clip) <= 2.0 ** -19 * clip
