@@ -29,11 +29,18 @@ namespace gemm4 {
 
 using namespace gemm;
 
+// Three warps share a tile row's columns: two chunks of 32 each, and at K = 2048 the MMAs of a tile
+// take no longer than that.
+constexpr int WAYS = 3, EPI4_WARPS = 4 * WAYS, THREADS4 = 64 + 32 * EPI4_WARPS;
 constexpr int CHUNK = 256;   // K of a stage
 constexpr int MAX_BN = 192;  // columns of a tile
 constexpr int A_BYTES = BM * CHUNK / 2;
 constexpr int SA_BYTES = 4 * 512;  // scales of 128 rows, up to four tiles (e4m3)
 constexpr int SF_BYTES = 3 * SA_BYTES;  // and of up to 256 weight rows
+
+constexpr int WARP_BYTES = EPI_STAGE_BYTES + 2 * 64 * 4;  // RoPE rows on their way, two vectors of its 64 columns
+// QKV: the rows' sums of squares of each chunk of columns, by TMEM lane quarter.
+constexpr int SUMS_BYTES = 4 * (MAX_BN / 32) * 32 * 4;
 
 // One CTA a tile, and CTA pairs (each stages half of the tile's weight rows).
 template <bool PAIR>
@@ -45,7 +52,8 @@ struct Layout {
   static constexpr int OFF_BAR = STAGES * STAGE_BYTES;
   static constexpr int OFF_MISC = OFF_BAR + (2 * STAGES + 6) * 8;  // full, empty, tfull[2], tempty[2], drain, parts_full
   static constexpr int OFF_EPI = (OFF_MISC + 16 + 127) / 128 * 128;
-  static constexpr int SMEM_ALLOC = OFF_EPI + EPI_WARPS * EPI_WARP_BYTES + 1024;
+  static constexpr int OFF_SUMS = OFF_EPI + EPI4_WARPS * WARP_BYTES;
+  static constexpr int SMEM_ALLOC = OFF_SUMS + SUMS_BYTES + 1024;
   static_assert(STAGE_BYTES % 1024 == 0 && OFF_SF % 1024 == 0, "swizzled tiles start on 1024 bytes");
   static_assert(SMEM_ALLOC <= 232448, "shared memory budget");
 };
@@ -63,6 +71,7 @@ struct Params4 : Params {
   int32_t w_tiles;                   // scale tiles of a tile's weight rows: 1 or 2
   int32_t sf_cols, sf_bufs;          // TMEM columns of a stage's scales, buffers of them
   uint32_t stage_tx;                 // bytes of a stage that one CTA loads
+  int32_t wide[3];                   // rows of the epilogue's tensors start on 32 bytes
   CUtensorMap tm_sa[3], tm_sw[3];
 };
 
@@ -71,85 +80,105 @@ struct Params4 : Params {
 __device__ __forceinline__ uint32_t idesc_mx4(int M, int N, int e8m0) {
   return (1u << 7) | (1u << 10) | (uint32_t(N >> 3) << 17) | (uint32_t(e8m0) << 23) | (uint32_t(M >> 4) << 24);
 }
-// Matrix descriptor of 32 rows of 16 bytes, 8 rows (128 bytes) after 8 rows, no swizzle.
-__device__ __forceinline__ uint64_t sdesc_scales(uint32_t saddr) {
-  return uint64_t((saddr >> 4) & 0x3FFFu) | (uint64_t(8) << 16) | (uint64_t(8) << 32) | (uint64_t(1) << 46);
-}
-
-// A stage's scales to TMEM columns sf.., then its MMAs (ksteps of 64, 1 to 4), by one thread of a
-// converged warp. One asm block, whose operands are the same in every lane and whose
-// addresses are the first ones plus immediates (tiles start on 1024 bytes, so that the sums never
-// carry out of a descriptor's address field): issued one by one from a single lane, with
-// descriptors made for each, 12 copies and 4 MMAs took 1.3 us, six times what the tensor core
-// needs for them. half_cols: columns by which the tile's first weight row lies inside a scale tile.
-#define RA_CP(GROUP, COL, DESC, UNITS)                                                                       \
-  "add.u32 c, %1, " COL ";\n\tadd.s64 s, " DESC ", " UNITS ";\n\t"                                           \
+// A stage's scales to TMEM columns sf.., then its MMAs (ksteps of 64, 1 to 4) and the commit that
+// frees the stage, by one thread of a converged warp. One asm block, whose operands are the same
+// in every lane and whose addresses are the first ones plus immediates (in units of 16 bytes;
+// below the descriptors' 14 bits of address): issued one by one from a single lane, with descriptors
+// made for each, 12 copies and 4 MMAs took 1.3 us, five times what they need. lo: the stage's shared
+// address / 16; sw: columns of the weight's scales (behind A's, and behind the rows of their
+// first tile that lie before the tile's first weight row).
+#define RA_CP(GROUP, COL, UNITS)                                                                             \
+  "add.u32 c, %1, " COL ";\n\tadd.u32 l, %2, " UNITS ";\n\tmov.b64 s, {l, %10};\n\t"                         \
   "@e tcgen05.cp.cta_group::" GROUP ".32x128b.warpx4 [c], s;\n\t"
-#define RA_MMA(GROUP, VEC, K, UNITS, IDESC, SA_COL, SW_COL, ACC)                                             \
-  "setp.gt.and.s32 q, %8, " K ", e;\n\t"                                                                     \
-  "add.s64 s, %4, " UNITS ";\n\tadd.s64 t, %5, " UNITS ";\n\tadd.u32 c, %1, " SA_COL ";\n\tadd.u32 w, %9, "  \
-  SW_COL ";\n\t"                                                                                             \
+#define RA_MMA(GROUP, VEC, K, A_UNITS, IDESC, SA_COL, SW_COL, ACC)                                           \
+  "setp.gt.and.s32 q, %5, " K ", e;\n\t"                                                                     \
+  "add.u32 l, %2, " A_UNITS ";\n\tmov.b64 s, {l, %9};\n\t"                                                   \
+  "add.u32 l, %7, " A_UNITS ";\n\tmov.b64 t, {l, %9};\n\t"                                                   \
+  "add.u32 c, %1, " SA_COL ";\n\tadd.u32 w, %8, " SW_COL ";\n\t"                                             \
   "@q tcgen05.mma.cta_group::" GROUP ".kind::mxf4nvf4.block_scale.scale_vec::" VEC " [%0], s, t, " IDESC     \
   ", [c], [w], " ACC ";\n\t"
-#define RA_STAGE(COPIES, MMAS)                                                                   \
+#define RA_STAGE(COPIES, MMAS, COMMIT)                                                                       \
   asm volatile(                                                                                              \
-      "{\n\t.reg .pred e, p, q, o;\n\t.reg .b64 s, t;\n\t.reg .b32 c, w, i;\n\t"                            \
+      "{\n\t.reg .pred e, p, q, o;\n\t.reg .b64 s, t;\n\t.reg .b32 c, w, i, l;\n\t"                         \
       "elect.sync _|e, 0xffffffff;\n\t"                                                                      \
-      "setp.ne.b32 p, %7, 0;\n\tsetp.eq.b32 o, %7, %7;\n\tor.b32 i, %6, 0x40000020;\n\t" COPIES MMAS "}" ::"r"(d), \
-      "r"(sf), "l"(s_a), "l"(s_w), "l"(a), "l"(b), "r"(idesc), "r"(acc), "r"(ksteps), "r"(sf + half_cols)      \
+      "setp.ne.b32 p, %4, 0;\n\tsetp.eq.b32 o, %4, %4;\n\tor.b32 i, %3, 0x40000020;\n\t" COPIES MMAS COMMIT "}" ::"r"(d), \
+      "r"(sf), "r"(lo), "r"(idesc), "r"(acc), "r"(ksteps), "r"(bar), "r"(lo + L::OFF_B / 16), "r"(sw),           \
+      "r"(HI_SW128), "r"(HI_SCALES)                                                                          \
       : "memory")
 // Scale tiles of a stage: e4m3 four for 64 of K each, e8m0 two for 128 each, whose halves the
 // descriptor selects (bits 4-5 and 30-31). Columns: A's tiles, four each, then for every one of
-// them the weight's, four or eight.
-#define RA_COPIES_E4M3(GROUP)                                                                                \
-  RA_CP(GROUP, "0", "%2", "0") RA_CP(GROUP, "16", "%3", "0") RA_CP(GROUP, "4", "%2", "32")                     \
-  RA_CP(GROUP, "20", "%3", "32") RA_CP(GROUP, "8", "%2", "64") RA_CP(GROUP, "24", "%3", "64")                  \
-  RA_CP(GROUP, "12", "%2", "96") RA_CP(GROUP, "28", "%3", "96")
-#define RA_COPIES_E4M3_2(GROUP)                                                                              \
-  RA_CP(GROUP, "0", "%2", "0") RA_CP(GROUP, "16", "%3", "0") RA_CP(GROUP, "20", "%3", "128")                   \
-  RA_CP(GROUP, "4", "%2", "32") RA_CP(GROUP, "24", "%3", "32") RA_CP(GROUP, "28", "%3", "160")                 \
-  RA_CP(GROUP, "8", "%2", "64") RA_CP(GROUP, "32", "%3", "64") RA_CP(GROUP, "36", "%3", "192")                 \
-  RA_CP(GROUP, "12", "%2", "96") RA_CP(GROUP, "40", "%3", "96") RA_CP(GROUP, "44", "%3", "224")
-#define RA_COPIES_E8M0(GROUP)                                                                                \
-  RA_CP(GROUP, "0", "%2", "0") RA_CP(GROUP, "8", "%3", "0") RA_CP(GROUP, "4", "%2", "32") RA_CP(GROUP, "12", "%3", "32")
-#define RA_COPIES_E8M0_2(GROUP)                                                                              \
-  RA_CP(GROUP, "0", "%2", "0") RA_CP(GROUP, "8", "%3", "0") RA_CP(GROUP, "12", "%3", "64")                     \
-  RA_CP(GROUP, "4", "%2", "32") RA_CP(GROUP, "16", "%3", "32") RA_CP(GROUP, "20", "%3", "96")
+// them the weight's, four or eight. The scales' units are counted from the stage on.
+#define RA_COPIES_E4M3(GROUP, A0, A1, A2, A3, W0, W1, W2, W3)                                                \
+  RA_CP(GROUP, "0", A0) RA_CP(GROUP, "16", W0) RA_CP(GROUP, "4", A1) RA_CP(GROUP, "20", W1)                    \
+  RA_CP(GROUP, "8", A2) RA_CP(GROUP, "24", W2) RA_CP(GROUP, "12", A3) RA_CP(GROUP, "28", W3)
+#define RA_COPIES_E4M3_2(GROUP, A0, A1, A2, A3, W0, W1, W2, W3, X0, X1, X2, X3)                              \
+  RA_CP(GROUP, "0", A0) RA_CP(GROUP, "16", W0) RA_CP(GROUP, "20", X0) RA_CP(GROUP, "4", A1)                    \
+  RA_CP(GROUP, "24", W1) RA_CP(GROUP, "28", X1) RA_CP(GROUP, "8", A2) RA_CP(GROUP, "32", W2)                   \
+  RA_CP(GROUP, "36", X2) RA_CP(GROUP, "12", A3) RA_CP(GROUP, "40", W3) RA_CP(GROUP, "44", X3)
+#define RA_COPIES_E8M0(GROUP, A0, A1, W0, W1)                                                                \
+  RA_CP(GROUP, "0", A0) RA_CP(GROUP, "8", W0) RA_CP(GROUP, "4", A1) RA_CP(GROUP, "12", W1)
+#define RA_COPIES_E8M0_2(GROUP, A0, A1, W0, W1, X0, X1)                                                      \
+  RA_CP(GROUP, "0", A0) RA_CP(GROUP, "8", W0) RA_CP(GROUP, "12", X0) RA_CP(GROUP, "4", A1)                     \
+  RA_CP(GROUP, "16", W1) RA_CP(GROUP, "20", X1)
 #define RA_MMAS_E4M3(GROUP)                                                                                  \
-  RA_MMA(GROUP, "4X", "0", "0", "%6", "0", "16", "p") RA_MMA(GROUP, "4X", "1", "2", "%6", "4", "20", "o")        \
-  RA_MMA(GROUP, "4X", "2", "4", "%6", "8", "24", "o") RA_MMA(GROUP, "4X", "3", "6", "%6", "12", "28", "o")
+  RA_MMA(GROUP, "4X", "0", "0", "%3", "0", "0", "p") RA_MMA(GROUP, "4X", "1", "2", "%3", "4", "4", "o")          \
+  RA_MMA(GROUP, "4X", "2", "4", "%3", "8", "8", "o") RA_MMA(GROUP, "4X", "3", "6", "%3", "12", "12", "o")
 #define RA_MMAS_E4M3_2(GROUP)                                                                                \
-  RA_MMA(GROUP, "4X", "0", "0", "%6", "0", "16", "p") RA_MMA(GROUP, "4X", "1", "2", "%6", "4", "24", "o")        \
-  RA_MMA(GROUP, "4X", "2", "4", "%6", "8", "32", "o") RA_MMA(GROUP, "4X", "3", "6", "%6", "12", "40", "o")
+  RA_MMA(GROUP, "4X", "0", "0", "%3", "0", "0", "p") RA_MMA(GROUP, "4X", "1", "2", "%3", "4", "8", "o")          \
+  RA_MMA(GROUP, "4X", "2", "4", "%3", "8", "16", "o") RA_MMA(GROUP, "4X", "3", "6", "%3", "12", "24", "o")
 #define RA_MMAS_E8M0(GROUP)                                                                                  \
-  RA_MMA(GROUP, "2X", "0", "0", "%6", "0", "8", "p") RA_MMA(GROUP, "2X", "1", "2", "i", "0", "8", "o")           \
-  RA_MMA(GROUP, "2X", "2", "4", "%6", "4", "12", "o") RA_MMA(GROUP, "2X", "3", "6", "i", "4", "12", "o")
+  RA_MMA(GROUP, "2X", "0", "0", "%3", "0", "0", "p") RA_MMA(GROUP, "2X", "1", "2", "i", "0", "0", "o")           \
+  RA_MMA(GROUP, "2X", "2", "4", "%3", "4", "4", "o") RA_MMA(GROUP, "2X", "3", "6", "i", "4", "4", "o")
 #define RA_MMAS_E8M0_2(GROUP)                                                                                \
-  RA_MMA(GROUP, "2X", "0", "0", "%6", "0", "8", "p") RA_MMA(GROUP, "2X", "1", "2", "i", "0", "8", "o")           \
-  RA_MMA(GROUP, "2X", "2", "4", "%6", "4", "16", "o") RA_MMA(GROUP, "2X", "3", "6", "i", "4", "16", "o")
-template <bool PAIR>
-__device__ __forceinline__ void issue_stage(const Params4& p, uint32_t stage, uint32_t sf, uint32_t d, uint32_t idesc,
-                                            uint32_t half_cols, int ksteps, bool first) {
+  RA_MMA(GROUP, "2X", "0", "0", "%3", "0", "0", "p") RA_MMA(GROUP, "2X", "1", "2", "i", "0", "0", "o")           \
+  RA_MMA(GROUP, "2X", "2", "4", "%3", "4", "8", "o") RA_MMA(GROUP, "2X", "3", "6", "i", "4", "8", "o")
+#define RA_COMMIT_2                                                                                          \
+  "mov.b32 c, 3;\n\t.reg .b16 m;\n\tcvt.u16.u32 m, c;\n\t"                                                  \
+  "@e tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%6], m;\n\t"
+#define RA_COMMIT_1 "@e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%6];\n\t"
+// Units of the scales within a stage, as immediates: pairs, single CTAs.
+#define RA_U2(N) RA_STR(1792 + N)
+#define RA_U1(N) RA_STR(2560 + N)
+#define RA_STR(N) RA_STR2(N)
+#define RA_STR2(N) #N
+static_assert(Layout<true>::OFF_SF / 16 == 1792 && Layout<false>::OFF_SF / 16 == 2560, "immediates of the copies");
+template <bool PAIR, bool E8M0>
+__device__ __forceinline__ void issue_stage(const Params4& p, uint32_t lo, uint32_t sf, uint32_t sw, uint32_t d,
+                                            uint32_t idesc, int ksteps, bool first, uint32_t bar) {
   using L = Layout<PAIR>;
-  const uint64_t a = sdesc_sw128(stage, 16, 1024), b = sdesc_sw128(stage + L::OFF_B, 16, 1024);
-  const uint64_t s_a = sdesc_scales(stage + L::OFF_SF), s_w = sdesc_scales(stage + L::OFF_SF + SA_BYTES);
+  constexpr uint32_t HI_SW128 = (1024u >> 4) | (1u << 14) | (2u << 29);  // 8 rows after 1024 bytes; version; swizzle
+  constexpr uint32_t HI_SCALES = 8u | (1u << 14);                        // 8 rows after 128 bytes; version
   const uint32_t acc = first ? 0u : 1u;
-  if constexpr (PAIR) {
-    if (p.e8m0) {
-      if (p.w_tiles == 2) RA_STAGE(RA_COPIES_E8M0_2("2"), RA_MMAS_E8M0_2("2"));
-      else RA_STAGE(RA_COPIES_E8M0("2"), RA_MMAS_E8M0("2"));
-    } else {
-      if (p.w_tiles == 2) RA_STAGE(RA_COPIES_E4M3_2("2"), RA_MMAS_E4M3_2("2"));
-      else RA_STAGE(RA_COPIES_E4M3("2"), RA_MMAS_E4M3("2"));
-    }
+  if constexpr (PAIR && E8M0) {
+    if (p.w_tiles == 2)
+      RA_STAGE(RA_COPIES_E8M0_2("2", RA_U2(0), RA_U2(32), RA_U2(128), RA_U2(160), RA_U2(192), RA_U2(224)),
+               RA_MMAS_E8M0_2("2"), RA_COMMIT_2);
+    else
+      RA_STAGE(RA_COPIES_E8M0("2", RA_U2(0), RA_U2(32), RA_U2(128), RA_U2(160)), RA_MMAS_E8M0("2"), RA_COMMIT_2);
+  } else if constexpr (PAIR) {
+    if (p.w_tiles == 2)
+      RA_STAGE(RA_COPIES_E4M3_2("2", RA_U2(0), RA_U2(32), RA_U2(64), RA_U2(96), RA_U2(128), RA_U2(160), RA_U2(192),
+                                RA_U2(224), RA_U2(256), RA_U2(288), RA_U2(320), RA_U2(352)),
+               RA_MMAS_E4M3_2("2"), RA_COMMIT_2);
+    else
+      RA_STAGE(RA_COPIES_E4M3("2", RA_U2(0), RA_U2(32), RA_U2(64), RA_U2(96), RA_U2(128), RA_U2(160), RA_U2(192),
+                              RA_U2(224)),
+               RA_MMAS_E4M3("2"), RA_COMMIT_2);
+  } else if constexpr (E8M0) {
+    if (p.w_tiles == 2)
+      RA_STAGE(RA_COPIES_E8M0_2("1", RA_U1(0), RA_U1(32), RA_U1(128), RA_U1(160), RA_U1(192), RA_U1(224)),
+               RA_MMAS_E8M0_2("1"), RA_COMMIT_1);
+    else
+      RA_STAGE(RA_COPIES_E8M0("1", RA_U1(0), RA_U1(32), RA_U1(128), RA_U1(160)), RA_MMAS_E8M0("1"), RA_COMMIT_1);
   } else {
-    if (p.e8m0) {
-      if (p.w_tiles == 2) RA_STAGE(RA_COPIES_E8M0_2("1"), RA_MMAS_E8M0_2("1"));
-      else RA_STAGE(RA_COPIES_E8M0("1"), RA_MMAS_E8M0("1"));
-    } else {
-      if (p.w_tiles == 2) RA_STAGE(RA_COPIES_E4M3_2("1"), RA_MMAS_E4M3_2("1"));
-      else RA_STAGE(RA_COPIES_E4M3("1"), RA_MMAS_E4M3("1"));
-    }
+    if (p.w_tiles == 2)
+      RA_STAGE(RA_COPIES_E4M3_2("1", RA_U1(0), RA_U1(32), RA_U1(64), RA_U1(96), RA_U1(128), RA_U1(160), RA_U1(192),
+                                RA_U1(224), RA_U1(256), RA_U1(288), RA_U1(320), RA_U1(352)),
+               RA_MMAS_E4M3_2("1"), RA_COMMIT_1);
+    else
+      RA_STAGE(RA_COPIES_E4M3("1", RA_U1(0), RA_U1(32), RA_U1(64), RA_U1(96), RA_U1(128), RA_U1(160), RA_U1(192),
+                              RA_U1(224)),
+               RA_MMAS_E4M3("1"), RA_COMMIT_1);
   }
 }
 #undef RA_CP
@@ -159,7 +188,7 @@ __device__ __forceinline__ void issue_stage(const Params4& p, uint32_t stage, ui
 // umma_commit and umma_commit_pair by one thread of a converged warp (the one that elect.sync
 // names is the same every time, so the commits cover what it issued).
 template <bool PAIR>
-__device__ __forceinline__ void commit_stage(uint64_t* bar) {
+__device__ __forceinline__ void commit_one(uint64_t* bar) {
   if constexpr (PAIR)
     asm volatile(
         "{\n\t.reg .pred e;\n\telect.sync _|e, 0xffffffff;\n\t"
@@ -185,6 +214,11 @@ __device__ __forceinline__ bool elect_one() {
 template <bool CLUSTER = false>
 __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, const WaitCtl& ctl) {
   return __all_sync(0xffffffffu, CLUSTER ? mbar_wait_cluster(bar, parity, ctl) : mbar_wait(bar, parity, ctl));
+}
+// Arrival on an mbarrier of another CTA of the cluster by a thread that publishes no memory with
+// it (its TMEM loads have ended): with release it waits for the thread's stores, about 0.5 us.
+__device__ __forceinline__ void mbar_arrive_remote_relaxed(uint32_t cluster_addr) {
+  asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
 // Has the phase completed? Asked before the work in front of it is issued, so that the answer's
 // latency (50 ns) passes meanwhile.
@@ -306,10 +340,261 @@ struct Scales {
   }
 };
 
+// 32 bytes of a row between global memory and a thread's registers; WIDE: 32-byte aligned (16 otherwise).
+template <bool WIDE>
+__device__ __forceinline__ void store32(char* dst, const uint32_t (&v)[8]) {
+  if (WIDE) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(dst), "r"(v[0]), "r"(v[1]), "r"(v[2]),
+                 "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
+                 : "memory");
+  } else {
+    reinterpret_cast<uint4*>(dst)[0] = make_uint4(v[0], v[1], v[2], v[3]);
+    reinterpret_cast<uint4*>(dst)[1] = make_uint4(v[4], v[5], v[6], v[7]);
+  }
+}
+template <bool WIDE>
+__device__ __forceinline__ void load32(const char* src, uint32_t (&v)[8]) {
+  if (WIDE) {
+    asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7])
+                 : "l"(src)
+                 : "memory");
+  } else {
+    const uint4 a = reinterpret_cast<const uint4*>(src)[0], b = reinterpret_cast<const uint4*>(src)[1];
+    v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+  }
+}
+// A thread's row of 32 columns, rounded to bf16.
+__device__ __forceinline__ void store_row(char* dst, bool wide, const float (&x)[32]) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    uint32_t v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = pack_bf16x2(x[16 * i + 2 * e], x[16 * i + 2 * e + 1]);
+    if (wide) store32<true>(dst + 32 * i, v);
+    else store32<false>(dst + 32 * i, v);
+  }
+}
+
+// gelu_tanh2 (gemm_body.cuh) with one reciprocal for the two: 1 / d0 = d1 / (d0 d1). The
+// exponents stop at 60, where the result is below 2^-60 of x: the special functions of a tile of
+// 192 columns (two a value) take as long as the MMAs of K = 1536.
+__device__ __forceinline__ void gelu_tanh2_1(float& x0, float& x1) {
+  constexpr float c = -2.f * 0.7978845608028654f * 1.4426950408889634f;
+  const uint64_t x = f2_pack(x0, x1);
+  float z0, z1;
+  f2_unpack(f2_mul(x, f2_fma(f2_mul(x, x), f2_pack(0.044715f * c, 0.044715f * c), f2_pack(c, c))), z0, z1);
+  float d0, d1;
+  f2_unpack(f2_add(f2_pack(ex2_approx(fminf(z0, 60.f)), ex2_approx(fminf(z1, 60.f))), f2_pack(1.f, 1.f)), d0, d1);
+  const float r = rcp_approx(d0 * d1);
+  f2_unpack(f2_mul(x, f2_mul(f2_pack(d1, d0), f2_pack(r, r))), x0, x1);
+}
+
+// Epilogues without gemm.cu's staging buffer: a thread reads and writes its own row, 32 bytes at a
+// time. The stages' way through shared memory (in by TMA, out to the tensor core: 63 KB for
+// 256 of K, half a microsecond) is what bounds the MMAs, and the buffer's traffic comes on top:
+// at K = 2048 they took 1.4 times as long beside it. A warp's chunks leave TMEM as
+// early as registers allow, so that the accumulator is free for the tile after the next:
+// release() says so.
+//
+// STORE, GELU, RESID: chunk j of the warp is tile columns 32 (half + WAYS j) ...
+template <int EPI, class Ready, class Release>
+__device__ __forceinline__ bool epilogue_linear4(const Params4& p, const Tile& tl, const EpiWarp& w, Ready ready,
+                                                 Release release) {
+  const Seg& sg = p.seg[tl.seg];
+  const int lane = threadIdx.x & 31, n0 = tl.n0 + 32 * w.half;
+  // this warp's, at most two; the last tile of a row may reach past N (a multiple of 32)
+  const int chunks = (min(w.cols, p.N - tl.n0) / 32 + WAYS - 1 - w.half) / WAYS;
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    if (j >= chunks) break;
+    w.vec0[32 * j + lane] = sg.bias ? sg.bias[n0 + 32 * WAYS * j + lane] : 0.f;
+    if (EPI == RA_EPI_RESID) w.vec1[32 * j + lane] = sg.gate[int64_t(tl.s) * sg.gate_ss + n0 + 32 * WAYS * j + lane];
+  }
+  const bool wide = p.wide[tl.seg], on = lane < w.nrow;
+  uint32_t r[2][2][8];
+  if (EPI == RA_EPI_RESID && on) {
+    const char* res =
+        reinterpret_cast<const char*>(sg.resid + int64_t(tl.s) * sg.res_ss + int64_t(w.row0 + lane) * sg.res_sr + n0);
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      if (j >= chunks) break;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        if (wide) load32<true>(res + 64 * WAYS * j + 32 * i, r[j][i]);
+        else load32<false>(res + 64 * WAYS * j + 32 * i, r[j][i]);
+      }
+    }
+  }
+  char* out = reinterpret_cast<char*>(sg.out + int64_t(tl.s) * sg.out_ss + int64_t(w.row0 + lane) * sg.out_sr + n0);
+  __syncwarp();
+  if (!ready()) return false;
+  // RESID: a chunk at a time, both would not fit the registers (spilled ones go through an L1 that
+  // shared memory has left nothing of)
+  constexpr int AHEAD = EPI == RA_EPI_RESID ? 1 : 2;
+  uint32_t v[AHEAD][32];
+  auto fetch = [&](int j) {
+    if (w.nrow > 0 && j < chunks) tmem_ld32(w.acc + 32 * (w.half + WAYS * j), v[j % AHEAD]);
+  };
+#pragma unroll
+  for (int j = 0; j < AHEAD; ++j) fetch(j);
+#pragma unroll
+  for (int j = 0; j < AHEAD; ++j) tmem_ld_wait_for(v[j]);
+  if (AHEAD == 2 || chunks < 2) release();
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    if (j >= chunks) break;
+    float x[32];
+    if (AHEAD == 1 && j == 1) {
+      tmem_ld_wait_for(v[0]);
+      release();
+    }
+    add_cols<true>(v[j % AHEAD], sg.alpha, w.vec0 + 32 * j, x);
+    if (AHEAD == 1 && j == 0) fetch(1);
+    if (EPI == RA_EPI_GELU) {
+#pragma unroll
+      for (int i = 0; i < 32; i += 2) gelu_tanh2_1(x[i], x[i + 1]);
+    } else if (EPI == RA_EPI_RESID) {
+      const float4* g4 = reinterpret_cast<const float4*>(w.vec1 + 32 * j);
+#pragma unroll
+      for (int q = 0; q < 8; ++q) {
+        const float4 g = g4[q];
+        const uint32_t lo = r[j][q / 4][2 * (q & 3)], hi = r[j][q / 4][2 * (q & 3) + 1];
+        x[4 * q] = fmaf(g.x, x[4 * q], __uint_as_float(lo << 16));
+        x[4 * q + 1] = fmaf(g.y, x[4 * q + 1], __uint_as_float(lo & 0xFFFF0000u));
+        x[4 * q + 2] = fmaf(g.z, x[4 * q + 2], __uint_as_float(hi << 16));
+        x[4 * q + 3] = fmaf(g.w, x[4 * q + 3], __uint_as_float(hi & 0xFFFF0000u));
+      }
+    }
+    if (on) store_row(out + 64 * WAYS * j, wide, x);
+  }
+  return true;
+}
+
+// True where `ok` is in every thread of the quarter's WAYS warps, which all get here.
+__device__ __forceinline__ bool quarter_all(int quarter, bool ok) {
+  uint32_t all;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\t"
+      "barrier.cta.red.and.pred q, %2, %3, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+      : "=r"(all)
+      : "r"(uint32_t(ok)), "r"(quarter + 1), "n"(32 * WAYS)
+      : "memory");
+  return all != 0;
+}
+
+// QKV: chunk j of the warp is tile columns 32 (half + WAYS j) ...; the warps of a quarter share
+// every head. Each sums its chunks' squares, the sums meet in shared memory, and the
+// chunks are normalised, turned and stored. (A head to a warp leaves two
+// thirds of them idle: heads of 128 fill a tile of 128 columns.)
+template <int D, class Ready, class Release>
+__device__ __forceinline__ bool epilogue_qkv4(const Params4& p, const Tile& tl, const EpiWarp& w, float* sums,
+                                              Ready ready, Release release) {
+  constexpr int CH = D / 32;
+  const Seg& sg = p.seg[tl.seg];
+  const int lane = threadIdx.x & 31, quarter = (threadIdx.x >> 5) & 3;
+  const int part = tl.n0 / p.C;                  // 0 q, 1 k, 2 v
+  const int c0 = tl.n0 - part * p.C + 32 * w.half;  // the first chunk's column within the part
+  const int chunks = (p.bn / 32 + WAYS - 1 - w.half) / WAYS;  // at most two
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    if (j >= chunks) break;
+    const int c = c0 + 32 * WAYS * j + lane;
+    w.vec0[32 * j + lane] = sg.bias ? sg.bias[part * p.C + c] : 0.f;
+    if (part < 2) w.vec1[32 * j + lane] = sg.norm_w[part][c % D];
+  }
+  __syncwarp();
+  const bool wide = p.wide[tl.seg], on = lane < w.nrow;
+  // RoPE rows of the warp's positions: (cos, sin) of D / 2 pairs, 64 bytes for half a chunk, eight
+  // rows an access (a row to a thread, 32 bytes each, took twice the whole tile's time)
+  const char* rope = reinterpret_cast<const char*>(p.rope + int64_t(sg.pos_offset + w.row0) * (D / 4));
+  uint4 cs[2][4];
+  auto turns = [&](int j) {
+#pragma unroll
+    for (int hf = 0; hf < 2; ++hf)
+      rows_fetch(rope + 64 * (2 * ((c0 / 32 + WAYS * j) % CH) + hf), 4 * D, w.nrow, cs[hf]);
+  };
+  if (part < 2 && chunks > 0) turns(0);
+  bool ok = ready();
+  uint32_t v[32];
+  if (part < 2 && ok && w.nrow > 0) {
+    // a first pass over the accumulators for the squares
+#pragma unroll 1
+    for (int j = 0; j < chunks; ++j) {
+      float x[32], s0 = 0.f, s1 = 0.f;
+      tmem_ld32(w.acc + 32 * (w.half + WAYS * j), v);
+      tmem_ld_wait_for(v);
+      add_cols<true>(v, sg.alpha, w.vec0 + 32 * j, x);
+#pragma unroll
+      for (int i = 0; i < 32; i += 2) {
+        s0 = fmaf(x[i], x[i], s0);
+        s1 = fmaf(x[i + 1], x[i + 1], s1);
+      }
+      sums[(w.half + WAYS * j) * 32 + lane] = s0 + s1;
+    }
+  }
+  // All three go on or none does: one that waits here for one that gave up would wait for ever.
+  if (!quarter_all(quarter, ok)) return false;
+  if (chunks <= 0 || w.nrow <= 0) {
+    release();
+    return part == 2 || quarter_all(quarter, true);
+  }
+  char* dst0 = reinterpret_cast<char*>(sg.dst[part] + tl.s * sg.dst_sb[part] + int64_t(w.row0 + lane) * sg.dst_sn[part]);
+#pragma unroll 1
+  for (int j = 0; j < chunks; ++j) {
+    float x[32];
+    tmem_ld32(w.acc + 32 * (w.half + WAYS * j), v);
+    tmem_ld_wait_for(v);
+    if (j + 1 == chunks) release();
+    add_cols<true>(v, sg.alpha, w.vec0 + 32 * j, x);
+    if (part < 2) {
+      float s = 0.f;
+      const int first = (w.half + WAYS * j) / CH * CH;  // chunk of the tile that the head starts with
+#pragma unroll
+      for (int c = 0; c < CH; ++c) s += sums[(first + c) * 32 + lane];
+      const float rstd = rsqrtf(s / float(D) + p.norm_eps);
+#pragma unroll
+      for (int hf = 0; hf < 2; ++hf) {
+        uint4 own[4];
+        rows_turn(w.stage, cs[hf], own);
+        const float4* w4 = reinterpret_cast<const float4*>(w.vec1 + 32 * j + 16 * hf);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const float4 wv = w4[q];
+          const float c0 = __uint_as_float(own[q].x), s0 = __uint_as_float(own[q].y);
+          const float c1 = __uint_as_float(own[q].z), s1 = __uint_as_float(own[q].w);
+          float* xe = &x[16 * hf + 4 * q];
+          const float a0 = xe[0] * rstd * wv.x, a1 = xe[1] * rstd * wv.y;
+          const float b0 = xe[2] * rstd * wv.z, b1 = xe[3] * rstd * wv.w;
+          xe[0] = a0 * c0 - a1 * s0;
+          xe[1] = a0 * s0 + a1 * c0;
+          xe[2] = b0 * c1 - b1 * s1;
+          xe[3] = b0 * s1 + b1 * c1;
+        }
+      }
+      if (j == 0 && chunks > 1) turns(1);
+    }
+    const int col = c0 + 32 * WAYS * j;
+    if (on) store_row(dst0 + 2 * (int64_t(col / D) * sg.dst_sh[part] + col % D), wide, x);
+  }
+  // the next tile's sums go where these were read
+  if (part < 2) return quarter_all(quarter, true);
+  return true;
+}
+
+template <int EPI, int D, class Ready, class Release>
+__device__ __forceinline__ bool epilogue4(const Params4& p, const Tile& tl, const EpiWarp& w, float* sums, Ready ready,
+                                          Release release) {
+  if constexpr (EPI == RA_EPI_QKV)
+    return epilogue_qkv4<D>(p, tl, w, sums, ready, release);
+  else
+    return epilogue_linear4<EPI>(p, tl, w, ready, release);
+}
+
 // One CTA a tile of 128 rows. SPLIT: a cluster takes a tile, each rank a contiguous part
 // of its K (merge_parts adds them up), then its share of the columns in the epilogue.
-template <int EPI, int D, bool SPLIT>
-__global__ void __launch_bounds__(THREADS, 1) gemm4_kernel(const __grid_constant__ Params4 p) {
+template <int EPI, int D, bool E8M0, bool SPLIT>
+__global__ void __launch_bounds__(THREADS4, 1) gemm4_kernel(const __grid_constant__ Params4 p) {
   using L = Layout<false>;
   constexpr int STAGES = L::STAGES;
   extern __shared__ uint8_t smem_raw[];
@@ -337,7 +622,7 @@ __global__ void __launch_bounds__(THREADS, 1) gemm4_kernel(const __grid_constant
     }
     for (int b = 0; b < 2; ++b) {
       mbar_init(tfull + b, 1);
-      mbar_init(tempty + b, EPI_WARPS);
+      mbar_init(tempty + b, EPI4_WARPS);
     }
     mbar_init(drain, 1);
     mbar_init(parts_full, 1);
@@ -399,8 +684,8 @@ __global__ void __launch_bounds__(THREADS, 1) gemm4_kernel(const __grid_constant
   } else if (warp == 1) {
     {
       // -------------------------------------------------------------- MMA issuer (a converged warp)
-      const uint32_t idesc = idesc_mx4(BM, bn, p.e8m0);
-      const uint32_t s0 = smem_u32(smem), sf0 = tmem + uint32_t(2 * bn);
+      const uint32_t idesc = idesc_mx4(BM, bn, E8M0);
+      const uint32_t s0 = smem_u32(smem) >> 4, sf0 = tmem + uint32_t(2 * bn);
       int i = 0;
       Ring<STAGES> in;  // stages as they are filled
       uint32_t filled = 0;
@@ -412,21 +697,21 @@ __global__ void __launch_bounds__(THREADS, 1) gemm4_kernel(const __grid_constant
         const int buf = i & 1, use = i >> 1;
         if (use > 0 && !(ok = warp_wait(tempty + buf, uint32_t((use - 1) & 1), ctl))) break;
         tc_fence_after();
+        const uint32_t sw0 = sf0 + (E8M0 ? 8u : 16u) + (uint32_t(tl.n0 & 64) >> 5);
         for (int kb = kb0; kb < kb1; ++kb) {
           if (!(ok = warp_wait(filled, full + in.st, in.ph, ctl) && sf.free(empty, ctl))) break;
           tc_fence_after();
           Ring<STAGES> next = in;
           next.next();
           filled = peek(full + next.st, next.ph);
-          issue_stage<false>(p, s0 + in.st * L::STAGE_BYTES, sf0 + sf.col, tmem + uint32_t(buf * bn), idesc,
-                             uint32_t(tl.n0 & 64) >> 5, ksteps_of(p, kb), kb == kb0);
-          commit_stage<false>(empty + in.st);
+          issue_stage<false, E8M0>(p, s0 + uint32_t(in.st * (L::STAGE_BYTES / 16)), sf0 + sf.col, sw0 + sf.col,
+                                tmem + uint32_t(buf * bn), idesc, ksteps_of(p, kb), kb == kb0, smem_u32(empty + in.st));
           issued = true;
           in = next;
           sf.next(p);
         }
         if (!ok) break;
-        commit_stage<false>(tfull + buf);
+        commit_one<false>(tfull + buf);
         ++i;
       }
     }
@@ -435,9 +720,10 @@ __global__ void __launch_bounds__(THREADS, 1) gemm4_kernel(const __grid_constant
     const int quarter = warp & 3;
     EpiWarp w;
     w.half = (warp - 2) >> 2;
-    w.stage = smem + L::OFF_EPI + (warp - 2) * EPI_WARP_BYTES;
+    w.stage = smem + L::OFF_EPI + (warp - 2) * WARP_BYTES;
     w.vec0 = reinterpret_cast<float*>(w.stage + EPI_STAGE_BYTES);
-    w.vec1 = w.vec0 + 128;
+    w.vec1 = w.vec0 + 64;
+    float* sums = reinterpret_cast<float*>(smem + L::OFF_SUMS) + quarter * (MAX_BN / 32) * 32;
     int i = 0;
     Tiles<BM, EPI> tiles;
     Tile tl;
@@ -453,16 +739,17 @@ __global__ void __launch_bounds__(THREADS, 1) gemm4_kernel(const __grid_constant
         w.acc += uint32_t(rank * w.cols);
         tl.n0 += rank * w.cols;
       }
-      if (!epilogue_tile<EPI, D, true>(p, tl, w, [&] {
+      if (!epilogue4<EPI, D>(p, tl, w, sums, [&] {
             bool ok = __all_sync(0xffffffffu, mbar_wait(tfull + buf, uint32_t(use & 1), ctl));
             tc_fence_after();
-            if (SPLIT) ok = merge_parts(ctl, smem, parts_full, acc, ok, bn, w.half, quarter, rank, cs);
+            if (SPLIT) ok = merge_parts<WAYS>(ctl, smem, parts_full, acc, ok, bn, w.half, quarter, rank, cs);
             return ok;
+          }, [&] {
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(tempty + buf);
           }))
         break;
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(tempty + buf);
       ++i;
     }
   }
@@ -483,7 +770,7 @@ __global__ void __launch_bounds__(THREADS, 1) gemm4_kernel(const __grid_constant
         if (n_s > 0) mbar_wait_drain(full + st, uint32_t((n_s - 1) & 1), p.budget_ns);
       }
     if (warp == 1 && issued) {
-      commit_stage<false>(drain);
+      commit_one<false>(drain);
       mbar_wait_drain(drain, 0, p.budget_ns);
     }
   }
@@ -497,8 +784,8 @@ __global__ void __launch_bounds__(THREADS, 1) gemm4_kernel(const __grid_constant
 // CTA pairs on tiles of 256 rows (as gemm_pair_kernel): each CTA stages its own 128 rows of
 // A with their scales, half of the tile's weight rows, and the scales of all of them, which
 // each tensor core wants in its own TMEM; rank 0 issues the copies and MMAs of both.
-template <int EPI, int D>
-__global__ void __launch_bounds__(THREADS, 1) gemm4_pair_kernel(const __grid_constant__ Params4 p) {
+template <int EPI, int D, bool E8M0>
+__global__ void __launch_bounds__(THREADS4, 1) gemm4_pair_kernel(const __grid_constant__ Params4 p) {
   using L = Layout<true>;
   constexpr int STAGES = L::STAGES;
   extern __shared__ uint8_t smem_raw[];
@@ -521,7 +808,7 @@ __global__ void __launch_bounds__(THREADS, 1) gemm4_pair_kernel(const __grid_con
     }
     for (int b = 0; b < 2; ++b) {
       mbar_init(tfull + b, 1);
-      mbar_init(tempty + b, 2 * EPI_WARPS);
+      mbar_init(tempty + b, 2 * EPI4_WARPS);
     }
     mbar_init(drain, 1);
     *abort_flag = 0;
@@ -575,8 +862,8 @@ __global__ void __launch_bounds__(THREADS, 1) gemm4_pair_kernel(const __grid_con
   } else if (warp == 1) {
     if (rank == 0) {
       // -------------------------------------------------------------- MMA issuer (rank 0, a converged warp)
-      const uint32_t idesc = idesc_mx4(P_TM, p.bn, p.e8m0);
-      const uint32_t s0 = smem_u32(smem), sf0 = tmem + uint32_t(2 * p.bn);
+      const uint32_t idesc = idesc_mx4(P_TM, p.bn, E8M0);
+      const uint32_t s0 = smem_u32(smem) >> 4, sf0 = tmem + uint32_t(2 * p.bn);
       int i = 0;
       Ring<STAGES> in;  // stages as they are filled
       uint32_t filled = 0;
@@ -588,21 +875,21 @@ __global__ void __launch_bounds__(THREADS, 1) gemm4_pair_kernel(const __grid_con
         const int buf = i & 1, use = i >> 1;
         if (use > 0 && !(ok = warp_wait<true>(tempty + buf, uint32_t((use - 1) & 1), ctl))) break;
         tc_fence_after();
+        const uint32_t sw0 = sf0 + (E8M0 ? 8u : 16u) + (uint32_t(tl.n0 & 64) >> 5);
         for (int kb = 0; kb < p.kblocks; ++kb) {
           if (!(ok = warp_wait(filled, full + in.st, in.ph, ctl) && sf.free(empty, ctl))) break;
           tc_fence_after();
           Ring<STAGES> next = in;
           next.next();
           filled = peek(full + next.st, next.ph);
-          issue_stage<true>(p, s0 + in.st * L::STAGE_BYTES, sf0 + sf.col, tmem + uint32_t(buf * p.bn), idesc,
-                            uint32_t(tl.n0 & 64) >> 5, ksteps_of(p, kb), kb == 0);
-          commit_stage<true>(empty + in.st);
+          issue_stage<true, E8M0>(p, s0 + uint32_t(in.st * (L::STAGE_BYTES / 16)), sf0 + sf.col, sw0 + sf.col,
+                                tmem + uint32_t(buf * p.bn), idesc, ksteps_of(p, kb), kb == 0, smem_u32(empty + in.st));
           issued = true;
           in = next;
           sf.next(p);
         }
         if (!ok) break;
-        commit_stage<true>(tfull + buf);
+        commit_one<true>(tfull + buf);
         ++i;
       }
     }
@@ -611,9 +898,10 @@ __global__ void __launch_bounds__(THREADS, 1) gemm4_pair_kernel(const __grid_con
     const int quarter = warp & 3;
     EpiWarp w;
     w.half = (warp - 2) >> 2;
-    w.stage = smem + L::OFF_EPI + (warp - 2) * EPI_WARP_BYTES;
+    w.stage = smem + L::OFF_EPI + (warp - 2) * WARP_BYTES;
     w.vec0 = reinterpret_cast<float*>(w.stage + EPI_STAGE_BYTES);
-    w.vec1 = w.vec0 + 128;
+    w.vec1 = w.vec0 + 64;
+    float* sums = reinterpret_cast<float*>(smem + L::OFF_SUMS) + quarter * (MAX_BN / 32) * 32;
     const uint32_t tempty0 = mapa_shared(smem_u32(tempty), 0);
     int i = 0;
     Tiles<P_TM, EPI> tiles;
@@ -624,20 +912,21 @@ __global__ void __launch_bounds__(THREADS, 1) gemm4_pair_kernel(const __grid_con
       w.cols = p.bn;
       w.nrow = min(32, p.rows[tl.seg] - w.row0);
       w.acc = tmem + (uint32_t(quarter * 32) << 16) + uint32_t(buf * p.bn);
-      if (!epilogue_tile<EPI, D, true>(p, tl, w, [&] {
+      if (!epilogue4<EPI, D>(p, tl, w, sums, [&] {
             const bool ok = __all_sync(0xffffffffu, mbar_wait(tfull + buf, uint32_t(use & 1), ctl));
             tc_fence_after();
             return ok;
+          }, [&] {
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) {
+              if (rank == 0)
+                mbar_arrive(tempty + buf);
+              else
+                mbar_arrive_remote_relaxed(tempty0 + 8u * buf);
+            }
           }))
         break;
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) {
-        if (rank == 0)
-          mbar_arrive(tempty + buf);
-        else
-          mbar_arrive_remote(tempty0 + 8u * buf);
-      }
       ++i;
     }
   }
@@ -656,7 +945,7 @@ __global__ void __launch_bounds__(THREADS, 1) gemm4_pair_kernel(const __grid_con
     }
     if (warp == 1 && issued) {
       // the peer's barrier of this name is not waited for and has its own CTA's life
-      commit_stage<true>(drain);
+      commit_one<true>(drain);
       mbar_wait_drain(drain, 0, p.budget_ns);
     }
     pause_ns(kLandNs);  // rank 1's loads, and the commits' arrivals at rank 1
@@ -671,19 +960,20 @@ using Kernel = void (*)(Params4);
 struct Kernels {
   Kernel single, pair, split;  // split: STORE, GELU and RESID
 };
-template <int EPI, int D>
+template <int EPI, int D, bool E8M0>
 Kernels kernels() {
   if constexpr (EPI == RA_EPI_QKV)
-    return {gemm4_kernel<EPI, D, false>, gemm4_pair_kernel<EPI, D>, nullptr};
+    return {gemm4_kernel<EPI, D, E8M0, false>, gemm4_pair_kernel<EPI, D, E8M0>, nullptr};
   else
-    return {gemm4_kernel<EPI, D, false>, gemm4_pair_kernel<EPI, D>, gemm4_kernel<EPI, D, true>};
+    return {gemm4_kernel<EPI, D, E8M0, false>, gemm4_pair_kernel<EPI, D, E8M0>, gemm4_kernel<EPI, D, E8M0, true>};
 }
+template <bool E8M0>
 Kernels pick(int epi, int d) {
   switch (epi) {
-    case RA_EPI_STORE: return kernels<RA_EPI_STORE, 0>();
-    case RA_EPI_GELU: return kernels<RA_EPI_GELU, 0>();
-    case RA_EPI_RESID: return kernels<RA_EPI_RESID, 0>();
-    default: return d == 128 ? kernels<RA_EPI_QKV, 128>() : kernels<RA_EPI_QKV, 64>();
+    case RA_EPI_STORE: return kernels<RA_EPI_STORE, 0, E8M0>();
+    case RA_EPI_GELU: return kernels<RA_EPI_GELU, 0, E8M0>();
+    case RA_EPI_RESID: return kernels<RA_EPI_RESID, 0, E8M0>();
+    default: return d == 128 ? kernels<RA_EPI_QKV, 128, E8M0>() : kernels<RA_EPI_QKV, 64, E8M0>();
   }
 }
 
@@ -708,7 +998,7 @@ int max_clusters(Kernel fn, int cs) {
              cudaLaunchConfig_t cfg;
              std::memset(&cfg, 0, sizeof(cfg));
              cfg.gridDim = dim3(c, 1, 1);
-             cfg.blockDim = dim3(THREADS, 1, 1);
+             cfg.blockDim = dim3(THREADS4, 1, 1);
              cfg.dynamicSmemBytes = smem;
              cfg.attrs = attr;
              cfg.numAttrs = 1;
@@ -862,6 +1152,17 @@ ra_status run(const char* who, const ra_gemm4_args& a, cudaStream_t st) {
       return RA_EINVAL;
     }
     if (!fill_epilogue(who, a, g, s, p.seg[g])) return RA_EINVAL;
+    auto on32 = [](const void* ptr, int64_t ss, int64_t sr, int64_t sh = 0) {  // strides in elements of 2 bytes
+      return (reinterpret_cast<uintptr_t>(ptr) & 31u) == 0 && ss % 16 == 0 && sr % 16 == 0 && sh % 16 == 0;
+    };
+    if (a.epilogue == RA_EPI_QKV) {
+      p.wide[g] = 1;
+      for (const ra_seg* o : {&s.q_out, &s.k_out, &s.v_out})
+        p.wide[g] &= on32(o->ptr, o->stride_b, o->stride_n, o->stride_h);
+    } else {
+      p.wide[g] = on32(s.out, s.out_stride_s, s.out_stride_r) &&
+                  (a.epilogue != RA_EPI_RESID || on32(s.resid, s.resid_stride_s, s.resid_stride_r));
+    }
     const int e = q.a_exponent + q.w_exponent;
     p.seg[g].alpha = ldexpf(1.f, e);
     const int64_t rows = s.rows, spans = (rows + 127) / 128 * ((a.K + 4 * block_of(a.format) - 1) / (4 * block_of(a.format)));
@@ -905,14 +1206,14 @@ ra_status run(const char* who, const ra_gemm4_args& a, cudaStream_t st) {
     return RA_EINVAL;
   }
   if (tiles == 0) return RA_OK;
-  const Kernels kn = pick(a.epilogue, a.d);
+  const Kernels kn = p.e8m0 ? pick<true>(a.epilogue, a.d) : pick<false>(a.epilogue, a.d);
   const int64_t slots = pair ? (sms / 2 > 0 ? sms / 2 : 1) : sms;
   if (pair) note_launch("CTA pairs, %d columns", plan.bn);
   else if (plan.cs > 1) note_launch("clusters of %d, %d columns", plan.cs, plan.bn);
   else note_launch("single CTAs, %d columns", plan.bn);
-  if (pair) return launch(who, p, kn.pair, Layout<true>::SMEM_ALLOC, 2 * (tiles < slots ? tiles : slots), 2, st);
-  if (plan.cs > 1) return launch(who, p, kn.split, Layout<false>::SMEM_ALLOC, tiles * plan.cs, plan.cs, st);
-  return launch(who, p, kn.single, Layout<false>::SMEM_ALLOC, tiles < slots ? tiles : slots, 1, st);
+  if (pair) return launch(who, p, kn.pair, Layout<true>::SMEM_ALLOC, 2 * (tiles < slots ? tiles : slots), 2, st, THREADS4);
+  if (plan.cs > 1) return launch(who, p, kn.split, Layout<false>::SMEM_ALLOC, tiles * plan.cs, plan.cs, st, THREADS4);
+  return launch(who, p, kn.single, Layout<false>::SMEM_ALLOC, tiles < slots ? tiles : slots, 1, st, THREADS4);
 }
 
 }  // namespace gemm4

@@ -160,7 +160,7 @@ __device__ __forceinline__ void gelu_tanh2(float& x0, float& x1) {
 }
 
 // What an epilogue warp works on: its 32 rows (row0 + lane, nrow of them in
-// the segment), its share of the tile's columns (half 0 or 1), its shared
+// the segment), its share of the tile's columns (half: 0 .. WAYS - 1), its shared
 // memory (staging buffer, two vectors of 128 per-column values) and the TMEM
 // address of its lanes in the tile's accumulator; cols: columns of the tile.
 struct EpiWarp {
@@ -186,25 +186,26 @@ __device__ __forceinline__ void add_cols(const uint32_t (&v)[32], float alpha, c
   }
 }
 
-// STORE, GELU, RESID: chunk j of the warp is tile columns 32 (half + 2 j) ...
-template <int EPI, bool SCALED, class Ready>
+// STORE, GELU, RESID: chunk j of the warp is tile columns 32 (half + WAYS j) ...; WAYS warps share
+// a row's columns.
+template <int EPI, bool SCALED, int WAYS, class Ready>
 __device__ __forceinline__ bool epilogue_linear(const Params& p, const Tile& tl, const EpiWarp& w, Ready ready) {
   const Seg& sg = p.seg[tl.seg];
   const int lane = threadIdx.x & 31, n0 = tl.n0 + 32 * w.half;
   // this warp's; the last tile of a row may reach past N (a multiple of 32)
-  const int chunks = (min(w.cols, p.N - tl.n0) / 32 + 1 - w.half) >> 1;
+  const int chunks = (min(w.cols, p.N - tl.n0) / 32 + WAYS - 1 - w.half) / WAYS;
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     if (j >= chunks) break;
-    w.vec0[32 * j + lane] = sg.bias ? sg.bias[n0 + 64 * j + lane] : 0.f;
-    if (EPI == RA_EPI_RESID) w.vec1[32 * j + lane] = sg.gate[int64_t(tl.s) * sg.gate_ss + n0 + 64 * j + lane];
+    w.vec0[32 * j + lane] = sg.bias ? sg.bias[n0 + 32 * WAYS * j + lane] : 0.f;
+    if (EPI == RA_EPI_RESID) w.vec1[32 * j + lane] = sg.gate[int64_t(tl.s) * sg.gate_ss + n0 + 32 * WAYS * j + lane];
   }
   const char* res = nullptr;
   uint4 ra[4], rb[4];  // residuals of the next even and odd chunk
   if (EPI == RA_EPI_RESID && chunks > 0) {
     res = reinterpret_cast<const char*>(sg.resid + int64_t(tl.s) * sg.res_ss + int64_t(w.row0) * sg.res_sr + n0);
     rows_fetch(res, 2 * sg.res_sr, w.nrow, ra);
-    if (chunks > 1) rows_fetch(res + 128, 2 * sg.res_sr, w.nrow, rb);
+    if (chunks > 1) rows_fetch(res + 64 * WAYS, 2 * sg.res_sr, w.nrow, rb);
   }
   char* out = reinterpret_cast<char*>(sg.out + int64_t(tl.s) * sg.out_ss + int64_t(w.row0) * sg.out_sr + n0);
   __syncwarp();
@@ -219,13 +220,13 @@ __device__ __forceinline__ bool epilogue_linear(const Params& p, const Tile& tl,
       // Residuals two chunks ahead (one ahead left about 1000 cycles of global
       // latency in every chunk); the accumulators are not loaded ahead in
       // exchange, the registers allow one of the two without spills.
-      tmem_ld32(w.acc + 32 * w.half + 64 * j, v);
+      tmem_ld32(w.acc + 32 * w.half + 32 * WAYS * j, v);
       rows_turn(w.stage, rc, r);
-      if (j + 2 < chunks) rows_fetch(res + 128 * (j + 2), 2 * sg.res_sr, w.nrow, rc);
+      if (j + 2 < chunks) rows_fetch(res + 64 * WAYS * (j + 2), 2 * sg.res_sr, w.nrow, rc);
     }
     tmem_ld_wait_for(v);
     add_cols<SCALED>(v, sg.alpha, w.vec0 + 32 * j, x);
-    if (EPI != RA_EPI_RESID && j + 1 < chunks) tmem_ld32(w.acc + 32 * w.half + 64 * (j + 1), v);
+    if (EPI != RA_EPI_RESID && j + 1 < chunks) tmem_ld32(w.acc + 32 * w.half + 32 * WAYS * (j + 1), v);
     if (EPI == RA_EPI_GELU) {
 #pragma unroll
       for (int i = 0; i < 32; i += 2) gelu_tanh2(x[i], x[i + 1]);
@@ -243,7 +244,7 @@ __device__ __forceinline__ bool epilogue_linear(const Params& p, const Tile& tl,
         }
       }
     }
-    rows_store(w.stage, x, out + 128 * j, 2 * sg.out_sr, w.nrow);
+    rows_store(w.stage, x, out + 64 * WAYS * j, 2 * sg.out_sr, w.nrow);
   };
 #pragma unroll 1
   for (int j = 0; j < chunks; j += 2) {
@@ -254,7 +255,7 @@ __device__ __forceinline__ bool epilogue_linear(const Params& p, const Tile& tl,
 }
 
 // QKV: heads half, half + 2, ... of the tile.
-template <int D, bool SCALED, class Ready>
+template <int D, class Ready>
 __device__ __forceinline__ bool epilogue_qkv(const Params& p, const Tile& tl, const EpiWarp& w, Ready ready) {
   constexpr int CH = D / 32;
   const int heads = (p.bn / D + 1 - w.half) >> 1;  // this warp's
@@ -292,7 +293,7 @@ __device__ __forceinline__ bool epilogue_qkv(const Params& p, const Tile& tl, co
       for (int c = 0; c < CH; ++c) {
         float x[32];
         tmem_ld_wait_for(v);
-        add_cols<SCALED>(v, sg.alpha, bias + 32 * c, x);
+        add_cols<false>(v, 1.f, bias + 32 * c, x);
         tmem_ld32(acc + 32 * ((c + 1) % CH), v);
 #pragma unroll
         for (int i = 0; i < 32; i += 2) {
@@ -307,7 +308,7 @@ __device__ __forceinline__ bool epilogue_qkv(const Params& p, const Tile& tl, co
     for (int c = 0; c < CH; ++c) {
       float x[32];
       tmem_ld_wait_for(v);
-      add_cols<SCALED>(v, sg.alpha, bias + 32 * c, x);
+      add_cols<false>(v, 1.f, bias + 32 * c, x);
       if (c + 1 < CH) tmem_ld32(acc + 32 * (c + 1), v);
       if (part < 2) {
 #pragma unroll
@@ -341,12 +342,12 @@ __device__ __forceinline__ bool epilogue_qkv(const Params& p, const Tile& tl, co
 
 // Epilogue of one warp's share of an output tile; ready() waits for the
 // accumulator (false: the wait was given up). D: head dim (QKV).
-template <int EPI, int D, bool SCALED = false, class Ready>
+template <int EPI, int D, class Ready>
 __device__ __forceinline__ bool epilogue_tile(const Params& p, const Tile& tl, const EpiWarp& w, Ready ready) {
   if constexpr (EPI == RA_EPI_QKV)
-    return epilogue_qkv<D, SCALED>(p, tl, w, ready);
+    return epilogue_qkv<D>(p, tl, w, ready);
   else
-    return epilogue_linear<EPI, SCALED>(p, tl, w, ready);
+    return epilogue_linear<EPI, false, 2>(p, tl, w, ready);
 }
 
 // A split tile: each CTA of the cluster has the sums over its part of K in its
@@ -360,6 +361,7 @@ __device__ __forceinline__ bool epilogue_tile(const Params& p, const Tile& tl, c
 // rank sends and waits for what it receives, also after a wait of this CTA was
 // given up: no CTA exits with a copy into it, or out of it, in flight.
 // The merge of a 128 x 256 tile between two CTAs (64 KB each way) takes 2.6 us.
+template <int WAYS = 2>
 __device__ __forceinline__ bool merge_parts(const WaitCtl& ctl, uint8_t* smem, uint64_t* parts_full, uint32_t acc,
                                             bool ok, int bn, int half, int quarter, int rank, int cs) {
   const int lane = threadIdx.x & 31, row = quarter * 32 + lane;
@@ -370,7 +372,7 @@ __device__ __forceinline__ bool merge_parts(const WaitCtl& ctl, uint8_t* smem, u
   const bool leader = quarter == 0 && half == 0 && lane == 0;
   if (leader) mbar_arrive_expect_tx(parts_full, (cs - 1) * part_bytes);
 #pragma unroll 1
-  for (int c0 = 32 * half; c0 < bn; c0 += 64) {
+  for (int c0 = 32 * half; c0 < bn; c0 += 32 * WAYS) {
     const int q = c0 / cw;
     if (q == rank) continue;
     uint32_t v[32];
@@ -397,7 +399,7 @@ __device__ __forceinline__ bool merge_parts(const WaitCtl& ctl, uint8_t* smem, u
                                                mbar_wait_drain(parts_full, 0, ctl.budget_ns));
   if (!got || !ok) return false;
 #pragma unroll 1
-  for (int c0 = 32 * half; c0 < cw; c0 += 64) {
+  for (int c0 = 32 * half; c0 < cw; c0 += 32 * WAYS) {
     uint32_t v[32];
     float x[32];
     tmem_ld32(acc + rank * cw + c0, v);
@@ -431,7 +433,8 @@ inline bool aligned16(const void* ptr) { return (reinterpret_cast<uintptr_t>(ptr
 
 // Launches `ctas` CTAs in clusters of cs.
 template <class P>
-ra_status launch(const char* who, const P& p, void (*fn)(P), int smem, int64_t ctas, int cs, cudaStream_t st) {
+ra_status launch(const char* who, const P& p, void (*fn)(P), int smem, int64_t ctas, int cs, cudaStream_t st,
+                 int threads = THREADS) {
   const ra_status as = ensure_dynamic_smem(reinterpret_cast<const void*>(fn), smem, who);
   if (as != RA_OK) return as;
   cudaLaunchAttribute attr[2];
@@ -443,7 +446,7 @@ ra_status launch(const char* who, const P& p, void (*fn)(P), int smem, int64_t c
   cudaLaunchConfig_t cfg;
   std::memset(&cfg, 0, sizeof(cfg));
   cfg.gridDim = dim3(unsigned(ctas), 1, 1);
-  cfg.blockDim = dim3(THREADS, 1, 1);
+  cfg.blockDim = dim3(threads, 1, 1);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
   cfg.attrs = attr;
