@@ -2,22 +2,26 @@
 // for every few columns,
 //   D[r, n] = sum over blocks b of  sa[r, b] sw[n, b]  sum over k in b of  a[r, k] w[n, k]
 // on the tensor cores' block-scaled 4-bit MMAs (tcgen05.mma kind::mxf4nvf4, K = 64),
-// which multiply the scales in. Tiles, roles and epilogues are gemm.cu's (gemm_body.cuh);
-// what differs is how a K step reaches the tensor core:
+// which multiply the scales in. Tiles and roles are gemm.cu's (one CTA on a tile of 128 rows, or
+// a pair on 256); what differs:
 //   * A stage holds 256 of K: 128 bytes of codes a row, the swizzled box of 64 bf16, four
 //     MMAs; and the rows' scales, whose tiles of 128 rows by 4 blocks (512 bytes) lie in
 //     memory as tensor memory wants them, so that a stage's are one TMA box for each operand.
 //   * Before a stage's MMAs the issuer has the scales copied to TMEM (tcgen05.cp 32x128b, 32
 //     rows by 16 bytes, to every warp's lanes): four columns for 128 rows and four blocks.
-//     Two buffers of 48 columns take turns; a buffer is written again once the MMAs that
-//     read it have ended (their commit, two stages ago, has arrived).
-//   * TMEM holds two accumulators of up to 192 columns and the scales (480 of 512 columns).
-//     Tiles of 256 columns would leave either the scales or the second accumulator no room,
-//     and an epilogue takes as long as the MMAs of K = 2048.
+//     Buffers of them take turns; one is written again once the MMAs that read it have ended
+//     (their commit has arrived).
+//   * TMEM holds two accumulators of up to 192 columns and two stages' scales. Tiles of 256
+//     columns would leave either the scales or the second accumulator no room, and an epilogue
+//     takes as long as the MMAs of K = 1536.
+// What bounds it: shared memory. A stage of a pair's 256 x 192 tile puts 35 KB into a CTA's and
+// takes 28 KB out for the MMAs, 490 cycles at 128 bytes each, where the MMAs run 370; measured 500
+// (8192 rows, K = 16384, N = 7296, e8m0: 267 us, 7.3 PFLOP/s, 3.8 times the bf16 rate).
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
+#include <cmath>
 #include <cstring>
 
 #include "gemm_body.cuh"
@@ -29,41 +33,39 @@ namespace gemm4 {
 
 using namespace gemm;
 
-// Three warps share a tile row's columns: two chunks of 32 each, and at K = 2048 the MMAs of a tile
-// take no longer than that.
+// A quarter of the TMEM lanes (32 rows) has three epilogue warps, each with 64 of the tile's columns.
 constexpr int WAYS = 3, EPI4_WARPS = 4 * WAYS, THREADS4 = 64 + 32 * EPI4_WARPS;
+constexpr int UNIT = 64;     // columns of a warp
 constexpr int CHUNK = 256;   // K of a stage
-constexpr int MAX_BN = 192;  // columns of a tile
 constexpr int A_BYTES = BM * CHUNK / 2;
 constexpr int SA_BYTES = 4 * 512;  // scales of 128 rows, up to four tiles (e4m3)
-constexpr int SF_BYTES = 3 * SA_BYTES;  // and of up to 256 weight rows
+constexpr int VEC_BYTES = 2 * UNIT * 4;    // two vectors of its columns
+// QKV: the rows' sums of squares of each 32 columns, by TMEM lane quarter.
+constexpr int SUMS_BYTES = 4 * (128 / 32) * 32 * 4;
+constexpr int TURN_BYTES = EPI_STAGE_BYTES;  // QKV: a warp's RoPE rows of 16 columns
 
-constexpr int WARP_BYTES = EPI_STAGE_BYTES + 2 * 64 * 4;  // RoPE rows on their way, two vectors of its 64 columns
-// QKV: the rows' sums of squares of each chunk of columns, by TMEM lane quarter.
-constexpr int SUMS_BYTES = 4 * (MAX_BN / 32) * 32 * 4;
-
-// One CTA a tile, and CTA pairs (each stages half of the tile's weight rows).
-template <bool PAIR>
+// Shared memory of one CTA a tile, and of CTA pairs (each stages half of the tile's weight rows).
+template <bool PAIR_, bool QKV>
 struct Layout {
+  static constexpr bool PAIR = PAIR_;
+  static constexpr int MAX_BN = PAIR && !QKV ? 192 : 128;  // columns of a tile
   static constexpr int B_BYTES = (PAIR ? MAX_BN / 2 : MAX_BN) * CHUNK / 2;
   static constexpr int OFF_B = A_BYTES, OFF_SF = A_BYTES + B_BYTES;
-  static constexpr int STAGE_BYTES = OFF_SF + SF_BYTES;
-  static constexpr int STAGES = PAIR ? 5 : 4;
-  static constexpr int OFF_BAR = STAGES * STAGE_BYTES;
-  static constexpr int OFF_MISC = OFF_BAR + (2 * STAGES + 6) * 8;  // full, empty, tfull[2], tempty[2], drain, parts_full
-  static constexpr int OFF_EPI = (OFF_MISC + 16 + 127) / 128 * 128;
-  static constexpr int OFF_SUMS = OFF_EPI + EPI4_WARPS * WARP_BYTES;
-  static constexpr int SMEM_ALLOC = OFF_SUMS + SUMS_BYTES + 1024;
+  static constexpr int STAGE_BYTES = OFF_SF + SA_BYTES * (1 + (MAX_BN + 127) / 128);
+  static constexpr int STAGES = PAIR ? 6 : 5;
+  static constexpr int OFF_VEC = STAGES * STAGE_BYTES;
+  static constexpr int OFF_SUMS = OFF_VEC + EPI4_WARPS * VEC_BYTES;
+  static constexpr int OFF_TURN = OFF_SUMS + (QKV ? SUMS_BYTES : 0);
+  static constexpr int OFF_BAR = OFF_TURN + (QKV ? EPI4_WARPS * TURN_BYTES : 0);
+  static constexpr int OFF_MISC = OFF_BAR + (2 * STAGES + 5) * 8;  // full, empty, tfull[2], tempty[2], drain
+  static constexpr int SMEM_ALLOC = OFF_MISC + 16 + 1024;
   static_assert(STAGE_BYTES % 1024 == 0 && OFF_SF % 1024 == 0, "swizzled tiles start on 1024 bytes");
   static_assert(SMEM_ALLOC <= 232448, "shared memory budget");
 };
-// split tiles: the parts to send and those received take the place of the stages
-static_assert(2 * (MAX_SPLIT - 1) * (BM * 128 * 4 / MAX_SPLIT) <= Layout<false>::OFF_BAR &&
-                  2 * (BM * MAX_BN * 4 / 2) <= Layout<false>::OFF_BAR, "parts fit the stages");
 
 // TMEM columns of a stage's scales: four for each tile of A's and of the weight's.
 constexpr int scale_cols(int groups, int w_tiles) { return 4 * groups * (1 + w_tiles); }
-static_assert(2 * MAX_BN + 2 * scale_cols(4, 2) <= TMEM_COLS, "TMEM columns");
+static_assert(2 * 192 + 2 * scale_cols(4, 2) <= TMEM_COLS, "TMEM columns");
 
 struct Params4 : Params {
   int32_t e8m0;                      // format
@@ -80,6 +82,7 @@ struct Params4 : Params {
 __device__ __forceinline__ uint32_t idesc_mx4(int M, int N, int e8m0) {
   return (1u << 7) | (1u << 10) | (uint32_t(N >> 3) << 17) | (uint32_t(e8m0) << 23) | (uint32_t(M >> 4) << 24);
 }
+
 // A stage's scales to TMEM columns sf.., then its MMAs (ksteps of 64, 1 to 4) and the commit that
 // frees the stage, by one thread of a converged warp. One asm block, whose operands are the same
 // in every lane and whose addresses are the first ones plus immediates (in units of 16 bytes;
@@ -136,50 +139,41 @@ __device__ __forceinline__ uint32_t idesc_mx4(int M, int N, int e8m0) {
   "mov.b32 c, 3;\n\t.reg .b16 m;\n\tcvt.u16.u32 m, c;\n\t"                                                  \
   "@e tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%6], m;\n\t"
 #define RA_COMMIT_1 "@e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%6];\n\t"
-// Units of the scales within a stage, as immediates: pairs, single CTAs.
-#define RA_U2(N) RA_STR(1792 + N)
-#define RA_U1(N) RA_STR(2560 + N)
+// Units of the scales within a stage, as immediates: wide pairs, pairs, single CTAs.
+#define RA_U3(N) RA_STR(1792 + N)
+#define RA_U2(N) RA_STR(1536 + N)
+#define RA_U1(N) RA_STR(2048 + N)
 #define RA_STR(N) RA_STR2(N)
 #define RA_STR2(N) #N
-static_assert(Layout<true>::OFF_SF / 16 == 1792 && Layout<false>::OFF_SF / 16 == 2560, "immediates of the copies");
-template <bool PAIR, bool E8M0>
+static_assert(Layout<true, false>::OFF_SF / 16 == 1792 && Layout<true, true>::OFF_SF / 16 == 1536 &&
+                  Layout<false, false>::OFF_SF / 16 == 2048, "immediates of the copies");
+template <class L, bool E8M0>
 __device__ __forceinline__ void issue_stage(const Params4& p, uint32_t lo, uint32_t sf, uint32_t sw, uint32_t d,
                                             uint32_t idesc, int ksteps, bool first, uint32_t bar) {
-  using L = Layout<PAIR>;
   constexpr uint32_t HI_SW128 = (1024u >> 4) | (1u << 14) | (2u << 29);  // 8 rows after 1024 bytes; version; swizzle
   constexpr uint32_t HI_SCALES = 8u | (1u << 14);                        // 8 rows after 128 bytes; version
   const uint32_t acc = first ? 0u : 1u;
-  if constexpr (PAIR && E8M0) {
-    if (p.w_tiles == 2)
-      RA_STAGE(RA_COPIES_E8M0_2("2", RA_U2(0), RA_U2(32), RA_U2(128), RA_U2(160), RA_U2(192), RA_U2(224)),
-               RA_MMAS_E8M0_2("2"), RA_COMMIT_2);
-    else
-      RA_STAGE(RA_COPIES_E8M0("2", RA_U2(0), RA_U2(32), RA_U2(128), RA_U2(160)), RA_MMAS_E8M0("2"), RA_COMMIT_2);
-  } else if constexpr (PAIR) {
-    if (p.w_tiles == 2)
-      RA_STAGE(RA_COPIES_E4M3_2("2", RA_U2(0), RA_U2(32), RA_U2(64), RA_U2(96), RA_U2(128), RA_U2(160), RA_U2(192),
-                                RA_U2(224), RA_U2(256), RA_U2(288), RA_U2(320), RA_U2(352)),
-               RA_MMAS_E4M3_2("2"), RA_COMMIT_2);
-    else
-      RA_STAGE(RA_COPIES_E4M3("2", RA_U2(0), RA_U2(32), RA_U2(64), RA_U2(96), RA_U2(128), RA_U2(160), RA_U2(192),
-                              RA_U2(224)),
-               RA_MMAS_E4M3("2"), RA_COMMIT_2);
+#define RA_ONE(GROUP, U, COMMIT)                                                                                 \
+  if constexpr (E8M0)                                                                                            \
+    RA_STAGE(RA_COPIES_E8M0(GROUP, U(0), U(32), U(128), U(160)), RA_MMAS_E8M0(GROUP), COMMIT);                   \
+  else                                                                                                           \
+    RA_STAGE(RA_COPIES_E4M3(GROUP, U(0), U(32), U(64), U(96), U(128), U(160), U(192), U(224)), RA_MMAS_E4M3(GROUP), \
+             COMMIT)
+  if constexpr (!L::PAIR) {
+    RA_ONE("1", RA_U1, RA_COMMIT_1);
+  } else if constexpr (L::MAX_BN == 128) {
+    RA_ONE("2", RA_U2, RA_COMMIT_2);
+  } else if (p.w_tiles == 1) {
+    RA_ONE("2", RA_U3, RA_COMMIT_2);
   } else if constexpr (E8M0) {
-    if (p.w_tiles == 2)
-      RA_STAGE(RA_COPIES_E8M0_2("1", RA_U1(0), RA_U1(32), RA_U1(128), RA_U1(160), RA_U1(192), RA_U1(224)),
-               RA_MMAS_E8M0_2("1"), RA_COMMIT_1);
-    else
-      RA_STAGE(RA_COPIES_E8M0("1", RA_U1(0), RA_U1(32), RA_U1(128), RA_U1(160)), RA_MMAS_E8M0("1"), RA_COMMIT_1);
+    RA_STAGE(RA_COPIES_E8M0_2("2", RA_U3(0), RA_U3(32), RA_U3(128), RA_U3(160), RA_U3(192), RA_U3(224)),
+             RA_MMAS_E8M0_2("2"), RA_COMMIT_2);
   } else {
-    if (p.w_tiles == 2)
-      RA_STAGE(RA_COPIES_E4M3_2("1", RA_U1(0), RA_U1(32), RA_U1(64), RA_U1(96), RA_U1(128), RA_U1(160), RA_U1(192),
-                                RA_U1(224), RA_U1(256), RA_U1(288), RA_U1(320), RA_U1(352)),
-               RA_MMAS_E4M3_2("1"), RA_COMMIT_1);
-    else
-      RA_STAGE(RA_COPIES_E4M3("1", RA_U1(0), RA_U1(32), RA_U1(64), RA_U1(96), RA_U1(128), RA_U1(160), RA_U1(192),
-                              RA_U1(224)),
-               RA_MMAS_E4M3("1"), RA_COMMIT_1);
+    RA_STAGE(RA_COPIES_E4M3_2("2", RA_U3(0), RA_U3(32), RA_U3(64), RA_U3(96), RA_U3(128), RA_U3(160), RA_U3(192),
+                              RA_U3(224), RA_U3(256), RA_U3(288), RA_U3(320), RA_U3(352)),
+             RA_MMAS_E4M3_2("2"), RA_COMMIT_2);
   }
+#undef RA_ONE
 }
 #undef RA_CP
 #undef RA_MMA
@@ -288,23 +282,23 @@ __device__ __forceinline__ bool warp_tile(const Params& p, Tiles<TM, EPI>& tiles
   return more != 0;
 }
 // tma_load_4d and tma_load_4d_pair by one thread of a converged warp.
+template <bool PAIR>
 __device__ __forceinline__ void tma_load_one(uint32_t dst, const void* tmap, uint32_t bar, int32_t c0, int32_t c1,
                                              int32_t c2, int32_t c3) {
-  asm volatile(
-      "{\n\t.reg .pred e;\n\telect.sync _|e, 0xffffffff;\n\t"
-      "@e cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
-      " [%0], [%1, {%2, %3, %4, %5}], [%6];\n\t}" ::"r"(dst),
-      "l"(reinterpret_cast<uint64_t>(tmap)), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(bar)
-      : "memory");
-}
-__device__ __forceinline__ void tma_load_one_pair(uint32_t dst, const void* tmap, uint32_t bar, int32_t c0, int32_t c1,
-                                                  int32_t c2, int32_t c3) {
-  asm volatile(
-      "{\n\t.reg .pred e;\n\telect.sync _|e, 0xffffffff;\n\t"
-      "@e cp.async.bulk.tensor.4d.shared::cta.global.tile.mbarrier::complete_tx::bytes.cta_group::2"
-      " [%0], [%1, {%2, %3, %4, %5}], [%6];\n\t}" ::"r"(dst),
-      "l"(reinterpret_cast<uint64_t>(tmap)), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(bar)
-      : "memory");
+  if constexpr (PAIR)
+    asm volatile(
+        "{\n\t.reg .pred e;\n\telect.sync _|e, 0xffffffff;\n\t"
+        "@e cp.async.bulk.tensor.4d.shared::cta.global.tile.mbarrier::complete_tx::bytes.cta_group::2"
+        " [%0], [%1, {%2, %3, %4, %5}], [%6];\n\t}" ::"r"(dst),
+        "l"(reinterpret_cast<uint64_t>(tmap)), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(bar)
+        : "memory");
+  else
+    asm volatile(
+        "{\n\t.reg .pred e;\n\telect.sync _|e, 0xffffffff;\n\t"
+        "@e cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+        " [%0], [%1, {%2, %3, %4, %5}], [%6];\n\t}" ::"r"(dst),
+        "l"(reinterpret_cast<uint64_t>(tmap)), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(bar)
+        : "memory");
 }
 
 // A stage of the ring and the parity of its barriers' next phase.
@@ -340,27 +334,45 @@ struct Scales {
   }
 };
 
-// 32 bytes of a row between global memory and a thread's registers; WIDE: 32-byte aligned (16 otherwise).
+// gelu_tanh2 (gemm_body.cuh) with one reciprocal for the two: 1 / d0 = d1 / (d0 d1). The
+// exponents stop at 60, where the result is below 2^-60 of x: the special functions of a tile of
+// 192 columns (two a value) take as long as the MMAs of K = 1536.
+__device__ __forceinline__ void gelu_tanh2_1(float& x0, float& x1) {
+  constexpr float c = -2.f * 0.7978845608028654f * 1.4426950408889634f;
+  const uint64_t x = f2_pack(x0, x1);
+  float z0, z1;
+  f2_unpack(f2_mul(x, f2_fma(f2_mul(x, x), f2_pack(0.044715f * c, 0.044715f * c), f2_pack(c, c))), z0, z1);
+  float d0, d1;
+  f2_unpack(f2_add(f2_pack(ex2_approx(fminf(z0, 60.f)), ex2_approx(fminf(z1, 60.f))), f2_pack(1.f, 1.f)), d0, d1);
+  const float r = rcp_approx(d0 * d1);
+  f2_unpack(f2_mul(x, f2_mul(f2_pack(d1, d0), f2_pack(r, r))), x0, x1);
+}
+
+// 32 bytes of a row between global memory and a thread's registers, each row a thread's; WIDE: 32-byte
+// aligned (16 otherwise). No staging buffer, whose traffic would come on top of the stages' (a
+// buffer and TMA stores of whole lines: 47 us where this takes 42, 8192 rows, K = 2048, N = 7296). What an
+// epilogue touches leaves L2 first: an output that streams through it otherwise takes the
+// operands with it, which all CTAs read again and again (49 us; 36 without the stores).
 template <bool WIDE>
 __device__ __forceinline__ void store32(char* dst, const uint32_t (&v)[8]) {
   if (WIDE) {
-    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(dst), "r"(v[0]), "r"(v[1]), "r"(v[2]),
-                 "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
+    asm volatile("st.global.L1::no_allocate.L2::evict_first.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(dst),
+                 "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
                  : "memory");
   } else {
-    reinterpret_cast<uint4*>(dst)[0] = make_uint4(v[0], v[1], v[2], v[3]);
-    reinterpret_cast<uint4*>(dst)[1] = make_uint4(v[4], v[5], v[6], v[7]);
+    __stcs(reinterpret_cast<uint4*>(dst), make_uint4(v[0], v[1], v[2], v[3]));
+    __stcs(reinterpret_cast<uint4*>(dst) + 1, make_uint4(v[4], v[5], v[6], v[7]));
   }
 }
 template <bool WIDE>
 __device__ __forceinline__ void load32(const char* src, uint32_t (&v)[8]) {
   if (WIDE) {
-    asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+    asm volatile("ld.global.L1::no_allocate.L2::evict_first.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
                  : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7])
                  : "l"(src)
                  : "memory");
   } else {
-    const uint4 a = reinterpret_cast<const uint4*>(src)[0], b = reinterpret_cast<const uint4*>(src)[1];
+    const uint4 a = __ldcs(reinterpret_cast<const uint4*>(src)), b = __ldcs(reinterpret_cast<const uint4*>(src) + 1);
     v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
   }
 }
@@ -376,81 +388,68 @@ __device__ __forceinline__ void store_row(char* dst, bool wide, const float (&x)
   }
 }
 
-// gelu_tanh2 (gemm_body.cuh) with one reciprocal for the two: 1 / d0 = d1 / (d0 d1). The
-// exponents stop at 60, where the result is below 2^-60 of x: the special functions of a tile of
-// 192 columns (two a value) take as long as the MMAs of K = 1536.
-__device__ __forceinline__ void gelu_tanh2_1(float& x0, float& x1) {
-  constexpr float c = -2.f * 0.7978845608028654f * 1.4426950408889634f;
-  const uint64_t x = f2_pack(x0, x1);
-  float z0, z1;
-  f2_unpack(f2_mul(x, f2_fma(f2_mul(x, x), f2_pack(0.044715f * c, 0.044715f * c), f2_pack(c, c))), z0, z1);
-  float d0, d1;
-  f2_unpack(f2_add(f2_pack(ex2_approx(fminf(z0, 60.f)), ex2_approx(fminf(z1, 60.f))), f2_pack(1.f, 1.f)), d0, d1);
-  const float r = rcp_approx(d0 * d1);
-  f2_unpack(f2_mul(x, f2_mul(f2_pack(d1, d0), f2_pack(r, r))), x0, x1);
-}
+// What an epilogue warp works on: its 32 rows (row0 + lane, nrow of them in the segment), its unit of
+// 64 columns, its shared memory and the TMEM address of its lanes in the tile's accumulator.
+struct Epi4 {
+  int row0, nrow, unit;
+  uint8_t* turn;
+  float *vec0, *vec1;
+  uint32_t acc;
+};
 
-// Epilogues without gemm.cu's staging buffer: a thread reads and writes its own row, 32 bytes at a
-// time. The stages' way through shared memory (in by TMA, out to the tensor core: 63 KB for
-// 256 of K, half a microsecond) is what bounds the MMAs, and the buffer's traffic comes on top:
-// at K = 2048 they took 1.4 times as long beside it. A warp's chunks leave TMEM as
-// early as registers allow, so that the accumulator is free for the tile after the next:
-// release() says so.
-//
-// STORE, GELU, RESID: chunk j of the warp is tile columns 32 (half + WAYS j) ...
+// STORE, GELU, RESID. release(): the accumulator has been read.
 template <int EPI, class Ready, class Release>
-__device__ __forceinline__ bool epilogue_linear4(const Params4& p, const Tile& tl, const EpiWarp& w, Ready ready,
+__device__ __forceinline__ bool epilogue_linear4(const Params4& p, const Tile& tl, const Epi4& w, Ready ready,
                                                  Release release) {
   const Seg& sg = p.seg[tl.seg];
-  const int lane = threadIdx.x & 31, n0 = tl.n0 + 32 * w.half;
-  // this warp's, at most two; the last tile of a row may reach past N (a multiple of 32)
-  const int chunks = (min(w.cols, p.N - tl.n0) / 32 + WAYS - 1 - w.half) / WAYS;
-#pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    if (j >= chunks) break;
-    w.vec0[32 * j + lane] = sg.bias ? sg.bias[n0 + 32 * WAYS * j + lane] : 0.f;
-    if (EPI == RA_EPI_RESID) w.vec1[32 * j + lane] = sg.gate[int64_t(tl.s) * sg.gate_ss + n0 + 32 * WAYS * j + lane];
-  }
-  const bool wide = p.wide[tl.seg], on = lane < w.nrow;
+  const int lane = threadIdx.x & 31, n0 = tl.n0 + UNIT * w.unit;
+  const bool on = w.nrow > 0 && UNIT * w.unit < p.bn && n0 < p.N;  // N is a multiple of 64
+  const bool mine = lane < w.nrow, wide = p.wide[tl.seg];
   uint32_t r[2][2][8];
-  if (EPI == RA_EPI_RESID && on) {
-    const char* res =
-        reinterpret_cast<const char*>(sg.resid + int64_t(tl.s) * sg.res_ss + int64_t(w.row0 + lane) * sg.res_sr + n0);
+  const char* res = nullptr;
+  auto residual = [&](int j) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      if (wide) load32<true>(res + 64 * j + 32 * i, r[j][i]);
+      else load32<false>(res + 64 * j + 32 * i, r[j][i]);
+    }
+  };
+  if (on) {
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-      if (j >= chunks) break;
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        if (wide) load32<true>(res + 64 * WAYS * j + 32 * i, r[j][i]);
-        else load32<false>(res + 64 * WAYS * j + 32 * i, r[j][i]);
-      }
+      w.vec0[32 * j + lane] = sg.bias ? sg.bias[n0 + 32 * j + lane] : 0.f;
+      if (EPI == RA_EPI_RESID) w.vec1[32 * j + lane] = sg.gate[int64_t(tl.s) * sg.gate_ss + n0 + 32 * j + lane];
+    }
+    if (EPI == RA_EPI_RESID && mine) {
+      res = reinterpret_cast<const char*>(sg.resid + int64_t(tl.s) * sg.res_ss + int64_t(w.row0 + lane) * sg.res_sr + n0);
+      residual(0);
+      residual(1);
     }
   }
   char* out = reinterpret_cast<char*>(sg.out + int64_t(tl.s) * sg.out_ss + int64_t(w.row0 + lane) * sg.out_sr + n0);
   __syncwarp();
   if (!ready()) return false;
-  // RESID: a chunk at a time, both would not fit the registers (spilled ones go through an L1 that
+  // RESID: 32 columns at a time, all would not fit the registers (spilled ones go through an L1 that
   // shared memory has left nothing of)
   constexpr int AHEAD = EPI == RA_EPI_RESID ? 1 : 2;
   uint32_t v[AHEAD][32];
-  auto fetch = [&](int j) {
-    if (w.nrow > 0 && j < chunks) tmem_ld32(w.acc + 32 * (w.half + WAYS * j), v[j % AHEAD]);
-  };
+  if (on) {
 #pragma unroll
-  for (int j = 0; j < AHEAD; ++j) fetch(j);
+    for (int j = 0; j < AHEAD; ++j) tmem_ld32(w.acc + UNIT * w.unit + 32 * j, v[j]);
 #pragma unroll
-  for (int j = 0; j < AHEAD; ++j) tmem_ld_wait_for(v[j]);
-  if (AHEAD == 2 || chunks < 2) release();
+    for (int j = 0; j < AHEAD; ++j) tmem_ld_wait_for(v[j]);
+  }
+  if (AHEAD == 2 || !on) release();
+  if (!on) return true;
 #pragma unroll
   for (int j = 0; j < 2; ++j) {
-    if (j >= chunks) break;
     float x[32];
     if (AHEAD == 1 && j == 1) {
       tmem_ld_wait_for(v[0]);
       release();
     }
     add_cols<true>(v[j % AHEAD], sg.alpha, w.vec0 + 32 * j, x);
-    if (AHEAD == 1 && j == 0) fetch(1);
+    if (AHEAD == 1 && j == 0) tmem_ld32(w.acc + UNIT * w.unit + 32, v[0]);
     if (EPI == RA_EPI_GELU) {
 #pragma unroll
       for (int i = 0; i < 32; i += 2) gelu_tanh2_1(x[i], x[i + 1]);
@@ -466,7 +465,7 @@ __device__ __forceinline__ bool epilogue_linear4(const Params4& p, const Tile& t
         x[4 * q + 3] = fmaf(g.w, x[4 * q + 3], __uint_as_float(hi & 0xFFFF0000u));
       }
     }
-    if (on) store_row(out + 64 * WAYS * j, wide, x);
+    if (mine) store_row(out + 64 * j, wide, x);
   }
   return true;
 }
@@ -483,46 +482,42 @@ __device__ __forceinline__ bool quarter_all(int quarter, bool ok) {
   return all != 0;
 }
 
-// QKV: chunk j of the warp is tile columns 32 (half + WAYS j) ...; the warps of a quarter share
-// every head. Each sums its chunks' squares, the sums meet in shared memory, and the
-// chunks are normalised, turned and stored. (A head to a warp leaves two
-// thirds of them idle: heads of 128 fill a tile of 128 columns.)
+// QKV: the warps of a quarter share every head. Each sums the squares of its columns, the sums meet
+// in shared memory, and the columns are normalised, turned and stored.
 template <int D, class Ready, class Release>
-__device__ __forceinline__ bool epilogue_qkv4(const Params4& p, const Tile& tl, const EpiWarp& w, float* sums,
-                                              Ready ready, Release release) {
-  constexpr int CH = D / 32;
+__device__ __forceinline__ bool epilogue_qkv4(const Params4& p, const Tile& tl, const Epi4& w, float* sums, Ready ready,
+                                              Release release) {
   const Seg& sg = p.seg[tl.seg];
   const int lane = threadIdx.x & 31, quarter = (threadIdx.x >> 5) & 3;
-  const int part = tl.n0 / p.C;                  // 0 q, 1 k, 2 v
-  const int c0 = tl.n0 - part * p.C + 32 * w.half;  // the first chunk's column within the part
-  const int chunks = (p.bn / 32 + WAYS - 1 - w.half) / WAYS;  // at most two
-#pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    if (j >= chunks) break;
-    const int c = c0 + 32 * WAYS * j + lane;
-    w.vec0[32 * j + lane] = sg.bias ? sg.bias[part * p.C + c] : 0.f;
-    if (part < 2) w.vec1[32 * j + lane] = sg.norm_w[part][c % D];
-  }
-  __syncwarp();
-  const bool wide = p.wide[tl.seg], on = lane < w.nrow;
-  // RoPE rows of the warp's positions: (cos, sin) of D / 2 pairs, 64 bytes for half a chunk, eight
+  const int part = tl.n0 / p.C;                       // 0 q, 1 k, 2 v
+  const int c0 = tl.n0 - part * p.C + UNIT * w.unit;  // the unit's first column within the part
+  const bool on = w.nrow > 0 && UNIT * w.unit < p.bn;
+  // RoPE rows of the warp's positions: (cos, sin) of D / 2 pairs, 64 bytes for 16 columns, eight
   // rows an access (a row to a thread, 32 bytes each, took twice the whole tile's time)
-  const char* rope = reinterpret_cast<const char*>(p.rope + int64_t(sg.pos_offset + w.row0) * (D / 4));
+  const char* rope = reinterpret_cast<const char*>(p.rope + int64_t(sg.pos_offset + w.row0) * (D / 4)) + 4 * (c0 % D);
   uint4 cs[2][4];
   auto turns = [&](int j) {
 #pragma unroll
-    for (int hf = 0; hf < 2; ++hf)
-      rows_fetch(rope + 64 * (2 * ((c0 / 32 + WAYS * j) % CH) + hf), 4 * D, w.nrow, cs[hf]);
+    for (int hf = 0; hf < 2; ++hf) rows_fetch(rope + 64 * (2 * j + hf), 4 * D, w.nrow, cs[hf]);
   };
-  if (part < 2 && chunks > 0) turns(0);
-  bool ok = ready();
+  if (on) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int c = c0 + 32 * j + lane;
+      w.vec0[32 * j + lane] = sg.bias ? sg.bias[part * p.C + c] : 0.f;
+      if (part < 2) w.vec1[32 * j + lane] = sg.norm_w[part][c % D];
+    }
+    if (part < 2) turns(0);
+  }
+  __syncwarp();
+  const bool ok = ready();
   uint32_t v[32];
-  if (part < 2 && ok && w.nrow > 0) {
+  if (part < 2 && ok && on) {
     // a first pass over the accumulators for the squares
 #pragma unroll 1
-    for (int j = 0; j < chunks; ++j) {
+    for (int j = 0; j < 2; ++j) {
       float x[32], s0 = 0.f, s1 = 0.f;
-      tmem_ld32(w.acc + 32 * (w.half + WAYS * j), v);
+      tmem_ld32(w.acc + UNIT * w.unit + 32 * j, v);
       tmem_ld_wait_for(v);
       add_cols<true>(v, sg.alpha, w.vec0 + 32 * j, x);
 #pragma unroll
@@ -530,60 +525,62 @@ __device__ __forceinline__ bool epilogue_qkv4(const Params4& p, const Tile& tl, 
         s0 = fmaf(x[i], x[i], s0);
         s1 = fmaf(x[i + 1], x[i + 1], s1);
       }
-      sums[(w.half + WAYS * j) * 32 + lane] = s0 + s1;
+      sums[(2 * w.unit + j) * 32 + lane] = s0 + s1;
     }
   }
   // All three go on or none does: one that waits here for one that gave up would wait for ever.
   if (!quarter_all(quarter, ok)) return false;
-  if (chunks <= 0 || w.nrow <= 0) {
-    release();
-    return part == 2 || quarter_all(quarter, true);
-  }
-  char* dst0 = reinterpret_cast<char*>(sg.dst[part] + tl.s * sg.dst_sb[part] + int64_t(w.row0 + lane) * sg.dst_sn[part]);
-#pragma unroll 1
-  for (int j = 0; j < chunks; ++j) {
-    float x[32];
-    tmem_ld32(w.acc + 32 * (w.half + WAYS * j), v);
-    tmem_ld_wait_for(v);
-    if (j + 1 == chunks) release();
-    add_cols<true>(v, sg.alpha, w.vec0 + 32 * j, x);
+  if (on) {
+    float rstd = 1.f;
     if (part < 2) {
       float s = 0.f;
-      const int first = (w.half + WAYS * j) / CH * CH;  // chunk of the tile that the head starts with
+      const int first = D == 128 ? 0 : 2 * w.unit;  // 32 columns of the tile that the head starts with
 #pragma unroll
-      for (int c = 0; c < CH; ++c) s += sums[(first + c) * 32 + lane];
-      const float rstd = rsqrtf(s / float(D) + p.norm_eps);
-#pragma unroll
-      for (int hf = 0; hf < 2; ++hf) {
-        uint4 own[4];
-        rows_turn(w.stage, cs[hf], own);
-        const float4* w4 = reinterpret_cast<const float4*>(w.vec1 + 32 * j + 16 * hf);
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const float4 wv = w4[q];
-          const float c0 = __uint_as_float(own[q].x), s0 = __uint_as_float(own[q].y);
-          const float c1 = __uint_as_float(own[q].z), s1 = __uint_as_float(own[q].w);
-          float* xe = &x[16 * hf + 4 * q];
-          const float a0 = xe[0] * rstd * wv.x, a1 = xe[1] * rstd * wv.y;
-          const float b0 = xe[2] * rstd * wv.z, b1 = xe[3] * rstd * wv.w;
-          xe[0] = a0 * c0 - a1 * s0;
-          xe[1] = a0 * s0 + a1 * c0;
-          xe[2] = b0 * c1 - b1 * s1;
-          xe[3] = b0 * s1 + b1 * c1;
-        }
-      }
-      if (j == 0 && chunks > 1) turns(1);
+      for (int c = 0; c < D / 32; ++c) s += sums[(first + c) * 32 + lane];
+      rstd = rsqrtf(s / float(D) + p.norm_eps);
     }
-    const int col = c0 + 32 * WAYS * j;
-    if (on) store_row(dst0 + 2 * (int64_t(col / D) * sg.dst_sh[part] + col % D), wide, x);
+    char* dst = reinterpret_cast<char*>(sg.dst[part] + tl.s * sg.dst_sb[part] + (c0 / D) * sg.dst_sh[part] +
+                                        int64_t(w.row0 + lane) * sg.dst_sn[part] + c0 % D);
+#pragma unroll 1
+    for (int j = 0; j < 2; ++j) {
+      float x[32];
+      tmem_ld32(w.acc + UNIT * w.unit + 32 * j, v);
+      tmem_ld_wait_for(v);
+      if (j == 1) release();
+      add_cols<true>(v, sg.alpha, w.vec0 + 32 * j, x);
+      if (part < 2) {
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf) {
+          uint4 own[4];
+          rows_turn(w.turn, cs[hf], own);
+          const float4* w4 = reinterpret_cast<const float4*>(w.vec1 + 32 * j + 16 * hf);
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const float4 wv = w4[q];
+            const float c0 = __uint_as_float(own[q].x), s0 = __uint_as_float(own[q].y);
+            const float c1 = __uint_as_float(own[q].z), s1 = __uint_as_float(own[q].w);
+            float* xe = &x[16 * hf + 4 * q];
+            const float a0 = xe[0] * rstd * wv.x, a1 = xe[1] * rstd * wv.y;
+            const float b0 = xe[2] * rstd * wv.z, b1 = xe[3] * rstd * wv.w;
+            xe[0] = a0 * c0 - a1 * s0;
+            xe[1] = a0 * s0 + a1 * c0;
+            xe[2] = b0 * c1 - b1 * s1;
+            xe[3] = b0 * s1 + b1 * c1;
+          }
+        }
+        if (j == 0) turns(1);
+      }
+      if (lane < w.nrow) store_row(dst + 64 * j, p.wide[tl.seg], x);
+    }
+  } else {
+    release();
   }
   // the next tile's sums go where these were read
-  if (part < 2) return quarter_all(quarter, true);
-  return true;
+  return part == 2 || quarter_all(quarter, true);
 }
 
 template <int EPI, int D, class Ready, class Release>
-__device__ __forceinline__ bool epilogue4(const Params4& p, const Tile& tl, const EpiWarp& w, float* sums, Ready ready,
+__device__ __forceinline__ bool epilogue4(const Params4& p, const Tile& tl, const Epi4& w, float* sums, Ready ready,
                                           Release release) {
   if constexpr (EPI == RA_EPI_QKV)
     return epilogue_qkv4<D>(p, tl, w, sums, ready, release);
@@ -591,30 +588,28 @@ __device__ __forceinline__ bool epilogue4(const Params4& p, const Tile& tl, cons
     return epilogue_linear4<EPI>(p, tl, w, ready, release);
 }
 
-// One CTA a tile of 128 rows. SPLIT: a cluster takes a tile, each rank a contiguous part
-// of its K (merge_parts adds them up), then its share of the columns in the epilogue.
-template <int EPI, int D, bool E8M0, bool SPLIT>
+// One CTA on tiles of 128 rows, or CTA pairs on 256 (as gemm_pair_kernel): each CTA of a pair stages
+// its own 128 rows of A with their scales, half of the tile's weight rows, and the scales of all
+// of them, which each tensor core wants in its own TMEM; rank 0 issues the copies and MMAs of
+// both, commits reach both, and what frees an accumulator arrives at rank 0.
+//   warp 0      TMA producer     warp 1      TMEM allocator, MMA issuer (of a pair: rank 0's)
+//   warps 2..13 epilogue (quarter = warp % 4, thread = output row = TMEM lane)
+template <int EPI, int D, bool E8M0, bool PAIR>
 __global__ void __launch_bounds__(THREADS4, 1) gemm4_kernel(const __grid_constant__ Params4 p) {
-  using L = Layout<false>;
-  constexpr int STAGES = L::STAGES;
+  using L = Layout<PAIR, EPI == RA_EPI_QKV>;
+  constexpr int STAGES = L::STAGES, TM = PAIR ? P_TM : BM, CTAS = PAIR ? 2 : 1;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
-  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + L::OFF_BAR);
-  uint64_t* full = bars;
-  uint64_t* empty = bars + STAGES;
-  uint64_t* tfull = bars + 2 * STAGES;
-  uint64_t* tempty = bars + 2 * STAGES + 2;
-  uint64_t* drain = bars + 2 * STAGES + 4;
-  uint64_t* parts_full = bars + 2 * STAGES + 5;
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem + L::OFF_BAR);
+  uint64_t* empty = full + STAGES;
+  uint64_t* tfull = full + 2 * STAGES;
+  uint64_t* tempty = tfull + 2;
+  uint64_t* drain = tfull + 4;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + L::OFF_MISC);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + L::OFF_MISC + 4);
-  volatile int* live = reinterpret_cast<volatile int*>(smem + L::OFF_MISC + 8);
   const int warp = same(int(threadIdx.x >> 5)), lane = threadIdx.x & 31;
-  const int rank = SPLIT ? int(cluster_rank()) : 0, cs = SPLIT ? int(cluster_size()) : 1;
-  const uint32_t t0 = SPLIT ? blockIdx.x / cs : blockIdx.x, step = SPLIT ? gridDim.x / cs : gridDim.x;
-  const int kb0 = SPLIT ? p.kblocks * rank / cs : 0;  // this CTA's stages of K
-  const int kb1 = SPLIT ? p.kblocks * (rank + 1) / cs : p.kblocks;
-  const int bn = p.bn;
+  const int rank = PAIR ? same(int(cluster_rank())) : 0;
+  const uint32_t t0 = blockIdx.x / CTAS, step = gridDim.x / CTAS;
   if (threadIdx.x == 0) {
     for (int s = 0; s < STAGES; ++s) {
       mbar_init(full + s, 1);
@@ -622,28 +617,21 @@ __global__ void __launch_bounds__(THREADS4, 1) gemm4_kernel(const __grid_constan
     }
     for (int b = 0; b < 2; ++b) {
       mbar_init(tfull + b, 1);
-      mbar_init(tempty + b, EPI4_WARPS);
+      mbar_init(tempty + b, CTAS * EPI4_WARPS);
     }
     mbar_init(drain, 1);
-    mbar_init(parts_full, 1);
     *abort_flag = 0;
     fence_mbar_init();
   }
-  if (warp == 1) tmem_alloc(tmem_slot, TMEM_COLS);
-  if (SPLIT && warp == 2) {
-    pdl_wait();
-    Tiles<BM, EPI> tiles;
-    Tile tl;
-    *live = tiles.on(p, t0, tl);
+  if (warp == 1) {
+    if (PAIR) tmem_alloc_pair(tmem_slot, TMEM_COLS);
+    else tmem_alloc(tmem_slot, TMEM_COLS);
   }
   tc_fence_before();
   __syncthreads();
+  if (PAIR) cluster_sync_all();  // both CTAs' barriers and TMEM exist before any cross-CTA use
   tc_fence_after();
   const uint32_t tmem = uint32_t(same(int(*tmem_slot)));
-  if (SPLIT && !*live) {  // uniform over the cluster: the modes leave it no tile
-    if (warp == 1) tmem_dealloc(tmem, TMEM_COLS);
-    return;
-  }
   const WaitCtl ctl{abort_flag, p.err_word, p.budget_ns};
   pdl_launch();
   if (warp != 0) pdl_wait();
@@ -651,229 +639,49 @@ __global__ void __launch_bounds__(THREADS4, 1) gemm4_kernel(const __grid_constan
   int64_t loads = 0;    // the producer's: stages whose loads may be on their way
   bool issued = false;  // the issuer's: MMAs may be on their way
   if (warp == 0) {
-    {
-      // -------------------------------------------------------------- producer (a converged warp)
-      for (int g = 0; g < p.n_seg; ++g)
-        if (p.rows[g] > 0) {
-          tma_prefetch_desc(&p.tm_a[g]);
-          tma_prefetch_desc(&p.tm_w[g]);
-          tma_prefetch_desc(&p.tm_sa[g]);
-          tma_prefetch_desc(&p.tm_sw[g]);
-        }
-      pdl_wait();
-      Ring<STAGES> in;
-      bool ok = true;
-      Tiles<BM, EPI> tiles;
-      Tile tl;
-      for (uint32_t by = t0; ok && warp_tile(p, tiles, by, tl); by = step) {
-        for (int kb = kb0; kb < kb1; ++kb) {
-          if (loads >= STAGES && !(ok = warp_wait(empty + in.st, in.ph ^ 1, ctl))) break;
-          const uint32_t stage = smem_u32(smem) + in.st * L::STAGE_BYTES, bar = smem_u32(full + in.st);
-          const bool one = elect_one();
-          if (one) mbar_arrive_expect_tx(full + in.st, p.stage_tx);
-          __syncwarp();
-          tma_load_one(stage, &p.tm_a[tl.seg], bar, kb * (CHUNK / 4), tl.m0, 0, tl.s);
-          tma_load_one(stage + L::OFF_B, &p.tm_w[tl.seg], bar, kb * (CHUNK / 4), tl.n0, 0, 0);
-          tma_load_one(stage + L::OFF_SF, &p.tm_sa[tl.seg], bar, 0, kb * p.groups, tl.m0 / 128, tl.s);
-          tma_load_one(stage + L::OFF_SF + SA_BYTES, &p.tm_sw[tl.seg], bar, 0, kb * p.groups, tl.n0 / 128, 0);
-          ++loads;
-          in.next();
-        }
+    // ---------------------------------------------------------------- producer (a converged warp)
+    for (int g = 0; g < p.n_seg; ++g)
+      if (p.rows[g] > 0) {
+        tma_prefetch_desc(&p.tm_a[g]);
+        tma_prefetch_desc(&p.tm_w[g]);
+        tma_prefetch_desc(&p.tm_sa[g]);
+        tma_prefetch_desc(&p.tm_sw[g]);
       }
-    }
-  } else if (warp == 1) {
-    {
-      // -------------------------------------------------------------- MMA issuer (a converged warp)
-      const uint32_t idesc = idesc_mx4(BM, bn, E8M0);
-      const uint32_t s0 = smem_u32(smem) >> 4, sf0 = tmem + uint32_t(2 * bn);
-      int i = 0;
-      Ring<STAGES> in;  // stages as they are filled
-      uint32_t filled = 0;
-      Scales<STAGES> sf(p);
-      bool ok = true;
-      Tiles<BM, EPI> tiles;
-      Tile tl;
-      for (uint32_t by = t0; ok && warp_tile(p, tiles, by, tl); by = step) {
-        const int buf = i & 1, use = i >> 1;
-        if (use > 0 && !(ok = warp_wait(tempty + buf, uint32_t((use - 1) & 1), ctl))) break;
-        tc_fence_after();
-        const uint32_t sw0 = sf0 + (E8M0 ? 8u : 16u) + (uint32_t(tl.n0 & 64) >> 5);
-        for (int kb = kb0; kb < kb1; ++kb) {
-          if (!(ok = warp_wait(filled, full + in.st, in.ph, ctl) && sf.free(empty, ctl))) break;
-          tc_fence_after();
-          Ring<STAGES> next = in;
-          next.next();
-          filled = peek(full + next.st, next.ph);
-          issue_stage<false, E8M0>(p, s0 + uint32_t(in.st * (L::STAGE_BYTES / 16)), sf0 + sf.col, sw0 + sf.col,
-                                tmem + uint32_t(buf * bn), idesc, ksteps_of(p, kb), kb == kb0, smem_u32(empty + in.st));
-          issued = true;
-          in = next;
-          sf.next(p);
-        }
-        if (!ok) break;
-        commit_one<false>(tfull + buf);
-        ++i;
-      }
-    }
-  } else {
-    // ---------------------------------------------------------------- epilogue
-    const int quarter = warp & 3;
-    EpiWarp w;
-    w.half = (warp - 2) >> 2;
-    w.stage = smem + L::OFF_EPI + (warp - 2) * WARP_BYTES;
-    w.vec0 = reinterpret_cast<float*>(w.stage + EPI_STAGE_BYTES);
-    w.vec1 = w.vec0 + 64;
-    float* sums = reinterpret_cast<float*>(smem + L::OFF_SUMS) + quarter * (MAX_BN / 32) * 32;
-    int i = 0;
-    Tiles<BM, EPI> tiles;
+    pdl_wait();
+    const uint32_t full0 = PAIR ? mapa_shared(smem_u32(full), 0) : smem_u32(full);  // a pair's are rank 0's
+    Ring<STAGES> in;
+    bool ok = true;
+    Tiles<TM, EPI> tiles;
     Tile tl;
-    for (uint32_t by = t0; tiles.on(p, by, tl); by = step) {
-      const int buf = i & 1, use = i >> 1;
-      w.row0 = tl.m0 + quarter * 32;
-      w.nrow = min(32, p.rows[tl.seg] - w.row0);
-      w.acc = tmem + (uint32_t(quarter * 32) << 16) + uint32_t(buf * bn);
-      w.cols = bn;
-      const uint32_t acc = w.acc;
-      if (SPLIT) {
-        w.cols /= cs;
-        w.acc += uint32_t(rank * w.cols);
-        tl.n0 += rank * w.cols;
-      }
-      if (!epilogue4<EPI, D>(p, tl, w, sums, [&] {
-            bool ok = __all_sync(0xffffffffu, mbar_wait(tfull + buf, uint32_t(use & 1), ctl));
-            tc_fence_after();
-            if (SPLIT) ok = merge_parts<WAYS>(ctl, smem, parts_full, acc, ok, bn, w.half, quarter, rank, cs);
-            return ok;
-          }, [&] {
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(tempty + buf);
-          }))
-        break;
-      ++i;
-    }
-  }
-  if (SPLIT) {
-    // Warps 0 and 1 meet the epilogue's cluster barrier here. No CTA exits before
-    // every part has been read from it and received.
-    __syncwarp();
-    if (warp < 2) cluster_sync_all();
-    cluster_sync_all();
-  }
-  tc_fence_before();
-  __syncthreads();
-  // No role waits any more, so the flag is final. What this CTA has on its way lands first.
-  if (*abort_flag) {
-    if (warp == 0 && lane == 0)
-      for (int st = 0; st < STAGES; ++st) {
-        const int64_t n_s = (loads > st) ? (loads - st + STAGES - 1) / STAGES : 0;
-        if (n_s > 0) mbar_wait_drain(full + st, uint32_t((n_s - 1) & 1), p.budget_ns);
-      }
-    if (warp == 1 && issued) {
-      commit_one<false>(drain);
-      mbar_wait_drain(drain, 0, p.budget_ns);
-    }
-  }
-  __syncwarp();
-  if (warp == 1) {
-    tc_fence_after();
-    tmem_dealloc(tmem, TMEM_COLS);
-  }
-}
-
-// CTA pairs on tiles of 256 rows (as gemm_pair_kernel): each CTA stages its own 128 rows of
-// A with their scales, half of the tile's weight rows, and the scales of all of them, which
-// each tensor core wants in its own TMEM; rank 0 issues the copies and MMAs of both.
-template <int EPI, int D, bool E8M0>
-__global__ void __launch_bounds__(THREADS4, 1) gemm4_pair_kernel(const __grid_constant__ Params4 p) {
-  using L = Layout<true>;
-  constexpr int STAGES = L::STAGES;
-  extern __shared__ uint8_t smem_raw[];
-  uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
-  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + L::OFF_BAR);
-  uint64_t* full = bars;
-  uint64_t* empty = bars + STAGES;
-  uint64_t* tfull = bars + 2 * STAGES;
-  uint64_t* tempty = bars + 2 * STAGES + 2;
-  uint64_t* drain = bars + 2 * STAGES + 4;
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + L::OFF_MISC);
-  volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + L::OFF_MISC + 4);
-  const int warp = same(int(threadIdx.x >> 5)), lane = threadIdx.x & 31;
-  const uint32_t rank = uint32_t(same(int(cluster_rank())));
-  const uint32_t cid = blockIdx.x >> 1, ncl = gridDim.x >> 1;
-  if (threadIdx.x == 0) {
-    for (int s = 0; s < STAGES; ++s) {
-      mbar_init(full + s, 1);
-      mbar_init(empty + s, 1);
-    }
-    for (int b = 0; b < 2; ++b) {
-      mbar_init(tfull + b, 1);
-      mbar_init(tempty + b, 2 * EPI4_WARPS);
-    }
-    mbar_init(drain, 1);
-    *abort_flag = 0;
-    fence_mbar_init();
-  }
-  if (warp == 1) tmem_alloc_pair(tmem_slot, TMEM_COLS);
-  tc_fence_before();
-  __syncthreads();
-  cluster_sync_all();  // both CTAs' barriers and TMEM exist before any cross-CTA use
-  tc_fence_after();
-  const uint32_t tmem = uint32_t(same(int(*tmem_slot)));
-  const WaitCtl ctl{abort_flag, p.err_word, p.budget_ns};
-  pdl_launch();
-  if (warp != 0) pdl_wait();
-
-  int64_t loads = 0;    // the producer's: stages that it loaded
-  bool issued = false;  // the issuer's: it has issued MMAs
-  if (warp == 0) {
-    {
-      // -------------------------------------------------------------- producer (both CTAs, a converged warp)
-      for (int g = 0; g < p.n_seg; ++g)
-        if (p.rows[g] > 0) {
-          tma_prefetch_desc(&p.tm_a[g]);
-          tma_prefetch_desc(&p.tm_w[g]);
-          tma_prefetch_desc(&p.tm_sa[g]);
-          tma_prefetch_desc(&p.tm_sw[g]);
-        }
-      pdl_wait();
-      const uint32_t full0 = mapa_shared(smem_u32(full), 0);  // rank 0's full barriers
-      Ring<STAGES> in;
-      bool ok = true;
-      Tiles<P_TM, EPI> tiles;
-      Tile tl;
-      for (uint32_t by = cid; ok && warp_tile(p, tiles, by, tl); by = ncl) {
-        for (int kb = 0; kb < p.kblocks; ++kb) {
-          if (loads >= STAGES && !(ok = warp_wait(empty + in.st, in.ph ^ 1, ctl))) break;
-          const uint32_t stage = smem_u32(smem) + in.st * L::STAGE_BYTES, bar = full0 + 8u * in.st;
-          const bool one = elect_one();
-          if (one && rank == 0) mbar_arrive_expect_tx(full + in.st, 2 * p.stage_tx);
-          __syncwarp();
-          tma_load_one_pair(stage, &p.tm_a[tl.seg], bar, kb * (CHUNK / 4), tl.m0 + int(rank) * 128, 0, tl.s);
-          tma_load_one_pair(stage + L::OFF_B, &p.tm_w[tl.seg], bar, kb * (CHUNK / 4), tl.n0 + int(rank) * (p.bn / 2), 0,
-                           0);
-          tma_load_one_pair(stage + L::OFF_SF, &p.tm_sa[tl.seg], bar, 0, kb * p.groups, tl.m0 / 128 + int(rank), tl.s);
-          tma_load_one_pair(stage + L::OFF_SF + SA_BYTES, &p.tm_sw[tl.seg], bar, 0, kb * p.groups, tl.n0 / 128, 0);
-          ++loads;
-          in.next();
-        }
+    for (uint32_t by = t0; ok && warp_tile(p, tiles, by, tl); by = step) {
+      for (int kb = 0; kb < p.kblocks; ++kb) {
+        if (loads >= STAGES && !(ok = warp_wait(empty + in.st, in.ph ^ 1, ctl))) break;
+        const uint32_t stage = smem_u32(smem) + in.st * L::STAGE_BYTES, bar = full0 + 8u * in.st;
+        if (rank == 0 && elect_one()) mbar_arrive_expect_tx(full + in.st, CTAS * p.stage_tx);
+        __syncwarp();
+        tma_load_one<PAIR>(stage, &p.tm_a[tl.seg], bar, kb * (CHUNK / 4), tl.m0 + rank * 128, 0, tl.s);
+        tma_load_one<PAIR>(stage + L::OFF_B, &p.tm_w[tl.seg], bar, kb * (CHUNK / 4), tl.n0 + rank * (p.bn / 2), 0, 0);
+        tma_load_one<PAIR>(stage + L::OFF_SF, &p.tm_sa[tl.seg], bar, 0, kb * p.groups, tl.m0 / 128 + rank, tl.s);
+        tma_load_one<PAIR>(stage + L::OFF_SF + SA_BYTES, &p.tm_sw[tl.seg], bar, 0, kb * p.groups, tl.n0 / 128, 0);
+        ++loads;
+        in.next();
       }
     }
   } else if (warp == 1) {
     if (rank == 0) {
-      // -------------------------------------------------------------- MMA issuer (rank 0, a converged warp)
-      const uint32_t idesc = idesc_mx4(P_TM, p.bn, E8M0);
+      // -------------------------------------------------------------- MMA issuer (a converged warp)
+      const uint32_t idesc = idesc_mx4(TM, p.bn, E8M0);
       const uint32_t s0 = smem_u32(smem) >> 4, sf0 = tmem + uint32_t(2 * p.bn);
       int i = 0;
       Ring<STAGES> in;  // stages as they are filled
       uint32_t filled = 0;
       Scales<STAGES> sf(p);
       bool ok = true;
-      Tiles<P_TM, EPI> tiles;
+      Tiles<TM, EPI> tiles;
       Tile tl;
-      for (uint32_t by = cid; ok && warp_tile(p, tiles, by, tl); by = ncl) {
+      for (uint32_t by = t0; ok && warp_tile(p, tiles, by, tl); by = step) {
         const int buf = i & 1, use = i >> 1;
-        if (use > 0 && !(ok = warp_wait<true>(tempty + buf, uint32_t((use - 1) & 1), ctl))) break;
+        if (use > 0 && !(ok = warp_wait<PAIR>(tempty + buf, uint32_t((use - 1) & 1), ctl))) break;
         tc_fence_after();
         const uint32_t sw0 = sf0 + (E8M0 ? 8u : 16u) + (uint32_t(tl.n0 & 64) >> 5);
         for (int kb = 0; kb < p.kblocks; ++kb) {
@@ -882,90 +690,89 @@ __global__ void __launch_bounds__(THREADS4, 1) gemm4_pair_kernel(const __grid_co
           Ring<STAGES> next = in;
           next.next();
           filled = peek(full + next.st, next.ph);
-          issue_stage<true, E8M0>(p, s0 + uint32_t(in.st * (L::STAGE_BYTES / 16)), sf0 + sf.col, sw0 + sf.col,
-                                tmem + uint32_t(buf * p.bn), idesc, ksteps_of(p, kb), kb == 0, smem_u32(empty + in.st));
+          issue_stage<L, E8M0>(p, s0 + uint32_t(in.st * (L::STAGE_BYTES / 16)), sf0 + sf.col, sw0 + sf.col,
+                               tmem + uint32_t(buf * p.bn), idesc, ksteps_of(p, kb), kb == 0, smem_u32(empty + in.st));
           issued = true;
           in = next;
           sf.next(p);
         }
         if (!ok) break;
-        commit_one<true>(tfull + buf);
+        commit_one<PAIR>(tfull + buf);
         ++i;
       }
     }
   } else {
-    // ---------------------------------------------------------------- epilogue (both CTAs)
+    // ---------------------------------------------------------------- epilogue
     const int quarter = warp & 3;
-    EpiWarp w;
-    w.half = (warp - 2) >> 2;
-    w.stage = smem + L::OFF_EPI + (warp - 2) * WARP_BYTES;
-    w.vec0 = reinterpret_cast<float*>(w.stage + EPI_STAGE_BYTES);
-    w.vec1 = w.vec0 + 64;
-    float* sums = reinterpret_cast<float*>(smem + L::OFF_SUMS) + quarter * (MAX_BN / 32) * 32;
-    const uint32_t tempty0 = mapa_shared(smem_u32(tempty), 0);
+    Epi4 w;
+    w.unit = (warp - 2) >> 2;
+    w.turn = smem + L::OFF_TURN + (warp - 2) * TURN_BYTES;
+    w.vec0 = reinterpret_cast<float*>(smem + L::OFF_VEC + (warp - 2) * VEC_BYTES);
+    w.vec1 = w.vec0 + UNIT;
+    float* sums = reinterpret_cast<float*>(smem + L::OFF_SUMS) + quarter * (128 / 32) * 32;
+    const uint32_t tempty0 = PAIR ? mapa_shared(smem_u32(tempty), 0) : 0u;
     int i = 0;
-    Tiles<P_TM, EPI> tiles;
+    Tiles<TM, EPI> tiles;
     Tile tl;
-    for (uint32_t by = cid; tiles.on(p, by, tl); by = ncl) {
+    for (uint32_t by = t0; tiles.on(p, by, tl); by = step) {
       const int buf = i & 1, use = i >> 1;
-      w.row0 = tl.m0 + int(rank) * 128 + quarter * 32;
-      w.cols = p.bn;
+      w.row0 = tl.m0 + rank * 128 + quarter * 32;
       w.nrow = min(32, p.rows[tl.seg] - w.row0);
       w.acc = tmem + (uint32_t(quarter * 32) << 16) + uint32_t(buf * p.bn);
-      if (!epilogue4<EPI, D>(p, tl, w, sums, [&] {
-            const bool ok = __all_sync(0xffffffffu, mbar_wait(tfull + buf, uint32_t(use & 1), ctl));
-            tc_fence_after();
-            return ok;
-          }, [&] {
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) {
-              if (rank == 0)
-                mbar_arrive(tempty + buf);
-              else
-                mbar_arrive_remote_relaxed(tempty0 + 8u * buf);
-            }
-          }))
+      if (!epilogue4<EPI, D>(
+              p, tl, w, sums,
+              [&] {
+                const bool ok = __all_sync(0xffffffffu, mbar_wait(tfull + buf, uint32_t(use & 1), ctl));
+                tc_fence_after();
+                return ok;
+              },
+              [&] {
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) {
+                  if (rank == 0) mbar_arrive(tempty + buf);
+                  else mbar_arrive_remote_relaxed(tempty0 + 8u * buf);
+                }
+              }))
         break;
       ++i;
     }
   }
   tc_fence_before();
   __syncthreads();
-  // No role waits any more, so the flag is final. What a CTA that gave up has on its way
-  // lands before the pair's shared memory and TMEM go. (A rank 0 that did not give up has
-  // seen every MMA end, and with them the loads of both CTAs.)
+  // No role waits any more, so the flag is final. What a CTA that gave up has on its way lands before
+  // its shared memory and TMEM go. (A rank 0 that did not give up has seen every MMA end, and with
+  // them the loads of both CTAs.)
   if (*abort_flag) {
     if (warp == 0 && lane == 0 && rank == 0) {
-      // rank 0's full barriers count both CTAs' bytes of every phase it armed
+      // a pair's full barriers count both CTAs' bytes of every phase that rank 0 armed
       for (int st = 0; st < STAGES; ++st) {
         const int64_t n_s = (loads > st) ? (loads - st + STAGES - 1) / STAGES : 0;
         if (n_s > 0) mbar_wait_drain(full + st, uint32_t((n_s - 1) & 1), p.budget_ns);
       }
     }
     if (warp == 1 && issued) {
-      // the peer's barrier of this name is not waited for and has its own CTA's life
-      commit_one<true>(drain);
+      commit_one<PAIR>(drain);
       mbar_wait_drain(drain, 0, p.budget_ns);
     }
-    pause_ns(kLandNs);  // rank 1's loads, and the commits' arrivals at rank 1
+    if (PAIR) pause_ns(kLandNs);  // rank 1's loads, and the commits' arrivals at rank 1
   }
   __syncwarp();
-  cluster_sync_all();
-  tc_fence_after();
-  if (warp == 1) tmem_dealloc_pair(tmem, TMEM_COLS);
+  if (PAIR) cluster_sync_all();
+  if (warp == 1) {
+    tc_fence_after();
+    if (PAIR) tmem_dealloc_pair(tmem, TMEM_COLS);
+    else tmem_dealloc(tmem, TMEM_COLS);
+  }
 }
 
 using Kernel = void (*)(Params4);
 struct Kernels {
-  Kernel single, pair, split;  // split: STORE, GELU and RESID
+  Kernel single, pair;
 };
 template <int EPI, int D, bool E8M0>
 Kernels kernels() {
-  if constexpr (EPI == RA_EPI_QKV)
-    return {gemm4_kernel<EPI, D, E8M0, false>, gemm4_pair_kernel<EPI, D, E8M0>, nullptr};
-  else
-    return {gemm4_kernel<EPI, D, E8M0, false>, gemm4_pair_kernel<EPI, D, E8M0>, gemm4_kernel<EPI, D, E8M0, true>};
+  return {gemm4_kernel<EPI, D, E8M0, false>, gemm4_kernel<EPI, D, E8M0, true>};
 }
 template <bool E8M0>
 Kernels pick(int epi, int d) {
@@ -977,68 +784,28 @@ Kernels pick(int epi, int d) {
   }
 }
 
-// Clusters of cs CTAs of a split kernel that run at once (ClusterTable asks 1 to 8; only
-// sizes up to MAX_SPLIT are used).
-int max_clusters(Kernel fn, int cs) {
-  static ClusterTable table;
-  int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess) {
-    cudaGetLastError();
-    return 0;
-  }
-  const int smem = Layout<false>::SMEM_ALLOC;
-  return table
-      .get(dev, reinterpret_cast<const void*>(fn), smem,
-           [&](int c) {
-             cudaLaunchAttribute attr[1];
-             attr[0].id = cudaLaunchAttributeClusterDimension;
-             attr[0].val.clusterDim.x = c;
-             attr[0].val.clusterDim.y = 1;
-             attr[0].val.clusterDim.z = 1;
-             cudaLaunchConfig_t cfg;
-             std::memset(&cfg, 0, sizeof(cfg));
-             cfg.gridDim = dim3(c, 1, 1);
-             cfg.blockDim = dim3(THREADS4, 1, 1);
-             cfg.dynamicSmemBytes = smem;
-             cfg.attrs = attr;
-             cfg.numAttrs = 1;
-             int found = 0;
-             if (cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess ||
-                 cudaOccupancyMaxActiveClusters(&found, fn, &cfg) != cudaSuccess) {
-               cudaGetLastError();
-               return -1;
-             }
-             return found;
-           })
-      .of[cs];
-}
-
 struct Plan {
   bool pair;
-  int bn, cs;
+  int bn;
 };
 
 // The cheapest cut: rounds of tiles on the SMs, each as long as its MMAs or its epilogue.
 Plan make_plan(const ra_gemm4_args& a, int sms) {
-  Plan best{false, 64, 1};
+  Plan best{false, 64};
   double best_us = 1e30;
-  auto tiles_of = [&](int tm, int bn, int64_t* all, int64_t* open) {
-    const int64_t cols = (a.N + bn - 1) / bn;
-    *all = *open = 0;  // tiles, and those of segments that are not gated
-    for (int g = 0; g < a.n_seg; ++g) {
-      const int64_t t = a.seg[g].lin.rows > 0 ? int64_t(a.B) * ((a.seg[g].lin.rows + tm - 1) / tm) * cols : 0;
-      *all += t;
-      if (!a.seg[g].lin.gated) *open += t;
-    }
-  };
   const double k = a.K / 1024.0;
   for (int pair = 0; pair < 2; ++pair) {
     if ((a.tile_mode == 1 && pair) || (a.tile_mode == 2 && !pair) || (pair && sms < 2)) continue;
     const int tm = pair ? P_TM : BM, slots = pair ? sms / 2 : sms;
-    for (int bn = MAX_BN; bn >= 64; bn -= 64) {
-      if (a.epilogue == RA_EPI_QKV && (bn % a.d != 0 || (a.H * a.d) % bn != 0)) continue;
-      int64_t all, open;
-      tiles_of(tm, bn, &all, &open);
+    for (int bn = pair && a.epilogue != RA_EPI_QKV ? 192 : 128; bn >= 64; bn -= 64) {
+      if (a.epilogue == RA_EPI_QKV && bn % a.d != 0) continue;
+      const int64_t cols = (a.N + bn - 1) / bn;
+      int64_t all = 0, open = 0;  // tiles, and those of segments that are not gated
+      for (int g = 0; g < a.n_seg; ++g) {
+        const int64_t t = a.seg[g].lin.rows > 0 ? int64_t(a.B) * ((a.seg[g].lin.rows + tm - 1) / tm) * cols : 0;
+        all += t;
+        if (!a.seg[g].lin.gated) open += t;
+      }
       const double epilogue = 0.0085 * bn;  // of a tile, hidden behind the next one's MMAs
       double round = k * (pair ? 0.8 + 0.0020 * bn : 0.9 + 0.0034 * bn);
       round = round > epilogue ? round : epilogue;
@@ -1047,7 +814,7 @@ Plan make_plan(const ra_gemm4_args& a, int sms) {
       if (open > 0 && open < all) us += fixed + round * double((open + slots - 1) / slots);
       if (us < best_us) {
         best_us = us;
-        best = Plan{pair != 0, bn, 1};
+        best = Plan{pair != 0, bn};
       }
     }
   }
@@ -1114,7 +881,10 @@ ra_status run(const char* who, const ra_gemm4_args& a, cudaStream_t st) {
   p.w_tiles = plan.bn > 128 ? 2 : 1;
   p.sf_cols = scale_cols(p.groups, p.w_tiles);
   p.sf_bufs = (TMEM_COLS - 2 * plan.bn) / p.sf_cols;
-  const int stages = pair ? Layout<true>::STAGES : Layout<false>::STAGES;
+  const bool qkv = a.epilogue == RA_EPI_QKV;
+  const int stages = pair ? Layout<true, false>::STAGES : Layout<false, false>::STAGES;
+  static_assert(Layout<true, false>::STAGES == Layout<true, true>::STAGES &&
+                    Layout<false, false>::STAGES == Layout<false, true>::STAGES, "stages of QKV");
   if (p.sf_bufs > stages) p.sf_bufs = stages;
   p.stage_tx = A_BYTES + (pair ? plan.bn / 2 : plan.bn) * (CHUNK / 2) + p.groups * 512 * (1 + p.w_tiles);
   const int64_t cols = (a.N + plan.bn - 1) / plan.bn;
@@ -1155,14 +925,6 @@ ra_status run(const char* who, const ra_gemm4_args& a, cudaStream_t st) {
     auto on32 = [](const void* ptr, int64_t ss, int64_t sr, int64_t sh = 0) {  // strides in elements of 2 bytes
       return (reinterpret_cast<uintptr_t>(ptr) & 31u) == 0 && ss % 16 == 0 && sr % 16 == 0 && sh % 16 == 0;
     };
-    if (a.epilogue == RA_EPI_QKV) {
-      p.wide[g] = 1;
-      for (const ra_seg* o : {&s.q_out, &s.k_out, &s.v_out})
-        p.wide[g] &= on32(o->ptr, o->stride_b, o->stride_n, o->stride_h);
-    } else {
-      p.wide[g] = on32(s.out, s.out_stride_s, s.out_stride_r) &&
-                  (a.epilogue != RA_EPI_RESID || on32(s.resid, s.resid_stride_s, s.resid_stride_r));
-    }
     const int e = q.a_exponent + q.w_exponent;
     p.seg[g].alpha = ldexpf(1.f, e);
     const int64_t rows = s.rows, spans = (rows + 127) / 128 * ((a.K + 4 * block_of(a.format) - 1) / (4 * block_of(a.format)));
@@ -1173,14 +935,23 @@ ra_status run(const char* who, const ra_gemm4_args& a, cudaStream_t st) {
     if (s.bias) in[n_in++] = RowSpan{s.bias, 0, 0, 1, 1, int64_t(a.N) * 4};
     if (a.epilogue == RA_EPI_QKV) {
       // the rows of the first head: outputs may interleave their heads
-      for (const ra_seg* o : {&s.q_out, &s.k_out, &s.v_out})
+      p.wide[g] = 1;
+      for (const ra_seg* o : {&s.q_out, &s.k_out, &s.v_out}) {
         out[n_out++] = RowSpan{o->ptr, o->stride_b * 2, o->stride_n * 2, a.B, rows, int64_t(a.d) * 2};
+        if ((a.B > 1 && o->stride_b < 1) || (a.H > 1 && o->stride_h < 1) || (rows > 1 && o->stride_n < a.d)) {
+          set_error("%s: seg %d: strides of q_out, k_out and v_out must be positive, their rows' at least d", who, g);
+          return RA_EINVAL;
+        }
+        p.wide[g] &= on32(o->ptr, o->stride_b, o->stride_n, o->stride_h);
+      }
     } else {
       if (a.B > 1 && s.out_stride_s < 1) {
         set_error("%s: seg %d: out_stride_s must be positive", who, g);
         return RA_EINVAL;
       }
       out[n_out++] = RowSpan{s.out, s.out_stride_s * 2, s.out_stride_r * 2, a.B, rows, int64_t(a.N) * 2};
+      p.wide[g] = on32(s.out, s.out_stride_s, s.out_stride_r) &&
+                  (a.epilogue != RA_EPI_RESID || on32(s.resid, s.resid_stride_s, s.resid_stride_r));
       if (a.epilogue == RA_EPI_RESID) {
         in[n_in++] = RowSpan{s.gate, s.gate_stride_s * 4, 0, a.B, 1, int64_t(a.N) * 4};
         if (s.resid != s.out || s.resid_stride_s != s.out_stride_s || s.resid_stride_r != s.out_stride_r)
@@ -1208,12 +979,11 @@ ra_status run(const char* who, const ra_gemm4_args& a, cudaStream_t st) {
   if (tiles == 0) return RA_OK;
   const Kernels kn = p.e8m0 ? pick<true>(a.epilogue, a.d) : pick<false>(a.epilogue, a.d);
   const int64_t slots = pair ? (sms / 2 > 0 ? sms / 2 : 1) : sms;
-  if (pair) note_launch("CTA pairs, %d columns", plan.bn);
-  else if (plan.cs > 1) note_launch("clusters of %d, %d columns", plan.cs, plan.bn);
-  else note_launch("single CTAs, %d columns", plan.bn);
-  if (pair) return launch(who, p, kn.pair, Layout<true>::SMEM_ALLOC, 2 * (tiles < slots ? tiles : slots), 2, st, THREADS4);
-  if (plan.cs > 1) return launch(who, p, kn.split, Layout<false>::SMEM_ALLOC, tiles * plan.cs, plan.cs, st, THREADS4);
-  return launch(who, p, kn.single, Layout<false>::SMEM_ALLOC, tiles < slots ? tiles : slots, 1, st, THREADS4);
+  note_launch(pair ? "CTA pairs, %d columns" : "single CTAs, %d columns", plan.bn);
+  const int smem = pair ? (qkv ? Layout<true, true>::SMEM_ALLOC : Layout<true, false>::SMEM_ALLOC)
+                        : (qkv ? Layout<false, true>::SMEM_ALLOC : Layout<false, false>::SMEM_ALLOC);
+  const int64_t groups = tiles < slots ? tiles : slots;
+  return launch(who, p, pair ? kn.pair : kn.single, smem, pair ? 2 * groups : groups, pair ? 2 : 1, st, THREADS4);
 }
 
 }  // namespace gemm4

@@ -160,7 +160,7 @@ __device__ __forceinline__ void gelu_tanh2(float& x0, float& x1) {
 }
 
 // What an epilogue warp works on: its 32 rows (row0 + lane, nrow of them in
-// the segment), its share of the tile's columns (half: 0 .. WAYS - 1), its shared
+// the segment), its share of the tile's columns (half 0 or 1), its shared
 // memory (staging buffer, two vectors of 128 per-column values) and the TMEM
 // address of its lanes in the tile's accumulator; cols: columns of the tile.
 struct EpiWarp {
@@ -186,26 +186,25 @@ __device__ __forceinline__ void add_cols(const uint32_t (&v)[32], float alpha, c
   }
 }
 
-// STORE, GELU, RESID: chunk j of the warp is tile columns 32 (half + WAYS j) ...; WAYS warps share
-// a row's columns.
-template <int EPI, bool SCALED, int WAYS, class Ready>
+// STORE, GELU, RESID: chunk j of the warp is tile columns 32 (half + 2 j) ...
+template <int EPI, class Ready>
 __device__ __forceinline__ bool epilogue_linear(const Params& p, const Tile& tl, const EpiWarp& w, Ready ready) {
   const Seg& sg = p.seg[tl.seg];
   const int lane = threadIdx.x & 31, n0 = tl.n0 + 32 * w.half;
   // this warp's; the last tile of a row may reach past N (a multiple of 32)
-  const int chunks = (min(w.cols, p.N - tl.n0) / 32 + WAYS - 1 - w.half) / WAYS;
+  const int chunks = (min(w.cols, p.N - tl.n0) / 32 + 1 - w.half) >> 1;
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     if (j >= chunks) break;
-    w.vec0[32 * j + lane] = sg.bias ? sg.bias[n0 + 32 * WAYS * j + lane] : 0.f;
-    if (EPI == RA_EPI_RESID) w.vec1[32 * j + lane] = sg.gate[int64_t(tl.s) * sg.gate_ss + n0 + 32 * WAYS * j + lane];
+    w.vec0[32 * j + lane] = sg.bias ? sg.bias[n0 + 64 * j + lane] : 0.f;
+    if (EPI == RA_EPI_RESID) w.vec1[32 * j + lane] = sg.gate[int64_t(tl.s) * sg.gate_ss + n0 + 64 * j + lane];
   }
   const char* res = nullptr;
   uint4 ra[4], rb[4];  // residuals of the next even and odd chunk
   if (EPI == RA_EPI_RESID && chunks > 0) {
     res = reinterpret_cast<const char*>(sg.resid + int64_t(tl.s) * sg.res_ss + int64_t(w.row0) * sg.res_sr + n0);
     rows_fetch(res, 2 * sg.res_sr, w.nrow, ra);
-    if (chunks > 1) rows_fetch(res + 64 * WAYS, 2 * sg.res_sr, w.nrow, rb);
+    if (chunks > 1) rows_fetch(res + 128, 2 * sg.res_sr, w.nrow, rb);
   }
   char* out = reinterpret_cast<char*>(sg.out + int64_t(tl.s) * sg.out_ss + int64_t(w.row0) * sg.out_sr + n0);
   __syncwarp();
@@ -220,13 +219,13 @@ __device__ __forceinline__ bool epilogue_linear(const Params& p, const Tile& tl,
       // Residuals two chunks ahead (one ahead left about 1000 cycles of global
       // latency in every chunk); the accumulators are not loaded ahead in
       // exchange, the registers allow one of the two without spills.
-      tmem_ld32(w.acc + 32 * w.half + 32 * WAYS * j, v);
+      tmem_ld32(w.acc + 32 * w.half + 64 * j, v);
       rows_turn(w.stage, rc, r);
-      if (j + 2 < chunks) rows_fetch(res + 64 * WAYS * (j + 2), 2 * sg.res_sr, w.nrow, rc);
+      if (j + 2 < chunks) rows_fetch(res + 128 * (j + 2), 2 * sg.res_sr, w.nrow, rc);
     }
     tmem_ld_wait_for(v);
-    add_cols<SCALED>(v, sg.alpha, w.vec0 + 32 * j, x);
-    if (EPI != RA_EPI_RESID && j + 1 < chunks) tmem_ld32(w.acc + 32 * w.half + 32 * WAYS * (j + 1), v);
+    add_cols<false>(v, 1.f, w.vec0 + 32 * j, x);
+    if (EPI != RA_EPI_RESID && j + 1 < chunks) tmem_ld32(w.acc + 32 * w.half + 64 * (j + 1), v);
     if (EPI == RA_EPI_GELU) {
 #pragma unroll
       for (int i = 0; i < 32; i += 2) gelu_tanh2(x[i], x[i + 1]);
@@ -244,7 +243,7 @@ __device__ __forceinline__ bool epilogue_linear(const Params& p, const Tile& tl,
         }
       }
     }
-    rows_store(w.stage, x, out + 64 * WAYS * j, 2 * sg.out_sr, w.nrow);
+    rows_store(w.stage, x, out + 128 * j, 2 * sg.out_sr, w.nrow);
   };
 #pragma unroll 1
   for (int j = 0; j < chunks; j += 2) {
@@ -347,7 +346,7 @@ __device__ __forceinline__ bool epilogue_tile(const Params& p, const Tile& tl, c
   if constexpr (EPI == RA_EPI_QKV)
     return epilogue_qkv<D>(p, tl, w, ready);
   else
-    return epilogue_linear<EPI, false, 2>(p, tl, w, ready);
+    return epilogue_linear<EPI>(p, tl, w, ready);
 }
 
 // A split tile: each CTA of the cluster has the sums over its part of K in its
@@ -361,7 +360,6 @@ __device__ __forceinline__ bool epilogue_tile(const Params& p, const Tile& tl, c
 // rank sends and waits for what it receives, also after a wait of this CTA was
 // given up: no CTA exits with a copy into it, or out of it, in flight.
 // The merge of a 128 x 256 tile between two CTAs (64 KB each way) takes 2.6 us.
-template <int WAYS = 2>
 __device__ __forceinline__ bool merge_parts(const WaitCtl& ctl, uint8_t* smem, uint64_t* parts_full, uint32_t acc,
                                             bool ok, int bn, int half, int quarter, int rank, int cs) {
   const int lane = threadIdx.x & 31, row = quarter * 32 + lane;
@@ -372,7 +370,7 @@ __device__ __forceinline__ bool merge_parts(const WaitCtl& ctl, uint8_t* smem, u
   const bool leader = quarter == 0 && half == 0 && lane == 0;
   if (leader) mbar_arrive_expect_tx(parts_full, (cs - 1) * part_bytes);
 #pragma unroll 1
-  for (int c0 = 32 * half; c0 < bn; c0 += 32 * WAYS) {
+  for (int c0 = 32 * half; c0 < bn; c0 += 64) {
     const int q = c0 / cw;
     if (q == rank) continue;
     uint32_t v[32];
@@ -399,7 +397,7 @@ __device__ __forceinline__ bool merge_parts(const WaitCtl& ctl, uint8_t* smem, u
                                                mbar_wait_drain(parts_full, 0, ctl.budget_ns));
   if (!got || !ok) return false;
 #pragma unroll 1
-  for (int c0 = 32 * half; c0 < cw; c0 += 32 * WAYS) {
+  for (int c0 = 32 * half; c0 < cw; c0 += 64) {
     uint32_t v[32];
     float x[32];
     tmem_ld32(acc + rank * cw + c0, v);
