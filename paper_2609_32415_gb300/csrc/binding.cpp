@@ -443,7 +443,7 @@ struct RowShape {
     if (o == Py_None) return Rows{nullptr, 0, 0, 0, 0};
     const at::Tensor& t = tensor(o);
     if (t.dim() != 3 || t.scalar_type() != at::kBFloat16 || !t.is_cuda() || t.size(2) != F ||
-        (F > 1 && t.stride(2) != 1) || (B >= 0 && (t.size(0) != B || t.size(1) != rows))) {
+        (F > 1 && t.numel() > 0 && t.stride(2) != 1) || (B >= 0 && (t.size(0) != B || t.size(1) != rows))) {
       char want[160];
       if (B >= 0)
         snprintf(want, sizeof(want), "a [%lld, %lld, %lld] bf16 CUDA tensor with contiguous last axis", (long long)B,

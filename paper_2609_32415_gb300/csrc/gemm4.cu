@@ -958,14 +958,6 @@ ra_status run(const char* who, const ra_gemm4_args& a, cudaStream_t st) {
           in[n_in++] = RowSpan{s.resid, s.resid_stride_s * 2, s.resid_stride_r * 2, a.B, rows, int64_t(a.N) * 2};
       }
     }
-    // Two bytes of codes as one element: a box of 64 is 128 bytes, 256 columns.
-    ra_seg as{const_cast<void*>(s.a), s.a_stride_s / 2, 0, s.a_stride_r / 2, s.rows, 0};
-    ra_seg ws{const_cast<void*>(s.w), 0, 0, a.K / 4, a.N, 0};
-    if (!encode_seg(&p.tm_a[g], as, a.B, 1, a.K / 4, CHUNK / 4, BM, true) ||
-        !encode_seg(&p.tm_w[g], ws, 1, 1, a.K / 4, CHUNK / 4, pair ? plan.bn / 2 : plan.bn, true) ||
-        !encode_scales(&p.tm_sa[g], q.a_scales, a.K, s.rows, a.B, a.format, p.groups, 1) ||
-        !encode_scales(&p.tm_sw[g], q.w_scales, a.K, a.N, 1, a.format, p.groups, p.w_tiles))
-      return RA_EINVAL;
     if (int64_t(p.m_tiles[g]) * cols > 2147483647) {
       set_error("%s: seg %d: too many rows", who, g);
       return RA_EINVAL;
@@ -977,6 +969,19 @@ ra_status run(const char* who, const ra_gemm4_args& a, cudaStream_t st) {
     return RA_EINVAL;
   }
   if (tiles == 0) return RA_OK;
+  for (int g = 0; g < a.n_seg; ++g) {
+    const ra_gemm4_seg& q = a.seg[g];
+    const ra_gemm_seg& s = q.lin;
+    if (s.rows == 0) continue;
+    // Two bytes of codes as one element: a box of 64 is 128 bytes, 256 columns.
+    ra_seg as{const_cast<void*>(s.a), s.a_stride_s / 2, 0, s.a_stride_r / 2, s.rows, 0};
+    ra_seg ws{const_cast<void*>(s.w), 0, 0, a.K / 4, a.N, 0};
+    if (!encode_seg(&p.tm_a[g], as, a.B, 1, a.K / 4, CHUNK / 4, BM, true) ||
+        !encode_seg(&p.tm_w[g], ws, 1, 1, a.K / 4, CHUNK / 4, pair ? plan.bn / 2 : plan.bn, true) ||
+        !encode_scales(&p.tm_sa[g], q.a_scales, a.K, s.rows, a.B, a.format, p.groups, 1) ||
+        !encode_scales(&p.tm_sw[g], q.w_scales, a.K, a.N, 1, a.format, p.groups, p.w_tiles))
+      return RA_EINVAL;
+  }
   const Kernels kn = p.e8m0 ? pick<true>(a.epilogue, a.d) : pick<false>(a.epilogue, a.d);
   const int64_t slots = pair ? (sms / 2 > 0 ? sms / 2 : 1) : sms;
   note_launch(pair ? "CTA pairs, %d columns" : "single CTAs, %d columns", plan.bn);

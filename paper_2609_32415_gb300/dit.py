@@ -30,6 +30,11 @@ activations (LN outputs, Q/K/V, attention outputs, MLP hidden) are one
 shared set reused by every block. The running text and target hidden states
 are updated in place by the gated-residual epilogues.
 
+With ``weights4`` the projections run on the tensor cores' 4-bit rate: their weights
+are given as ``api.Weight4`` (``api.weight4`` makes one), the rows that enter a
+projection are rounded to the same format in front of it (refadapt_quant4,
+refadapt_gemm4), and everything else is as with bf16 weights.
+
 Results are deterministic, but a sample's may depend on the other samples of its
 batch in their last rounding: the rows and modes of a call decide how the
 attention divides a row's keys and the projections a tile's K.
@@ -37,19 +42,25 @@ attention divides a row's keys and the projections a tile's K.
 import torch
 
 from . import api
-from ._lib import RA_EPI_GELU, RA_EPI_QKV, RA_EPI_RESID
+from ._lib import RA_EPI_GELU, RA_EPI_QKV, RA_EPI_RESID, RA_Q4_E4M3, RA_Q4_E8M0
 
 ROLES = ("text", "ref", "tgt")
 STREAM_OF = {"text": "text", "ref": "image", "tgt": "image"}
 CUES = {"product": 0, "change": 1, "exposure": 2}
+FORMATS4 = {"e4m3": RA_Q4_E4M3, "e8m0": RA_Q4_E8M0}
 
 
 class DiTExecutor:
+    """weights4: None, "e4m3" or "e8m0" (the projections' weights are api.Weight4 of that
+    format); activation_exponent: of the scales that e4m3 gives the rows."""
+
     def __init__(self, n_blocks, B, H, d, n_text, n_ref, n_tgt, theta, delta_max, eps=1e-6, mlp_ratio=4,
                  forced_boundary=-1, mass_rows=0, ln_eps=1e-6, norm_eps=1e-6, rope_base=10000.0, log_steps=8,
-                 cue="product", device="cuda", mlp_width=None):
+                 cue="product", device="cuda", mlp_width=None, weights4=None, activation_exponent=0):
         if cue not in CUES:
             raise ValueError("unknown cue %r" % (cue,))
+        if weights4 is not None and weights4 not in FORMATS4:
+            raise ValueError("unknown weights4 %r" % (weights4,))
         dev = torch.device(device)
         self.n_blocks, self.B, self.H, self.d = n_blocks, B, H, d
         self.C = C = H * d
@@ -86,6 +97,14 @@ class DiTExecutor:
         self.qkv = {r: [torch.empty((B, H, self.n[r], d), **bf) for _ in range(3)] for r in ("text", "tgt")}
         self.q_ref = torch.empty((B, H, n_ref, d), **bf)
         self.pos0 = {"text": 0, "ref": n_text, "tgt": n_text + n_ref}
+        self.format4 = None if weights4 is None else FORMATS4[weights4]
+        self.activation_exponent = int(activation_exponent)
+        if self.format4 is not None:
+            # the rows of a call's segments in 4 bits, shared by all projections
+            most = max(n_text, n_ref, n_tgt)
+            size = [max(f(k) for k in (C, F)) for f in
+                    (lambda k: most * k // 2, lambda k: api.refadapt_quant4_scales_size(most, k, self.format4))]
+            self.rows4 = [[torch.empty(B * n, dtype=torch.uint8, device=dev) for n in size] for _ in ROLES]
         self.gemm_hook = None   # optional callable(phase, name, t, b), e.g. CUDA events
         self.attn_hook = None
 
@@ -94,10 +113,30 @@ class DiTExecutor:
         B, n, _ = t.shape
         return t.view(B, n, self.H, self.d).permute(0, 2, 1, 3)
 
+    def _gemm4(self, segs, N, K, epilogue, mode=None, stream=None, **kw):
+        rows, products = [], []
+        for s, (codes, scales) in zip(segs, self.rows4):
+            w = s["w"]
+            if not isinstance(w, api.Weight4) or w.format != self.format4:
+                raise ValueError("weights4: expected an api.Weight4 of format %d" % self.format4)
+            B, n, _ = s["a"].shape
+            codes = codes[:B * n * K // 2].view(B, n, K // 2)
+            scales = scales[:B * api.refadapt_quant4_scales_size(n, K, self.format4)]
+            e = self.activation_exponent
+            gated = s.get("gated", False)
+            rows.append({"x": s["a"], "codes": codes, "scales": scales, "exponent": e, "gated": gated})
+            products.append({**s, "a": codes, "a_scales": scales, "a_exponent": e, "w": w.codes, "w_scales": w.scales,
+                             "w_exponent": w.exponent})
+        api.refadapt_quant4(rows, K, self.format4, mode=mode, stream=stream)
+        api.refadapt_gemm4(products, N, K, epilogue, self.format4, mode=mode, stream=stream, **kw)
+
     def _gemm(self, name, t, b, *args, **kw):
         if self.gemm_hook is not None:
             self.gemm_hook("pre", name, t, b)
-        api.refadapt_gemm(*args, **kw)
+        if self.format4 is None:
+            api.refadapt_gemm(*args, **kw)
+        else:
+            self._gemm4(*args, **kw)
         if self.gemm_hook is not None:
             self.gemm_hook("post", name, t, b)
 

@@ -34,7 +34,8 @@ class GatedDiTExecutor(DiTExecutor):
     "none". Weights per stream: w_qkv, b_qkv, q_norm, k_norm, w_o, b_o as for
     DiTExecutor; w_gate, w_up [F, C], w_2 [C, F] bf16, b_2 [C] fp32; optional
     norm weights pre_a, post_a, pre_m, post_m [C] fp32 (attention and
-    feed-forward branch)."""
+    feed-forward branch). With weights4 (see DiTExecutor) w_qkv, w_o and w_2 are
+    api.Weight4; w_gate and w_up stay bf16."""
 
     def __init__(self, n_blocks, B, H, d, n_text, n_ref, n_tgt, theta, delta_max, pos, axes, ff_width, pre="rms",
                  post="rms", act="silu", rope_base=10000.0, device="cuda", **kw):

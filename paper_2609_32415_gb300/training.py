@@ -1,19 +1,22 @@
-"""The gated block's layers as torch.autograd functions.
+"""The gated block's layers as torch.autograd functions, linear layers through 4-bit
+products, and the optimiser.
 
 Forward and backward run in librefadapt.so (refadapt_glu, refadapt_residual_norm,
-refadapt_rope_axes and their backward passes); torch keeps the graph, allocates
-the results and supplies the stream. bf16 rows and weights, fp32 vectors, on one
-GPU; shapes as in ``api``. Gradients of bf16 tensors are bf16, of fp32 vectors
-fp32. ``rope_axes`` can be differentiated any number of times (its gradient is the
-inverse turn); the other two once: a second time raises."""
+refadapt_rope_axes, refadapt_quant4 with refadapt_gemm4, and their backward passes);
+torch keeps the graph, allocates the results and supplies the stream. bf16 rows and
+weights, fp32 vectors, on one GPU; shapes as in ``api``. Gradients of bf16 tensors are
+bf16, of fp32 vectors fp32. ``rope_axes`` can be differentiated any number of times (its
+gradient is the inverse turn); the others once: a second time raises. ``AdamW`` steps
+over all parameters in one call (refadapt_grad_norm, refadapt_adamw)."""
 import functools
+import math
 
 import torch
 
 from . import api
-from ._lib import RA_EPI_STORE
+from ._lib import RA_EPI_STORE, RA_Q4_E8M0
 
-__all__ = ["gated_feed_forward", "residual_norm", "rope_axes"]
+__all__ = ["gated_feed_forward", "residual_norm", "rope_axes", "linear4", "AdamW"]
 
 
 # Gradients come in whatever layout the graph gave them (transposed, strides of zero,
@@ -39,7 +42,7 @@ class _Gradients(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, *_):
-        raise RuntimeError("gated_feed_forward and residual_norm cannot be differentiated twice")
+        raise RuntimeError("gated_feed_forward, residual_norm and linear4 cannot be differentiated twice")
 
 
 def _once(backward):
@@ -160,3 +163,110 @@ class _RopeAxes(torch.autograd.Function):
 def rope_axes(x, pos, axes, base=10000.0):
     """x [B, H, n, d] bf16 turned by the rows' coordinates pos ([n, len(axes)] or [B, n, len(axes)] fp32)."""
     return _RopeAxes.apply(x, pos, tuple(axes), base, False)
+
+
+class _Linear4(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, w, format, x_exponent, w_exponent, err_word):
+        (B, n, K), N = x.shape, w.shape[0]
+        y = torch.empty((B, n, N), dtype=x.dtype, device=x.device)
+        w4 = api.weight4(w, format, w_exponent)
+        codes, scales = api.quant4_buffers(B, n, K, format, x.device)
+        api.refadapt_quant4([{"x": x, "codes": codes, "scales": scales, "exponent": x_exponent}], K, format)
+        api.refadapt_gemm4([{"a": codes, "a_scales": scales, "a_exponent": x_exponent, "w": w4.codes,
+                             "w_scales": w4.scales, "w_exponent": w4.exponent, "out": y}], N, K, RA_EPI_STORE, format,
+                           err_word=err_word)
+        ctx.save_for_backward(x, w)
+        ctx.err_word = err_word
+        return y
+
+    @staticmethod
+    @_once
+    def backward(ctx, dy):
+        x, w = ctx.saved_tensors
+        dx, dw = (torch.empty_like(t, memory_format=torch.contiguous_format) if need else None
+                  for t, need in zip((x, w), ctx.needs_input_grad))
+        if dx is not None or dw is not None:
+            ws = api.linear4_backward_workspace(x.shape[0], x.shape[1], x.shape[2], w.shape[0], x.device)
+            api.refadapt_linear4_backward(_rows(dy), x, w, ws, dx=dx, dw=dw, err_word=ctx.err_word)
+        return dx, dw, None, None, None, None
+
+
+def linear4(x, w, format=RA_Q4_E8M0, x_exponent=0, w_exponent=0, err_word=None):
+    """x w^T through 4-bit products, x [B, rows, K], w [N, K] bf16 (N and K multiples of
+    64): forward in the format given (RA_Q4_E4M3: with the exponents of its scales), the
+    gradients in RA_Q4_E8M0, which has no range to choose. Rounding to 4 bits counts as
+    the identity in the backward pass."""
+    return _Linear4.apply(x, w, format, x_exponent, w_exponent, err_word)
+
+
+class AdamW:
+    """AdamW over a list of parameters (contiguous, fp32 or bf16; bf16 ones get an fp32
+    copy that the steps add up in), with clipping to max_norm. bits: 32 or 8, of the
+    moments. capturable: the rate and the step's number live on the GPU (``lr``, fp32, and
+    ``count``, int32), so that a captured step goes on when it is replayed. A step whose
+    gradients' norm is not finite changes no parameter. ``norm`` holds the last step's
+    gradient norm and clipping factor (on the GPU)."""
+
+    def __init__(self, params, lr, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, bits=32, max_norm=math.inf, seed=0,
+                 capturable=False):
+        self.params = list(params)
+        if not self.params:
+            raise ValueError("AdamW: no parameters")
+        if len({id(p) for p in self.params}) < len(self.params):
+            raise ValueError("AdamW: a parameter twice")
+        for p in self.params:
+            if p.dtype not in (torch.float32, torch.bfloat16) or not p.is_cuda or not p.is_contiguous():
+                raise ValueError("AdamW: expected contiguous fp32 or bf16 CUDA parameters, got %s %s %s"
+                                 % (tuple(p.shape), p.dtype, p.device))
+        dev = self.params[0].device
+        self.betas, self.eps, self.weight_decay, self.max_norm, self.seed = betas, eps, weight_decay, max_norm, seed
+        self.bits, self.capturable = bits, capturable
+        self.lr = torch.tensor([lr], dtype=torch.float32, device=dev) if capturable else lr
+        self.count = torch.zeros(1, dtype=torch.int32, device=dev) if capturable else 0
+        self.state = [dict(api.adamw_moments(p, bits), **({} if p.dtype == torch.float32 else {"p": p.detach().float()}))
+                      for p in self.params]
+        self.norm = torch.zeros(2, dtype=torch.float32, device=dev)
+        self._workspace = api.grad_norm_workspace(dev)
+
+    def zero_grad(self, set_to_none=True):
+        for p in self.params:
+            if set_to_none:
+                p.grad = None
+            elif p.grad is not None:
+                p.grad.detach_().zero_()
+
+    @torch.no_grad()
+    def step(self):
+        tensors = []
+        for p, state in zip(self.params, self.state):
+            if p.grad is None:
+                continue
+            g = p.grad.contiguous()
+            tensors.append({"p": p, "g": g, **state} if p.dtype == torch.float32 else {"g": g, "w": p, **state})
+        if self.capturable:
+            self.count.add_(1)
+        else:
+            self.count += 1
+        api.refadapt_grad_norm([t["g"] for t in tensors], self.max_norm, self.norm, self._workspace)
+        api.refadapt_adamw(tensors, self.lr, self.count, beta1=self.betas[0], beta2=self.betas[1], eps=self.eps,
+                           weight_decay=self.weight_decay, grad_scale=self.norm[1:], seed=self.seed)
+
+    def state_dict(self):
+        """The moments, the fp32 copies and the step's number (the tensors themselves)."""
+        return {"state": self.state, "count": self.count, "bits": self.bits}
+
+    def load_state_dict(self, saved):
+        if saved["bits"] != self.bits or len(saved["state"]) != len(self.state):
+            raise ValueError("AdamW: a state of %d tensors in %d bits for %d in %d"
+                             % (len(saved["state"]), saved["bits"], len(self.state), self.bits))
+        for mine, theirs in zip(self.state, saved["state"]):
+            if {k: (v.shape, v.dtype) for k, v in mine.items()} != {k: (v.shape, v.dtype) for k, v in theirs.items()}:
+                raise ValueError("AdamW: a state of other shapes or types")
+        for mine, theirs in zip(self.state, saved["state"]):
+            for k, v in mine.items():
+                v.view(torch.uint8).copy_(theirs[k].view(torch.uint8)) if v.element_size() == 1 else v.copy_(theirs[k])
+        if self.capturable:
+            self.count.copy_(torch.as_tensor(saved["count"], dtype=torch.int32).reshape(1))
+        else:
+            self.count = int(saved["count"])
