@@ -61,20 +61,28 @@ __device__ __forceinline__ uint32_t to_e2m1(const float (&x)[8]) {
       : "f"(x[0]), "f"(x[1]), "f"(x[2]), "f"(x[3]), "f"(x[4]), "f"(x[5]), "f"(x[6]), "f"(x[7]));
   return r;
 }
+// Two values times a factor, cut towards zero.
+__device__ __forceinline__ uint64_t mul2_rz(uint64_t x, uint64_t f) {
+  uint64_t r;
+  asm("mul.rz.f32x2 %0, %1, %2;" : "=l"(r) : "l"(x), "l"(f));
+  return r;
+}
 // Eight bf16 in four words.
 __device__ __forceinline__ uint32_t codes_of(const uint32_t (&w)[4], float factor) {
+  const uint64_t f = f2_pack(factor, factor);
   float x[8];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    x[2 * i] = __fmul_rz(__uint_as_float(w[i] << 16), factor);
-    x[2 * i + 1] = __fmul_rz(__uint_as_float(w[i] & 0xffff0000u), factor);
-  }
+  for (int i = 0; i < 4; ++i) f2_unpack(mul2_rz(bf2_unpack(w[i]), f), x[2 * i], x[2 * i + 1]);
   return to_e2m1(x);
 }
-// Magnitudes of the two bf16 of a word, as two 16-bit integers (NaN above infinity above the rest).
-__device__ __forceinline__ uint32_t abs2(uint32_t w) { return w & 0x7fff7fffu; }
-__device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b) { return __vmaxu2(a, b); }
-__device__ __forceinline__ uint32_t top2(uint32_t a) { return max(a & 0xffffu, a >> 16); }
+// The larger magnitudes of two pairs of bf16 (NaN above infinity above the rest); the signs of the
+// result say nothing.
+__device__ __forceinline__ uint32_t max_abs2(uint32_t a, uint32_t b) {
+  uint32_t m;
+  asm("max.NaN.xorsign.abs.bf16x2 %0, %1, %2;" : "=r"(m) : "r"(a), "r"(b));
+  return m;
+}
+__device__ __forceinline__ uint32_t top2(uint32_t a) { return max(a & 0x7fffu, (a >> 16) & 0x7fffu); }
 
 struct Seg {
   const char* x;
@@ -128,10 +136,8 @@ __global__ void __launch_bounds__(THREADS) rows_kernel(const __grid_constant__ P
     const int row = int(rt) * ROWS + (threadIdx.x >> 4) + 16 * k;
     const bool on = row < sg.rows && col < p.C;
     const uint32_t a[4] = {v[k][0].x, v[k][0].y, v[k][0].z, v[k][0].w}, b[4] = {v[k][1].x, v[k][1].y, v[k][1].z, v[k][1].w};
-    uint32_t m = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) m = max2(m, max2(abs2(a[i]), abs2(b[i])));
-    m = top2(m);
+    uint32_t m = top2(max_abs2(max_abs2(max_abs2(a[0], a[1]), max_abs2(a[2], a[3])),
+                               max_abs2(max_abs2(b[0], b[1]), max_abs2(b[2], b[3]))));
     if (E8M0) m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
     const Block blk = block_scale<E8M0>(m, sg.down);
     if (on)
@@ -154,12 +160,18 @@ __global__ void __launch_bounds__(THREADS) rows_kernel(const __grid_constant__ P
 
 // Blocks along the rows (tokens: all samples' rows, one after another), and along the
 // features where codes are wanted too. A CTA: 128 tokens by 64 columns, kept in shared
-// memory (16 KB; 16-byte pieces permuted by the token's block of 32, so that four
-// blocks of a column are read without conflicts); then a thread takes 32 tokens of a
-// column and four threads write 64 contiguous bytes.
+// memory, 16 KB. A thread loads 16 columns of two tokens (and rounds them along the features),
+// then takes two columns of 16 tokens from there, a word of both a token; the eight threads of
+// a column pair write 64 contiguous bytes of each column. 16-byte pieces of a token are permuted by
+// its group of 16 and its parity, which keeps both accesses free of conflicts.
+// Bound by instruction issue: 24 a value where a thread took 8 columns and then 32 tokens of one
+// column with 16-bit loads (16384 x 4096, both forms: 48 us).
 template <bool E8M0>
 __global__ void __launch_bounds__(THREADS) tokens_kernel(const __grid_constant__ Params p) {
   __shared__ __align__(16) uint8_t tile[T_TOKENS * T_COLS * 2];
+  auto piece_at = [&](int token, int piece) {
+    return reinterpret_cast<uint4*>(tile + token * (T_COLS * 2) + ((piece ^ (token >> 4) ^ (token & 1)) << 4));
+  };
   pdl_wait();
   pdl_launch();
   int g = 0;
@@ -170,94 +182,107 @@ __global__ void __launch_bounds__(THREADS) tokens_kernel(const __grid_constant__
   const int ct = int(at % col_tiles), tt = int(at / col_tiles);
   const int tokens = sg.rows * sg.samples, c0 = ct * T_COLS, t0 = tt * T_TOKENS;
   {
-    const int piece = threadIdx.x & 7, col = c0 + 8 * piece;
-    uint4 v[4];
+    const int unit = threadIdx.x & 3, col = c0 + 16 * unit;
+    uint4 v[2][2];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const int t = t0 + (threadIdx.x >> 3) + 32 * k;
-      const bool on = t < tokens && col < sg.C;
+    for (int k = 0; k < 2; ++k) {
+      const int t = t0 + (threadIdx.x >> 2) + 64 * k;
       const uint32_t s = sg.samples > 1 ? uint32_t(t) / uint32_t(sg.rows) : 0u, r = uint32_t(t) - s * uint32_t(sg.rows);
-      v[k] = on ? *reinterpret_cast<const uint4*>(sg.x + s * sg.x_ss + r * sg.x_sr + 2 * int64_t(col))
-                : make_uint4(0, 0, 0, 0);
+      const uint4* src = reinterpret_cast<const uint4*>(sg.x + s * sg.x_ss + r * sg.x_sr + 2 * int64_t(col));
+      v[k][0] = t < tokens && col < sg.C ? src[0] : make_uint4(0, 0, 0, 0);  // C is a multiple of 8
+      v[k][1] = t < tokens && col + 8 < sg.C ? src[1] : make_uint4(0, 0, 0, 0);
     }
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const int tl = (threadIdx.x >> 3) + 32 * k;
-      *reinterpret_cast<uint4*>(tile + tl * (T_COLS * 2) + ((piece ^ k) << 4)) = v[k];
+    for (int k = 0; k < 2; ++k) {
+      const int tl = (threadIdx.x >> 2) + 64 * k, t = t0 + tl;
+      *piece_at(tl, 2 * unit) = v[k][0];
+      *piece_at(tl, 2 * unit + 1) = v[k][1];
       if (sg.codes) {
-        const int t = t0 + tl;
-        const uint32_t w[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
-        uint32_t m = top2(max2(max2(abs2(w[0]), abs2(w[1])), max2(abs2(w[2]), abs2(w[3]))));
-        m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
-        if (E8M0) m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
+        const uint32_t a[4] = {v[k][0].x, v[k][0].y, v[k][0].z, v[k][0].w};
+        const uint32_t b[4] = {v[k][1].x, v[k][1].y, v[k][1].z, v[k][1].w};
+        uint32_t m = top2(max_abs2(max_abs2(max_abs2(a[0], a[1]), max_abs2(a[2], a[3])),
+                                   max_abs2(max_abs2(b[0], b[1]), max_abs2(b[2], b[3]))));
+        if (E8M0) m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
         const Block blk = block_scale<E8M0>(m, sg.down);
-        const bool on = t < tokens && col < sg.C;
-        if (on) *reinterpret_cast<uint32_t*>(sg.codes + t * sg.c_sr + col / 2) = codes_of(w, blk.factor);
+        const bool on = t < tokens && col < sg.C;  // C is a multiple of 64 here
+        if (on)
+          *reinterpret_cast<uint2*>(sg.codes + t * sg.c_sr + col / 2) =
+              make_uint2(codes_of(a, blk.factor), codes_of(b, blk.factor));
         // the scale tile of these 128 tokens: e4m3 four blocks are its 64 columns, e8m0 two are half of 128
-        uint32_t b = on ? blk.byte : 0u;
+        uint32_t w = on ? blk.byte : 0u;
         constexpr int GROUP = E8M0 ? 128 : 64;
         const int64_t groups = (sg.C + GROUP - 1) / GROUP;
         uint8_t* dst = sg.scales + (tt * groups + c0 / GROUP) * 512 + 16 * (tl & 31) + 4 * ((tl >> 5) & 3);
         if (E8M0) {
-          b |= __shfl_down_sync(0xffffffffu, b, 4) << 8;
-          if (piece == 0) {
+          w |= __shfl_down_sync(0xffffffffu, w, 2) << 8;
+          if (unit == 0) {
             if (ct & 1)
-              *reinterpret_cast<uint16_t*>(dst + 2) = uint16_t(b);
+              *reinterpret_cast<uint16_t*>(dst + 2) = uint16_t(w);
             else if (ct + 1 == int(col_tiles))
-              *reinterpret_cast<uint32_t*>(dst) = b & 0xffffu;
+              *reinterpret_cast<uint32_t*>(dst) = w & 0xffffu;
             else
-              *reinterpret_cast<uint16_t*>(dst) = uint16_t(b);
+              *reinterpret_cast<uint16_t*>(dst) = uint16_t(w);
           }
         } else {
-          b |= __shfl_down_sync(0xffffffffu, b, 2) << 8;
-          b |= __shfl_down_sync(0xffffffffu, b, 4) << 16;
-          if (piece == 0) *reinterpret_cast<uint32_t*>(dst) = b;
+          w |= __shfl_down_sync(0xffffffffu, w, 1) << 8;
+          w |= __shfl_down_sync(0xffffffffu, w, 2) << 16;
+          if (unit == 0) *reinterpret_cast<uint32_t*>(dst) = w;
         }
       }
     }
   }
   if (!sg.codes_t) return;
   __syncthreads();
-  const int blk = threadIdx.x & 3, cl = threadIdx.x >> 2, col = c0 + cl;  // 32 tokens from 32 blk on, of column cl
-  const int padded = (tokens + 63) / 64 * 64;
-  uint32_t w[16];  // the tokens, two to a word
-  const uint8_t* src = tile + blk * 32 * (T_COLS * 2) + (((cl >> 3) ^ blk) << 4) + 2 * (cl & 7);
+  const int tg = threadIdx.x & 7, pair = threadIdx.x >> 3, col = c0 + 2 * pair;  // 16 tokens from 16 tg on; C is even
+  const int padded = (tokens + 63) / 64 * 64, first = t0 + 16 * tg;
+  uint32_t w[16];
 #pragma unroll
-  for (int i = 0; i < 16; ++i)
-    w[i] = uint32_t(*reinterpret_cast<const uint16_t*>(src + (2 * i) * (T_COLS * 2))) |
-           uint32_t(*reinterpret_cast<const uint16_t*>(src + (2 * i + 1) * (T_COLS * 2))) << 16;
-  uint32_t m[2] = {0, 0};
+  for (int i = 0; i < 16; ++i) w[i] = reinterpret_cast<const uint32_t*>(piece_at(16 * tg + i, pair >> 2))[pair & 3];
+  uint32_t m = w[0];
 #pragma unroll
-  for (int i = 0; i < 16; ++i) m[i / 8] = max2(m[i / 8], abs2(w[i]));
-  m[0] = top2(m[0]), m[1] = top2(m[1]);
+  for (int i = 1; i < 16; ++i) m = max_abs2(m, w[i]);
+  uint32_t top[2] = {m & 0x7fffu, (m >> 16) & 0x7fffu};
   Block b[2];
-  if (E8M0) {
-    b[0] = b[1] = block_scale<true>(max(m[0], m[1]), sg.down);
-  } else {
-    b[0] = block_scale<false>(m[0], sg.down);
-    b[1] = block_scale<false>(m[1], sg.down);
-  }
-  uint32_t c[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const uint32_t q[4] = {w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]};
-    c[i] = codes_of(q, b[i / 2].factor);
+  for (int c = 0; c < 2; ++c) {
+    if (E8M0) top[c] = max(top[c], __shfl_xor_sync(0xffffffffu, top[c], 1));
+    b[c] = block_scale<E8M0>(top[c], sg.down);
   }
-  const int first = t0 + 32 * blk;
-  if (col < sg.C && first < padded)
-    *reinterpret_cast<uint4*>(sg.codes_t + col * sg.t_stride + first / 2) = make_uint4(c[0], c[1], c[2], c[3]);
-  // scales of the transposed matrix: 64 of a tile's 128 rows; those behind the last column are zero
-  uint32_t e = (b[0].byte | (E8M0 ? 0u : b[1].byte << 8));
+#pragma unroll
+  for (int c = 0; c < 2; ++c) {
+    const uint64_t f = f2_pack(b[c].factor, b[c].factor);
+    uint32_t q[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      float x[8];
+#pragma unroll
+      for (int i = 0; i < 8; i += 2) {
+        const uint32_t lo = w[8 * h + i], hi = w[8 * h + i + 1];
+        const uint64_t y = c == 0 ? f2_pack(__uint_as_float(lo << 16), __uint_as_float(hi << 16))
+                                  : f2_pack(__uint_as_float(lo & 0xffff0000u), __uint_as_float(hi & 0xffff0000u));
+        f2_unpack(mul2_rz(y, f), x[i], x[i + 1]);
+      }
+      q[h] = to_e2m1(x);
+    }
+    if (col < sg.C && first < padded)
+      *reinterpret_cast<uint2*>(sg.codes_t + int64_t(col + c) * sg.t_stride + first / 2) = make_uint2(q[0], q[1]);
+  }
+  // Scales of the transposed matrix: 64 of a tile's 128 rows; those behind the last column are zero.
+  // Four blocks' bytes of both columns meet in the first of their threads.
+  constexpr int STEP = E8M0 ? 2 : 1;  // threads from block to block
+  uint32_t e = b[0].byte | b[1].byte << 16;
   if (col >= sg.C || first >= padded) e = 0;
-  e |= __shfl_down_sync(0xffffffffu, e, 1) << (E8M0 ? 8 : 16);
-  if (E8M0) e |= __shfl_down_sync(0xffffffffu, e, 2) << 16;
+  e |= __shfl_down_sync(0xffffffffu, e, STEP) << 8;
+  const uint32_t o = __shfl_down_sync(0xffffffffu, e, 2 * STEP);
   const int64_t groups = E8M0 ? (padded + 127) / 128 : padded / 64;
-  const int64_t group = E8M0 ? tt : 2 * tt + blk / 2;
+  const int64_t group = E8M0 ? tt : 2 * tt + tg / 4;
   const int rows_up = (sg.C + 127) / 128 * 128;
-  if (E8M0 ? blk == 0 : (blk & 1) == 0) {
-    uint8_t* dst = sg.scales_t + (int64_t(col >> 7) * groups + group) * 512 + 16 * (col & 31) + 4 * ((col >> 5) & 3);
-    if (group < groups) {
-      *reinterpret_cast<uint32_t*>(dst) = e;
+  if (tg % (4 * STEP) == 0 && group < groups) {
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      const int r = col + c;
+      uint8_t* dst = sg.scales_t + (int64_t(r >> 7) * groups + group) * 512 + 16 * (r & 31) + 4 * ((r >> 5) & 3);
+      *reinterpret_cast<uint32_t*>(dst) = c == 0 ? (e & 0xffffu) | o << 16 : e >> 16 | (o & 0xffff0000u);
       // the half tile behind the last columns has no CTA of its own
       if (ct + 1 == int(col_tiles) && c0 + T_COLS < rows_up) *reinterpret_cast<uint32_t*>(dst + 8) = 0;
     }
