@@ -789,11 +789,16 @@ struct Plan {
   int bn;
 };
 
-// The cheapest cut: rounds of tiles on the SMs, each as long as its MMAs or its epilogue.
+// The cheapest cut by a model of the call's time (microseconds), from one and four whole rounds of
+// tiles at K = 256 to 8192 (each within 8 %): a round takes what its stages take, or its
+// epilogue, and 0.3 between tiles. Few tiles: 152 single CTAs of narrow tiles beat 76 pairs, whose
+// set-up takes longer too.
 Plan make_plan(const ra_gemm4_args& a, int sms) {
   Plan best{false, 64};
   double best_us = 1e30;
   const double k = a.K / 1024.0;
+  const double epilogue = a.epilogue == RA_EPI_STORE ? 0.0057 : a.epilogue == RA_EPI_RESID ? 0.008
+                          : a.epilogue == RA_EPI_GELU ? 0.0115 : 0.020;  // of a tile, per column
   for (int pair = 0; pair < 2; ++pair) {
     if ((a.tile_mode == 1 && pair) || (a.tile_mode == 2 && !pair) || (pair && sms < 2)) continue;
     const int tm = pair ? P_TM : BM, slots = pair ? sms / 2 : sms;
@@ -806,10 +811,9 @@ Plan make_plan(const ra_gemm4_args& a, int sms) {
         all += t;
         if (!a.seg[g].lin.gated) open += t;
       }
-      const double epilogue = 0.0085 * bn;  // of a tile, hidden behind the next one's MMAs
-      double round = k * (pair ? 0.8 + 0.0020 * bn : 0.9 + 0.0034 * bn);
-      round = round > epilogue ? round : epilogue;
-      const double fixed = (pair ? 4.4 : 3.6) + 0.0088 * bn;
+      const double stages = k * (pair ? (bn == 192 ? 1.02 : 0.77 + 0.0006 * bn) : 0.56 + 0.002 * bn);
+      const double round = (stages > epilogue * bn ? stages : epilogue * bn) + 0.3;
+      const double fixed = pair ? 4.2 + 0.0075 * bn : 3.3;
       double us = fixed + round * double((all + slots - 1) / slots);
       if (open > 0 && open < all) us += fixed + round * double((open + slots - 1) / slots);
       if (us < best_us) {
