@@ -32,7 +32,9 @@ constexpr int THREADS = 256;
 constexpr int CHUNK = 8192;
 template <int BITS>
 constexpr int STEP_CHUNK = BITS == 8 ? CHUNK : CHUNK / 2;
-constexpr int MAX_TENSORS = 256;  // of a launch
+// Tensors of a launch; calls of few tensors take kernels whose arguments (2.6 KB, not 20) are copied in
+// less time than these run.
+constexpr int MAX_TENSORS = 256, FEW_TENSORS = 32;
 
 // ------------------------------------------------------------------ norm
 constexpr int NORM_CTAS = 2048;  // at most, over all launches of a call
@@ -45,6 +47,7 @@ struct NormTensor {
   uint32_t first;  // chunk of the launch that the tensor starts with
   int32_t bf16;
 };
+template <int MAX>
 struct NormParams {
   int32_t n_tensors;
   uint32_t chunks;
@@ -53,7 +56,7 @@ struct NormParams {
   float* out;
   uint32_t* ticket;
   double* partial;
-  NormTensor t[MAX_TENSORS];
+  NormTensor t[MAX];
 };
 
 // The tensor whose chunks include `chunk` (the last one that starts at or before it).
@@ -83,7 +86,8 @@ __device__ __forceinline__ double block_sum(double v, double* warps) {
 // Sums in an order that the sizes alone decide: a thread's squares of a chunk in fp32 (32 of
 // them), its chunks, the CTA's threads and the CTAs in fp64; the CTA that takes the last
 // ticket of the call adds the CTAs' sums up.
-__global__ void __launch_bounds__(THREADS) norm_kernel(const __grid_constant__ NormParams p) {
+template <int MAX>
+__global__ void __launch_bounds__(THREADS) norm_kernel(const __grid_constant__ NormParams<MAX> p) {
   __shared__ double warps[THREADS / 32];
   __shared__ bool last;
   pdl_wait();
@@ -171,7 +175,7 @@ struct StepTensor {
   uint32_t first;    // chunk of the launch that the tensor starts with
   uint8_t bf16, wide, pad[2];  // wide: pointers allow 16-byte access
 };
-struct StepParams {
+struct StepRates {
   int32_t n_tensors;
   float lr, beta1, beta2, rest1, rest2, eps, decay;  // rest: 1 - beta
   float log1, log2;                                  // natural logarithms of the betas
@@ -179,7 +183,10 @@ struct StepParams {
   const float* lr_dev;
   const int32_t* step_dev;
   const float* grad_scale;
-  StepTensor t[MAX_TENSORS];
+};
+template <int MAX>
+struct StepParams : StepRates {
+  StepTensor t[MAX];
 };
 
 // A mix of 32 bits in which every input bit reaches every output bit: shifts, and products
@@ -198,7 +205,7 @@ struct Rates {
 // the product with the scale is exact wherever it stands). m and v by the fp32 operations
 // that the formula names, each rounded: their 8-bit forms depend on the last bit. The root and the
 // quotient are the hardware's (2 ulp), of which the weight takes lr times.
-__device__ __forceinline__ void update(const StepParams& h, const Rates& r, float b1, float b2, const float (&g)[8],
+__device__ __forceinline__ void update(const StepRates& h, const Rates& r, float b1, float b2, const float (&g)[8],
                                        float (&p)[8], float (&m)[8], float (&v)[8]) {
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
@@ -372,7 +379,7 @@ __device__ __forceinline__ void finish8(const StepTensor& t, uint32_t key, int64
 // Eight elements of a tensor from `at` on, n of them in the tensor (at most 0: none, but
 // the thread takes part in its block's scale).
 template <int BITS, bool WIDE>
-__device__ __forceinline__ void step8(const StepParams& h, const StepTensor& t, const Rates& r, uint32_t key,
+__device__ __forceinline__ void step8(const StepRates& h, const StepTensor& t, const Rates& r, uint32_t key,
                                       int64_t at, int n) {
   float p[8], g[8], m[8], v[8], b1 = h.beta1, b2 = h.beta2;
   if (n > 0) {
@@ -435,7 +442,7 @@ struct Raw8 {
 // these are computed (70 instructions an element); without, the warps waited for memory half
 // their time: 1144 -> 833 us for 317 M weights, 6.1 TB/s.
 template <bool BF16>
-__device__ __forceinline__ void whole_chunk(const StepParams& h, const StepTensor& t, const Rates& r, uint32_t key,
+__device__ __forceinline__ void whole_chunk(const StepRates& h, const StepTensor& t, const Rates& r, uint32_t key,
                                             int64_t i0) {
   constexpr int PASSES = CHUNK / (8 * THREADS);
   int64_t at = i0 + int(threadIdx.x) * 8;
@@ -458,8 +465,8 @@ __device__ __forceinline__ void whole_chunk(const StepParams& h, const StepTenso
   }
 }
 
-template <int BITS>
-__global__ void __launch_bounds__(THREADS, BITS == 8 ? 3 : 4) step_kernel(const __grid_constant__ StepParams h) {
+template <int BITS, int MAX>
+__global__ void __launch_bounds__(THREADS, BITS == 8 ? 3 : 4) step_kernel(const __grid_constant__ StepParams<MAX> h) {
   pdl_wait();
   pdl_launch();
   const uint32_t chunk = blockIdx.x;
@@ -532,6 +539,106 @@ bool meet(std::vector<Range>& r) {
   return false;
 }
 
+struct NormCall {
+  const ra_grad* tensors;
+  int32_t n_tensors;
+  float max_norm;
+  float* out;
+  void* workspace;
+  int64_t most;  // CTAs of a launch
+  cudaStream_t st;
+};
+template <int MAX>
+ra_status launch_norm(const NormCall& c) {
+  NormParams<MAX> p;
+  std::memset(&p, 0, sizeof(p));
+  p.max_norm = c.max_norm;
+  p.out = c.out;
+  p.ticket = static_cast<uint32_t*>(c.workspace);
+  p.partial = reinterpret_cast<double*>(static_cast<char*>(c.workspace) + 16);
+  auto ctas_of = [&](int64_t n) { return n < 1 ? 1 : n < c.most ? n : c.most; };
+  for (int pass = 0; pass < 2; ++pass) {  // counts the CTAs, then launches
+    int32_t base = 0, i = 0;
+    do {
+      p.n_tensors = 0;
+      int64_t first = 0;
+      for (; i < c.n_tensors && p.n_tensors < MAX; ++i) {
+        if (c.tensors[i].n == 0) continue;
+        p.t[p.n_tensors++] = NormTensor{c.tensors[i].g, c.tensors[i].n, uint32_t(first), c.tensors[i].type == RA_BF16};
+        first += (c.tensors[i].n + CHUNK - 1) / CHUNK;
+      }
+      while (i < c.n_tensors && c.tensors[i].n == 0) ++i;
+      p.chunks = uint32_t(first);
+      p.base = base;
+      const int64_t ctas = ctas_of(first);
+      base += int32_t(ctas);
+      if (pass == 1) {
+        const ra_status r = opt::launch("refadapt_grad_norm", p, norm_kernel<MAX>, ctas, c.st);
+        if (r != RA_OK) return r;
+      }
+    } while (i < c.n_tensors);
+    p.total = base;
+  }
+  return RA_OK;
+}
+
+template <int BITS, int MAX>
+ra_status launch_step(const ra_adamw_args& a, cudaStream_t st) {
+  StepParams<MAX> p;
+  std::memset(static_cast<void*>(&p), 0, sizeof(p));
+  p.lr = float(a.lr);
+  p.beta1 = float(a.beta1);
+  p.beta2 = float(a.beta2);
+  p.rest1 = float(1.0 - a.beta1);
+  p.rest2 = float(1.0 - a.beta2);
+  p.eps = float(a.eps);
+  p.decay = float(a.decay);
+  p.log1 = a.beta1 > 0 ? float(std::log(a.beta1)) : 0.f;
+  p.log2 = a.beta2 > 0 ? float(std::log(a.beta2)) : 0.f;
+  p.step = uint32_t(a.step);
+  p.seed_lo = uint32_t(a.seed);
+  p.seed_hi = uint32_t(a.seed >> 32);
+  p.lr_dev = a.lr_dev;
+  p.step_dev = a.step_dev;
+  p.grad_scale = a.grad_scale;
+  uint64_t counter = 0;
+  int64_t chunks = 0;
+  constexpr int chunk = STEP_CHUNK<BITS>, states = BITS == 8 ? 8 : 16;  // states: what vectors of moments align to
+  auto flush = [&]() {
+    if (p.n_tensors == 0) return RA_OK;
+    const ra_status r = opt::launch("refadapt_adamw", p, step_kernel<BITS, MAX>, chunks, st);
+    p.n_tensors = 0;
+    chunks = 0;
+    return r;
+  };
+  for (int32_t i = 0; i < a.n_tensors; ++i) {
+    const ra_adamw_tensor& t = a.tensors[i];
+    if (t.n == 0) continue;
+    const int64_t mine = (t.n + chunk - 1) / chunk;
+    if (p.n_tensors == MAX || chunks + mine > 2147483647) {
+      const ra_status r = flush();
+      if (r != RA_OK) return r;
+    }
+    StepTensor& d = p.t[p.n_tensors++];
+    d.p = static_cast<float*>(t.p);
+    d.g = t.g;
+    d.m = t.m;
+    d.v = t.v;
+    d.m_scale = static_cast<uint8_t*>(t.m_scale);
+    d.v_scale = static_cast<uint8_t*>(t.v_scale);
+    d.w = static_cast<__nv_bfloat16*>(t.w);
+    d.n = t.n;
+    d.counter = counter;
+    d.first = uint32_t(chunks);
+    d.bf16 = t.g_type == RA_BF16;
+    d.wide = aligned(t.p, 16) && aligned(t.g, 16) && aligned(t.m, states) && aligned(t.v, states) &&
+             aligned(t.w, 16);
+    chunks += mine;
+    counter += uint64_t(t.n + 31) / 32 * 32;
+  }
+  return flush();
+}
+
 }  // namespace opt
 }  // namespace ra
 
@@ -572,7 +679,6 @@ extern "C" ra_status refadapt_grad_norm(const ra_grad* tensors, int32_t n_tensor
     used += t.n > 0;
     chunks += (t.n + CHUNK - 1) / CHUNK;
   }
-  const cudaStream_t st = static_cast<cudaStream_t>(stream);
   const int64_t launches = used > 0 ? (used + MAX_TENSORS - 1) / MAX_TENSORS : 1;
   if (launches > NORM_CTAS || chunks > (int64_t(1) << 31)) {
     set_error("refadapt_grad_norm: too many tensors or elements");
@@ -580,36 +686,8 @@ extern "C" ra_status refadapt_grad_norm(const ra_grad* tensors, int32_t n_tensor
   }
   // CTAs of a launch: eight for an SM, as many as the workspace has room for
   const int64_t most = std::min<int64_t>(int64_t(num_sms()) * 8, NORM_CTAS / launches);
-  NormParams p;
-  std::memset(&p, 0, sizeof(p));
-  p.max_norm = max_norm;
-  p.out = out;
-  p.ticket = static_cast<uint32_t*>(workspace);
-  p.partial = reinterpret_cast<double*>(static_cast<char*>(workspace) + 16);
-  auto ctas_of = [&](int64_t c) { return c < 1 ? 1 : c < most ? c : most; };
-  for (int pass = 0; pass < 2; ++pass) {  // counts the CTAs, then launches
-    int32_t base = 0, i = 0;
-    do {
-      p.n_tensors = 0;
-      int64_t first = 0;
-      for (; i < n_tensors && p.n_tensors < MAX_TENSORS; ++i) {
-        if (tensors[i].n == 0) continue;
-        p.t[p.n_tensors++] = NormTensor{tensors[i].g, tensors[i].n, uint32_t(first), tensors[i].type == RA_BF16};
-        first += (tensors[i].n + CHUNK - 1) / CHUNK;
-      }
-      while (i < n_tensors && tensors[i].n == 0) ++i;
-      p.chunks = uint32_t(first);
-      p.base = base;
-      const int64_t ctas = ctas_of(first);
-      base += int32_t(ctas);
-      if (pass == 1) {
-        const ra_status r = opt::launch("refadapt_grad_norm", p, norm_kernel, ctas, st);
-        if (r != RA_OK) return r;
-      }
-    } while (i < n_tensors);
-    p.total = base;
-  }
-  return RA_OK;
+  const NormCall call{tensors, n_tensors, max_norm, out, workspace, most, static_cast<cudaStream_t>(stream)};
+  return used <= FEW_TENSORS ? launch_norm<FEW_TENSORS>(call) : launch_norm<MAX_TENSORS>(call);
 }
 
 extern "C" ra_status refadapt_adamw(const ra_adamw_args* a, void* stream) {
@@ -674,58 +752,9 @@ extern "C" ra_status refadapt_adamw(const ra_adamw_args* a, void* stream) {
     set_error("refadapt_adamw: out of host memory");
     return RA_EINVAL;
   }
+  int32_t used = 0;
+  for (int32_t i = 0; i < a->n_tensors; ++i) used += a->tensors[i].n > 0;
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
-  StepParams p;
-  std::memset(&p, 0, sizeof(p));
-  p.lr = float(a->lr);
-  p.beta1 = float(a->beta1);
-  p.beta2 = float(a->beta2);
-  p.rest1 = float(1.0 - a->beta1);
-  p.rest2 = float(1.0 - a->beta2);
-  p.eps = float(a->eps);
-  p.decay = float(a->decay);
-  p.log1 = a->beta1 > 0 ? float(std::log(a->beta1)) : 0.f;
-  p.log2 = a->beta2 > 0 ? float(std::log(a->beta2)) : 0.f;
-  p.step = uint32_t(a->step);
-  p.seed_lo = uint32_t(a->seed);
-  p.seed_hi = uint32_t(a->seed >> 32);
-  p.lr_dev = a->lr_dev;
-  p.step_dev = a->step_dev;
-  p.grad_scale = a->grad_scale;
-  uint64_t counter = 0;
-  int64_t chunks = 0;
-  const int chunk = small ? STEP_CHUNK<8> : STEP_CHUNK<32>;
-  auto flush = [&]() {
-    if (p.n_tensors == 0) return RA_OK;
-    const ra_status r = opt::launch("refadapt_adamw", p, small ? step_kernel<8> : step_kernel<32>, chunks, st);
-    p.n_tensors = 0;
-    chunks = 0;
-    return r;
-  };
-  for (int32_t i = 0; i < a->n_tensors; ++i) {
-    const ra_adamw_tensor& t = a->tensors[i];
-    if (t.n == 0) continue;
-    const int64_t mine = (t.n + chunk - 1) / chunk;
-    if (p.n_tensors == MAX_TENSORS || chunks + mine > 2147483647) {
-      const ra_status r = flush();
-      if (r != RA_OK) return r;
-    }
-    StepTensor& d = p.t[p.n_tensors++];
-    d.p = static_cast<float*>(t.p);
-    d.g = t.g;
-    d.m = t.m;
-    d.v = t.v;
-    d.m_scale = static_cast<uint8_t*>(t.m_scale);
-    d.v_scale = static_cast<uint8_t*>(t.v_scale);
-    d.w = static_cast<__nv_bfloat16*>(t.w);
-    d.n = t.n;
-    d.counter = counter;
-    d.first = uint32_t(chunks);
-    d.bf16 = t.g_type == RA_BF16;
-    d.wide = aligned(t.p, 16) && aligned(t.g, 16) && aligned(t.m, small ? 8 : 16) && aligned(t.v, small ? 8 : 16) &&
-             aligned(t.w, 16);
-    chunks += mine;
-    counter += uint64_t(t.n + 31) / 32 * 32;
-  }
-  return flush();
+  if (small) return used <= FEW_TENSORS ? launch_step<8, FEW_TENSORS>(*a, st) : launch_step<8, MAX_TENSORS>(*a, st);
+  return used <= FEW_TENSORS ? launch_step<32, FEW_TENSORS>(*a, st) : launch_step<32, MAX_TENSORS>(*a, st);
 }
