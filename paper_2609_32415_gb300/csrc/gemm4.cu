@@ -973,6 +973,13 @@ ra_status run(const char* who, const ra_gemm4_args& a, cudaStream_t st) {
     return RA_EINVAL;
   }
   if (tiles == 0) return RA_OK;
+  int64_t single = 0, more = 0;  // segments of one row, of more
+  for (int g = 0; g < a.n_seg; ++g) {
+    single += a.seg[g].lin.rows == 1;
+    more += a.seg[g].lin.rows > 1;
+  }
+  if (a.B == 1 && more == 0 && !qkv && a.tile_mode == 0 && a.K <= MAX_ROW_K && single * a.N <= int64_t(sms) * 64)
+    return run_row(who, a, st);
   for (int g = 0; g < a.n_seg; ++g) {
     const ra_gemm4_seg& q = a.seg[g];
     const ra_gemm_seg& s = q.lin;

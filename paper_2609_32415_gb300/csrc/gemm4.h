@@ -2,6 +2,8 @@
 #pragma once
 #include <cuda_runtime.h>
 
+#include <cstdint>
+
 #include "refadapt.h"
 
 namespace ra {
@@ -10,6 +12,10 @@ namespace ra {
 constexpr int block_of(int format) { return format == RA_Q4_E8M0 ? 32 : 16; }
 
 namespace gemm4 {
+// Calls of one row a segment have a kernel of their own (gemm4_row.cu) where it is the faster one: as long
+// as one tile of 64 columns to an SM covers the weights' rows; K up to MAX_ROW_K. The arguments are checked.
+constexpr int MAX_ROW_K = 32768;
+ra_status run_row(const char* who, const ra_gemm4_args& a, cudaStream_t st);
 ra_status run(const char* who, const ra_gemm4_args& a, cudaStream_t st);
 }  // namespace gemm4
 

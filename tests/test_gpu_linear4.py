@@ -238,6 +238,67 @@ def test_epilogues_of_two_segments(cuda_ok, epilogue, fmt, tile_mode):
         within(seg["out"], ref, tol)
 
 
+@pytest.mark.parametrize("fmt", [E4M3, E8M0])
+@pytest.mark.parametrize("epilogue", [STORE, GELU, RESID])
+@pytest.mark.parametrize("B, rows, N, K, mode", [(1, 1, 64, 64, 0), (1, 1, 192, 1088, 2), (1, 1, 448, 2048, 2), (1, 1, 320, 1024, 1),
+                                                 (1, 1, 128, 4160, 2), (1, 1, 64, 8192, 0), (2, 1, 256, 128, 2),
+                                                 (1, 3, 448, 2048, 2)])
+def test_few_rows(cuda_ok, fmt, epilogue, B, rows, N, K, mode):
+    """One row goes to a kernel of its own: two segments, the second gated; the tensor cores' result beside it
+    (tile_mode 1) is within the same bound, as are those of a few rows."""
+    a, g = api(), torch.Generator().manual_seed(N + K + epilogue)
+    mode = torch.tensor([mode, 0][:B], dtype=torch.int32, device="cuda")
+    segs, want = [], []
+    for gated in (False, True):
+        seg, y, acc = operands(B, rows, N, K, fmt, g, *((1, -5) if fmt == E4M3 else (0, 0)))
+        seg.update(gated=gated, bias=(0.3 * torch.randn(N, generator=g)).cuda() if not gated else None)
+        seg["out"] = torch.full((B, rows, N + 8), 7.0, dtype=torch.bfloat16, device="cuda")[..., :N]
+        x = y + (f64_32(seg["bias"]) if not gated else 0.0)
+        if epilogue == STORE:
+            ref, tol = x, acc
+        elif epilogue == GELU:
+            ref, tol = gelu64(x), 1.2 * acc + 16 * F32 * np.abs(x)
+        else:
+            seg.update(gate=torch.randn((B, N), generator=g).cuda(), resid=bf((B, rows, N), g))
+            gate = f64_32(seg["gate"])[:, None]
+            ref, tol = f64(seg["resid"]) + gate * x, np.abs(gate) * acc
+        segs.append(seg)
+        want.append((ref, tol + BF * np.abs(ref) + 4 * F32 * (np.abs(x) + np.abs(ref)) + 1e-30))
+    for tile_mode in (0, 1):
+        a.refadapt_gemm4(segs, N, K, epilogue, fmt, mode=mode, tile_mode=tile_mode)
+        assert ("one row" in a.refadapt_last_launch()) == (tile_mode == 0 and B * rows == 1)
+        for seg, (ref, tol) in zip(segs, want):
+            for s in range(B):
+                if seg["gated"] and int(mode[s]) == 0:
+                    assert bool((seg["out"][s] == 7.0).all())
+                else:
+                    within(seg["out"][s], ref[s], tol[s])
+        for seg in segs:
+            seg["out"].fill_(7.0)
+
+
+def test_one_row_of_every_code_and_scale(cuda_ok):
+    """Every code and scale byte, NaN ones among them, as the tensor cores have it."""
+    a, N, K = api(), 1024, 512
+    g = torch.Generator().manual_seed(5)
+    for fmt in (E4M3, E8M0):
+        codes, w = (torch.randint(0, 256, s, generator=g, dtype=torch.uint8).cuda() for s in ((1, 1, K // 2), (N, K // 2)))
+        sizes = [a.refadapt_quant4_scales_size(r, K, fmt) for r in (1, N)]
+        lo, hi = (0, 128) if fmt == E4M3 else (120, 134)
+        scales = [torch.randint(lo, hi, (n,), generator=g, dtype=torch.uint8).cuda() for n in sizes]
+        scales[1][::97] = 0x7f if fmt == E4M3 else 0xff
+        outs = []
+        for tile_mode in (0, 1):
+            out = torch.empty((1, 1, N), dtype=torch.bfloat16, device="cuda")
+            a.refadapt_gemm4([{"a": codes, "a_scales": scales[0], "w": w, "w_scales": scales[1], "out": out}], N, K, STORE, fmt,
+                             tile_mode=tile_mode)
+            outs.append(out.float())
+        nan = [torch.isnan(o) for o in outs]
+        assert torch.equal(*nan) and bool(nan[0].any()) and not bool(nan[0].all())
+        rel = (outs[0] - outs[1])[~nan[0]].norm() / outs[1][~nan[0]].norm()
+        assert float(rel) < BF  # both within half a bf16 step of sums that differ by far less
+
+
 @pytest.mark.parametrize("H, d", [(4, 64), (2, 128), (6, 128)])
 @pytest.mark.parametrize("fmt", [E4M3, E8M0])
 @pytest.mark.parametrize("tile_mode", [1, 2])
