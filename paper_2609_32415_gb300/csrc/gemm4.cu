@@ -44,15 +44,19 @@ constexpr int VEC_BYTES = 2 * UNIT * 4;    // two vectors of its columns
 constexpr int SUMS_BYTES = 4 * (128 / 32) * 32 * 4;
 constexpr int TURN_BYTES = EPI_STAGE_BYTES;  // QKV: a warp's RoPE rows of 16 columns
 
+// Stages of the ring. e8m0 pairs: as many as there are buffers of scales beside two accumulators of 192
+// columns, so that no wait for a buffer comes on top of the stage's (6: 245 ns a stage, 5: 217).
+constexpr int stages_of(bool pair, bool e8m0) { return pair && !e8m0 ? 6 : 5; }
+
 // Shared memory of one CTA a tile, and of CTA pairs (each stages half of the tile's weight rows).
-template <bool PAIR_, bool QKV>
+template <bool PAIR_, bool QKV, bool E8M0>
 struct Layout {
   static constexpr bool PAIR = PAIR_;
   static constexpr int MAX_BN = PAIR && !QKV ? 192 : 128;  // columns of a tile
   static constexpr int B_BYTES = (PAIR ? MAX_BN / 2 : MAX_BN) * CHUNK / 2;
   static constexpr int OFF_B = A_BYTES, OFF_SF = A_BYTES + B_BYTES;
   static constexpr int STAGE_BYTES = OFF_SF + SA_BYTES * (1 + (MAX_BN + 127) / 128);
-  static constexpr int STAGES = PAIR ? 6 : 5;
+  static constexpr int STAGES = stages_of(PAIR, E8M0);
   static constexpr int OFF_VEC = STAGES * STAGE_BYTES;
   static constexpr int OFF_SUMS = OFF_VEC + EPI4_WARPS * VEC_BYTES;
   static constexpr int OFF_TURN = OFF_SUMS + (QKV ? SUMS_BYTES : 0);
@@ -145,8 +149,8 @@ __device__ __forceinline__ uint32_t idesc_mx4(int M, int N, int e8m0) {
 #define RA_U1(N) RA_STR(2048 + N)
 #define RA_STR(N) RA_STR2(N)
 #define RA_STR2(N) #N
-static_assert(Layout<true, false>::OFF_SF / 16 == 1792 && Layout<true, true>::OFF_SF / 16 == 1536 &&
-                  Layout<false, false>::OFF_SF / 16 == 2048, "immediates of the copies");
+static_assert(Layout<true, false, false>::OFF_SF / 16 == 1792 && Layout<true, true, false>::OFF_SF / 16 == 1536 &&
+                  Layout<false, false, false>::OFF_SF / 16 == 2048, "immediates of the copies");
 template <class L, bool E8M0>
 __device__ __forceinline__ void issue_stage(const Params4& p, uint32_t lo, uint32_t sf, uint32_t sw, uint32_t d,
                                             uint32_t idesc, int ksteps, bool first, uint32_t bar) {
@@ -324,7 +328,13 @@ struct Scales {
   __device__ __forceinline__ explicit Scales(const Params4& p)
       : end(p.sf_cols * p.sf_bufs), wait(p.sf_bufs < STAGES ? p.sf_bufs : -1) {}
   __device__ __forceinline__ bool free(uint64_t* empty, const WaitCtl& ctl) const {
-    return wait != 0 || warp_wait(empty + old.st, old.ph, ctl);
+    if (wait != 0) return true;
+    // it is about to be: a warp that polls goes on sooner than one that is woken (e4m3 pairs, two buffers:
+    // 249 ns a stage, 264)
+#pragma unroll 1
+    for (int i = 0; i < 64; ++i)
+      if (__all_sync(0xffffffffu, peek(empty + old.st, old.ph) != 0)) return true;
+    return warp_wait(empty + old.st, old.ph, ctl);
   }
   __device__ __forceinline__ void next(const Params4& p) {
     col += p.sf_cols;
@@ -596,7 +606,7 @@ __device__ __forceinline__ bool epilogue4(const Params4& p, const Tile& tl, cons
 //   warps 2..13 epilogue (quarter = warp % 4, thread = output row = TMEM lane)
 template <int EPI, int D, bool E8M0, bool PAIR>
 __global__ void __launch_bounds__(THREADS4, 1) gemm4_kernel(const __grid_constant__ Params4 p) {
-  using L = Layout<PAIR, EPI == RA_EPI_QKV>;
+  using L = Layout<PAIR, EPI == RA_EPI_QKV, E8M0>;
   constexpr int STAGES = L::STAGES, TM = PAIR ? P_TM : BM, CTAS = PAIR ? 2 : 1;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
@@ -784,6 +794,12 @@ Kernels pick(int epi, int d) {
   }
 }
 
+template <bool E8M0>
+constexpr int smem_of(bool pair, bool qkv) {
+  return pair ? (qkv ? Layout<true, true, E8M0>::SMEM_ALLOC : Layout<true, false, E8M0>::SMEM_ALLOC)
+              : (qkv ? Layout<false, true, E8M0>::SMEM_ALLOC : Layout<false, false, E8M0>::SMEM_ALLOC);
+}
+
 struct Plan {
   bool pair;
   int bn;
@@ -886,9 +902,7 @@ ra_status run(const char* who, const ra_gemm4_args& a, cudaStream_t st) {
   p.sf_cols = scale_cols(p.groups, p.w_tiles);
   p.sf_bufs = (TMEM_COLS - 2 * plan.bn) / p.sf_cols;
   const bool qkv = a.epilogue == RA_EPI_QKV;
-  const int stages = pair ? Layout<true, false>::STAGES : Layout<false, false>::STAGES;
-  static_assert(Layout<true, false>::STAGES == Layout<true, true>::STAGES &&
-                    Layout<false, false>::STAGES == Layout<false, true>::STAGES, "stages of QKV");
+  const int stages = stages_of(pair, p.e8m0);
   if (p.sf_bufs > stages) p.sf_bufs = stages;
   p.stage_tx = A_BYTES + (pair ? plan.bn / 2 : plan.bn) * (CHUNK / 2) + p.groups * 512 * (1 + p.w_tiles);
   const int64_t cols = (a.N + plan.bn - 1) / plan.bn;
@@ -996,8 +1010,7 @@ ra_status run(const char* who, const ra_gemm4_args& a, cudaStream_t st) {
   const Kernels kn = p.e8m0 ? pick<true>(a.epilogue, a.d) : pick<false>(a.epilogue, a.d);
   const int64_t slots = pair ? (sms / 2 > 0 ? sms / 2 : 1) : sms;
   note_launch(pair ? "CTA pairs, %d columns" : "single CTAs, %d columns", plan.bn);
-  const int smem = pair ? (qkv ? Layout<true, true>::SMEM_ALLOC : Layout<true, false>::SMEM_ALLOC)
-                        : (qkv ? Layout<false, true>::SMEM_ALLOC : Layout<false, false>::SMEM_ALLOC);
+  const int smem = p.e8m0 ? smem_of<true>(pair, qkv) : smem_of<false>(pair, qkv);
   const int64_t groups = tiles < slots ? tiles : slots;
   return launch(who, p, pair ? kn.pair : kn.single, smem, pair ? 2 * groups : groups, pair ? 2 : 1, st, THREADS4);
 }
