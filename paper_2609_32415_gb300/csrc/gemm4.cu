@@ -11,12 +11,14 @@
 //     rows by 16 bytes, to every warp's lanes): four columns for 128 rows and four blocks.
 //     Buffers of them take turns; one is written again once the MMAs that read it have ended
 //     (their commit has arrived).
-//   * TMEM holds two accumulators of up to 192 columns and two stages' scales. Tiles of 256
-//     columns would leave either the scales or the second accumulator no room, and an epilogue
-//     takes as long as the MMAs of K = 1536.
-// What bounds it: shared memory. A stage of a pair's 256 x 192 tile puts 35 KB into a CTA's and
-// takes 28 KB out for the MMAs, 490 cycles at 128 bytes each, where the MMAs run 370; measured 500
-// (8192 rows, K = 16384, N = 7296, e8m0: 267 us, 7.3 PFLOP/s, 3.8 times the bf16 rate).
+//   * TMEM holds two accumulators of 192 columns or three of up to 128, and two to six stages' scales.
+//     Tiles of 256 columns would leave either the scales or the second accumulator no room, and
+//     an epilogue takes as long as the MMAs of K = 1536.
+// What bounds it: a stage of a pair's 256 x 192 tile takes 212 ns (e8m0; e4m3, whose scales have two buffers,
+// 249), its MMAs alone 198 (9.7 PFLOP/s), its loads less; a stage of 128 columns 200 (single CTAs 185), of
+// which 190 are the issuing warp's waits, copies and commit. Long calls reach the power cap: 8192 rows, K =
+// 16384, N = 7296 take 260 us with e8m0 (7.5 PFLOP/s, 3.9 times the bf16 rate), 274 with e4m3. Unrolling
+// the issuer by two stages, its tiles from the producer, and two producers each measured even or slower.
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -33,49 +35,61 @@ namespace gemm4 {
 
 using namespace gemm;
 
-// A quarter of the TMEM lanes (32 rows) has three epilogue warps, each with 64 of the tile's columns.
+// A quarter of the TMEM lanes (32 rows) has three epilogue warps, which take the units of 64 columns of all
+// tiles in turn: with two units to a tile all three are at work, on one tile and a half.
 constexpr int WAYS = 3, EPI4_WARPS = 4 * WAYS, THREADS4 = 64 + 32 * EPI4_WARPS;
 constexpr int UNIT = 64;     // columns of a warp
 constexpr int CHUNK = 256;   // K of a stage
+constexpr int MAX_ACCS = 3;  // accumulators
 constexpr int A_BYTES = BM * CHUNK / 2;
 constexpr int SA_BYTES = 4 * 512;  // scales of 128 rows, up to four tiles (e4m3)
 constexpr int VEC_BYTES = 2 * UNIT * 4;    // two vectors of its columns
-// QKV: the rows' sums of squares of each 32 columns, by TMEM lane quarter.
-constexpr int SUMS_BYTES = 4 * (128 / 32) * 32 * 4;
+// QKV: the rows' sums of squares of each 32 columns, by tile (one in three) and TMEM lane quarter.
+constexpr int SUMS = (128 / 32) * 32, SUMS_BYTES = WAYS * 4 * SUMS * 4;
 constexpr int TURN_BYTES = EPI_STAGE_BYTES;  // QKV: a warp's RoPE rows of 16 columns
 
-// Stages of the ring. e8m0 pairs: as many as there are buffers of scales beside two accumulators of 192
-// columns, so that no wait for a buffer comes on top of the stage's (6: 245 ns a stage, 5: 217).
-constexpr int stages_of(bool pair, bool e8m0) { return pair && !e8m0 ? 6 : 5; }
+// Stages of the ring: five, whose shared memory leaves room for a CTA of the kernel before or after this
+// one (a block's gradients, with quantisations around the products: 64 us, 69 with six) and L1 for the
+// outputs (single CTAs, GELU: 40 and 44 us). Pairs whose call is long take a sixth (16384 rows, K =
+// 4096, N = 16384: 349 us, 367 with five; 4096 rows, K = 16384, N = 4096 with e8m0: 83 and 87, but
+// 16384 rows, K = 4096: 84.4 and 83.5).
+constexpr int FEW_STAGES = 5, MAX_STAGES = 6;
+constexpr double LONG_CALL = 100;  // microseconds of the plan
 
 // Shared memory of one CTA a tile, and of CTA pairs (each stages half of the tile's weight rows).
-template <bool PAIR_, bool QKV, bool E8M0>
+template <bool PAIR_, bool QKV>
 struct Layout {
   static constexpr bool PAIR = PAIR_;
   static constexpr int MAX_BN = PAIR && !QKV ? 192 : 128;  // columns of a tile
   static constexpr int B_BYTES = (PAIR ? MAX_BN / 2 : MAX_BN) * CHUNK / 2;
   static constexpr int OFF_B = A_BYTES, OFF_SF = A_BYTES + B_BYTES;
   static constexpr int STAGE_BYTES = OFF_SF + SA_BYTES * (1 + (MAX_BN + 127) / 128);
-  static constexpr int STAGES = stages_of(PAIR, E8M0);
-  static constexpr int OFF_VEC = STAGES * STAGE_BYTES;
-  static constexpr int OFF_SUMS = OFF_VEC + EPI4_WARPS * VEC_BYTES;
+  // behind the stages
+  static constexpr int OFF_SUMS = EPI4_WARPS * VEC_BYTES;
   static constexpr int OFF_TURN = OFF_SUMS + (QKV ? SUMS_BYTES : 0);
   static constexpr int OFF_BAR = OFF_TURN + (QKV ? EPI4_WARPS * TURN_BYTES : 0);
-  static constexpr int OFF_MISC = OFF_BAR + (2 * STAGES + 5) * 8;  // full, empty, tfull[2], tempty[2], drain
-  static constexpr int SMEM_ALLOC = OFF_MISC + 16 + 1024;
+  static constexpr int OFF_MISC = OFF_BAR + (2 * MAX_STAGES + 2 * MAX_ACCS + 1) * 8;  // full, empty, tfull, tempty, drain
+  static constexpr int smem(int stages) { return stages * STAGE_BYTES + OFF_MISC + 16 + 1024; }
   static_assert(STAGE_BYTES % 1024 == 0 && OFF_SF % 1024 == 0, "swizzled tiles start on 1024 bytes");
-  static_assert(SMEM_ALLOC <= 232448, "shared memory budget");
 };
+
+static_assert(Layout<true, false>::smem(MAX_STAGES) <= 232448 && Layout<true, true>::smem(MAX_STAGES) <= 232448 &&
+                  Layout<false, false>::smem(FEW_STAGES) <= 232448 && Layout<false, true>::smem(FEW_STAGES) <= 232448,
+              "shared memory budget");
 
 // TMEM columns of a stage's scales: four for each tile of A's and of the weight's.
 constexpr int scale_cols(int groups, int w_tiles) { return 4 * groups * (1 + w_tiles); }
 static_assert(2 * 192 + 2 * scale_cols(4, 2) <= TMEM_COLS, "TMEM columns");
+static_assert(MAX_ACCS * 64 + MAX_STAGES * scale_cols(4, 1) <= TMEM_COLS && MAX_ACCS == WAYS,
+              "tiles of one unit have as many accumulators as warps that take them in turn");
 
 struct Params4 : Params {
   int32_t e8m0;                      // format
   int32_t groups;                    // scale tiles of a stage: 4 (e4m3) or 2 (e8m0)
   int32_t w_tiles;                   // scale tiles of a tile's weight rows: 1 or 2
   int32_t sf_cols, sf_bufs;          // TMEM columns of a stage's scales, buffers of them
+  int32_t units, accs;               // of 64 columns in a tile; accumulators
+  int32_t stages;                    // of the ring
   uint32_t stage_tx;                 // bytes of a stage that one CTA loads
   int32_t wide[3];                   // rows of the epilogue's tensors start on 32 bytes
   CUtensorMap tm_sa[3], tm_sw[3];
@@ -149,8 +163,8 @@ __device__ __forceinline__ uint32_t idesc_mx4(int M, int N, int e8m0) {
 #define RA_U1(N) RA_STR(2048 + N)
 #define RA_STR(N) RA_STR2(N)
 #define RA_STR2(N) #N
-static_assert(Layout<true, false, false>::OFF_SF / 16 == 1792 && Layout<true, true, false>::OFF_SF / 16 == 1536 &&
-                  Layout<false, false, false>::OFF_SF / 16 == 2048, "immediates of the copies");
+static_assert(Layout<true, false>::OFF_SF / 16 == 1792 && Layout<true, true>::OFF_SF / 16 == 1536 &&
+                  Layout<false, false>::OFF_SF / 16 == 2048, "immediates of the copies");
 template <class L, bool E8M0>
 __device__ __forceinline__ void issue_stage(const Params4& p, uint32_t lo, uint32_t sf, uint32_t sw, uint32_t d,
                                             uint32_t idesc, int ksteps, bool first, uint32_t bar) {
@@ -219,20 +233,31 @@ __device__ __forceinline__ void mbar_arrive_remote_relaxed(uint32_t cluster_addr
   asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
 // Has the phase completed? Asked before the work in front of it is issued, so that the answer's
-// latency (50 ns) passes meanwhile.
+// latency (50 ns) passes meanwhile. CLUSTER: what arrives may come from the other CTA of the pair.
+template <bool CLUSTER = false>
 __device__ __forceinline__ uint32_t peek(uint64_t* bar, uint32_t parity) {
   uint32_t ok;
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-      "selp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(ok)
-      : "r"(smem_u32(bar)), "r"(parity)
-      : "memory");
+  if constexpr (CLUSTER)
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.test_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(smem_u32(bar)), "r"(parity)
+        : "memory");
+  else
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(smem_u32(bar)), "r"(parity)
+        : "memory");
   return ok;
 }
+template <bool CLUSTER = false>
 __device__ __forceinline__ bool warp_wait(uint32_t peeked, uint64_t* bar, uint32_t parity, const WaitCtl& ctl) {
-  return __all_sync(0xffffffffu, peeked != 0) || warp_wait(bar, parity, ctl);
+  return __all_sync(0xffffffffu, peeked != 0) || warp_wait<CLUSTER>(bar, parity, ctl);
 }
 // A value that is the same in every lane, known to be so.
 __device__ __forceinline__ int same(int v) { return __shfl_sync(0xffffffffu, v, 0); }
@@ -306,12 +331,11 @@ __device__ __forceinline__ void tma_load_one(uint32_t dst, const void* tmap, uin
 }
 
 // A stage of the ring and the parity of its barriers' next phase.
-template <int STAGES>
 struct Ring {
   int st = 0;
   uint32_t ph = 0;
-  __device__ __forceinline__ void next() {
-    if (++st == STAGES) {
+  __device__ __forceinline__ void next(const Params4& p) {
+    if (++st == p.stages) {
       st = 0;
       ph ^= 1;
     }
@@ -321,12 +345,11 @@ struct Ring {
 // The buffers of scales in TMEM, one for a stage's MMAs after another. A buffer is written
 // again once the MMAs that read it, sf_bufs stages ago, have ended. As many buffers as
 // stages: the stage itself was filled again after that.
-template <int STAGES>
 struct Scales {
-  Ring<STAGES> old;  // the stage whose MMAs read the buffer last
+  Ring old;  // the stage whose MMAs read the buffer last
   int col = 0, end, wait;
   __device__ __forceinline__ explicit Scales(const Params4& p)
-      : end(p.sf_cols * p.sf_bufs), wait(p.sf_bufs < STAGES ? p.sf_bufs : -1) {}
+      : end(p.sf_cols * p.sf_bufs), wait(p.sf_bufs < p.stages ? p.sf_bufs : -1) {}
   __device__ __forceinline__ bool free(uint64_t* empty, const WaitCtl& ctl) const {
     if (wait != 0) return true;
     // it is about to be: a warp that polls goes on sooner than one that is woken (e4m3 pairs, two buffers:
@@ -340,7 +363,7 @@ struct Scales {
     col += p.sf_cols;
     if (col == end) col = 0;
     if (wait > 0) --wait;
-    else if (wait == 0) old.next();
+    else if (wait == 0) old.next(p);
   }
 };
 
@@ -413,7 +436,7 @@ __device__ __forceinline__ bool epilogue_linear4(const Params4& p, const Tile& t
                                                  Release release) {
   const Seg& sg = p.seg[tl.seg];
   const int lane = threadIdx.x & 31, n0 = tl.n0 + UNIT * w.unit;
-  const bool on = w.nrow > 0 && UNIT * w.unit < p.bn && n0 < p.N;  // N is a multiple of 64
+  const bool on = w.nrow > 0 && n0 < p.N;  // N is a multiple of 64
   const bool mine = lane < w.nrow, wide = p.wide[tl.seg];
   uint32_t r[2][2][8];
   const char* res = nullptr;
@@ -480,28 +503,31 @@ __device__ __forceinline__ bool epilogue_linear4(const Params4& p, const Tile& t
   return true;
 }
 
-// True where `ok` is in every thread of the quarter's WAYS warps, which all get here.
-__device__ __forceinline__ bool quarter_all(int quarter, bool ok) {
+// True where `ok` is in every thread of the two warps that share a tile's quarter, which both get here.
+// Tiles in flight have barriers of their own (turn 0 to 2).
+__device__ __forceinline__ bool both(int quarter, int turn, bool ok) {
   uint32_t all;
   asm volatile(
       "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\t"
       "barrier.cta.red.and.pred q, %2, %3, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
       : "=r"(all)
-      : "r"(uint32_t(ok)), "r"(quarter + 1), "n"(32 * WAYS)
+      : "r"(uint32_t(ok)), "r"(1 + quarter * WAYS + turn), "n"(64)
       : "memory");
   return all != 0;
 }
 
-// QKV: the warps of a quarter share every head. Each sums the squares of its columns, the sums meet
-// in shared memory, and the columns are normalised, turned and stored.
+// QKV: sums the squares of its columns, which for heads of 128 meet the other warp's in shared memory;
+// then the columns are normalised, turned and stored. `turn`: the tile's number modulo three. Its
+// sums are written again three tiles on, by the same warps: that tile's accumulators are
+// ready only after both have given this one's back, past their reads of the sums.
 template <int D, class Ready, class Release>
-__device__ __forceinline__ bool epilogue_qkv4(const Params4& p, const Tile& tl, const Epi4& w, float* sums, Ready ready,
-                                              Release release) {
+__device__ __forceinline__ bool epilogue_qkv4(const Params4& p, const Tile& tl, const Epi4& w, float* sums, int turn,
+                                              Ready ready, Release release) {
   const Seg& sg = p.seg[tl.seg];
   const int lane = threadIdx.x & 31, quarter = (threadIdx.x >> 5) & 3;
   const int part = tl.n0 / p.C;                       // 0 q, 1 k, 2 v
   const int c0 = tl.n0 - part * p.C + UNIT * w.unit;  // the unit's first column within the part
-  const bool on = w.nrow > 0 && UNIT * w.unit < p.bn;
+  const bool on = w.nrow > 0;
   // RoPE rows of the warp's positions: (cos, sin) of D / 2 pairs, 64 bytes for 16 columns, eight
   // rows an access (a row to a thread, 32 bytes each, took twice the whole tile's time)
   const char* rope = reinterpret_cast<const char*>(p.rope + int64_t(sg.pos_offset + w.row0) * (D / 4)) + 4 * (c0 % D);
@@ -538,8 +564,8 @@ __device__ __forceinline__ bool epilogue_qkv4(const Params4& p, const Tile& tl, 
       sums[(2 * w.unit + j) * 32 + lane] = s0 + s1;
     }
   }
-  // All three go on or none does: one that waits here for one that gave up would wait for ever.
-  if (!quarter_all(quarter, ok)) return false;
+  // Both go on or neither does.
+  if (!(D == 128 && part < 2 ? both(quarter, turn, ok) : ok)) return false;
   if (on) {
     float rstd = 1.f;
     if (part < 2) {
@@ -585,15 +611,14 @@ __device__ __forceinline__ bool epilogue_qkv4(const Params4& p, const Tile& tl, 
   } else {
     release();
   }
-  // the next tile's sums go where these were read
-  return part == 2 || quarter_all(quarter, true);
+  return true;
 }
 
 template <int EPI, int D, class Ready, class Release>
-__device__ __forceinline__ bool epilogue4(const Params4& p, const Tile& tl, const Epi4& w, float* sums, Ready ready,
-                                          Release release) {
+__device__ __forceinline__ bool epilogue4(const Params4& p, const Tile& tl, const Epi4& w, float* sums, int turn,
+                                          Ready ready, Release release) {
   if constexpr (EPI == RA_EPI_QKV)
-    return epilogue_qkv4<D>(p, tl, w, sums, ready, release);
+    return epilogue_qkv4<D>(p, tl, w, sums + turn * (4 * SUMS), turn, ready, release);
   else
     return epilogue_linear4<EPI>(p, tl, w, ready, release);
 }
@@ -606,28 +631,29 @@ __device__ __forceinline__ bool epilogue4(const Params4& p, const Tile& tl, cons
 //   warps 2..13 epilogue (quarter = warp % 4, thread = output row = TMEM lane)
 template <int EPI, int D, bool E8M0, bool PAIR>
 __global__ void __launch_bounds__(THREADS4, 1) gemm4_kernel(const __grid_constant__ Params4 p) {
-  using L = Layout<PAIR, EPI == RA_EPI_QKV, E8M0>;
-  constexpr int STAGES = L::STAGES, TM = PAIR ? P_TM : BM, CTAS = PAIR ? 2 : 1;
+  using L = Layout<PAIR, EPI == RA_EPI_QKV>;
+  constexpr int TM = PAIR ? P_TM : BM, CTAS = PAIR ? 2 : 1;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
-  uint64_t* full = reinterpret_cast<uint64_t*>(smem + L::OFF_BAR);
-  uint64_t* empty = full + STAGES;
-  uint64_t* tfull = full + 2 * STAGES;
-  uint64_t* tempty = tfull + 2;
-  uint64_t* drain = tfull + 4;
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + L::OFF_MISC);
-  volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + L::OFF_MISC + 4);
+  uint8_t* rest = smem + p.stages * L::STAGE_BYTES;
+  uint64_t* full = reinterpret_cast<uint64_t*>(rest + L::OFF_BAR);
+  uint64_t* empty = full + MAX_STAGES;
+  uint64_t* tfull = empty + MAX_STAGES;
+  uint64_t* tempty = tfull + MAX_ACCS;
+  uint64_t* drain = tempty + MAX_ACCS;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(rest + L::OFF_MISC);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(rest + L::OFF_MISC + 4);
   const int warp = same(int(threadIdx.x >> 5)), lane = threadIdx.x & 31;
   const int rank = PAIR ? same(int(cluster_rank())) : 0;
   const uint32_t t0 = blockIdx.x / CTAS, step = gridDim.x / CTAS;
   if (threadIdx.x == 0) {
-    for (int s = 0; s < STAGES; ++s) {
+    for (int s = 0; s < p.stages; ++s) {
       mbar_init(full + s, 1);
       mbar_init(empty + s, 1);
     }
-    for (int b = 0; b < 2; ++b) {
+    for (int b = 0; b < MAX_ACCS; ++b) {
       mbar_init(tfull + b, 1);
-      mbar_init(tempty + b, CTAS * EPI4_WARPS);
+      mbar_init(tempty + b, uint32_t(CTAS * 4 * p.units));
     }
     mbar_init(drain, 1);
     *abort_flag = 0;
@@ -659,13 +685,13 @@ __global__ void __launch_bounds__(THREADS4, 1) gemm4_kernel(const __grid_constan
       }
     pdl_wait();
     const uint32_t full0 = PAIR ? mapa_shared(smem_u32(full), 0) : smem_u32(full);  // a pair's are rank 0's
-    Ring<STAGES> in;
-    bool ok = true;
+    Ring in;
     Tiles<TM, EPI> tiles;
     Tile tl;
+    bool ok = true;
     for (uint32_t by = t0; ok && warp_tile(p, tiles, by, tl); by = step) {
       for (int kb = 0; kb < p.kblocks; ++kb) {
-        if (loads >= STAGES && !(ok = warp_wait(empty + in.st, in.ph ^ 1, ctl))) break;
+        if (loads >= p.stages && !(ok = warp_wait(empty + in.st, in.ph ^ 1, ctl))) break;
         const uint32_t stage = smem_u32(smem) + in.st * L::STAGE_BYTES, bar = full0 + 8u * in.st;
         if (rank == 0 && elect_one()) mbar_arrive_expect_tx(full + in.st, CTAS * p.stage_tx);
         __syncwarp();
@@ -674,31 +700,31 @@ __global__ void __launch_bounds__(THREADS4, 1) gemm4_kernel(const __grid_constan
         tma_load_one<PAIR>(stage + L::OFF_SF, &p.tm_sa[tl.seg], bar, 0, kb * p.groups, tl.m0 / 128 + rank, tl.s);
         tma_load_one<PAIR>(stage + L::OFF_SF + SA_BYTES, &p.tm_sw[tl.seg], bar, 0, kb * p.groups, tl.n0 / 128, 0);
         ++loads;
-        in.next();
+        in.next(p);
       }
     }
   } else if (warp == 1) {
     if (rank == 0) {
       // -------------------------------------------------------------- MMA issuer (a converged warp)
       const uint32_t idesc = idesc_mx4(TM, p.bn, E8M0);
-      const uint32_t s0 = smem_u32(smem) >> 4, sf0 = tmem + uint32_t(2 * p.bn);
-      int i = 0;
-      Ring<STAGES> in;  // stages as they are filled
-      uint32_t filled = 0;
-      Scales<STAGES> sf(p);
-      bool ok = true;
+      const uint32_t s0 = smem_u32(smem) >> 4, sf0 = tmem + uint32_t(p.accs * p.bn);
+      int i = 0, buf = 0;   // tiles so far, the next one's accumulator
+      uint32_t ph = 1;      // of its release
+      uint32_t freed = 0;   // which was asked for early
+      Ring in;              // stages as they are filled
+      uint32_t filled = 0;  // asked for early
+      Scales sf(p);
       Tiles<TM, EPI> tiles;
       Tile tl;
+      bool ok = true;
       for (uint32_t by = t0; ok && warp_tile(p, tiles, by, tl); by = step) {
-        const int buf = i & 1, use = i >> 1;
-        if (use > 0 && !(ok = warp_wait<PAIR>(tempty + buf, uint32_t((use - 1) & 1), ctl))) break;
-        tc_fence_after();
+        if (i >= p.accs && !(ok = warp_wait<PAIR>(freed, tempty + buf, ph, ctl))) break;
         const uint32_t sw0 = sf0 + (E8M0 ? 8u : 16u) + (uint32_t(tl.n0 & 64) >> 5);
         for (int kb = 0; kb < p.kblocks; ++kb) {
           if (!(ok = warp_wait(filled, full + in.st, in.ph, ctl) && sf.free(empty, ctl))) break;
           tc_fence_after();
-          Ring<STAGES> next = in;
-          next.next();
+          Ring next = in;
+          next.next(p);
           filled = peek(full + next.st, next.ph);
           issue_stage<L, E8M0>(p, s0 + uint32_t(in.st * (L::STAGE_BYTES / 16)), sf0 + sf.col, sw0 + sf.col,
                                tmem + uint32_t(buf * p.bn), idesc, ksteps_of(p, kb), kb == 0, smem_u32(empty + in.st));
@@ -709,43 +735,64 @@ __global__ void __launch_bounds__(THREADS4, 1) gemm4_kernel(const __grid_constan
         if (!ok) break;
         commit_one<PAIR>(tfull + buf);
         ++i;
+        if (++buf == p.accs) {
+          buf = 0;
+          ph ^= 1;
+        }
+        freed = peek<PAIR>(tempty + buf, ph);
       }
     }
   } else {
     // ---------------------------------------------------------------- epilogue
     const int quarter = warp & 3;
     Epi4 w;
-    w.unit = (warp - 2) >> 2;
-    w.turn = smem + L::OFF_TURN + (warp - 2) * TURN_BYTES;
-    w.vec0 = reinterpret_cast<float*>(smem + L::OFF_VEC + (warp - 2) * VEC_BYTES);
+    const int way = (warp - 2) >> 2;
+    w.turn = rest + L::OFF_TURN + (warp - 2) * TURN_BYTES;
+    w.vec0 = reinterpret_cast<float*>(rest + (warp - 2) * VEC_BYTES);
     w.vec1 = w.vec0 + UNIT;
-    float* sums = reinterpret_cast<float*>(smem + L::OFF_SUMS) + quarter * (128 / 32) * 32;
+    float* sums = reinterpret_cast<float*>(rest + L::OFF_SUMS) + quarter * SUMS;
     const uint32_t tempty0 = PAIR ? mapa_shared(smem_u32(tempty), 0) : 0u;
-    int i = 0;
+    int turn = 0;    // the tile's number modulo three
+    int unit = way;  // the tile's unit whose turn is this warp's; behind the last one: none
+    int buf = 0;     // the tile's accumulator
+    uint32_t ph = 0;
+    bool ok = true;
     Tiles<TM, EPI> tiles;
     Tile tl;
+    // The phase before the one that a warp waits for has ended: with two units to a tile it has taken one
+    // of the two tiles before; with one it takes every third tile, whose accumulator is always the same.
     for (uint32_t by = t0; tiles.on(p, by, tl); by = step) {
-      const int buf = i & 1, use = i >> 1;
-      w.row0 = tl.m0 + rank * 128 + quarter * 32;
-      w.nrow = min(32, p.rows[tl.seg] - w.row0);
-      w.acc = tmem + (uint32_t(quarter * 32) << 16) + uint32_t(buf * p.bn);
-      if (!epilogue4<EPI, D>(
-              p, tl, w, sums,
-              [&] {
-                const bool ok = __all_sync(0xffffffffu, mbar_wait(tfull + buf, uint32_t(use & 1), ctl));
-                tc_fence_after();
-                return ok;
-              },
-              [&] {
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) {
-                  if (rank == 0) mbar_arrive(tempty + buf);
-                  else mbar_arrive_remote_relaxed(tempty0 + 8u * buf);
-                }
-              }))
-        break;
-      ++i;
+      if (unit < p.units) {
+        w.unit = unit;
+        w.row0 = tl.m0 + rank * 128 + quarter * 32;
+        w.nrow = min(32, p.rows[tl.seg] - w.row0);
+        w.acc = tmem + (uint32_t(quarter * 32) << 16) + uint32_t(buf * p.bn);
+        ok = epilogue4<EPI, D>(
+            p, tl, w, sums, turn,
+            [&] {
+              const bool there = ok && __all_sync(0xffffffffu, mbar_wait(tfull + buf, ph, ctl));
+              tc_fence_after();
+              return there;
+            },
+            [&] {
+              tc_fence_before();
+              __syncwarp();
+              if (lane == 0) {
+                if (rank == 0) mbar_arrive(tempty + buf);
+                else mbar_arrive_remote_relaxed(tempty0 + 8u * buf);
+              }
+            });
+        // Where two warps meet at a barrier, one that gave up comes there for all its tiles: the other one
+        // would wait for ever.
+        if (!ok && !(EPI == RA_EPI_QKV && D == 128)) break;
+      }
+      unit -= p.units;
+      if (unit < 0) unit += WAYS;
+      if (++turn == WAYS) turn = 0;
+      if (++buf == p.accs) {
+        buf = 0;
+        ph ^= 1;
+      }
     }
   }
   tc_fence_before();
@@ -756,8 +803,8 @@ __global__ void __launch_bounds__(THREADS4, 1) gemm4_kernel(const __grid_constan
   if (*abort_flag) {
     if (warp == 0 && lane == 0 && rank == 0) {
       // a pair's full barriers count both CTAs' bytes of every phase that rank 0 armed
-      for (int st = 0; st < STAGES; ++st) {
-        const int64_t n_s = (loads > st) ? (loads - st + STAGES - 1) / STAGES : 0;
+      for (int st = 0; st < p.stages; ++st) {
+        const int64_t n_s = (loads > st) ? (loads - st + p.stages - 1) / p.stages : 0;
         if (n_s > 0) mbar_wait_drain(full + st, uint32_t((n_s - 1) & 1), p.budget_ns);
       }
     }
@@ -794,27 +841,22 @@ Kernels pick(int epi, int d) {
   }
 }
 
-template <bool E8M0>
-constexpr int smem_of(bool pair, bool qkv) {
-  return pair ? (qkv ? Layout<true, true, E8M0>::SMEM_ALLOC : Layout<true, false, E8M0>::SMEM_ALLOC)
-              : (qkv ? Layout<false, true, E8M0>::SMEM_ALLOC : Layout<false, false, E8M0>::SMEM_ALLOC);
-}
-
 struct Plan {
   bool pair;
-  int bn;
+  int bn, stages;
 };
 
-// The cheapest cut by a model of the call's time (microseconds), from one and four whole rounds of
-// tiles at K = 256 to 8192 (each within 8 %): a round takes what its stages take, or its
-// epilogue, and 0.3 between tiles. Few tiles: 152 single CTAs of narrow tiles beat 76 pairs, whose
-// set-up takes longer too.
+// The cheapest cut by a model of the call's time (microseconds), fitted to one, four and nine whole rounds of
+// tiles at K = 256 to 4096 of every cut, format and epilogue (rms error 5.5 %): a round takes what its
+// stages or its epilogue take, whichever is longer, and some of the other. Few tiles: 152 single
+// CTAs of narrow tiles beat 76 pairs, whose set-up takes longer too.
 Plan make_plan(const ra_gemm4_args& a, int sms) {
-  Plan best{false, 64};
+  Plan best{false, 64, FEW_STAGES};
   double best_us = 1e30;
   const double k = a.K / 1024.0;
-  const double epilogue = a.epilogue == RA_EPI_STORE ? 0.0057 : a.epilogue == RA_EPI_RESID ? 0.008
-                          : a.epilogue == RA_EPI_GELU ? 0.0115 : 0.020;  // of a tile, per column
+  const bool e4m3 = a.format == RA_Q4_E4M3;
+  const double epilogue = a.epilogue == RA_EPI_STORE ? 0.0047 : a.epilogue == RA_EPI_RESID ? 0.0116
+                          : a.epilogue == RA_EPI_GELU ? 0.0076 : 0.019;  // of a tile, per column
   for (int pair = 0; pair < 2; ++pair) {
     if ((a.tile_mode == 1 && pair) || (a.tile_mode == 2 && !pair) || (pair && sms < 2)) continue;
     const int tm = pair ? P_TM : BM, slots = pair ? sms / 2 : sms;
@@ -827,14 +869,17 @@ Plan make_plan(const ra_gemm4_args& a, int sms) {
         all += t;
         if (!a.seg[g].lin.gated) open += t;
       }
-      const double stages = k * (pair ? (bn == 192 ? 1.02 : 0.77 + 0.0006 * bn) : 0.56 + 0.002 * bn);
-      const double round = (stages > epilogue * bn ? stages : epilogue * bn) + 0.3;
-      const double fixed = pair ? 4.2 + 0.0075 * bn : 3.3;
+      const double stages = k * (bn == 192 ? (e4m3 ? 1.18 : 1.0)
+                                           : (pair ? 0.89 : bn == 128 ? 0.84 : 0.65) * (e4m3 ? 1.086 : 1.0)) + 0.16;
+      const double ends = epilogue * bn * (!pair ? 1.0 : a.epilogue == RA_EPI_QKV ? 0.87 : 1.06);
+      const double more = stages > ends ? stages : ends, less = stages > ends ? ends : stages;
+      const double round = more + 0.49 * less * less / more;
+      const double fixed = pair ? 4.0 + 0.0032 * bn : 3.7;
       double us = fixed + round * double((all + slots - 1) / slots);
       if (open > 0 && open < all) us += fixed + round * double((open + slots - 1) / slots);
       if (us < best_us) {
         best_us = us;
-        best = Plan{pair != 0, bn};
+        best = Plan{pair != 0, bn, pair && us > LONG_CALL ? MAX_STAGES : FEW_STAGES};
       }
     }
   }
@@ -900,10 +945,12 @@ ra_status run(const char* who, const ra_gemm4_args& a, cudaStream_t st) {
   p.bn = plan.bn;
   p.w_tiles = plan.bn > 128 ? 2 : 1;
   p.sf_cols = scale_cols(p.groups, p.w_tiles);
-  p.sf_bufs = (TMEM_COLS - 2 * plan.bn) / p.sf_cols;
   const bool qkv = a.epilogue == RA_EPI_QKV;
-  const int stages = stages_of(pair, p.e8m0);
-  if (p.sf_bufs > stages) p.sf_bufs = stages;
+  p.stages = plan.stages;
+  p.units = plan.bn / UNIT;
+  p.accs = MAX_ACCS * plan.bn + p.stages * p.sf_cols <= TMEM_COLS ? MAX_ACCS : 2;
+  p.sf_bufs = (TMEM_COLS - p.accs * plan.bn) / p.sf_cols;
+  if (p.sf_bufs > p.stages) p.sf_bufs = p.stages;
   p.stage_tx = A_BYTES + (pair ? plan.bn / 2 : plan.bn) * (CHUNK / 2) + p.groups * 512 * (1 + p.w_tiles);
   const int64_t cols = (a.N + plan.bn - 1) / plan.bn;
   p.cols = int32_t(cols);
@@ -1010,9 +1057,13 @@ ra_status run(const char* who, const ra_gemm4_args& a, cudaStream_t st) {
   const Kernels kn = p.e8m0 ? pick<true>(a.epilogue, a.d) : pick<false>(a.epilogue, a.d);
   const int64_t slots = pair ? (sms / 2 > 0 ? sms / 2 : 1) : sms;
   note_launch(pair ? "CTA pairs, %d columns" : "single CTAs, %d columns", plan.bn);
-  const int smem = p.e8m0 ? smem_of<true>(pair, qkv) : smem_of<false>(pair, qkv);
+  const auto smem = [&](int stages) {
+    return pair ? (qkv ? Layout<true, true>::smem(stages) : Layout<true, false>::smem(stages))
+                : (qkv ? Layout<false, true>::smem(stages) : Layout<false, false>::smem(stages));
+  };
   const int64_t groups = tiles < slots ? tiles : slots;
-  return launch(who, p, pair ? kn.pair : kn.single, smem, pair ? 2 * groups : groups, pair ? 2 : 1, st, THREADS4);
+  return launch(who, p, pair ? kn.pair : kn.single, smem(p.stages), pair ? 2 * groups : groups, pair ? 2 : 1, st, THREADS4,
+                smem(pair ? MAX_STAGES : FEW_STAGES));
 }
 
 }  // namespace gemm4

@@ -432,8 +432,9 @@ inline bool aligned16(const void* ptr) { return (reinterpret_cast<uintptr_t>(ptr
 // Launches `ctas` CTAs in clusters of cs.
 template <class P>
 ra_status launch(const char* who, const P& p, void (*fn)(P), int smem, int64_t ctas, int cs, cudaStream_t st,
-                 int threads = THREADS) {
-  const ra_status as = ensure_dynamic_smem(reinterpret_cast<const void*>(fn), smem, who);
+                 int threads = THREADS, int most_smem = 0) {
+  const ra_status as =
+      ensure_dynamic_smem(reinterpret_cast<const void*>(fn), most_smem > smem ? most_smem : smem, who);
   if (as != RA_OK) return as;
   cudaLaunchAttribute attr[2];
   attr[0] = pdl_attribute();

@@ -347,6 +347,65 @@ def test_qkv(cuda_ok, H, d, fmt, tile_mode):
                 within(seg[z][s], ref[s], tol[s])
 
 
+@pytest.mark.parametrize("fmt", [E4M3, E8M0])
+@pytest.mark.parametrize("epilogue", [STORE, GELU, RESID, QKV])
+@pytest.mark.parametrize("tile_mode, N, d", [(1, 64, 0), (1, 128, 0), (1, 320, 0), (2, 64, 0), (2, 128, 0), (2, 192, 0), (2, 448, 0),
+                                             (1, 768, 64), (2, 768, 64), (1, 768, 128), (2, 768, 128)])
+def test_many_tiles(cuda_ok, fmt, epilogue, tile_mode, N, d):
+    """Several tiles to a CTA, with one to three units of columns: every row has what the same row has in a
+    call of one tile to a CTA (the sums' order is the same), whose values other tests check."""
+    if (epilogue == QKV) != (d > 0):
+        pytest.skip("widths of heads are QKV's")
+    a, g = api(), torch.Generator().manual_seed(N + epilogue)
+    few, rows, K = 301, 128 * 152 * 3 + 77, 192
+    base, w = bf((1, few, K), g), bf((N, K), g) * 0.1
+    wc, ws = (t[0] for t in quantised(w[None].to(torch.bfloat16), fmt))
+    at = (torch.arange(rows, device="cuda") * 7) % few
+    resid, gate, bias = bf((1, few, N), g), torch.randn((1, N), generator=g).cuda(), torch.randn(N, generator=g).cuda()
+
+    def run(x, res):
+        codes, scales = quantised(x, fmt)
+        n = x.shape[1]
+        seg = {"a": codes, "a_scales": scales, "w": wc, "w_scales": ws, "bias": bias}
+        kw = {}
+        if epilogue == QKV:
+            H = N // 3 // d
+            outs = [torch.empty((1, H, n, d), dtype=torch.bfloat16, device="cuda") for _ in range(3)]
+            norm = torch.linspace(0.5, 1.5, d, device="cuda")
+            seg.update(q=outs[0], k=outs[1], v=outs[2], q_norm=norm, k_norm=norm, pos_offset=0)
+            kw = dict(rope=a.rope_table(5, d)[4:].expand(n, -1, -1).contiguous(), H=H, d=d)
+        else:
+            outs = [torch.empty((1, n, N), dtype=torch.bfloat16, device="cuda")]
+            seg["out"] = outs[0]
+            if epilogue == RESID:
+                seg.update(resid=res, gate=gate)
+        a.refadapt_gemm4([seg], N, K, epilogue, fmt, tile_mode=tile_mode, **kw)
+        return torch.cat(outs, 1) if epilogue == QKV else outs[0]
+
+    want = run(base, resid)
+    got = run(base[:, at].contiguous(), resid[:, at].contiguous())
+    assert torch.equal(got, want[..., at, :])
+
+
+@pytest.mark.parametrize("fmt", [E4M3, E8M0])
+def test_long_call_after_short(cuda_ok, fmt):
+    """Long calls keep more of their operands on the way than short ones do, which came first here."""
+    a, g = api(), torch.Generator().manual_seed(41)
+    rows, N, K = 8192, 8192, 8192
+    x, w = bf((1, rows, K), g), bf((1, N, K), g)
+    wc, ws = (t[0] for t in quantised(w, fmt))
+    outs = []
+    for n in (256, rows):
+        codes, scales = quantised(x[:, :n].contiguous(), fmt)
+        out = torch.empty((1, n, N), dtype=torch.bfloat16, device="cuda")
+        a.refadapt_gemm4([{"a": codes, "a_scales": scales, "w": wc, "w_scales": ws, "out": out}], N, K, STORE, fmt, tile_mode=2)
+        outs.append(out)
+    assert torch.equal(outs[1][:, :256], outs[0])
+    a.refadapt_gemm4([{"a": codes[:, :256].contiguous(), "a_scales": scales[:, :2].contiguous(), "w": wc, "w_scales": ws,
+                       "out": outs[0].zero_()}], N, K, STORE, fmt, tile_mode=2)
+    assert torch.equal(outs[1][:, :256], outs[0])
+
+
 def test_product_of_no_rows_and_nan_rows(cuda_ok):
     """A segment without rows is skipped; a row with a NaN scale is NaN and no other one."""
     g = torch.Generator().manual_seed(23)
