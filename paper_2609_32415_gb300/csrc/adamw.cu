@@ -71,23 +71,32 @@ __device__ __forceinline__ int tensor_of(const T* t, int n, uint32_t chunk) {
   return lo;
 }
 
+// The CTA's sum of what the first lanes of its warps have, in thread 0.
 __device__ __forceinline__ double block_sum(double v, double* warps) {
-#pragma unroll
-  for (int d = 16; d > 0; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+  static_assert(THREADS / 32 == 8, "eight warps");
   if ((threadIdx.x & 31) == 0) warps[threadIdx.x >> 5] = v;
   __syncthreads();
   double s = 0;
+  if (threadIdx.x < 8) {
+    s = warps[threadIdx.x];
 #pragma unroll
-  for (int i = 0; i < THREADS / 32; ++i) s += warps[i];
+    for (int d = 4; d > 0; d >>= 1) s += __shfl_xor_sync(0xffu, s, d);
+  }
   __syncthreads();
   return s;
 }
+__device__ __forceinline__ float warp_sum(float v) {
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+  return v;
+}
 
-// Sums in an order that the sizes alone decide: a thread's squares of a chunk in fp32 (32 of
-// them), its chunks, the CTA's threads and the CTAs in fp64; the CTA that takes the last
-// ticket of the call adds the CTAs' sums up.
+// Sums in an order that the sizes alone decide: a warp's squares of a chunk in fp32 (16 in a row, two of these
+// a thread, 32 threads), its chunks, the CTA's warps and the CTAs in fp64; the CTA that takes the
+// last ticket of the call adds the CTAs' sums up. This GPU adds two fp64 numbers a clock and SM: trees of
+// all threads' in fp64 took 8 us beside the loads (21 M bf16 gradients: 16.7 us, now 8.8; 317 M: 94 us, 6.7 TB/s).
 template <int MAX>
-__global__ void __launch_bounds__(THREADS) norm_kernel(const __grid_constant__ NormParams<MAX> p) {
+__global__ void __launch_bounds__(THREADS, 8) norm_kernel(const __grid_constant__ NormParams<MAX> p) {
   __shared__ double warps[THREADS / 32];
   __shared__ bool last;
   pdl_wait();
@@ -97,7 +106,7 @@ __global__ void __launch_bounds__(THREADS) norm_kernel(const __grid_constant__ N
     const NormTensor& t = p.t[tensor_of(p.t, p.n_tensors, c)];
     const int64_t i0 = int64_t(c - t.first) * CHUNK;
     const int n = int(min(int64_t(CHUNK), t.n - i0));
-    float s = 0.f;
+    uint64_t s = f2_pack(0.f, 0.f);  // two sums
     if (t.bf16) {
       const __nv_bfloat16* g = static_cast<const __nv_bfloat16*>(t.g) + i0;
       if (n == CHUNK && (reinterpret_cast<uintptr_t>(g) & 15) == 0) {
@@ -110,36 +119,43 @@ __global__ void __launch_bounds__(THREADS) norm_kernel(const __grid_constant__ N
           const uint32_t w[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const float a = __uint_as_float(w[i] << 16), b = __uint_as_float(w[i] & 0xffff0000u);
-            s = fmaf(a, a, s);
-            s = fmaf(b, b, s);
+            const uint64_t a = bf2_unpack(w[i]);
+            s = f2_fma(a, a, s);
           }
         }
       } else {
         for (int i = threadIdx.x; i < n; i += THREADS) {
-          const float a = __bfloat162float(g[i]);
-          s = fmaf(a, a, s);
+          const uint64_t a = f2_pack(__bfloat162float(g[i]), 0.f);
+          s = f2_fma(a, a, s);
         }
       }
     } else {
       const float* g = static_cast<const float*>(t.g) + i0;
       if (n == CHUNK && (reinterpret_cast<uintptr_t>(g) & 15) == 0) {
-        constexpr int PIECES = CHUNK / (4 * THREADS);
-        float4 v[PIECES];
+        constexpr int PIECES = CHUNK / (8 * THREADS);
+#pragma unroll 1
+        for (int h = 0; h < 2; ++h) {
+          float4 v[PIECES];
 #pragma unroll
-        for (int k = 0; k < PIECES; ++k) v[k] = reinterpret_cast<const float4*>(g)[threadIdx.x + k * THREADS];
+          for (int k = 0; k < PIECES; ++k)
+            v[k] = reinterpret_cast<const float4*>(g)[threadIdx.x + (h * PIECES + k) * THREADS];
 #pragma unroll
-        for (int k = 0; k < PIECES; ++k) {
-          s = fmaf(v[k].x, v[k].x, s);
-          s = fmaf(v[k].y, v[k].y, s);
-          s = fmaf(v[k].z, v[k].z, s);
-          s = fmaf(v[k].w, v[k].w, s);
+          for (int k = 0; k < PIECES; ++k) {
+            const uint64_t a = f2_pack(v[k].x, v[k].y), b = f2_pack(v[k].z, v[k].w);
+            s = f2_fma(a, a, s);
+            s = f2_fma(b, b, s);
+          }
         }
       } else {
-        for (int i = threadIdx.x; i < n; i += THREADS) s = fmaf(g[i], g[i], s);
+        for (int i = threadIdx.x; i < n; i += THREADS) {
+          const uint64_t a = f2_pack(g[i], 0.f);
+          s = f2_fma(a, a, s);
+        }
       }
     }
-    sum += double(s);
+    float s0, s1;
+    f2_unpack(s, s0, s1);
+    sum += double(warp_sum(s0 + s1));
   }
   sum = block_sum(sum, warps);
   if (threadIdx.x == 0) {
@@ -152,11 +168,14 @@ __global__ void __launch_bounds__(THREADS) norm_kernel(const __grid_constant__ N
   __threadfence();
   sum = 0;
   for (int i = threadIdx.x; i < p.total; i += THREADS) sum += __ldcg(p.partial + i);
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
   sum = block_sum(sum, warps);
   if (threadIdx.x == 0) {
-    const double norm = sqrt(sum);
-    p.out[0] = float(norm);
-    p.out[1] = !isfinite(float(norm)) ? __int_as_float(0x7fffffff) : norm > double(p.max_norm) ? float(double(p.max_norm) / norm) : 1.f;
+    // root and quotient in fp32 (half a unit of the result each) wherever the sum is far from its ends
+    const float norm = sum > 1e-30 && sum < 1e30 ? sqrtf(float(sum)) : float(sqrt(sum));
+    p.out[0] = norm;
+    p.out[1] = !isfinite(norm) ? __int_as_float(0x7fffffff) : norm > p.max_norm ? p.max_norm / norm : 1.f;
     *p.ticket = 0;
   }
 }
