@@ -90,6 +90,8 @@ struct Params4 : Params {
   int32_t sf_cols, sf_bufs;          // TMEM columns of a stage's scales, buffers of them
   int32_t units, accs;               // of 64 columns in a tile; accumulators
   int32_t stages;                    // of the ring
+  int32_t n[3], k[3], kb[3], nt[3];  // by segment: N, K, stages of a tile, column tiles
+  int32_t rounds, light;             // Tiles
   uint32_t stage_tx;                 // bytes of a stage that one CTA loads
   int32_t wide[3];                   // rows of the epilogue's tensors start on 32 bytes
   CUtensorMap tm_sa[3], tm_sw[3];
@@ -215,8 +217,6 @@ __device__ __forceinline__ void commit_one(uint64_t* bar) {
         : "memory");
 }
 
-__device__ __forceinline__ int ksteps_of(const Params4& p, int kb) { return min(CHUNK, p.K - kb * CHUNK) / 64; }
-
 __device__ __forceinline__ bool elect_one() {
   uint32_t one;
   asm volatile("{\n\t.reg .pred e;\n\telect.sync _|e, 0xffffffff;\n\tselp.u32 %0, 1, 0, e;\n\t}" : "=r"(one));
@@ -264,22 +264,29 @@ __device__ __forceinline__ int same(int v) { return __shfl_sync(0xffffffffu, v, 
 // Walk's order of the tiles (gemm_body.cuh) by counting on from the tile before, without
 // divisions but in the last band: the issuer, whose stages take about as long to issue as their
 // MMAs run, spent 0.6 us a tile on those.
+// Two products in one launch are two segments, the one of the longer K first: where its tiles leave some CTAs
+// one more than others, these (the first `light`) take no tile after `rounds` rounds of all, which
+// is about when the others have taken their share of the rest.
 template <int TM, int EPI>
 struct Tiles {
   int g = 0, s = 0, cols = -1;  // the piece: a segment's sample, and its column tiles
   int band = 0;                 // first row tile of the band of GROUP_M
   uint32_t idx = 0;             // the tile's number within the band
-  __device__ __forceinline__ int piece_cols(const Params& p) const {
+  int taken = 0;
+  __device__ __forceinline__ int piece_cols(const Params4& p) const {
     if (p.m_tiles[g] == 0) return 0;
+    if (!p.gated[g]) return p.nt[g];
     Walk<TM, EPI> w;
     w.g = g;
     w.s = s;
     return w.piece_cols(p);
   }
-  // `by` tiles on (the first call: from the first one); false past the last one.
-  __device__ __forceinline__ bool on(const Params& p, uint32_t by, Tile& r) {
+  // The next tile of the CTA (or pair) t0 of `step`; false past the last one.
+  __device__ __forceinline__ bool on(const Params4& p, uint32_t t0, uint32_t step, Tile& r) {
     if (cols < 0) cols = piece_cols(p);
-    idx += by;
+    if (taken >= p.rounds && t0 < uint32_t(p.light)) return false;
+    idx += taken == 0 ? t0 : taken < p.rounds ? step : step - uint32_t(p.light);
+    ++taken;
     uint32_t rows = uint32_t(min(GROUP_M, p.m_tiles[g] - band));
     while (idx >= rows * uint32_t(cols)) {
       idx -= rows * uint32_t(cols);
@@ -304,9 +311,10 @@ struct Tiles {
 };
 // The same for a converged warp, whose values are then known to be the same in every lane.
 template <int TM, int EPI>
-__device__ __forceinline__ bool warp_tile(const Params& p, Tiles<TM, EPI>& tiles, uint32_t by, Tile& tl) {
+__device__ __forceinline__ bool warp_tile(const Params4& p, Tiles<TM, EPI>& tiles, uint32_t t0, uint32_t step,
+                                          Tile& tl) {
   Tile r{0, 0, 0, 0};
-  const int more = same(tiles.on(p, by, r));
+  const int more = same(tiles.on(p, t0, step, r));
   tl = Tile{same(r.seg), same(r.s), same(r.m0), same(r.n0)};
   return more != 0;
 }
@@ -436,7 +444,7 @@ __device__ __forceinline__ bool epilogue_linear4(const Params4& p, const Tile& t
                                                  Release release) {
   const Seg& sg = p.seg[tl.seg];
   const int lane = threadIdx.x & 31, n0 = tl.n0 + UNIT * w.unit;
-  const bool on = w.nrow > 0 && n0 < p.N;  // N is a multiple of 64
+  const bool on = w.nrow > 0 && n0 < p.n[tl.seg];  // N is a multiple of 64
   const bool mine = lane < w.nrow, wide = p.wide[tl.seg];
   uint32_t r[2][2][8];
   const char* res = nullptr;
@@ -689,8 +697,9 @@ __global__ void __launch_bounds__(THREADS4, 1) gemm4_kernel(const __grid_constan
     Tiles<TM, EPI> tiles;
     Tile tl;
     bool ok = true;
-    for (uint32_t by = t0; ok && warp_tile(p, tiles, by, tl); by = step) {
-      for (int kb = 0; kb < p.kblocks; ++kb) {
+    while (ok && warp_tile(p, tiles, t0, step, tl)) {
+      const int kblocks = same(p.kb[tl.seg]);
+      for (int kb = 0; kb < kblocks; ++kb) {
         if (loads >= p.stages && !(ok = warp_wait(empty + in.st, in.ph ^ 1, ctl))) break;
         const uint32_t stage = smem_u32(smem) + in.st * L::STAGE_BYTES, bar = full0 + 8u * in.st;
         if (rank == 0 && elect_one()) mbar_arrive_expect_tx(full + in.st, CTAS * p.stage_tx);
@@ -717,17 +726,18 @@ __global__ void __launch_bounds__(THREADS4, 1) gemm4_kernel(const __grid_constan
       Tiles<TM, EPI> tiles;
       Tile tl;
       bool ok = true;
-      for (uint32_t by = t0; ok && warp_tile(p, tiles, by, tl); by = step) {
+      while (ok && warp_tile(p, tiles, t0, step, tl)) {
         if (i >= p.accs && !(ok = warp_wait<PAIR>(freed, tempty + buf, ph, ctl))) break;
         const uint32_t sw0 = sf0 + (E8M0 ? 8u : 16u) + (uint32_t(tl.n0 & 64) >> 5);
-        for (int kb = 0; kb < p.kblocks; ++kb) {
+        const int kblocks = same(p.kb[tl.seg]), steps = same(p.k[tl.seg]) / 64;  // of 64 columns
+        for (int kb = 0; kb < kblocks; ++kb) {
           if (!(ok = warp_wait(filled, full + in.st, in.ph, ctl) && sf.free(empty, ctl))) break;
           tc_fence_after();
           Ring next = in;
           next.next(p);
           filled = peek(full + next.st, next.ph);
           issue_stage<L, E8M0>(p, s0 + uint32_t(in.st * (L::STAGE_BYTES / 16)), sf0 + sf.col, sw0 + sf.col,
-                               tmem + uint32_t(buf * p.bn), idesc, ksteps_of(p, kb), kb == 0, smem_u32(empty + in.st));
+                               tmem + uint32_t(buf * p.bn), idesc, min(CHUNK / 64, steps - kb * (CHUNK / 64)), kb == 0, smem_u32(empty + in.st));
           issued = true;
           in = next;
           sf.next(p);
@@ -761,7 +771,7 @@ __global__ void __launch_bounds__(THREADS4, 1) gemm4_kernel(const __grid_constan
     Tile tl;
     // The phase before the one that a warp waits for has ended: with two units to a tile it has taken one
     // of the two tiles before; with one it takes every third tile, whose accumulator is always the same.
-    for (uint32_t by = t0; tiles.on(p, by, tl); by = step) {
+    while (tiles.on(p, t0, step, tl)) {
       if (unit < p.units) {
         w.unit = unit;
         w.row0 = tl.m0 + rank * 128 + quarter * 32;
@@ -844,43 +854,72 @@ Kernels pick(int epi, int d) {
 struct Plan {
   bool pair;
   int bn, stages;
+  double us;
+  int32_t rounds, light;
 };
 
-// The cheapest cut by a model of the call's time (microseconds), fitted to one, four and nine whole rounds of
-// tiles at K = 256 to 4096 of every cut, format and epilogue (rms error 5.5 %): a round takes what its
-// stages or its epilogue take, whichever is longer, and some of the other. Few tiles: 152 single
-// CTAs of narrow tiles beat 76 pairs, whose set-up takes longer too.
-Plan make_plan(const ra_gemm4_args& a, int sms) {
-  Plan best{false, 64, FEW_STAGES};
-  double best_us = 1e30;
+// A cut's times (microseconds) by a model fitted to one, four and nine whole rounds of tiles at K = 256 to
+// 4096 of every cut, format and epilogue (rms error 5.5 %): a round takes what its stages or its
+// epilogue take, whichever is longer, and some of the other.
+double round_us(const ra_gemm4_args& a, bool pair, int bn) {
   const double k = a.K / 1024.0;
   const bool e4m3 = a.format == RA_Q4_E4M3;
   const double epilogue = a.epilogue == RA_EPI_STORE ? 0.0047 : a.epilogue == RA_EPI_RESID ? 0.0116
                           : a.epilogue == RA_EPI_GELU ? 0.0076 : 0.019;  // of a tile, per column
+  const double stages = k * (bn == 192 ? (e4m3 ? 1.18 : 1.0)
+                                       : (pair ? 0.89 : bn == 128 ? 0.84 : 0.65) * (e4m3 ? 1.086 : 1.0)) + 0.16;
+  const double ends = epilogue * bn * (!pair ? 1.0 : a.epilogue == RA_EPI_QKV ? 0.87 : 1.06);
+  const double more = stages > ends ? stages : ends, less = stages > ends ? ends : stages;
+  return more + 0.49 * less * less / more;
+}
+int64_t tiles_of(const ra_gemm4_args& a, int g, int tm, int bn) {
+  const int64_t rows = a.seg[g].lin.rows;
+  return rows > 0 ? int64_t(a.B) * ((rows + tm - 1) / tm) * ((a.N + bn - 1) / bn) : 0;
+}
+
+// The cheapest cut. Few tiles: 152 single CTAs of narrow tiles beat 76 pairs, whose set-up takes longer too.
+// `then`: a second product in the launch, of a K no longer than the first one's.
+Plan make_plan(const ra_gemm4_args& a, const ra_gemm4_args* then, int sms) {
+  Plan best{false, 64, FEW_STAGES, 1e30, INT32_MAX, 0};
   for (int pair = 0; pair < 2; ++pair) {
     if ((a.tile_mode == 1 && pair) || (a.tile_mode == 2 && !pair) || (pair && sms < 2)) continue;
     const int tm = pair ? P_TM : BM, slots = pair ? sms / 2 : sms;
     for (int bn = pair && a.epilogue != RA_EPI_QKV ? 192 : 128; bn >= 64; bn -= 64) {
       if (a.epilogue == RA_EPI_QKV && bn % a.d != 0) continue;
-      const int64_t cols = (a.N + bn - 1) / bn;
       int64_t all = 0, open = 0;  // tiles, and those of segments that are not gated
       for (int g = 0; g < a.n_seg; ++g) {
-        const int64_t t = a.seg[g].lin.rows > 0 ? int64_t(a.B) * ((a.seg[g].lin.rows + tm - 1) / tm) * cols : 0;
+        const int64_t t = tiles_of(a, g, tm, bn);
         all += t;
         if (!a.seg[g].lin.gated) open += t;
       }
-      const double stages = k * (bn == 192 ? (e4m3 ? 1.18 : 1.0)
-                                           : (pair ? 0.89 : bn == 128 ? 0.84 : 0.65) * (e4m3 ? 1.086 : 1.0)) + 0.16;
-      const double ends = epilogue * bn * (!pair ? 1.0 : a.epilogue == RA_EPI_QKV ? 0.87 : 1.06);
-      const double more = stages > ends ? stages : ends, less = stages > ends ? ends : stages;
-      const double round = more + 0.49 * less * less / more;
-      const double fixed = pair ? 4.0 + 0.0032 * bn : 3.7;
-      double us = fixed + round * double((all + slots - 1) / slots);
-      if (open > 0 && open < all) us += fixed + round * double((open + slots - 1) / slots);
-      if (us < best_us) {
-        best_us = us;
-        best = Plan{pair != 0, bn, pair && us > LONG_CALL ? MAX_STAGES : FEW_STAGES};
+      const double fixed = pair ? 4.0 + 0.0032 * bn : 3.7, round = round_us(a, pair, bn);
+      Plan one{pair != 0, bn, FEW_STAGES, fixed, INT32_MAX, 0};
+      if (!then) {
+        one.us += round * double((all + slots - 1) / slots);
+        if (open > 0 && open < all) one.us += fixed + round * double((open + slots - 1) / slots);
+      } else {
+        const int64_t total = all + tiles_of(*then, 0, tm, bn), ctas = total < slots ? total : slots;
+        const double second = round_us(*then, pair, bn);
+        // the first `light` CTAs have `most` tiles of the first product, the others one less
+        const int64_t most = (all + ctas - 1) / ctas, light = all % ctas, whole = (total + ctas - 1) / ctas;
+        const double even = double(most) * round + double(whole - most) * second;
+        const int64_t r = int64_t((double(total) - (round / second - 1) * double(ctas - light)) / double(ctas));
+        const int64_t rounds = r > most ? r : most, rest = total - rounds * ctas;
+        if (light > 0 && rest > 0) {
+          const double few = double(most) * round + double(rounds - most) * second;
+          const double many = double(most - 1) * round +
+                              double(rounds - most + 1 + (rest + ctas - light - 1) / (ctas - light)) * second;
+          if ((few > many ? few : many) < even) {
+            one.rounds = int32_t(rounds);
+            one.light = int32_t(light);
+          }
+          one.us += one.light ? (few > many ? few : many) : even;
+        } else {
+          one.us += even;
+        }
       }
+      if (pair && one.us > LONG_CALL) one.stages = MAX_STAGES;
+      if (one.us < best.us) best = one;
     }
   }
   return best;
@@ -893,8 +932,7 @@ bool encode_scales(CUtensorMap* tm, const void* scales, int K, int rows, int B, 
   return encode_words(tm, scales, 128, along, down, B, 512, 512 * along, 512 * along * down, groups, tiles);
 }
 
-// The checks that need no epilogue, and the launch. `who` names the entry point in errors.
-ra_status run(const char* who, const ra_gemm4_args& a, cudaStream_t st) {
+ra_status run(const char* who, const ra_gemm4_args& a, cudaStream_t st, const ra_gemm4_args* then) {
   if (a.B < 1 || a.n_seg < 1 || a.n_seg > 3 || a.K < 64 || a.K % 64 != 0 || a.N < 64 || a.N % 64 != 0) {
     set_error("%s: need B >= 1, 1 <= n_seg <= 3, N and K positive multiples of 64 (B=%d n_seg=%d N=%d K=%d)", who, a.B,
               a.n_seg, a.N, a.K);
@@ -914,11 +952,8 @@ ra_status run(const char* who, const ra_gemm4_args& a, cudaStream_t st) {
   }
   Params4 p;
   std::memset(static_cast<void*>(&p), 0, sizeof(p));
-  p.n_seg = a.n_seg;
+  p.n_seg = a.n_seg + (then ? 1 : 0);
   p.B = a.B;
-  p.N = a.N;
-  p.K = a.K;
-  p.kblocks = (a.K + CHUNK - 1) / CHUNK;
   p.mode = a.mode;
   p.err_word = a.err_word;
   p.budget_ns = wait_budget_ns();
@@ -939,7 +974,7 @@ ra_status run(const char* who, const ra_gemm4_args& a, cudaStream_t st) {
     p.rope_len = a.rope_len;
   }
   const int sms = num_sms();
-  const Plan plan = make_plan(a, sms);
+  const Plan plan = make_plan(a, then, sms);
   const bool pair = plan.pair;
   const int tm = pair ? P_TM : BM;
   p.bn = plan.bn;
@@ -952,14 +987,23 @@ ra_status run(const char* who, const ra_gemm4_args& a, cudaStream_t st) {
   p.sf_bufs = (TMEM_COLS - p.accs * plan.bn) / p.sf_cols;
   if (p.sf_bufs > p.stages) p.sf_bufs = p.stages;
   p.stage_tx = A_BYTES + (pair ? plan.bn / 2 : plan.bn) * (CHUNK / 2) + p.groups * 512 * (1 + p.w_tiles);
-  const int64_t cols = (a.N + plan.bn - 1) / plan.bn;
-  p.cols = int32_t(cols);
+  p.rounds = plan.rounds;
+  p.light = plan.light;
+  p.cols = (a.N + plan.bn - 1) / plan.bn;
   p.cols_q = p.C / plan.bn;
   int64_t tiles = 0;
   RowSpan out[9], in[21];
   int n_out = 0, n_in = 0;
-  for (int g = 0; g < a.n_seg; ++g) {
-    const ra_gemm_seg& s = a.seg[g].lin;
+  // Segment g: a's, behind them the second product's.
+  const auto call_of = [&](int g) -> const ra_gemm4_args& { return g < a.n_seg ? a : *then; };
+  const auto seg_of = [&](int g) -> const ra_gemm4_seg& { return g < a.n_seg ? a.seg[g] : then->seg[0]; };
+  for (int g = 0; g < p.n_seg; ++g) {
+    const ra_gemm_seg& s = seg_of(g).lin;
+    const int32_t N = call_of(g).N, K = call_of(g).K;
+    p.n[g] = N;
+    p.k[g] = K;
+    p.kb[g] = (K + CHUNK - 1) / CHUNK;
+    p.nt[g] = (N + plan.bn - 1) / plan.bn;
     if (s.rows < 0) {
       set_error("%s: seg %d rows < 0", who, g);
       return RA_EINVAL;
@@ -972,9 +1016,9 @@ ra_status run(const char* who, const ra_gemm4_args& a, cudaStream_t st) {
     p.m_tiles[g] = int32_t((int64_t(s.rows) + tm - 1) / tm);
     p.gated[g] = s.gated ? 1 : 0;
     if (s.rows == 0) continue;
-    const ra_gemm4_seg& q = a.seg[g];
+    const ra_gemm4_seg& q = seg_of(g);
     if (!s.a || !s.w || !q.a_scales || !q.w_scales || !aligned16(s.a) || !aligned16(s.w) || !aligned16(q.a_scales) ||
-        !aligned16(q.w_scales) || s.a_stride_r % 16 != 0 || s.a_stride_s % 16 != 0 || s.a_stride_r < a.K / 2 ||
+        !aligned16(q.w_scales) || s.a_stride_r % 16 != 0 || s.a_stride_s % 16 != 0 || s.a_stride_r < K / 2 ||
         s.a_stride_s < 0) {
       set_error("%s: seg %d: codes and scales of A and W must be 16-byte aligned, strides multiples of 16 bytes, "
                 "a_stride_r >= K / 2", who, g);
@@ -986,18 +1030,18 @@ ra_status run(const char* who, const ra_gemm4_args& a, cudaStream_t st) {
                 q.w_exponent);
       return RA_EINVAL;
     }
-    if (!fill_epilogue(who, a, g, s, p.seg[g])) return RA_EINVAL;
+    if (!fill_epilogue(who, call_of(g), g, s, p.seg[g])) return RA_EINVAL;
     auto on32 = [](const void* ptr, int64_t ss, int64_t sr, int64_t sh = 0) {  // strides in elements of 2 bytes
       return (reinterpret_cast<uintptr_t>(ptr) & 31u) == 0 && ss % 16 == 0 && sr % 16 == 0 && sh % 16 == 0;
     };
     const int e = q.a_exponent + q.w_exponent;
     p.seg[g].alpha = ldexpf(1.f, e);
-    const int64_t rows = s.rows, spans = (rows + 127) / 128 * ((a.K + 4 * block_of(a.format) - 1) / (4 * block_of(a.format)));
-    in[n_in++] = RowSpan{s.a, s.a_stride_s, s.a_stride_r, a.B, rows, a.K / 2};
+    const int64_t rows = s.rows, spans = (rows + 127) / 128 * ((K + 4 * block_of(a.format) - 1) / (4 * block_of(a.format)));
+    in[n_in++] = RowSpan{s.a, s.a_stride_s, s.a_stride_r, a.B, rows, K / 2};
     in[n_in++] = RowSpan{q.a_scales, spans * 512, 0, a.B, 1, spans * 512};
-    in[n_in++] = RowSpan{s.w, 0, a.K / 2, 1, a.N, a.K / 2};
-    in[n_in++] = RowSpan{q.w_scales, 0, 0, 1, 1, int64_t(refadapt_quant4_scales_size(a.N, a.K, a.format))};
-    if (s.bias) in[n_in++] = RowSpan{s.bias, 0, 0, 1, 1, int64_t(a.N) * 4};
+    in[n_in++] = RowSpan{s.w, 0, K / 2, 1, N, K / 2};
+    in[n_in++] = RowSpan{q.w_scales, 0, 0, 1, 1, int64_t(refadapt_quant4_scales_size(N, K, a.format))};
+    if (s.bias) in[n_in++] = RowSpan{s.bias, 0, 0, 1, 1, int64_t(N) * 4};
     if (a.epilogue == RA_EPI_QKV) {
       // the rows of the first head: outputs may interleave their heads
       p.wide[g] = 1;
@@ -1014,20 +1058,20 @@ ra_status run(const char* who, const ra_gemm4_args& a, cudaStream_t st) {
         set_error("%s: seg %d: out_stride_s must be positive", who, g);
         return RA_EINVAL;
       }
-      out[n_out++] = RowSpan{s.out, s.out_stride_s * 2, s.out_stride_r * 2, a.B, rows, int64_t(a.N) * 2};
+      out[n_out++] = RowSpan{s.out, s.out_stride_s * 2, s.out_stride_r * 2, a.B, rows, int64_t(N) * 2};
       p.wide[g] = on32(s.out, s.out_stride_s, s.out_stride_r) &&
                   (a.epilogue != RA_EPI_RESID || on32(s.resid, s.resid_stride_s, s.resid_stride_r));
       if (a.epilogue == RA_EPI_RESID) {
-        in[n_in++] = RowSpan{s.gate, s.gate_stride_s * 4, 0, a.B, 1, int64_t(a.N) * 4};
+        in[n_in++] = RowSpan{s.gate, s.gate_stride_s * 4, 0, a.B, 1, int64_t(N) * 4};
         if (s.resid != s.out || s.resid_stride_s != s.out_stride_s || s.resid_stride_r != s.out_stride_r)
-          in[n_in++] = RowSpan{s.resid, s.resid_stride_s * 2, s.resid_stride_r * 2, a.B, rows, int64_t(a.N) * 2};
+          in[n_in++] = RowSpan{s.resid, s.resid_stride_s * 2, s.resid_stride_r * 2, a.B, rows, int64_t(N) * 2};
       }
     }
-    if (int64_t(p.m_tiles[g]) * cols > 2147483647) {
+    if (int64_t(p.m_tiles[g]) * p.nt[g] > 2147483647) {
       set_error("%s: seg %d: too many rows", who, g);
       return RA_EINVAL;
     }
-    tiles += int64_t(a.B) * p.m_tiles[g] * cols;
+    tiles += int64_t(a.B) * p.m_tiles[g] * p.nt[g];
   }
   if (overlapping(out, n_out, in, n_in) >= 0) {
     set_error("%s: an output overlaps an input or another output", who);
@@ -1039,24 +1083,25 @@ ra_status run(const char* who, const ra_gemm4_args& a, cudaStream_t st) {
     single += a.seg[g].lin.rows == 1;
     more += a.seg[g].lin.rows > 1;
   }
-  if (a.B == 1 && more == 0 && !qkv && a.tile_mode == 0 && a.K <= MAX_ROW_K && single * a.N <= int64_t(sms) * 64)
+  if (!then && a.B == 1 && more == 0 && !qkv && a.tile_mode == 0 && a.K <= MAX_ROW_K && single * a.N <= int64_t(sms) * 64)
     return run_row(who, a, st);
-  for (int g = 0; g < a.n_seg; ++g) {
-    const ra_gemm4_seg& q = a.seg[g];
+  for (int g = 0; g < p.n_seg; ++g) {
+    const ra_gemm4_seg& q = seg_of(g);
     const ra_gemm_seg& s = q.lin;
     if (s.rows == 0) continue;
     // Two bytes of codes as one element: a box of 64 is 128 bytes, 256 columns.
     ra_seg as{const_cast<void*>(s.a), s.a_stride_s / 2, 0, s.a_stride_r / 2, s.rows, 0};
-    ra_seg ws{const_cast<void*>(s.w), 0, 0, a.K / 4, a.N, 0};
-    if (!encode_seg(&p.tm_a[g], as, a.B, 1, a.K / 4, CHUNK / 4, BM, true) ||
-        !encode_seg(&p.tm_w[g], ws, 1, 1, a.K / 4, CHUNK / 4, pair ? plan.bn / 2 : plan.bn, true) ||
-        !encode_scales(&p.tm_sa[g], q.a_scales, a.K, s.rows, a.B, a.format, p.groups, 1) ||
-        !encode_scales(&p.tm_sw[g], q.w_scales, a.K, a.N, 1, a.format, p.groups, p.w_tiles))
+    ra_seg ws{const_cast<void*>(s.w), 0, 0, p.k[g] / 4, p.n[g], 0};
+    if (!encode_seg(&p.tm_a[g], as, a.B, 1, p.k[g] / 4, CHUNK / 4, BM, true) ||
+        !encode_seg(&p.tm_w[g], ws, 1, 1, p.k[g] / 4, CHUNK / 4, pair ? plan.bn / 2 : plan.bn, true) ||
+        !encode_scales(&p.tm_sa[g], q.a_scales, p.k[g], s.rows, a.B, a.format, p.groups, 1) ||
+        !encode_scales(&p.tm_sw[g], q.w_scales, p.k[g], p.n[g], 1, a.format, p.groups, p.w_tiles))
       return RA_EINVAL;
   }
   const Kernels kn = p.e8m0 ? pick<true>(a.epilogue, a.d) : pick<false>(a.epilogue, a.d);
   const int64_t slots = pair ? (sms / 2 > 0 ? sms / 2 : 1) : sms;
-  note_launch(pair ? "CTA pairs, %d columns" : "single CTAs, %d columns", plan.bn);
+  note_launch(pair ? (then ? "two products, CTA pairs, %d columns" : "CTA pairs, %d columns")
+                   : (then ? "two products, single CTAs, %d columns" : "single CTAs, %d columns"), plan.bn);
   const auto smem = [&](int stages) {
     return pair ? (qkv ? Layout<true, true>::smem(stages) : Layout<true, false>::smem(stages))
                 : (qkv ? Layout<false, true>::smem(stages) : Layout<false, false>::smem(stages));
@@ -1064,6 +1109,17 @@ ra_status run(const char* who, const ra_gemm4_args& a, cudaStream_t st) {
   const int64_t groups = tiles < slots ? tiles : slots;
   return launch(who, p, pair ? kn.pair : kn.single, smem(p.stages), pair ? 2 * groups : groups, pair ? 2 : 1, st, THREADS4,
                 smem(pair ? MAX_STAGES : FEW_STAGES));
+}
+
+// Two products of one segment each in one launch, if that takes less than one after the other (the second
+// one's first loads come while the first one ends).
+ra_status run_two(const char* who, const ra_gemm4_args& a, const ra_gemm4_args& b, cudaStream_t st) {
+  const int sms = num_sms();
+  const ra_gemm4_args &first = a.K >= b.K ? a : b, &then = a.K >= b.K ? b : a;
+  if (make_plan(first, &then, sms).us < make_plan(a, nullptr, sms).us + make_plan(b, nullptr, sms).us - 2)
+    return run(who, first, st, &then);
+  const ra_status r = run(who, a, st);
+  return r != RA_OK ? r : run(who, b, st);
 }
 
 }  // namespace gemm4

@@ -602,7 +602,7 @@ extern "C" ra_status refadapt_linear4_backward(const ra_linear4_grad_args* a, vo
     d->scales = ws + pl.dy.scales;
     d->c_sr = a->N / 2;
   }
-  ra_status r = launch_tokens(who, p, RA_Q4_E8M0, st);
+  const ra_status r = launch_tokens(who, p, RA_Q4_E8M0, st);
   if (r != RA_OK) return r;
   auto product = [&](const linear4::Matrix& am, const linear4::Matrix& wm, int64_t rows, int32_t N, int32_t K) {
     ra_gemm4_args g;
@@ -623,18 +623,16 @@ extern "C" ra_status refadapt_linear4_backward(const ra_linear4_grad_args* a, vo
     s.w_scales = ws + wm.scales;
     return g;
   };
+  ra_gemm4_args dw, dx;
   if (a->dw) {
-    ra_gemm4_args g = product(pl.dyt, pl.xt, a->N, a->K, int32_t(pl.tokens));
-    g.seg[0].lin.out = a->dw;
-    g.seg[0].lin.out_stride_r = a->K;
-    r = gemm4::run(who, g, st);
-    if (r != RA_OK) return r;
+    dw = product(pl.dyt, pl.xt, a->N, a->K, int32_t(pl.tokens));
+    dw.seg[0].lin.out = a->dw;
+    dw.seg[0].lin.out_stride_r = a->K;
   }
   if (a->dx) {
-    ra_gemm4_args g = product(pl.dy, pl.wt, n, a->K, a->N);
-    g.seg[0].lin.out = a->dx;
-    g.seg[0].lin.out_stride_r = n == 1 ? a->K : (a->B == 1 ? a->dx_stride_r : dx_sr);
-    r = gemm4::run(who, g, st);
+    dx = product(pl.dy, pl.wt, n, a->K, a->N);
+    dx.seg[0].lin.out = a->dx;
+    dx.seg[0].lin.out_stride_r = n == 1 ? a->K : (a->B == 1 ? a->dx_stride_r : dx_sr);
   }
-  return r;
+  return a->dw && a->dx ? gemm4::run_two(who, dw, dx, st) : gemm4::run(who, a->dw ? dw : dx, st);
 }

@@ -477,6 +477,21 @@ def test_gradients(cuda_ok, B, rows, K, N, wanted):
         within(dw, ref, BF * np.abs(ref) + (B * rows + 64) * 2.0 ** -23 * (np.abs(p) @ np.abs(q).T) + 1e-30)
 
 
+@pytest.mark.parametrize("B, rows, K, N", [(1, 130, 1024, 1024), (2, 1209, 2048, 8192), (1, 5000, 1024, 4096), (1, 300, 4096, 64),
+                                           (1, 7000, 64, 192), (3, 700, 3008, 2048)])
+def test_gradients_together_are_those_alone(cuda_ok, B, rows, K, N):
+    """Both products of a call share a launch, whose CTAs take unlike numbers of their tiles."""
+    a, g = api(), torch.Generator().manual_seed(rows)
+    dy, x, w = bf((B, rows, N), g, 0.01), bf((B, rows, K), g), bf((N, K), g, K ** -0.5)
+    ws = a.linear4_backward_workspace(B, rows, K, N)
+    both = torch.full_like(x, 7.0), torch.full_like(w, 7.0)
+    a.refadapt_linear4_backward(dy, x, w, ws, dx=both[0], dw=both[1])
+    dx, dw = torch.empty_like(x), torch.empty_like(w)
+    a.refadapt_linear4_backward(dy, x, w, ws, dx=dx)
+    a.refadapt_linear4_backward(dy, x, w, ws, dw=dw)
+    assert torch.equal(both[0], dx) and torch.equal(both[1], dw)
+
+
 def test_gradients_without_rows(cuda_ok):
     a = api()
     e = lambda *s: torch.empty(s, dtype=torch.bfloat16, device="cuda")  # noqa: E731
