@@ -925,8 +925,8 @@ ra_status refadapt_adamw(const ra_adamw_args* args, void* stream);
 const char* refadapt_status_string(ra_status s);
 const char* refadapt_last_error(void);
 
-/* Diagnostic: how this thread's last refadapt_joint_attn, refadapt_gemm or
- * refadapt_ln_modulate was launched, e.g. "clusters of 2" (text for people and
+/* Diagnostic: how this thread's last refadapt_joint_attn, refadapt_gemm,
+ * refadapt_gemm4 or refadapt_ln_modulate was launched, e.g. "clusters of 2" (text for people and
  * tests, valid until the thread's next call of this function). */
 const char* refadapt_last_launch(void);
 

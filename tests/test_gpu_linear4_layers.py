@@ -279,6 +279,42 @@ def test_a_wait_that_runs_out(cuda_ok, tile_mode, epilogue):
         assert torch.equal(o, v)
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("tile_mode", [1, 2])
+def test_a_wait_that_runs_out_before_other_tiles(cuda_ok, tile_mode, d):
+    """The same with several tiles to a CTA, whose epilogue warps take turns and, for heads of 128, meet: those
+    that did not give up wait for no one."""
+    from paper_2609_32415_gb300._lib import RA_ETIMEOUT, RefAdaptError
+    a, n, K, N = api(), 128 * 70, 65536, 768
+    g = torch.Generator(device="cuda").manual_seed(d)
+    codes, w = (torch.randint(0, 256, s, dtype=torch.uint8, device="cuda", generator=g) for s in ((1, n, K // 2), (N, K // 2)))
+    scales = [torch.full((a.refadapt_quant4_scales_size(r, K, 1),), 120, dtype=torch.uint8, device="cuda") for r in (n, N)]
+    outs = [torch.empty((1, N // 3 // d, n, d), dtype=torch.bfloat16, device="cuda") for _ in range(3)]
+    seg = {"a": codes, "a_scales": scales[0], "w": w, "w_scales": scales[1], "q": outs[0], "k": outs[1], "v": outs[2],
+           "q_norm": torch.ones(d, device="cuda"), "k_norm": torch.ones(d, device="cuda")}
+    err, rope = torch.zeros(1, dtype=torch.int32, device="cuda"), a.rope_table(n, d)
+
+    def call():
+        a.refadapt_gemm4([seg], N, K, 3, 1, err_word=err, tile_mode=tile_mode, rope=rope, H=N // 3 // d, d=d)
+
+    call()
+    a.refadapt_check_error(err)
+    want = [o.clone() for o in outs]
+    a.refadapt_set_wait_budget_ns(1)
+    try:
+        for _ in range(3):
+            call()
+            with pytest.raises(RefAdaptError) as e:
+                a.refadapt_check_error(err)
+            assert e.value.status == RA_ETIMEOUT
+    finally:
+        a.refadapt_set_wait_budget_ns(500_000_000)
+    call()
+    a.refadapt_check_error(err)
+    for o, v in zip(outs, want):
+        assert torch.equal(o, v)
+
+
 # ------------------------------------------------------------------ the optimiser
 @pytest.mark.parametrize("bits", [32, 8])
 def test_adamw_class(cuda_ok, bits):
