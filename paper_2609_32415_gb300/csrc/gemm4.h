@@ -16,10 +16,11 @@ namespace gemm4 {
 // as one tile of 64 columns to an SM covers the weights' rows; K up to MAX_ROW_K. The arguments are checked.
 constexpr int MAX_ROW_K = 32768;
 ra_status run_row(const char* who, const ra_gemm4_args& a, cudaStream_t st);
-// The checks, and the launch. `who` names the entry point in errors. `then`: a second product of one segment in the
-// launch (B = 1, STORE, same format, K no longer than a's); outputs and inputs of both are checked together.
-ra_status run(const char* who, const ra_gemm4_args& a, cudaStream_t st, const ra_gemm4_args* then = nullptr);
-ra_status run_two(const char* who, const ra_gemm4_args& a, const ra_gemm4_args& b, cudaStream_t st);
+// The checks, and the launch. `who` names the entry point in errors. made: the weights' codes come from the launch
+// before (asking for them early is no use then). `then`: a second product of one segment in the launch (B = 1,
+// STORE, same format, K no longer than a's); outputs and inputs of both are checked together.
+ra_status run(const char* who, const ra_gemm4_args& a, cudaStream_t st, bool made, const ra_gemm4_args* then = nullptr);
+ra_status run_two(const char* who, const ra_gemm4_args& a, const ra_gemm4_args& b, cudaStream_t st, bool made);
 }  // namespace gemm4
 
 }  // namespace ra

@@ -77,24 +77,34 @@ __device__ __forceinline__ float scale_of(uint32_t byte, int e8m0) {
 // lanes two apart are permuted, so that a warp's reads have no conflicts.
 __device__ __forceinline__ int piece_at(int chunk, int q) { return chunk * 4 + (q ^ ((chunk >> 1) & 3)); }
 
+__device__ __forceinline__ void prefetch_l2(const void* ptr) { asm volatile("prefetch.global.L2 [%0];" ::"l"(ptr)); }
+
 __global__ void __launch_bounds__(THREADS) row_kernel(const __grid_constant__ RowParams p) {
   extern __shared__ __align__(16) uint8_t smem[];
   __shared__ float sums[WARPS * N_ROWS];
   uint4* av = reinterpret_cast<uint4*>(smem);              // K / 8 pieces of 8 fp16
   float* as = reinterpret_cast<float*>(smem + p.K * 2);    // the scales of 16 of K
-  pdl_wait();
-  pdl_launch();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   int g = 0;
   while (g + 1 < p.n_seg && int(blockIdx.x) >= p.seg[g + 1].first) ++g;
   const RowSeg& sg = p.seg[g];
-  if (sg.gated && *p.mode == RA_MODE_REUSE) return;
   const int units = WARPS / p.share;
   const int unit = (int(blockIdx.x) - sg.first) * units + warp / p.share, part = warp % p.share;
   const int tile = unit >> 4, i2 = 2 * (unit & 15);  // weight rows 128 tile + 32 q + i2 + i
   const int block = p.e8m0 ? 32 : 16;
   const int64_t groups = (p.K + 4 * block - 1) / (4 * block);
   const bool mine = tile * 128 < p.N;
+  // What the warp reads of the weights goes to L2 while the kernel before this one runs: with the row's
+  // quantisation 7.3 us, 6.5 (2048 -> 8192). (If that one writes them, it writes to L2 as well.)
+  for (int step = part; mine && step * STEP < p.K; step += p.share) {
+    const int n = tile * 128 + 32 * (lane >> 3) + i2 + ((lane >> 2) & 1), k = step * STEP + 256 * (lane & 3);
+    if (n < p.N && k < p.K) prefetch_l2(sg.w + int64_t(n) * (p.K / 2) + k / 2);
+    const int ks = step * STEP + 4 * block * lane;
+    if (ks < min(p.K, (step + 1) * STEP)) prefetch_l2(sg.w_scales + (tile * groups + ks / (4 * block)) * 512 + 16 * i2);
+  }
+  pdl_wait();
+  pdl_launch();
+  if (sg.gated && *p.mode == RA_MODE_REUSE) return;
   // the first step's weights are on their way while A is unpacked
   uint4 c[N_ROWS], s[2];
   auto fetch = [&](int step) {

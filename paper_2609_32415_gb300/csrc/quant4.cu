@@ -634,5 +634,5 @@ extern "C" ra_status refadapt_linear4_backward(const ra_linear4_grad_args* a, vo
     dx.seg[0].lin.out = a->dx;
     dx.seg[0].lin.out_stride_r = n == 1 ? a->K : (a->B == 1 ? a->dx_stride_r : dx_sr);
   }
-  return a->dw && a->dx ? gemm4::run_two(who, dw, dx, st) : gemm4::run(who, a->dw ? dw : dx, st);
+  return a->dw && a->dx ? gemm4::run_two(who, dw, dx, st, true) : gemm4::run(who, a->dw ? dw : dx, st, true);
 }
