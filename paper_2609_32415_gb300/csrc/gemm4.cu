@@ -758,9 +758,12 @@ __global__ void __launch_bounds__(THREADS4, 1) gemm4_kernel(const __grid_constan
           tc_fence_after();
           Ring next = in;
           next.next(p);
-          filled = peek(full + next.st, next.ph);
+          // the next stage's answer: single CTAs ask before this one is issued (8.0 us, 8.5 after it; 256 rows, K =
+          // 8192, N = 2048), pairs, whose stage takes longer, after it (5120 rows: 29.0 us, 30.3 before it)
+          if (!PAIR) filled = peek(full + next.st, next.ph);
           issue_stage<L, E8M0>(p, s0 + uint32_t(in.st * (L::STAGE_BYTES / 16)), sf0 + sf.col, sw0 + sf.col,
                                tmem + uint32_t(buf * p.bn), idesc, min(CHUNK / 64, steps - kb * (CHUNK / 64)), kb == 0, smem_u32(empty + in.st));
+          if (PAIR) filled = peek(full + next.st, next.ph);
           issued = true;
           in = next;
           sf.next(p);
