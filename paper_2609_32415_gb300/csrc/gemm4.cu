@@ -14,10 +14,10 @@
 //   * TMEM holds two accumulators of 192 columns or three of up to 128, and two to six stages' scales.
 //     Tiles of 256 columns would leave either the scales or the second accumulator no room, and
 //     an epilogue takes as long as the MMAs of K = 1536.
-// What bounds it: a stage of a pair's 256 x 192 tile takes 212 ns (e8m0; e4m3, whose scales have two buffers,
-// 249), its MMAs alone 198 (9.7 PFLOP/s), its loads less; a stage of 128 columns 200 (single CTAs 185), of
+// What bounds it: a stage of a pair's 256 x 192 tile takes 212 to 217 ns (e8m0; e4m3, whose scales have two
+// buffers, 240), its MMAs alone 198 (9.7 PFLOP/s), its loads less; a stage of 128 columns 200 (single CTAs 185), of
 // which 190 are the issuing warp's waits, copies and commit. Long calls reach the power cap: 8192 rows, K =
-// 16384, N = 7296 take 260 us with e8m0 (7.5 PFLOP/s, 3.9 times the bf16 rate), 274 with e4m3. Unrolling
+// 16384, N = 7296 take 254 to 263 us with e8m0 (7.5 to 7.7 PFLOP/s, four times the bf16 rate), 264 with e4m3. Unrolling
 // the issuer by two stages, its tiles from the producer, and two producers each measured even or slower.
 #include <cuda.h>
 #include <cuda_bf16.h>
@@ -762,7 +762,8 @@ __global__ void __launch_bounds__(THREADS4, 1) gemm4_kernel(const __grid_constan
           // 8192, N = 2048), pairs, whose stage takes longer, after it (5120 rows: 29.0 us, 30.3 before it)
           if (!PAIR) filled = peek(full + next.st, next.ph);
           issue_stage<L, E8M0>(p, s0 + uint32_t(in.st * (L::STAGE_BYTES / 16)), sf0 + sf.col, sw0 + sf.col,
-                               tmem + uint32_t(buf * p.bn), idesc, min(CHUNK / 64, steps - kb * (CHUNK / 64)), kb == 0, smem_u32(empty + in.st));
+                               tmem + uint32_t(buf * p.bn), idesc, min(CHUNK / 64, steps - kb * (CHUNK / 64)), kb == 0,
+                               smem_u32(empty + in.st));
           if (PAIR) filled = peek(full + next.st, next.ph);
           issued = true;
           in = next;
@@ -1062,7 +1063,7 @@ ra_status run(const char* who, const ra_gemm4_args& a, cudaStream_t st, bool mad
     };
     const int e = q.a_exponent + q.w_exponent;
     p.seg[g].alpha = ldexpf(1.f, e);
-    const int64_t rows = s.rows, spans = (rows + 127) / 128 * ((K + 4 * block_of(a.format) - 1) / (4 * block_of(a.format)));
+    const int64_t rows = s.rows, group = 4 * block_of(a.format), spans = (rows + 127) / 128 * ((K + group - 1) / group);
     in[n_in++] = RowSpan{s.a, s.a_stride_s, s.a_stride_r, a.B, rows, K / 2};
     in[n_in++] = RowSpan{q.a_scales, spans * 512, 0, a.B, 1, spans * 512};
     in[n_in++] = RowSpan{s.w, 0, K / 2, 1, N, K / 2};
