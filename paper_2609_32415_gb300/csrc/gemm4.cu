@@ -469,6 +469,7 @@ __device__ __forceinline__ bool epilogue_linear4(const Params4& p, const Tile& t
       else load32<false>(res + 64 * j + 32 * i, r[j][i]);
     }
   };
+  __syncwarp();  // all lanes, those without a row too, have read the vectors of the warp's tile before
   if (on) {
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
@@ -558,6 +559,7 @@ __device__ __forceinline__ bool epilogue_qkv4(const Params4& p, const Tile& tl, 
 #pragma unroll
     for (int hf = 0; hf < 2; ++hf) rows_fetch(rope + 64 * (2 * j + hf), 4 * D, w.nrow, cs[hf]);
   };
+  __syncwarp();  // as in epilogue_linear4
   if (on) {
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
