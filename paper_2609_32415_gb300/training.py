@@ -251,6 +251,8 @@ class AdamW:
         api.refadapt_grad_norm([t["g"] for t in tensors], self.max_norm, self.norm, self._workspace)
         api.refadapt_adamw(tensors, self.lr, self.count, beta1=self.betas[0], beta2=self.betas[1], eps=self.eps,
                            weight_decay=self.weight_decay, grad_scale=self.norm[1:], seed=self.seed)
+        # written behind torch's back: a graph that saved one of them must not use it any more
+        torch.autograd.graph.increment_version([t["w"] if "w" in t else t["p"] for t in tensors])
 
     def state_dict(self):
         """The moments, the fp32 copies and the step's number (the tensors themselves)."""
