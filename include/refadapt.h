@@ -870,8 +870,8 @@ ra_status refadapt_grad_norm(const ra_grad* tensors, int32_t n_tensors, float ma
  *   m  = beta1 m + (1 - beta1) g'
  *   v  = beta2 v + (1 - beta2) g'^2
  *   p  = p - lr decay p - lr (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps)
- * in fp32, p in place, its rounding to bf16 in w. Where c is not finite the call
- * changes nothing.
+ * in fp32, p in place, its rounding to bf16 in w (a |g'| beyond 1.8e19, whose square passes
+ * fp32's end, makes v infinite). Where c is not finite the call changes nothing.
  *  bits = 32  m and v are fp32.
  *  bits = 8   m and v are e4m3 in blocks of 32 elements, with a power of two (e8m0
  *             byte, 2^(byte - 127)) for each in m_scale and v_scale: the smallest one

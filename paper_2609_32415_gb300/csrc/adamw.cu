@@ -231,12 +231,28 @@ __device__ __forceinline__ void update(const StepRates& h, const Rates& r, float
     const float gc = __fmul_rn(g[i], r.c);
     m[i] = __fadd_rn(__fmul_rn(b1, m[i]), __fmul_rn(h.rest1, gc));
     v[i] = __fadd_rn(__fmul_rn(b2, v[i]), __fmul_rn(h.rest2, __fmul_rn(gc, gc)));
-    // lr m / (1 - beta1^t) / (sqrt(v) / sqrt(1 - beta2^t) + eps); the root of 2^24 v, which is no
-    // denormal number, so that the short form of the root will do
-    float root, move;
-    asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(root) : "f"(v[i] * 16777216.f));
-    asm("div.approx.ftz.f32 %0, %1, %2;" : "=f"(move) : "f"(r.lr1 * m[i]), "f"(fmaf(root, r.root2, h.eps)));
-    p[i] = fmaf(-r.decay, p[i], p[i]) - move;
+  }
+  // lr m / (1 - beta1^t) / (sqrt(v) / sqrt(1 - beta2^t) + eps)
+  auto move = [&](int i, float up, float root2) {
+    float root, q;
+    asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(root) : "f"(v[i] * up));
+    asm("div.approx.ftz.f32 %0, %1, %2;" : "=f"(q) : "f"(r.lr1 * m[i]), "f"(fmaf(root, root2, h.eps)));
+    p[i] = fmaf(-r.decay, p[i], p[i]) - q;
+  };
+  // The root of 2^24 v, which is no denormal number, so that the short form of the root will do; of v itself
+  // where that could pass fp32's end (gradients beyond 10^16).
+  float top = fmaxf(v[0], v[1]);
+#pragma unroll
+  for (int i = 2; i < 8; i += 2) top = fmaxf(top, fmaxf(v[i], v[i + 1]));
+  if (top < 0x1p100f) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) move(i, 16777216.f, r.root2);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const bool big = v[i] >= 0x1p100f;
+      move(i, big ? 1.f : 16777216.f, big ? r.root2 * 4096.f : r.root2);
+    }
   }
 }
 

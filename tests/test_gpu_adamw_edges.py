@@ -1,0 +1,42 @@
+"""The optimiser's step and the norm over whole chunks of elements (the loads of several are on their way at once there),
+and at the ends of fp32's range. Bounds as in test_gpu_adamw."""
+import numpy as np
+import pytest
+import torch
+
+from test_gpu_adamw import HYPER, api, check_step, check_step8, cloned, d64, small, tensor
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("grad", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("n", [40, 8192 + 64])
+@pytest.mark.parametrize("top", [1e15, 1.5e17, 1e18, 1.8e19])
+def test_large_gradients_move_the_weights(cuda_ok, bits, grad, n, top):
+    """Squares up to the end of fp32: the step is lr times a number near one for them, and what it was for the
+    ordinary gradients beside them."""
+    g = torch.Generator().manual_seed(7)
+    t = tensor(n, g, grad)
+    large = torch.arange(0, n, 3, device="cuda")
+    t["g"][large] = (torch.sign(t["g"][large].float()) * top).to(grad)
+    if bits == 8:
+        t = small(t)
+    before = cloned(t)
+    api().refadapt_adamw([t], 1e-3, 12, seed=3, **HYPER)
+    if bits == 8:
+        check_step8(before, t, 1e-3, 12, 3, 0)
+    else:
+        check_step(before, t, 1e-3, 12)
+    assert bool(((t["p"] - before["p"])[large].abs() > 1e-4).all())
+
+
+def test_large_moments_move_the_weights(cuda_ok):
+    """Second moments from 2^100 to the end of fp32, without a gradient."""
+    n = 64
+    v = (2.0 ** torch.linspace(90, 127.9, n, dtype=torch.float64)).float().cuda()
+    t = {"p": torch.ones(n, device="cuda"), "g": torch.zeros(n, device="cuda"), "m": v.sqrt(), "v": v}
+    before = cloned(t)
+    api().refadapt_adamw([t], 1e-2, 2, **HYPER)
+    check_step(before, t, 1e-2, 2)
+    assert bool(((t["p"] - before["p"]).abs() > 1e-5).all())
