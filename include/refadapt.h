@@ -894,7 +894,7 @@ ra_status refadapt_grad_norm(const ra_grad* tensors, int32_t n_tensors, float ma
  *  lr, step   the rate and the number t >= 1 of the step; lr_dev, step_dev: device fp32
  *             and int32, or NULL, which count instead (a captured call then goes on with
  *             what they hold when it is replayed; a step below 1 there counts as 1).
- *  beta1, beta2 in [0, 1), eps > 0, decay >= 0, lr >= 0. */
+ *  beta1, beta2 in [0, 1), eps >= 2^-126 (1.2e-38), decay >= 0, lr >= 0, all finite in fp32. */
 typedef struct {
   void* p;
   const void* g;

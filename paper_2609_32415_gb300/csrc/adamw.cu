@@ -14,6 +14,7 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <cstring>
 #include <new>
@@ -737,10 +738,13 @@ extern "C" ra_status refadapt_adamw(const ra_adamw_args* a, void* stream) {
     set_error("refadapt_adamw: need n_tensors >= 0 with their array, and bits 32 or 8");
     return RA_EINVAL;
   }
-  if (!(a->beta1 >= 0 && a->beta1 < 1 && a->beta2 >= 0 && a->beta2 < 1 && a->eps > 0 && std::isfinite(a->eps) &&
-        a->decay >= 0 && std::isfinite(a->decay) && a->lr >= 0 && std::isfinite(a->lr)) ||
+  // The rates count in fp32: eps as 2^-126 or more there (the quotient takes denormal numbers for zero, and an
+  // element without moments would be 0 / 0), the others as finite.
+  if (!(a->beta1 >= 0 && a->beta1 < 1 && a->beta2 >= 0 && a->beta2 < 1 && float(a->eps) >= FLT_MIN &&
+        std::isfinite(float(a->eps)) && a->decay >= 0 && std::isfinite(float(a->decay)) && a->lr >= 0 &&
+        std::isfinite(float(a->lr))) ||
       (!a->step_dev && (a->step < 1 || a->step > 2147483647))) {
-    set_error("refadapt_adamw: need betas in [0, 1), eps > 0, lr and decay >= 0, 1 <= step < 2^31");
+    set_error("refadapt_adamw: need betas in [0, 1), eps >= 2^-126, lr and decay >= 0, all finite in fp32, 1 <= step < 2^31");
     return RA_EINVAL;
   }
   const bool small = a->bits == 8;

@@ -40,3 +40,18 @@ def test_large_moments_move_the_weights(cuda_ok):
     api().refadapt_adamw([t], 1e-2, 2, **HYPER)
     check_step(before, t, 1e-2, 2)
     assert bool(((t["p"] - before["p"]).abs() > 1e-5).all())
+
+
+@pytest.mark.parametrize("eps", [1.2e-38, 1e-30])
+def test_smallest_eps_and_tiny_gradients(cuda_ok, eps):
+    """Elements whose moments are zero stay where they are but for the decay; the roots of the smallest second moments
+    are not lost beside such an eps."""
+    n = 256
+    t = {"p": torch.ones(n, device="cuda"), "g": torch.zeros(n, device="cuda"), "m": torch.zeros(n, device="cuda"),
+         "v": torch.zeros(n, device="cuda")}
+    t["v"][128:] = (2.0 ** torch.linspace(-126, -100, 128, dtype=torch.float64)).float().cuda()
+    t["m"][128:] = t["v"][128:].sqrt() * 0.5
+    before = cloned(t)
+    api().refadapt_adamw([t], 1e-3, 4, **{**HYPER, "eps": eps})
+    check_step(before, t, 1e-3, 4, eps=eps)
+    assert bool((t["p"][:128] == t["p"][0]).all()) and abs(float(t["p"][0]) - (1 - 1e-5)) < 1e-6
