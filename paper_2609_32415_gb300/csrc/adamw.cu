@@ -334,16 +334,6 @@ __device__ __forceinline__ float scale_value(uint32_t scale) {
   return scale == 0xffu ? __int_as_float(0x7fffffff)
                         : scale == 0 ? __uint_as_float(0x00400000u) : __uint_as_float(scale << 23);
 }
-__device__ __forceinline__ float max_nan(float a, float b) {
-  float m;
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(a), "f"(b));
-  return m;
-}
-__device__ __forceinline__ float max_nan(float a, float b, float c) {
-  float m;
-  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(m) : "f"(a), "f"(b), "f"(c));
-  return m;
-}
 // Four threads (8 elements each) have a block of 32.
 __device__ __forceinline__ uint32_t scale_of_block(const float (&x)[8]) {
   float top = max_nan(fabsf(x[0]), fabsf(x[1]));

@@ -390,8 +390,10 @@ struct Scales {
 };
 
 // gelu_tanh2 (gemm_body.cuh) with one reciprocal for the two: 1 / d0 = d1 / (d0 d1). The
-// exponents stop at 60, where the result is below 2^-60 of x: the special functions of a tile of
-// 192 columns (two a value) take as long as the MMAs of K = 1536.
+// exponents stop at 60, which x below -7.5 passes; the factor there is 2^-60, and x counts as
+// GELU_END, so that the result is -6.5e-18 down to minus infinity (the formula's is closer to zero; with x itself
+// it grew to minus infinity, and took 1 % less: 29.4 us, 29.6, 3858 rows, 1536 -> 6144). The special functions of a
+// tile of 192 columns (two a value) take as long as the MMAs of K = 1536.
 __device__ __forceinline__ void gelu_tanh2_1(float& x0, float& x1) {
   constexpr float c = -2.f * 0.7978845608028654f * 1.4426950408889634f;
   const uint64_t x = f2_pack(x0, x1);
@@ -400,7 +402,8 @@ __device__ __forceinline__ void gelu_tanh2_1(float& x0, float& x1) {
   float d0, d1;
   f2_unpack(f2_add(f2_pack(ex2_approx(fminf(z0, 60.f)), ex2_approx(fminf(z1, 60.f))), f2_pack(1.f, 1.f)), d0, d1);
   const float r = rcp_approx(d0 * d1);
-  f2_unpack(f2_mul(x, f2_mul(f2_pack(d1, d0), f2_pack(r, r))), x0, x1);
+  const uint64_t y = f2_pack(max_nan(x0, GELU_END), max_nan(x1, GELU_END));
+  f2_unpack(f2_mul(y, f2_mul(f2_pack(d1, d0), f2_pack(r, r))), x0, x1);
 }
 
 // 32 bytes of a row between global memory and a thread's registers, each row a thread's; WIDE: 32-byte

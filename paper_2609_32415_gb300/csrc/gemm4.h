@@ -12,6 +12,9 @@ namespace ra {
 constexpr int block_of(int format) { return format == RA_Q4_E8M0 ? 32 : 16; }
 
 namespace gemm4 {
+// GELU of x below this is taken as at it, 1e-17 or less from zero (NaN stays NaN): the tanh form has infinity times
+// zero at minus infinity.
+constexpr float GELU_END = -7.5f;
 // Calls of one row a segment have a kernel of their own (gemm4_row.cu) where it is the faster one: as long
 // as one tile of 64 columns to an SM covers the weights' rows; K up to MAX_ROW_K. The arguments are checked.
 constexpr int MAX_ROW_K = 32768;

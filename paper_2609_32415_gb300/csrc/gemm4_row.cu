@@ -188,6 +188,7 @@ __global__ void __launch_bounds__(THREADS) row_kernel(const __grid_constant__ Ro
   v = fmaf(v, sg.alpha, sg.bias ? sg.bias[n] : 0.f);
   if (p.epilogue == RA_EPI_GELU) {
     float other = 0.f;
+    v = max_nan(v, GELU_END);
     gemm::gelu_tanh2(v, other);
   } else if (p.epilogue == RA_EPI_RESID) {
     v = fmaf(sg.gate[n], v, __bfloat162float(sg.resid[n]));

@@ -5,9 +5,8 @@ import numpy as np
 import pytest
 import torch
 
-from oracle import lowbit
-from test_gpu_linear4 import (BF, E4M3, E8M0, F32, GELU, QKV, RESID, STORE, api, bf, f64, f64_32, gelu64, operands, quantised,
-                              values_of, within)
+from test_gpu_linear4 import (BF, E4M3, E8M0, F32, GELU, QKV, RESID, STORE, api, bf, f64, f64_32, gelu64, operands, values_of,
+                              within)
 
 pytestmark = pytest.mark.gpu
 
@@ -63,3 +62,32 @@ def test_partial_row_tiles_one_after_another(cuda_ok, fmt, tile_mode, epilogue, 
     a.refadapt_gemm4([seg], N, K, epilogue, fmt, tile_mode=tile_mode, **kw)
     for got, ref, tol in want:
         within(got, ref, tol + 1e-30)
+
+
+@pytest.mark.parametrize("fmt", [E4M3, E8M0])
+@pytest.mark.parametrize("tile_mode, rows", [(0, 1), (1, 2), (2, 2)])
+def test_gelu_at_its_ends(cuda_ok, fmt, tile_mode, rows):
+    """x from the bias, the products being zero: what is far below zero gives nothing, at minus infinity as well, NaN
+    and infinity stay where they are, in the kernel of one row and in the tiles alike. x (1 + e^z)^-1 is below 8 2^-60
+    from -7.5 on, so 2^-56 is allowed there; above, three roundings of an exponent up to 60 are
+    within 2^-16 of the value."""
+    a, K = api(), 128
+    inf = float("inf")
+    x = [-inf, 1.0, -3e38, -1e30, inf, -1e18, float("nan"), -2.0, -1e6, -1000.0, -100.0, -20.0, -10.0, -8.0, -7.6, -7.5, -7.4, -7.0,
+         -6.0, -5.0, -4.0, -3.0, -1.0, -1e-3, 0.0, 1e-30, 1e-3, 0.5, 3.0, 7.0, 20.0, 1e6, 1e18, 3e38, float("nan"), -1e20]
+    x = np.array(x + [-0.25 * i for i in range(64 - len(x))])
+    N = 64
+    seg, _, _ = operands(1, rows, N, K, fmt, torch.Generator().manual_seed(1))
+    seg["a"].zero_()
+    seg["bias"] = torch.tensor(x, dtype=torch.float32, device="cuda")
+    x = seg["bias"].double().cpu().numpy()
+    seg["out"] = torch.zeros((1, rows, N), dtype=torch.bfloat16, device="cuda")
+    a.refadapt_gemm4([seg], N, K, GELU, fmt, tile_mode=tile_mode)
+    with np.errstate(all="ignore"):
+        ref = np.where(x == -inf, 0.0, x / (1 + np.exp(-2 * np.sqrt(2 / np.pi) * (x + 0.044715 * x ** 3))))
+    got = seg["out"].double().cpu().numpy()[0]
+    plain = np.isfinite(x) | (x == -inf)
+    for r in range(rows):
+        assert np.isnan(got[r][np.isnan(x)]).all() and (got[r][x == inf] == inf).all()
+        assert np.isfinite(got[r][plain]).all()
+        assert (np.abs(got[r][plain] - ref[plain]) <= (BF + 2.0 ** -15) * np.abs(ref[plain]) + 2.0 ** -56).all()
