@@ -188,15 +188,19 @@ class _Linear4(torch.autograd.Function):
                   for t, need in zip((x, w), ctx.needs_input_grad))
         if dx is not None or dw is not None:
             ws = api.linear4_backward_workspace(x.shape[0], x.shape[1], x.shape[2], w.shape[0], x.device)
-            api.refadapt_linear4_backward(_rows(dy), x, w, ws, dx=dx, dw=dw, err_word=ctx.err_word)
+            # the product takes weights in rows of any stride, their gradient whole ones
+            api.refadapt_linear4_backward(_rows(dy), x, w.contiguous(), ws, dx=dx, dw=dw, err_word=ctx.err_word)
         return dx, dw, None, None, None, None
 
 
 def linear4(x, w, format=RA_Q4_E8M0, x_exponent=0, w_exponent=0, err_word=None):
     """x w^T through 4-bit products, x [B, rows, K], w [N, K] bf16 (N and K multiples of
-    64): forward in the format given (RA_Q4_E4M3: with the exponents of its scales), the
-    gradients in RA_Q4_E8M0, which has no range to choose. Rounding to 4 bits counts as
-    the identity in the backward pass."""
+    64; rows of a wider buffer are fine): forward in the format given, the gradients in RA_Q4_E8M0,
+    which has no range to choose. RA_Q4_E4M3 has one for x and one for w: scales (a block's
+    largest magnitude / 6) are within 1 / 16 from 2^(exponent - 6) to 448 2^exponent, so that
+    w_exponent 0 suits blocks that reach 0.1 to 2688; None takes api.weight4's, from the weight's
+    largest magnitude (which waits for the GPU). Rounding to 4 bits counts as the identity
+    in the backward pass."""
     return _Linear4.apply(x, w, format, x_exponent, w_exponent, err_word)
 
 

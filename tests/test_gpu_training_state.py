@@ -2,7 +2,7 @@
 import pytest
 import torch
 
-from test_gpu_linear4 import bf
+from test_gpu_linear4 import E4M3, E8M0, bf
 
 pytestmark = pytest.mark.gpu
 
@@ -30,3 +30,37 @@ def test_a_graph_of_older_weights_raises(cuda_ok, bits):
     kept.float().sum().backward()
     assert still.grad is not None
     t.linear4(x, w).float().sum().backward()  # a graph of the new weights
+
+
+@pytest.mark.parametrize("fmt, exps", [(E8M0, (0, 0)), (E4M3, (1, -5))])
+def test_linear4_of_a_weight_in_a_wider_buffer(cuda_ok, fmt, exps):
+    """Rows with a stride of their own, forward and backward: what the same weight gives on its own."""
+    t, g = training(), torch.Generator().manual_seed(2)
+    wide, x, up = bf((64, 256), g, 0.1), bf((2, 40, 128), g), bf((2, 40, 64), g)
+    got = []
+    for w in (wide[:, 64:192], wide[:, 64:192].contiguous()):
+        w, xr = w.detach().requires_grad_(True), x.clone().requires_grad_(True)
+        y = t.linear4(xr, w, fmt, *exps)
+        got.append((y.detach(), *torch.autograd.grad(y, (xr, w), up)))
+    for a, b in zip(*got):
+        assert a.shape == b.shape and torch.equal(a, b)
+
+
+def test_linear4_of_a_weight_in_a_wider_buffer_without_its_own_gradient(cuda_ok):
+    t, g = training(), torch.Generator().manual_seed(3)
+    wide, x, up = bf((64, 256), g, 0.1), bf((1, 40, 128), g), bf((1, 40, 64), g)
+    xr = x.clone().requires_grad_(True)
+    (dx,) = torch.autograd.grad(t.linear4(xr, wide[:, :128]), xr, up)
+    xs = x.clone().requires_grad_(True)
+    (want,) = torch.autograd.grad(t.linear4(xs, wide[:, :128].contiguous()), xs, up)
+    assert torch.equal(dx, want)
+
+
+def test_linear4_takes_the_weights_own_exponent(cuda_ok):
+    """w_exponent None: the one that api.weight4 takes from the weight's largest magnitude."""
+    from paper_2609_32415_gb300 import api
+    t, g = training(), torch.Generator().manual_seed(4)
+    x, w = bf((1, 40, 128), g), bf((64, 128), g, 0.02)
+    exponent = api.weight4(w, E4M3).exponent
+    assert exponent < 0
+    assert torch.equal(t.linear4(x, w, E4M3, 0, None), t.linear4(x, w, E4M3, 0, exponent))
