@@ -782,7 +782,7 @@ ra_status refadapt_quant4(const ra_quant4_args* args, void* stream);
  * 16, a_stride_r >= K / 2); lin.w: codes [N][K / 2]; a_scales, w_scales as above; all
  * 16-byte aligned. N a multiple of 64 (QKV: as for refadapt_gemm), K of 64. The other
  * fields, the epilogues, gates, tile_mode and err_word are refadapt_gemm's. No output
- * may overlap an input (but out may be resid) or another output. Deterministic; the
+ * may overlap an input (but out may be resid), another output or itself. Deterministic; the
  * order of the fp32 sums follows from the sizes of the call. */
 typedef struct {
   ra_gemm_seg lin;

@@ -2,6 +2,7 @@
 // can be checked without a GPU.
 #pragma once
 #include <cstdint>
+#include <initializer_list>
 #include <mutex>
 
 namespace ra {
@@ -79,6 +80,105 @@ inline int overlapping(const RowSpan* out, int n_out, const RowSpan* in, int n_i
       if (surely_overlap(out[i], out[j])) return i;
   }
   return -1;
+}
+
+// Where a tensor lies, exactly: runs of `run` bytes at `at` plus every sum of multiples of the steps (step i taken
+// 0 to n[i] - 1 times; largest step first, positive). run 0: nowhere.
+struct Place {
+  int64_t at, run;
+  int dims;
+  int64_t n[3], step[3];
+  int64_t extent(int from) const {
+    int64_t e = run;
+    for (int i = from; i < dims; ++i) e += (n[i] - 1) * step[i];
+    return e;
+  }
+};
+// Up to three dimensions of n entries, `step` bytes apart.
+struct PlaceDim {
+  int64_t n, step;
+};
+inline Place place_of(const void* ptr, int64_t run, PlaceDim a = {1, 0}, PlaceDim b = {1, 0}, PlaceDim c = {1, 0}) {
+  Place p{int64_t(reinterpret_cast<uintptr_t>(ptr)), ptr && run > 0 ? run : 0, 0, {}, {}};
+  for (PlaceDim d : {a, b, c}) {
+    if (d.n < 1) p.run = 0;
+    if (d.n <= 1 || d.step == 0) continue;
+    if (d.step < 0) {
+      p.at += (d.n - 1) * d.step;
+      d.step = -d.step;
+    }
+    int i = p.dims++;
+    for (; i > 0 && p.step[i - 1] < d.step; --i) p.n[i] = p.n[i - 1], p.step[i] = p.step[i - 1];
+    p.n[i] = d.n;
+    p.step[i] = d.step;
+  }
+  return p;
+}
+// The same bytes by fewer dimensions: runs that touch are one, steps that go on with one another too.
+inline Place merged(Place p) {
+  while (p.dims > 0 && p.step[p.dims - 1] <= p.run) {
+    p.run += (p.n[p.dims - 1] - 1) * p.step[p.dims - 1];
+    --p.dims;
+  }
+  for (int i = p.dims - 2; i >= 0; --i)
+    if (p.step[i] == p.step[i + 1] * p.n[i + 1]) {
+      p.n[i + 1] *= p.n[i];
+      for (int j = i; j + 1 < p.dims; ++j) p.n[j] = p.n[j + 1], p.step[j] = p.step[j + 1];
+      --p.dims;
+    }
+  return p;
+}
+// Do a's dimensions from i on, at `shift` bytes from b's from j on, share a byte with those? Only what can meet is looked at:
+// parts of one buffer (equal steps) in a few steps whatever their sizes, others row by row. `left`: steps until
+// it is given up, with no for an answer.
+inline bool parts_meet(const Place& a, int i, int64_t shift, const Place& b, int j, int* left) {
+  if (--*left < 0) return false;
+  if (shift >= b.extent(j) || -shift >= a.extent(i)) return false;
+  const int64_t sa = i < a.dims ? a.step[i] : 0, sb = j < b.dims ? b.step[j] : 0;
+  if (sa == 0 && sb == 0) return true;
+  // the smallest and largest k with shift + k step in (-e, f)
+  auto from = [](int64_t shift, int64_t e, int64_t step) {
+    const int64_t x = -e - shift + 1;
+    return x >= 0 ? (x + step - 1) / step : -(-x / step);
+  };
+  auto to = [](int64_t shift, int64_t f, int64_t step) {
+    const int64_t x = f - shift - 1;
+    return x >= 0 ? x / step : -((-x + step - 1) / step);
+  };
+  auto least = [](int64_t x, int64_t y) { return x < y ? x : y; };
+  auto most = [](int64_t x, int64_t y) { return x > y ? x : y; };
+  if (sa == sb) {  // entry x of a and y of b: k = x - y
+    const int64_t e = a.extent(i + 1), f = b.extent(j + 1);
+    const int64_t end = least(to(shift, f, sa), a.n[i] - 1);
+    for (int64_t k = most(from(shift, e, sa), 1 - b.n[j]); k <= end && *left >= 0; ++k)
+      if (parts_meet(a, i + 1, shift + k * sa, b, j + 1, left)) return true;
+  } else if (sa > sb) {
+    const int64_t end = least(to(shift, b.extent(j), sa), a.n[i] - 1);
+    for (int64_t k = most(from(shift, a.extent(i + 1), sa), 0); k <= end && *left >= 0; ++k)
+      if (parts_meet(a, i + 1, shift + k * sa, b, j, left)) return true;
+  } else {
+    const int64_t end = least(to(-shift, a.extent(i), sb), b.n[j] - 1);
+    for (int64_t k = most(from(-shift, b.extent(j + 1), sb), 0); k <= end && *left >= 0; ++k)
+      if (parts_meet(a, i, shift - k * sb, b, j + 1, left)) return true;
+  }
+  return false;
+}
+constexpr int PLACE_STEPS = 1 << 16;
+// Do two tensors share memory? (merged ones)
+inline bool meet(const Place& a, const Place& b) {
+  if (a.run == 0 || b.run == 0) return false;
+  int left = PLACE_STEPS;
+  return parts_meet(a, 0, a.at - b.at, b, 0, &left);
+}
+// Does a tensor have a byte twice? (as place_of gives it)
+inline bool meets_itself(const Place& p) {
+  int left = PLACE_STEPS;
+  for (int i = 0; i < p.dims && p.run > 0; ++i) {
+    const int64_t inner = p.extent(i + 1);
+    for (int64_t k = 1; k < p.n[i] && k * p.step[i] < inner && left >= 0; ++k)
+      if (parts_meet(p, i + 1, k * p.step[i], p, i + 1, &left)) return true;
+  }
+  return false;
 }
 
 }  // namespace ra

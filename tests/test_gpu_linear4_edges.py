@@ -91,3 +91,34 @@ def test_gelu_at_its_ends(cuda_ok, fmt, tile_mode, rows):
         assert np.isnan(got[r][np.isnan(x)]).all() and (got[r][x == inf] == inf).all()
         assert np.isfinite(got[r][plain]).all()
         assert (np.abs(got[r][plain] - ref[plain]) <= (BF + 2.0 ** -15) * np.abs(ref[plain]) + 2.0 ** -56).all()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_qkv_side_by_side(cuda_ok, d):
+    """q, k and v as parts of one buffer of rows, and in slots of a longer cache: what separate tensors hold, and
+    nothing beside them is touched."""
+    a, g = api(), torch.Generator().manual_seed(d)
+    B, rows, K, H = 2, 70, 128, 512 // d
+    N = 3 * H * d
+    norm = torch.linspace(0.5, 1.5, d, device="cuda")
+    seg, _, _ = operands(B, rows, N, K, E8M0, g)
+
+    def run(q, k, v):
+        a.refadapt_gemm4([{**seg, "q": q, "k": k, "v": v, "q_norm": norm, "k_norm": norm, "pos_offset": 3}], N, K, QKV, E8M0,
+                         rope=a.rope_table(rows + 3, d), H=H, d=d)
+        return q, k, v
+
+    def empty(*s):
+        return torch.full(s, 7.0, dtype=torch.bfloat16, device="cuda")
+
+    want = run(*(empty(B, H, rows, d) for _ in range(3)))
+    whole = empty(B, rows + 1, 3, H, d)
+    side = run(*(whole[:, :rows, i].transpose(1, 2) for i in range(3)))
+    cache = empty(B, 2, H, rows + 40, d)
+    slots = run(empty(B, H, rows, d), cache[:, 0, :, 11:11 + rows], cache[:, 1, :, 11:11 + rows])
+    two = empty(B, H, 2 * rows, d)  # q and k take turns along the rows of one tensor
+    turns = run(two[:, :, ::2], two[:, :, 1::2], empty(B, H, rows, d))
+    for got in (side, slots, turns):
+        assert all(torch.equal(x, y) for x, y in zip(got, want))
+    assert bool((whole[:, rows] == 7.0).all())
+    assert bool((cache[:, :, :, :11] == 7.0).all()) and bool((cache[:, :, :, 11 + rows:] == 7.0).all())
