@@ -207,10 +207,11 @@ def linear4(x, w, format=RA_Q4_E8M0, x_exponent=0, w_exponent=0, err_word=None):
 class AdamW:
     """AdamW over a list of parameters (contiguous, fp32 or bf16; bf16 ones get an fp32
     copy that the steps add up in), with clipping to max_norm. bits: 32 or 8, of the
-    moments. capturable: the rate and the step's number live on the GPU (``lr``, fp32, and
-    ``count``, int32), so that a captured step goes on when it is replayed. A step whose
-    gradients' norm is not finite changes no parameter. ``norm`` holds the last step's
-    gradient norm and clipping factor (on the GPU)."""
+    moments. capturable: the rate lives on the GPU too (``lr``, fp32), so that a captured
+    step goes on when it is replayed. A step whose gradients' norm (refadapt_grad_norm's) is
+    not finite changes no parameter and does not count. ``count`` is the number of the steps that did:
+    an int32 tensor with capturable, else an int (reading it waits for the GPU). ``norm`` holds the last
+    step's gradient norm and clipping factor (on the GPU)."""
 
     def __init__(self, params, lr, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, bits=32, max_norm=math.inf, seed=0,
                  capturable=False):
@@ -227,11 +228,20 @@ class AdamW:
         self.betas, self.eps, self.weight_decay, self.max_norm, self.seed = betas, eps, weight_decay, max_norm, seed
         self.bits, self.capturable = bits, capturable
         self.lr = torch.tensor([lr], dtype=torch.float32, device=dev) if capturable else lr
-        self.count = torch.zeros(1, dtype=torch.int32, device=dev) if capturable else 0
+        self._count = torch.zeros(1, dtype=torch.int32, device=dev)
         self.state = [dict(api.adamw_moments(p, bits), **({} if p.dtype == torch.float32 else {"p": p.detach().float()}))
                       for p in self.params]
         self.norm = torch.zeros(2, dtype=torch.float32, device=dev)
+        self._factor = self.norm[1:]
         self._workspace = api.grad_norm_workspace(dev)
+
+    @property
+    def count(self):
+        return self._count if self.capturable else int(self._count)
+
+    @count.setter
+    def count(self, value):
+        self._count.copy_(torch.as_tensor(value, dtype=torch.int32).reshape(1))
 
     def zero_grad(self, set_to_none=True):
         for p in self.params:
@@ -248,13 +258,16 @@ class AdamW:
                 continue
             g = p.grad.contiguous()
             tensors.append({"p": p, "g": g, **state} if p.dtype == torch.float32 else {"g": g, "w": p, **state})
-        if self.capturable:
-            self.count.add_(1)
-        else:
-            self.count += 1
         api.refadapt_grad_norm([t["g"] for t in tensors], self.max_norm, self.norm, self._workspace)
-        api.refadapt_adamw(tensors, self.lr, self.count, beta1=self.betas[0], beta2=self.betas[1], eps=self.eps,
-                           weight_decay=self.weight_decay, grad_scale=self.norm[1:], seed=self.seed)
+        # the factor is NaN where the norm is not finite, which is known on the GPU only
+        taken = self._factor >= 0
+        self._count.add_(taken)
+        try:
+            api.refadapt_adamw(tensors, self.lr, self._count, beta1=self.betas[0], beta2=self.betas[1], eps=self.eps,
+                               weight_decay=self.weight_decay, grad_scale=self._factor, seed=self.seed)
+        except Exception:  # refused: nothing has changed
+            self._count.sub_(taken.int())
+            raise
         # written behind torch's back: a graph that saved one of them must not use it any more
         torch.autograd.graph.increment_version([t["w"] if "w" in t else t["p"] for t in tensors])
 
@@ -272,7 +285,4 @@ class AdamW:
         for mine, theirs in zip(self.state, saved["state"]):
             for k, v in mine.items():
                 v.view(torch.uint8).copy_(theirs[k].view(torch.uint8)) if v.element_size() == 1 else v.copy_(theirs[k])
-        if self.capturable:
-            self.count.copy_(torch.as_tensor(saved["count"], dtype=torch.int32).reshape(1))
-        else:
-            self.count = int(saved["count"])
+        self.count = saved["count"]

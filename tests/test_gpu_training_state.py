@@ -64,3 +64,72 @@ def test_linear4_takes_the_weights_own_exponent(cuda_ok):
     exponent = api.weight4(w, E4M3).exponent
     assert exponent < 0
     assert torch.equal(t.linear4(x, w, E4M3, 0, None), t.linear4(x, w, E4M3, 0, exponent))
+
+
+@pytest.mark.parametrize("capturable", [False, True])
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("bad_at", [0, 2])
+def test_skipped_steps_do_not_count(cuda_ok, capturable, bits, bad_at):
+    """A step whose gradients are not finite changes nothing: the steps behind it are those of a run without it."""
+    t, g = training(), torch.Generator().manual_seed(5)
+    start = [torch.randn(300, generator=g).cuda(), bf((20, 10), g)]
+    grads = [[torch.randn(p.shape, generator=g).to(p.dtype).cuda() for p in start] for _ in range(4)]
+    runs = []
+    for skip in (False, True):
+        params = [torch.nn.Parameter(p.clone()) for p in start]
+        opt = t.AdamW(params, 1e-2, bits=bits, max_norm=1.0, seed=9, capturable=capturable)
+        for k, step in enumerate(grads):
+            if skip and k == bad_at:
+                params[0].grad, params[1].grad = step[0].clone(), step[1].clone()
+                params[0].grad[7] = float("nan")
+                was = [p.detach().clone() for p in params]
+                opt.step()
+                assert all(torch.equal(p.detach(), q) for p, q in zip(params, was))
+            for p, v in zip(params, step):
+                p.grad = v.clone()
+            opt.step()
+        assert int(opt.count) == len(grads)
+        runs.append((params, opt.state_dict()))
+    for p, q in zip(runs[0][0], runs[1][0]):
+        assert torch.equal(p.detach(), q.detach())
+    assert int(runs[0][1]["count"]) == int(runs[1][1]["count"])
+
+
+def test_a_captured_step_that_is_skipped_does_not_count(cuda_ok):
+    t, g = training(), torch.Generator().manual_seed(6)
+    start, grad = torch.randn(100, generator=g).cuda(), torch.randn(100, generator=g).cuda()
+    p, q = (torch.nn.Parameter(start.clone()) for _ in range(2))
+    one, two = (t.AdamW([z], 1e-2, max_norm=1.0, capturable=True) for z in (p, q))
+    p.grad, q.grad = grad.clone(), grad.clone()
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(graph, stream=side):
+        one.step()
+    for bad in (True, False, True, False):
+        p.grad.copy_(grad)
+        if bad:
+            p.grad[3] = float("inf")
+        graph.replay()
+    torch.cuda.synchronize()
+    two.step()
+    two.step()
+    assert int(one.count) == 2 and torch.equal(p.detach(), q.detach())
+
+
+@pytest.mark.parametrize("capturable", [False, True])
+def test_refused_steps_do_not_count(cuda_ok, capturable):
+    """Parameters that share memory: the call is refused, and count and weights stay; count can be set."""
+    from paper_2609_32415_gb300 import RefAdaptError
+    t = training()
+    base = torch.arange(150.0, device="cuda")
+    params = [torch.nn.Parameter(base[:100]), torch.nn.Parameter(base[50:])]
+    opt = t.AdamW(params, 1e-2, capturable=capturable)
+    opt.count = 5
+    for p in params:
+        p.grad = torch.ones_like(p)
+    with pytest.raises(RefAdaptError, match="overlaps"):
+        opt.step()
+    assert int(opt.count) == 5 and torch.equal(base, torch.arange(150.0, device="cuda"))
+    other = t.AdamW(params[:1], 1e-2, capturable=not capturable)
+    other.load_state_dict({**other.state_dict(), "count": opt.count})
+    assert int(other.count) == 5
