@@ -778,12 +778,13 @@ ra_status refadapt_quant4(const ra_quant4_args* args, void* stream);
 
 /* refadapt_gemm4 — refadapt_gemm with 4-bit operands of one format:
  *   out = epilogue(2^(a_exponent + w_exponent) A W^T + bias)
- * with exact products and fp32 sums. lin.a: codes, its strides in bytes (multiples of
- * 16, a_stride_r >= K / 2); lin.w: codes [N][K / 2]; a_scales, w_scales as above; all
- * 16-byte aligned. N a multiple of 64 (QKV: as for refadapt_gemm), K of 64. The other
- * fields, the epilogues, gates, tile_mode and err_word are refadapt_gemm's. No output
- * may overlap an input (but out may be resid), another output or itself. Deterministic; the
- * order of the fp32 sums follows from the sizes of the call. */
+ * with exact products and fp32 sums (a_exponent + w_exponent up to 127). lin.a: codes, its
+ * strides in bytes (multiples of 16, a_stride_r >= K / 2); lin.w: codes [N][K / 2];
+ * a_scales, w_scales as above; all 16-byte aligned. N a multiple of 64 (QKV: as for
+ * refadapt_gemm), K of 64. The other fields, the epilogues, gates, tile_mode and err_word
+ * are refadapt_gemm's. No output may overlap an input (but out may be resid), another
+ * output or itself. Deterministic; the order of the fp32 sums follows from the sizes of
+ * the call. */
 typedef struct {
   ra_gemm_seg lin;
   const void* a_scales;

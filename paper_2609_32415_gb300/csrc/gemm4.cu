@@ -1068,10 +1068,11 @@ ra_status run(const char* who, const ra_gemm4_args& a, cudaStream_t st, bool mad
                 "a_stride_r >= K / 2", who, g);
       return RA_EINVAL;
     }
+    // 2^128 is no fp32 number: the sums would count infinitely, zeros as NaN
     if (q.a_exponent < -64 || q.a_exponent > 64 || q.w_exponent < -64 || q.w_exponent > 64 ||
-        (p.e8m0 && (q.a_exponent || q.w_exponent))) {
-      set_error("%s: seg %d: exponents need -64 to 64, and 0 for RA_Q4_E8M0 (%d, %d)", who, g, q.a_exponent,
-                q.w_exponent);
+        q.a_exponent + q.w_exponent > 127 || (p.e8m0 && (q.a_exponent || q.w_exponent))) {
+      set_error("%s: seg %d: exponents need -64 to 64, together at most 127, and 0 for RA_Q4_E8M0 (%d, %d)", who, g,
+                q.a_exponent, q.w_exponent);
       return RA_EINVAL;
     }
     if (!fill_epilogue(who, call_of(g), g, s, p.seg[g])) return RA_EINVAL;

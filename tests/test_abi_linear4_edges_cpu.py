@@ -55,3 +55,9 @@ def test_gemm4_refuses_outputs_that_meet_other_tensors_anywhere(lib):  # noqa: F
     a = gemm()
     a.B, a.seg[0].lin.out_stride_s = 2, 768 * 39
     refused(lib, call(a), b"itself")
+
+
+def test_gemm4_refuses_exponents_that_pass_fp32_together(lib):  # noqa: F811
+    a = gemm()
+    a.seg[0].a_exponent = a.seg[0].w_exponent = 64
+    refused(lib, lib.refadapt_gemm4(ctypes.byref(a), None), b"together at most 127")

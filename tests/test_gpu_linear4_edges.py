@@ -93,6 +93,26 @@ def test_gelu_at_its_ends(cuda_ok, fmt, tile_mode, rows):
         assert (np.abs(got[r][plain] - ref[plain]) <= (BF + 2.0 ** -15) * np.abs(ref[plain]) + 2.0 ** -56).all()
 
 
+@pytest.mark.parametrize("tile_mode, rows", [(0, 1), (0, 40), (2, 300)])
+@pytest.mark.parametrize("exps", [(64, 63), (63, 64), (-64, -63), (-64, -64), (64, -64)])
+def test_exponents_at_their_ends(cuda_ok, tile_mode, rows, exps):
+    """2^127 and 2^-128 are numbers; half a step of bf16's smallest ones is 2^-134 (and fp32's 2^-150)."""
+    a, N, K = api(), 128, 192
+    g = torch.Generator().manual_seed(rows)
+    seg, _, _ = operands(1, rows, N, K, E4M3, g, 0, -6)
+    seg.update(a_exponent=exps[0], w_exponent=exps[1])
+    if sum(exps) > 100:  # scales of 2^-9 on both sides: values of one over K times 2^127 at most
+        seg["a_scales"].clamp_(max=1)
+        seg["w_scales"].clamp_(max=1)
+    p = values_of(seg["a"][0], seg["a_scales"][0], E4M3, exps[0])
+    q = values_of(seg["w"], seg["w_scales"], E4M3, exps[1])
+    ref = p @ q.T
+    assert np.abs(ref).max() < 2.0 ** 126
+    seg["out"] = torch.zeros((1, rows, N), dtype=torch.bfloat16, device="cuda")
+    a.refadapt_gemm4([seg], N, K, STORE, E4M3, tile_mode=tile_mode)
+    within(seg["out"][0], ref, BF * np.abs(ref) + K * 2.0 ** -23 * (np.abs(p) @ np.abs(q).T) + 2.0 ** -133.9)
+
+
 @pytest.mark.parametrize("d", [64, 128])
 def test_qkv_side_by_side(cuda_ok, d):
     """q, k and v as parts of one buffer of rows, and in slots of a longer cache: what separate tensors hold, and
