@@ -677,7 +677,7 @@ ra_status refadapt_glu(const ra_glu_args* args, void* stream);
  *                      bytes (on the device that is current), 16-byte aligned;
  *                      calls that share it must be stream-ordered.
  * C, F, O multiples of 8, at least 64; pointers and strides as for refadapt_glu;
- * neither outputs nor the workspace may overlap inputs or one another. Rows of
+ * neither outputs nor the workspace may overlap inputs, one another or themselves. Rows of
  * zero: the weights' gradients are zero. Deterministic. */
 typedef struct {
   int32_t B, rows, C, F, O, act;
@@ -751,8 +751,8 @@ size_t refadapt_quant4_scales_size(int32_t rows, int32_t K, int32_t format);
  *              a multiple of 8.
  *  scales_t    as of one matrix of C rows, contiguous, 16-byte aligned.
  *  exponent    -64 to 64; 0 for RA_Q4_E8M0.
- * codes and scales go together, codes_t and scales_t too; no output may overlap x or
- * another output. A segment with gated = 1 is skipped for samples whose mode is
+ * codes and scales go together, codes_t and scales_t too; no output may overlap an input,
+ * another output or itself. A segment with gated = 1 is skipped for samples whose mode is
  * RA_MODE_REUSE (not with codes_t). B * rows of a segment below 2^30. */
 typedef struct {
   const void* x;
@@ -817,7 +817,7 @@ ra_status refadapt_gemm4(const ra_gemm4_args* args, void* stream);
  *  workspace    device scratch of refadapt_linear4_backward_workspace_size() bytes,
  *               16-byte aligned; calls that share it must be stream-ordered.
  * N and K multiples of 64; pointers 16-byte aligned, strides multiples of 8 elements;
- * neither outputs nor the workspace may overlap inputs or one another. Rows of zero:
+ * neither outputs nor the workspace may overlap inputs, one another or themselves. Rows of zero:
  * dw is zero. B * rows below 2^30. Deterministic. */
 typedef struct {
   int32_t B, rows, K, N;

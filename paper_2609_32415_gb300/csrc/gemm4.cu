@@ -1027,17 +1027,10 @@ ra_status run(const char* who, const ra_gemm4_args& a, cudaStream_t st, bool mad
   p.cols = (a.N + plan.bn - 1) / plan.bn;
   p.cols_q = p.C / plan.bn;
   int64_t tiles = 0;
-  Place out[9], in[30];
-  int n_out = 0, n_in = 0;
-  bool twice = false;  // an output's byte is another tensor's too, or its own twice
-  const auto reads = [&](const Place& t) { in[n_in++] = merged(t); };
-  const auto writes = [&](const Place& t) {
-    twice |= meets_itself(t);
-    out[n_out++] = merged(t);
-  };
-  if (a.mode) reads(place_of(a.mode, int64_t(a.B) * 4));
-  if (a.epilogue == RA_EPI_QKV) reads(place_of(a.rope, int64_t(a.rope_len) * a.d * 4));
-  if (a.err_word) reads(place_of(a.err_word, 4));
+  CallPlaces<9, 24> places;  // read: three of the call, seven of a segment
+  if (a.mode) places.reads(place_of(a.mode, int64_t(a.B) * 4));
+  if (a.epilogue == RA_EPI_QKV) places.reads(place_of(a.rope, int64_t(a.rope_len) * a.d * 4));
+  if (a.err_word) places.reads(place_of(a.err_word, 4));
   // Segment g: a's, behind them the second product's.
   const auto call_of = [&](int g) -> const ra_gemm4_args& { return g < a.n_seg ? a : *then; };
   const auto seg_of = [&](int g) -> const ra_gemm4_seg& { return g < a.n_seg ? a.seg[g] : then->seg[0]; };
@@ -1082,17 +1075,17 @@ ra_status run(const char* who, const ra_gemm4_args& a, cudaStream_t st, bool mad
     const int e = q.a_exponent + q.w_exponent;
     p.seg[g].alpha = ldexpf(1.f, e);
     const int64_t rows = s.rows, group = 4 * block_of(a.format), spans = (rows + 127) / 128 * ((K + group - 1) / group);
-    reads(place_of(s.a, K / 2, {a.B, s.a_stride_s}, {rows, s.a_stride_r}));
-    reads(place_of(q.a_scales, spans * 512 * a.B));
-    reads(place_of(s.w, int64_t(N) * (K / 2)));
-    reads(place_of(q.w_scales, int64_t(refadapt_quant4_scales_size(N, K, a.format))));
-    if (s.bias) reads(place_of(s.bias, int64_t(N) * 4));
+    places.reads(place_of(s.a, K / 2, {a.B, s.a_stride_s}, {rows, s.a_stride_r}));
+    places.reads(place_of(q.a_scales, spans * 512 * a.B));
+    places.reads(place_of(s.w, int64_t(N) * (K / 2)));
+    places.reads(place_of(q.w_scales, int64_t(refadapt_quant4_scales_size(N, K, a.format))));
+    if (s.bias) places.reads(place_of(s.bias, int64_t(N) * 4));
     if (a.epilogue == RA_EPI_QKV) {
-      reads(place_of(s.q_norm, int64_t(a.d) * 4));
-      reads(place_of(s.k_norm, int64_t(a.d) * 4));
+      places.reads(place_of(s.q_norm, int64_t(a.d) * 4));
+      places.reads(place_of(s.k_norm, int64_t(a.d) * 4));
       p.wide[g] = 1;
       for (const ra_seg* o : {&s.q_out, &s.k_out, &s.v_out}) {
-        writes(place_of(o->ptr, int64_t(a.d) * 2, {a.B, o->stride_b * 2}, {a.H, o->stride_h * 2}, {rows, o->stride_n * 2}));
+        places.writes(place_of(o->ptr, int64_t(a.d) * 2, {a.B, o->stride_b * 2}, {a.H, o->stride_h * 2}, {rows, o->stride_n * 2}));
         if ((a.B > 1 && o->stride_b < 1) || (a.H > 1 && o->stride_h < 1) || (rows > 1 && o->stride_n < a.d)) {
           set_error("%s: seg %d: strides of q_out, k_out and v_out must be positive, their rows' at least d", who, g);
           return RA_EINVAL;
@@ -1104,13 +1097,13 @@ ra_status run(const char* who, const ra_gemm4_args& a, cudaStream_t st, bool mad
         set_error("%s: seg %d: out_stride_s must be positive", who, g);
         return RA_EINVAL;
       }
-      writes(place_of(s.out, int64_t(N) * 2, {a.B, s.out_stride_s * 2}, {rows, s.out_stride_r * 2}));
+      places.writes(place_of(s.out, int64_t(N) * 2, {a.B, s.out_stride_s * 2}, {rows, s.out_stride_r * 2}));
       p.wide[g] = on32(s.out, s.out_stride_s, s.out_stride_r) &&
                   (a.epilogue != RA_EPI_RESID || on32(s.resid, s.resid_stride_s, s.resid_stride_r));
       if (a.epilogue == RA_EPI_RESID) {
-        reads(place_of(s.gate, int64_t(N) * 4, {a.B, s.gate_stride_s * 4}));
+        places.reads(place_of(s.gate, int64_t(N) * 4, {a.B, s.gate_stride_s * 4}));
         if (s.resid != s.out || s.resid_stride_s != s.out_stride_s || s.resid_stride_r != s.out_stride_r)
-          reads(place_of(s.resid, int64_t(N) * 2, {a.B, s.resid_stride_s * 2}, {rows, s.resid_stride_r * 2}));
+          places.reads(place_of(s.resid, int64_t(N) * 2, {a.B, s.resid_stride_s * 2}, {rows, s.resid_stride_r * 2}));
       }
     }
     if (int64_t(p.m_tiles[g]) * p.nt[g] > 2147483647) {
@@ -1119,11 +1112,7 @@ ra_status run(const char* who, const ra_gemm4_args& a, cudaStream_t st, bool mad
     }
     tiles += int64_t(a.B) * p.m_tiles[g] * p.nt[g];
   }
-  for (int i = 0; i < n_out; ++i) {
-    for (int j = 0; j < n_in && !twice; ++j) twice = meet(out[i], in[j]);
-    for (int j = 0; j < i && !twice; ++j) twice = meet(out[i], out[j]);
-  }
-  if (twice) {
+  if (places.clash()) {
     set_error("%s: an output overlaps an input, another output or itself", who);
     return RA_EINVAL;
   }

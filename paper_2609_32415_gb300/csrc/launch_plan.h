@@ -180,5 +180,28 @@ inline bool meets_itself(const Place& p) {
   }
   return false;
 }
+// The tensors of a call. clash(): an output's byte is another tensor's too, or its own twice.
+template <int OUT, int IN>
+class CallPlaces {
+ public:
+  void reads(const Place& t) { in_[n_in_++] = merged(t); }
+  void writes(const Place& t) {
+    twice_ = twice_ || meets_itself(t);
+    out_[n_out_++] = merged(t);
+  }
+  bool clash() const {
+    bool yes = twice_;
+    for (int i = 0; i < n_out_; ++i) {
+      for (int j = 0; j < n_in_ && !yes; ++j) yes = meet(out_[i], in_[j]);
+      for (int j = 0; j < i && !yes; ++j) yes = meet(out_[i], out_[j]);
+    }
+    return yes;
+  }
+
+ private:
+  Place out_[OUT], in_[IN];
+  int n_out_ = 0, n_in_ = 0;
+  bool twice_ = false;
+};
 
 }  // namespace ra

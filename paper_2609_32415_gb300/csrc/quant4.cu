@@ -364,8 +364,8 @@ extern "C" ra_status refadapt_quant4(const ra_quant4_args* a, void* stream) {
   rows.mode = a->mode;
   tokens = rows;
   int64_t ctas = 0;
-  RowSpan out[12], in[3];
-  int n_out = 0, n_in = 0;
+  CallPlaces<12, 4> places;
+  if (a->mode) places.reads(place_of(a->mode, int64_t(a->B) * 4));
   for (int g = 0; g < a->n_seg; ++g) {
     const ra_quant4_seg& s = a->seg[g];
     if (s.rows < 0 || int64_t(a->B) * s.rows >= (int64_t(1) << 30)) {
@@ -403,9 +403,8 @@ extern "C" ra_status refadapt_quant4(const ra_quant4_args* a, void* stream) {
                   "multiples of 16 bytes, codes_stride_r >= C / 2", g);
         return RA_EINVAL;
       }
-      const int64_t bytes = int64_t(refadapt_quant4_scales_size(s.rows, a->C, a->format));
-      out[n_out++] = RowSpan{s.codes, s.codes_stride_s, s.codes_stride_r, a->B, s.rows, a->C / 2};
-      out[n_out++] = RowSpan{s.scales, bytes, 0, a->B, 1, bytes};
+      places.writes(place_of(s.codes, a->C / 2, {a->B, s.codes_stride_s}, {s.rows, s.codes_stride_r}));
+      places.writes(place_of(s.scales, a->B * int64_t(refadapt_quant4_scales_size(s.rows, a->C, a->format))));
     }
     if (s.codes_t) {
       if (!aligned16(s.codes_t) || !aligned16(s.scales_t) || s.codes_t_stride % 16 != 0 ||
@@ -414,11 +413,10 @@ extern "C" ra_status refadapt_quant4(const ra_quant4_args* a, void* stream) {
                   "16 bytes and holds all rows", g);
         return RA_EINVAL;
       }
-      out[n_out++] = RowSpan{s.codes_t, 0, s.codes_t_stride, 1, a->C, padded / 2};
-      out[n_out++] =
-          RowSpan{s.scales_t, 0, 0, 1, 1, int64_t(refadapt_quant4_scales_size(a->C, int32_t(padded), a->format))};
+      places.writes(place_of(s.codes_t, padded / 2, {a->C, s.codes_t_stride}));
+      places.writes(place_of(s.scales_t, int64_t(refadapt_quant4_scales_size(a->C, int32_t(padded), a->format))));
     }
-    in[n_in++] = RowSpan{s.x, s.x_stride_s * 2, s.x_stride_r * 2, a->B, s.rows, int64_t(a->C) * 2};
+    places.reads(place_of(s.x, int64_t(a->C) * 2, {a->B, s.x_stride_s * 2}, {s.rows, s.x_stride_r * 2}));
     Seg d;
     std::memset(&d, 0, sizeof(d));
     d.x = static_cast<const char*>(s.x);
@@ -449,8 +447,8 @@ extern "C" ra_status refadapt_quant4(const ra_quant4_args* a, void* stream) {
       tokens.seg[tokens.n_seg++] = d;
     }
   }
-  if (overlapping(out, n_out, in, n_in) >= 0) {
-    set_error("refadapt_quant4: an output overlaps an input or another output");
+  if (places.clash()) {
+    set_error("refadapt_quant4: an output overlaps an input, another output or itself");
     return RA_EINVAL;
   }
   if (ctas > 2147483647) {
@@ -563,15 +561,15 @@ extern "C" ra_status refadapt_linear4_backward(const ra_linear4_grad_args* a, vo
               a->workspace_bytes);
     return RA_EINVAL;
   }
-  RowSpan out[3], in[3];
-  int n_out = 0, n_in = 0;
-  out[n_out++] = RowSpan{a->workspace, 0, 0, 1, 1, int64_t(pl.bytes)};
-  if (a->dx) out[n_out++] = RowSpan{a->dx, a->dx_stride_s * 2, a->dx_stride_r * 2, a->B, a->rows, int64_t(a->K) * 2};
-  if (a->dw) out[n_out++] = RowSpan{a->dw, 0, int64_t(a->K) * 2, 1, a->N, int64_t(a->K) * 2};
-  in[n_in++] = RowSpan{a->dy, a->dy_stride_s * 2, a->dy_stride_r * 2, a->B, a->rows, int64_t(a->N) * 2};
-  if (a->dw) in[n_in++] = RowSpan{a->x, a->x_stride_s * 2, a->x_stride_r * 2, a->B, a->rows, int64_t(a->K) * 2};
-  if (a->dx) in[n_in++] = RowSpan{a->w, 0, int64_t(a->K) * 2, 1, a->N, int64_t(a->K) * 2};
-  if (overlapping(out, n_out, in, n_in) >= 0) {
+  CallPlaces<3, 4> places;
+  places.writes(place_of(a->workspace, int64_t(pl.bytes)));
+  if (a->dx) places.writes(place_of(a->dx, int64_t(a->K) * 2, {a->B, a->dx_stride_s * 2}, {a->rows, a->dx_stride_r * 2}));
+  if (a->dw) places.writes(place_of(a->dw, int64_t(a->N) * a->K * 2));
+  places.reads(place_of(a->dy, int64_t(a->N) * 2, {a->B, a->dy_stride_s * 2}, {a->rows, a->dy_stride_r * 2}));
+  if (a->dw) places.reads(place_of(a->x, int64_t(a->K) * 2, {a->B, a->x_stride_s * 2}, {a->rows, a->x_stride_r * 2}));
+  if (a->dx) places.reads(place_of(a->w, int64_t(a->N) * a->K * 2));
+  if (a->err_word) places.reads(place_of(a->err_word, 4));
+  if (places.clash()) {
     set_error("%s: an output or the workspace overlaps an input or another output", who);
     return RA_EINVAL;
   }

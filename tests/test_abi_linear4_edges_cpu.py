@@ -5,7 +5,7 @@ import ctypes
 import pytest
 
 from test_abi_layers_cpu import refused
-from test_abi_linear4_cpu import gemm, lib  # noqa: F401
+from test_abi_linear4_cpu import gemm, grad, lib, quant  # noqa: F401
 
 
 @pytest.mark.parametrize("field, value", [("eps", 1e-39), ("eps", 1e-46), ("eps", 5e-324), ("eps", -1.0), ("eps", 1e39),
@@ -61,3 +61,27 @@ def test_gemm4_refuses_exponents_that_pass_fp32_together(lib):  # noqa: F811
     a = gemm()
     a.seg[0].a_exponent = a.seg[0].w_exponent = 64
     refused(lib, lib.refadapt_gemm4(ctypes.byref(a), None), b"together at most 127")
+
+
+def test_quant4_and_gradients_refuse_outputs_that_meet_rows_of_wider_buffers(lib):  # noqa: F811
+    call = lambda a: lib.refadapt_quant4(ctypes.byref(a), None)  # noqa: E731
+    for field, value in (("codes", 0x100000 + 512 * 3 + 240), ("scales", 0x100000 + 512 * 39 + 16), ("codes_t", 0x100000 + 512 * 20),
+                         ("scales_t", 0x100000 - 512 + 16)):
+        a = quant(both=True)  # rows of 256 bytes, 512 apart
+        a.seg[0].x_stride_r, a.seg[0].x_stride_s = 256, 256 * 40
+        setattr(a.seg[0], field, value)
+        refused(lib, call(a), b"overlaps")
+    a = quant()  # the second sample begins in the first one's last row
+    a.B, a.seg[0].codes_stride_s = 2, 64 * 40 - 16
+    refused(lib, call(a), b"itself")
+    a = quant()
+    a.seg[0].gated, a.mode = 1, 0x200000 + 64 * 39
+    refused(lib, call(a), b"overlaps")
+
+    call = lambda a: lib.refadapt_linear4_backward(ctypes.byref(a), None)  # noqa: E731
+    for field, value in (("dx", 0x100000 + 512 * 30 + 128), ("dw", 0x100000 + 512 * 39 + 368), ("workspace", 0x100000 + 512 * 39),
+                         ("err_word", 0x500000 + 128 * 192 * 2 - 4)):
+        a = grad()  # dy: rows of 384 bytes, 512 apart
+        a.dy_stride_r, a.dy_stride_s = 256, 256 * 20
+        setattr(a, field, value)
+        refused(lib, call(a), b"overlaps")
