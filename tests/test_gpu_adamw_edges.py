@@ -9,6 +9,43 @@ from test_gpu_adamw import HYPER, api, check_step, check_step8, cloned, d64, sma
 pytestmark = pytest.mark.gpu
 
 
+@pytest.mark.parametrize("grad", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("n", [8192, 8193, 3 * 8192 + 77, 65536])
+def test_whole_chunks_in_8_bits(cuda_ok, grad, n):
+    t = small(tensor(n, torch.Generator().manual_seed(n), grad))
+    t["w"] = torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    before = cloned(t)
+    api().refadapt_adamw([t], 1e-3, 12, seed=(5 << 33) + n, **HYPER)
+    check_step8(before, t, 1e-3, 12, (5 << 33) + n, 0)
+    assert torch.equal(t["w"], t["p"].bfloat16())
+
+
+@pytest.mark.parametrize("grad", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("n", [8192, 3 * 8192 + 77])
+def test_whole_chunks_behind_another_tensor(cuda_ok, grad, n):
+    """Chunks of the second tensor of a call, whose random numbers go on from the first."""
+    g = torch.Generator().manual_seed(n)
+    ts = [small(tensor(100, g)), small(tensor(n, g, grad))]
+    before = [cloned(t) for t in ts]
+    api().refadapt_adamw(ts, 1e-3, 3, seed=17, **HYPER)
+    for t, b, first in zip(ts, before, (0, 128)):
+        check_step8(b, t, 1e-3, 3, 17, first)
+
+
+@pytest.mark.parametrize("grad", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("sizes", [[8192], [5 * 8192 + 1234], [8192, 3, 2 * 8192 + 9, 8192], [152 * 8 * 8192 + 3 * 8192 + 5]])
+def test_norm_of_whole_chunks(cuda_ok, grad, sizes):
+    """Each type's whole chunks, remainders, and more chunks than CTAs."""
+    a, g = api(), torch.Generator().manual_seed(len(sizes))
+    grads = [torch.randn(n, generator=g).to(grad).cuda() for n in sizes]
+    out, ws = torch.zeros(2, device="cuda"), a.grad_norm_workspace()
+    for _ in range(2):
+        a.refadapt_grad_norm(grads, 0.5, out, ws)
+        want = np.sqrt(sum(float((d64(t) ** 2).sum()) for t in grads))
+        assert abs(float(out[0]) - want) <= 2.0 ** -19 * want
+        assert abs(float(out[1]) - 0.5 / want) <= 2.0 ** -19 * 0.5 / want
+
+
 @pytest.mark.parametrize("bits", [32, 8])
 @pytest.mark.parametrize("grad", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("n", [40, 8192 + 64])

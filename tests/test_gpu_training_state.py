@@ -1,4 +1,4 @@
-"""What training.AdamW and training.linear4 leave behind in torch's graph and in their own state."""
+"""training.AdamW and training.linear4 as torch has them: gradients, graphs of older weights, steps that count."""
 import pytest
 import torch
 
@@ -133,3 +133,27 @@ def test_refused_steps_do_not_count(cuda_ok, capturable):
     other = t.AdamW(params[:1], 1e-2, capturable=not capturable)
     other.load_state_dict({**other.state_dict(), "count": opt.count})
     assert int(other.count) == 5
+
+
+def test_linear4_difference_along_the_gradient(cuda_ok):
+    """Along its own gradient G = up W (and up^T x for the weight) the loss changes by step |G|. 4 bits change that by
+    the operands' errors, together below 0.2 of |G| normwise (test_gpu_linear4_layers derives it), and each of the two
+    losses by at most 0.2 |G| rms(x): beside a step of 64 that is 0.01. The gradient that came back, 0.2 off G at most, along the same
+    step likewise. A gradient of zero or of the wrong sign is 1 or 2 off."""
+    t4, g = training().linear4, torch.Generator().manual_seed(33)
+    x, w, up = (torch.randn(s, generator=g).mul(k).to(torch.bfloat16).cuda()
+                for s, k in (((1, 256, 256), 1.0), ((256, 256), 0.06), ((1, 256, 256), 1.0)))
+    xr, wr = x.clone().requires_grad_(True), w.clone().requires_grad_(True)
+    (t4(xr, wr) * up).float().sum().backward()
+
+    def loss(x, w):
+        return float((t4(x.to(torch.bfloat16), w.to(torch.bfloat16)).double() * up.double()).sum())
+
+    for i, (t, got, G) in enumerate(((x, xr.grad, up.double() @ w.double()), (w, wr.grad, up[0].double().T @ x[0].double()))):
+        size = float(G.norm())
+        length = 64.0 if i == 0 else 64.0 * 0.06
+        step = G / size * length
+        a, b = ((t.double() + s * step) for s in (0.5, -0.5))
+        moved = loss(a, w) - loss(b, w) if i == 0 else loss(x, a) - loss(x, b)
+        assert abs(moved - length * size) < 0.22 * length * size
+        assert abs(float((got.double() * step).sum()) - length * size) < 0.2 * length * size
