@@ -854,7 +854,9 @@ typedef enum { RA_F32 = 0, RA_BF16 = 1 } ra_type;
  *  out        device fp32 [2].
  *  workspace  device scratch of refadapt_grad_norm_workspace_size() bytes, 16-byte
  *             aligned, zero-filled once before its first use; every call leaves it ready
- *             for the next. Calls that share it must be stream-ordered. */
+ *             for the next. Calls that share it must be stream-ordered. Its second 32-bit
+ *             word counts the calls whose norm was finite, the steps that refadapt_adamw
+ *             takes (a step_dev that needs no launch of its own). */
 typedef struct {
   const void* g;
   int64_t n;

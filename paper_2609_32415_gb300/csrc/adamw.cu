@@ -39,7 +39,7 @@ constexpr int MAX_TENSORS = 256, FEW_TENSORS = 32;
 
 // ------------------------------------------------------------------ norm
 constexpr int NORM_CTAS = 2048;  // at most, over all launches of a call
-// Workspace: a ticket, then a partial sum of squares (fp64) per CTA.
+// Workspace: a ticket, the number of finite norms, then a partial sum of squares (fp64) per CTA.
 constexpr size_t NORM_WORKSPACE = 16 + NORM_CTAS * sizeof(double);
 
 struct NormTensor {
@@ -177,7 +177,8 @@ __global__ void __launch_bounds__(THREADS, 8) norm_kernel(const __grid_constant_
     const float norm = sum > 1e-30 && sum < 1e30 ? sqrtf(float(sum)) : float(sqrt(sum));
     p.out[0] = norm;
     p.out[1] = !isfinite(norm) ? __int_as_float(0x7fffffff) : norm > p.max_norm ? p.max_norm / norm : 1.f;
-    *p.ticket = 0;
+    p.ticket[0] = 0;
+    if (isfinite(norm)) ++p.ticket[1];
   }
 }
 

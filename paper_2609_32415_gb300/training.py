@@ -228,12 +228,12 @@ class AdamW:
         self.betas, self.eps, self.weight_decay, self.max_norm, self.seed = betas, eps, weight_decay, max_norm, seed
         self.bits, self.capturable = bits, capturable
         self.lr = torch.tensor([lr], dtype=torch.float32, device=dev) if capturable else lr
-        self._count = torch.zeros(1, dtype=torch.int32, device=dev)
         self.state = [dict(api.adamw_moments(p, bits), **({} if p.dtype == torch.float32 else {"p": p.detach().float()}))
                       for p in self.params]
         self.norm = torch.zeros(2, dtype=torch.float32, device=dev)
         self._factor = self.norm[1:]
         self._workspace = api.grad_norm_workspace(dev)
+        self._count = self._workspace[4:8].view(torch.int32)  # norms that were finite
 
     @property
     def count(self):
@@ -259,14 +259,11 @@ class AdamW:
             g = p.grad.contiguous()
             tensors.append({"p": p, "g": g, **state} if p.dtype == torch.float32 else {"g": g, "w": p, **state})
         api.refadapt_grad_norm([t["g"] for t in tensors], self.max_norm, self.norm, self._workspace)
-        # the factor is NaN where the norm is not finite, which is known on the GPU only
-        taken = self._factor >= 0
-        self._count.add_(taken)
         try:
             api.refadapt_adamw(tensors, self.lr, self._count, beta1=self.betas[0], beta2=self.betas[1], eps=self.eps,
                                weight_decay=self.weight_decay, grad_scale=self._factor, seed=self.seed)
-        except Exception:  # refused: nothing has changed
-            self._count.sub_(taken.int())
+        except Exception:  # refused: nothing has changed (the factor of a norm that is not finite is NaN)
+            self._count.sub_((self._factor >= 0).int())
             raise
         # written behind torch's back: a graph that saved one of them must not use it any more
         torch.autograd.graph.increment_version([t["w"] if "w" in t else t["p"] for t in tensors])

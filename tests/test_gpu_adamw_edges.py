@@ -92,3 +92,28 @@ def test_smallest_eps_and_tiny_gradients(cuda_ok, eps):
     api().refadapt_adamw([t], 1e-3, 4, **{**HYPER, "eps": eps})
     check_step(before, t, 1e-3, 4, eps=eps)
     assert bool((t["p"][:128] == t["p"][0]).all()) and abs(float(t["p"][0]) - (1 - 1e-5)) < 1e-6
+
+
+@pytest.mark.parametrize("tensors", [0, 3, 600])
+def test_workspace_counts_finite_norms(cuda_ok, tensors):
+    """Once a call, whatever its launches; a step reads its number there."""
+    a, g = api(), torch.Generator().manual_seed(2)
+    grads = [torch.randn(50, generator=g).cuda() for _ in range(tensors)]
+    out, ws = torch.zeros(2, device="cuda"), a.grad_norm_workspace()
+    count = ws[4:8].view(torch.int32)
+    t = tensor(100, g)
+    u = cloned(t)
+    for k, bad in enumerate([False, True, False, True, True, False]):
+        if tensors:
+            grads[-1][7] = float("inf") if bad else 1.0
+        a.refadapt_grad_norm(grads, 1.0, out, ws)
+        a.refadapt_adamw([t], 1e-3, count, grad_scale=out[1:], **HYPER)
+    taken = 3 if tensors else 6
+    assert int(count) == taken
+    if tensors:
+        grads[-1][7] = 1.0
+    fresh = a.grad_norm_workspace()
+    for k in range(taken):
+        a.refadapt_grad_norm(grads, 1.0, out, fresh)
+        a.refadapt_adamw([u], 1e-3, k + 1, grad_scale=out[1:], **HYPER)
+    assert all(torch.equal(t[z], u[z]) for z in t)
