@@ -846,9 +846,9 @@ typedef enum { RA_F32 = 0, RA_BF16 = 1 } ra_type;
 /* refadapt_grad_norm — out[0] = sqrt(sum of g^2) over the elements of all tensors,
  * out[1] = min(1, max_norm / out[0]), the factor that clips them to max_norm (out[1]
  * is NaN where the norm is not finite). Squares are formed in fp32 (a gradient beyond
- * 1.8e19 makes the norm infinite, a thousand beyond 5e17 may), summed in fp32 over up
- * to 1024 elements, at most 16 in a row, and in fp64 above that, in a fixed order
- * (deterministic).
+ * 1.8e19 makes the norm infinite, a thousand beyond 5e17 may; below 1.1e-19 they lose bits,
+ * below 2.6e-23 they are zero), summed in fp32 over up to 1024 elements, at most 32 in a
+ * row, and in fp64 above that, in a fixed order (deterministic).
  *  tensors    host array; g device, fp32 or bf16, aligned to its type, n >= 0 elements.
  *  max_norm   > 0 (INFINITY: no clipping).
  *  out        device fp32 [2].

@@ -1,5 +1,7 @@
-// What the GEMM kernels of 16-bit and of 4-bit operands have in common: the order of the
-// tiles, the epilogues, the merge of tiles whose K is shared, and the host's part.
+// Parts of the GEMM kernels. Of 16-bit and of 4-bit operands: the tiles' order (Walk), a segment's epilogue tensors
+// and their checks, bias and scale (add_cols), the launch; the one-row kernel of 4-bit operands: gelu_tanh2. Of 16-bit
+// operands alone: round_tiles and tile_at, the epilogues (epilogue_*), the merge of tiles whose K is shared (4-bit
+// tiles have epilogues of their own, gemm4.cu, and share no K).
 #pragma once
 #include <cuda.h>
 #include <cuda_bf16.h>

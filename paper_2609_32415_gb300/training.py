@@ -206,7 +206,7 @@ def linear4(x, w, format=RA_Q4_E8M0, x_exponent=0, w_exponent=0, err_word=None):
 
 class AdamW:
     """AdamW over a list of parameters (contiguous, fp32 or bf16; bf16 ones get an fp32
-    copy that the steps add up in), with clipping to max_norm. bits: 32 or 8, of the
+    copy, made here, that the steps add up in: load weights first), with clipping to max_norm. bits: 32 or 8, of the
     moments. capturable: the rate lives on the GPU too (``lr``, fp32), so that a captured
     step goes on when it is replayed. A step whose gradients' norm (refadapt_grad_norm's) is
     not finite changes no parameter and does not count. ``count`` is the number of the steps that did:
