@@ -94,8 +94,9 @@ __device__ __forceinline__ float warp_sum(float v) {
 
 // Sums in an order that the sizes and alignments alone decide: a warp's squares of a chunk in fp32 (16 in a row, two
 // of these a thread, 32 threads; 32 in a row where a chunk is not whole or not aligned), its chunks, the CTA's warps
-// and the CTAs in fp64; the CTA that takes the last ticket of the call adds the CTAs' sums up. This GPU adds two fp64 numbers a clock and SM: trees of
-// all threads' in fp64 took 8 us beside the loads (21 M bf16 gradients: 16.7 us, now 8.8; 317 M: 94 us, 6.7 TB/s).
+// and the CTAs in fp64; the CTA that takes the last ticket of the call adds the CTAs' sums up. This GPU adds two fp64
+// numbers a clock and SM: trees of all threads' in fp64 took 8 us beside the loads (21 M bf16 gradients: 16.7 us, now
+// 8.8; 317 M: 94 us, 6.7 TB/s).
 template <int MAX>
 __global__ void __launch_bounds__(THREADS, 8) norm_kernel(const __grid_constant__ NormParams<MAX> p) {
   __shared__ double warps[THREADS / 32];

@@ -1085,7 +1085,8 @@ ra_status run(const char* who, const ra_gemm4_args& a, cudaStream_t st, bool mad
       places.reads(place_of(s.k_norm, int64_t(a.d) * 4));
       p.wide[g] = 1;
       for (const ra_seg* o : {&s.q_out, &s.k_out, &s.v_out}) {
-        places.writes(place_of(o->ptr, int64_t(a.d) * 2, {a.B, o->stride_b * 2}, {a.H, o->stride_h * 2}, {rows, o->stride_n * 2}));
+        places.writes(place_of(o->ptr, int64_t(a.d) * 2, {a.B, o->stride_b * 2}, {a.H, o->stride_h * 2},
+                               {rows, o->stride_n * 2}));
         if ((a.B > 1 && o->stride_b < 1) || (a.H > 1 && o->stride_h < 1) || (rows > 1 && o->stride_n < a.d)) {
           set_error("%s: seg %d: strides of q_out, k_out and v_out must be positive, their rows' at least d", who, g);
           return RA_EINVAL;

@@ -128,9 +128,9 @@ inline Place merged(Place p) {
     }
   return p;
 }
-// Do a's dimensions from i on, at `shift` bytes from b's from j on, share a byte with those? Only what can meet is looked at:
-// parts of one buffer (equal steps) in a few steps whatever their sizes, others row by row. `left`: steps until
-// it is given up, with no for an answer.
+// Do a's dimensions from i on, at `shift` bytes from b's from j on, share a byte with those? Only what can meet is
+// looked at: parts of one buffer (equal steps) in a few steps whatever their sizes, others row by row. `left`: steps
+// until it is given up, with no for an answer.
 inline bool parts_meet(const Place& a, int i, int64_t shift, const Place& b, int j, int* left) {
   if (--*left < 0) return false;
   if (shift >= b.extent(j) || -shift >= a.extent(i)) return false;
